@@ -1,0 +1,173 @@
+// Parameter blocks and launch wrappers of the training operators (include/rps_ops.h).
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "rps_ops.h"
+
+namespace rps_ops {
+
+using bf16 = __nv_bfloat16;
+
+inline int64_t round_up(int64_t a, int64_t b) { return (a + b - 1) / b * b; }
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// ---------------------------------------------------------------------------------------------------- products
+// Token rows are padded to whole tiles, and the vocabulary goes through the loss in whole tiles.
+constexpr int kTokenTile = 256;
+constexpr int kVocabTile = 64;
+
+// An operand of a product: bf16 [worker][plane][rows][row stride].  fp32 values lie in three planes whose sum they are.
+struct Operand {
+    const bf16* base;
+    int64_t worker, plane, row;  // strides
+    int64_t rows, cols;          // what exists; zero outside
+};
+
+enum class Product {
+    kLse,      // A = hidden [m][k], B = weight [n][k]: softmax statistics of each row over a tile of columns
+    kDlogits,  // the same product: dl = g (exp(l - lse) - [v == target]) into planes
+    kDhidden,  // A = dl [m][k], B = weight [k][n]: a sum over pieces of the vocabulary, then scattered to the tokens' rows
+    kDweight   // A = dl or dy [k][m], B = hidden or x [k][n]
+};
+
+struct ProductParams {
+    Operand a, b;
+    int workers, planes;
+    int m, n, k;        // upper bounds where the token count (m, or k in kDweight) is the device's to say
+    const int* count;   // [worker] tokens that take part, or NULL: all
+    // kLse, kDlogits
+    int v0, vocab;          // first row of the vocabulary in this piece; all of it
+    int vocab_tiles;
+    const int* target;      // [worker][tokens_padded]
+    float2* part;           // [worker][tiles of the vocabulary][tokens_padded]: running maximum and sum
+    float* hit;             // [worker][tokens_padded]: the target's logit
+    const float2* info;     // [worker][tokens_padded]: lse, g
+    bf16* dl;               // [worker][plane][tokens_padded][piece]
+    int64_t tokens_padded, piece;
+    // kDhidden
+    float* acc;             // [worker][tokens_padded][n]
+    const int* rows;        // [worker][tokens]: token of each row
+    int64_t tokens;
+    int first, last;        // first and last piece
+    // kDhidden, kDweight
+    void* out;
+    int64_t out_row, out_worker;
+    int out_f32;
+};
+
+cudaError_t launch_product(Product which, const ProductParams& prm, cudaStream_t stream);
+
+// ---------------------------------------------------------------------------------------------------- the loss
+struct LceParams {
+    int n, planes, f32, reduction, backward;
+    int64_t tokens, tokens_padded, vocab, cols, cols_padded, ignore_index;
+    const int64_t* targets;
+    int* rows;        // [n][tokens]: tokens that take part in their order, then the others
+    int* count;       // [n]
+    int* target;      // [n][tokens_padded]: targets of the rows, -1 for one that names no row of weight
+    float2* info;     // [n][tokens_padded] (backward)
+    const float* lse_in;
+    const float* dloss;
+    const void* hidden;
+    int64_t hidden_row, hidden_worker;
+    bf16* packed;     // [n][planes][tokens_padded][cols_padded]
+    void* dhidden;    // backward: the rows of ignored tokens are cleared along the way
+    // forward's end
+    const float2* part;
+    const float* hit;
+    int64_t vocab_tiles;
+    float* loss;
+    float* lse;
+    float* sums;      // [n][blocks of rows]
+    int* done;        // [n]
+};
+
+cudaError_t launch_lce_select(const LceParams& prm, cudaStream_t stream);
+cudaError_t launch_lce_gather(const LceParams& prm, cudaStream_t stream);
+int64_t lce_merge_blocks(int64_t tokens);
+cudaError_t launch_lce_merge(const LceParams& prm, cudaStream_t stream);
+
+// Lays `rows` rows of a matrix of each worker out as planes; rows past `valid` and columns past `cols` become zero.
+struct PlanesParams {
+    const void* src;
+    int f32, n, planes;
+    int64_t rows, valid, cols, src_row, src_worker;
+    bf16* dst;
+    int64_t dst_row, dst_plane, dst_worker;
+};
+cudaError_t launch_planes(const PlanesParams& prm, cudaStream_t stream);
+
+// ---------------------------------------------------------------------------------------------------- 8 bits
+struct PackParams {
+    int f32;
+    int64_t rows, cols, x_row, pitch, groups;
+    const void* x;
+    void* out;
+    int8_t* codes;
+    float* scales;
+    // unpacking into planes: rows of one worker are `tokens`
+    bf16* planes_out;
+    int planes;
+    int64_t tokens, dst_row, dst_plane, dst_worker;
+};
+cudaError_t launch_pack(const PackParams& prm, cudaStream_t stream);
+cudaError_t launch_unpack(const PackParams& prm, cudaStream_t stream);
+cudaError_t launch_unpack_planes(const PackParams& prm, cudaStream_t stream);
+
+// ---------------------------------------------------------------------------------------------------- norm
+struct NormParams {
+    int f32, n, packed;
+    int64_t tokens, cols, gates, rows_per_gate;
+    int64_t post_worker, pre_worker, gate_worker;
+    float scale, eps;
+    const void *x, *f, *h_in, *gate, *post, *pre, *dh, *dy;
+    void *h, *y, *dx, *df, *dgate, *dpost, *dpre;
+    float *r_f, *r_h;
+    int8_t *f_codes, *h_codes;
+    float *f_scales, *h_scales;
+    int64_t pitch, groups;
+    // backward: each worker's tokens are cut over blocks that lie inside one gate group (chunks > 0: `chunks` blocks a group),
+    // or hold whole groups (chunks == 0)
+    int64_t rows_per_block, blocks, chunks;
+    float* partial;  // [n][blocks][3][cols]: dpost, dpre, dgate
+};
+void plan_norm_backward(NormParams* prm);
+cudaError_t launch_norm_forward(const NormParams& prm, cudaStream_t stream);
+cudaError_t launch_norm_backward(const NormParams& prm, cudaStream_t stream);
+
+// ---------------------------------------------------------------------------------------------------- device helpers
+#ifdef __CUDACC__
+template <typename T>
+__device__ __forceinline__ float to_float(T v);
+template <>
+__device__ __forceinline__ float to_float<float>(float v) { return v; }
+template <>
+__device__ __forceinline__ float to_float<bf16>(bf16 v) { return __bfloat162float(v); }
+
+template <typename T>
+__device__ __forceinline__ T from_float(float v);
+template <>
+__device__ __forceinline__ float from_float<float>(float v) { return v; }
+template <>
+__device__ __forceinline__ bf16 from_float<bf16>(float v) { return __float2bfloat16_rn(v); }
+
+// v = p0 + p1 + p2 exactly: each part is the leading 8 bits of what the parts before it leave, cut off rather than rounded
+// so that no part can overflow.  An infinity or a NaN stays in the first part (as such) and the others are zero.
+__device__ __forceinline__ void split_planes(float v, bf16 (&p)[3])
+{
+    const uint32_t bits = __float_as_uint(v);
+    uint32_t top = bits & 0xFFFF0000u;
+    const bool finite = (bits & 0x7F800000u) != 0x7F800000u;
+    if (!finite && (bits & 0x007FFFFFu) != 0) top |= 0x00400000u;  // a NaN whose payload lies in the bits cut off
+    p[0] = __ushort_as_bfloat16((unsigned short)(top >> 16));
+    const float rest = finite ? v - __uint_as_float(top) : 0.0f;
+    const uint32_t mid = __float_as_uint(rest) & 0xFFFF0000u;
+    p[1] = __ushort_as_bfloat16((unsigned short)(mid >> 16));
+    p[2] = __float2bfloat16_rn(rest - __uint_as_float(mid));
+}
+#endif
+
+}  // namespace rps_ops

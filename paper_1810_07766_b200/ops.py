@@ -1,0 +1,476 @@
+"""Training operators next to the RPS step: the gradient of a worker's own step, for all workers in one call.
+
+A thin layer over the C ABI of ``include/rps_ops.h``: argument checks, outputs and workspaces (PyTorch lends the device
+memory and the current stream), nothing else.  Every operator takes its tensors with a leading worker axis (``[n, ...]``) or
+without one (a single worker), in float32 or bfloat16, one type for all tensors of a call.  Parameters may be views
+into the rows of an ``[n][pitch]`` array such as ``RPS.x_dev``: only the innermost axis has to be contiguous.
+
+* ``linear_cross_entropy``: softmax cross entropy of ``hidden @ weight.T`` over a large vocabulary without keeping the logits;
+* ``gated_residual_norm``: norm after a block, gate, residual scale, residual sum, norm before the next block;
+* ``pack_activation`` / ``unpack_activation`` / ``packed_weight_grad``: activations kept in 8 bits, and their use in the
+  backward pass (``gated_residual_norm(..., keep="int8")``, ``linear_8bit``).
+
+The functions named ``*_forward`` and ``*_backward`` are single calls of the library; the names without a suffix are
+differentiable.  There is no CPU fallback: a missing library, a CPU tensor or a failing call raises.
+"""
+from __future__ import annotations
+
+import ctypes
+from typing import NamedTuple, Optional, Tuple
+
+import torch
+
+from . import binding
+from .binding import RPS_BF16, RPS_F32, RPS_OK, RPSError
+
+GROUP = 128               # columns that share a scale in 8-bit activations (RPS_PACK_GROUP)
+MAX_NORM_COLS = 16384     # RPS_MAX_NORM_COLS
+_REDUCTION = {"none": 0, "sum": 1, "mean": 2}
+_DTYPE = {torch.float32: RPS_F32, torch.bfloat16: RPS_BF16}
+
+# every symbol include/rps_ops.h declares
+SYMBOLS = (
+    "rps_lce_workspace", "rps_lce_forward", "rps_lce_backward", "rps_norm_forward", "rps_norm_workspace",
+    "rps_norm_backward", "rps_pack_pitch", "rps_pack", "rps_unpack", "rps_wgrad_workspace", "rps_packed_wgrad",
+    "rps_ops_last_error",
+)
+
+_i32, _i64, _dbl = ctypes.c_int32, ctypes.c_int64, ctypes.c_double
+
+
+class rps_lce_desc(ctypes.Structure):
+    _fields_ = [("dtype", _i32), ("reduction", _i32), ("n", _i32), ("tokens", _i64), ("vocab", _i64), ("cols", _i64),
+                ("ignore_index", _i64), ("hidden_row", _i64), ("hidden_worker", _i64), ("weight_row", _i64),
+                ("weight_worker", _i64), ("dweight_row", _i64), ("dweight_worker", _i64)]
+
+
+class rps_norm_desc(ctypes.Structure):
+    _fields_ = [("dtype", _i32), ("n", _i32), ("tokens", _i64), ("cols", _i64), ("gates", _i64), ("post_worker", _i64),
+                ("pre_worker", _i64), ("gate_worker", _i64), ("scale", _dbl), ("eps", _dbl)]
+
+
+class rps_wgrad_desc(ctypes.Structure):
+    _fields_ = [("dtype", _i32), ("n", _i32), ("tokens", _i64), ("outs", _i64), ("cols", _i64), ("dy_row", _i64),
+                ("dy_worker", _i64), ("dweight_row", _i64), ("dweight_worker", _i64)]
+
+
+_lib = None
+
+
+def _library() -> ctypes.CDLL:
+    global _lib
+    if _lib is None:
+        lib = binding.load_library()
+        vp, cint, size = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t
+        lce, norm, wgrad = (ctypes.POINTER(t) for t in (rps_lce_desc, rps_norm_desc, rps_wgrad_desc))
+        sizep = ctypes.POINTER(size)
+        sig = {
+            "rps_lce_workspace": (cint, [lce, vp, cint, sizep]),
+            "rps_lce_forward": (cint, [lce] + [vp] * 6 + [size, vp]),
+            "rps_lce_backward": (cint, [lce] + [vp] * 8 + [size, vp]),
+            "rps_norm_forward": (cint, [norm] + [vp] * 14),
+            "rps_norm_workspace": (cint, [norm, sizep]),
+            "rps_norm_backward": (cint, [norm] + [vp] * 17 + [size, vp]),
+            "rps_pack_pitch": (_i64, [_i64]),
+            "rps_pack": (cint, [cint, _i64, _i64, vp, _i64, vp, vp, vp]),
+            "rps_unpack": (cint, [cint, _i64, _i64, vp, vp, vp, _i64, vp]),
+            "rps_wgrad_workspace": (cint, [wgrad, vp, sizep]),
+            "rps_packed_wgrad": (cint, [wgrad] + [vp] * 5 + [size, vp]),
+            "rps_ops_last_error": (ctypes.c_char_p, []),
+        }
+        for name, (res, args) in sig.items():
+            fn = getattr(lib, name)
+            fn.restype, fn.argtypes = res, args
+        _lib = lib
+    return _lib
+
+
+def _call(name: str, device: torch.device, *args) -> None:
+    """One call of the library with the tensors' device current."""
+    lib = _library()
+    if torch.cuda.current_device() == device.index:
+        rc = getattr(lib, name)(*args)
+    else:
+        with torch.cuda.device(device):
+            rc = getattr(lib, name)(*args)
+    if rc != RPS_OK:
+        raise RPSError(rc, name, lib.rps_ops_last_error().decode())
+
+
+def _stream(device: torch.device) -> int:
+    return torch.cuda.current_stream(device).cuda_stream
+
+
+def _workspace(device: torch.device, size: int) -> torch.Tensor:
+    # torch's allocations start on 512-byte boundaries; memory of the current stream goes back to it when the tensor is dropped
+    return torch.empty(max(size, 1), dtype=torch.uint8, device=device)
+
+
+def _check(name: str, t: torch.Tensor, like: Optional[torch.Tensor], shape: Tuple[int, ...]) -> None:
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    if t.dtype not in _DTYPE:
+        raise ValueError(f"{name} must be float32 or bfloat16, not {t.dtype}")
+    if like is not None and (t.dtype != like.dtype or t.device != like.device):
+        raise ValueError(f"{name} must have the type and device of the other tensors ({like.dtype}, {like.device})")
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{name} must have shape {shape}, not {tuple(t.shape)}")
+
+
+def _dense(name: str, t: torch.Tensor) -> None:
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+
+
+def _matrix_strides(name: str, t: torch.Tensor) -> Tuple[int, int]:
+    """(row, worker) strides of a [..., rows, cols] tensor whose rows are contiguous; an axis of one element takes any."""
+    rows, cols = t.shape[-2:]
+    if cols > 1 and t.stride(-1) != 1:
+        raise ValueError(f"the last axis of {name} must be contiguous")
+    row = t.stride(-2) if rows > 1 else max(cols, 1)
+    if row < cols:
+        raise ValueError(f"the rows of {name} overlap")
+    if t.dim() == 2 or t.shape[0] <= 1:
+        return row, 0
+    return row, t.stride(0)
+
+
+def _parameter_stride(name: str, t: torch.Tensor) -> int:
+    """Stride between the workers' parts of a parameter whose own part is contiguous (t has a worker axis)."""
+    part = t[0] if t.dim() and t.shape[0] else t
+    if not part.is_contiguous():
+        raise ValueError(f"each worker's part of {name} must be contiguous")
+    return t.stride(0) if t.shape[0] > 1 else 0
+
+
+# ------------------------------------------------------------------------------------------------------------ the loss
+def _lce_desc(hidden, weight, targets, ignore_index, reduction):
+    if reduction not in _REDUCTION:
+        raise ValueError(f"reduction must be one of {sorted(_REDUCTION)}")
+    if not isinstance(hidden, torch.Tensor) or hidden.dim() not in (2, 3):
+        raise ValueError("hidden must be a tensor [n, tokens, cols] or [tokens, cols]")
+    lead = tuple(hidden.shape[:-2])
+    tokens, cols = hidden.shape[-2:]
+    _check("hidden", hidden, None, tuple(hidden.shape))
+    if not isinstance(weight, torch.Tensor) or weight.dim() != hidden.dim():
+        raise ValueError("weight must be [n, vocab, cols] with hidden [n, tokens, cols], or [vocab, cols] with [tokens, cols]")
+    vocab = weight.shape[-2]
+    _check("weight", weight, hidden, lead + (vocab, cols))
+    if not isinstance(targets, torch.Tensor) or targets.dtype != torch.int64 or targets.device != hidden.device:
+        raise ValueError("targets must be an int64 tensor on the device of hidden")
+    if tuple(targets.shape) != lead + (tokens,):
+        raise ValueError(f"targets must have shape {lead + (tokens,)}, not {tuple(targets.shape)}")
+    d = rps_lce_desc(dtype=_DTYPE[hidden.dtype], reduction=_REDUCTION[reduction], n=lead[0] if lead else 1, tokens=tokens,
+                     vocab=vocab, cols=cols, ignore_index=ignore_index)
+    d.hidden_row, d.hidden_worker = _matrix_strides("hidden", hidden)
+    d.weight_row, d.weight_worker = _matrix_strides("weight", weight)
+    return d, lead
+
+
+def _lce_workspace(d, weight, backward):
+    size = ctypes.c_size_t()
+    _call("rps_lce_workspace", weight.device, ctypes.byref(d), weight.data_ptr(), backward, ctypes.byref(size))
+    return _workspace(weight.device, size.value), size.value
+
+
+def linear_cross_entropy_forward(hidden: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor, *,
+                                 ignore_index: int = -100, reduction: str = "mean") -> Tuple[torch.Tensor, torch.Tensor]:
+    """(loss, lse) of ``hidden @ weight.T`` against ``targets`` (``rps_lce_forward``).
+
+    hidden ``[n, tokens, cols]``, weight ``[n, vocab, cols]``, targets int64 ``[n, tokens]`` (all without ``n`` for a single
+    worker).  loss is float32: one value for each worker ("mean" over its tokens that are not ignored, "sum") or each token
+    ("none"); lse, float32 ``[n, tokens]``, is what the backward pass wants.  Ignored tokens have loss and lse 0."""
+    d, lead = _lce_desc(hidden, weight, targets, ignore_index, reduction)
+    targets = targets.contiguous()
+    loss = torch.empty(lead + ((d.tokens,) if reduction == "none" else ()), dtype=torch.float32, device=hidden.device)
+    lse = torch.empty(lead + (d.tokens,), dtype=torch.float32, device=hidden.device)
+    ws, size = _lce_workspace(d, weight, 0)
+    _call("rps_lce_forward", hidden.device, ctypes.byref(d), hidden.data_ptr(), weight.data_ptr(), targets.data_ptr(),
+          loss.data_ptr(), lse.data_ptr(), ws.data_ptr(), size, _stream(hidden.device))
+    return loss, lse
+
+
+def linear_cross_entropy_backward(dloss: torch.Tensor, hidden: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor,
+                                  lse: torch.Tensor, *, ignore_index: int = -100, reduction: str = "mean",
+                                  dweight: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(dhidden, dweight) for the gradient ``dloss`` (float32, shaped as the loss) of the forward call with the same
+    arguments (``rps_lce_backward``).  ``dweight``, if given, is written (not added to) and may be strided, a view into
+    the rows of a larger array for instance."""
+    d, lead = _lce_desc(hidden, weight, targets, ignore_index, reduction)
+    targets = targets.contiguous()
+    want = lead + ((d.tokens,) if reduction == "none" else ())
+    for name, t, shape in (("dloss", dloss, want), ("lse", lse, lead + (d.tokens,))):
+        if not isinstance(t, torch.Tensor) or t.dtype != torch.float32 or t.device != hidden.device or tuple(t.shape) != shape:
+            raise ValueError(f"{name} must be a float32 tensor of shape {shape} on the device of hidden")
+        _dense(name, t)
+    if dweight is None:
+        dweight = torch.empty(weight.shape, dtype=weight.dtype, device=weight.device)
+    else:
+        _check("dweight", dweight, hidden, tuple(weight.shape))
+    d.dweight_row, d.dweight_worker = _matrix_strides("dweight", dweight)
+    dhidden = torch.empty(hidden.shape, dtype=hidden.dtype, device=hidden.device)
+    ws, size = _lce_workspace(d, weight, 1)
+    _call("rps_lce_backward", hidden.device, ctypes.byref(d), hidden.data_ptr(), weight.data_ptr(), targets.data_ptr(),
+          lse.data_ptr(), dloss.data_ptr(), dhidden.data_ptr(), dweight.data_ptr(), ws.data_ptr(), size, _stream(hidden.device))
+    return dhidden, dweight
+
+
+class _LinearCrossEntropy(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, hidden, weight, targets, ignore_index, reduction):
+        loss, lse = linear_cross_entropy_forward(hidden, weight, targets, ignore_index=ignore_index, reduction=reduction)
+        ctx.save_for_backward(hidden, weight, targets, lse)
+        ctx.settings = {"ignore_index": ignore_index, "reduction": reduction}
+        return loss
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dloss):
+        dhidden, dweight = linear_cross_entropy_backward(dloss.float().contiguous(), *ctx.saved_tensors, **ctx.settings)
+        return dhidden, dweight, None, None, None
+
+
+def linear_cross_entropy(hidden: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor, *, ignore_index: int = -100,
+                         reduction: str = "mean") -> torch.Tensor:
+    """Differentiable ``linear_cross_entropy_forward``: the loss alone."""
+    return _LinearCrossEntropy.apply(hidden, weight, targets, ignore_index, reduction)
+
+
+# ------------------------------------------------------------------------------------------------------ 8-bit activations
+class PackedActivation(NamedTuple):
+    """Activations ``[..., columns]`` in 8 bits: int8 codes ``[..., columns rounded up to 16]`` and a float32 scale for each
+    128 columns, ``[..., groups]``; ``dtype`` is the type that they are read back in."""
+
+    codes: torch.Tensor
+    scales: torch.Tensor
+    columns: int
+    dtype: torch.dtype
+
+
+def packed_like(shape: Tuple[int, ...], dtype: torch.dtype, device: torch.device) -> PackedActivation:
+    """Room for the packed form of a tensor of this shape (the codes behind the last column are written by pack calls)."""
+    cols = shape[-1]
+    codes = torch.empty(tuple(shape[:-1]) + (-(-cols // 16) * 16,), dtype=torch.int8, device=device)
+    scales = torch.empty(tuple(shape[:-1]) + (-(-cols // GROUP),), dtype=torch.float32, device=device)
+    return PackedActivation(codes, scales, cols, dtype)
+
+
+def _check_packed(name: str, p: PackedActivation, lead: Optional[Tuple[int, ...]] = None) -> None:
+    if not isinstance(p, PackedActivation):
+        raise ValueError(f"{name} must be a PackedActivation")
+    c, s = p.codes, p.scales
+    if not (c.is_cuda and s.is_cuda and c.device == s.device and c.dtype == torch.int8 and s.dtype == torch.float32):
+        raise ValueError(f"{name}: codes must be int8 and scales float32, on one CUDA device")
+    if p.dtype not in _DTYPE:
+        raise ValueError(f"{name}: dtype must be float32 or bfloat16")
+    if p.columns < 1 or c.dim() < 1 or c.shape[-1] != -(-p.columns // 16) * 16 or tuple(s.shape) != tuple(c.shape[:-1]) + (-(-p.columns // GROUP),):
+        raise ValueError(f"{name}: codes {tuple(c.shape)} and scales {tuple(s.shape)} do not fit {p.columns} columns")
+    if lead is not None and tuple(c.shape[:-1]) != lead:
+        raise ValueError(f"{name} must hold {lead} rows, not {tuple(c.shape[:-1])}")
+    _dense(f"{name}.codes", c)
+    _dense(f"{name}.scales", s)
+
+
+def pack_activation(x: torch.Tensor) -> PackedActivation:
+    """``x`` in 8 bits (``rps_pack``).  x is ``[..., columns]`` and contiguous, or a matrix with contiguous rows."""
+    if not isinstance(x, torch.Tensor) or x.dim() < 1 or x.shape[-1] < 1:
+        raise ValueError("x must be a tensor [..., columns] with at least one column")
+    _check("x", x, None, tuple(x.shape))
+    row = _matrix_strides("x", x)[0] if x.dim() == 2 else x.shape[-1]
+    if x.dim() != 2:
+        _dense("x", x)
+    p = packed_like(tuple(x.shape), x.dtype, x.device)
+    _call("rps_pack", x.device, _DTYPE[x.dtype], x.numel() // x.shape[-1], x.shape[-1], x.data_ptr(), row, p.codes.data_ptr(),
+          p.scales.data_ptr(), _stream(x.device))
+    return p
+
+
+def unpack_activation(packed: PackedActivation) -> torch.Tensor:
+    """The values that ``packed`` stands for, in its dtype (``rps_unpack``)."""
+    _check_packed("packed", packed)
+    c = packed.codes
+    out = torch.empty(tuple(c.shape[:-1]) + (packed.columns,), dtype=packed.dtype, device=c.device)
+    _call("rps_unpack", c.device, _DTYPE[packed.dtype], out.numel() // packed.columns, packed.columns, c.data_ptr(),
+          packed.scales.data_ptr(), out.data_ptr(), packed.columns, _stream(c.device))
+    return out
+
+
+def packed_weight_grad(dy: torch.Tensor, packed: PackedActivation, *, dweight: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """``dy.mT @ x`` for the values x that ``packed`` stands for (``rps_packed_wgrad``): the weight gradient
+    ``[n, outs, columns]`` of ``y = x @ weight.mT`` out of dy ``[n, tokens, outs]``.  ``dweight`` as in
+    ``linear_cross_entropy_backward``."""
+    if not isinstance(dy, torch.Tensor) or dy.dim() not in (2, 3) or dy.shape[-1] < 1:
+        raise ValueError("dy must be a tensor [n, tokens, outs] or [tokens, outs]")
+    _check("dy", dy, None, tuple(dy.shape))
+    lead, (tokens, outs) = tuple(dy.shape[:-2]), dy.shape[-2:]
+    _check_packed("packed", packed, lead + (tokens,))
+    if packed.dtype != dy.dtype or packed.codes.device != dy.device:
+        raise ValueError("dy and packed must have one type and device")
+    d = rps_wgrad_desc(dtype=_DTYPE[dy.dtype], n=lead[0] if lead else 1, tokens=tokens, outs=outs, cols=packed.columns)
+    d.dy_row, d.dy_worker = _matrix_strides("dy", dy)
+    if dweight is None:
+        dweight = torch.empty(lead + (outs, packed.columns), dtype=dy.dtype, device=dy.device)
+    else:
+        _check("dweight", dweight, dy, lead + (outs, packed.columns))
+    d.dweight_row, d.dweight_worker = _matrix_strides("dweight", dweight)
+    size = ctypes.c_size_t()
+    _call("rps_wgrad_workspace", dy.device, ctypes.byref(d), dy.data_ptr(), ctypes.byref(size))
+    ws = _workspace(dy.device, size.value)
+    _call("rps_packed_wgrad", dy.device, ctypes.byref(d), dy.data_ptr(), packed.codes.data_ptr(), packed.scales.data_ptr(),
+          dweight.data_ptr(), ws.data_ptr(), size.value, _stream(dy.device))
+    return dweight
+
+
+class _Linear8bit(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight):
+        packed = pack_activation(x.contiguous())
+        ctx.save_for_backward(packed.codes, packed.scales, weight)
+        ctx.kept = packed.columns, packed.dtype
+        return torch.matmul(x, weight.mT)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        codes, scales, weight = ctx.saved_tensors
+        dy = dy.contiguous()
+        return torch.matmul(dy, weight), packed_weight_grad(dy, PackedActivation(codes, scales, *ctx.kept))
+
+
+def linear_8bit(x: torch.Tensor, weight: torch.Tensor) -> torch.Tensor:
+    """``x @ weight.mT`` with the input kept in 8 bits for the weight gradient: x ``[n, tokens, cols]``, weight ``[n, outs, cols]``,
+    or both without ``n``.  The two plain products are PyTorch's."""
+    if x.dim() != weight.dim() or x.dim() not in (2, 3):
+        raise ValueError("x must be [n, tokens, cols] with weight [n, outs, cols], or [tokens, cols] with [outs, cols]")
+    return _Linear8bit.apply(x, weight)
+
+
+# ------------------------------------------------------------------------------------------------- norms around a block
+class GatedResidualNormKept(NamedTuple):
+    """What ``gated_residual_norm_backward`` reads of the forward pass: f and h (tensors, or both packed) and the
+    reciprocal root mean squares of their rows, float32 ``[n, tokens]``."""
+
+    f: object
+    h: object
+    r_f: torch.Tensor
+    r_h: torch.Tensor
+    eps: float
+
+
+def _norm_desc(x, gate, post, pre, scale, eps):
+    if not isinstance(x, torch.Tensor) or x.dim() not in (2, 3):
+        raise ValueError("x must be a tensor [n, tokens, cols] or [tokens, cols]")
+    lead, (tokens, cols) = tuple(x.shape[:-2]), x.shape[-2:]
+    if not isinstance(gate, torch.Tensor) or gate.dim() != x.dim():
+        raise ValueError("gate must be [n, gates, cols] with x [n, tokens, cols], or [gates, cols] with [tokens, cols]")
+    gates = gate.shape[-2]
+    _check("gate", gate, x, lead + (gates, cols))
+    _check("post", post, x, lead + (cols,))
+    _check("pre", pre, x, lead + (cols,))
+    n = lead[0] if lead else 1
+    d = rps_norm_desc(dtype=_DTYPE[x.dtype], n=n, tokens=tokens, cols=cols, gates=gates, scale=scale, eps=eps)
+    strides = [_parameter_stride(name, t if lead else t[None]) for name, t in (("post", post), ("pre", pre), ("gate", gate))]
+    d.post_worker, d.pre_worker, d.gate_worker = strides
+    return d, lead
+
+
+def gated_residual_norm_forward(x: torch.Tensor, f: torch.Tensor, gate: torch.Tensor, post: torch.Tensor, pre: torch.Tensor, *,
+                                scale: float = 1.0, eps: float = 1e-6, keep: str = "values"):
+    """(h, y, kept) with ``h = x + scale * gate * norm(f) * post`` and ``y = norm(h) * pre``, norm being division by the
+    root mean square of a row (``rps_norm_forward``).
+
+    x, f ``[n, tokens, cols]``; post, pre ``[n, cols]``; gate ``[n, gates, cols]``, gates a divisor of tokens (consecutive tokens
+    share a row: 1 for a gate of each channel, tokens for one of each token); all without ``n`` for a single worker.
+    keep: "values" (kept holds f and h themselves), "int8" (8-bit copies, written along the way)."""
+    if keep not in ("values", "int8"):
+        raise ValueError('keep must be "values" or "int8"')
+    _check("x", x, None, tuple(x.shape))
+    d, lead = _norm_desc(x, gate, post, pre, scale, eps)
+    _check("f", f, x, tuple(x.shape))
+    _dense("x", x)
+    _dense("f", f)
+    h, y = torch.empty_like(x), torch.empty_like(x)
+    r = torch.empty((2,) + tuple(x.shape[:-1]), dtype=torch.float32, device=x.device)
+    r_f, r_h = r[0], r[1]
+    packed = (None, None, None, None)
+    if keep == "int8":
+        kept_f, kept_h = (packed_like(tuple(x.shape), x.dtype, x.device) for _ in range(2))
+        packed = tuple(t.data_ptr() for t in (kept_f.codes, kept_f.scales, kept_h.codes, kept_h.scales))
+    else:
+        kept_f, kept_h = f, h
+    _call("rps_norm_forward", x.device, ctypes.byref(d), x.data_ptr(), f.data_ptr(), gate.data_ptr(), post.data_ptr(),
+          pre.data_ptr(), h.data_ptr(), y.data_ptr(), r_f.data_ptr(), r_h.data_ptr(), *packed, _stream(x.device))
+    return h, y, GatedResidualNormKept(kept_f, kept_h, r_f, r_h, eps)
+
+
+def gated_residual_norm_backward(dh: Optional[torch.Tensor], dy: torch.Tensor, kept: GatedResidualNormKept, gate: torch.Tensor,
+                                 post: torch.Tensor, pre: torch.Tensor, *, scale: float = 1.0):
+    """(dx, df, dgate, dpost, dpre) for the gradients dh (None: none reaches h but through y) and dy of the forward call's h
+    and y (``rps_norm_backward``)."""
+    _check("dy", dy, None, tuple(dy.shape))
+    d, lead = _norm_desc(dy, gate, post, pre, scale, kept.eps)
+    _dense("dy", dy)
+    if dh is not None:
+        _check("dh", dh, dy, tuple(dy.shape))
+        _dense("dh", dh)
+    rows = tuple(dy.shape[:-1])
+    if isinstance(kept.f, PackedActivation):
+        for name, p in (("kept.f", kept.f), ("kept.h", kept.h)):
+            _check_packed(name, p, rows)
+            if p.columns != d.cols or p.dtype != dy.dtype or p.codes.device != dy.device:
+                raise ValueError(f"{name} does not go with dy")
+        f, f_scales, h, h_scales = (t.data_ptr() for t in (kept.f.codes, kept.f.scales, kept.h.codes, kept.h.scales))
+    else:
+        for name, t in (("kept.f", kept.f), ("kept.h", kept.h)):
+            _check(name, t, dy, tuple(dy.shape))
+            _dense(name, t)
+        f, f_scales, h, h_scales = kept.f.data_ptr(), None, kept.h.data_ptr(), None
+    for name, t in (("kept.r_f", kept.r_f), ("kept.r_h", kept.r_h)):
+        if t.dtype != torch.float32 or t.device != dy.device or tuple(t.shape) != rows:
+            raise ValueError(f"{name} must be a float32 tensor of shape {rows} on the device of dy")
+        _dense(name, t)
+    dx, df = torch.empty_like(dy), torch.empty_like(dy)
+    dgate, dpost, dpre = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (gate, post, pre))
+    size = ctypes.c_size_t()
+    _call("rps_norm_workspace", dy.device, ctypes.byref(d), ctypes.byref(size))
+    ws = _workspace(dy.device, size.value)
+    _call("rps_norm_backward", dy.device, ctypes.byref(d), None if dh is None else dh.data_ptr(), dy.data_ptr(), f, f_scales, h,
+          h_scales, kept.r_f.data_ptr(), kept.r_h.data_ptr(), gate.data_ptr(), post.data_ptr(), pre.data_ptr(), dx.data_ptr(),
+          df.data_ptr(), dgate.data_ptr(), dpost.data_ptr(), dpre.data_ptr(), ws.data_ptr(), size.value, _stream(dy.device))
+    return dx, df, dgate, dpost, dpre
+
+
+class _GatedResidualNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, f, gate, post, pre, scale, eps, keep):
+        h, y, kept = gated_residual_norm_forward(x, f, gate, post, pre, scale=scale, eps=eps, keep=keep)
+        ctx.set_materialize_grads(False)
+        ctx.settings = scale, eps, keep
+        if keep == "int8":
+            ctx.columns = kept.f.columns, kept.f.dtype
+            ctx.save_for_backward(gate, post, pre, kept.r_f, kept.r_h, kept.f.codes, kept.f.scales, kept.h.codes, kept.h.scales)
+        else:
+            ctx.save_for_backward(gate, post, pre, kept.r_f, kept.r_h, f, h)
+        return h, y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dh, dy):
+        scale, eps, keep = ctx.settings
+        gate, post, pre, r_f, r_h, *rest = ctx.saved_tensors
+        if keep == "int8":
+            f, h = (PackedActivation(c, s, *ctx.columns) for c, s in (rest[:2], rest[2:]))
+        else:
+            f, h = rest
+        if dy is None:  # y was not used
+            shape = r_f.shape + (post.shape[-1],)
+            dy = torch.zeros(shape, dtype=post.dtype, device=post.device)
+        grads = gated_residual_norm_backward(None if dh is None else dh.contiguous(), dy.contiguous(),
+                                             GatedResidualNormKept(f, h, r_f, r_h, eps), gate, post, pre, scale=scale)
+        return grads + (None, None, None)
+
+
+def gated_residual_norm(x: torch.Tensor, f: torch.Tensor, gate: torch.Tensor, post: torch.Tensor, pre: torch.Tensor, *,
+                        scale: float = 1.0, eps: float = 1e-6, keep: str = "values") -> Tuple[torch.Tensor, torch.Tensor]:
+    """Differentiable ``gated_residual_norm_forward``: (h, y)."""
+    return _GatedResidualNorm.apply(x, f, gate, post, pre, scale, eps, keep)
