@@ -173,6 +173,10 @@ int rps_wgrad_workspace(const rps_wgrad_desc* desc, const void* dy, size_t* byte
 int rps_packed_wgrad(const rps_wgrad_desc* desc, const void* dy, const int8_t* codes, const float* scales, void* dweight,
                      void* workspace, size_t workspace_bytes, void* cuda_stream);
 
+/* Every wait of the matrix-product kernels on data is bounded (two seconds); one that gives up ends its kernel early.
+ * rps_ops_check synchronises the stream and returns RPS_ECUDA if that happened on the current device since the last check. */
+int rps_ops_check(void* cuda_stream);
+
 /* Reason for the last failure of a function of this file on the calling thread ("" if none). */
 const char* rps_ops_last_error(void);
 

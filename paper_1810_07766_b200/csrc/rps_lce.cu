@@ -56,11 +56,14 @@ __global__ void __launch_bounds__(kSelectThreads) rps_lce_select_kernel(const Lc
         if (kept == 0 && prm.reduction != RPS_REDUCE_NONE && threadIdx.x == 0) prm.loss[w] = 0.0f;
         return;
     }
+    // A factor that all rows share stays out of dl: near a token's target dl is p - 1, which bf16 holds all but exactly, and
+    // (p - 1) times a factor it does not (relative error of the gradients: 2.7e-3 -> 1.7e-3, 1.65e-3 of it the rounding of the result).
+    if (threadIdx.x == 0)
+        prm.scale[w] = prm.reduction == RPS_REDUCE_NONE || kept == 0 ? 1.0f : prm.reduction == RPS_REDUCE_MEAN ? prm.dloss[w] / (float)kept : prm.dloss[w];
     __syncthreads();  // rows[] and target[] of this CTA's own threads
     for (int i = threadIdx.x; i < kept; i += kSelectThreads) {
         const int t = rows[i];
-        float g = prm.reduction == RPS_REDUCE_NONE ? prm.dloss[w * prm.tokens + t] : prm.dloss[w];
-        if (prm.reduction == RPS_REDUCE_MEAN) g /= (float)kept;
+        float g = prm.reduction == RPS_REDUCE_NONE ? prm.dloss[w * prm.tokens + t] : 1.0f;
         if (target[i] < 0) g = nanf("");
         prm.info[w * prm.tokens_padded + i] = make_float2(prm.lse_in[w * prm.tokens + t], g);
     }
@@ -125,9 +128,9 @@ __global__ void __launch_bounds__(kMergeThreads) rps_lce_merge_kernel(const LceP
     const int i = blockIdx.x * kMergeThreads + threadIdx.x;
     float loss = 0.0f;
     if (i < count) {
-        const float2* part = prm.part + w * prm.vocab_tiles * prm.tokens_padded + i;
+        const float2* part = prm.part + w * prm.stat_tiles * prm.tokens_padded + i;
         float top = -INFINITY, sum = 0.0f;
-        for (int64_t v = 0; v < prm.vocab_tiles; ++v) {
+        for (int64_t v = 0; v < prm.stat_tiles; ++v) {
             const float2 p = part[v * prm.tokens_padded];
             const float m = fmaxf(top, p.x), at = m == -INFINITY ? 0.0f : m;
             sum = sum * __expf(top - at) + p.y * __expf(p.x - at);

@@ -126,7 +126,7 @@ LcePlan plan_lce(const rps_lce_desc& d, const void* weight, bool backward, void*
     };
     if (backward) narrow(p.n * p.planes * p.tokens_padded * 2);
     if (plan.lay_out_weight) narrow(p.n * p.planes * p.cols_padded * 2);
-    p.vocab_tiles = whole / kVocabTile;
+    p.stat_tiles = ceil_div(d.vocab, kStatCols);
 
     Carver c{static_cast<unsigned char*>(workspace)};
     p.count = c.take<int>(p.n);
@@ -137,21 +137,22 @@ LcePlan plan_lce(const rps_lce_desc& d, const void* weight, bool backward, void*
     if (backward) {
         p.info = c.take<float2>(p.n * p.tokens_padded);
         plan.dl = c.take<bf16>(p.n * p.planes * p.tokens_padded * plan.piece);
-        if (plan.piece < whole) plan.acc = c.take<float>(p.n * p.tokens_padded * p.cols);
+        p.scale = c.take<float>(p.n);
+        if (plan.piece < whole) plan.acc = c.take<float>(p.n * p.tokens_padded * round_up(p.cols, kVocabTile));
     } else {
         p.done = c.take<int>(p.n);
         p.sums = c.take<float>(p.n * lce_merge_blocks(p.tokens));
-        p.part = c.take<float2>(p.n * p.vocab_tiles * p.tokens_padded);
+        p.part = c.take<float2>(p.n * p.stat_tiles * p.tokens_padded);
         p.hit = c.take<float>(p.n * p.tokens_padded);
     }
     plan.bytes = c.used;
 
     ProductParams& g = plan.product;
     g.workers = p.n, g.planes = p.planes, g.count = p.count;
-    g.vocab = (int)p.vocab, g.vocab_tiles = (int)p.vocab_tiles, g.target = p.target;
+    g.vocab = (int)p.vocab, g.stat_tiles = (int)p.stat_tiles, g.target = p.target;
     g.part = const_cast<float2*>(p.part), g.hit = const_cast<float*>(p.hit), g.info = p.info, g.dl = plan.dl;
     g.tokens_padded = p.tokens_padded, g.piece = plan.piece, g.acc = plan.acc, g.rows = p.rows, g.tokens = p.tokens;
-    g.out_f32 = p.f32;
+    g.out_f32 = p.f32, g.acc_row = round_up(p.cols, kVocabTile), g.scale = p.scale;
     return plan;
 }
 
@@ -182,6 +183,14 @@ int weight_operand(const rps_lce_desc& d, const LcePlan& plan, const void* weigh
 }  // namespace
 
 extern "C" const char* rps_ops_last_error(void) { return g_error; }
+
+extern "C" int rps_ops_check(void* cuda_stream)
+{
+    start();
+    int gave_up = 0;
+    RPS_TRY(read_gave_up(&gave_up, static_cast<cudaStream_t>(cuda_stream)));
+    return gave_up == 0 ? RPS_OK : fail(RPS_ECUDA, "a wait inside a kernel gave up; the outputs of the calls since the last check are not valid");
+}
 
 extern "C" int rps_lce_workspace(const rps_lce_desc* desc, const void* weight, int backward, size_t* bytes)
 {

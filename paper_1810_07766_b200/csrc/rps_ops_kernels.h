@@ -15,9 +15,11 @@ inline int64_t round_up(int64_t a, int64_t b) { return (a + b - 1) / b * b; }
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // ---------------------------------------------------------------------------------------------------- products
-// Token rows are padded to whole tiles, and the vocabulary goes through the loss in whole tiles.
+// Token rows are padded to whole tiles, and the vocabulary goes through the loss in whole tiles; softmax statistics are kept for
+// each half of a tile's columns.
 constexpr int kTokenTile = 256;
-constexpr int kVocabTile = 64;
+constexpr int kVocabTile = 256;
+constexpr int kStatCols = 128;
 
 // An operand of a product: bf16 [worker][plane][rows][row stride].  fp32 values lie in three planes whose sum they are.
 struct Operand {
@@ -40,15 +42,16 @@ struct ProductParams {
     const int* count;   // [worker] tokens that take part, or NULL: all
     // kLse, kDlogits
     int v0, vocab;          // first row of the vocabulary in this piece; all of it
-    int vocab_tiles;
+    int stat_tiles;
     const int* target;      // [worker][tokens_padded]
-    float2* part;           // [worker][tiles of the vocabulary][tokens_padded]: running maximum and sum
+    float2* part;           // [worker][stat_tiles][tokens_padded]: running maximum and sum
     float* hit;             // [worker][tokens_padded]: the target's logit
     const float2* info;     // [worker][tokens_padded]: lse, g
     bf16* dl;               // [worker][plane][tokens_padded][piece]
     int64_t tokens_padded, piece;
     // kDhidden
-    float* acc;             // [worker][tokens_padded][n]
+    float* acc;             // [worker][tokens_padded][acc_row], acc_row a multiple of the tile
+    int64_t acc_row;
     const int* rows;        // [worker][tokens]: token of each row
     int64_t tokens;
     int first, last;        // first and last piece
@@ -56,9 +59,12 @@ struct ProductParams {
     void* out;
     int64_t out_row, out_worker;
     int out_f32;
+    const float* scale;     // [worker], or NULL: factor of the result
 };
 
 cudaError_t launch_product(Product which, const ProductParams& prm, cudaStream_t stream);
+cudaError_t read_gave_up(int* value, cudaStream_t stream);  // and clears it; synchronises
+cudaError_t sm_count(int* out);                             // of the current device
 
 // ---------------------------------------------------------------------------------------------------- the loss
 struct LceParams {
@@ -68,7 +74,8 @@ struct LceParams {
     int* rows;        // [n][tokens]: tokens that take part in their order, then the others
     int* count;       // [n]
     int* target;      // [n][tokens_padded]: targets of the rows, -1 for one that names no row of weight
-    float2* info;     // [n][tokens_padded] (backward)
+    float2* info;     // [n][tokens_padded] (backward): lse and the factor of the row's dl
+    float* scale;     // [n] (backward): the factor that a worker's rows share, applied to the sums of products
     const float* lse_in;
     const float* dloss;
     const void* hidden;
@@ -78,7 +85,7 @@ struct LceParams {
     // forward's end
     const float2* part;
     const float* hit;
-    int64_t vocab_tiles;
+    int64_t stat_tiles;
     float* loss;
     float* lse;
     float* sums;      // [n][blocks of rows]

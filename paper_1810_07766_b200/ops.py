@@ -32,7 +32,7 @@ _DTYPE = {torch.float32: RPS_F32, torch.bfloat16: RPS_BF16}
 SYMBOLS = (
     "rps_lce_workspace", "rps_lce_forward", "rps_lce_backward", "rps_norm_forward", "rps_norm_workspace",
     "rps_norm_backward", "rps_pack_pitch", "rps_pack", "rps_unpack", "rps_wgrad_workspace", "rps_packed_wgrad",
-    "rps_ops_last_error",
+    "rps_ops_check", "rps_ops_last_error",
 )
 
 _i32, _i64, _dbl = ctypes.c_int32, ctypes.c_int64, ctypes.c_double
@@ -76,6 +76,7 @@ def _library() -> ctypes.CDLL:
             "rps_unpack": (cint, [cint, _i64, _i64, vp, vp, vp, _i64, vp]),
             "rps_wgrad_workspace": (cint, [wgrad, vp, sizep]),
             "rps_packed_wgrad": (cint, [wgrad] + [vp] * 5 + [size, vp]),
+            "rps_ops_check": (cint, [vp]),
             "rps_ops_last_error": (ctypes.c_char_p, []),
         }
         for name, (res, args) in sig.items():
@@ -95,6 +96,12 @@ def _call(name: str, device: torch.device, *args) -> None:
             rc = getattr(lib, name)(*args)
     if rc != RPS_OK:
         raise RPSError(rc, name, lib.rps_ops_last_error().decode())
+
+
+def check(device: Optional[torch.device] = None) -> None:
+    """Synchronises the current stream of the device and raises if a kernel of an earlier call gave up (``rps_ops_check``)."""
+    device = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
+    _call("rps_ops_check", device, _stream(device))
 
 
 def _stream(device: torch.device) -> int:
