@@ -1,69 +1,153 @@
 // The step between two blocks of a network: norm, gate, residual scale, residual sum, norm; forward and backward.
-#include "rps_ops_kernels.h"
+//
+// Bound by memory: forward reads x, f (and gate) and writes h, y; backward reads dh, dy, f, h (and gate) and writes dx, df
+// (and dgate).  So every tensor is touched once.  A row is spread over a CTA of at most 512 threads, 16 bytes of it to a thread (a wider
+// row over a cluster of CTAs that exchange their sums through distributed shared memory), so that a row lives in
+// registers between its sums and its results; CTAs walk many rows and read the next row before they work on this one.
+//
+// Backward needs two means of a row, of a * h and of b * f, where b depends on the first one.  With q = scale * gate * post * f,
+//   sum b f = sum q (dh + r_h a) - r_h^3 mean(a h) sum q h,
+// so both come out of three sums made in one pass, with one barrier for a row.  The sums over rows (dpost, dpre, and dgate where
+// tokens share a gate) stay in the registers of the thread that owns the columns; a block writes its own once, and a
+// second kernel adds the blocks' in a fixed order.
+#include "rps_rows.cuh"
+
+#include "rps_kernels.h"
 
 namespace rps_ops {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kMostThreads = 512;
+constexpr int kMostCluster = 8;
+constexpr int kMostWarps = kMostThreads / 32 * kMostCluster;
 
-__device__ __forceinline__ float block_sum(float v, float* buf)
+__device__ __forceinline__ uint32_t cluster_rank()
 {
-    for (int s = 16; s > 0; s /= 2) v += __shfl_xor_sync(0xFFFFFFFFu, v, s);
-    __syncthreads();
-    if (threadIdx.x % 32 == 0) buf[threadIdx.x / 32] = v;
-    __syncthreads();
-    v = 0.0f;
-    for (int i = 0; i < kThreads / 32; ++i) v += buf[i];
-    return v;
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kThreads) rps_norm_forward_kernel(const NormParams prm)
+// Sums of N values over the threads that share a row.  `slots` is double-buffered over successive calls (`turn`), so
+// that one barrier a call is enough.  Every thread gets the sums, added in the same order.
+template <int N>
+__device__ __forceinline__ void row_sums(float (&v)[N], float (*slots)[N][kMostWarps], int turn, int cluster, uint32_t rank)
 {
-    extern __shared__ float hrow[];
-    __shared__ float buf[kThreads / 32];
-    const int64_t row = blockIdx.x, w = row / prm.tokens, t = row % prm.tokens, D = prm.cols;
-    const T* x = static_cast<const T*>(prm.x) + row * D;
-    const T* f = static_cast<const T*>(prm.f) + row * D;
-    const T* gate = static_cast<const T*>(prm.gate) + w * prm.gate_worker + t / prm.rows_per_gate * D;
-    const T* post = static_cast<const T*>(prm.post) + w * prm.post_worker;
-    const T* pre = static_cast<const T*>(prm.pre) + w * prm.pre_worker;
-    float s = 0.0f;
-    for (int64_t c = threadIdx.x; c < D; c += kThreads) {
-        const float v = to_float<T>(f[c]);
-        s = fmaf(v, v, s);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int s = 16; s > 0; s /= 2) v[i] += __shfl_xor_sync(0xFFFFFFFFu, v[i], s);
+    const int warps = blockDim.x / 32, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    if (warps * cluster == 1) return;
+    if (cluster == 1) {
+        if (lane == 0) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) slots[turn][i][warp] = v[i];
+        }
+        __syncthreads();
+    } else {
+        if (lane < cluster) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const uint32_t own = (uint32_t)__cvta_generic_to_shared(&slots[turn][i][rank * warps + warp]);
+                uint32_t there;
+                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(own), "r"(lane));
+                asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(there), "f"(v[i]) : "memory");
+            }
+        }
+        __syncwarp();
+        asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
     }
-    const float r_f = rsqrtf(block_sum(s, buf) / (float)D + prm.eps);
-    s = 0.0f;
-    for (int64_t c = threadIdx.x; c < D; c += kThreads) {
-        const float u = to_float<T>(f[c]) * r_f * to_float<T>(post[c]);
-        const float h = fmaf(prm.scale * to_float<T>(gate[c]), u, to_float<T>(x[c]));
-        static_cast<T*>(prm.h)[row * D + c] = from_float<T>(h);
-        hrow[c] = h;
-        s = fmaf(h, h, s);
-    }
-    const float r_h = rsqrtf(block_sum(s, buf) / (float)D + prm.eps);
-    for (int64_t c = threadIdx.x; c < D; c += kThreads)
-        static_cast<T*>(prm.y)[row * D + c] = from_float<T>(hrow[c] * r_h * to_float<T>(pre[c]));
-    if (threadIdx.x == 0 && prm.r_f != nullptr) {
-        prm.r_f[row] = r_f;
-        prm.r_h[row] = r_h;
+    const int slots_used = warps * cluster;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        float s = 0.0f;
+        for (int k = lane; k < slots_used; k += 32) s += slots[turn][i][k];
+#pragma unroll
+        for (int k = 16; k > 0; k /= 2) s += __shfl_xor_sync(0xFFFFFFFFu, s, k);
+        v[i] = s;
     }
 }
 
-template <typename T>
-__device__ __forceinline__ float kept(const void* values, const float* scales, const NormParams& prm, int64_t row, int64_t c)
+template <typename T, bool ALIGNED, bool PACK>
+__global__ void __launch_bounds__(kMostThreads, 2) rps_norm_forward_kernel(const NormParams prm)
 {
-    if (scales == nullptr) return to_float<T>(static_cast<const T*>(values)[row * prm.cols + c]);
-    return (float)static_cast<const int8_t*>(values)[row * prm.pitch + c] * scales[row * prm.groups + c / RPS_PACK_GROUP];
+    constexpr int W = Slice<T>::kWidth;
+    __shared__ float slots[2][1][kMostWarps];
+    const int cluster = prm.cluster, D = (int)prm.cols;
+    const uint32_t rank = cluster > 1 ? cluster_rank() : 0;
+    const int c = ((int)rank * blockDim.x + threadIdx.x) * W;
+    const int64_t rows = prm.n * prm.tokens, step = gridDim.x / cluster;
+    const float inv = 1.0f / (float)D;
+    int64_t row = blockIdx.x / cluster;
+    uint4 x_next, f_next, gate_next;
+    const auto read = [&](int64_t r) {
+        const int64_t w = r / prm.tokens, t = r - w * prm.tokens;
+        x_next = load_slice<T, ALIGNED, true>(static_cast<const T*>(prm.x) + r * D, c, D);
+        f_next = load_slice<T, ALIGNED, true>(static_cast<const T*>(prm.f) + r * D, c, D);
+        gate_next = load_slice<T, ALIGNED, false>(static_cast<const T*>(prm.gate) + w * prm.gate_worker + t / prm.rows_per_gate * D, c, D);
+    };
+    if (row < rows) read(row);
+    int turn = 0;
+    for (; row < rows; row += step) {
+        float x[W], f[W], gate[W], post[W], pre[W];
+        widen(x_next, x), widen(f_next, f), widen(gate_next, gate);
+        const int64_t w = row / prm.tokens;
+        widen(load_slice<T, ALIGNED, false>(static_cast<const T*>(prm.post) + w * prm.post_worker, c, D), post);
+        widen(load_slice<T, ALIGNED, false>(static_cast<const T*>(prm.pre) + w * prm.pre_worker, c, D), pre);
+        if (row + step < rows) read(row + step);
+        float s[1] = {0.0f};
+#pragma unroll
+        for (int j = 0; j < W; ++j) s[0] = fmaf(f[j], f[j], s[0]);
+        row_sums<1>(s, slots, turn, cluster, rank), turn ^= 1;
+        const float r_f = rsqrtf(fmaf(s[0], inv, prm.eps));
+        if constexpr (PACK) {
+            const bool in = c < prm.pitch;
+            pack_slice(f, in ? prm.f_codes + row * prm.pitch + c : nullptr, c < D ? prm.f_scales + row * prm.groups + c / RPS_PACK_GROUP : nullptr);
+        }
+        s[0] = 0.0f;
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+            x[j] = fmaf(prm.scale * gate[j], f[j] * r_f * post[j], x[j]);  // h
+            s[0] = fmaf(x[j], x[j], s[0]);
+        }
+        const uint4 h = narrow(x);
+        store_slice<T, ALIGNED>(static_cast<T*>(prm.h) + row * D, c, D, h);
+        row_sums<1>(s, slots, turn, cluster, rank), turn ^= 1;
+        const float r_h = rsqrtf(fmaf(s[0], inv, prm.eps));
+        if constexpr (PACK) {
+            float stored[W];  // as a reader of h sees it
+            widen(h, stored);
+            if constexpr (!ALIGNED) {
+#pragma unroll
+                for (int j = 0; j < W; ++j)
+                    if (c + j >= D) stored[j] = 0.0f;
+            }
+            pack_slice(stored, c < prm.pitch ? prm.h_codes + row * prm.pitch + c : nullptr,
+                       c < D ? prm.h_scales + row * prm.groups + c / RPS_PACK_GROUP : nullptr);
+        }
+#pragma unroll
+        for (int j = 0; j < W; ++j) x[j] = x[j] * r_h * pre[j];
+        store_slice<T, ALIGNED>(static_cast<T*>(prm.y) + row * D, c, D, narrow(x));
+        if (prm.r_f != nullptr && rank == 0 && threadIdx.x == 0) {
+            prm.r_f[row] = r_f;
+            prm.r_h[row] = r_h;
+        }
+    }
+    // another CTA's sums may still be on their way here
+    if (cluster > 1) asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kThreads) rps_norm_backward_kernel(const NormParams prm)
+template <typename T, bool ALIGNED, bool PACKED>
+__global__ void __launch_bounds__(kMostThreads, 1) rps_norm_backward_kernel(const NormParams prm)
 {
-    extern __shared__ float trow[];
-    __shared__ float buf[kThreads / 32];
-    const int64_t D = prm.cols, w = blockIdx.y, block = blockIdx.x;
+    constexpr int W = Slice<T>::kWidth;
+    __shared__ float slots[2][3][kMostWarps];
+    const int cluster = prm.cluster, D = (int)prm.cols;
+    const uint32_t rank = cluster > 1 ? cluster_rank() : 0;
+    const int c = ((int)rank * blockDim.x + threadIdx.x) * W;
+    const float inv = 1.0f / (float)D;
+    const int64_t block = blockIdx.x / cluster, w = blockIdx.y;
     int64_t first, end;
     if (prm.chunks > 0) {
         const int64_t g = block / prm.chunks;
@@ -73,111 +157,212 @@ __global__ void __launch_bounds__(kThreads) rps_norm_backward_kernel(const NormP
         first = block * prm.rows_per_block;
         end = min(first + prm.rows_per_block, prm.tokens);
     }
-    const T* post = static_cast<const T*>(prm.post) + w * prm.post_worker;
-    const T* pre = static_cast<const T*>(prm.pre) + w * prm.pre_worker;
-    float* partial = prm.partial + (w * prm.blocks + block) * 3 * D;
-    for (int64_t c = threadIdx.x; c < 3 * D; c += kThreads) partial[c] = 0.0f;
-    __syncthreads();
+    const uint4 post_slice = load_slice<T, ALIGNED, false>(static_cast<const T*>(prm.post) + w * prm.post_worker, c, D);
+    const uint4 pre_slice = load_slice<T, ALIGNED, false>(static_cast<const T*>(prm.pre) + w * prm.pre_worker, c, D);
+    float dpost[W] = {}, dpre[W] = {}, dgate[W] = {};
+
+    uint4 dh_next = make_uint4(0, 0, 0, 0), dy_next, f_next, h_next, gate_next;
+    Codes<W> f_codes, h_codes;
+    float f_scale, h_scale, rf_next, rh_next;
+    int64_t gate_row = first / prm.rows_per_gate, in_gate = first - gate_row * prm.rows_per_gate;  // of the next row to be read
+    const auto read = [&](int64_t t) {
+        const int64_t r = w * prm.tokens + t;
+        dy_next = load_slice<T, ALIGNED, true>(static_cast<const T*>(prm.dy) + r * D, c, D);
+        if (prm.dh != nullptr) dh_next = load_slice<T, ALIGNED, true>(static_cast<const T*>(prm.dh) + r * D, c, D);
+        if constexpr (PACKED) {
+            f_codes.clear(), h_codes.clear(), f_scale = h_scale = 0.0f;
+            if (c < D) {
+                f_codes.load(static_cast<const int8_t*>(prm.f) + r * prm.pitch + c);
+                h_codes.load(static_cast<const int8_t*>(prm.h_in) + r * prm.pitch + c);
+                f_scale = prm.f_scales[r * prm.groups + c / RPS_PACK_GROUP];
+                h_scale = prm.h_scales[r * prm.groups + c / RPS_PACK_GROUP];
+            }
+        } else {
+            f_next = load_slice<T, ALIGNED, true>(static_cast<const T*>(prm.f) + r * D, c, D);
+            h_next = load_slice<T, ALIGNED, true>(static_cast<const T*>(prm.h_in) + r * D, c, D);
+        }
+        gate_next = load_slice<T, ALIGNED, false>(static_cast<const T*>(prm.gate) + w * prm.gate_worker + gate_row * D, c, D);
+        if (++in_gate == prm.rows_per_gate) in_gate = 0, ++gate_row;
+        rf_next = prm.r_f[r], rh_next = prm.r_h[r];
+    };
+    if (first < end) read(first);
+    int64_t left_in_gate = prm.rows_per_gate - (first - first / prm.rows_per_gate * prm.rows_per_gate);
+    int turn = 0;
     for (int64_t t = first; t < end; ++t) {
         const int64_t row = w * prm.tokens + t;
-        const T* gate = static_cast<const T*>(prm.gate) + w * prm.gate_worker + t / prm.rows_per_gate * D;
-        const float r_f = prm.r_f[row], r_h = prm.r_h[row];
-        float s = 0.0f;
-        for (int64_t c = threadIdx.x; c < D; c += kThreads)
-            s = fmaf(to_float<T>(static_cast<const T*>(prm.dy)[row * D + c]) * to_float<T>(pre[c]), kept<T>(prm.h_in, prm.h_scales, prm, row, c), s);
-        const float mean_h = block_sum(s, buf) / (float)D * r_h * r_h;
-        s = 0.0f;
-        for (int64_t c = threadIdx.x; c < D; c += kThreads) {
-            const float h = kept<T>(prm.h_in, prm.h_scales, prm, row, c), f = kept<T>(prm.f, prm.f_scales, prm, row, c);
-            const float dy = to_float<T>(static_cast<const T*>(prm.dy)[row * D + c]);
-            float v = r_h * (dy * to_float<T>(pre[c]) - h * mean_h);
-            if (prm.dh != nullptr) v += to_float<T>(static_cast<const T*>(prm.dh)[row * D + c]);
-            static_cast<T*>(prm.dx)[row * D + c] = from_float<T>(v);
-            trow[c] = v;
-            const float du = prm.scale * to_float<T>(gate[c]) * v;
-            s = fmaf(du * to_float<T>(post[c]), f, s);
-            partial[c] += du * f * r_f;
-            partial[D + c] += dy * h * r_h;
-            partial[2 * D + c] += prm.scale * v * f * r_f * to_float<T>(post[c]);
+        float f[W], h[W], dy[W], dx[W], gate[W], post[W];
+        if constexpr (PACKED) {
+            f_codes.values(f_scale, f), h_codes.values(h_scale, h);
+        } else {
+            widen(f_next, f), widen(h_next, h);
         }
-        const float mean_f = block_sum(s, buf) / (float)D * r_f * r_f;
-        for (int64_t c = threadIdx.x; c < D; c += kThreads) {
-            const float f = kept<T>(prm.f, prm.f_scales, prm, row, c);
-            const float b = prm.scale * to_float<T>(gate[c]) * trow[c] * to_float<T>(post[c]);
-            static_cast<T*>(prm.df)[row * D + c] = from_float<T>(r_f * (b - f * mean_f));
+        widen(dy_next, dy), widen(dh_next, dx), widen(gate_next, gate), widen(post_slice, post);
+        const float r_f = rf_next, r_h = rh_next;
+        if (t + 1 < end) read(t + 1);
+        float s[3] = {};
+        {
+            float pre[W];
+            widen(pre_slice, pre);
+#pragma unroll
+            for (int j = 0; j < W; ++j) {
+                dpre[j] = fmaf(dy[j], h[j] * r_h, dpre[j]);
+                const float a = dy[j] * pre[j], q = prm.scale * gate[j] * post[j] * f[j];
+                dx[j] = fmaf(r_h, a, dx[j]);  // dh + r_h a
+                s[0] = fmaf(a, h[j], s[0]);
+                s[1] = fmaf(q, dx[j], s[1]);
+                s[2] = fmaf(q, h[j], s[2]);
+            }
         }
-        if (prm.chunks == 0 && (t + 1) % prm.rows_per_gate == 0) {  // the block holds the whole gate group
-            for (int64_t c = threadIdx.x; c < D; c += kThreads) {
-                static_cast<T*>(prm.dgate)[(w * prm.gates + t / prm.rows_per_gate) * D + c] = from_float<T>(partial[2 * D + c]);
-                partial[2 * D + c] = 0.0f;
+        row_sums<3>(s, slots, turn, cluster, rank), turn ^= 1;
+        const float mean_h = s[0] * inv * r_h * r_h * r_h;
+        const float mean_f = (s[1] - mean_h * s[2]) * inv * r_f * r_f;
+        float df[W];
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+            dx[j] = fmaf(-h[j], mean_h, dx[j]);
+            const float g = prm.scale * dx[j], n = f[j] * r_f;
+            dgate[j] = fmaf(g, n * post[j], dgate[j]);
+            dpost[j] = fmaf(g * gate[j], n, dpost[j]);
+            df[j] = r_f * (g * gate[j] * post[j] - f[j] * mean_f);
+        }
+        store_slice<T, ALIGNED>(static_cast<T*>(prm.dx) + row * D, c, D, narrow(dx));
+        store_slice<T, ALIGNED>(static_cast<T*>(prm.df) + row * D, c, D, narrow(df));
+        if (--left_in_gate == 0) {
+            left_in_gate = prm.rows_per_gate;
+            if (prm.chunks == 0) {  // the block held the whole gate group
+                store_slice<T, ALIGNED>(static_cast<T*>(prm.dgate) + (w * prm.gates + t / prm.rows_per_gate) * D, c, D, narrow(dgate));
+#pragma unroll
+                for (int j = 0; j < W; ++j) dgate[j] = 0.0f;
             }
         }
     }
+    float* partial = prm.partial + (w * prm.blocks + block) * 3 * D;
+#pragma unroll
+    for (int j = 0; j < W; ++j) {
+        if (c + j < D) {
+            partial[c + j] = dpost[j];
+            partial[D + c + j] = dpre[j];
+            if (prm.chunks > 0) partial[2 * D + c + j] = dgate[j];
+        }
+    }
+    if (cluster > 1) asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
 }
 
-// Sums of the blocks' partial sums, a thread for each column, always in the same order.
+// Sums of the blocks' sums: 32 columns to a CTA, the blocks dealt to its 16 warps, whose sums are added in their order.
 template <typename T>
-__global__ void __launch_bounds__(128) rps_norm_reduce_kernel(const NormParams prm)
+__global__ void __launch_bounds__(512) rps_norm_reduce_kernel(const NormParams prm)
 {
-    const int64_t c = (int64_t)blockIdx.x * 128 + threadIdx.x, w = blockIdx.y, D = prm.cols, job = blockIdx.z;
-    if (c >= D) return;
-    const float* partial = prm.partial + w * prm.blocks * 3 * D + c;
-    float s = 0.0f;
-    if (job < 2) {
-        for (int64_t b = 0; b < prm.blocks; ++b) s += partial[(3 * b + job) * D];
-        static_cast<T*>(job == 0 ? prm.dpost : prm.dpre)[w * D + c] = from_float<T>(s);
-    } else {
-        const int64_t g = job - 2;
-        for (int64_t b = g * prm.chunks; b < (g + 1) * prm.chunks; ++b) s += partial[(3 * b + 2) * D];
-        static_cast<T*>(prm.dgate)[(w * prm.gates + g) * D + c] = from_float<T>(s);
+    __shared__ float slots[16][33];
+    const int64_t c = (int64_t)blockIdx.x * 32 + threadIdx.x % 32, w = blockIdx.z, D = prm.cols;
+    const int warp = threadIdx.x / 32;
+    for (int64_t job = blockIdx.y; job < 2 + (prm.chunks > 0 ? prm.gates : 0); job += gridDim.y) {
+        const int64_t b0 = job < 2 ? 0 : (job - 2) * prm.chunks, b1 = job < 2 ? prm.blocks : b0 + prm.chunks;
+        const float* partial = prm.partial + (w * prm.blocks * 3 + (job < 2 ? job : 2)) * D + c;
+        float s = 0.0f;
+        if (c < D) {
+#pragma unroll 4
+            for (int64_t b = b0 + warp; b < b1; b += 16) s += partial[b * 3 * D];
+        }
+        slots[warp][threadIdx.x % 32] = s;
+        __syncthreads();
+        if (warp == 0 && c < D) {
+            for (int k = 1; k < 16; ++k) s += slots[k][threadIdx.x];
+            T* out = static_cast<T*>(job == 0 ? prm.dpost : job == 1 ? prm.dpre : prm.dgate);
+            out[(job < 2 ? w : w * prm.gates + job - 2) * D + c] = from_float<T>(s);
+        }
+        __syncthreads();
     }
 }
 
-template <typename T>
-cudaError_t backward(const NormParams& prm, cudaStream_t stream)
+bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+// Threads of a CTA and CTAs of a cluster for a row of `slices` 16-byte slices: the fewest threads (a power of two of
+// warps) that hold it, up to 512, then a cluster.
+void shape_of_row(int64_t slices, int* threads, int* cluster)
 {
-    cudaError_t err = cudaFuncSetAttribute(rps_norm_backward_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, RPS_MAX_NORM_COLS * 4);
-    if (err != cudaSuccess) return err;
-    rps_norm_backward_kernel<T><<<dim3((unsigned)prm.blocks, (unsigned)prm.n), kThreads, prm.cols * 4, stream>>>(prm);
-    rps_norm_reduce_kernel<T><<<dim3((unsigned)ceil_div(prm.cols, 128), (unsigned)prm.n, (unsigned)(2 + (prm.chunks > 0 ? prm.gates : 0))), 128, 0, stream>>>(prm);
-    return cudaGetLastError();
+    *threads = 32, *cluster = 1;
+    while (*threads < kMostThreads && *threads < slices) *threads *= 2;
+    while (*threads * *cluster < slices) *cluster *= 2;
+}
+
+template <typename Kernel>
+cudaError_t launch_rows(Kernel kernel, const NormParams& prm, dim3 grid, int threads, cudaStream_t stream)
+{
+    cudaLaunchConfig_t config{};
+    config.gridDim = grid, config.blockDim = dim3((unsigned)threads), config.stream = stream;
+    cudaLaunchAttribute attribute{};
+    attribute.id = cudaLaunchAttributeClusterDimension;
+    attribute.val.clusterDim.x = (unsigned)prm.cluster, attribute.val.clusterDim.y = attribute.val.clusterDim.z = 1;
+    config.attrs = &attribute, config.numAttrs = prm.cluster > 1 ? 1 : 0;
+    return cudaLaunchKernelEx(&config, kernel, prm);
 }
 
 template <typename T>
-cudaError_t forward(const NormParams& prm, cudaStream_t stream)
+cudaError_t forward(NormParams prm, cudaStream_t stream)
 {
-    cudaError_t err = cudaFuncSetAttribute(rps_norm_forward_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, RPS_MAX_NORM_COLS * 4);
+    constexpr int W = Slice<T>::kWidth;
+    int threads = 0, sms = 0;
+    shape_of_row(ceil_div(prm.f_codes != nullptr ? prm.pitch : prm.cols, W), &threads, &prm.cluster);
+    cudaError_t err = sm_count(&sms);
     if (err != cudaSuccess) return err;
-    rps_norm_forward_kernel<T><<<(unsigned)(prm.n * prm.tokens), kThreads, prm.cols * 4, stream>>>(prm);
-    if ((err = cudaGetLastError()) != cudaSuccess || prm.f_codes == nullptr) return err;
-    PackParams pack{};
-    pack.f32 = prm.f32;
-    pack.rows = prm.n * prm.tokens;
-    pack.cols = pack.x_row = prm.cols;
-    pack.pitch = prm.pitch;
-    pack.groups = prm.groups;
-    pack.x = prm.f, pack.codes = prm.f_codes, pack.scales = prm.f_scales;
-    if ((err = launch_pack(pack, stream)) != cudaSuccess) return err;
-    pack.x = prm.h, pack.codes = prm.h_codes, pack.scales = prm.h_scales;
-    return launch_pack(pack, stream);
+    const bool aligned = prm.cols % W == 0 && aligned16(prm.x) && aligned16(prm.f) && aligned16(prm.gate) && aligned16(prm.post) &&
+                         aligned16(prm.pre) && aligned16(prm.h) && aligned16(prm.y) && prm.gate_worker % W == 0 && prm.post_worker % W == 0 &&
+                         prm.pre_worker % W == 0;
+    // 1024 threads of an SM are resident; more rows than that come round by round
+    const int64_t rows = prm.n * prm.tokens, resident = (int64_t)sms * (1024 / threads) / prm.cluster;
+    const dim3 grid((unsigned)((rows < resident ? rows : resident) * prm.cluster));
+    if (prm.f_codes != nullptr)
+        return aligned ? launch_rows(rps_norm_forward_kernel<T, true, true>, prm, grid, threads, stream)
+                       : launch_rows(rps_norm_forward_kernel<T, false, true>, prm, grid, threads, stream);
+    return aligned ? launch_rows(rps_norm_forward_kernel<T, true, false>, prm, grid, threads, stream)
+                   : launch_rows(rps_norm_forward_kernel<T, false, false>, prm, grid, threads, stream);
+}
+
+template <typename T>
+cudaError_t backward(NormParams prm, cudaStream_t stream)
+{
+    constexpr int W = Slice<T>::kWidth;
+    int threads = 0;
+    shape_of_row(ceil_div(prm.cols, W), &threads, &prm.cluster);
+    const bool values = prm.packed || (aligned16(prm.f) && aligned16(prm.h_in));
+    const bool aligned = values && prm.cols % W == 0 && aligned16(prm.dh) && aligned16(prm.dy) && aligned16(prm.gate) && aligned16(prm.post) &&
+                         aligned16(prm.pre) && aligned16(prm.dx) && aligned16(prm.df) && aligned16(prm.dgate) && prm.gate_worker % W == 0 &&
+                         prm.post_worker % W == 0 && prm.pre_worker % W == 0;
+    const dim3 grid((unsigned)(prm.blocks * prm.cluster), (unsigned)prm.n);
+    cudaError_t err;
+    if (prm.packed)
+        err = aligned ? launch_rows(rps_norm_backward_kernel<T, true, true>, prm, grid, threads, stream)
+                      : launch_rows(rps_norm_backward_kernel<T, false, true>, prm, grid, threads, stream);
+    else
+        err = aligned ? launch_rows(rps_norm_backward_kernel<T, true, false>, prm, grid, threads, stream)
+                      : launch_rows(rps_norm_backward_kernel<T, false, false>, prm, grid, threads, stream);
+    if (err != cudaSuccess) return err;
+    const int64_t jobs = 2 + (prm.chunks > 0 ? prm.gates : 0);
+    rps_norm_reduce_kernel<T><<<dim3((unsigned)ceil_div(prm.cols, 32), (unsigned)(jobs < 4096 ? jobs : 4096), (unsigned)prm.n), 512, 0, stream>>>(prm);
+    return cudaGetLastError();
 }
 
 }  // namespace
 
 void plan_norm_backward(NormParams* prm)
 {
-    // about four blocks per SM over all workers
-    const int64_t want = ceil_div(148 * 4, prm->n), rows = prm->rows_per_gate;
-    const int64_t target = prm->tokens / want > 0 ? prm->tokens / want : 1;
-    if (rows <= target) {
-        prm->chunks = 0;
-        prm->rows_per_block = target / rows * rows;
-        prm->blocks = ceil_div(prm->tokens, prm->rows_per_block);
-    } else {
-        prm->rows_per_block = target;
-        prm->chunks = ceil_div(rows, target);
-        prm->blocks = prm->gates * prm->chunks;
-    }
+    int threads = 0, cluster = 0;
+    shape_of_row(ceil_div(prm->cols, prm->f32 ? Slice<float>::kWidth : Slice<bf16>::kWidth), &threads, &cluster);
+    // as many blocks over all workers as are resident at once (512 threads of each of the 148 SMs); of the two nearest ways
+    // to cut the rows the one whose longest SM has fewer of them
+    int64_t want = (int64_t)148 * (kMostThreads / threads) / cluster / prm->n;
+    if (want < 1) want = 1;
+    const int64_t rows = prm->rows_per_gate, target = ceil_div(prm->tokens, want);
+    const bool whole = rows <= target;
+    const auto cut = [&](int64_t k) {  // k gate groups a block, or k blocks a gate group
+        prm->chunks = whole ? 0 : k;
+        prm->rows_per_block = whole ? k * rows : ceil_div(rows, k);
+        prm->blocks = whole ? ceil_div(prm->tokens, prm->rows_per_block) : prm->gates * k;
+        return ceil_div(prm->blocks, want) * prm->rows_per_block;
+    };
+    const int64_t k = whole ? target / rows : rows / target;
+    if (cut(k + 1) > cut(k)) return;
+    cut(k + 1);
 }
 
 cudaError_t launch_norm_forward(const NormParams& prm, cudaStream_t stream)

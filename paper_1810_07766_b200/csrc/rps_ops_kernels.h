@@ -127,6 +127,7 @@ cudaError_t launch_unpack_planes(const PackParams& prm, cudaStream_t stream);
 // ---------------------------------------------------------------------------------------------------- norm
 struct NormParams {
     int f32, n, packed;
+    int cluster;  // CTAs that share a row
     int64_t tokens, cols, gates, rows_per_gate;
     int64_t post_worker, pre_worker, gate_worker;
     float scale, eps;

@@ -1,87 +1,177 @@
 // Activations in 8 bits: a scale for each 128 columns of a row.
-#include "rps_ops_kernels.h"
+//
+// Bound by memory.  A unit of work is a warp's worth of slices of one row (256 columns of bf16, 128 of fp32); a warp takes
+// kUnits of them at a time, so that their loads are all on their way before the first is used.
+#include "rps_rows.cuh"
 
 namespace rps_ops {
 namespace {
 
-constexpr int kGroup = RPS_PACK_GROUP;
-constexpr float kSmallest = 0x1p-100f;  // a group with nothing larger is kept as zeros: 127 / max stays finite
+constexpr int kThreads = 256, kUnits = 4;
 
-// One warp per group, four columns a lane.
-template <typename T>
-__global__ void __launch_bounds__(256) rps_pack_kernel(const PackParams prm)
+struct Place {
+    int64_t row;
+    int c;
+};
+
+// Column of this lane in unit u; units_per_row of them to a row.
+template <int W>
+__device__ __forceinline__ Place place(uint32_t u, uint32_t units_per_row)
 {
-    const int64_t g = (int64_t)blockIdx.x * 8 + threadIdx.x / 32;
-    if (g >= prm.rows * prm.groups) return;
-    const int lane = threadIdx.x % 32;
-    const int64_t row = g / prm.groups, c0 = g % prm.groups * kGroup + lane * 4;
-    const T* x = static_cast<const T*>(prm.x) + row * prm.x_row;
-    float v[4], top = 0.0f;
-    bool finite = true;
-    for (int j = 0; j < 4; ++j) {
-        v[j] = c0 + j < prm.cols ? to_float<T>(x[c0 + j]) : 0.0f;
-        finite &= fabsf(v[j]) <= 3.402823466e38f;
-        top = fmaxf(top, fabsf(v[j]));
-    }
-    for (int s = 16; s > 0; s /= 2) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, s));
-    finite = __all_sync(0xFFFFFFFFu, finite);
-    const bool zero = !finite || top < kSmallest;
-    const float factor = zero ? 0.0f : __fdiv_rn(127.0f, top);
-    for (int j = 0; j < 4; ++j)
-        if (c0 + j < prm.pitch) prm.codes[row * prm.pitch + c0 + j] = zero ? 0 : (int8_t)__float2int_rn(__fmul_rn(v[j], factor));
-    if (lane == 0) prm.scales[g] = !finite ? nanf("") : zero ? 0.0f : __fmul_rn(top, 1.0f / 127.0f);
+    const uint32_t row = u / units_per_row;
+    return {row, (int)((u - row * units_per_row) * 32 + threadIdx.x % 32) * W};
 }
 
-template <typename T>
-__global__ void __launch_bounds__(256) rps_unpack_kernel(const PackParams prm)
+template <typename T, bool ALIGNED>
+__global__ void __launch_bounds__(kThreads) rps_pack_kernel(const PackParams prm, uint32_t units, uint32_t units_per_row)
 {
-    const int64_t row = blockIdx.x;
-    for (int64_t c = threadIdx.x; c < prm.cols; c += blockDim.x)
-        static_cast<T*>(prm.out)[row * prm.x_row + c] =
-            from_float<T>(__fmul_rn((float)prm.codes[row * prm.pitch + c], prm.scales[row * prm.groups + c / kGroup]));
-}
-
-__global__ void __launch_bounds__(256) rps_unpack_planes_kernel(const PackParams prm)
-{
-    const int64_t row = blockIdx.x, w = row / prm.tokens;
-    bf16* dst = prm.planes_out + w * prm.dst_worker + row % prm.tokens * prm.dst_row;
-    for (int64_t c = threadIdx.x; c < prm.dst_row; c += blockDim.x) {
-        const float v = c < prm.cols ? __fmul_rn((float)prm.codes[row * prm.pitch + c], prm.scales[row * prm.groups + c / kGroup]) : 0.0f;
-        if (prm.planes == 1) {
-            dst[c] = __float2bfloat16_rn(v);
-        } else {
-            bf16 p[3];
-            split_planes(v, p);
-            for (int q = 0; q < 3; ++q) dst[q * prm.dst_plane + c] = p[q];
+    constexpr int W = Slice<T>::kWidth;
+    const int D = (int)prm.cols;
+    const uint32_t warp = blockIdx.x * (kThreads / 32) + threadIdx.x / 32, step = gridDim.x * (kThreads / 32);
+    for (uint64_t u0 = warp; u0 < units; u0 += (uint64_t)step * kUnits) {
+        uint4 x[kUnits];
+        Place at[kUnits];
+#pragma unroll
+        for (int i = 0; i < kUnits; ++i) {
+            const uint64_t u = u0 + (uint64_t)i * step;
+            if (u >= units) break;
+            at[i] = place<W>((uint32_t)u, units_per_row);
+            x[i] = load_slice<T, ALIGNED, true>(static_cast<const T*>(prm.x) + at[i].row * prm.x_row, at[i].c, D);
+        }
+#pragma unroll
+        for (int i = 0; i < kUnits; ++i) {
+            if (u0 + (uint64_t)i * step >= units) break;
+            const int c = at[i].c;
+            float v[W];
+            widen(x[i], v);
+            pack_slice(v, c < prm.pitch ? prm.codes + at[i].row * prm.pitch + c : nullptr,
+                       c < D ? prm.scales + at[i].row * prm.groups + c / RPS_PACK_GROUP : nullptr);
         }
     }
+}
+
+template <int W>
+__device__ __forceinline__ void load_codes(const PackParams& prm, const Place& at, Codes<W>& codes, float& scale)
+{
+    codes.clear(), scale = 0.0f;
+    if (at.c < prm.cols) {
+        codes.load(prm.codes + at.row * prm.pitch + at.c);
+        scale = __ldg(prm.scales + at.row * prm.groups + at.c / RPS_PACK_GROUP);
+    }
+}
+
+template <typename T, bool ALIGNED>
+__global__ void __launch_bounds__(kThreads) rps_unpack_kernel(const PackParams prm, uint32_t units, uint32_t units_per_row)
+{
+    constexpr int W = Slice<T>::kWidth;
+    const uint32_t warp = blockIdx.x * (kThreads / 32) + threadIdx.x / 32, step = gridDim.x * (kThreads / 32);
+    for (uint64_t u0 = warp; u0 < units; u0 += (uint64_t)step * kUnits) {
+        Codes<W> codes[kUnits];
+        float scale[kUnits];
+        Place at[kUnits];
+#pragma unroll
+        for (int i = 0; i < kUnits; ++i) {
+            const uint64_t u = u0 + (uint64_t)i * step;
+            if (u >= units) break;
+            at[i] = place<W>((uint32_t)u, units_per_row);
+            load_codes(prm, at[i], codes[i], scale[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < kUnits; ++i) {
+            if (u0 + (uint64_t)i * step >= units) break;
+            float v[W];
+            codes[i].values(scale[i], v);
+            store_slice<T, ALIGNED>(static_cast<T*>(prm.out) + at[i].row * prm.x_row, at[i].c, (int)prm.cols, narrow(v));
+        }
+    }
+}
+
+// The values as operands of a product: bf16, or the three bf16 parts of fp32 values; rows of dst_row columns, zero behind the last.
+template <typename T>
+__global__ void __launch_bounds__(kThreads) rps_unpack_planes_kernel(const PackParams prm, uint32_t units, uint32_t units_per_row)
+{
+    constexpr int W = 8;
+    const uint32_t warp = blockIdx.x * (kThreads / 32) + threadIdx.x / 32, step = gridDim.x * (kThreads / 32);
+    for (uint64_t u0 = warp; u0 < units; u0 += (uint64_t)step * kUnits) {
+        Codes<W> codes[kUnits];
+        float scale[kUnits];
+        Place at[kUnits];
+#pragma unroll
+        for (int i = 0; i < kUnits; ++i) {
+            const uint64_t u = u0 + (uint64_t)i * step;
+            if (u >= units) break;
+            at[i] = place<W>((uint32_t)u, units_per_row);
+            load_codes(prm, at[i], codes[i], scale[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < kUnits; ++i) {
+            if (u0 + (uint64_t)i * step >= units) break;
+            if (at[i].c >= prm.dst_row) continue;
+            const int64_t w = at[i].row / prm.tokens;
+            bf16* dst = prm.planes_out + w * prm.dst_worker + (at[i].row - w * prm.tokens) * prm.dst_row + at[i].c;
+            float v[W];
+            codes[i].values(scale[i], v);
+            if constexpr (sizeof(T) == 2) {
+                *reinterpret_cast<uint4*>(dst) = narrow(v);
+            } else {
+                uint4 parts[3];
+                split_slice(v, parts);
+#pragma unroll
+                for (int q = 0; q < 3; ++q) *reinterpret_cast<uint4*>(dst + q * prm.dst_plane) = parts[q];
+            }
+        }
+    }
+}
+
+template <typename Kernel>
+cudaError_t launch_units(Kernel kernel, const PackParams& prm, int64_t row_cols, int width, cudaStream_t stream)
+{
+    int sms = 0;
+    cudaError_t err = sm_count(&sms);
+    if (err != cudaSuccess) return err;
+    const int64_t units_per_row = ceil_div(row_cols, 32 * width), units = prm.rows * units_per_row;
+    if (units >= 1ll << 32) return cudaErrorInvalidValue;  // 2 TB of activations
+    const int64_t blocks = ceil_div(units, kThreads / 32), resident = (int64_t)sms * 8;
+    kernel<<<(unsigned)(blocks < resident ? blocks : resident), kThreads, 0, stream>>>(prm, (uint32_t)units, (uint32_t)units_per_row);
+    return cudaGetLastError();
+}
+
+template <typename T>
+bool aligned_rows(const void* p, const PackParams& prm)
+{
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && prm.x_row % Slice<T>::kWidth == 0 && prm.cols % Slice<T>::kWidth == 0;
+}
+
+template <typename T>
+cudaError_t pack(const PackParams& prm, cudaStream_t stream)
+{
+    return aligned_rows<T>(prm.x, prm) ? launch_units(rps_pack_kernel<T, true>, prm, prm.pitch, Slice<T>::kWidth, stream)
+                                       : launch_units(rps_pack_kernel<T, false>, prm, prm.pitch, Slice<T>::kWidth, stream);
+}
+
+template <typename T>
+cudaError_t unpack(const PackParams& prm, cudaStream_t stream)
+{
+    return aligned_rows<T>(prm.out, prm) ? launch_units(rps_unpack_kernel<T, true>, prm, prm.cols, Slice<T>::kWidth, stream)
+                                         : launch_units(rps_unpack_kernel<T, false>, prm, prm.cols, Slice<T>::kWidth, stream);
 }
 
 }  // namespace
 
 cudaError_t launch_pack(const PackParams& prm, cudaStream_t stream)
 {
-    const unsigned grid = (unsigned)ceil_div(prm.rows * prm.groups, 8);
-    if (prm.f32)
-        rps_pack_kernel<float><<<grid, 256, 0, stream>>>(prm);
-    else
-        rps_pack_kernel<bf16><<<grid, 256, 0, stream>>>(prm);
-    return cudaGetLastError();
+    return prm.f32 ? pack<float>(prm, stream) : pack<bf16>(prm, stream);
 }
 
 cudaError_t launch_unpack(const PackParams& prm, cudaStream_t stream)
 {
-    if (prm.f32)
-        rps_unpack_kernel<float><<<(unsigned)prm.rows, 256, 0, stream>>>(prm);
-    else
-        rps_unpack_kernel<bf16><<<(unsigned)prm.rows, 256, 0, stream>>>(prm);
-    return cudaGetLastError();
+    return prm.f32 ? unpack<float>(prm, stream) : unpack<bf16>(prm, stream);
 }
 
 cudaError_t launch_unpack_planes(const PackParams& prm, cudaStream_t stream)
 {
-    rps_unpack_planes_kernel<<<(unsigned)prm.rows, 256, 0, stream>>>(prm);
-    return cudaGetLastError();
+    return prm.f32 ? launch_units(rps_unpack_planes_kernel<float>, prm, prm.dst_row, 8, stream)
+                   : launch_units(rps_unpack_planes_kernel<bf16>, prm, prm.dst_row, 8, stream);
 }
 
 }  // namespace rps_ops

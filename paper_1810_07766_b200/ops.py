@@ -86,10 +86,10 @@ def _library() -> ctypes.CDLL:
     return _lib
 
 
-def _call(name: str, device: torch.device, *args) -> None:
+def _call(name: str, device: int, *args) -> None:
     """One call of the library with the tensors' device current."""
-    lib = _library()
-    if torch.cuda.current_device() == device.index:
+    lib = _lib or _library()
+    if torch.cuda.current_device() == device:
         rc = getattr(lib, name)(*args)
     else:
         with torch.cuda.device(device):
@@ -98,28 +98,52 @@ def _call(name: str, device: torch.device, *args) -> None:
         raise RPSError(rc, name, lib.rps_ops_last_error().decode())
 
 
+# What a call says about its arguments' types, shapes and strides is checked and described to the library once; the checked
+# descriptions are kept by exactly those (never by an address or a value), as a small call's time is mostly such work.
+_plans: dict = {}
+_MOST_PLANS = 4096
+
+
+def _keep(key, plan):
+    if len(_plans) >= _MOST_PLANS:
+        _plans.clear()
+    _plans[key] = plan
+    return plan
+
+
+def _device_of(**tensors) -> int:
+    """Index of the one CUDA device that all of them are on."""
+    device = -1
+    for name, t in tensors.items():
+        if not isinstance(t, torch.Tensor) or not t.is_cuda:
+            raise ValueError(f"{name} must be a CUDA tensor")
+        if device < 0:
+            device = t.get_device()
+        elif t.get_device() != device:
+            raise ValueError(f"{name} must be on the device of the other tensors")
+    return device
+
+
 def check(device: Optional[torch.device] = None) -> None:
     """Synchronises the current stream of the device and raises if a kernel of an earlier call gave up (``rps_ops_check``)."""
-    device = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
-    _call("rps_ops_check", device, _stream(device))
+    index = torch.cuda.current_device() if device is None else torch.empty(0, device=device).get_device()
+    _call("rps_ops_check", index, _stream(index))
 
 
-def _stream(device: torch.device) -> int:
-    return torch.cuda.current_stream(device).cuda_stream
+def _stream(device: int) -> int:
+    return torch._C._cuda_getCurrentRawStream(device)
 
 
-def _workspace(device: torch.device, size: int) -> torch.Tensor:
+def _workspace(like: torch.Tensor, size: int) -> torch.Tensor:
     # torch's allocations start on 512-byte boundaries; memory of the current stream goes back to it when the tensor is dropped
-    return torch.empty(max(size, 1), dtype=torch.uint8, device=device)
+    return torch.empty(size, dtype=torch.uint8, device=like.device)
 
 
 def _check(name: str, t: torch.Tensor, like: Optional[torch.Tensor], shape: Tuple[int, ...]) -> None:
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
-        raise ValueError(f"{name} must be a CUDA tensor")
     if t.dtype not in _DTYPE:
         raise ValueError(f"{name} must be float32 or bfloat16, not {t.dtype}")
-    if like is not None and (t.dtype != like.dtype or t.device != like.device):
-        raise ValueError(f"{name} must have the type and device of the other tensors ({like.dtype}, {like.device})")
+    if like is not None and t.dtype != like.dtype:
+        raise ValueError(f"{name} must have the type of the other tensors ({like.dtype})")
     if tuple(t.shape) != shape:
         raise ValueError(f"{name} must have shape {shape}, not {tuple(t.shape)}")
 
@@ -151,33 +175,49 @@ def _parameter_stride(name: str, t: torch.Tensor) -> int:
 
 
 # ------------------------------------------------------------------------------------------------------------ the loss
-def _lce_desc(hidden, weight, targets, ignore_index, reduction):
+class _LcePlan(NamedTuple):
+    desc: object
+    tokens_shape: Tuple[int, ...]
+    loss_shape: Tuple[int, ...]
+    workspace: Tuple[int, int]       # forward, backward
+
+
+def _lce_plan(hidden, weight, targets, ignore_index, reduction, dweight=None) -> _LcePlan:
+    at = weight.data_ptr() & 15
+    key = ("lce", hidden.dtype, hidden.shape, hidden.stride(), weight.dtype, weight.shape, weight.stride(), at, targets.dtype, targets.shape,
+           ignore_index, reduction) + (() if dweight is None else (dweight.dtype, dweight.shape, dweight.stride()))
+    plan = _plans.get(key)
+    if plan is not None:
+        return plan
     if reduction not in _REDUCTION:
         raise ValueError(f"reduction must be one of {sorted(_REDUCTION)}")
-    if not isinstance(hidden, torch.Tensor) or hidden.dim() not in (2, 3):
+    if hidden.dim() not in (2, 3):
         raise ValueError("hidden must be a tensor [n, tokens, cols] or [tokens, cols]")
     lead = tuple(hidden.shape[:-2])
     tokens, cols = hidden.shape[-2:]
     _check("hidden", hidden, None, tuple(hidden.shape))
-    if not isinstance(weight, torch.Tensor) or weight.dim() != hidden.dim():
+    if weight.dim() != hidden.dim():
         raise ValueError("weight must be [n, vocab, cols] with hidden [n, tokens, cols], or [vocab, cols] with [tokens, cols]")
     vocab = weight.shape[-2]
     _check("weight", weight, hidden, lead + (vocab, cols))
-    if not isinstance(targets, torch.Tensor) or targets.dtype != torch.int64 or targets.device != hidden.device:
-        raise ValueError("targets must be an int64 tensor on the device of hidden")
-    if tuple(targets.shape) != lead + (tokens,):
-        raise ValueError(f"targets must have shape {lead + (tokens,)}, not {tuple(targets.shape)}")
+    if targets.dtype != torch.int64 or tuple(targets.shape) != lead + (tokens,):
+        raise ValueError(f"targets must be int64 of shape {lead + (tokens,)}, not {targets.dtype} of {tuple(targets.shape)}")
     d = rps_lce_desc(dtype=_DTYPE[hidden.dtype], reduction=_REDUCTION[reduction], n=lead[0] if lead else 1, tokens=tokens,
                      vocab=vocab, cols=cols, ignore_index=ignore_index)
     d.hidden_row, d.hidden_worker = _matrix_strides("hidden", hidden)
     d.weight_row, d.weight_worker = _matrix_strides("weight", weight)
-    return d, lead
-
-
-def _lce_workspace(d, weight, backward):
-    size = ctypes.c_size_t()
-    _call("rps_lce_workspace", weight.device, ctypes.byref(d), weight.data_ptr(), backward, ctypes.byref(size))
-    return _workspace(weight.device, size.value), size.value
+    if dweight is not None:
+        _check("dweight", dweight, hidden, tuple(weight.shape))
+        d.dweight_row, d.dweight_worker = _matrix_strides("dweight", dweight)
+    else:
+        d.dweight_row, d.dweight_worker = cols, vocab * cols
+    sizes = []
+    for backward in (0, 1):
+        size = ctypes.c_size_t()
+        _call("rps_lce_workspace", hidden.get_device(), ctypes.byref(d), at, backward, ctypes.byref(size))
+        sizes.append(size.value)
+    loss_shape = lead + ((tokens,) if reduction == "none" else ())
+    return _keep(key, _LcePlan(ctypes.byref(d), lead + (tokens,), loss_shape, tuple(sizes)))
 
 
 def linear_cross_entropy_forward(hidden: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor, *,
@@ -187,13 +227,14 @@ def linear_cross_entropy_forward(hidden: torch.Tensor, weight: torch.Tensor, tar
     hidden ``[n, tokens, cols]``, weight ``[n, vocab, cols]``, targets int64 ``[n, tokens]`` (all without ``n`` for a single
     worker).  loss is float32: one value for each worker ("mean" over its tokens that are not ignored, "sum") or each token
     ("none"); lse, float32 ``[n, tokens]``, is what the backward pass wants.  Ignored tokens have loss and lse 0."""
-    d, lead = _lce_desc(hidden, weight, targets, ignore_index, reduction)
+    device = _device_of(hidden=hidden, weight=weight, targets=targets)
+    plan = _lce_plan(hidden, weight, targets, ignore_index, reduction)
     targets = targets.contiguous()
-    loss = torch.empty(lead + ((d.tokens,) if reduction == "none" else ()), dtype=torch.float32, device=hidden.device)
-    lse = torch.empty(lead + (d.tokens,), dtype=torch.float32, device=hidden.device)
-    ws, size = _lce_workspace(d, weight, 0)
-    _call("rps_lce_forward", hidden.device, ctypes.byref(d), hidden.data_ptr(), weight.data_ptr(), targets.data_ptr(),
-          loss.data_ptr(), lse.data_ptr(), ws.data_ptr(), size, _stream(hidden.device))
+    loss = torch.empty(plan.loss_shape, dtype=torch.float32, device=hidden.device)
+    lse = torch.empty(plan.tokens_shape, dtype=torch.float32, device=hidden.device)
+    ws = _workspace(hidden, plan.workspace[0])
+    _call("rps_lce_forward", device, plan.desc, hidden.data_ptr(), weight.data_ptr(), targets.data_ptr(), loss.data_ptr(), lse.data_ptr(),
+          ws.data_ptr(), plan.workspace[0], _stream(device))
     return loss, lse
 
 
@@ -203,22 +244,21 @@ def linear_cross_entropy_backward(dloss: torch.Tensor, hidden: torch.Tensor, wei
     """(dhidden, dweight) for the gradient ``dloss`` (float32, shaped as the loss) of the forward call with the same
     arguments (``rps_lce_backward``).  ``dweight``, if given, is written (not added to) and may be strided, a view into
     the rows of a larger array for instance."""
-    d, lead = _lce_desc(hidden, weight, targets, ignore_index, reduction)
+    device = _device_of(hidden=hidden, weight=weight, targets=targets, dloss=dloss, lse=lse)
+    if dweight is not None:
+        _device_of(hidden=hidden, dweight=dweight)
+    plan = _lce_plan(hidden, weight, targets, ignore_index, reduction, dweight)
     targets = targets.contiguous()
-    want = lead + ((d.tokens,) if reduction == "none" else ())
-    for name, t, shape in (("dloss", dloss, want), ("lse", lse, lead + (d.tokens,))):
-        if not isinstance(t, torch.Tensor) or t.dtype != torch.float32 or t.device != hidden.device or tuple(t.shape) != shape:
-            raise ValueError(f"{name} must be a float32 tensor of shape {shape} on the device of hidden")
+    for name, t, shape in (("dloss", dloss, plan.loss_shape), ("lse", lse, plan.tokens_shape)):
+        if t.dtype != torch.float32 or t.shape != shape:
+            raise ValueError(f"{name} must be a float32 tensor of shape {shape}")
         _dense(name, t)
     if dweight is None:
         dweight = torch.empty(weight.shape, dtype=weight.dtype, device=weight.device)
-    else:
-        _check("dweight", dweight, hidden, tuple(weight.shape))
-    d.dweight_row, d.dweight_worker = _matrix_strides("dweight", dweight)
     dhidden = torch.empty(hidden.shape, dtype=hidden.dtype, device=hidden.device)
-    ws, size = _lce_workspace(d, weight, 1)
-    _call("rps_lce_backward", hidden.device, ctypes.byref(d), hidden.data_ptr(), weight.data_ptr(), targets.data_ptr(),
-          lse.data_ptr(), dloss.data_ptr(), dhidden.data_ptr(), dweight.data_ptr(), ws.data_ptr(), size, _stream(hidden.device))
+    ws = _workspace(hidden, plan.workspace[1])
+    _call("rps_lce_backward", device, plan.desc, hidden.data_ptr(), weight.data_ptr(), targets.data_ptr(), lse.data_ptr(), dloss.data_ptr(),
+          dhidden.data_ptr(), dweight.data_ptr(), ws.data_ptr(), plan.workspace[1], _stream(device))
     return dhidden, dweight
 
 
@@ -257,48 +297,58 @@ class PackedActivation(NamedTuple):
 def packed_like(shape: Tuple[int, ...], dtype: torch.dtype, device: torch.device) -> PackedActivation:
     """Room for the packed form of a tensor of this shape (the codes behind the last column are written by pack calls)."""
     cols = shape[-1]
-    codes = torch.empty(tuple(shape[:-1]) + (-(-cols // 16) * 16,), dtype=torch.int8, device=device)
-    scales = torch.empty(tuple(shape[:-1]) + (-(-cols // GROUP),), dtype=torch.float32, device=device)
+    lead = tuple(shape[:-1])
+    codes = torch.empty(lead + (-(-cols // 16) * 16,), dtype=torch.int8, device=device)
+    scales = torch.empty(lead + (-(-cols // GROUP),), dtype=torch.float32, device=device)
     return PackedActivation(codes, scales, cols, dtype)
 
 
-def _check_packed(name: str, p: PackedActivation, lead: Optional[Tuple[int, ...]] = None) -> None:
+def _packed_shape(name: str, p: PackedActivation) -> Tuple[int, ...]:
+    """Checks ``p`` and gives the shape of the tensor that it stands for."""
     if not isinstance(p, PackedActivation):
         raise ValueError(f"{name} must be a PackedActivation")
     c, s = p.codes, p.scales
-    if not (c.is_cuda and s.is_cuda and c.device == s.device and c.dtype == torch.int8 and s.dtype == torch.float32):
-        raise ValueError(f"{name}: codes must be int8 and scales float32, on one CUDA device")
+    key = ("packed", c.dtype, c.shape, c.stride(), s.dtype, s.shape, s.stride(), p.columns, p.dtype)
+    shape = _plans.get(key)
+    if shape is not None:
+        return shape
+    if c.dtype != torch.int8 or s.dtype != torch.float32:
+        raise ValueError(f"{name}: codes must be int8 and scales float32")
     if p.dtype not in _DTYPE:
         raise ValueError(f"{name}: dtype must be float32 or bfloat16")
     if p.columns < 1 or c.dim() < 1 or c.shape[-1] != -(-p.columns // 16) * 16 or tuple(s.shape) != tuple(c.shape[:-1]) + (-(-p.columns // GROUP),):
         raise ValueError(f"{name}: codes {tuple(c.shape)} and scales {tuple(s.shape)} do not fit {p.columns} columns")
-    if lead is not None and tuple(c.shape[:-1]) != lead:
-        raise ValueError(f"{name} must hold {lead} rows, not {tuple(c.shape[:-1])}")
     _dense(f"{name}.codes", c)
     _dense(f"{name}.scales", s)
+    return _keep(key, tuple(c.shape[:-1]) + (p.columns,))
 
 
 def pack_activation(x: torch.Tensor) -> PackedActivation:
     """``x`` in 8 bits (``rps_pack``).  x is ``[..., columns]`` and contiguous, or a matrix with contiguous rows."""
-    if not isinstance(x, torch.Tensor) or x.dim() < 1 or x.shape[-1] < 1:
-        raise ValueError("x must be a tensor [..., columns] with at least one column")
-    _check("x", x, None, tuple(x.shape))
-    row = _matrix_strides("x", x)[0] if x.dim() == 2 else x.shape[-1]
-    if x.dim() != 2:
-        _dense("x", x)
-    p = packed_like(tuple(x.shape), x.dtype, x.device)
-    _call("rps_pack", x.device, _DTYPE[x.dtype], x.numel() // x.shape[-1], x.shape[-1], x.data_ptr(), row, p.codes.data_ptr(),
-          p.scales.data_ptr(), _stream(x.device))
+    device = _device_of(x=x)
+    key = ("pack", x.dtype, x.shape, x.stride())
+    plan = _plans.get(key)
+    if plan is None:
+        if x.dim() < 1 or x.shape[-1] < 1:
+            raise ValueError("x must be a tensor [..., columns] with at least one column")
+        _check("x", x, None, tuple(x.shape))
+        row = _matrix_strides("x", x)[0] if x.dim() == 2 else x.shape[-1]
+        if x.dim() != 2:
+            _dense("x", x)
+        plan = _keep(key, (_DTYPE[x.dtype], x.numel() // x.shape[-1], x.shape[-1], row))
+    dtype, rows, cols, row = plan
+    p = packed_like(x.shape, x.dtype, x.device)
+    _call("rps_pack", device, dtype, rows, cols, x.data_ptr(), row, p.codes.data_ptr(), p.scales.data_ptr(), _stream(device))
     return p
 
 
 def unpack_activation(packed: PackedActivation) -> torch.Tensor:
     """The values that ``packed`` stands for, in its dtype (``rps_unpack``)."""
-    _check_packed("packed", packed)
-    c = packed.codes
-    out = torch.empty(tuple(c.shape[:-1]) + (packed.columns,), dtype=packed.dtype, device=c.device)
-    _call("rps_unpack", c.device, _DTYPE[packed.dtype], out.numel() // packed.columns, packed.columns, c.data_ptr(),
-          packed.scales.data_ptr(), out.data_ptr(), packed.columns, _stream(c.device))
+    shape = _packed_shape("packed", packed)
+    device = _device_of(codes=packed.codes, scales=packed.scales)
+    out = torch.empty(shape, dtype=packed.dtype, device=packed.codes.device)
+    _call("rps_unpack", device, _DTYPE[packed.dtype], out.numel() // packed.columns, packed.columns, packed.codes.data_ptr(),
+          packed.scales.data_ptr(), out.data_ptr(), packed.columns, _stream(device))
     return out
 
 
@@ -306,25 +356,37 @@ def packed_weight_grad(dy: torch.Tensor, packed: PackedActivation, *, dweight: O
     """``dy.mT @ x`` for the values x that ``packed`` stands for (``rps_packed_wgrad``): the weight gradient
     ``[n, outs, columns]`` of ``y = x @ weight.mT`` out of dy ``[n, tokens, outs]``.  ``dweight`` as in
     ``linear_cross_entropy_backward``."""
-    if not isinstance(dy, torch.Tensor) or dy.dim() not in (2, 3) or dy.shape[-1] < 1:
-        raise ValueError("dy must be a tensor [n, tokens, outs] or [tokens, outs]")
-    _check("dy", dy, None, tuple(dy.shape))
-    lead, (tokens, outs) = tuple(dy.shape[:-2]), dy.shape[-2:]
-    _check_packed("packed", packed, lead + (tokens,))
-    if packed.dtype != dy.dtype or packed.codes.device != dy.device:
-        raise ValueError("dy and packed must have one type and device")
-    d = rps_wgrad_desc(dtype=_DTYPE[dy.dtype], n=lead[0] if lead else 1, tokens=tokens, outs=outs, cols=packed.columns)
-    d.dy_row, d.dy_worker = _matrix_strides("dy", dy)
+    shape = _packed_shape("packed", packed)
+    device = _device_of(dy=dy, codes=packed.codes, scales=packed.scales)
+    if dweight is not None:
+        _device_of(dy=dy, dweight=dweight)
+    at = dy.data_ptr() & 15
+    key = ("wgrad", dy.dtype, dy.shape, dy.stride(), at, shape, packed.dtype) + (() if dweight is None else (dweight.dtype, dweight.shape, dweight.stride()))
+    plan = _plans.get(key)
+    if plan is None:
+        if dy.dim() not in (2, 3) or dy.shape[-1] < 1:
+            raise ValueError("dy must be a tensor [n, tokens, outs] or [tokens, outs]")
+        _check("dy", dy, None, tuple(dy.shape))
+        lead, (tokens, outs), cols = tuple(dy.shape[:-2]), dy.shape[-2:], packed.columns
+        if shape != lead + (tokens, cols):
+            raise ValueError(f"packed must stand for a tensor {lead + (tokens, cols)}, not {shape}")
+        if packed.dtype != dy.dtype:
+            raise ValueError("dy and packed must have one type")
+        d = rps_wgrad_desc(dtype=_DTYPE[dy.dtype], n=lead[0] if lead else 1, tokens=tokens, outs=outs, cols=cols)
+        d.dy_row, d.dy_worker = _matrix_strides("dy", dy)
+        d.dweight_row, d.dweight_worker = cols, outs * cols
+        if dweight is not None:
+            _check("dweight", dweight, dy, lead + (outs, cols))
+            d.dweight_row, d.dweight_worker = _matrix_strides("dweight", dweight)
+        size = ctypes.c_size_t()
+        _call("rps_wgrad_workspace", device, ctypes.byref(d), at, ctypes.byref(size))
+        plan = _keep(key, (ctypes.byref(d), lead + (outs, cols), size.value))
+    desc, out_shape, size = plan
     if dweight is None:
-        dweight = torch.empty(lead + (outs, packed.columns), dtype=dy.dtype, device=dy.device)
-    else:
-        _check("dweight", dweight, dy, lead + (outs, packed.columns))
-    d.dweight_row, d.dweight_worker = _matrix_strides("dweight", dweight)
-    size = ctypes.c_size_t()
-    _call("rps_wgrad_workspace", dy.device, ctypes.byref(d), dy.data_ptr(), ctypes.byref(size))
-    ws = _workspace(dy.device, size.value)
-    _call("rps_packed_wgrad", dy.device, ctypes.byref(d), dy.data_ptr(), packed.codes.data_ptr(), packed.scales.data_ptr(),
-          dweight.data_ptr(), ws.data_ptr(), size.value, _stream(dy.device))
+        dweight = torch.empty(out_shape, dtype=dy.dtype, device=dy.device)
+    ws = _workspace(dy, size)
+    _call("rps_packed_wgrad", device, desc, dy.data_ptr(), packed.codes.data_ptr(), packed.scales.data_ptr(), dweight.data_ptr(), ws.data_ptr(),
+          size, _stream(device))
     return dweight
 
 
@@ -355,20 +417,35 @@ def linear_8bit(x: torch.Tensor, weight: torch.Tensor) -> torch.Tensor:
 # ------------------------------------------------------------------------------------------------- norms around a block
 class GatedResidualNormKept(NamedTuple):
     """What ``gated_residual_norm_backward`` reads of the forward pass: f and h (tensors, or both packed) and the
-    reciprocal root mean squares of their rows, float32 ``[n, tokens]``."""
+    reciprocal root mean squares of their rows, float32 ``[2, n, tokens]``."""
 
     f: object
     h: object
-    r_f: torch.Tensor
-    r_h: torch.Tensor
+    r: torch.Tensor
     eps: float
 
+    @property
+    def r_f(self) -> torch.Tensor:
+        return self.r[0]
 
-def _norm_desc(x, gate, post, pre, scale, eps):
-    if not isinstance(x, torch.Tensor) or x.dim() not in (2, 3):
+    @property
+    def r_h(self) -> torch.Tensor:
+        return self.r[1]
+
+
+def _norm_plan(x, gate, post, pre, scale, eps):
+    """(description, bytes between r_f and r_h, workspace of the backward pass)"""
+    key = ("norm", x.dtype, x.shape, x.stride(), gate.dtype, gate.shape, gate.stride(), post.dtype, post.shape, post.stride(), pre.dtype,
+           pre.shape, pre.stride(), scale, eps)
+    plan = _plans.get(key)
+    if plan is not None:
+        return plan
+    if x.dim() not in (2, 3):
         raise ValueError("x must be a tensor [n, tokens, cols] or [tokens, cols]")
+    _check("x", x, None, tuple(x.shape))
+    _dense("x", x)
     lead, (tokens, cols) = tuple(x.shape[:-2]), x.shape[-2:]
-    if not isinstance(gate, torch.Tensor) or gate.dim() != x.dim():
+    if gate.dim() != x.dim():
         raise ValueError("gate must be [n, gates, cols] with x [n, tokens, cols], or [gates, cols] with [tokens, cols]")
     gates = gate.shape[-2]
     _check("gate", gate, x, lead + (gates, cols))
@@ -376,9 +453,17 @@ def _norm_desc(x, gate, post, pre, scale, eps):
     _check("pre", pre, x, lead + (cols,))
     n = lead[0] if lead else 1
     d = rps_norm_desc(dtype=_DTYPE[x.dtype], n=n, tokens=tokens, cols=cols, gates=gates, scale=scale, eps=eps)
-    strides = [_parameter_stride(name, t if lead else t[None]) for name, t in (("post", post), ("pre", pre), ("gate", gate))]
-    d.post_worker, d.pre_worker, d.gate_worker = strides
-    return d, lead
+    d.post_worker, d.pre_worker, d.gate_worker = (_parameter_stride(name, t if lead else t[None])
+                                                  for name, t in (("post", post), ("pre", pre), ("gate", gate)))
+    size = ctypes.c_size_t()
+    _call("rps_norm_workspace", x.get_device(), ctypes.byref(d), ctypes.byref(size))
+    return _keep(key, (ctypes.byref(d), 4 * n * tokens, size.value))
+
+
+def _same(name: str, t: torch.Tensor, like: torch.Tensor) -> None:
+    """t is laid out as ``like``, which is contiguous."""
+    if t.dtype != like.dtype or t.shape != like.shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {like.dtype} tensor of shape {tuple(like.shape)}")
 
 
 def gated_residual_norm_forward(x: torch.Tensor, f: torch.Tensor, gate: torch.Tensor, post: torch.Tensor, pre: torch.Tensor, *,
@@ -391,59 +476,52 @@ def gated_residual_norm_forward(x: torch.Tensor, f: torch.Tensor, gate: torch.Te
     keep: "values" (kept holds f and h themselves), "int8" (8-bit copies, written along the way)."""
     if keep not in ("values", "int8"):
         raise ValueError('keep must be "values" or "int8"')
-    _check("x", x, None, tuple(x.shape))
-    d, lead = _norm_desc(x, gate, post, pre, scale, eps)
-    _check("f", f, x, tuple(x.shape))
-    _dense("x", x)
-    _dense("f", f)
+    device = _device_of(x=x, f=f, gate=gate, post=post, pre=pre)
+    desc, between, _ = _norm_plan(x, gate, post, pre, scale, eps)
+    _same("f", f, x)
     h, y = torch.empty_like(x), torch.empty_like(x)
-    r = torch.empty((2,) + tuple(x.shape[:-1]), dtype=torch.float32, device=x.device)
-    r_f, r_h = r[0], r[1]
-    packed = (None, None, None, None)
+    r = torch.empty((2,) + x.shape[:-1], dtype=torch.float32, device=x.device)
+    r_f = r.data_ptr()
     if keep == "int8":
-        kept_f, kept_h = (packed_like(tuple(x.shape), x.dtype, x.device) for _ in range(2))
-        packed = tuple(t.data_ptr() for t in (kept_f.codes, kept_f.scales, kept_h.codes, kept_h.scales))
+        kept_f, kept_h = packed_like(x.shape, x.dtype, x.device), packed_like(x.shape, x.dtype, x.device)
+        packed = kept_f.codes.data_ptr(), kept_f.scales.data_ptr(), kept_h.codes.data_ptr(), kept_h.scales.data_ptr()
     else:
         kept_f, kept_h = f, h
-    _call("rps_norm_forward", x.device, ctypes.byref(d), x.data_ptr(), f.data_ptr(), gate.data_ptr(), post.data_ptr(),
-          pre.data_ptr(), h.data_ptr(), y.data_ptr(), r_f.data_ptr(), r_h.data_ptr(), *packed, _stream(x.device))
-    return h, y, GatedResidualNormKept(kept_f, kept_h, r_f, r_h, eps)
+        packed = None, None, None, None
+    _call("rps_norm_forward", device, desc, x.data_ptr(), f.data_ptr(), gate.data_ptr(), post.data_ptr(), pre.data_ptr(), h.data_ptr(),
+          y.data_ptr(), r_f, r_f + between, *packed, _stream(device))
+    return h, y, GatedResidualNormKept(kept_f, kept_h, r, eps)
 
 
 def gated_residual_norm_backward(dh: Optional[torch.Tensor], dy: torch.Tensor, kept: GatedResidualNormKept, gate: torch.Tensor,
                                  post: torch.Tensor, pre: torch.Tensor, *, scale: float = 1.0):
     """(dx, df, dgate, dpost, dpre) for the gradients dh (None: none reaches h but through y) and dy of the forward call's h
     and y (``rps_norm_backward``)."""
-    _check("dy", dy, None, tuple(dy.shape))
-    d, lead = _norm_desc(dy, gate, post, pre, scale, kept.eps)
-    _dense("dy", dy)
+    device = _device_of(dy=dy, gate=gate, post=post, pre=pre, r=kept.r)
+    desc, between, size = _norm_plan(dy, gate, post, pre, scale, kept.eps)
     if dh is not None:
-        _check("dh", dh, dy, tuple(dy.shape))
-        _dense("dh", dh)
-    rows = tuple(dy.shape[:-1])
+        _device_of(dy=dy, dh=dh)
+        _same("dh", dh, dy)
     if isinstance(kept.f, PackedActivation):
+        _device_of(dy=dy, f_codes=kept.f.codes, f_scales=kept.f.scales, h_codes=kept.h.codes, h_scales=kept.h.scales)
         for name, p in (("kept.f", kept.f), ("kept.h", kept.h)):
-            _check_packed(name, p, rows)
-            if p.columns != d.cols or p.dtype != dy.dtype or p.codes.device != dy.device:
+            if _packed_shape(name, p) != tuple(dy.shape) or p.dtype != dy.dtype:
                 raise ValueError(f"{name} does not go with dy")
         f, f_scales, h, h_scales = (t.data_ptr() for t in (kept.f.codes, kept.f.scales, kept.h.codes, kept.h.scales))
     else:
-        for name, t in (("kept.f", kept.f), ("kept.h", kept.h)):
-            _check(name, t, dy, tuple(dy.shape))
-            _dense(name, t)
+        _device_of(dy=dy, f=kept.f, h=kept.h)
+        _same("kept.f", kept.f, dy)
+        _same("kept.h", kept.h, dy)
         f, f_scales, h, h_scales = kept.f.data_ptr(), None, kept.h.data_ptr(), None
-    for name, t in (("kept.r_f", kept.r_f), ("kept.r_h", kept.r_h)):
-        if t.dtype != torch.float32 or t.device != dy.device or tuple(t.shape) != rows:
-            raise ValueError(f"{name} must be a float32 tensor of shape {rows} on the device of dy")
-        _dense(name, t)
+    r = kept.r
+    if r.dtype != torch.float32 or r.shape != (2,) + dy.shape[:-1] or not r.is_contiguous():
+        raise ValueError(f"kept.r must be a contiguous float32 tensor of shape {(2,) + tuple(dy.shape[:-1])}")
     dx, df = torch.empty_like(dy), torch.empty_like(dy)
     dgate, dpost, dpre = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (gate, post, pre))
-    size = ctypes.c_size_t()
-    _call("rps_norm_workspace", dy.device, ctypes.byref(d), ctypes.byref(size))
-    ws = _workspace(dy.device, size.value)
-    _call("rps_norm_backward", dy.device, ctypes.byref(d), None if dh is None else dh.data_ptr(), dy.data_ptr(), f, f_scales, h,
-          h_scales, kept.r_f.data_ptr(), kept.r_h.data_ptr(), gate.data_ptr(), post.data_ptr(), pre.data_ptr(), dx.data_ptr(),
-          df.data_ptr(), dgate.data_ptr(), dpost.data_ptr(), dpre.data_ptr(), ws.data_ptr(), size.value, _stream(dy.device))
+    ws = _workspace(dy, size)
+    _call("rps_norm_backward", device, desc, None if dh is None else dh.data_ptr(), dy.data_ptr(), f, f_scales, h, h_scales, r.data_ptr(),
+          r.data_ptr() + between, gate.data_ptr(), post.data_ptr(), pre.data_ptr(), dx.data_ptr(), df.data_ptr(), dgate.data_ptr(),
+          dpost.data_ptr(), dpre.data_ptr(), ws.data_ptr(), size, _stream(device))
     return dx, df, dgate, dpost, dpre
 
 
@@ -455,25 +533,24 @@ class _GatedResidualNorm(torch.autograd.Function):
         ctx.settings = scale, eps, keep
         if keep == "int8":
             ctx.columns = kept.f.columns, kept.f.dtype
-            ctx.save_for_backward(gate, post, pre, kept.r_f, kept.r_h, kept.f.codes, kept.f.scales, kept.h.codes, kept.h.scales)
+            ctx.save_for_backward(gate, post, pre, kept.r, kept.f.codes, kept.f.scales, kept.h.codes, kept.h.scales)
         else:
-            ctx.save_for_backward(gate, post, pre, kept.r_f, kept.r_h, f, h)
+            ctx.save_for_backward(gate, post, pre, kept.r, f, h)
         return h, y
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dh, dy):
         scale, eps, keep = ctx.settings
-        gate, post, pre, r_f, r_h, *rest = ctx.saved_tensors
+        gate, post, pre, r, *rest = ctx.saved_tensors
         if keep == "int8":
             f, h = (PackedActivation(c, s, *ctx.columns) for c, s in (rest[:2], rest[2:]))
         else:
             f, h = rest
         if dy is None:  # y was not used
-            shape = r_f.shape + (post.shape[-1],)
-            dy = torch.zeros(shape, dtype=post.dtype, device=post.device)
+            dy = torch.zeros(r.shape[1:] + (post.shape[-1],), dtype=post.dtype, device=post.device)
         grads = gated_residual_norm_backward(None if dh is None else dh.contiguous(), dy.contiguous(),
-                                             GatedResidualNormKept(f, h, r_f, r_h, eps), gate, post, pre, scale=scale)
+                                             GatedResidualNormKept(f, h, r, eps), gate, post, pre, scale=scale)
         return grads + (None, None, None)
 
 
