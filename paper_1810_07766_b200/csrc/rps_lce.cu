@@ -1,12 +1,13 @@
 // The loss around its matrix products: which tokens take part, their rows laid out for the tensor cores, and the end of
 // the softmax statistics.
-#include "rps_ops_kernels.h"
+#include "rps_rows.cuh"
 
 namespace rps_ops {
 namespace {
 
 constexpr int kSelectThreads = 1024;
-constexpr int kMergeThreads = 128;
+constexpr int kMergeThreads = 512, kMergeRows = 32;
+constexpr int kRowThreads = 256;
 
 // One CTA per worker.  rows[] becomes a permutation of the worker's tokens: those that take part in their order, then
 // the ignored ones; a ballot and a scan over the warps' counts give each token its place.
@@ -69,73 +70,124 @@ __global__ void __launch_bounds__(kSelectThreads) rps_lce_select_kernel(const Lc
     }
 }
 
-template <typename T>
-__global__ void __launch_bounds__(256) rps_lce_gather_kernel(const LceParams prm)
+// Eight columns from c on, as fp32; zero from `cols` on.
+template <typename T, bool ALIGNED>
+__device__ __forceinline__ void load_eight(const T* row, int c, int cols, float (&v)[8])
 {
-    const int w = blockIdx.y;
-    const int64_t i = blockIdx.x;
-    const int count = prm.count[w];
+    if constexpr (sizeof(T) == 2) {
+        widen(load_slice<T, ALIGNED, true>(row, c, cols), v);
+    } else {
+        float a[4], b[4];
+        widen(load_slice<T, ALIGNED, true>(row, c, cols), a);
+        widen(load_slice<T, ALIGNED, true>(row, c + 4, cols), b);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = a[j], v[4 + j] = b[j];
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ void store_parts(bf16* dst, int64_t plane, const float (&v)[8])
+{
+    if constexpr (sizeof(T) == 2) {
+        *reinterpret_cast<uint4*>(dst) = narrow(v);
+    } else {
+        uint4 parts[3];
+        split_slice(v, parts);
+#pragma unroll
+        for (int q = 0; q < 3; ++q) *reinterpret_cast<uint4*>(dst + q * plane) = parts[q];
+    }
+}
+
+// A warp to a row.
+template <typename T, bool ALIGNED>
+__global__ void __launch_bounds__(kRowThreads) rps_lce_gather_kernel(const LceParams prm)
+{
+    const int w = blockIdx.y, lane = threadIdx.x % 32;
+    const int64_t i = (int64_t)blockIdx.x * (kRowThreads / 32) + threadIdx.x / 32;
+    const int count = prm.count[w], D = (int)prm.cols;
     const bool in = i < count;
     if (!in && i < prm.tokens && prm.backward) {  // an ignored token's gradient
         T* out = static_cast<T*>(prm.dhidden) + (w * prm.tokens + prm.rows[w * prm.tokens + i]) * prm.cols;
-        for (int64_t c = threadIdx.x; c < prm.cols; c += blockDim.x) out[c] = from_float<T>(0.0f);
+        for (int c = lane; c < D; c += 32) out[c] = from_float<T>(0.0f);
     }
     // products read whole token tiles: the rows behind the last one are cleared
     if (i >= (count + kTokenTile - 1) / kTokenTile * kTokenTile) return;
     const T* src = static_cast<const T*>(prm.hidden) + w * prm.hidden_worker + (in ? prm.rows[w * prm.tokens + i] : 0) * prm.hidden_row;
     bf16* dst = prm.packed + (w * prm.planes * prm.tokens_padded + i) * prm.cols_padded;
     const int64_t plane = prm.tokens_padded * prm.cols_padded;
-    for (int64_t c = threadIdx.x; c < prm.cols_padded; c += blockDim.x) {
-        const float v = in && c < prm.cols ? to_float<T>(src[c]) : 0.0f;
-        if (prm.planes == 1) {
-            dst[c] = __float2bfloat16_rn(v);
-        } else {
-            bf16 p[3];
-            split_planes(v, p);
-            for (int q = 0; q < 3; ++q) dst[q * plane + c] = p[q];
-        }
+#pragma unroll 4
+    for (int c = lane * 8; c < prm.cols_padded; c += 256) {
+        float v[8];
+        load_eight<T, ALIGNED>(src, c, in ? D : 0, v);
+        store_parts<T>(dst + c, plane, v);
     }
 }
 
-template <typename T>
-__global__ void __launch_bounds__(256) rps_planes_kernel(const PlanesParams prm)
+// Rows of a matrix of each worker as operands, eight columns to a thread.
+template <typename T, bool ALIGNED>
+__global__ void __launch_bounds__(kRowThreads) rps_planes_kernel(const PlanesParams prm)
 {
-    const int w = blockIdx.y;
-    const int64_t i = blockIdx.x;
-    const T* src = static_cast<const T*>(prm.src) + w * prm.src_worker + i * prm.src_row;
-    bf16* dst = prm.dst + w * prm.dst_worker + i * prm.dst_row;
-    for (int64_t c = threadIdx.x; c < prm.dst_row; c += blockDim.x) {
-        const float v = i < prm.valid && c < prm.cols ? to_float<T>(src[c]) : 0.0f;
-        if (prm.planes == 1) {
-            dst[c] = __float2bfloat16_rn(v);
-        } else {
-            bf16 p[3];
-            split_planes(v, p);
-            for (int q = 0; q < 3; ++q) dst[q * prm.dst_plane + c] = p[q];
+    const int w = blockIdx.y, per_row = (int)(prm.dst_row / 8);
+    const uint32_t total = (uint32_t)(prm.rows * per_row);  // below 2^32: the matrix has 16 bytes for each
+    const uint32_t step = gridDim.x * kRowThreads;
+    const T* src = static_cast<const T*>(prm.src) + w * prm.src_worker;
+    bf16* dst = prm.dst + w * prm.dst_worker;
+    constexpr int kAtATime = 2;
+    for (uint64_t u0 = blockIdx.x * kRowThreads + threadIdx.x; u0 < total; u0 += (uint64_t)step * kAtATime) {
+        float v[kAtATime][8];
+        uint32_t row[kAtATime];
+        int c[kAtATime];
+#pragma unroll
+        for (int k = 0; k < kAtATime; ++k) {
+            const uint64_t u = u0 + (uint64_t)k * step;
+            if (u >= total) break;
+            row[k] = (uint32_t)u / (uint32_t)per_row;
+            c[k] = (int)((uint32_t)u - row[k] * (uint32_t)per_row) * 8;
+            load_eight<T, ALIGNED>(src + (int64_t)row[k] * prm.src_row, c[k], (int)prm.cols, v[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < kAtATime; ++k) {
+            if (u0 + (uint64_t)k * step >= total) break;
+            store_parts<T>(dst + (int64_t)row[k] * prm.dst_row + c[k], prm.dst_plane, v[k]);
         }
     }
 }
 
-// Joins the (maximum, sum) pairs of a row's vocabulary tiles, a thread for each row.  The sum over a worker's rows is made
-// of the blocks' sums by the block that finishes last, always in the same order.
+// Joins the (maximum, sum) pairs of a row's vocabulary tiles: a CTA for 32 rows, a lane to a row so that reads are whole lines, the tiles
+// dealt to the 16 warps.  (One thread for all tiles of a row took 248 us for 4096 rows of 1024 tiles.)  The sum over a worker's
+// rows is made of the CTAs' sums by the one that finishes last, always in the same order.
 __global__ void __launch_bounds__(kMergeThreads) rps_lce_merge_kernel(const LceParams prm)
 {
-    __shared__ float warp_sum[kMergeThreads / 32];
-    __shared__ bool last;
-    const int w = blockIdx.y, count = prm.count[w];
-    const int blocks = (count + kMergeThreads - 1) / kMergeThreads;
+    constexpr int kWarps = kMergeThreads / 32;
+    __shared__ float2 parts[kWarps][32];
+    const int w = blockIdx.y, count = prm.count[w], lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    const int blocks = (count + kMergeRows - 1) / kMergeRows;
     if ((int)blockIdx.x >= blocks) return;
-    const int i = blockIdx.x * kMergeThreads + threadIdx.x;
-    float loss = 0.0f;
+    const int i = blockIdx.x * kMergeRows + lane;
+    float top = -INFINITY, sum = 0.0f;
+    const auto join = [&](float2 p) {
+        const float m = fmaxf(top, p.x), at = m == -INFINITY ? 0.0f : m;
+        sum = sum * __expf(top - at) + p.y * __expf(p.x - at);
+        top = m;
+    };
     if (i < count) {
         const float2* part = prm.part + w * prm.stat_tiles * prm.tokens_padded + i;
-        float top = -INFINITY, sum = 0.0f;
-        for (int64_t v = 0; v < prm.stat_tiles; ++v) {
-            const float2 p = part[v * prm.tokens_padded];
-            const float m = fmaxf(top, p.x), at = m == -INFINITY ? 0.0f : m;
-            sum = sum * __expf(top - at) + p.y * __expf(p.x - at);
-            top = m;
+        constexpr int kAtATime = 4;
+        for (int64_t v = warp; v < prm.stat_tiles; v += kWarps * kAtATime) {
+            float2 p[kAtATime];
+#pragma unroll
+            for (int k = 0; k < kAtATime; ++k)
+                p[k] = v + k * kWarps < prm.stat_tiles ? __ldcs(part + (v + k * kWarps) * prm.tokens_padded) : make_float2(-INFINITY, 0.0f);
+#pragma unroll
+            for (int k = 0; k < kAtATime; ++k) join(p[k]);
         }
+    }
+    parts[warp][lane] = make_float2(top, sum);
+    __syncthreads();
+    if (warp != 0) return;
+    float loss = 0.0f;
+    if (i < count) {
+        for (int k = 1; k < kWarps; ++k) join(parts[k][lane]);
         const float lse = top + logf(sum);
         loss = lse - prm.hit[w * prm.tokens_padded + i];
         const int64_t t = prm.rows[w * prm.tokens + i];
@@ -144,21 +196,53 @@ __global__ void __launch_bounds__(kMergeThreads) rps_lce_merge_kernel(const LceP
     }
     if (prm.reduction == RPS_REDUCE_NONE) return;
     for (int s = 16; s > 0; s /= 2) loss += __shfl_xor_sync(0xFFFFFFFFu, loss, s);
-    if (threadIdx.x % 32 == 0) warp_sum[threadIdx.x / 32] = loss;
-    __syncthreads();
-    if (threadIdx.x != 0) return;
-    float sum = 0.0f;
-    for (int k = 0; k < kMergeThreads / 32; ++k) sum += warp_sum[k];
     float* sums = prm.sums + w * gridDim.x;
-    sums[blockIdx.x] = sum;
-    __threadfence();
-    last = atomicAdd(&prm.done[w], 1) == blocks - 1;
-    if (!last) return;
-    __threadfence();
+    int before = 0;
+    if (lane == 0) {
+        sums[blockIdx.x] = loss;
+        __threadfence();
+        before = atomicAdd(&prm.done[w], 1);
+        __threadfence();
+    }
+    if (__shfl_sync(0xFFFFFFFFu, before, 0) != blocks - 1) return;
     double all = 0.0;
-    for (int b = 0; b < blocks; ++b) all += (double)__ldcg(&sums[b]);
+    for (int b = lane; b < blocks; b += 32) all += (double)__ldcg(&sums[b]);
+    for (int s = 16; s > 0; s /= 2) all += __shfl_xor_sync(0xFFFFFFFFu, all, s);
     if (prm.reduction == RPS_REDUCE_MEAN) all /= (double)count;
-    prm.loss[w] = (float)all;
+    if (lane == 0) prm.loss[w] = (float)all;
+}
+
+template <typename T>
+bool aligned_source(const void* p, int64_t cols, int64_t row, int64_t worker)
+{
+    constexpr int W = Slice<T>::kWidth;
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && cols % W == 0 && row % W == 0 && worker % W == 0;
+}
+
+template <typename T>
+cudaError_t gather(const LceParams& prm, cudaStream_t stream)
+{
+    const dim3 grid((unsigned)ceil_div(prm.tokens_padded, kRowThreads / 32), (unsigned)prm.n);
+    if (aligned_source<T>(prm.hidden, prm.cols, prm.hidden_row, prm.hidden_worker))
+        rps_lce_gather_kernel<T, true><<<grid, kRowThreads, 0, stream>>>(prm);
+    else
+        rps_lce_gather_kernel<T, false><<<grid, kRowThreads, 0, stream>>>(prm);
+    return cudaGetLastError();
+}
+
+template <typename T>
+cudaError_t planes(const PlanesParams& prm, cudaStream_t stream)
+{
+    int sms = 0;
+    cudaError_t err = sm_count(&sms);
+    if (err != cudaSuccess) return err;
+    const int64_t blocks = ceil_div(prm.rows * (prm.dst_row / 8), kRowThreads), resident = ceil_div((int64_t)sms * 8, prm.n);
+    const dim3 grid((unsigned)(blocks < resident ? blocks : resident), (unsigned)prm.n);
+    if (aligned_source<T>(prm.src, prm.cols, prm.src_row, prm.src_worker))
+        rps_planes_kernel<T, true><<<grid, kRowThreads, 0, stream>>>(prm);
+    else
+        rps_planes_kernel<T, false><<<grid, kRowThreads, 0, stream>>>(prm);
+    return cudaGetLastError();
 }
 
 }  // namespace
@@ -171,15 +255,10 @@ cudaError_t launch_lce_select(const LceParams& prm, cudaStream_t stream)
 
 cudaError_t launch_lce_gather(const LceParams& prm, cudaStream_t stream)
 {
-    const dim3 grid((unsigned)prm.tokens_padded, (unsigned)prm.n);
-    if (prm.f32)
-        rps_lce_gather_kernel<float><<<grid, 256, 0, stream>>>(prm);
-    else
-        rps_lce_gather_kernel<bf16><<<grid, 256, 0, stream>>>(prm);
-    return cudaGetLastError();
+    return prm.f32 ? gather<float>(prm, stream) : gather<bf16>(prm, stream);
 }
 
-int64_t lce_merge_blocks(int64_t tokens) { return ceil_div(tokens, kMergeThreads); }
+int64_t lce_merge_blocks(int64_t tokens) { return ceil_div(tokens, kMergeRows); }
 
 cudaError_t launch_lce_merge(const LceParams& prm, cudaStream_t stream)
 {
@@ -190,12 +269,7 @@ cudaError_t launch_lce_merge(const LceParams& prm, cudaStream_t stream)
 
 cudaError_t launch_planes(const PlanesParams& prm, cudaStream_t stream)
 {
-    const dim3 grid((unsigned)prm.rows, (unsigned)prm.n);
-    if (prm.f32)
-        rps_planes_kernel<float><<<grid, 256, 0, stream>>>(prm);
-    else
-        rps_planes_kernel<bf16><<<grid, 256, 0, stream>>>(prm);
-    return cudaGetLastError();
+    return prm.f32 ? planes<float>(prm, stream) : planes<bf16>(prm, stream);
 }
 
 }  // namespace rps_ops

@@ -57,7 +57,7 @@ bool aligned(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p
 bool aligned_matrix(const void* p, int64_t row, int64_t worker) { return aligned(p, 16) && row % 8 == 0 && worker % 8 == 0; }
 
 // A piece of the vocabulary is as wide as lets dl (and the weight, where it has to be laid out anew) of one piece stay within this.
-constexpr int64_t kPieceBytes = 256ll << 20;
+constexpr int64_t kPieceBytes = 512ll << 20;
 constexpr int64_t kMaxSize = (1ll << 24) - 1;
 
 int check_output_strides(const char* name, int n, int64_t rows, int64_t cols, int64_t row, int64_t worker)
@@ -174,7 +174,7 @@ int weight_operand(const rps_lce_desc& d, const LcePlan& plan, const void* weigh
     PlanesParams q{};
     q.src = static_cast<const unsigned char*>(weight) + v0 * d.weight_row * (p.f32 ? 4 : 2);
     q.f32 = p.f32, q.n = p.n, q.planes = p.planes;
-    q.rows = q.valid = rows, q.cols = d.cols, q.src_row = d.weight_row, q.src_worker = d.weight_worker;
+    q.rows = rows, q.cols = d.cols, q.src_row = d.weight_row, q.src_worker = d.weight_worker;
     q.dst = plan.weight, q.dst_row = p.cols_padded, q.dst_plane = plane, q.dst_worker = p.planes * plane;
     *out = {plan.weight, p.planes * plane, plane, p.cols_padded, rows, p.cols_padded};
     return cuda_status(launch_planes(q, stream), "laying the weight out");
@@ -459,7 +459,7 @@ WgradPlan plan_wgrad(const rps_wgrad_desc& d, const void* dy, void* workspace)
         bf16* to = c.take<bf16>(d.n * planes * plane);
         plan.dy = {to, planes * plane, plane, row, d.tokens, row};
         PlanesParams& q = plan.lay_out;
-        q.src = dy, q.f32 = d.dtype == RPS_F32, q.n = d.n, q.planes = planes, q.rows = q.valid = d.tokens, q.cols = d.outs;
+        q.src = dy, q.f32 = d.dtype == RPS_F32, q.n = d.n, q.planes = planes, q.rows = d.tokens, q.cols = d.outs;
         q.src_row = d.dy_row, q.src_worker = d.dy_worker, q.dst = to, q.dst_row = row, q.dst_plane = plane, q.dst_worker = planes * plane;
     }
     plan.bytes = c.used;

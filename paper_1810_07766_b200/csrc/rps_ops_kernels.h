@@ -88,7 +88,7 @@ struct LceParams {
     int64_t stat_tiles;
     float* loss;
     float* lse;
-    float* sums;      // [n][blocks of rows]
+    float* sums;      // [n][lce_merge_blocks(tokens)]
     int* done;        // [n]
 };
 
@@ -97,11 +97,11 @@ cudaError_t launch_lce_gather(const LceParams& prm, cudaStream_t stream);
 int64_t lce_merge_blocks(int64_t tokens);
 cudaError_t launch_lce_merge(const LceParams& prm, cudaStream_t stream);
 
-// Lays `rows` rows of a matrix of each worker out as planes; rows past `valid` and columns past `cols` become zero.
+// Lays the rows of a matrix of each worker out as planes; columns past `cols` become zero.
 struct PlanesParams {
     const void* src;
     int f32, n, planes;
-    int64_t rows, valid, cols, src_row, src_worker;
+    int64_t rows, cols, src_row, src_worker;
     bf16* dst;
     int64_t dst_row, dst_plane, dst_worker;
 };
@@ -162,19 +162,23 @@ __device__ __forceinline__ float from_float<float>(float v) { return v; }
 template <>
 __device__ __forceinline__ bf16 from_float<bf16>(float v) { return __float2bfloat16_rn(v); }
 
-// v = p0 + p1 + p2 exactly: each part is the leading 8 bits of what the parts before it leave, cut off rather than rounded
-// so that no part can overflow.  An infinity or a NaN stays in the first part (as such) and the others are zero.
-__device__ __forceinline__ void split_planes(float v, bf16 (&p)[3])
+// An fp32 value is the sum of three bf16 values exactly: each is the leading 8 bits of what the ones before it leave, cut off
+// rather than rounded so that none can overflow.  An infinity or a NaN stays in the first one and the others are zero.
+__device__ __forceinline__ float leading_bits(float v)
 {
     const uint32_t bits = __float_as_uint(v);
-    uint32_t top = bits & 0xFFFF0000u;
-    const bool finite = (bits & 0x7F800000u) != 0x7F800000u;
-    if (!finite && (bits & 0x007FFFFFu) != 0) top |= 0x00400000u;  // a NaN whose payload lies in the bits cut off
-    p[0] = __ushort_as_bfloat16((unsigned short)(top >> 16));
-    const float rest = finite ? v - __uint_as_float(top) : 0.0f;
-    const uint32_t mid = __float_as_uint(rest) & 0xFFFF0000u;
-    p[1] = __ushort_as_bfloat16((unsigned short)(mid >> 16));
-    p[2] = __float2bfloat16_rn(rest - __uint_as_float(mid));
+    // a NaN whose payload lies in the bits cut off stays one
+    return __uint_as_float(v != v ? bits | 0x00400000u : bits & 0xFFFF0000u);
+}
+
+__device__ __forceinline__ float rest_of(float v, float lead) { return fabsf(v) <= 3.402823466e38f ? v - lead : 0.0f; }
+
+__device__ __forceinline__ void split_planes(float v, bf16 (&p)[3])
+{
+    const float lead = leading_bits(v), rest = rest_of(v, lead), mid = leading_bits(rest);
+    p[0] = __float2bfloat16_rn(lead);  // exact, as the next one
+    p[1] = __float2bfloat16_rn(mid);
+    p[2] = __float2bfloat16_rn(rest - mid);
 }
 #endif
 

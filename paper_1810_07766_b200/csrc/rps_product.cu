@@ -42,7 +42,17 @@ constexpr uint64_t kWaitNs = 2000000000ull;
 
 static_assert(kTileM == kTokenTile && kTileN == kVocabTile, "operands are padded to whole tiles");
 
+// Rows leave through shared memory: a lane holds one row, and 32 lanes writing 16 bytes of 32 rows each would touch 32 lines at a time and
+// half a sector of each.  Instead 64 bytes of each of the warp's 32 rows are laid down (parts of 16 bytes, exchanged by the row's
+// number so that neither side has bank conflicts) and written out as 4 lanes to a row; rows that are not 16-byte aligned go out
+// element by element, still in the order of memory.  (Gradient of 8 fp32 weights of 10001 x 650, rows of 2600 bytes: 453 -> XXX us.)
+struct Staging {
+    uint4 part[32][4];
+    int64_t at[32];
+};
+
 struct Control {
+    Staging staging[kEpilogueWarps];
     uint64_t full[kStages], empty[kStages], sum_full[2], sum_empty[2];
     uint32_t tensor_memory;
     int start[RPS_MAX_WORKERS + 1];  // first tile of each worker
@@ -197,36 +207,78 @@ __device__ __forceinline__ uint32_t two_bf16(float lo, float hi)
     return *reinterpret_cast<const uint32_t*>(&p);
 }
 
-// A row's columns, `cols` of them; `wide`: 16 bytes at a time where all 128 are there.
-__device__ __forceinline__ void store_row(float* out, const float (&v)[kHalf], int cols, bool wide)
+// Part q of an fp32 value.
+__device__ __forceinline__ float part_of(float v, int q)
 {
-    if (wide && cols >= kHalf) {
-#pragma unroll
-        for (int j = 0; j < kHalf; j += 4) *reinterpret_cast<float4*>(out + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
-    } else {
-#pragma unroll
-        for (int j = 0; j < kHalf; ++j)
-            if (j < cols) out[j] = v[j];
-    }
+    const float lead = leading_bits(v), rest = rest_of(v, lead), mid = leading_bits(rest);
+    return q == 0 ? lead : q == 1 ? mid : rest - mid;
 }
 
-__device__ __forceinline__ void store_row(bf16* out, const float (&v)[kHalf], int cols, bool wide)
+// `at`: offset of this lane's row in `out`, or -1 if it is not to be written; `cols` of the 128 columns exist.  ADD: to what is there
+// (fp32, wide).  PART: not the values but that part of them.
+template <bool ADD, bool PART, typename T>
+__device__ __forceinline__ void store_rows(Staging& stage, const float (&v)[kHalf], T* out, int64_t at, int cols, bool wide, int part = 0)
 {
-    if (wide && cols >= kHalf) {
+    constexpr int kChunk = 64 / sizeof(T), kPart = 16 / sizeof(T);  // columns
+    const int lane = threadIdx.x % 32;
+    __syncwarp();
+    stage.at[lane] = at;
 #pragma unroll
-        for (int j = 0; j < kHalf; j += 8)
-            *reinterpret_cast<uint4*>(out + j) =
-                make_uint4(two_bf16(v[j], v[j + 1]), two_bf16(v[j + 2], v[j + 3]), two_bf16(v[j + 4], v[j + 5]), two_bf16(v[j + 6], v[j + 7]));
-    } else {
+    for (int c = 0; c < kHalf / kChunk; ++c) {
+        __syncwarp();
 #pragma unroll
-        for (int j = 0; j < kHalf; ++j)
-            if (j < cols) out[j] = __float2bfloat16_rn(v[j]);
+        for (int q = 0; q < 4; ++q) {
+            const float* f = v + c * kChunk + q * kPart;
+            uint4 word;
+            if constexpr (sizeof(T) == 4)
+                word = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+            else
+                word = PART ? make_uint4(two_bf16(part_of(f[0], part), part_of(f[1], part)), two_bf16(part_of(f[2], part), part_of(f[3], part)),
+                                         two_bf16(part_of(f[4], part), part_of(f[5], part)), two_bf16(part_of(f[6], part), part_of(f[7], part)))
+                            : make_uint4(two_bf16(f[0], f[1]), two_bf16(f[2], f[3]), two_bf16(f[4], f[5]), two_bf16(f[6], f[7]));
+            stage.part[lane][q ^ (lane >> 1 & 3)] = word;
+        }
+        __syncwarp();
+        if (wide) {
+            const int col = c * kChunk + lane % 4 * kPart;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int r = lane / 4 + 8 * i;
+                uint4 word = stage.part[r][lane % 4 ^ (r >> 1 & 3)];
+                const int64_t row_at = stage.at[r];
+                T* to = out + row_at + col;
+                if (row_at < 0 || col >= cols) continue;
+                if constexpr (ADD) {
+                    const float4 old = *reinterpret_cast<const float4*>(to);
+                    word = make_uint4(__float_as_uint(__uint_as_float(word.x) + old.x), __float_as_uint(__uint_as_float(word.y) + old.y),
+                                      __float_as_uint(__uint_as_float(word.z) + old.z), __float_as_uint(__uint_as_float(word.w) + old.w));
+                }
+                if (col + kPart <= cols) {
+                    *reinterpret_cast<uint4*>(to) = word;
+                } else {
+                    const T* e = reinterpret_cast<const T*>(&word);
+#pragma unroll
+                    for (int k = 0; k < kPart; ++k)
+                        if (col + k < cols) to[k] = e[k];
+                }
+            }
+        } else {
+            constexpr int kRows = 32 / kChunk;  // rows that the warp writes at a time, an element to a lane: 2 of fp32, 1 of bf16
+            const int col = lane % kChunk;
+#pragma unroll 4
+            for (int r0 = 0; r0 < 32; r0 += kRows) {
+                const int r = r0 + lane / kChunk;
+                const int64_t to = stage.at[r];
+                const T e = reinterpret_cast<const T*>(&stage.part[r][col / kPart ^ (r >> 1 & 3)])[col % kPart];
+                if (to >= 0 && c * kChunk + col < cols) out[to + c * kChunk + col] = e;
+            }
+        }
     }
 }
 
 // One row's 128 columns of a tile.
 template <Product WHICH>
-__device__ __forceinline__ void epilogue(const ProductParams& prm, int w, int row, int n0, int count, float (&v)[kHalf], bool wide)
+__device__ __forceinline__ void epilogue(const ProductParams& prm, int w, int row, int n0, int count, float (&v)[kHalf], bool wide, Staging& stage)
 {
     const int cols = prm.n - n0;
     if (cols <= 0 && WHICH != Product::kDlogits) return;
@@ -256,7 +308,7 @@ __device__ __forceinline__ void epilogue(const ProductParams& prm, int w, int ro
         const bool in = row < count;
         const float2 info = in ? prm.info[w * prm.tokens_padded + row] : make_float2(0.0f, 0.0f);
         const int t = in ? prm.target[w * prm.tokens_padded + row] - prm.v0 - n0 : -1;
-        bf16* dl = prm.dl + ((int64_t)w * prm.planes * prm.tokens_padded + row) * prm.piece + n0;
+        const int64_t at_dl = ((int64_t)w * prm.planes * prm.tokens_padded + row) * prm.piece + n0;
         const float at = info.x * kLog2e;
 #pragma unroll
         for (int j = 0; j < kHalf; ++j) {
@@ -264,52 +316,40 @@ __device__ __forceinline__ void epilogue(const ProductParams& prm, int w, int ro
             v[j] = in && j < cols ? info.y * p : 0.0f;
         }
         if (prm.planes == 1) {
-            store_row(dl, v, kHalf, true);
+            store_rows<false, false>(stage, v, prm.dl, at_dl, kHalf, true);
         } else {
-#pragma unroll
-            for (int j = 0; j < kHalf; j += 8) {
-                uint32_t packed[3][4];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    bf16 p[3];
-                    split_planes(v[j + i], p);
-#pragma unroll
-                    for (int q = 0; q < 3; ++q) {
-                        const uint32_t bits = __bfloat16_as_ushort(p[q]);
-                        packed[q][i / 2] = i % 2 == 0 ? bits : packed[q][i / 2] | bits << 16;
-                    }
-                }
-#pragma unroll
-                for (int q = 0; q < 3; ++q)
-                    *reinterpret_cast<uint4*>(dl + q * prm.tokens_padded * prm.piece + j) =
-                        make_uint4(packed[q][0], packed[q][1], packed[q][2], packed[q][3]);
-            }
+#pragma unroll 1
+            for (int q = 0; q < 3; ++q) store_rows<false, true>(stage, v, prm.dl + q * prm.tokens_padded * prm.piece, at_dl, kHalf, true, q);
         }
     } else {
         constexpr bool kHidden = WHICH == Product::kDhidden;
-        if (row >= (kHidden ? count : prm.m)) return;
+        const bool in = row < (kHidden ? count : prm.m);
         if constexpr (kHidden) {
-            float* acc = prm.acc + (w * prm.tokens_padded + row) * prm.acc_row + n0;
-            if (!prm.first) {
+            const int64_t at = in ? (w * prm.tokens_padded + row) * prm.acc_row + n0 : -1;
+            if (!prm.last) {
+                if (prm.first)
+                    store_rows<false, false>(stage, v, prm.acc, at, kHalf, true);
+                else
+                    store_rows<true, false>(stage, v, prm.acc, at, kHalf, true);
+                return;
+            }
+            if (!prm.first && in) {
+                const float* acc = prm.acc + at;
 #pragma unroll
                 for (int j = 0; j < kHalf; j += 4) {
                     const float4 a = *reinterpret_cast<const float4*>(acc + j);
                     v[j] += a.x, v[j + 1] += a.y, v[j + 2] += a.z, v[j + 3] += a.w;
                 }
             }
-            if (!prm.last) {
-                store_row(acc, v, kHalf, true);
-                return;
-            }
         }
         const float g = prm.scale != nullptr ? prm.scale[w] : 1.0f;
-        const int64_t at = w * prm.out_worker + (kHidden ? (int64_t)prm.rows[w * prm.tokens + row] : (int64_t)(prm.v0 + row)) * prm.out_row + n0;
+        const int64_t at = !in ? -1 : w * prm.out_worker + (kHidden ? (int64_t)prm.rows[w * prm.tokens + row] : (int64_t)(prm.v0 + row)) * prm.out_row + n0;
 #pragma unroll
         for (int j = 0; j < kHalf; ++j) v[j] *= g;
         if (prm.out_f32)
-            store_row(static_cast<float*>(prm.out) + at, v, cols, wide);
+            store_rows<false, false>(stage, v, static_cast<float*>(prm.out), at, cols, wide);
         else
-            store_row(static_cast<bf16*>(prm.out) + at, v, cols, wide);
+            store_rows<false, false>(stage, v, static_cast<bf16*>(prm.out), at, cols, wide);
     }
 }
 
@@ -490,7 +530,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                 ++made;
             }
             if (!fine) break;
-            epilogue<WHICH>(prm, t.w, t.m0 + (int)rank * 128 + quarter * 32 + lane, t.n0 + half * kHalf, t.count, v, wide);
+            epilogue<WHICH>(prm, t.w, t.m0 + (int)rank * 128 + quarter * 32 + lane, t.n0 + half * kHalf, t.count, v, wide, control.staging[warp - 2]);
         }
     }
     if (!fine && lane == 0) atomicExch(&g_gave_up, 1);
