@@ -1,5 +1,7 @@
 // The loss around its matrix products: which tokens take part, their rows laid out for the tensor cores, and the end of
 // the softmax statistics.
+#include <algorithm>
+
 #include "rps_rows.cuh"
 
 namespace rps_ops {
@@ -71,15 +73,15 @@ __global__ void __launch_bounds__(kSelectThreads) rps_lce_select_kernel(const Lc
 }
 
 // Eight columns from c on, as fp32; zero from `cols` on.
-template <typename T, bool ALIGNED>
+template <typename T, int ALIGN>
 __device__ __forceinline__ void load_eight(const T* row, int c, int cols, float (&v)[8])
 {
     if constexpr (sizeof(T) == 2) {
-        widen(load_slice<T, ALIGNED, true>(row, c, cols), v);
+        widen(load_slice<T, ALIGN, true>(row, c, cols), v);
     } else {
         float a[4], b[4];
-        widen(load_slice<T, ALIGNED, true>(row, c, cols), a);
-        widen(load_slice<T, ALIGNED, true>(row, c + 4, cols), b);
+        widen(load_slice<T, ALIGN, true>(row, c, cols), a);
+        widen(load_slice<T, ALIGN, true>(row, c + 4, cols), b);
 #pragma unroll
         for (int j = 0; j < 4; ++j) v[j] = a[j], v[4 + j] = b[j];
     }
@@ -99,7 +101,7 @@ __device__ __forceinline__ void store_parts(bf16* dst, int64_t plane, const floa
 }
 
 // A warp to a row.
-template <typename T, bool ALIGNED>
+template <typename T, int ALIGN>
 __global__ void __launch_bounds__(kRowThreads) rps_lce_gather_kernel(const LceParams prm)
 {
     const int w = blockIdx.y, lane = threadIdx.x % 32;
@@ -118,13 +120,13 @@ __global__ void __launch_bounds__(kRowThreads) rps_lce_gather_kernel(const LcePa
 #pragma unroll 4
     for (int c = lane * 8; c < prm.cols_padded; c += 256) {
         float v[8];
-        load_eight<T, ALIGNED>(src, c, in ? D : 0, v);
+        load_eight<T, ALIGN>(src, c, in ? D : 0, v);
         store_parts<T>(dst + c, plane, v);
     }
 }
 
 // Rows of a matrix of each worker as operands, eight columns to a thread.
-template <typename T, bool ALIGNED>
+template <typename T, int ALIGN>
 __global__ void __launch_bounds__(kRowThreads) rps_planes_kernel(const PlanesParams prm)
 {
     const int w = blockIdx.y, per_row = (int)(prm.dst_row / 8);
@@ -143,7 +145,7 @@ __global__ void __launch_bounds__(kRowThreads) rps_planes_kernel(const PlanesPar
             if (u >= total) break;
             row[k] = (uint32_t)u / (uint32_t)per_row;
             c[k] = (int)((uint32_t)u - row[k] * (uint32_t)per_row) * 8;
-            load_eight<T, ALIGNED>(src + (int64_t)row[k] * prm.src_row, c[k], (int)prm.cols, v[k]);
+            load_eight<T, ALIGN>(src + (int64_t)row[k] * prm.src_row, c[k], (int)prm.cols, v[k]);
         }
 #pragma unroll
         for (int k = 0; k < kAtATime; ++k) {
@@ -213,20 +215,18 @@ __global__ void __launch_bounds__(kMergeThreads) rps_lce_merge_kernel(const LceP
 }
 
 template <typename T>
-bool aligned_source(const void* p, int64_t cols, int64_t row, int64_t worker)
+int aligned_source(const void* p, int64_t cols, int64_t row, int64_t worker)
 {
-    constexpr int W = Slice<T>::kWidth;
-    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && cols % W == 0 && row % W == 0 && worker % W == 0;
+    return std::min(alignment<T>(p, cols, row), alignment<T>(p, cols, worker));
 }
 
 template <typename T>
 cudaError_t gather(const LceParams& prm, cudaStream_t stream)
 {
     const dim3 grid((unsigned)ceil_div(prm.tokens_padded, kRowThreads / 32), (unsigned)prm.n);
-    if (aligned_source<T>(prm.hidden, prm.cols, prm.hidden_row, prm.hidden_worker))
-        rps_lce_gather_kernel<T, true><<<grid, kRowThreads, 0, stream>>>(prm);
-    else
-        rps_lce_gather_kernel<T, false><<<grid, kRowThreads, 0, stream>>>(prm);
+    const int align = aligned_source<T>(prm.hidden, prm.cols, prm.hidden_row, prm.hidden_worker);
+    const auto kernel = align == 16 ? rps_lce_gather_kernel<T, 16> : align == 4 ? rps_lce_gather_kernel<T, 4> : rps_lce_gather_kernel<T, sizeof(T)>;
+    kernel<<<grid, kRowThreads, 0, stream>>>(prm);
     return cudaGetLastError();
 }
 
@@ -238,10 +238,9 @@ cudaError_t planes(const PlanesParams& prm, cudaStream_t stream)
     if (err != cudaSuccess) return err;
     const int64_t blocks = ceil_div(prm.rows * (prm.dst_row / 8), kRowThreads), resident = ceil_div((int64_t)sms * 8, prm.n);
     const dim3 grid((unsigned)(blocks < resident ? blocks : resident), (unsigned)prm.n);
-    if (aligned_source<T>(prm.src, prm.cols, prm.src_row, prm.src_worker))
-        rps_planes_kernel<T, true><<<grid, kRowThreads, 0, stream>>>(prm);
-    else
-        rps_planes_kernel<T, false><<<grid, kRowThreads, 0, stream>>>(prm);
+    const int align = aligned_source<T>(prm.src, prm.cols, prm.src_row, prm.src_worker);
+    const auto kernel = align == 16 ? rps_planes_kernel<T, 16> : align == 4 ? rps_planes_kernel<T, 4> : rps_planes_kernel<T, sizeof(T)>;
+    kernel<<<grid, kRowThreads, 0, stream>>>(prm);
     return cudaGetLastError();
 }
 

@@ -3,21 +3,25 @@
 // Bound by memory: forward reads x, f (and gate) and writes h, y; backward reads dh, dy, f, h (and gate) and writes dx, df
 // (and dgate).  So every tensor is touched once.  A row is spread over a CTA of at most 512 threads, 16 bytes of it to a thread (a wider
 // row over a cluster of CTAs that exchange their sums through distributed shared memory), so that a row lives in
-// registers between its sums and its results; CTAs walk many rows and read the next row before they work on this one.
+// registers between its sums and its results.  CTAs walk many rows; each thread copies its own slices of the next kAhead rows into
+// shared memory meanwhile (cp.async: no registers, and no barrier, as a thread reads what it copied itself).
 //
 // Backward needs two means of a row, of a * h and of b * f, where b depends on the first one.  With q = scale * gate * post * f,
 //   sum b f = sum q (dh + r_h a) - r_h^3 mean(a h) sum q h,
 // so both come out of three sums made in one pass, with one barrier for a row.  The sums over rows (dpost, dpre, and dgate where
 // tokens share a gate) stay in the registers of the thread that owns the columns; a block writes its own once, and a
 // second kernel adds the blocks' in a fixed order.
-#include "rps_rows.cuh"
+#include <algorithm>
 
 #include "rps_kernels.h"
+#include "rps_rows.cuh"
 
 namespace rps_ops {
 namespace {
 
 constexpr int kMostThreads = 512;
+constexpr int kSlots = 4, kAhead = kSlots - 1;      // rows in shared memory: this one and those ahead
+constexpr int kForwardThreads = 1024, kBackwardThreads = 512;  // resident on an SM: 48 KB and 40 KB of slots for each row
 constexpr int kMostCluster = 8;
 constexpr int kMostWarps = kMostThreads / 32 * kMostCluster;
 
@@ -69,33 +73,51 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float (*slots)[N][kMostW
     }
 }
 
-template <typename T, bool ALIGNED, bool PACK>
-__global__ void __launch_bounds__(kMostThreads, 2) rps_norm_forward_kernel(const NormParams prm)
+// This thread's slots: `arrays` of 16 bytes for each row of the ring.
+template <int ARRAYS>
+__device__ __forceinline__ uint32_t slot_of(uint32_t slots, int turn, int array)
+{
+    return slots + ((uint32_t)(turn * ARRAYS + array) * blockDim.x + threadIdx.x) * 16;
+}
+
+template <typename T, int ALIGN, bool PACK>
+__global__ void __launch_bounds__(kMostThreads, kForwardThreads / kMostThreads) rps_norm_forward_kernel(const NormParams prm)
 {
     constexpr int W = Slice<T>::kWidth;
+    extern __shared__ uint4 ring[];
     __shared__ float slots[2][1][kMostWarps];
+    const uint32_t copied = (uint32_t)__cvta_generic_to_shared(ring);
     const int cluster = prm.cluster, D = (int)prm.cols;
     const uint32_t rank = cluster > 1 ? cluster_rank() : 0;
     const int c = ((int)rank * blockDim.x + threadIdx.x) * W;
-    const int64_t rows = prm.n * prm.tokens, step = gridDim.x / cluster;
+    const uint32_t rows = (uint32_t)(prm.n * prm.tokens), step = gridDim.x / cluster, tokens = (uint32_t)prm.tokens;
     const float inv = 1.0f / (float)D;
-    int64_t row = blockIdx.x / cluster;
-    uint4 x_next, f_next, gate_next;
-    const auto read = [&](int64_t r) {
-        const int64_t w = r / prm.tokens, t = r - w * prm.tokens;
-        x_next = load_slice<T, ALIGNED, true>(static_cast<const T*>(prm.x) + r * D, c, D);
-        f_next = load_slice<T, ALIGNED, true>(static_cast<const T*>(prm.f) + r * D, c, D);
-        gate_next = load_slice<T, ALIGNED, false>(static_cast<const T*>(prm.gate) + w * prm.gate_worker + t / prm.rows_per_gate * D, c, D);
+    int into = 0;
+    const auto send = [&](uint32_t r) {
+        if (r < rows) {
+            const uint32_t w = r / tokens, g = (r - w * tokens) / (uint32_t)prm.rows_per_gate;
+            copy_slice<T, ALIGN>(slot_of<3>(copied, into, 0), static_cast<const T*>(prm.x) + (int64_t)r * D, c, D);
+            copy_slice<T, ALIGN>(slot_of<3>(copied, into, 1), static_cast<const T*>(prm.f) + (int64_t)r * D, c, D);
+            copy_slice<T, ALIGN>(slot_of<3>(copied, into, 2), static_cast<const T*>(prm.gate) + w * prm.gate_worker + (int64_t)g * D, c, D);
+        }
+        copies_sent();
+        into = into + 1 == kSlots ? 0 : into + 1;
     };
-    if (row < rows) read(row);
-    int turn = 0;
+    uint32_t row = blockIdx.x / cluster;
+    for (int i = 0; i < kAhead; ++i) send(row + i * step);
+    int turn = 0, from = 0;
     for (; row < rows; row += step) {
         float x[W], f[W], gate[W], post[W], pre[W];
-        widen(x_next, x), widen(f_next, f), widen(gate_next, gate);
-        const int64_t w = row / prm.tokens;
-        widen(load_slice<T, ALIGNED, false>(static_cast<const T*>(prm.post) + w * prm.post_worker, c, D), post);
-        widen(load_slice<T, ALIGNED, false>(static_cast<const T*>(prm.pre) + w * prm.pre_worker, c, D), pre);
-        if (row + step < rows) read(row + step);
+        const uint32_t w = row / tokens;
+        const uint4 post_slice = load_slice<T, ALIGN, false>(static_cast<const T*>(prm.post) + w * prm.post_worker, c, D);
+        const uint4 pre_slice = load_slice<T, ALIGN, false>(static_cast<const T*>(prm.pre) + w * prm.pre_worker, c, D);
+        send(row + kAhead * step);
+        copies_arrived<kAhead>();
+        widen(read_slot(slot_of<3>(copied, from, 0)), x);
+        widen(read_slot(slot_of<3>(copied, from, 1)), f);
+        widen(read_slot(slot_of<3>(copied, from, 2)), gate);
+        from = from + 1 == kSlots ? 0 : from + 1;
+        widen(post_slice, post), widen(pre_slice, pre);
         float s[1] = {0.0f};
 #pragma unroll
         for (int j = 0; j < W; ++j) s[0] = fmaf(f[j], f[j], s[0]);
@@ -103,7 +125,7 @@ __global__ void __launch_bounds__(kMostThreads, 2) rps_norm_forward_kernel(const
         const float r_f = rsqrtf(fmaf(s[0], inv, prm.eps));
         if constexpr (PACK) {
             const bool in = c < prm.pitch;
-            pack_slice(f, in ? prm.f_codes + row * prm.pitch + c : nullptr, c < D ? prm.f_scales + row * prm.groups + c / RPS_PACK_GROUP : nullptr);
+            pack_slice(f, in ? prm.f_codes + (int64_t)row * prm.pitch + c : nullptr, c < D ? prm.f_scales + (int64_t)row * prm.groups + c / RPS_PACK_GROUP : nullptr);
         }
         s[0] = 0.0f;
 #pragma unroll
@@ -112,23 +134,23 @@ __global__ void __launch_bounds__(kMostThreads, 2) rps_norm_forward_kernel(const
             s[0] = fmaf(x[j], x[j], s[0]);
         }
         const uint4 h = narrow(x);
-        store_slice<T, ALIGNED>(static_cast<T*>(prm.h) + row * D, c, D, h);
+        store_slice<T, ALIGN>(static_cast<T*>(prm.h) + (int64_t)row * D, c, D, h);
         row_sums<1>(s, slots, turn, cluster, rank), turn ^= 1;
         const float r_h = rsqrtf(fmaf(s[0], inv, prm.eps));
         if constexpr (PACK) {
             float stored[W];  // as a reader of h sees it
             widen(h, stored);
-            if constexpr (!ALIGNED) {
+            if constexpr (ALIGN != 16) {
 #pragma unroll
                 for (int j = 0; j < W; ++j)
                     if (c + j >= D) stored[j] = 0.0f;
             }
-            pack_slice(stored, c < prm.pitch ? prm.h_codes + row * prm.pitch + c : nullptr,
-                       c < D ? prm.h_scales + row * prm.groups + c / RPS_PACK_GROUP : nullptr);
+            pack_slice(stored, c < prm.pitch ? prm.h_codes + (int64_t)row * prm.pitch + c : nullptr,
+                       c < D ? prm.h_scales + (int64_t)row * prm.groups + c / RPS_PACK_GROUP : nullptr);
         }
 #pragma unroll
         for (int j = 0; j < W; ++j) x[j] = x[j] * r_h * pre[j];
-        store_slice<T, ALIGNED>(static_cast<T*>(prm.y) + row * D, c, D, narrow(x));
+        store_slice<T, ALIGN>(static_cast<T*>(prm.y) + (int64_t)row * D, c, D, narrow(x));
         if (prm.r_f != nullptr && rank == 0 && threadIdx.x == 0) {
             prm.r_f[row] = r_f;
             prm.r_h[row] = r_h;
@@ -138,11 +160,13 @@ __global__ void __launch_bounds__(kMostThreads, 2) rps_norm_forward_kernel(const
     if (cluster > 1) asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
 }
 
-template <typename T, bool ALIGNED, bool PACKED>
-__global__ void __launch_bounds__(kMostThreads, 1) rps_norm_backward_kernel(const NormParams prm)
+template <typename T, int ALIGN, bool PACKED>
+__global__ void __launch_bounds__(kMostThreads, kBackwardThreads / kMostThreads) rps_norm_backward_kernel(const NormParams prm)
 {
     constexpr int W = Slice<T>::kWidth;
+    extern __shared__ uint4 ring[];
     __shared__ float slots[2][3][kMostWarps];
+    const uint32_t copied = (uint32_t)__cvta_generic_to_shared(ring);
     const int cluster = prm.cluster, D = (int)prm.cols;
     const uint32_t rank = cluster > 1 ? cluster_rank() : 0;
     const int c = ((int)rank * blockDim.x + threadIdx.x) * W;
@@ -157,48 +181,66 @@ __global__ void __launch_bounds__(kMostThreads, 1) rps_norm_backward_kernel(cons
         first = block * prm.rows_per_block;
         end = min(first + prm.rows_per_block, prm.tokens);
     }
-    const uint4 post_slice = load_slice<T, ALIGNED, false>(static_cast<const T*>(prm.post) + w * prm.post_worker, c, D);
-    const uint4 pre_slice = load_slice<T, ALIGNED, false>(static_cast<const T*>(prm.pre) + w * prm.pre_worker, c, D);
+    const uint4 post_slice = load_slice<T, ALIGN, false>(static_cast<const T*>(prm.post) + w * prm.post_worker, c, D);
+    const uint4 pre_slice = load_slice<T, ALIGN, false>(static_cast<const T*>(prm.pre) + w * prm.pre_worker, c, D);
     float dpost[W] = {}, dpre[W] = {}, dgate[W] = {};
 
-    uint4 dh_next = make_uint4(0, 0, 0, 0), dy_next, f_next, h_next, gate_next;
-    Codes<W> f_codes, h_codes;
-    float f_scale, h_scale, rf_next, rh_next;
-    int64_t gate_row = first / prm.rows_per_gate, in_gate = first - gate_row * prm.rows_per_gate;  // of the next row to be read
-    const auto read = [&](int64_t t) {
-        const int64_t r = w * prm.tokens + t;
-        dy_next = load_slice<T, ALIGNED, true>(static_cast<const T*>(prm.dy) + r * D, c, D);
-        if (prm.dh != nullptr) dh_next = load_slice<T, ALIGNED, true>(static_cast<const T*>(prm.dh) + r * D, c, D);
-        if constexpr (PACKED) {
-            f_codes.clear(), h_codes.clear(), f_scale = h_scale = 0.0f;
-            if (c < D) {
-                f_codes.load(static_cast<const int8_t*>(prm.f) + r * prm.pitch + c);
-                h_codes.load(static_cast<const int8_t*>(prm.h_in) + r * prm.pitch + c);
-                f_scale = prm.f_scales[r * prm.groups + c / RPS_PACK_GROUP];
-                h_scale = prm.h_scales[r * prm.groups + c / RPS_PACK_GROUP];
+    float rf_next = 0.0f, rh_next = 0.0f;
+    int64_t gate_row = first / prm.rows_per_gate, in_gate = first - gate_row * prm.rows_per_gate;  // of the next row to be copied
+    int64_t left_in_gate = prm.rows_per_gate - in_gate;
+    int into = 0;
+    const auto send = [&](int64_t t) {
+        if (t < end) {
+            const int64_t r = w * prm.tokens + t;
+            copy_slice<T, ALIGN>(slot_of<5>(copied, into, 0), static_cast<const T*>(prm.dy) + r * D, c, D);
+            if (prm.dh != nullptr) copy_slice<T, ALIGN>(slot_of<5>(copied, into, 1), static_cast<const T*>(prm.dh) + r * D, c, D);
+            copy_slice<T, ALIGN>(slot_of<5>(copied, into, 2), static_cast<const T*>(prm.gate) + w * prm.gate_worker + gate_row * D, c, D);
+            if constexpr (PACKED) {  // the codes, and behind them the scale
+                const bool in = c < D;
+                const int64_t at = in ? r * prm.pitch + c : 0, group = in ? r * prm.groups + c / RPS_PACK_GROUP : 0;
+                copy_async<W>(slot_of<5>(copied, into, 3), static_cast<const int8_t*>(prm.f) + at, in);
+                copy_async<4>(slot_of<5>(copied, into, 3) + 8, prm.f_scales + group, in);
+                copy_async<W>(slot_of<5>(copied, into, 4), static_cast<const int8_t*>(prm.h_in) + at, in);
+                copy_async<4>(slot_of<5>(copied, into, 4) + 8, prm.h_scales + group, in);
+            } else {
+                copy_slice<T, ALIGN>(slot_of<5>(copied, into, 3), static_cast<const T*>(prm.f) + r * D, c, D);
+                copy_slice<T, ALIGN>(slot_of<5>(copied, into, 4), static_cast<const T*>(prm.h_in) + r * D, c, D);
             }
-        } else {
-            f_next = load_slice<T, ALIGNED, true>(static_cast<const T*>(prm.f) + r * D, c, D);
-            h_next = load_slice<T, ALIGNED, true>(static_cast<const T*>(prm.h_in) + r * D, c, D);
+            if (++in_gate == prm.rows_per_gate) in_gate = 0, ++gate_row;
         }
-        gate_next = load_slice<T, ALIGNED, false>(static_cast<const T*>(prm.gate) + w * prm.gate_worker + gate_row * D, c, D);
-        if (++in_gate == prm.rows_per_gate) in_gate = 0, ++gate_row;
-        rf_next = prm.r_f[r], rh_next = prm.r_h[r];
+        copies_sent();
+        into = into + 1 == kSlots ? 0 : into + 1;
     };
-    if (first < end) read(first);
-    int64_t left_in_gate = prm.rows_per_gate - (first - first / prm.rows_per_gate * prm.rows_per_gate);
-    int turn = 0;
+    const auto kept = [&](int from, int array, float (&v)[W]) {
+        const uint4 slot = read_slot(slot_of<5>(copied, from, array));
+        if constexpr (PACKED) {
+            Codes<W> codes;
+            codes.w[0] = slot.x;
+            if constexpr (W == 8) codes.w[1] = slot.y;
+            codes.values(__uint_as_float(slot.z), v);
+        } else {
+            widen(slot, v);
+        }
+    };
+    const auto statistics = [&](int64_t t) {
+        if (t < end) rf_next = __ldg(prm.r_f + w * prm.tokens + t), rh_next = __ldg(prm.r_h + w * prm.tokens + t);
+    };
+    for (int i = 0; i < kAhead; ++i) send(first + i);
+    statistics(first);
+    int turn = 0, from = 0;
     for (int64_t t = first; t < end; ++t) {
         const int64_t row = w * prm.tokens + t;
-        float f[W], h[W], dy[W], dx[W], gate[W], post[W];
-        if constexpr (PACKED) {
-            f_codes.values(f_scale, f), h_codes.values(h_scale, h);
-        } else {
-            widen(f_next, f), widen(h_next, h);
-        }
-        widen(dy_next, dy), widen(dh_next, dx), widen(gate_next, gate), widen(post_slice, post);
+        float f[W], h[W], dy[W], dx[W] = {}, gate[W], post[W];
+        send(t + kAhead);
+        copies_arrived<kAhead>();
+        widen(read_slot(slot_of<5>(copied, from, 0)), dy);
+        if (prm.dh != nullptr) widen(read_slot(slot_of<5>(copied, from, 1)), dx);
+        widen(read_slot(slot_of<5>(copied, from, 2)), gate);
+        kept(from, 3, f), kept(from, 4, h);
+        from = from + 1 == kSlots ? 0 : from + 1;
+        widen(post_slice, post);
         const float r_f = rf_next, r_h = rh_next;
-        if (t + 1 < end) read(t + 1);
+        statistics(t + 1);
         float s[3] = {};
         {
             float pre[W];
@@ -225,12 +267,12 @@ __global__ void __launch_bounds__(kMostThreads, 1) rps_norm_backward_kernel(cons
             dpost[j] = fmaf(g * gate[j], n, dpost[j]);
             df[j] = r_f * (g * gate[j] * post[j] - f[j] * mean_f);
         }
-        store_slice<T, ALIGNED>(static_cast<T*>(prm.dx) + row * D, c, D, narrow(dx));
-        store_slice<T, ALIGNED>(static_cast<T*>(prm.df) + row * D, c, D, narrow(df));
+        store_slice<T, ALIGN>(static_cast<T*>(prm.dx) + row * D, c, D, narrow(dx));
+        store_slice<T, ALIGN>(static_cast<T*>(prm.df) + row * D, c, D, narrow(df));
         if (--left_in_gate == 0) {
             left_in_gate = prm.rows_per_gate;
             if (prm.chunks == 0) {  // the block held the whole gate group
-                store_slice<T, ALIGNED>(static_cast<T*>(prm.dgate) + (w * prm.gates + t / prm.rows_per_gate) * D, c, D, narrow(dgate));
+                store_slice<T, ALIGN>(static_cast<T*>(prm.dgate) + (w * prm.gates + t / prm.rows_per_gate) * D, c, D, narrow(dgate));
 #pragma unroll
                 for (int j = 0; j < W; ++j) dgate[j] = 0.0f;
             }
@@ -274,8 +316,6 @@ __global__ void __launch_bounds__(512) rps_norm_reduce_kernel(const NormParams p
     }
 }
 
-bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
-
 // Threads of a CTA and CTAs of a cluster for a row of `slices` 16-byte slices: the fewest threads (a power of two of
 // warps) that hold it, up to 512, then a cluster.
 void shape_of_row(int64_t slices, int* threads, int* cluster)
@@ -285,11 +325,15 @@ void shape_of_row(int64_t slices, int* threads, int* cluster)
     while (*threads * *cluster < slices) *cluster *= 2;
 }
 
+// `arrays` slices of each of kSlots rows to a thread in shared memory.
 template <typename Kernel>
-cudaError_t launch_rows(Kernel kernel, const NormParams& prm, dim3 grid, int threads, cudaStream_t stream)
+cudaError_t launch_rows(rps::LaunchState& state, Kernel kernel, const NormParams& prm, dim3 grid, int threads, int arrays, cudaStream_t stream)
 {
+    const uint32_t bytes = (uint32_t)(threads * 16 * arrays * kSlots);
+    cudaError_t err = rps::grant_smem(state, kernel, bytes);
+    if (err != cudaSuccess) return err;
     cudaLaunchConfig_t config{};
-    config.gridDim = grid, config.blockDim = dim3((unsigned)threads), config.stream = stream;
+    config.gridDim = grid, config.blockDim = dim3((unsigned)threads), config.dynamicSmemBytes = bytes, config.stream = stream;
     cudaLaunchAttribute attribute{};
     attribute.id = cudaLaunchAttributeClusterDimension;
     attribute.val.clusterDim.x = (unsigned)prm.cluster, attribute.val.clusterDim.y = attribute.val.clusterDim.z = 1;
@@ -297,45 +341,64 @@ cudaError_t launch_rows(Kernel kernel, const NormParams& prm, dim3 grid, int thr
     return cudaLaunchKernelEx(&config, kernel, prm);
 }
 
+template <typename T, int ALIGN, bool PACK>
+cudaError_t run_forward(const NormParams& prm, dim3 grid, int threads, cudaStream_t stream)
+{
+    static rps::LaunchState state;
+    return launch_rows(state, rps_norm_forward_kernel<T, ALIGN, PACK>, prm, grid, threads, 3, stream);
+}
+
+template <typename T, int ALIGN, bool PACKED>
+cudaError_t run_backward(const NormParams& prm, dim3 grid, int threads, cudaStream_t stream)
+{
+    static rps::LaunchState state;
+    return launch_rows(state, rps_norm_backward_kernel<T, ALIGN, PACKED>, prm, grid, threads, 5, stream);
+}
+
+// What all arrays of a call can be moved in.
+template <typename T>
+int common_alignment(const NormParams& prm)
+{
+    int align = std::min({alignment<T>(prm.gate, prm.cols, prm.gate_worker), alignment<T>(prm.post, prm.cols, prm.post_worker),
+                          alignment<T>(prm.pre, prm.cols, prm.pre_worker)});
+    for (const void* p : {prm.x, prm.dh, prm.dy, (const void*)prm.h, (const void*)prm.y, (const void*)prm.dx, (const void*)prm.df, (const void*)prm.dgate,
+                          prm.packed ? nullptr : prm.f, prm.packed ? nullptr : prm.h_in})
+        align = std::min(align, alignment<T>(p, prm.cols, 0));
+    return align;
+}
+
 template <typename T>
 cudaError_t forward(NormParams prm, cudaStream_t stream)
 {
-    constexpr int W = Slice<T>::kWidth;
+    const bool pack = prm.f_codes != nullptr;
     int threads = 0, sms = 0;
-    shape_of_row(ceil_div(prm.f_codes != nullptr ? prm.pitch : prm.cols, W), &threads, &prm.cluster);
+    shape_of_row(ceil_div(pack ? prm.pitch : prm.cols, Slice<T>::kWidth), &threads, &prm.cluster);
     cudaError_t err = sm_count(&sms);
     if (err != cudaSuccess) return err;
-    const bool aligned = prm.cols % W == 0 && aligned16(prm.x) && aligned16(prm.f) && aligned16(prm.gate) && aligned16(prm.post) &&
-                         aligned16(prm.pre) && aligned16(prm.h) && aligned16(prm.y) && prm.gate_worker % W == 0 && prm.post_worker % W == 0 &&
-                         prm.pre_worker % W == 0;
-    // 1024 threads of an SM are resident; more rows than that come round by round
-    const int64_t rows = prm.n * prm.tokens, resident = (int64_t)sms * (1024 / threads) / prm.cluster;
+    const int align = common_alignment<T>(prm);
+    const int64_t rows = prm.n * prm.tokens, resident = (int64_t)sms * (kForwardThreads / threads) / prm.cluster;
     const dim3 grid((unsigned)((rows < resident ? rows : resident) * prm.cluster));
-    if (prm.f_codes != nullptr)
-        return aligned ? launch_rows(rps_norm_forward_kernel<T, true, true>, prm, grid, threads, stream)
-                       : launch_rows(rps_norm_forward_kernel<T, false, true>, prm, grid, threads, stream);
-    return aligned ? launch_rows(rps_norm_forward_kernel<T, true, false>, prm, grid, threads, stream)
-                   : launch_rows(rps_norm_forward_kernel<T, false, false>, prm, grid, threads, stream);
+    constexpr int kLeast = sizeof(T);
+    if (align == 16) return pack ? run_forward<T, 16, true>(prm, grid, threads, stream) : run_forward<T, 16, false>(prm, grid, threads, stream);
+    if (align == 4) return pack ? run_forward<T, 4, true>(prm, grid, threads, stream) : run_forward<T, 4, false>(prm, grid, threads, stream);
+    return pack ? run_forward<T, kLeast, true>(prm, grid, threads, stream) : run_forward<T, kLeast, false>(prm, grid, threads, stream);
 }
 
 template <typename T>
 cudaError_t backward(NormParams prm, cudaStream_t stream)
 {
-    constexpr int W = Slice<T>::kWidth;
     int threads = 0;
-    shape_of_row(ceil_div(prm.cols, W), &threads, &prm.cluster);
-    const bool values = prm.packed || (aligned16(prm.f) && aligned16(prm.h_in));
-    const bool aligned = values && prm.cols % W == 0 && aligned16(prm.dh) && aligned16(prm.dy) && aligned16(prm.gate) && aligned16(prm.post) &&
-                         aligned16(prm.pre) && aligned16(prm.dx) && aligned16(prm.df) && aligned16(prm.dgate) && prm.gate_worker % W == 0 &&
-                         prm.post_worker % W == 0 && prm.pre_worker % W == 0;
+    shape_of_row(ceil_div(prm.cols, Slice<T>::kWidth), &threads, &prm.cluster);
+    const int align = common_alignment<T>(prm);
     const dim3 grid((unsigned)(prm.blocks * prm.cluster), (unsigned)prm.n);
+    constexpr int kLeast = sizeof(T);
     cudaError_t err;
-    if (prm.packed)
-        err = aligned ? launch_rows(rps_norm_backward_kernel<T, true, true>, prm, grid, threads, stream)
-                      : launch_rows(rps_norm_backward_kernel<T, false, true>, prm, grid, threads, stream);
+    if (align == 16)
+        err = prm.packed ? run_backward<T, 16, true>(prm, grid, threads, stream) : run_backward<T, 16, false>(prm, grid, threads, stream);
+    else if (align == 4)
+        err = prm.packed ? run_backward<T, 4, true>(prm, grid, threads, stream) : run_backward<T, 4, false>(prm, grid, threads, stream);
     else
-        err = aligned ? launch_rows(rps_norm_backward_kernel<T, true, false>, prm, grid, threads, stream)
-                      : launch_rows(rps_norm_backward_kernel<T, false, false>, prm, grid, threads, stream);
+        err = prm.packed ? run_backward<T, kLeast, true>(prm, grid, threads, stream) : run_backward<T, kLeast, false>(prm, grid, threads, stream);
     if (err != cudaSuccess) return err;
     const int64_t jobs = 2 + (prm.chunks > 0 ? prm.gates : 0);
     rps_norm_reduce_kernel<T><<<dim3((unsigned)ceil_div(prm.cols, 32), (unsigned)(jobs < 4096 ? jobs : 4096), (unsigned)prm.n), 512, 0, stream>>>(prm);
@@ -350,7 +413,7 @@ void plan_norm_backward(NormParams* prm)
     shape_of_row(ceil_div(prm->cols, prm->f32 ? Slice<float>::kWidth : Slice<bf16>::kWidth), &threads, &cluster);
     // as many blocks over all workers as are resident at once (512 threads of each of the 148 SMs); of the two nearest ways
     // to cut the rows the one whose longest SM has fewer of them
-    int64_t want = (int64_t)148 * (kMostThreads / threads) / cluster / prm->n;
+    int64_t want = (int64_t)148 * (kBackwardThreads / threads) / cluster / prm->n;
     if (want < 1) want = 1;
     const int64_t rows = prm->rows_per_gate, target = ceil_div(prm->tokens, want);
     const bool whole = rows <= target;

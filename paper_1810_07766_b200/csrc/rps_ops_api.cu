@@ -91,7 +91,9 @@ struct LcePlan {
     int64_t piece = 0;
     bf16* weight = nullptr;
     bf16* dl = nullptr;
-    float* acc = nullptr;
+    float* hidden_parts = nullptr;
+    float* weight_parts = nullptr;
+    int hidden_splits = 1, weight_splits = 1;
     size_t bytes = 0;
 };
 
@@ -138,7 +140,11 @@ LcePlan plan_lce(const rps_lce_desc& d, const void* weight, bool backward, void*
         p.info = c.take<float2>(p.n * p.tokens_padded);
         plan.dl = c.take<bf16>(p.n * p.planes * p.tokens_padded * plan.piece);
         p.scale = c.take<float>(p.n);
-        if (plan.piece < whole) plan.acc = c.take<float>(p.n * p.tokens_padded * round_up(p.cols, kVocabTile));
+        const int64_t part_row = round_up(p.cols, kVocabTile);
+        plan.hidden_splits = product_splits(product_tiles(p.tokens, p.cols, p.n), product_blocks(plan.piece), p.planes);
+        if (plan.piece < whole || plan.hidden_splits > 1) plan.hidden_parts = c.take<float>(plan.hidden_splits * p.n * p.tokens_padded * part_row);
+        plan.weight_splits = product_splits(product_tiles(plan.piece, p.cols, p.n), product_blocks(p.tokens), p.planes);
+        if (plan.weight_splits > 1) plan.weight_parts = c.take<float>(plan.weight_splits * p.n * plan.piece * part_row);
     } else {
         p.done = c.take<int>(p.n);
         p.sums = c.take<float>(p.n * lce_merge_blocks(p.tokens));
@@ -151,8 +157,8 @@ LcePlan plan_lce(const rps_lce_desc& d, const void* weight, bool backward, void*
     g.workers = p.n, g.planes = p.planes, g.count = p.count;
     g.vocab = (int)p.vocab, g.stat_tiles = (int)p.stat_tiles, g.target = p.target;
     g.part = const_cast<float2*>(p.part), g.hit = const_cast<float*>(p.hit), g.info = p.info, g.dl = plan.dl;
-    g.tokens_padded = p.tokens_padded, g.piece = plan.piece, g.acc = plan.acc, g.rows = p.rows, g.tokens = p.tokens;
-    g.out_f32 = p.f32, g.acc_row = round_up(p.cols, kVocabTile), g.scale = p.scale;
+    g.tokens_padded = p.tokens_padded, g.piece = plan.piece, g.rows = p.rows, g.tokens = p.tokens;
+    g.part_row = round_up(p.cols, kVocabTile), g.scale = p.scale;
     return plan;
 }
 
@@ -263,13 +269,16 @@ extern "C" int rps_lce_backward(const rps_lce_desc* desc, const void* hidden, co
             g.a = h, g.b = weight_rows, g.m = (int)d.tokens, g.n = (int)rows, g.k = (int)d.cols;
             RPS_TRY(launch_product(Product::kDlogits, g, stream));
             g.a = dl, g.n = (int)d.cols, g.k = (int)rows;
-            g.first = v0 == 0, g.last = v0 + rows == d.vocab;
+            g.splits = plan.hidden_splits, g.parts = plan.hidden_parts, g.part_rows = p.tokens_padded, g.add = v0 > 0;
             g.out = dhidden, g.out_row = d.cols, g.out_worker = d.tokens * d.cols;
             RPS_TRY(launch_product(Product::kDhidden, g, stream));
+            if (g.parts != nullptr && v0 + rows == d.vocab) RPS_TRY(launch_join(Product::kDhidden, g, stream));
         }
         g.a = dl, g.b = h, g.m = (int)rows, g.n = (int)d.cols, g.k = (int)d.tokens;
-        g.out = dweight, g.out_row = d.dweight_row, g.out_worker = d.dweight_worker;
+        g.splits = plan.weight_splits, g.parts = plan.weight_parts, g.part_rows = plan.piece, g.add = 0;
+        g.out = static_cast<unsigned char*>(dweight) + v0 * d.dweight_row * (p.f32 ? 4 : 2), g.out_row = d.dweight_row, g.out_worker = d.dweight_worker;
         RPS_TRY(launch_product(Product::kDweight, g, stream));
+        if (g.parts != nullptr) RPS_TRY(launch_join(Product::kDweight, g, stream));
     }
     return RPS_OK;
 }
@@ -425,6 +434,8 @@ struct WgradPlan {
     PlanesParams lay_out{};
     PackParams unpack{};
     bool lay_out_dy = false;
+    int splits = 1;
+    float* parts = nullptr;
     size_t bytes = 0;
 };
 
@@ -462,6 +473,8 @@ WgradPlan plan_wgrad(const rps_wgrad_desc& d, const void* dy, void* workspace)
         q.src = dy, q.f32 = d.dtype == RPS_F32, q.n = d.n, q.planes = planes, q.rows = d.tokens, q.cols = d.outs;
         q.src_row = d.dy_row, q.src_worker = d.dy_worker, q.dst = to, q.dst_row = row, q.dst_plane = plane, q.dst_worker = planes * plane;
     }
+    plan.splits = product_splits(product_tiles(d.outs, d.cols, d.n), product_blocks(d.tokens), planes);
+    if (plan.splits > 1) plan.parts = c.take<float>(plan.splits * d.n * round_up(d.outs, kVocabTile) * round_up(d.cols, kVocabTile));
     plan.bytes = c.used;
     return plan;
 }
@@ -496,7 +509,9 @@ extern "C" int rps_packed_wgrad(const rps_wgrad_desc* desc, const void* dy, cons
     ProductParams g{};
     g.a = plan.dy, g.b = plan.x, g.workers = d.n, g.planes = d.dtype == RPS_F32 ? 3 : 1;
     g.m = (int)d.outs, g.n = (int)d.cols, g.k = (int)d.tokens;
-    g.out = dweight, g.out_row = d.dweight_row, g.out_worker = d.dweight_worker, g.out_f32 = d.dtype == RPS_F32;
+    g.out = dweight, g.out_row = d.dweight_row, g.out_worker = d.dweight_worker;
+    g.splits = plan.splits, g.parts = plan.parts, g.part_rows = round_up(d.outs, kVocabTile), g.part_row = round_up(d.cols, kVocabTile);
     RPS_TRY(launch_product(Product::kDweight, g, stream));
+    if (g.parts != nullptr) RPS_TRY(launch_join(Product::kDweight, g, stream));
     return RPS_OK;
 }

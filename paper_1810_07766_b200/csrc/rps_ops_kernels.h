@@ -37,7 +37,7 @@ enum class Product {
 
 struct ProductParams {
     Operand a, b;
-    int workers, planes;
+    int workers, planes;  // three planes: fp32 operands and results, one: bf16
     int m, n, k;        // upper bounds where the token count (m, or k in kDweight) is the device's to say
     const int* count;   // [worker] tokens that take part, or NULL: all
     // kLse, kDlogits
@@ -49,20 +49,26 @@ struct ProductParams {
     const float2* info;     // [worker][tokens_padded]: lse, g
     bf16* dl;               // [worker][plane][tokens_padded][piece]
     int64_t tokens_padded, piece;
-    // kDhidden
-    float* acc;             // [worker][tokens_padded][acc_row], acc_row a multiple of the tile
-    int64_t acc_row;
-    const int* rows;        // [worker][tokens]: token of each row
-    int64_t tokens;
-    int first, last;        // first and last piece
-    // kDhidden, kDweight
+    // kDhidden, kDweight: the result, scaled and in the caller's type, or (part != NULL) fp32 parts of it that launch_join adds up
     void* out;
     int64_t out_row, out_worker;
-    int out_f32;
     const float* scale;     // [worker], or NULL: factor of the result
+    const int* rows;        // kDhidden: [worker][tokens]: token of each row
+    int64_t tokens;
+    // The summed axis may be cut into `splits` runs of blocks, each with its own part [split][worker][part_rows][part_row]; over several
+    // pieces of the vocabulary a part goes on growing (`add`).
+    int splits, add;
+    float* parts;
+    int64_t part_rows, part_row;  // multiples of the tile
 };
 
+// How many runs to cut a product's summed axis into, for `tiles` tiles of `blocks` blocks of 64 each.
+int product_splits(int64_t tiles, int64_t blocks, int planes);
+int64_t product_tiles(int64_t m, int64_t n, int workers);
+int64_t product_blocks(int64_t k);
+
 cudaError_t launch_product(Product which, const ProductParams& prm, cudaStream_t stream);
+cudaError_t launch_join(Product which, const ProductParams& prm, cudaStream_t stream);  // the parts into `out`
 cudaError_t read_gave_up(int* value, cudaStream_t stream);  // and clears it; synchronises
 cudaError_t sm_count(int* out);                             // of the current device
 

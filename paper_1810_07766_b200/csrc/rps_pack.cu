@@ -22,7 +22,7 @@ __device__ __forceinline__ Place place(uint32_t u, uint32_t units_per_row)
     return {row, (int)((u - row * units_per_row) * 32 + threadIdx.x % 32) * W};
 }
 
-template <typename T, bool ALIGNED>
+template <typename T, int ALIGN>
 __global__ void __launch_bounds__(kThreads) rps_pack_kernel(const PackParams prm, uint32_t units, uint32_t units_per_row)
 {
     constexpr int W = Slice<T>::kWidth;
@@ -36,7 +36,7 @@ __global__ void __launch_bounds__(kThreads) rps_pack_kernel(const PackParams prm
             const uint64_t u = u0 + (uint64_t)i * step;
             if (u >= units) break;
             at[i] = place<W>((uint32_t)u, units_per_row);
-            x[i] = load_slice<T, ALIGNED, true>(static_cast<const T*>(prm.x) + at[i].row * prm.x_row, at[i].c, D);
+            x[i] = load_slice<T, ALIGN, true>(static_cast<const T*>(prm.x) + at[i].row * prm.x_row, at[i].c, D);
         }
 #pragma unroll
         for (int i = 0; i < kUnits; ++i) {
@@ -60,7 +60,7 @@ __device__ __forceinline__ void load_codes(const PackParams& prm, const Place& a
     }
 }
 
-template <typename T, bool ALIGNED>
+template <typename T, int ALIGN>
 __global__ void __launch_bounds__(kThreads) rps_unpack_kernel(const PackParams prm, uint32_t units, uint32_t units_per_row)
 {
     constexpr int W = Slice<T>::kWidth;
@@ -81,7 +81,7 @@ __global__ void __launch_bounds__(kThreads) rps_unpack_kernel(const PackParams p
             if (u0 + (uint64_t)i * step >= units) break;
             float v[W];
             codes[i].values(scale[i], v);
-            store_slice<T, ALIGNED>(static_cast<T*>(prm.out) + at[i].row * prm.x_row, at[i].c, (int)prm.cols, narrow(v));
+            store_slice<T, ALIGN>(static_cast<T*>(prm.out) + at[i].row * prm.x_row, at[i].c, (int)prm.cols, narrow(v));
         }
     }
 }
@@ -137,23 +137,19 @@ cudaError_t launch_units(Kernel kernel, const PackParams& prm, int64_t row_cols,
 }
 
 template <typename T>
-bool aligned_rows(const void* p, const PackParams& prm)
-{
-    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && prm.x_row % Slice<T>::kWidth == 0 && prm.cols % Slice<T>::kWidth == 0;
-}
-
-template <typename T>
 cudaError_t pack(const PackParams& prm, cudaStream_t stream)
 {
-    return aligned_rows<T>(prm.x, prm) ? launch_units(rps_pack_kernel<T, true>, prm, prm.pitch, Slice<T>::kWidth, stream)
-                                       : launch_units(rps_pack_kernel<T, false>, prm, prm.pitch, Slice<T>::kWidth, stream);
+    const int align = alignment<T>(prm.x, prm.cols, prm.x_row);
+    return launch_units(align == 16 ? rps_pack_kernel<T, 16> : align == 4 ? rps_pack_kernel<T, 4> : rps_pack_kernel<T, sizeof(T)>, prm, prm.pitch,
+                        Slice<T>::kWidth, stream);
 }
 
 template <typename T>
 cudaError_t unpack(const PackParams& prm, cudaStream_t stream)
 {
-    return aligned_rows<T>(prm.out, prm) ? launch_units(rps_unpack_kernel<T, true>, prm, prm.cols, Slice<T>::kWidth, stream)
-                                         : launch_units(rps_unpack_kernel<T, false>, prm, prm.cols, Slice<T>::kWidth, stream);
+    const int align = alignment<T>(prm.out, prm.cols, prm.x_row);
+    return launch_units(align == 16 ? rps_unpack_kernel<T, 16> : align == 4 ? rps_unpack_kernel<T, 4> : rps_unpack_kernel<T, sizeof(T)>, prm,
+                        prm.cols, Slice<T>::kWidth, stream);
 }
 
 }  // namespace

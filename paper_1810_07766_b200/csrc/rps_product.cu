@@ -13,7 +13,7 @@
 // the other one contiguous, which the descriptors of the shared-memory tiles express; nothing is transposed.
 //
 // fp32 operands are three bf16 parts each (24 significant bits); of the nine products of parts the six that reach 2^-24
-// of the result are made, the smallest first, into the same accumulator.
+// of the result are made.  The three parts of a block lie in three stages of the ring, so each is copied once for its three products.
 #include <mutex>
 
 #include "rps_ops_kernels.h"
@@ -35,9 +35,10 @@ constexpr int kEpilogueWarps = 8;
 constexpr int kThreads = 32 * (2 + kEpilogueWarps);
 // The tensor cores cut an fp32 sum off after each step of 16 instead of rounding it, a bias that grows with the number of steps
 // (relative error of a 512-long sum of random terms: 5e-7).  Where fp32 accuracy is asked for, the summed axis goes
-// through in segments whose sums the epilogue adds in fp32, rounded: every 512 of fp32 operands' leading parts, and every 1024 for
-// the softmax statistics of bf16 operands.  An extra segment costs the epilogue about 600 cycles under at least 4096 of products.
-constexpr int kSegmentF32 = 8, kSegmentStatistics = 16;  // in blocks of kDepth
+// through in segments whose sums the epilogue adds in fp32, rounded: every 2 blocks of fp32 operands (48 steps), and every 16 blocks (64
+// steps) for the softmax statistics of bf16 operands.  Adding a segment takes the epilogue about 600 cycles under the 6144 or 8192
+// cycles of the products of the next one.
+constexpr int kSegmentF32 = 2, kSegmentStatistics = 16;  // in blocks of kDepth
 constexpr uint64_t kWaitNs = 2000000000ull;
 
 static_assert(kTileM == kTokenTile && kTileN == kVocabTile, "operands are padded to whole tiles");
@@ -207,78 +208,126 @@ __device__ __forceinline__ uint32_t two_bf16(float lo, float hi)
     return *reinterpret_cast<const uint32_t*>(&p);
 }
 
-// Part q of an fp32 value.
-__device__ __forceinline__ float part_of(float v, int q)
-{
-    const float lead = leading_bits(v), rest = rest_of(v, lead), mid = leading_bits(rest);
-    return q == 0 ? lead : q == 1 ? mid : rest - mid;
-}
+__device__ __forceinline__ void store_element(float* to, float e) { __stcg(to, e); }
+__device__ __forceinline__ void store_element(bf16* to, bf16 e) { __stcg(reinterpret_cast<unsigned short*>(to), __bfloat16_as_ushort(e)); }
 
-// `at`: offset of this lane's row in `out`, or -1 if it is not to be written; `cols` of the 128 columns exist.  ADD: to what is there
-// (fp32, wide).  PART: not the values but that part of them.
-template <bool ADD, bool PART, typename T>
-__device__ __forceinline__ void store_rows(Staging& stage, const float (&v)[kHalf], T* out, int64_t at, int cols, bool wide, int part = 0)
+// 64 bytes of each of the warp's rows, from column `c` on.  Loads come before stores, several at a time.
+template <bool ADD, typename T>
+__device__ __forceinline__ void store_chunk(Staging& stage, const uint4 (&mine)[4], T* out, int c, int cols, bool wide)
 {
     constexpr int kChunk = 64 / sizeof(T), kPart = 16 / sizeof(T);  // columns
     const int lane = threadIdx.x % 32;
     __syncwarp();
-    stage.at[lane] = at;
 #pragma unroll
-    for (int c = 0; c < kHalf / kChunk; ++c) {
-        __syncwarp();
+    for (int q = 0; q < 4; ++q) stage.part[lane][q ^ (lane >> 1 & 3)] = mine[q];
+    __syncwarp();
+    if (wide) {
+        const int col = c + lane % 4 * kPart;
+        uint4 word[4];
+        int64_t at[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = lane / 4 + 8 * i;
+            word[i] = stage.part[r][lane % 4 ^ (r >> 1 & 3)];
+            at[i] = stage.at[r];
+        }
+        if (col >= cols) return;
+        if constexpr (ADD) {
+            float4 old[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) old[i] = at[i] < 0 ? make_float4(0, 0, 0, 0) : __ldcg(reinterpret_cast<const float4*>(out + at[i] + col));
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                word[i] = make_uint4(__float_as_uint(__uint_as_float(word[i].x) + old[i].x), __float_as_uint(__uint_as_float(word[i].y) + old[i].y),
+                                     __float_as_uint(__uint_as_float(word[i].z) + old[i].z), __float_as_uint(__uint_as_float(word[i].w) + old[i].w));
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (at[i] < 0) continue;
+            T* to = out + at[i] + col;
+            if (col + kPart <= cols) {
+                __stcg(reinterpret_cast<uint4*>(to), word[i]);
+            } else {
+                const T* e = reinterpret_cast<const T*>(&word[i]);
+#pragma unroll
+                for (int k = 0; k < kPart; ++k)
+                    if (col + k < cols) store_element(to + k, e[k]);
+            }
+        }
+    } else {
+        constexpr int kRows = 32 / kChunk, kAtATime = 8;  // rows that the warp writes at a time, an element to a lane: 2 of fp32, 1 of bf16
+        const int col = lane % kChunk;
+        const bool there = c + col < cols;
+#pragma unroll 1
+        for (int r0 = 0; r0 < 32; r0 += kRows * kAtATime) {
+            T e[kAtATime];
+            int64_t at[kAtATime];
+#pragma unroll
+            for (int i = 0; i < kAtATime; ++i) {
+                const int r = r0 + i * kRows + lane / kChunk;
+                at[i] = stage.at[r];
+                e[i] = reinterpret_cast<const T*>(&stage.part[r][col / kPart ^ (r >> 1 & 3)])[col % kPart];
+            }
+#pragma unroll
+            for (int i = 0; i < kAtATime; ++i)
+                if (at[i] >= 0 && there) store_element(out + at[i] + c + col, e[i]);
+        }
+    }
+}
+
+// `at`: offset of this lane's row in `out`, or -1 if it is not to be written; `cols` of the 128 columns exist.  ADD: to what is there
+// (fp32, wide).
+template <bool ADD, typename T>
+__device__ __forceinline__ void store_rows(Staging& stage, const float (&v)[kHalf], T* out, int64_t at, int cols, bool wide)
+{
+    constexpr int kChunk = 64 / sizeof(T), kPart = 16 / sizeof(T);
+    __syncwarp();
+    stage.at[threadIdx.x % 32] = at;
+#pragma unroll
+    for (int c = 0; c < kHalf; c += kChunk) {
+        uint4 mine[4];
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            const float* f = v + c * kChunk + q * kPart;
-            uint4 word;
+            const float* f = v + c + q * kPart;
             if constexpr (sizeof(T) == 4)
-                word = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+                mine[q] = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
             else
-                word = PART ? make_uint4(two_bf16(part_of(f[0], part), part_of(f[1], part)), two_bf16(part_of(f[2], part), part_of(f[3], part)),
-                                         two_bf16(part_of(f[4], part), part_of(f[5], part)), two_bf16(part_of(f[6], part), part_of(f[7], part)))
-                            : make_uint4(two_bf16(f[0], f[1]), two_bf16(f[2], f[3]), two_bf16(f[4], f[5]), two_bf16(f[6], f[7]));
-            stage.part[lane][q ^ (lane >> 1 & 3)] = word;
+                mine[q] = make_uint4(two_bf16(f[0], f[1]), two_bf16(f[2], f[3]), two_bf16(f[4], f[5]), two_bf16(f[6], f[7]));
         }
-        __syncwarp();
-        if (wide) {
-            const int col = c * kChunk + lane % 4 * kPart;
+        store_chunk<ADD>(stage, mine, out, c, cols, wide);
+    }
+}
+
+// fp32 values as three planes of bf16 parts.
+__device__ __forceinline__ void store_parts(Staging& stage, float (&v)[kHalf], bf16* out, int64_t plane, int64_t at)
+{
+    __syncwarp();
+    stage.at[threadIdx.x % 32] = at;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int r = lane / 4 + 8 * i;
-                uint4 word = stage.part[r][lane % 4 ^ (r >> 1 & 3)];
-                const int64_t row_at = stage.at[r];
-                T* to = out + row_at + col;
-                if (row_at < 0 || col >= cols) continue;
-                if constexpr (ADD) {
-                    const float4 old = *reinterpret_cast<const float4*>(to);
-                    word = make_uint4(__float_as_uint(__uint_as_float(word.x) + old.x), __float_as_uint(__uint_as_float(word.y) + old.y),
-                                      __float_as_uint(__uint_as_float(word.z) + old.z), __float_as_uint(__uint_as_float(word.w) + old.w));
-                }
-                if (col + kPart <= cols) {
-                    *reinterpret_cast<uint4*>(to) = word;
-                } else {
-                    const T* e = reinterpret_cast<const T*>(&word);
+    for (int c = 0; c < kHalf; c += 32) {
 #pragma unroll
-                    for (int k = 0; k < kPart; ++k)
-                        if (col + k < cols) to[k] = e[k];
+        for (int q = 0; q < 3; ++q) {
+            uint4 mine[4];
+            uint32_t* word = reinterpret_cast<uint32_t*>(mine);
+#pragma unroll
+            for (int j = 0; j < 32; j += 2) {
+                float part[2];
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    float& f = v[c + j + k];
+                    part[k] = q < 2 ? leading_bits(f) : f;
+                    if (q < 2) f = rest_of(f, part[k]);
                 }
+                word[j / 2] = two_bf16(part[0], part[1]);
             }
-        } else {
-            constexpr int kRows = 32 / kChunk;  // rows that the warp writes at a time, an element to a lane: 2 of fp32, 1 of bf16
-            const int col = lane % kChunk;
-#pragma unroll 4
-            for (int r0 = 0; r0 < 32; r0 += kRows) {
-                const int r = r0 + lane / kChunk;
-                const int64_t to = stage.at[r];
-                const T e = reinterpret_cast<const T*>(&stage.part[r][col / kPart ^ (r >> 1 & 3)])[col % kPart];
-                if (to >= 0 && c * kChunk + col < cols) out[to + c * kChunk + col] = e;
-            }
+            store_chunk<false>(stage, mine, out + q * plane, c, kHalf, true);
         }
     }
 }
 
 // One row's 128 columns of a tile.
-template <Product WHICH>
-__device__ __forceinline__ void epilogue(const ProductParams& prm, int w, int row, int n0, int count, float (&v)[kHalf], bool wide, Staging& stage)
+template <Product WHICH, int PLANES>
+__device__ __forceinline__ void epilogue(const ProductParams& prm, int w, int split, int row, int n0, int count, float (&v)[kHalf], bool wide, Staging& stage)
 {
     const int cols = prm.n - n0;
     if (cols <= 0 && WHICH != Product::kDlogits) return;
@@ -308,53 +357,42 @@ __device__ __forceinline__ void epilogue(const ProductParams& prm, int w, int ro
         const bool in = row < count;
         const float2 info = in ? prm.info[w * prm.tokens_padded + row] : make_float2(0.0f, 0.0f);
         const int t = in ? prm.target[w * prm.tokens_padded + row] - prm.v0 - n0 : -1;
-        const int64_t at_dl = ((int64_t)w * prm.planes * prm.tokens_padded + row) * prm.piece + n0;
+        const int64_t at_dl = ((int64_t)w * PLANES * prm.tokens_padded + row) * prm.piece + n0;
         const float at = info.x * kLog2e;
 #pragma unroll
         for (int j = 0; j < kHalf; ++j) {
             const float p = exp2_fast(fmaf(v[j], kLog2e, -at)) - (j == t ? 1.0f : 0.0f);
             v[j] = in && j < cols ? info.y * p : 0.0f;
         }
-        if (prm.planes == 1) {
-            store_rows<false, false>(stage, v, prm.dl, at_dl, kHalf, true);
+        if constexpr (PLANES == 1) {
+            store_rows<false>(stage, v, prm.dl, at_dl, kHalf, true);
         } else {
-#pragma unroll 1
-            for (int q = 0; q < 3; ++q) store_rows<false, true>(stage, v, prm.dl + q * prm.tokens_padded * prm.piece, at_dl, kHalf, true, q);
+            store_parts(stage, v, prm.dl, prm.tokens_padded * prm.piece, at_dl);
         }
     } else {
         constexpr bool kHidden = WHICH == Product::kDhidden;
         const bool in = row < (kHidden ? count : prm.m);
-        if constexpr (kHidden) {
-            const int64_t at = in ? (w * prm.tokens_padded + row) * prm.acc_row + n0 : -1;
-            if (!prm.last) {
-                if (prm.first)
-                    store_rows<false, false>(stage, v, prm.acc, at, kHalf, true);
-                else
-                    store_rows<true, false>(stage, v, prm.acc, at, kHalf, true);
-                return;
-            }
-            if (!prm.first && in) {
-                const float* acc = prm.acc + at;
-#pragma unroll
-                for (int j = 0; j < kHalf; j += 4) {
-                    const float4 a = *reinterpret_cast<const float4*>(acc + j);
-                    v[j] += a.x, v[j + 1] += a.y, v[j + 2] += a.z, v[j + 3] += a.w;
-                }
-            }
+        if (prm.parts != nullptr) {
+            const int64_t at = in ? (((int64_t)split * prm.workers + w) * prm.part_rows + row) * prm.part_row + n0 : -1;
+            if (prm.add)
+                store_rows<true>(stage, v, prm.parts, at, kHalf, true);
+            else
+                store_rows<false>(stage, v, prm.parts, at, kHalf, true);
+            return;
         }
         const float g = prm.scale != nullptr ? prm.scale[w] : 1.0f;
-        const int64_t at = !in ? -1 : w * prm.out_worker + (kHidden ? (int64_t)prm.rows[w * prm.tokens + row] : (int64_t)(prm.v0 + row)) * prm.out_row + n0;
+        const int64_t at = !in ? -1 : w * prm.out_worker + (kHidden ? (int64_t)prm.rows[w * prm.tokens + row] : (int64_t)row) * prm.out_row + n0;
 #pragma unroll
         for (int j = 0; j < kHalf; ++j) v[j] *= g;
-        if (prm.out_f32)
-            store_rows<false, false>(stage, v, static_cast<float*>(prm.out), at, cols, wide);
+        if constexpr (PLANES == 3)
+            store_rows<false>(stage, v, static_cast<float*>(prm.out), at, cols, wide);
         else
-            store_rows<false, false>(stage, v, static_cast<bf16*>(prm.out), at, cols, wide);
+            store_rows<false>(stage, v, static_cast<bf16*>(prm.out), at, cols, wide);
     }
 }
 
 // ------------------------------------------------------------------------------------------------------------ kernel
-template <Product WHICH>
+template <Product WHICH, int PLANES>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     rps_product_kernel(const __grid_constant__ ProductParams prm, const __grid_constant__ Maps maps)
 {
@@ -400,30 +438,31 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tensor_memory = control.tensor_memory;
 
-    const int total = control.start[prm.workers], pairs = gridDim.x / 2;
+    const int tiles = control.start[prm.workers], pairs = gridDim.x / 2, total = tiles * prm.splits;
     struct Tile {
-        int w, m0, n0, blocks, count, first_segment;  // blocks up to the end of the first segment
+        int w, split, m0, n0, count, first, blocks;  // blocks of the summed axis: the first one and how many
     };
-    const int segment = prm.planes == 3 ? kSegmentF32 : WHICH == Product::kLse ? kSegmentStatistics : 0;  // 0: one segment
-    int worker = 0;
-    const auto tile_at = [&](int tile) {
-        while (tile >= control.start[worker + 1]) ++worker;
+    const auto tile_at = [&](int item) {
         Tile t;
-        t.w = worker;
-        tile -= control.start[worker];
-        const int m_tiles = (control.start[worker + 1] - control.start[worker]) / n_tiles;
+        t.split = item / tiles;
+        int tile = item - t.split * tiles;
+        t.w = 0;
+        while (tile >= control.start[t.w + 1]) ++t.w;
+        tile -= control.start[t.w];
+        const int m_tiles = (control.start[t.w + 1] - control.start[t.w]) / n_tiles;
         // kLse, kDlogits: all rows of a column of tiles before the next one, so that the weight is read from memory once; kDweight: all
         // columns of a row of tiles, for dl's sake
         const int m = kRowsFirst ? tile % m_tiles : tile / n_tiles, n = kRowsFirst ? tile / m_tiles : tile % n_tiles;
         t.m0 = m * kTileM, t.n0 = n * kTileN;
-        t.count = prm.count != nullptr ? prm.count[worker] : (WHICH == Product::kDweight ? prm.k : prm.m);
+        t.count = prm.count != nullptr ? prm.count[t.w] : (WHICH == Product::kDweight ? prm.k : prm.m);
         const int k = WHICH == Product::kDweight ? t.count : prm.k;
-        const int depth = (k + kDepth - 1) / kDepth;
-        t.blocks = depth * (prm.planes == 1 ? 1 : 6);
-        // of fp32 operands the five products that are small against the sixth are one segment with its beginning
-        t.first_segment = segment == 0 ? t.blocks : min(t.blocks, segment + (prm.planes == 1 ? 0 : 5 * depth));
+        const int depth = (k + kDepth - 1) / kDepth, run = (depth + prm.splits - 1) / prm.splits;
+        t.first = t.split * run;
+        t.blocks = max(0, min(depth - t.first, run));
         return t;
     };
+    // blocks to a segment
+    const int segment = PLANES == 3 ? kSegmentF32 : WHICH == Product::kLse ? kSegmentStatistics : 1 << 30;
     bool fine = true;
 
     if (warp == 0) {
@@ -432,30 +471,26 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             uint32_t phase = 0;
             for (int tile = blockIdx.x / 2; tile < total && fine; tile += pairs) {
                 const Tile t = tile_at(tile);
-                const int depth = prm.planes == 1 ? t.blocks : t.blocks / 6;
                 const int m0 = t.m0 + rank * 128, n0 = t.n0 + rank * 128;
                 const int wa = prm.a.worker != 0 ? t.w : 0, wb = prm.b.worker != 0 ? t.w : 0;
-                for (int kb = 0; kb < t.blocks; ++kb) {
+                for (int i = 0; i < t.blocks * PLANES; ++i) {
                     fine = wait(smem_addr(&control.empty[stage]), phase ^ 1);
                     if (!fine) break;
-                    const int product = kb / depth, k0 = (kb - product * depth) * kDepth;
-                    // parts of A and B: (2,0) (1,1) (0,2) (1,0) (0,1) (0,0)
-                    const int pa = prm.planes == 1 ? 0 : (0x001012 >> (4 * product)) & 3;
-                    const int pb = prm.planes == 1 ? 0 : (0x010210 >> (4 * product)) & 3;
+                    const int kb = PLANES == 1 ? i : i / 3, plane = i - kb * PLANES, k0 = (t.first + kb) * kDepth;
                     const uint32_t bar = in_first_cta(smem_addr(&control.full[stage]));
                     if (rank == 0) mbar_arrive_expect_tx(smem_addr(&control.full[stage]), 2 * kStageBytes);
                     const uint32_t a = base + stage * kStageBytes, b = a + kOperandBytes;
                     if (kAOther) {
-                        load_box(a, &maps.a, m0, k0, pa, wa, bar);
-                        load_box(a + kOperandBytes / 2, &maps.a, m0 + 64, k0, pa, wa, bar);
+                        load_box(a, &maps.a, m0, k0, plane, wa, bar);
+                        load_box(a + kOperandBytes / 2, &maps.a, m0 + 64, k0, plane, wa, bar);
                     } else {
-                        load_box(a, &maps.a, k0, m0, pa, wa, bar);
+                        load_box(a, &maps.a, k0, m0, plane, wa, bar);
                     }
                     if (kBOther) {
-                        load_box(b, &maps.b, n0, k0, pb, wb, bar);
-                        load_box(b + kOperandBytes / 2, &maps.b, n0 + 64, k0, pb, wb, bar);
+                        load_box(b, &maps.b, n0, k0, plane, wb, bar);
+                        load_box(b + kOperandBytes / 2, &maps.b, n0 + 64, k0, plane, wb, bar);
                     } else {
-                        load_box(b, &maps.b, k0, n0, pb, wb, bar);
+                        load_box(b, &maps.b, k0, n0, plane, wb, bar);
                     }
                     ++issued;
                     if (++stage == kStages) stage = 0, phase ^= 1;
@@ -482,23 +517,43 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             uint32_t phase = 0;
             for (int tile = blockIdx.x / 2; tile < total && fine; tile += pairs) {
                 const Tile t = tile_at(tile);
-                int end = t.first_segment;
-                for (int kb = 0; kb < t.blocks && fine; end = min(end + segment, t.blocks)) {
-                    const int buffer = made & 1, begin = kb;
+                for (int kb = 0; kb < t.blocks && fine;) {
+                    const int buffer = made & 1, begin = kb, end = min(kb + segment, t.blocks);
                     fine = wait(smem_addr(&control.sum_empty[buffer]), (made >> 1 & 1) ^ 1);
                     if (!fine) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    for (; kb < end; ++kb) {
-                        fine = wait(smem_addr(&control.full[stage]), phase);
-                        if (!fine) break;
-                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                        const uint32_t a = base + stage * kStageBytes, b = a + kOperandBytes;
+                    const uint32_t sum = tensor_memory + buffer * kTileN;
+                    const auto block = [&](uint32_t a, uint32_t b, bool add) {
 #pragma unroll
                         for (int k = 0; k < kDepth / 16; ++k)
-                            multiply(tensor_memory + buffer * kTileN, tile_descriptor(a + k * a_step, kAOther ? kOperandBytes / 2 : 16, 1024),
-                                     tile_descriptor(b + k * b_step, kBOther ? kOperandBytes / 2 : 16, 1024), descriptor, kb > begin || k > 0);
-                        commit_to_pair(smem_addr(&control.empty[stage]));
-                        if (++stage == kStages) stage = 0, phase ^= 1;
+                            multiply(sum, tile_descriptor(a + k * a_step, kAOther ? kOperandBytes / 2 : 16, 1024),
+                                     tile_descriptor(b + k * b_step, kBOther ? kOperandBytes / 2 : 16, 1024), descriptor, add || k > 0);
+                    };
+                    for (; kb < end; ++kb) {
+                        uint32_t at[PLANES];
+                        int s = stage;
+                        uint32_t ph = phase;
+#pragma unroll
+                        for (int q = 0; q < PLANES; ++q) {
+                            fine = fine && wait(smem_addr(&control.full[s]), ph);
+                            at[q] = base + s * kStageBytes;
+                            if (++s == kStages) s = 0, ph ^= 1;
+                        }
+                        if (!fine) break;
+                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                        if constexpr (PLANES == 1) {
+                            block(at[0], at[0] + kOperandBytes, kb > begin);
+                        } else {  // parts of A and B, the smallest products first
+                            block(at[2], at[0] + kOperandBytes, kb > begin);
+                            block(at[0], at[2] + kOperandBytes, true);
+                            block(at[1], at[1] + kOperandBytes, true);
+                            block(at[1], at[0] + kOperandBytes, true);
+                            block(at[0], at[1] + kOperandBytes, true);
+                            block(at[0], at[0] + kOperandBytes, true);
+                        }
+#pragma unroll
+                        for (int q = 0; q < PLANES; ++q) commit_to_pair(smem_addr(&control.empty[(at[q] - base) / kStageBytes]));
+                        stage = s, phase = ph;
                     }
                     if (!fine) break;
                     commit_to_pair(smem_addr(&control.sum_full[buffer]));
@@ -508,7 +563,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         }
     } else {
         const int quarter = warp % 4, half = (warp - 2) / 4;
-        const bool wide = (reinterpret_cast<uintptr_t>(prm.out) | (prm.out_row | prm.out_worker) * (prm.out_f32 ? 4 : 2)) % 16 == 0;
+        const bool wide = (reinterpret_cast<uintptr_t>(prm.out) | (prm.out_row | prm.out_worker) * (PLANES == 3 ? 4 : 2)) % 16 == 0;
         int made = 0;
         for (int tile = blockIdx.x / 2; tile < total && fine; tile += pairs) {
             const Tile t = tile_at(tile);
@@ -517,8 +572,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 #pragma unroll
                 for (int j = 0; j < kHalf; ++j) v[j] = 0.0f;
             }
-            int end = t.first_segment;
-            for (int kb = 0; kb < t.blocks; kb = end, end = min(end + segment, t.blocks)) {
+            for (int kb = 0; kb < t.blocks; kb = min(kb + segment, t.blocks)) {
                 const int buffer = made & 1;
                 fine = __all_sync(0xFFFFFFFFu, wait(smem_addr(&control.sum_full[buffer]), made >> 1 & 1));
                 if (!fine) break;
@@ -530,7 +584,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                 ++made;
             }
             if (!fine) break;
-            epilogue<WHICH>(prm, t.w, t.m0 + (int)rank * 128 + quarter * 32 + lane, t.n0 + half * kHalf, t.count, v, wide, control.staging[warp - 2]);
+            epilogue<WHICH, PLANES>(prm, t.w, t.split, t.m0 + (int)rank * 128 + quarter * 32 + lane, t.n0 + half * kHalf, t.count, v, wide, control.staging[warp - 2]);
         }
     }
     if (!fine && lane == 0) atomicExch(&g_gave_up, 1);
@@ -558,11 +612,11 @@ bool encode_operand(CUtensorMap* map, const Operand& o, int planes, int workers,
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <Product WHICH>
+template <Product WHICH, int PLANES>
 cudaError_t launch(const ProductParams& prm, cudaStream_t stream)
 {
     static rps::LaunchState state;
-    cudaError_t err = rps::grant_smem(state, rps_product_kernel<WHICH>, kSharedBytes);
+    cudaError_t err = rps::grant_smem(state, rps_product_kernel<WHICH, PLANES>, kSharedBytes);
     if (err != cudaSuccess) return err;
     int sms = 0;
     if ((err = sm_count(&sms)) != cudaSuccess) return err;
@@ -574,21 +628,97 @@ cudaError_t launch(const ProductParams& prm, cudaStream_t stream)
     } else if (!encode_operand(&maps.a, p.a, p.planes, p.workers, a_other ? 64 : 128) || !encode_operand(&maps.b, p.b, p.planes, p.workers, b_other ? 64 : 128)) {
         return cudaErrorInvalidValue;
     }
-    const int64_t tiles = ceil_div(p.m, kTileM) * ceil_div(p.n, kTileN) * p.workers;
+    if (p.splits < 1) p.splits = 1;
+    const int64_t tiles = product_tiles(p.m, p.n, p.workers) * p.splits;
     const int pairs = (int)(tiles < sms / 2 ? tiles : sms / 2);
-    rps_product_kernel<WHICH><<<2 * pairs, kThreads, kSharedBytes, stream>>>(p, maps);
+    rps_product_kernel<WHICH, PLANES><<<2 * pairs, kThreads, kSharedBytes, stream>>>(p, maps);
     return cudaGetLastError();
 }
 
 }  // namespace
 
+int64_t product_tiles(int64_t m, int64_t n, int workers) { return ceil_div(m, kTileM) * ceil_div(n, kTileN) * workers; }
+
+int64_t product_blocks(int64_t k) { return ceil_div(k, kDepth); }
+
+// A product with fewer tiles than the 74 pairs and a long summed axis is cut, so that all pairs work.  In microseconds: a block takes a
+// pair 0.27 (the six products of parts of fp32: 1.6) and a tile's end 1; a part's 256 KB written and read 0.1, the launch that joins
+// them 5.  (48 tiles of 157 fp32 blocks: 312 us whole, 222 + 10 in three runs.  From 74 tiles on cutting only evens the last
+// round out, and the board's power, not the idle pairs, bounds it: 120 tiles of 1024 bf16 blocks took 745 us whole, 740 + 15 in three.)
+int product_splits(int64_t tiles, int64_t blocks, int planes)
+{
+    constexpr int64_t kPairs = 148 / 2;
+    const double block = planes == 1 ? 0.27 : 1.6;
+    int best = 1;
+    double least = 0.0;
+    for (int s = 1; s <= 32 && (s == 1 || (tiles < kPairs && s * 4 <= blocks)); ++s) {
+        const double rounds = (double)ceil_div(tiles * s, kPairs);
+        const double cost = rounds * ((double)ceil_div(blocks, s) * block + 1.0) + (s > 1 ? 5.0 + 0.1 * (double)(tiles * s) : 0.0);
+        if (s == 1 || cost < least) best = s, least = cost;
+    }
+    return best;
+}
+
+namespace {
+
+// Parts of a product added up in their order, scaled and rounded into the result: a warp to a row, four columns to a lane.
+template <typename T, bool HIDDEN>
+__global__ void __launch_bounds__(256) rps_join_kernel(const ProductParams prm)
+{
+    const int w = blockIdx.y, lane = threadIdx.x % 32;
+    const int64_t row = (int64_t)blockIdx.x * 8 + threadIdx.x / 32;
+    if (row >= (HIDDEN ? (int64_t)prm.count[w] : (int64_t)prm.m)) return;
+    const float g = prm.scale != nullptr ? prm.scale[w] : 1.0f;
+    T* out = static_cast<T*>(prm.out) + w * prm.out_worker + (HIDDEN ? (int64_t)prm.rows[w * prm.tokens + row] : row) * prm.out_row;
+    const float* part = prm.parts + (w * prm.part_rows + row) * prm.part_row;
+    const int64_t next = prm.workers * prm.part_rows * prm.part_row;
+    const bool wide = (reinterpret_cast<uintptr_t>(out) / sizeof(T)) % 4 == 0;
+    for (int c = lane * 4; c < prm.n; c += 128) {
+        float4 s = __ldcs(reinterpret_cast<const float4*>(part + c));
+        for (int k = 1; k < prm.splits; ++k) {
+            const float4 p = __ldcs(reinterpret_cast<const float4*>(part + k * next + c));
+            s.x += p.x, s.y += p.y, s.z += p.z, s.w += p.w;
+        }
+        const T e[4] = {from_float<T>(s.x * g), from_float<T>(s.y * g), from_float<T>(s.z * g), from_float<T>(s.w * g)};
+        if (wide && c + 4 <= prm.n) {
+            if constexpr (sizeof(T) == 4)
+                *reinterpret_cast<float4*>(out + c) = make_float4(e[0], e[1], e[2], e[3]);
+            else
+                *reinterpret_cast<uint2*>(out + c) = make_uint2(two_bf16(s.x * g, s.y * g), two_bf16(s.z * g, s.w * g));
+        } else {
+            for (int k = 0; k < 4; ++k)
+                if (c + k < prm.n) out[c + k] = e[k];
+        }
+    }
+}
+
+}  // namespace
+
+cudaError_t launch_join(Product which, const ProductParams& prm, cudaStream_t stream)
+{
+    const dim3 grid((unsigned)ceil_div(prm.m, 8), (unsigned)prm.workers);
+    if (which == Product::kDhidden) {
+        if (prm.planes == 3)
+            rps_join_kernel<float, true><<<grid, 256, 0, stream>>>(prm);
+        else
+            rps_join_kernel<bf16, true><<<grid, 256, 0, stream>>>(prm);
+    } else {
+        if (prm.planes == 3)
+            rps_join_kernel<float, false><<<grid, 256, 0, stream>>>(prm);
+        else
+            rps_join_kernel<bf16, false><<<grid, 256, 0, stream>>>(prm);
+    }
+    return cudaGetLastError();
+}
+
 cudaError_t launch_product(Product which, const ProductParams& prm, cudaStream_t stream)
 {
+    const bool f32 = prm.planes == 3;
     switch (which) {
-        case Product::kLse: return launch<Product::kLse>(prm, stream);
-        case Product::kDlogits: return launch<Product::kDlogits>(prm, stream);
-        case Product::kDhidden: return launch<Product::kDhidden>(prm, stream);
-        default: return launch<Product::kDweight>(prm, stream);
+        case Product::kLse: return f32 ? launch<Product::kLse, 3>(prm, stream) : launch<Product::kLse, 1>(prm, stream);
+        case Product::kDlogits: return f32 ? launch<Product::kDlogits, 3>(prm, stream) : launch<Product::kDlogits, 1>(prm, stream);
+        case Product::kDhidden: return f32 ? launch<Product::kDhidden, 3>(prm, stream) : launch<Product::kDhidden, 1>(prm, stream);
+        default: return f32 ? launch<Product::kDweight, 3>(prm, stream) : launch<Product::kDweight, 1>(prm, stream);
     }
 }
 

@@ -1,6 +1,6 @@
-// Slices of rows: what a lane owns of a row is 16 bytes of values (8 bf16 or 4 fp32 consecutive columns), read and written in one piece
-// where everything is aligned and element by element otherwise.  128 columns, which share a scale in 8-bit form, are then
-// 16 or 32 neighbouring lanes.
+// Slices of rows: what a lane owns of a row is 16 bytes of values (8 bf16 or 4 fp32 consecutive columns).  128 columns, which
+// share a scale in 8-bit form, are then 16 or 32 neighbouring lanes.  ALIGN says what a slice is moved in: 16 bytes where every
+// row starts on such a boundary, else 4 (two bf16 of an even row, or one fp32), else 2.
 #pragma once
 
 #include "rps_ops_kernels.h"
@@ -29,20 +29,68 @@ __device__ __forceinline__ uint4 load_streaming(const void* p)
 }
 
 // The 16 bytes of columns c..c+width-1, zero from `cols` on.
-template <typename T, bool ALIGNED, bool STREAM>
+template <typename T, int ALIGN, bool STREAM>
 __device__ __forceinline__ uint4 load_slice(const T* row, int c, int cols)
 {
-    if constexpr (ALIGNED) {
+    if constexpr (ALIGN == 16) {
         if (c >= cols) return make_uint4(0, 0, 0, 0);
         return STREAM ? load_streaming(row + c) : *reinterpret_cast<const uint4*>(row + c);
-    } else {
-        uint4 v = make_uint4(0, 0, 0, 0);
-        T* e = reinterpret_cast<T*>(&v);
+    } else if constexpr (ALIGN == 4) {
+        constexpr int kPer = 4 / sizeof(T);
+        uint32_t r[4];
 #pragma unroll
-        for (int j = 0; j < Slice<T>::kWidth; ++j)
-            if (c + j < cols) e[j] = row[c + j];
-        return v;
+        for (int j = 0; j < 4; ++j) r[j] = c + j * kPer < cols ? __ldg(reinterpret_cast<const uint32_t*>(row + c + j * kPer)) : 0u;
+        return make_uint4(r[0], r[1], r[2], r[3]);
+    } else {
+        uint32_t r[4] = {};
+        const unsigned short* half = reinterpret_cast<const unsigned short*>(row);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (c + j < cols) r[j / 2] |= (uint32_t)__ldg(half + c + j) << (j % 2 * 16);
+        return make_uint4(r[0], r[1], r[2], r[3]);
     }
+}
+
+template <int BYTES>
+__device__ __forceinline__ void copy_async(uint32_t slot, const void* from, bool there)
+{
+    const uint32_t bytes = there ? BYTES : 0;  // what is not there becomes zero
+    if constexpr (BYTES == 16)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(slot), "l"(from), "r"(bytes) : "memory");
+    else
+        asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(slot), "l"(from), "n"(BYTES), "r"(bytes) : "memory");
+}
+
+// load_slice into this thread's slot of shared memory, without waiting for it where the alignment allows.
+template <typename T, int ALIGN>
+__device__ __forceinline__ void copy_slice(uint32_t slot, const T* row, int c, int cols)
+{
+    if constexpr (ALIGN == 16) {
+        copy_async<16>(slot, c < cols ? row + c : row, c < cols);
+    } else if constexpr (ALIGN == 4) {
+        constexpr int kPer = 4 / sizeof(T);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) copy_async<4>(slot + 4 * j, c + j * kPer < cols ? row + c + j * kPer : row, c + j * kPer < cols);
+    } else {
+        const uint4 v = load_slice<T, 2, true>(row, c, cols);
+        asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(slot), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+    }
+}
+
+__device__ __forceinline__ void copies_sent() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+
+// All but the last N groups of this thread's copies have arrived.
+template <int N>
+__device__ __forceinline__ void copies_arrived()
+{
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
+__device__ __forceinline__ uint4 read_slot(uint32_t slot)
+{
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(slot) : "memory");
+    return v;
 }
 
 __device__ __forceinline__ void widen(const uint4& s, float (&v)[4])
@@ -76,17 +124,30 @@ __device__ __forceinline__ uint4 narrow(const float (&v)[8])
     return make_uint4(r[0], r[1], r[2], r[3]);
 }
 
-template <typename T, bool ALIGNED>
+template <typename T, int ALIGN>
 __device__ __forceinline__ void store_slice(T* row, int c, int cols, const uint4& v)
 {
-    if constexpr (ALIGNED) {
+    const uint32_t r[4] = {v.x, v.y, v.z, v.w};
+    if constexpr (ALIGN == 16) {
         if (c < cols) *reinterpret_cast<uint4*>(row + c) = v;
-    } else {
-        const T* e = reinterpret_cast<const T*>(&v);
+    } else if constexpr (ALIGN == 4) {
+        constexpr int kPer = 4 / sizeof(T);
 #pragma unroll
-        for (int j = 0; j < Slice<T>::kWidth; ++j)
-            if (c + j < cols) row[c + j] = e[j];
+        for (int j = 0; j < 4; ++j)
+            if (c + j * kPer < cols) *reinterpret_cast<uint32_t*>(row + c + j * kPer) = r[j];
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (c + j < cols) reinterpret_cast<unsigned short*>(row)[c + j] = (unsigned short)(r[j / 2] >> (j % 2 * 16));
     }
+}
+
+// What rows that start at `p` and are `stride` elements apart (of `cols` elements) can be moved in.
+template <typename T>
+int alignment(const void* p, int64_t cols, int64_t stride)
+{
+    const uint64_t bits = reinterpret_cast<uintptr_t>(p) | (uint64_t)cols * sizeof(T) | (uint64_t)stride * sizeof(T);
+    return bits % 16 == 0 ? 16 : bits % 4 == 0 ? 4 : 2;
 }
 
 // Eight fp32 values as three slices of bf16 parts that add up to them.
@@ -115,28 +176,23 @@ template <int WIDTH>
 __device__ __forceinline__ void pack_slice(const float (&v)[WIDTH], int8_t* codes, float* scale)
 {
     constexpr int kLanes = RPS_PACK_GROUP / WIDTH;
-    float top = 0.0f;
-    bool finite = true;
+    // sizes compare as integers: finite < infinity < NaN
+    uint32_t top = 0;
 #pragma unroll
-    for (int j = 0; j < WIDTH; ++j) {
-        finite &= fabsf(v[j]) <= 3.402823466e38f;
-        top = fmaxf(top, fabsf(v[j]));
-    }
-    if (!finite) top = INFINITY;  // a NaN that the maximum does not see
+    for (int j = 0; j < WIDTH; ++j) top = max(top, __float_as_uint(v[j]) & 0x7FFFFFFFu);
 #pragma unroll
-    for (int s = kLanes / 2; s > 0; s /= 2) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, s));
-    finite = top <= 3.402823466e38f;
-    const bool zero = !finite || top < kSmallestPacked;
-    const float factor = zero ? 0.0f : __fdiv_rn(127.0f, top);
+    for (int s = kLanes / 2; s > 0; s /= 2) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, s));
+    const bool finite = top < 0x7F800000u, zero = !finite || __uint_as_float(top) < kSmallestPacked;
+    const float factor = zero ? 0.0f : __fdiv_rn(127.0f, __uint_as_float(top));
+    // 1.5 * 2^23 has units of one in its last place, so adding it rounds to an integer, ties to even, and leaves it in the low bits
     uint32_t word[WIDTH / 4];
 #pragma unroll
     for (int i = 0; i < WIDTH / 4; ++i) {
-        word[i] = 0;
+        uint32_t q[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int q = zero ? 0 : __float2int_rn(__fmul_rn(v[4 * i + j], factor));
-            word[i] |= (uint32_t)(q & 0xFF) << (8 * j);
-        }
+        for (int j = 0; j < 4; ++j) q[j] = __float_as_uint(__fadd_rn(__fmul_rn(v[4 * i + j], factor), 12582912.0f));
+        word[i] = __byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410);
+        if (zero) word[i] = 0;  // infinities and NaN times zero
     }
     if (codes != nullptr) {
         if constexpr (WIDTH == 8)
@@ -144,35 +200,39 @@ __device__ __forceinline__ void pack_slice(const float (&v)[WIDTH], int8_t* code
         else
             *reinterpret_cast<uint32_t*>(codes) = word[0];
     }
-    if (scale != nullptr && threadIdx.x % kLanes == 0) *scale = !finite ? __int_as_float(0x7FFFFFFF) : zero ? 0.0f : __fmul_rn(top, 1.0f / 127.0f);
+    if (scale != nullptr && threadIdx.x % kLanes == 0) *scale = !finite ? __int_as_float(0x7FFFFFFF) : zero ? 0.0f : __fmul_rn(__uint_as_float(top), 1.0f / 127.0f);
 }
 
-// Codes as they lie in memory, and their values.
-template <int WIDTH>
-struct Codes;
-template <>
-struct Codes<8> {
-    uint2 w;
-    __device__ __forceinline__ void load(const int8_t* p) { w = __ldg(reinterpret_cast<const uint2*>(p)); }
-    __device__ __forceinline__ void clear() { w = make_uint2(0, 0); }
-    __device__ __forceinline__ void values(float scale, float (&v)[8]) const
-    {
+// The values of four codes: a byte with its sign bit turned over, put under the bits of 2^23, is 2^23 + 128 + code.
+__device__ __forceinline__ void code_values(uint32_t word, float scale, float* v)
+{
+    const uint32_t w = word ^ 0x80808080u;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            v[j] = __fmul_rn((float)(int8_t)(w.x >> (8 * j)), scale);
-            v[4 + j] = __fmul_rn((float)(int8_t)(w.y >> (8 * j)), scale);
+    for (int j = 0; j < 4; ++j) v[j] = __fmul_rn(__uint_as_float(__byte_perm(w, 0x4B000000u, 0x7540u + j)) - 8388736.0f, scale);
+}
+
+// Codes of a slice as they lie in memory, and their values.
+template <int WIDTH>
+struct Codes {
+    uint32_t w[WIDTH / 4];
+    __device__ __forceinline__ void load(const int8_t* p)
+    {
+        if constexpr (WIDTH == 8) {
+            const uint2 v = __ldg(reinterpret_cast<const uint2*>(p));
+            w[0] = v.x, w[1] = v.y;
+        } else {
+            w[0] = __ldg(reinterpret_cast<const uint32_t*>(p));
         }
     }
-};
-template <>
-struct Codes<4> {
-    uint32_t w;
-    __device__ __forceinline__ void load(const int8_t* p) { w = __ldg(reinterpret_cast<const uint32_t*>(p)); }
-    __device__ __forceinline__ void clear() { w = 0; }
-    __device__ __forceinline__ void values(float scale, float (&v)[4]) const
+    __device__ __forceinline__ void clear()
     {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = __fmul_rn((float)(int8_t)(w >> (8 * j)), scale);
+        for (int i = 0; i < WIDTH / 4; ++i) w[i] = 0;
+    }
+    __device__ __forceinline__ void values(float scale, float (&v)[WIDTH]) const
+    {
+#pragma unroll
+        for (int i = 0; i < WIDTH / 4; ++i) code_values(w[i], scale, v + 4 * i);
     }
 };
 
