@@ -32,112 +32,173 @@ __device__ __forceinline__ uint32_t cluster_rank()
     return r;
 }
 
-// Sums of N values over the threads that share a row.  `slots` is double-buffered over successive calls (`turn`), so
-// that one barrier a call is enough.  Every thread gets the sums, added in the same order.
-template <int N>
-__device__ __forceinline__ void row_sums(float (&v)[N], float (*slots)[N][kMostWarps], int turn, int cluster, uint32_t rank)
+// Room for the warps' sums of up to four values, double-buffered over successive rows, so that one barrier is enough.
+struct Sums {
+    float of[2][4][kMostWarps];
+};
+
+// A warp's sum of a value to every CTA that shares the row, and the barrier.
+template <bool CLUSTER>
+__device__ __forceinline__ void exchange(float* slots, float v, bool mine, int cluster, uint32_t rank)
 {
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-#pragma unroll
-        for (int s = 16; s > 0; s /= 2) v[i] += __shfl_xor_sync(0xFFFFFFFFu, v[i], s);
-    const int warps = blockDim.x / 32, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    if (warps * cluster == 1) return;
-    if (cluster == 1) {
-        if (lane == 0) {
-#pragma unroll
-            for (int i = 0; i < N; ++i) slots[turn][i][warp] = v[i];
-        }
+    const int warps = blockDim.x / 32, warp = threadIdx.x / 32;
+    if constexpr (!CLUSTER) {
+        if (mine) slots[warp] = v;
         __syncthreads();
     } else {
-        if (lane < cluster) {
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const uint32_t own = (uint32_t)__cvta_generic_to_shared(&slots[turn][i][rank * warps + warp]);
+        if (mine) {
+            const uint32_t own = (uint32_t)__cvta_generic_to_shared(&slots[rank * warps + warp]);
+            for (int k = 0; k < cluster; ++k) {
                 uint32_t there;
-                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(own), "r"(lane));
-                asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(there), "f"(v[i]) : "memory");
+                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(own), "r"(k));
+                asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(there), "f"(v) : "memory");
             }
         }
         __syncwarp();
         asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
     }
-    const int slots_used = warps * cluster;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        float s = 0.0f;
-        for (int k = lane; k < slots_used; k += 32) s += slots[turn][i][k];
-#pragma unroll
-        for (int k = 16; k > 0; k /= 2) s += __shfl_xor_sync(0xFFFFFFFFu, s, k);
-        v[i] = s;
-    }
 }
 
-// This thread's slots: `arrays` of 16 bytes for each row of the ring.
-template <int ARRAYS>
-__device__ __forceinline__ uint32_t slot_of(uint32_t slots, int turn, int array)
+// The sum of a value over the threads that share a row; every thread gets it, added in the same order.
+template <bool CLUSTER>
+__device__ __forceinline__ float row_sum(float v, Sums& sums, int turn, int cluster, uint32_t rank)
 {
-    return slots + ((uint32_t)(turn * ARRAYS + array) * blockDim.x + threadIdx.x) * 16;
+    const int lane = threadIdx.x % 32, used = blockDim.x / 32 * cluster;
+#pragma unroll
+    for (int s = 16; s > 0; s /= 2) v += __shfl_xor_sync(0xFFFFFFFFu, v, s);
+    if (!CLUSTER && used == 1) return v;
+    exchange<CLUSTER>(sums.of[turn][0], v, lane == 0, cluster, rank);
+    if constexpr (!CLUSTER) {  // at most 16 warps
+        v = lane % 16 < used ? sums.of[turn][0][lane % 16] : 0.0f;
+    } else {
+        v = 0.0f;
+        for (int k = lane % 16; k < used; k += 16) v += sums.of[turn][0][k];
+    }
+#pragma unroll
+    for (int s = 8; s > 0; s /= 2) v += __shfl_xor_sync(0xFFFFFFFFu, v, s);
+    return v;
 }
 
-template <typename T, int ALIGN, bool PACK>
+// The same of three values at a time: the lanes share the values out while they add (8 lanes to a value), 6 exchanges between lanes
+// instead of 15.
+template <bool CLUSTER>
+__device__ __forceinline__ void row_sums(float (&v)[3], Sums& sums, int turn, int cluster, uint32_t rank)
+{
+    const int lane = threadIdx.x % 32, used = blockDim.x / 32 * cluster, value = lane / 8;
+    const bool high = lane & 16, odd = lane & 8;
+    float a = high ? v[2] : v[0], b = high ? 0.0f : v[1];  // values 0, 1 stay below, 2 (and an empty 3) above
+    a += __shfl_xor_sync(0xFFFFFFFFu, high ? v[0] : v[2], 16);
+    b += __shfl_xor_sync(0xFFFFFFFFu, high ? v[1] : 0.0f, 16);
+    float s = odd ? b : a;
+    s += __shfl_xor_sync(0xFFFFFFFFu, odd ? a : b, 8);
+#pragma unroll
+    for (int k = 4; k > 0; k /= 2) s += __shfl_xor_sync(0xFFFFFFFFu, s, k);
+    if (CLUSTER || used > 1) {
+        exchange<CLUSTER>(sums.of[turn][value], s, lane % 8 == 0, cluster, rank);
+        s = 0.0f;
+        for (int k = lane % 8; k < used; k += 8) s += sums.of[turn][value][k];
+#pragma unroll
+        for (int k = 4; k > 0; k /= 2) s += __shfl_xor_sync(0xFFFFFFFFu, s, k);
+    }
+#pragma unroll
+    for (int i = 0; i < 3; ++i) v[i] = __shfl_sync(0xFFFFFFFFu, s, 8 * i);
+}
+
+// Rows of one CTA follow one another, so that their addresses, their worker and their gate are counted up instead of divided out.
+// The arithmetic goes two columns at a time: at one column an instruction (447 of them for 8 columns of a row forward, 640 backward)
+// the kernels were bound by instruction issue, at 4.3 TB/s.
+template <typename T, int ALIGN, bool PACK, bool CLUSTER>
 __global__ void __launch_bounds__(kMostThreads, kForwardThreads / kMostThreads) rps_norm_forward_kernel(const NormParams prm)
 {
-    constexpr int W = Slice<T>::kWidth;
+    constexpr int W = Slice<T>::kWidth, P = W / 2;
     extern __shared__ uint4 ring[];
-    __shared__ float slots[2][1][kMostWarps];
+    __shared__ Sums sums;
     const uint32_t copied = (uint32_t)__cvta_generic_to_shared(ring);
-    const int cluster = prm.cluster, D = (int)prm.cols;
-    const uint32_t rank = cluster > 1 ? cluster_rank() : 0;
+    const int cluster = CLUSTER ? prm.cluster : 1, D = (int)prm.cols;
+    const uint32_t rank = CLUSTER ? cluster_rank() : 0;
     const int c = ((int)rank * blockDim.x + threadIdx.x) * W;
-    const uint32_t rows = (uint32_t)(prm.n * prm.tokens), step = gridDim.x / cluster, tokens = (uint32_t)prm.tokens;
+    const int64_t rows = prm.n * prm.tokens, first = rows * (blockIdx.x / cluster) / (gridDim.x / cluster);
+    const int count = (int)(rows * (blockIdx.x / cluster + 1) / (gridDim.x / cluster) - first);
     const float inv = 1.0f / (float)D;
-    int into = 0;
-    const auto send = [&](uint32_t r) {
-        if (r < rows) {
-            const uint32_t w = r / tokens, g = (r - w * tokens) / (uint32_t)prm.rows_per_gate;
-            copy_slice<T, ALIGN>(slot_of<3>(copied, into, 0), static_cast<const T*>(prm.x) + (int64_t)r * D, c, D);
-            copy_slice<T, ALIGN>(slot_of<3>(copied, into, 1), static_cast<const T*>(prm.f) + (int64_t)r * D, c, D);
-            copy_slice<T, ALIGN>(slot_of<3>(copied, into, 2), static_cast<const T*>(prm.gate) + w * prm.gate_worker + (int64_t)g * D, c, D);
+    const T* const x_rows = static_cast<const T*>(prm.x) + first * D;
+    const T* const f_rows = static_cast<const T*>(prm.f) + first * D;
+    T* const h_rows = static_cast<T*>(prm.h) + first * D;
+    T* const y_rows = static_cast<T*>(prm.y) + first * D;
+    const int64_t worker0 = first / prm.tokens, token0 = first - worker0 * prm.tokens;
+
+    // of the next row to be copied
+    const uint32_t array = blockDim.x * 16, slot = 3 * array, end_of_ring = copied + kSlots * slot + threadIdx.x * 16;
+    uint32_t into = copied + threadIdx.x * 16;
+    int to_send = count, rows_per_gate = (int)prm.rows_per_gate, tokens = (int)prm.tokens;
+    int left_in_gate = rows_per_gate - (int)(token0 % rows_per_gate), left_in_worker = tokens - (int)token0;
+    int64_t worker = worker0, ahead = 0;
+    const T* gate_at = static_cast<const T*>(prm.gate) + worker0 * prm.gate_worker + token0 / prm.rows_per_gate * D;
+    const auto send = [&] {
+        if (to_send > 0) {
+            --to_send;
+            copy_slice<T, ALIGN>(into, x_rows + ahead, c, D);
+            copy_slice<T, ALIGN>(into + array, f_rows + ahead, c, D);
+            copy_slice<T, ALIGN>(into + 2 * array, gate_at, c, D);
+            ahead += D;
+            if (--left_in_gate == 0) left_in_gate = rows_per_gate, gate_at += D;
+            if (--left_in_worker == 0) left_in_worker = tokens, gate_at = static_cast<const T*>(prm.gate) + ++worker * prm.gate_worker;
         }
         copies_sent();
-        into = into + 1 == kSlots ? 0 : into + 1;
+        into += slot;
+        if (into == end_of_ring) into -= kSlots * slot;
     };
-    uint32_t row = blockIdx.x / cluster;
-    for (int i = 0; i < kAhead; ++i) send(row + i * step);
-    int turn = 0, from = 0;
-    for (; row < rows; row += step) {
-        float x[W], f[W], gate[W], post[W], pre[W];
-        const uint32_t w = row / tokens;
-        const uint4 post_slice = load_slice<T, ALIGN, false>(static_cast<const T*>(prm.post) + w * prm.post_worker, c, D);
-        const uint4 pre_slice = load_slice<T, ALIGN, false>(static_cast<const T*>(prm.pre) + w * prm.pre_worker, c, D);
-        send(row + kAhead * step);
-        copies_arrived<kAhead>();
-        widen(read_slot(slot_of<3>(copied, from, 0)), x);
-        widen(read_slot(slot_of<3>(copied, from, 1)), f);
-        widen(read_slot(slot_of<3>(copied, from, 2)), gate);
-        from = from + 1 == kSlots ? 0 : from + 1;
-        widen(post_slice, post), widen(pre_slice, pre);
-        float s[1] = {0.0f};
+    for (int i = 0; i < kAhead; ++i) send();
+
+    // of the row that is worked on
+    Pair post[P], pre[P];
+    int rows_of_worker = tokens - (int)token0;
+    const T* post_at = static_cast<const T*>(prm.post) + worker0 * prm.post_worker;
+    const T* pre_at = static_cast<const T*>(prm.pre) + worker0 * prm.pre_worker;
+    const auto parameters = [&] {
+        widen(load_slice<T, ALIGN, false>(post_at, c, D), post);
+        widen(load_slice<T, ALIGN, false>(pre_at, c, D), pre);
 #pragma unroll
-        for (int j = 0; j < W; ++j) s[0] = fmaf(f[j], f[j], s[0]);
-        row_sums<1>(s, slots, turn, cluster, rank), turn ^= 1;
-        const float r_f = rsqrtf(fmaf(s[0], inv, prm.eps));
-        if constexpr (PACK) {
-            const bool in = c < prm.pitch;
-            pack_slice(f, in ? prm.f_codes + (int64_t)row * prm.pitch + c : nullptr, c < D ? prm.f_scales + (int64_t)row * prm.groups + c / RPS_PACK_GROUP : nullptr);
+        for (int j = 0; j < P; ++j) post[j] = post[j] * Pair(prm.scale);
+    };
+    parameters();
+    uint32_t from = copied + threadIdx.x * 16;
+    int64_t at = 0;
+    for (int i = 0; i < count; ++i, at += D) {
+        if (rows_of_worker-- == 0) {
+            rows_of_worker = tokens - 1;
+            post_at += prm.post_worker, pre_at += prm.pre_worker;
+            parameters();
         }
-        s[0] = 0.0f;
+        Pair x[P], f[P], gate[P];
+        send();
+        copies_arrived<kAhead>();
+        widen(read_slot(from), x);
+        widen(read_slot(from + array), f);
+        widen(read_slot(from + 2 * array), gate);
+        from += slot;
+        if (from == end_of_ring) from -= kSlots * slot;
+        Pair s(0.0f);
 #pragma unroll
-        for (int j = 0; j < W; ++j) {
-            x[j] = fmaf(prm.scale * gate[j], f[j] * r_f * post[j], x[j]);  // h
-            s[0] = fmaf(x[j], x[j], s[0]);
+        for (int j = 0; j < P; ++j) s = fma(f[j], f[j], s);
+        const float r_f = rsqrtf(fmaf(row_sum<CLUSTER>(s.sum(), sums, 0, cluster, rank), inv, prm.eps));
+        if constexpr (PACK) {
+            const int64_t row = first + i;
+            float v[W];
+#pragma unroll
+            for (int j = 0; j < P; ++j) f[j].get(v[2 * j], v[2 * j + 1]);
+            pack_slice(v, c < prm.pitch ? prm.f_codes + row * prm.pitch + c : nullptr, c < D ? prm.f_scales + row * prm.groups + c / RPS_PACK_GROUP : nullptr);
+        }
+        s = Pair(0.0f);
+#pragma unroll
+        for (int j = 0; j < P; ++j) {
+            x[j] = fma(gate[j] * post[j] * f[j], Pair(r_f), x[j]);  // h
+            s = fma(x[j], x[j], s);
         }
         const uint4 h = narrow(x);
-        store_slice<T, ALIGN>(static_cast<T*>(prm.h) + (int64_t)row * D, c, D, h);
-        row_sums<1>(s, slots, turn, cluster, rank), turn ^= 1;
-        const float r_h = rsqrtf(fmaf(s[0], inv, prm.eps));
+        store_slice<T, ALIGN>(h_rows + at, c, D, h);
+        const float r_h = rsqrtf(fmaf(row_sum<CLUSTER>(s.sum(), sums, 1, cluster, rank), inv, prm.eps));
         if constexpr (PACK) {
+            const int64_t row = first + i;
             float stored[W];  // as a reader of h sees it
             widen(h, stored);
             if constexpr (ALIGN != 16) {
@@ -145,34 +206,34 @@ __global__ void __launch_bounds__(kMostThreads, kForwardThreads / kMostThreads) 
                 for (int j = 0; j < W; ++j)
                     if (c + j >= D) stored[j] = 0.0f;
             }
-            pack_slice(stored, c < prm.pitch ? prm.h_codes + (int64_t)row * prm.pitch + c : nullptr,
-                       c < D ? prm.h_scales + (int64_t)row * prm.groups + c / RPS_PACK_GROUP : nullptr);
+            pack_slice(stored, c < prm.pitch ? prm.h_codes + row * prm.pitch + c : nullptr,
+                       c < D ? prm.h_scales + row * prm.groups + c / RPS_PACK_GROUP : nullptr);
         }
 #pragma unroll
-        for (int j = 0; j < W; ++j) x[j] = x[j] * r_h * pre[j];
-        store_slice<T, ALIGN>(static_cast<T*>(prm.y) + (int64_t)row * D, c, D, narrow(x));
+        for (int j = 0; j < P; ++j) x[j] = x[j] * (pre[j] * Pair(r_h));
+        store_slice<T, ALIGN>(y_rows + at, c, D, narrow(x));
         if (prm.r_f != nullptr && rank == 0 && threadIdx.x == 0) {
-            prm.r_f[row] = r_f;
-            prm.r_h[row] = r_h;
+            prm.r_f[first + i] = r_f;
+            prm.r_h[first + i] = r_h;
         }
     }
     // another CTA's sums may still be on their way here
-    if (cluster > 1) asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+    if (CLUSTER) asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
 }
 
-template <typename T, int ALIGN, bool PACKED>
+template <typename T, int ALIGN, bool PACKED, bool CLUSTER>
 __global__ void __launch_bounds__(kMostThreads, kBackwardThreads / kMostThreads) rps_norm_backward_kernel(const NormParams prm)
 {
-    constexpr int W = Slice<T>::kWidth;
+    constexpr int W = Slice<T>::kWidth, P = W / 2;
     extern __shared__ uint4 ring[];
-    __shared__ float slots[2][3][kMostWarps];
+    __shared__ Sums sums;
     const uint32_t copied = (uint32_t)__cvta_generic_to_shared(ring);
-    const int cluster = prm.cluster, D = (int)prm.cols;
-    const uint32_t rank = cluster > 1 ? cluster_rank() : 0;
+    const int cluster = CLUSTER ? prm.cluster : 1, D = (int)prm.cols;
+    const uint32_t rank = CLUSTER ? cluster_rank() : 0;
     const int c = ((int)rank * blockDim.x + threadIdx.x) * W;
     const float inv = 1.0f / (float)D;
     const int64_t block = blockIdx.x / cluster, w = blockIdx.y;
-    int64_t first, end;
+    int64_t first, end;  // tokens of this block
     if (prm.chunks > 0) {
         const int64_t g = block / prm.chunks;
         first = g * prm.rows_per_gate + block % prm.chunks * prm.rows_per_block;
@@ -181,113 +242,149 @@ __global__ void __launch_bounds__(kMostThreads, kBackwardThreads / kMostThreads)
         first = block * prm.rows_per_block;
         end = min(first + prm.rows_per_block, prm.tokens);
     }
-    const uint4 post_slice = load_slice<T, ALIGN, false>(static_cast<const T*>(prm.post) + w * prm.post_worker, c, D);
-    const uint4 pre_slice = load_slice<T, ALIGN, false>(static_cast<const T*>(prm.pre) + w * prm.pre_worker, c, D);
-    float dpost[W] = {}, dpre[W] = {}, dgate[W] = {};
+    const int count = (int)max((int64_t)0, end - first);
+    const int64_t row0 = w * prm.tokens + first;
+    const T* const dy_rows = static_cast<const T*>(prm.dy) + row0 * D;
+    const T* const dh_rows = prm.dh != nullptr ? static_cast<const T*>(prm.dh) + row0 * D : nullptr;
+    T* const dx_rows = static_cast<T*>(prm.dx) + row0 * D;
+    T* const df_rows = static_cast<T*>(prm.df) + row0 * D;
+    Pair post[P], pre[P], dpost[P], dpre[P], dgate[P];
+    widen(load_slice<T, ALIGN, false>(static_cast<const T*>(prm.post) + w * prm.post_worker, c, D), post);
+    widen(load_slice<T, ALIGN, false>(static_cast<const T*>(prm.pre) + w * prm.pre_worker, c, D), pre);
+#pragma unroll
+    for (int j = 0; j < P; ++j) {
+        post[j] = post[j] * Pair(prm.scale);
+        dpost[j] = dpre[j] = dgate[j] = Pair(0.0f);
+    }
 
-    float rf_next = 0.0f, rh_next = 0.0f;
-    int64_t gate_row = first / prm.rows_per_gate, in_gate = first - gate_row * prm.rows_per_gate;  // of the next row to be copied
-    int64_t left_in_gate = prm.rows_per_gate - in_gate;
-    int into = 0;
-    const auto send = [&](int64_t t) {
-        if (t < end) {
-            const int64_t r = w * prm.tokens + t;
-            copy_slice<T, ALIGN>(slot_of<5>(copied, into, 0), static_cast<const T*>(prm.dy) + r * D, c, D);
-            if (prm.dh != nullptr) copy_slice<T, ALIGN>(slot_of<5>(copied, into, 1), static_cast<const T*>(prm.dh) + r * D, c, D);
-            copy_slice<T, ALIGN>(slot_of<5>(copied, into, 2), static_cast<const T*>(prm.gate) + w * prm.gate_worker + gate_row * D, c, D);
+    // of the next row to be copied
+    const uint32_t array = blockDim.x * 16, slot = 5 * array, end_of_ring = copied + kSlots * slot + threadIdx.x * 16;
+    uint32_t into = copied + threadIdx.x * 16;
+    const int rows_per_gate = (int)prm.rows_per_gate;
+    int to_send = count, left_in_gate = rows_per_gate - (int)(first % rows_per_gate);
+    int rows_of_gate = left_in_gate;  // of the row that is worked on
+    int64_t gate_row = w * prm.gates + first / rows_per_gate, ahead = 0;
+    const T* gate_at = static_cast<const T*>(prm.gate) + w * prm.gate_worker + first / rows_per_gate * D;
+    const T* const f_rows = PACKED ? nullptr : static_cast<const T*>(prm.f) + row0 * D;
+    const T* const kept_rows = PACKED ? nullptr : static_cast<const T*>(prm.h_in) + row0 * D;
+    int64_t code_at = c < D ? row0 * prm.pitch + c : 0, scale_at = c < D ? row0 * prm.groups + c / RPS_PACK_GROUP : 0;
+    const auto send = [&] {
+        if (to_send > 0) {
+            --to_send;
+            copy_slice<T, ALIGN>(into, dy_rows + ahead, c, D);
+            if (dh_rows != nullptr) copy_slice<T, ALIGN>(into + array, dh_rows + ahead, c, D);
+            copy_slice<T, ALIGN>(into + 2 * array, gate_at, c, D);
             if constexpr (PACKED) {  // the codes, and behind them the scale
                 const bool in = c < D;
-                const int64_t at = in ? r * prm.pitch + c : 0, group = in ? r * prm.groups + c / RPS_PACK_GROUP : 0;
-                copy_async<W>(slot_of<5>(copied, into, 3), static_cast<const int8_t*>(prm.f) + at, in);
-                copy_async<4>(slot_of<5>(copied, into, 3) + 8, prm.f_scales + group, in);
-                copy_async<W>(slot_of<5>(copied, into, 4), static_cast<const int8_t*>(prm.h_in) + at, in);
-                copy_async<4>(slot_of<5>(copied, into, 4) + 8, prm.h_scales + group, in);
+                copy_async<W>(into + 3 * array, static_cast<const int8_t*>(prm.f) + code_at, in);
+                copy_async<4>(into + 3 * array + 8, prm.f_scales + scale_at, in);
+                copy_async<W>(into + 4 * array, static_cast<const int8_t*>(prm.h_in) + code_at, in);
+                copy_async<4>(into + 4 * array + 8, prm.h_scales + scale_at, in);
+                if (in) code_at += prm.pitch, scale_at += prm.groups;
             } else {
-                copy_slice<T, ALIGN>(slot_of<5>(copied, into, 3), static_cast<const T*>(prm.f) + r * D, c, D);
-                copy_slice<T, ALIGN>(slot_of<5>(copied, into, 4), static_cast<const T*>(prm.h_in) + r * D, c, D);
+                copy_slice<T, ALIGN>(into + 3 * array, f_rows + ahead, c, D);
+                copy_slice<T, ALIGN>(into + 4 * array, kept_rows + ahead, c, D);
             }
-            if (++in_gate == prm.rows_per_gate) in_gate = 0, ++gate_row;
+            ahead += D;
+            if (--left_in_gate == 0) left_in_gate = rows_per_gate, gate_at += D;
         }
         copies_sent();
-        into = into + 1 == kSlots ? 0 : into + 1;
+        into += slot;
+        if (into == end_of_ring) into -= kSlots * slot;
     };
-    const auto kept = [&](int from, int array, float (&v)[W]) {
-        const uint4 slot = read_slot(slot_of<5>(copied, from, array));
+    const auto kept = [&](const uint4& held, Pair (&v)[P]) {
         if constexpr (PACKED) {
+            float e[W];
             Codes<W> codes;
-            codes.w[0] = slot.x;
-            if constexpr (W == 8) codes.w[1] = slot.y;
-            codes.values(__uint_as_float(slot.z), v);
+            codes.w[0] = held.x;
+            if constexpr (W == 8) codes.w[1] = held.y;
+            codes.values(__uint_as_float(held.z), e);
+#pragma unroll
+            for (int j = 0; j < P; ++j) v[j] = Pair(e[2 * j], e[2 * j + 1]);
         } else {
-            widen(slot, v);
+            widen(held, v);
         }
     };
-    const auto statistics = [&](int64_t t) {
-        if (t < end) rf_next = __ldg(prm.r_f + w * prm.tokens + t), rh_next = __ldg(prm.r_h + w * prm.tokens + t);
+    float rf_next = 0.0f, rh_next = 0.0f;
+    const auto statistics = [&](int i) {
+        if (i < count) rf_next = __ldg(prm.r_f + row0 + i), rh_next = __ldg(prm.r_h + row0 + i);
     };
-    for (int i = 0; i < kAhead; ++i) send(first + i);
-    statistics(first);
-    int turn = 0, from = 0;
-    for (int64_t t = first; t < end; ++t) {
-        const int64_t row = w * prm.tokens + t;
-        float f[W], h[W], dy[W], dx[W] = {}, gate[W], post[W];
-        send(t + kAhead);
+    for (int i = 0; i < kAhead; ++i) send();
+    statistics(0);
+    uint32_t from = copied + threadIdx.x * 16;
+    int64_t at = 0;
+    for (int i = 0; i < count; ++i, at += D) {
+        Pair f[P], h[P], dx[P], sgp[P], gate[P];  // sgp: scale * gate * post
+        float s[3];
+        send();
         copies_arrived<kAhead>();
-        widen(read_slot(slot_of<5>(copied, from, 0)), dy);
-        if (prm.dh != nullptr) widen(read_slot(slot_of<5>(copied, from, 1)), dx);
-        widen(read_slot(slot_of<5>(copied, from, 2)), gate);
-        kept(from, 3, f), kept(from, 4, h);
-        from = from + 1 == kSlots ? 0 : from + 1;
-        widen(post_slice, post);
         const float r_f = rf_next, r_h = rh_next;
-        statistics(t + 1);
-        float s[3] = {};
+        statistics(i + 1);
+        kept(read_slot(from + 3 * array), f), kept(read_slot(from + 4 * array), h);
         {
-            float pre[W];
-            widen(pre_slice, pre);
+            Pair dy[P], s0(0.0f), s1(0.0f), s2(0.0f);
+            widen(read_slot(from), dy);
+            if (dh_rows != nullptr) {
+                widen(read_slot(from + array), dx);
+            } else {
 #pragma unroll
-            for (int j = 0; j < W; ++j) {
-                dpre[j] = fmaf(dy[j], h[j] * r_h, dpre[j]);
-                const float a = dy[j] * pre[j], q = prm.scale * gate[j] * post[j] * f[j];
-                dx[j] = fmaf(r_h, a, dx[j]);  // dh + r_h a
-                s[0] = fmaf(a, h[j], s[0]);
-                s[1] = fmaf(q, dx[j], s[1]);
-                s[2] = fmaf(q, h[j], s[2]);
+                for (int j = 0; j < P; ++j) dx[j] = Pair(0.0f);
             }
+            widen(read_slot(from + 2 * array), gate);
+#pragma unroll
+            for (int j = 0; j < P; ++j) {
+                dpre[j] = fma(dy[j], h[j] * Pair(r_h), dpre[j]);
+                const Pair a = dy[j] * pre[j];
+                sgp[j] = gate[j] * post[j];
+                const Pair q = sgp[j] * f[j];
+                dx[j] = fma(a, Pair(r_h), dx[j]);  // dh + r_h a
+                s0 = fma(a, h[j], s0);
+                s1 = fma(q, dx[j], s1);
+                s2 = fma(q, h[j], s2);
+            }
+            s[0] = s0.sum(), s[1] = s1.sum(), s[2] = s2.sum();
         }
-        row_sums<3>(s, slots, turn, cluster, rank), turn ^= 1;
+        from += slot;
+        if (from == end_of_ring) from -= kSlots * slot;
+        row_sums<CLUSTER>(s, sums, i & 1, cluster, rank);
         const float mean_h = s[0] * inv * r_h * r_h * r_h;
-        const float mean_f = (s[1] - mean_h * s[2]) * inv * r_f * r_f;
-        float df[W];
+        const float mean_f = (s[1] - mean_h * s[2]) * inv * r_f * r_f * r_f;
+        Pair df[P];
 #pragma unroll
-        for (int j = 0; j < W; ++j) {
-            dx[j] = fmaf(-h[j], mean_h, dx[j]);
-            const float g = prm.scale * dx[j], n = f[j] * r_f;
-            dgate[j] = fmaf(g, n * post[j], dgate[j]);
-            dpost[j] = fmaf(g * gate[j], n, dpost[j]);
-            df[j] = r_f * (g * gate[j] * post[j] - f[j] * mean_f);
+        for (int j = 0; j < P; ++j) {
+            dx[j] = fma(h[j], Pair(-mean_h), dx[j]);
+            const Pair e = dx[j] * f[j] * Pair(r_f);
+            dgate[j] = fma(e, post[j], dgate[j]);
+            dpost[j] = fma(e, gate[j], dpost[j]);
+            df[j] = fma(dx[j] * sgp[j], Pair(r_f), f[j] * Pair(-mean_f));
         }
-        store_slice<T, ALIGN>(static_cast<T*>(prm.dx) + row * D, c, D, narrow(dx));
-        store_slice<T, ALIGN>(static_cast<T*>(prm.df) + row * D, c, D, narrow(df));
-        if (--left_in_gate == 0) {
-            left_in_gate = prm.rows_per_gate;
+        store_slice<T, ALIGN>(dx_rows + at, c, D, narrow(dx));
+        store_slice<T, ALIGN>(df_rows + at, c, D, narrow(df));
+        if (--rows_of_gate == 0) {
+            rows_of_gate = rows_per_gate;
             if (prm.chunks == 0) {  // the block held the whole gate group
-                store_slice<T, ALIGN>(static_cast<T*>(prm.dgate) + (w * prm.gates + t / prm.rows_per_gate) * D, c, D, narrow(dgate));
+                store_slice<T, ALIGN>(static_cast<T*>(prm.dgate) + gate_row * D, c, D, narrow(dgate));
+                ++gate_row;
 #pragma unroll
-                for (int j = 0; j < W; ++j) dgate[j] = 0.0f;
+                for (int j = 0; j < P; ++j) dgate[j] = Pair(0.0f);
             }
         }
     }
     float* partial = prm.partial + (w * prm.blocks + block) * 3 * D;
 #pragma unroll
-    for (int j = 0; j < W; ++j) {
-        if (c + j < D) {
-            partial[c + j] = dpost[j];
-            partial[D + c + j] = dpre[j];
-            if (prm.chunks > 0) partial[2 * D + c + j] = dgate[j];
+    for (int j = 0; j < P; ++j) {
+        float v[3][2];
+        (dpost[j] * Pair(prm.scale)).get(v[0][0], v[0][1]), dpre[j].get(v[1][0], v[1][1]), dgate[j].get(v[2][0], v[2][1]);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            if (c + 2 * j + k < D) {
+                partial[c + 2 * j + k] = v[0][k];
+                partial[D + c + 2 * j + k] = v[1][k];
+                if (prm.chunks > 0) partial[2 * D + c + 2 * j + k] = v[2][k];
+            }
         }
     }
-    if (cluster > 1) asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+    if (CLUSTER) asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
 }
 
 // Sums of the blocks' sums: 32 columns to a CTA, the blocks dealt to its 16 warps, whose sums are added in their order.
@@ -344,15 +441,17 @@ cudaError_t launch_rows(rps::LaunchState& state, Kernel kernel, const NormParams
 template <typename T, int ALIGN, bool PACK>
 cudaError_t run_forward(const NormParams& prm, dim3 grid, int threads, cudaStream_t stream)
 {
-    static rps::LaunchState state;
-    return launch_rows(state, rps_norm_forward_kernel<T, ALIGN, PACK>, prm, grid, threads, 3, stream);
+    static rps::LaunchState state, shared_rows;
+    return prm.cluster > 1 ? launch_rows(shared_rows, rps_norm_forward_kernel<T, ALIGN, PACK, true>, prm, grid, threads, 3, stream)
+                           : launch_rows(state, rps_norm_forward_kernel<T, ALIGN, PACK, false>, prm, grid, threads, 3, stream);
 }
 
 template <typename T, int ALIGN, bool PACKED>
 cudaError_t run_backward(const NormParams& prm, dim3 grid, int threads, cudaStream_t stream)
 {
-    static rps::LaunchState state;
-    return launch_rows(state, rps_norm_backward_kernel<T, ALIGN, PACKED>, prm, grid, threads, 5, stream);
+    static rps::LaunchState state, shared_rows;
+    return prm.cluster > 1 ? launch_rows(shared_rows, rps_norm_backward_kernel<T, ALIGN, PACKED, true>, prm, grid, threads, 5, stream)
+                           : launch_rows(state, rps_norm_backward_kernel<T, ALIGN, PACKED, false>, prm, grid, threads, 5, stream);
 }
 
 // What all arrays of a call can be moved in.

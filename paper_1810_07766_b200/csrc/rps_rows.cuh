@@ -108,6 +108,67 @@ __device__ __forceinline__ void widen(const uint4& s, float (&v)[8])
     }
 }
 
+// Two fp32 values that one instruction works on (fma.rn.f32x2 and its like round each as the single instructions do).
+struct Pair {
+    uint64_t bits;
+    __device__ __forceinline__ Pair() {}
+    __device__ __forceinline__ Pair(float a, float b) { asm("mov.b64 %0, {%1, %2};" : "=l"(bits) : "f"(a), "f"(b)); }
+    __device__ __forceinline__ explicit Pair(float a) : Pair(a, a) {}
+    __device__ __forceinline__ void get(float& a, float& b) const { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(bits)); }
+    __device__ __forceinline__ float sum() const
+    {
+        float a, b;
+        get(a, b);
+        return a + b;
+    }
+};
+
+__device__ __forceinline__ Pair operator*(const Pair& a, const Pair& b)
+{
+    Pair r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.bits) : "l"(a.bits), "l"(b.bits));
+    return r;
+}
+
+__device__ __forceinline__ Pair fma(const Pair& a, const Pair& b, const Pair& c)
+{
+    Pair r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.bits) : "l"(a.bits), "l"(b.bits), "l"(c.bits));
+    return r;
+}
+
+__device__ __forceinline__ void widen(const uint4& s, Pair (&v)[2])
+{
+    v[0] = Pair(__uint_as_float(s.x), __uint_as_float(s.y)), v[1] = Pair(__uint_as_float(s.z), __uint_as_float(s.w));
+}
+
+__device__ __forceinline__ void widen(const uint4& s, Pair (&v)[4])
+{
+    const uint32_t r[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = Pair(__uint_as_float(r[i] << 16), __uint_as_float(r[i] & 0xFFFF0000u));
+}
+
+__device__ __forceinline__ uint4 narrow(const Pair (&v)[2])
+{
+    float a, b, c, d;
+    v[0].get(a, b), v[1].get(c, d);
+    return make_uint4(__float_as_uint(a), __float_as_uint(b), __float_as_uint(c), __float_as_uint(d));
+}
+
+__device__ __forceinline__ uint4 narrow(const Pair (&v)[4])
+{
+    uint32_t r[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float a, b;
+        v[i].get(a, b);
+        const __nv_bfloat162 p = __floats2bfloat162_rn(a, b);
+        r[i] = *reinterpret_cast<const uint32_t*>(&p);
+    }
+    return make_uint4(r[0], r[1], r[2], r[3]);
+}
+
 __device__ __forceinline__ uint4 narrow(const float (&v)[4])
 {
     return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
