@@ -15,6 +15,7 @@ constexpr int kRowThreads = 256;
 // the ignored ones; a ballot and a scan over the warps' counts give each token its place.
 __global__ void __launch_bounds__(kSelectThreads) rps_lce_select_kernel(const LceParams prm)
 {
+    after_the_kernel_before();
     __shared__ int warp_count[kSelectThreads / 32];
     const int w = blockIdx.x, lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     const int64_t* targets = prm.targets + w * prm.tokens;
@@ -104,6 +105,7 @@ __device__ __forceinline__ void store_parts(bf16* dst, int64_t plane, const floa
 template <typename T, int ALIGN>
 __global__ void __launch_bounds__(kRowThreads) rps_lce_gather_kernel(const LceParams prm)
 {
+    after_the_kernel_before();
     const int w = blockIdx.y, lane = threadIdx.x % 32;
     const int64_t i = (int64_t)blockIdx.x * (kRowThreads / 32) + threadIdx.x / 32;
     const int count = prm.count[w], D = (int)prm.cols;
@@ -129,6 +131,7 @@ __global__ void __launch_bounds__(kRowThreads) rps_lce_gather_kernel(const LcePa
 template <typename T, int ALIGN>
 __global__ void __launch_bounds__(kRowThreads) rps_planes_kernel(const PlanesParams prm)
 {
+    after_the_kernel_before();
     const int w = blockIdx.y, per_row = (int)(prm.dst_row / 8);
     const uint32_t total = (uint32_t)(prm.rows * per_row);  // below 2^32: the matrix has 16 bytes for each
     const uint32_t step = gridDim.x * kRowThreads;
@@ -160,6 +163,7 @@ __global__ void __launch_bounds__(kRowThreads) rps_planes_kernel(const PlanesPar
 // rows is made of the CTAs' sums by the one that finishes last, always in the same order.
 __global__ void __launch_bounds__(kMergeThreads) rps_lce_merge_kernel(const LceParams prm)
 {
+    after_the_kernel_before();
     constexpr int kWarps = kMergeThreads / 32;
     __shared__ float2 parts[kWarps][32];
     const int w = blockIdx.y, count = prm.count[w], lane = threadIdx.x % 32, warp = threadIdx.x / 32;
@@ -226,8 +230,7 @@ cudaError_t gather(const LceParams& prm, cudaStream_t stream)
     const dim3 grid((unsigned)ceil_div(prm.tokens_padded, kRowThreads / 32), (unsigned)prm.n);
     const int align = aligned_source<T>(prm.hidden, prm.cols, prm.hidden_row, prm.hidden_worker);
     const auto kernel = align == 16 ? rps_lce_gather_kernel<T, 16> : align == 4 ? rps_lce_gather_kernel<T, 4> : rps_lce_gather_kernel<T, sizeof(T)>;
-    kernel<<<grid, kRowThreads, 0, stream>>>(prm);
-    return cudaGetLastError();
+    return launch_after(kernel, grid, kRowThreads, 0, stream, 1, prm);
 }
 
 template <typename T>
@@ -240,16 +243,14 @@ cudaError_t planes(const PlanesParams& prm, cudaStream_t stream)
     const dim3 grid((unsigned)(blocks < resident ? blocks : resident), (unsigned)prm.n);
     const int align = aligned_source<T>(prm.src, prm.cols, prm.src_row, prm.src_worker);
     const auto kernel = align == 16 ? rps_planes_kernel<T, 16> : align == 4 ? rps_planes_kernel<T, 4> : rps_planes_kernel<T, sizeof(T)>;
-    kernel<<<grid, kRowThreads, 0, stream>>>(prm);
-    return cudaGetLastError();
+    return launch_after(kernel, grid, kRowThreads, 0, stream, 1, prm);
 }
 
 }  // namespace
 
 cudaError_t launch_lce_select(const LceParams& prm, cudaStream_t stream)
 {
-    rps_lce_select_kernel<<<prm.n, kSelectThreads, 0, stream>>>(prm);
-    return cudaGetLastError();
+    return launch_after(rps_lce_select_kernel, dim3((unsigned)prm.n), kSelectThreads, 0, stream, 1, prm);
 }
 
 cudaError_t launch_lce_gather(const LceParams& prm, cudaStream_t stream)
@@ -262,8 +263,7 @@ int64_t lce_merge_blocks(int64_t tokens) { return ceil_div(tokens, kMergeRows); 
 cudaError_t launch_lce_merge(const LceParams& prm, cudaStream_t stream)
 {
     const dim3 grid((unsigned)lce_merge_blocks(prm.tokens), (unsigned)prm.n);
-    rps_lce_merge_kernel<<<grid, kMergeThreads, 0, stream>>>(prm);
-    return cudaGetLastError();
+    return launch_after(rps_lce_merge_kernel, grid, kMergeThreads, 0, stream, 1, prm);
 }
 
 cudaError_t launch_planes(const PlanesParams& prm, cudaStream_t stream)

@@ -110,6 +110,7 @@ __device__ __forceinline__ void row_sums(float (&v)[3], Sums& sums, int turn, in
 template <typename T, int ALIGN, bool PACK, bool CLUSTER>
 __global__ void __launch_bounds__(kMostThreads, kForwardThreads / kMostThreads) rps_norm_forward_kernel(const NormParams prm)
 {
+    after_the_kernel_before();
     constexpr int W = Slice<T>::kWidth, P = W / 2;
     extern __shared__ uint4 ring[];
     __shared__ Sums sums;
@@ -224,6 +225,7 @@ __global__ void __launch_bounds__(kMostThreads, kForwardThreads / kMostThreads) 
 template <typename T, int ALIGN, bool PACKED, bool CLUSTER>
 __global__ void __launch_bounds__(kMostThreads, kBackwardThreads / kMostThreads) rps_norm_backward_kernel(const NormParams prm)
 {
+    after_the_kernel_before();
     constexpr int W = Slice<T>::kWidth, P = W / 2;
     extern __shared__ uint4 ring[];
     __shared__ Sums sums;
@@ -391,6 +393,7 @@ __global__ void __launch_bounds__(kMostThreads, kBackwardThreads / kMostThreads)
 template <typename T>
 __global__ void __launch_bounds__(512) rps_norm_reduce_kernel(const NormParams prm)
 {
+    after_the_kernel_before();
     __shared__ float slots[16][33];
     const int64_t c = (int64_t)blockIdx.x * 32 + threadIdx.x % 32, w = blockIdx.z, D = prm.cols;
     const int warp = threadIdx.x / 32;
@@ -429,13 +432,7 @@ cudaError_t launch_rows(rps::LaunchState& state, Kernel kernel, const NormParams
     const uint32_t bytes = (uint32_t)(threads * 16 * arrays * kSlots);
     cudaError_t err = rps::grant_smem(state, kernel, bytes);
     if (err != cudaSuccess) return err;
-    cudaLaunchConfig_t config{};
-    config.gridDim = grid, config.blockDim = dim3((unsigned)threads), config.dynamicSmemBytes = bytes, config.stream = stream;
-    cudaLaunchAttribute attribute{};
-    attribute.id = cudaLaunchAttributeClusterDimension;
-    attribute.val.clusterDim.x = (unsigned)prm.cluster, attribute.val.clusterDim.y = attribute.val.clusterDim.z = 1;
-    config.attrs = &attribute, config.numAttrs = prm.cluster > 1 ? 1 : 0;
-    return cudaLaunchKernelEx(&config, kernel, prm);
+    return launch_after(kernel, grid, threads, bytes, stream, prm.cluster, prm);
 }
 
 template <typename T, int ALIGN, bool PACK>
@@ -500,8 +497,8 @@ cudaError_t backward(NormParams prm, cudaStream_t stream)
         err = prm.packed ? run_backward<T, kLeast, true>(prm, grid, threads, stream) : run_backward<T, kLeast, false>(prm, grid, threads, stream);
     if (err != cudaSuccess) return err;
     const int64_t jobs = 2 + (prm.chunks > 0 ? prm.gates : 0);
-    rps_norm_reduce_kernel<T><<<dim3((unsigned)ceil_div(prm.cols, 32), (unsigned)(jobs < 4096 ? jobs : 4096), (unsigned)prm.n), 512, 0, stream>>>(prm);
-    return cudaGetLastError();
+    return launch_after(rps_norm_reduce_kernel<T>, dim3((unsigned)ceil_div(prm.cols, 32), (unsigned)(jobs < 4096 ? jobs : 4096), (unsigned)prm.n), 512,
+                        0, stream, 1, prm);
 }
 
 }  // namespace

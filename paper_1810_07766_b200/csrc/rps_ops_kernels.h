@@ -14,6 +14,23 @@ using bf16 = __nv_bfloat16;
 inline int64_t round_up(int64_t a, int64_t b) { return (a + b - 1) / b * b; }
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+// Launches a kernel so that its CTAs may be placed while the kernel before it in the stream drains (programmatic stream
+// serialization).  Each of these kernels begins with after_the_kernel_before(): nothing is read or written in global memory ahead of
+// it, and every CTA passes it, so that a kernel's end implies the end of all before it.
+template <typename Kernel, typename... Args>
+cudaError_t launch_after(Kernel kernel, dim3 grid, int threads, size_t shared, cudaStream_t stream, int cluster, const Args&... args)
+{
+    cudaLaunchConfig_t config{};
+    config.gridDim = grid, config.blockDim = dim3((unsigned)threads), config.dynamicSmemBytes = shared, config.stream = stream;
+    cudaLaunchAttribute attributes[2] = {};
+    attributes[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attributes[0].val.programmaticStreamSerializationAllowed = 1;
+    attributes[1].id = cudaLaunchAttributeClusterDimension;
+    attributes[1].val.clusterDim.x = (unsigned)cluster, attributes[1].val.clusterDim.y = attributes[1].val.clusterDim.z = 1;
+    config.attrs = attributes, config.numAttrs = cluster > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&config, kernel, args...);
+}
+
 // ---------------------------------------------------------------------------------------------------- products
 // Token rows are padded to whole tiles, and the vocabulary goes through the loss in whole tiles; softmax statistics are kept for
 // each half of a tile's columns.
@@ -154,6 +171,11 @@ cudaError_t launch_norm_backward(const NormParams& prm, cudaStream_t stream);
 
 // ---------------------------------------------------------------------------------------------------- device helpers
 #ifdef __CUDACC__
+__device__ __forceinline__ void after_the_kernel_before()
+{
+    asm volatile("griddepcontrol.launch_dependents;\n\tgriddepcontrol.wait;" ::: "memory");
+}
+
 template <typename T>
 __device__ __forceinline__ float to_float(T v);
 template <>

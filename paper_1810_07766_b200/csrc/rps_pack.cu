@@ -25,6 +25,7 @@ __device__ __forceinline__ Place place(uint32_t u, uint32_t units_per_row)
 template <typename T, int ALIGN>
 __global__ void __launch_bounds__(kThreads) rps_pack_kernel(const PackParams prm, uint32_t units, uint32_t units_per_row)
 {
+    after_the_kernel_before();
     constexpr int W = Slice<T>::kWidth;
     const int D = (int)prm.cols;
     const uint32_t warp = blockIdx.x * (kThreads / 32) + threadIdx.x / 32, step = gridDim.x * (kThreads / 32);
@@ -63,6 +64,7 @@ __device__ __forceinline__ void load_codes(const PackParams& prm, const Place& a
 template <typename T, int ALIGN>
 __global__ void __launch_bounds__(kThreads) rps_unpack_kernel(const PackParams prm, uint32_t units, uint32_t units_per_row)
 {
+    after_the_kernel_before();
     constexpr int W = Slice<T>::kWidth;
     const uint32_t warp = blockIdx.x * (kThreads / 32) + threadIdx.x / 32, step = gridDim.x * (kThreads / 32);
     for (uint64_t u0 = warp; u0 < units; u0 += (uint64_t)step * kUnits) {
@@ -90,6 +92,7 @@ __global__ void __launch_bounds__(kThreads) rps_unpack_kernel(const PackParams p
 template <typename T>
 __global__ void __launch_bounds__(kThreads) rps_unpack_planes_kernel(const PackParams prm, uint32_t units, uint32_t units_per_row)
 {
+    after_the_kernel_before();
     constexpr int W = 8;
     const uint32_t warp = blockIdx.x * (kThreads / 32) + threadIdx.x / 32, step = gridDim.x * (kThreads / 32);
     for (uint64_t u0 = warp; u0 < units; u0 += (uint64_t)step * kUnits) {
@@ -132,8 +135,8 @@ cudaError_t launch_units(Kernel kernel, const PackParams& prm, int64_t row_cols,
     const int64_t units_per_row = ceil_div(row_cols, 32 * width), units = prm.rows * units_per_row;
     if (units >= 1ll << 32) return cudaErrorInvalidValue;  // 2 TB of activations
     const int64_t blocks = ceil_div(units, kThreads / 32), resident = (int64_t)sms * 8;
-    kernel<<<(unsigned)(blocks < resident ? blocks : resident), kThreads, 0, stream>>>(prm, (uint32_t)units, (uint32_t)units_per_row);
-    return cudaGetLastError();
+    return launch_after(kernel, dim3((unsigned)(blocks < resident ? blocks : resident)), kThreads, 0, stream, 1, prm, (uint32_t)units,
+                        (uint32_t)units_per_row);
 }
 
 template <typename T>

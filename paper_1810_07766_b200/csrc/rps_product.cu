@@ -393,7 +393,7 @@ __device__ __forceinline__ void epilogue(const ProductParams& prm, int w, int sp
 
 // ------------------------------------------------------------------------------------------------------------ kernel
 template <Product WHICH, int PLANES>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(kThreads, 1)
     rps_product_kernel(const __grid_constant__ ProductParams prm, const __grid_constant__ Maps maps)
 {
     constexpr bool kAOther = WHICH == Product::kDweight;                                  // A's rows are contiguous, not the summed axis
@@ -421,7 +421,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&control.tensor_memory)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
     }
+    if (warp == 0 && lane == 0) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.a) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.b) : "memory");
+    }
     const int n_tiles = (prm.n + kTileN - 1) / kTileN;
+    after_the_kernel_before();
     if (warp == 2) {
         // tiles of each worker: where the tokens are rows, only those that hold a token that takes part
         int total = 0;
@@ -631,8 +636,7 @@ cudaError_t launch(const ProductParams& prm, cudaStream_t stream)
     if (p.splits < 1) p.splits = 1;
     const int64_t tiles = product_tiles(p.m, p.n, p.workers) * p.splits;
     const int pairs = (int)(tiles < sms / 2 ? tiles : sms / 2);
-    rps_product_kernel<WHICH, PLANES><<<2 * pairs, kThreads, kSharedBytes, stream>>>(p, maps);
-    return cudaGetLastError();
+    return launch_after(rps_product_kernel<WHICH, PLANES>, dim3(2 * pairs), kThreads, kSharedBytes, stream, 2, p, maps);
 }
 
 }  // namespace
@@ -665,6 +669,7 @@ namespace {
 template <typename T, bool HIDDEN>
 __global__ void __launch_bounds__(256) rps_join_kernel(const ProductParams prm)
 {
+    after_the_kernel_before();
     const int w = blockIdx.y, lane = threadIdx.x % 32;
     const int64_t row = (int64_t)blockIdx.x * 8 + threadIdx.x / 32;
     if (row >= (HIDDEN ? (int64_t)prm.count[w] : (int64_t)prm.m)) return;
@@ -697,18 +702,10 @@ __global__ void __launch_bounds__(256) rps_join_kernel(const ProductParams prm)
 cudaError_t launch_join(Product which, const ProductParams& prm, cudaStream_t stream)
 {
     const dim3 grid((unsigned)ceil_div(prm.m, 8), (unsigned)prm.workers);
-    if (which == Product::kDhidden) {
-        if (prm.planes == 3)
-            rps_join_kernel<float, true><<<grid, 256, 0, stream>>>(prm);
-        else
-            rps_join_kernel<bf16, true><<<grid, 256, 0, stream>>>(prm);
-    } else {
-        if (prm.planes == 3)
-            rps_join_kernel<float, false><<<grid, 256, 0, stream>>>(prm);
-        else
-            rps_join_kernel<bf16, false><<<grid, 256, 0, stream>>>(prm);
-    }
-    return cudaGetLastError();
+    const bool hidden = which == Product::kDhidden, f32 = prm.planes == 3;
+    const auto kernel = hidden ? (f32 ? rps_join_kernel<float, true> : rps_join_kernel<bf16, true>)
+                               : (f32 ? rps_join_kernel<float, false> : rps_join_kernel<bf16, false>);
+    return launch_after(kernel, grid, 256, 0, stream, 1, prm);
 }
 
 cudaError_t launch_product(Product which, const ProductParams& prm, cudaStream_t stream)
