@@ -12,64 +12,77 @@ constexpr int kMergeThreads = 512, kMergeRows = 32;
 constexpr int kRowThreads = 256;
 
 // One CTA per worker.  rows[] becomes a permutation of the worker's tokens: those that take part in their order, then
-// the ignored ones; a ballot and a scan over the warps' counts give each token its place.
+// the ignored ones.  A thread takes four tokens at a time; a scan over the lanes and one over the warps give each its place.
 __global__ void __launch_bounds__(kSelectThreads) rps_lce_select_kernel(const LceParams prm)
 {
     after_the_kernel_before();
-    __shared__ int warp_count[kSelectThreads / 32];
+    constexpr int kEach = 4, kWarps = kSelectThreads / 32;
+    static_assert(kWarps == 32, "a lane for each warp's count");
+    __shared__ int warp_count[kWarps];
     const int w = blockIdx.x, lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     const int64_t* targets = prm.targets + w * prm.tokens;
     int* rows = prm.rows + w * prm.tokens;
-    int* target = prm.target + w * prm.tokens_padded;
+    const int64_t padded = w * prm.tokens_padded;
     int kept = 0;
-    for (int64_t t0 = 0; t0 < prm.tokens; t0 += kSelectThreads) {
-        const int64_t t = t0 + threadIdx.x;
-        const int64_t y = t < prm.tokens ? targets[t] : prm.ignore_index;
-        const bool in = t < prm.tokens && y != prm.ignore_index;
-        const unsigned mask = __ballot_sync(0xFFFFFFFFu, in);
-        if (lane == 0) warp_count[warp] = __popc(mask);
-        __syncthreads();
-        int before = __popc(mask & ((1u << lane) - 1)), total = 0;
-        for (int i = 0; i < kSelectThreads / 32; ++i) {
-            if (i < warp) before += warp_count[i];
-            total += warp_count[i];
+    for (int64_t t0 = 0; t0 < prm.tokens; t0 += kSelectThreads * kEach) {
+        const int64_t t = t0 + threadIdx.x * kEach;
+        int64_t y[kEach];
+        int mine = 0;
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            y[j] = t + j < prm.tokens ? targets[t + j] : prm.ignore_index;
+            mine += y[j] != prm.ignore_index;
         }
-        if (in) {
-            const int at = kept + before;
-            const bool names_a_row = y >= 0 && y < prm.vocab;
-            rows[at] = (int)t;
-            target[at] = names_a_row ? (int)y : -1;
-            if (!prm.backward) const_cast<float*>(prm.hit)[w * prm.tokens_padded + at] = names_a_row ? 0.0f : nanf("");
-        } else if (t < prm.tokens) {
-            // filled from the end, so that the places do not depend on the count: ignored token number i lies i from the end
-            const int ignored = (int)t - (kept + before);
-            rows[prm.tokens - 1 - ignored] = (int)t;
-            if (!prm.backward) {
-                prm.lse[w * prm.tokens + t] = 0.0f;
-                if (prm.reduction == RPS_REDUCE_NONE) prm.loss[w * prm.tokens + t] = 0.0f;
+        int upto = mine;  // of this lane and those before it
+#pragma unroll
+        for (int s = 1; s < 32; s *= 2) {
+            const int n = __shfl_up_sync(0xFFFFFFFFu, upto, s);
+            if (lane >= s) upto += n;
+        }
+        if (lane == 31) warp_count[warp] = upto;
+        __syncthreads();
+        int warps_upto = warp_count[lane];
+#pragma unroll
+        for (int s = 1; s < 32; s *= 2) {
+            const int n = __shfl_up_sync(0xFFFFFFFFu, warps_upto, s);
+            if (lane >= s) warps_upto += n;
+        }
+        int at = kept + upto - mine + (warp > 0 ? __shfl_sync(0xFFFFFFFFu, warps_upto, warp - 1) : 0);
+        kept += __shfl_sync(0xFFFFFFFFu, warps_upto, 31);
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            if (t + j >= prm.tokens) break;
+            if (y[j] != prm.ignore_index) {
+                const bool names_a_row = y[j] >= 0 && y[j] < prm.vocab;
+                rows[at] = (int)t + j;
+                prm.target[padded + at] = names_a_row ? (int)y[j] : -1;
+                if (prm.backward) {
+                    const float g = prm.reduction == RPS_REDUCE_NONE ? prm.dloss[w * prm.tokens + t + j] : 1.0f;
+                    prm.info[padded + at] = make_float2(prm.lse_in[w * prm.tokens + t + j], names_a_row ? g : nanf(""));
+                } else {
+                    const_cast<float*>(prm.hit)[padded + at] = names_a_row ? 0.0f : nanf("");
+                }
+                ++at;
+            } else {
+                // filled from the end, so that the places do not depend on the count: ignored token number i lies i from the end
+                rows[prm.tokens - 1 - ((int)t + j - at)] = (int)t + j;
+                if (!prm.backward) {
+                    prm.lse[w * prm.tokens + t + j] = 0.0f;
+                    if (prm.reduction == RPS_REDUCE_NONE) prm.loss[w * prm.tokens + t + j] = 0.0f;
+                }
             }
         }
-        kept += total;
         __syncthreads();
     }
-    if (threadIdx.x == 0) {
-        prm.count[w] = kept;
-        if (!prm.backward) prm.done[w] = 0;
-    }
-    if (!prm.backward) {
-        if (kept == 0 && prm.reduction != RPS_REDUCE_NONE && threadIdx.x == 0) prm.loss[w] = 0.0f;
-        return;
-    }
-    // A factor that all rows share stays out of dl: near a token's target dl is p - 1, which bf16 holds all but exactly, and
-    // (p - 1) times a factor it does not (relative error of the gradients: 2.7e-3 -> 1.7e-3, 1.65e-3 of it the rounding of the result).
-    if (threadIdx.x == 0)
+    if (threadIdx.x != 0) return;
+    prm.count[w] = kept;
+    if (prm.backward) {
+        // A factor that all rows share stays out of dl: near a token's target dl is p - 1, which bf16 holds all but exactly, and
+        // (p - 1) times a factor it does not (relative error of the gradients: 2.7e-3 -> 1.7e-3, 1.65e-3 of it the rounding of the result).
         prm.scale[w] = prm.reduction == RPS_REDUCE_NONE || kept == 0 ? 1.0f : prm.reduction == RPS_REDUCE_MEAN ? prm.dloss[w] / (float)kept : prm.dloss[w];
-    __syncthreads();  // rows[] and target[] of this CTA's own threads
-    for (int i = threadIdx.x; i < kept; i += kSelectThreads) {
-        const int t = rows[i];
-        float g = prm.reduction == RPS_REDUCE_NONE ? prm.dloss[w * prm.tokens + t] : 1.0f;
-        if (target[i] < 0) g = nanf("");
-        prm.info[w * prm.tokens_padded + i] = make_float2(prm.lse_in[w * prm.tokens + t], g);
+    } else {
+        prm.done[w] = 0;
+        if (kept == 0 && prm.reduction != RPS_REDUCE_NONE) prm.loss[w] = 0.0f;
     }
 }
 
