@@ -75,6 +75,7 @@ struct ProductParams {
     // The summed axis may be cut into `splits` runs of blocks, each with its own part [split][worker][part_rows][part_row]; over several
     // pieces of the vocabulary a part goes on growing (`add`).
     int splits, add;
+    int tile_cols;                // kDhidden, kDweight: columns of a tile (launch_product's to set)
     float* parts;
     int64_t part_rows, part_row;  // multiples of the tile
 };

@@ -26,8 +26,8 @@ using rps::mbar_arrive_expect_tx;
 using rps::mbar_init;
 using rps::smem_addr;
 
-constexpr int kTileM = 256, kTileN = 256, kDepth = 64;  // of a pair; 64 bf16 are one 128-byte swizzled line
-constexpr int kHalf = kTileN / 2;  // columns of a warp of the epilogue
+constexpr int kTileM = 256, kTileN = 256, kDepth = 64;  // of a pair (kTileN at most); 64 bf16 are one 128-byte swizzled line
+constexpr int kHalf = kTileN / 2;  // columns of a warp of the epilogue, at most
 constexpr int kStages = 6;
 constexpr int kOperandBytes = 128 * kDepth * 2;  // one operand's part of a stage in one CTA
 constexpr int kStageBytes = 2 * kOperandBytes;
@@ -137,10 +137,10 @@ __device__ __forceinline__ uint64_t tile_descriptor(uint32_t addr, uint32_t lead
            2ull << 61;
 }
 
-// fp32 sums of bf16 products, 256 x 256 over the pair.
-__host__ __device__ constexpr uint32_t instruction_descriptor(bool a_other, bool b_other)
+// fp32 sums of bf16 products, 256 x tile_n over the pair.
+__device__ __forceinline__ uint32_t instruction_descriptor(bool a_other, bool b_other, int tile_n)
 {
-    return 1u << 4 | 1u << 7 | 1u << 10 | (a_other ? 1u : 0u) << 15 | (b_other ? 1u : 0u) << 16 | (uint32_t)(kTileN / 8) << 17 |
+    return 1u << 4 | 1u << 7 | 1u << 10 | (a_other ? 1u : 0u) << 15 | (b_other ? 1u : 0u) << 16 | (uint32_t)(tile_n / 8) << 17 |
            (uint32_t)(kTileM / 16) << 24;
 }
 
@@ -172,7 +172,8 @@ __device__ __forceinline__ void load_sums(float* v, uint32_t addr)
         : "memory");
 }
 
-// 128 columns of this lane's row: taken over, or added to those of the segments before.
+// 128 columns of this lane's row: taken over, or added to those of the segments before.  (Of a narrower tile the last ones are whatever
+// tensor memory holds; they are not stored.)
 __device__ __forceinline__ void take_sums(float (&v)[kHalf], uint32_t addr, bool add)
 {
     __syncwarp();
@@ -211,8 +212,8 @@ __device__ __forceinline__ uint32_t two_bf16(float lo, float hi)
 __device__ __forceinline__ void store_element(float* to, float e) { __stcg(to, e); }
 __device__ __forceinline__ void store_element(bf16* to, bf16 e) { __stcg(reinterpret_cast<unsigned short*>(to), __bfloat16_as_ushort(e)); }
 
-// 64 bytes of each of the warp's rows, from column `c` on.  Loads come before stores, several at a time.
-template <bool ADD, typename T>
+// 64 bytes of each of the warp's rows, from column `c` on.  Loads come before stores, several at a time.  ADD, WHOLE: see store_rows.
+template <bool ADD, bool WHOLE, typename T>
 __device__ __forceinline__ void store_chunk(Staging& stage, const uint4 (&mine)[4], T* out, int c, int cols, bool wide)
 {
     constexpr int kChunk = 64 / sizeof(T), kPart = 16 / sizeof(T);  // columns
@@ -221,7 +222,7 @@ __device__ __forceinline__ void store_chunk(Staging& stage, const uint4 (&mine)[
 #pragma unroll
     for (int q = 0; q < 4; ++q) stage.part[lane][q ^ (lane >> 1 & 3)] = mine[q];
     __syncwarp();
-    if (wide) {
+    if (WHOLE || wide) {
         const int col = c + lane % 4 * kPart;
         uint4 word[4];
         int64_t at[4];
@@ -245,7 +246,7 @@ __device__ __forceinline__ void store_chunk(Staging& stage, const uint4 (&mine)[
         for (int i = 0; i < 4; ++i) {
             if (at[i] < 0) continue;
             T* to = out + at[i] + col;
-            if (col + kPart <= cols) {
+            if (WHOLE || col + kPart <= cols) {
                 __stcg(reinterpret_cast<uint4*>(to), word[i]);
             } else {
                 const T* e = reinterpret_cast<const T*>(&word[i]);
@@ -275,9 +276,9 @@ __device__ __forceinline__ void store_chunk(Staging& stage, const uint4 (&mine)[
     }
 }
 
-// `at`: offset of this lane's row in `out`, or -1 if it is not to be written; `cols` of the 128 columns exist.  ADD: to what is there
-// (fp32, wide).
-template <bool ADD, typename T>
+// `at`: offset of this lane's row in `out`, or -1 if it is not to be written; `cols` of the 128 columns exist.  WHOLE: rows are 16-byte
+// aligned and `cols` a multiple of 16 bytes.  ADD: to what is there (fp32, WHOLE).
+template <bool ADD, bool WHOLE, typename T>
 __device__ __forceinline__ void store_rows(Staging& stage, const float (&v)[kHalf], T* out, int64_t at, int cols, bool wide)
 {
     constexpr int kChunk = 64 / sizeof(T), kPart = 16 / sizeof(T);
@@ -294,7 +295,7 @@ __device__ __forceinline__ void store_rows(Staging& stage, const float (&v)[kHal
             else
                 mine[q] = make_uint4(two_bf16(f[0], f[1]), two_bf16(f[2], f[3]), two_bf16(f[4], f[5]), two_bf16(f[6], f[7]));
         }
-        store_chunk<ADD>(stage, mine, out, c, cols, wide);
+        store_chunk<ADD, WHOLE>(stage, mine, out, c, cols, wide);
     }
 }
 
@@ -320,16 +321,16 @@ __device__ __forceinline__ void store_parts(Staging& stage, float (&v)[kHalf], b
                 }
                 word[j / 2] = two_bf16(part[0], part[1]);
             }
-            store_chunk<false>(stage, mine, out + q * plane, c, kHalf, true);
+            store_chunk<false, true>(stage, mine, out + q * plane, c, kHalf, true);
         }
     }
 }
 
 // One row's 128 columns of a tile.
 template <Product WHICH, int PLANES>
-__device__ __forceinline__ void epilogue(const ProductParams& prm, int w, int split, int row, int n0, int count, float (&v)[kHalf], bool wide, Staging& stage)
+__device__ __forceinline__ void epilogue(const ProductParams& prm, int w, int split, int row, int n0, int width, int count, float (&v)[kHalf], bool wide, Staging& stage)
 {
-    const int cols = prm.n - n0;
+    const int cols = min(width, prm.n - n0);
     if (cols <= 0 && WHICH != Product::kDlogits) return;
     if constexpr (WHICH == Product::kLse) {
         if (row >= count) return;
@@ -365,7 +366,7 @@ __device__ __forceinline__ void epilogue(const ProductParams& prm, int w, int sp
             v[j] = in && j < cols ? info.y * p : 0.0f;
         }
         if constexpr (PLANES == 1) {
-            store_rows<false>(stage, v, prm.dl, at_dl, kHalf, true);
+            store_rows<false, true>(stage, v, prm.dl, at_dl, kHalf, true);
         } else {
             store_parts(stage, v, prm.dl, prm.tokens_padded * prm.piece, at_dl);
         }
@@ -375,9 +376,9 @@ __device__ __forceinline__ void epilogue(const ProductParams& prm, int w, int sp
         if (prm.parts != nullptr) {
             const int64_t at = in ? (((int64_t)split * prm.workers + w) * prm.part_rows + row) * prm.part_row + n0 : -1;
             if (prm.add)
-                store_rows<true>(stage, v, prm.parts, at, kHalf, true);
+                store_rows<true, true>(stage, v, prm.parts, at, width, true);
             else
-                store_rows<false>(stage, v, prm.parts, at, kHalf, true);
+                store_rows<false, true>(stage, v, prm.parts, at, width, true);
             return;
         }
         const float g = prm.scale != nullptr ? prm.scale[w] : 1.0f;
@@ -385,9 +386,9 @@ __device__ __forceinline__ void epilogue(const ProductParams& prm, int w, int sp
 #pragma unroll
         for (int j = 0; j < kHalf; ++j) v[j] *= g;
         if constexpr (PLANES == 3)
-            store_rows<false>(stage, v, static_cast<float*>(prm.out), at, cols, wide);
+            store_rows<false, false>(stage, v, static_cast<float*>(prm.out), at, cols, wide);
         else
-            store_rows<false>(stage, v, static_cast<bf16*>(prm.out), at, cols, wide);
+            store_rows<false, false>(stage, v, static_cast<bf16*>(prm.out), at, cols, wide);
     }
 }
 
@@ -425,7 +426,10 @@ __global__ void __launch_bounds__(kThreads, 1)
         asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.a) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.b) : "memory");
     }
-    const int n_tiles = (prm.n + kTileN - 1) / kTileN;
+    // Columns of a tile.  Where they are a width that 256 does not divide, the tiles are made as narrow as their number allows (650
+    // columns: three of 224 instead of 256), as a tile's products take time by its columns.
+    const int tile_n = WHICH == Product::kDhidden || WHICH == Product::kDweight ? prm.tile_cols : kTileN, half_n = tile_n / 2;
+    const int n_tiles = (prm.n + tile_n - 1) / tile_n;
     after_the_kernel_before();
     if (warp == 2) {
         // tiles of each worker: where the tokens are rows, only those that hold a token that takes part
@@ -458,7 +462,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         // kLse, kDlogits: all rows of a column of tiles before the next one, so that the weight is read from memory once; kDweight: all
         // columns of a row of tiles, for dl's sake
         const int m = kRowsFirst ? tile % m_tiles : tile / n_tiles, n = kRowsFirst ? tile / m_tiles : tile % n_tiles;
-        t.m0 = m * kTileM, t.n0 = n * kTileN;
+        t.m0 = m * kTileM, t.n0 = n * tile_n;
         t.count = prm.count != nullptr ? prm.count[t.w] : (WHICH == Product::kDweight ? prm.k : prm.m);
         const int k = WHICH == Product::kDweight ? t.count : prm.k;
         const int depth = (k + kDepth - 1) / kDepth, run = (depth + prm.splits - 1) / prm.splits;
@@ -476,14 +480,14 @@ __global__ void __launch_bounds__(kThreads, 1)
             uint32_t phase = 0;
             for (int tile = blockIdx.x / 2; tile < total && fine; tile += pairs) {
                 const Tile t = tile_at(tile);
-                const int m0 = t.m0 + rank * 128, n0 = t.n0 + rank * 128;
+                const int m0 = t.m0 + rank * 128, n0 = t.n0 + rank * half_n;
                 const int wa = prm.a.worker != 0 ? t.w : 0, wb = prm.b.worker != 0 ? t.w : 0;
                 for (int i = 0; i < t.blocks * PLANES; ++i) {
                     fine = wait(smem_addr(&control.empty[stage]), phase ^ 1);
                     if (!fine) break;
                     const int kb = PLANES == 1 ? i : i / 3, plane = i - kb * PLANES, k0 = (t.first + kb) * kDepth;
                     const uint32_t bar = in_first_cta(smem_addr(&control.full[stage]));
-                    if (rank == 0) mbar_arrive_expect_tx(smem_addr(&control.full[stage]), 2 * kStageBytes);
+                    if (rank == 0) mbar_arrive_expect_tx(smem_addr(&control.full[stage]), kBOther && half_n <= 64 ? 2 * kStageBytes - kOperandBytes : 2 * kStageBytes);
                     const uint32_t a = base + stage * kStageBytes, b = a + kOperandBytes;
                     if (kAOther) {
                         load_box(a, &maps.a, m0, k0, plane, wa, bar);
@@ -493,7 +497,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                     if (kBOther) {
                         load_box(b, &maps.b, n0, k0, plane, wb, bar);
-                        load_box(b + kOperandBytes / 2, &maps.b, n0 + 64, k0, plane, wb, bar);
+                        if (half_n > 64) load_box(b + kOperandBytes / 2, &maps.b, n0 + 64, k0, plane, wb, bar);
                     } else {
                         load_box(b, &maps.b, k0, n0, plane, wb, bar);
                     }
@@ -515,7 +519,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
     } else if (warp == 1) {
         if (rank == 0 && lane == 0) {
-            constexpr uint32_t descriptor = instruction_descriptor(kAOther, kBOther);
+            const uint32_t descriptor = instruction_descriptor(kAOther, kBOther, tile_n);
             // one product covers 16 of the summed axis: 32 bytes further along swizzled rows, or 16 rows of 128 bytes further
             constexpr uint32_t a_step = kAOther ? 2048 : 32, b_step = kBOther ? 2048 : 32;
             int stage = 0, made = 0;
@@ -582,14 +586,14 @@ __global__ void __launch_bounds__(kThreads, 1)
                 fine = __all_sync(0xFFFFFFFFu, wait(smem_addr(&control.sum_full[buffer]), made >> 1 & 1));
                 if (!fine) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                take_sums(v, tensor_memory + ((uint32_t)(quarter * 32) << 16) + buffer * kTileN + half * kHalf, kb > 0);
+                take_sums(v, tensor_memory + ((uint32_t)(quarter * 32) << 16) + buffer * kTileN + half * half_n, kb > 0);
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) arrive_cluster(in_first_cta(smem_addr(&control.sum_empty[buffer])));
                 ++made;
             }
             if (!fine) break;
-            epilogue<WHICH, PLANES>(prm, t.w, t.split, t.m0 + (int)rank * 128 + quarter * 32 + lane, t.n0 + half * kHalf, t.count, v, wide, control.staging[warp - 2]);
+            epilogue<WHICH, PLANES>(prm, t.w, t.split, t.m0 + (int)rank * 128 + quarter * 32 + lane, t.n0 + half * half_n, half_n, t.count, v, wide, control.staging[warp - 2]);
         }
     }
     if (!fine && lane == 0) atomicExch(&g_gave_up, 1);
@@ -634,6 +638,7 @@ cudaError_t launch(const ProductParams& prm, cudaStream_t stream)
         return cudaErrorInvalidValue;
     }
     if (p.splits < 1) p.splits = 1;
+    p.tile_cols = (int)round_up(ceil_div(p.n, ceil_div(p.n, kTileN)), 32);
     const int64_t tiles = product_tiles(p.m, p.n, p.workers) * p.splits;
     const int pairs = (int)(tiles < sms / 2 ? tiles : sms / 2);
     return launch_after(rps_product_kernel<WHICH, PLANES>, dim3(2 * pairs), kThreads, kSharedBytes, stream, 2, p, maps);

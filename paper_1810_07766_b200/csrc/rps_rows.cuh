@@ -231,37 +231,59 @@ __device__ __forceinline__ void split_slice(const float (&v)[8], uint4 (&parts)[
 
 constexpr float kSmallestPacked = 0x1p-100f;  // a group with nothing larger is kept as zeros: 127 / max stays finite
 
-// A lane's part of a group in 8 bits: all lanes of the warp call it.  Columns past the end hold zeros.  The scale goes out from
-// the group's first lane (`scale` NULL in lanes that are past the end), the codes where `codes` is not NULL.
+// The largest size among a lane's values, as bits: as integers, finite < infinity < NaN.
 template <int WIDTH>
-__device__ __forceinline__ void pack_slice(const float (&v)[WIDTH], int8_t* codes, float* scale)
+__device__ __forceinline__ uint32_t largest(const float (&v)[WIDTH])
 {
-    constexpr int kLanes = RPS_PACK_GROUP / WIDTH;
-    // sizes compare as integers: finite < infinity < NaN
     uint32_t top = 0;
 #pragma unroll
     for (int j = 0; j < WIDTH; ++j) top = max(top, __float_as_uint(v[j]) & 0x7FFFFFFFu);
-#pragma unroll
-    for (int s = kLanes / 2; s > 0; s /= 2) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, s));
-    const bool finite = top < 0x7F800000u, zero = !finite || __uint_as_float(top) < kSmallestPacked;
-    const float factor = zero ? 0.0f : __fdiv_rn(127.0f, __uint_as_float(top));
-    // 1.5 * 2^23 has units of one in its last place, so adding it rounds to an integer, ties to even, and leaves it in the low bits
-    uint32_t word[WIDTH / 4];
-#pragma unroll
-    for (int i = 0; i < WIDTH / 4; ++i) {
-        uint32_t q[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) q[j] = __float_as_uint(__fadd_rn(__fmul_rn(v[4 * i + j], factor), 12582912.0f));
-        word[i] = __byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410);
-        if (zero) word[i] = 0;  // infinities and NaN times zero
+    return top;
+}
+
+// Codes and scale of a group whose largest size is `top`.
+struct Quantiser {
+    float largest, factor;
+    bool finite, zero;
+    __device__ __forceinline__ explicit Quantiser(uint32_t top)
+    {
+        largest = __uint_as_float(top);
+        finite = top < 0x7F800000u, zero = !finite || largest < kSmallestPacked;
+        factor = zero ? 0.0f : __fdiv_rn(127.0f, largest);
     }
-    if (codes != nullptr) {
+    __device__ __forceinline__ float scale() const { return !finite ? __int_as_float(0x7FFFFFFF) : zero ? 0.0f : __fmul_rn(largest, 1.0f / 127.0f); }
+    // 1.5 * 2^23 has units of one in its last place, so adding it rounds to an integer, ties to even, and leaves it in the low bits
+    template <int WIDTH>
+    __device__ __forceinline__ void store(const float (&v)[WIDTH], int8_t* codes) const
+    {
+        uint32_t word[WIDTH / 4];
+#pragma unroll
+        for (int i = 0; i < WIDTH / 4; ++i) {
+            uint32_t q[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) q[j] = __float_as_uint(__fadd_rn(__fmul_rn(v[4 * i + j], factor), 12582912.0f));
+            word[i] = __byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410);
+            if (zero) word[i] = 0;  // infinities and NaN times zero
+        }
         if constexpr (WIDTH == 8)
             *reinterpret_cast<uint2*>(codes) = make_uint2(word[0], word[1]);
         else
             *reinterpret_cast<uint32_t*>(codes) = word[0];
     }
-    if (scale != nullptr && threadIdx.x % kLanes == 0) *scale = !finite ? __int_as_float(0x7FFFFFFF) : zero ? 0.0f : __fmul_rn(__uint_as_float(top), 1.0f / 127.0f);
+};
+
+// A lane's slice of a group in 8 bits: all lanes of the warp call it.  Columns past the end hold zeros.  The scale goes out from
+// the group's first lane (`scale` NULL in lanes that are past the end), the codes where `codes` is not NULL.
+template <int WIDTH>
+__device__ __forceinline__ void pack_slice(const float (&v)[WIDTH], int8_t* codes, float* scale)
+{
+    constexpr int kLanes = RPS_PACK_GROUP / WIDTH;
+    uint32_t top = largest(v);
+#pragma unroll
+    for (int s = kLanes / 2; s > 0; s /= 2) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, s));
+    const Quantiser q(top);
+    if (codes != nullptr) q.store(v, codes);
+    if (scale != nullptr && threadIdx.x % kLanes == 0) *scale = q.scale();
 }
 
 // The values of four codes: a byte with its sign bit turned over, put under the bits of 2^23, is 2^23 + 128 + code.
