@@ -93,7 +93,7 @@ struct LcePlan {
     bf16* dl = nullptr;
     float* hidden_parts = nullptr;
     float* weight_parts = nullptr;
-    int hidden_splits = 1, weight_splits = 1;
+    ProductShape hidden_shape{}, weight_shape{};
     size_t bytes = 0;
 };
 
@@ -128,7 +128,11 @@ LcePlan plan_lce(const rps_lce_desc& d, const void* weight, bool backward, void*
     };
     if (backward) narrow(p.n * p.planes * p.tokens_padded * 2);
     if (plan.lay_out_weight) narrow(p.n * p.planes * p.cols_padded * 2);
-    p.stat_tiles = ceil_div(d.vocab, kStatCols);
+    ProductParams& g = plan.product;
+    // in several pieces the tiles are whole, so that the pieces' statistics lie side by side
+    g.tile_cols = plan.piece < whole ? kVocabTile : product_shape(d.tokens, d.vocab, d.cols, d.n, p.planes, false).tile_cols;
+    g.stat_cols = g.tile_cols / 2;
+    p.stat_tiles = ceil_div(d.vocab, g.stat_cols);
 
     Carver c{static_cast<unsigned char*>(workspace)};
     p.count = c.take<int>(p.n);
@@ -141,10 +145,11 @@ LcePlan plan_lce(const rps_lce_desc& d, const void* weight, bool backward, void*
         plan.dl = c.take<bf16>(p.n * p.planes * p.tokens_padded * plan.piece);
         p.scale = c.take<float>(p.n);
         const int64_t part_row = round_up(p.cols, kVocabTile);
-        plan.hidden_splits = product_splits(product_tiles(p.tokens, p.cols, p.n), product_blocks(plan.piece), p.planes);
-        if (plan.piece < whole || plan.hidden_splits > 1) plan.hidden_parts = c.take<float>(plan.hidden_splits * p.n * p.tokens_padded * part_row);
-        plan.weight_splits = product_splits(product_tiles(plan.piece, p.cols, p.n), product_blocks(p.tokens), p.planes);
-        if (plan.weight_splits > 1) plan.weight_parts = c.take<float>(plan.weight_splits * p.n * plan.piece * part_row);
+        plan.hidden_shape = product_shape(d.tokens, d.cols, plan.piece < d.vocab ? plan.piece : d.vocab, p.n, p.planes, true);
+        if (plan.piece < whole || plan.hidden_shape.splits > 1)
+            plan.hidden_parts = c.take<float>(plan.hidden_shape.splits * p.n * p.tokens_padded * part_row);
+        plan.weight_shape = product_shape(plan.piece < d.vocab ? plan.piece : d.vocab, d.cols, d.tokens, p.n, p.planes, true);
+        if (plan.weight_shape.splits > 1) plan.weight_parts = c.take<float>(plan.weight_shape.splits * p.n * plan.piece * part_row);
     } else {
         p.done = c.take<int>(p.n);
         p.sums = c.take<float>(p.n * lce_merge_blocks(p.tokens));
@@ -153,7 +158,6 @@ LcePlan plan_lce(const rps_lce_desc& d, const void* weight, bool backward, void*
     }
     plan.bytes = c.used;
 
-    ProductParams& g = plan.product;
     g.workers = p.n, g.planes = p.planes, g.count = p.count;
     g.vocab = (int)p.vocab, g.stat_tiles = (int)p.stat_tiles, g.target = p.target;
     g.part = const_cast<float2*>(p.part), g.hit = const_cast<float*>(p.hit), g.info = p.info, g.dl = plan.dl;
@@ -258,7 +262,7 @@ extern "C" int rps_lce_backward(const rps_lce_desc* desc, const void* hidden, co
     const Operand h = hidden_operand(p);
     for (int64_t v0 = 0; v0 < d.vocab; v0 += plan.piece) {
         const int64_t rows = d.vocab - v0 < plan.piece ? d.vocab - v0 : plan.piece;
-        const int64_t tiled = round_up(rows, kVocabTile);  // dl is written (zeros behind the last row) in whole tiles
+        const int64_t tiled = round_up(rows, plan.product.tile_cols);  // dl is written (zeros behind the last row) in whole tiles
         Operand weight_rows;
         if (int rc = weight_operand(d, plan, weight, v0, rows, &weight_rows, stream)) return rc;
         const int64_t plane = p.tokens_padded * plan.piece;
@@ -268,14 +272,14 @@ extern "C" int rps_lce_backward(const rps_lce_desc* desc, const void* hidden, co
         if (d.tokens > 0) {
             g.a = h, g.b = weight_rows, g.m = (int)d.tokens, g.n = (int)rows, g.k = (int)d.cols;
             RPS_TRY(launch_product(Product::kDlogits, g, stream));
-            g.a = dl, g.n = (int)d.cols, g.k = (int)rows;
-            g.splits = plan.hidden_splits, g.parts = plan.hidden_parts, g.part_rows = p.tokens_padded, g.add = v0 > 0;
+            g.a = dl, g.n = (int)d.cols, g.k = (int)rows, g.tile_cols = plan.hidden_shape.tile_cols;
+            g.splits = plan.hidden_shape.splits, g.parts = plan.hidden_parts, g.part_rows = p.tokens_padded, g.add = v0 > 0;
             g.out = dhidden, g.out_row = d.cols, g.out_worker = d.tokens * d.cols;
             RPS_TRY(launch_product(Product::kDhidden, g, stream));
             if (g.parts != nullptr && v0 + rows == d.vocab) RPS_TRY(launch_join(Product::kDhidden, g, stream));
         }
-        g.a = dl, g.b = h, g.m = (int)rows, g.n = (int)d.cols, g.k = (int)d.tokens;
-        g.splits = plan.weight_splits, g.parts = plan.weight_parts, g.part_rows = plan.piece, g.add = 0;
+        g.a = dl, g.b = h, g.m = (int)rows, g.n = (int)d.cols, g.k = (int)d.tokens, g.tile_cols = plan.weight_shape.tile_cols;
+        g.splits = plan.weight_shape.splits, g.parts = plan.weight_parts, g.part_rows = plan.piece, g.add = 0;
         g.out = static_cast<unsigned char*>(dweight) + v0 * d.dweight_row * (p.f32 ? 4 : 2), g.out_row = d.dweight_row, g.out_worker = d.dweight_worker;
         RPS_TRY(launch_product(Product::kDweight, g, stream));
         if (g.parts != nullptr) RPS_TRY(launch_join(Product::kDweight, g, stream));
@@ -434,7 +438,7 @@ struct WgradPlan {
     PlanesParams lay_out{};
     PackParams unpack{};
     bool lay_out_dy = false;
-    int splits = 1;
+    ProductShape shape{};
     float* parts = nullptr;
     size_t bytes = 0;
 };
@@ -473,8 +477,8 @@ WgradPlan plan_wgrad(const rps_wgrad_desc& d, const void* dy, void* workspace)
         q.src = dy, q.f32 = d.dtype == RPS_F32, q.n = d.n, q.planes = planes, q.rows = d.tokens, q.cols = d.outs;
         q.src_row = d.dy_row, q.src_worker = d.dy_worker, q.dst = to, q.dst_row = row, q.dst_plane = plane, q.dst_worker = planes * plane;
     }
-    plan.splits = product_splits(product_tiles(d.outs, d.cols, d.n), product_blocks(d.tokens), planes);
-    if (plan.splits > 1) plan.parts = c.take<float>(plan.splits * d.n * round_up(d.outs, kVocabTile) * round_up(d.cols, kVocabTile));
+    plan.shape = product_shape(d.outs, d.cols, d.tokens, d.n, planes, true);
+    if (plan.shape.splits > 1) plan.parts = c.take<float>(plan.shape.splits * d.n * round_up(d.outs, kVocabTile) * round_up(d.cols, kVocabTile));
     plan.bytes = c.used;
     return plan;
 }
@@ -508,9 +512,9 @@ extern "C" int rps_packed_wgrad(const rps_wgrad_desc* desc, const void* dy, cons
     }
     ProductParams g{};
     g.a = plan.dy, g.b = plan.x, g.workers = d.n, g.planes = d.dtype == RPS_F32 ? 3 : 1;
-    g.m = (int)d.outs, g.n = (int)d.cols, g.k = (int)d.tokens;
+    g.m = (int)d.outs, g.n = (int)d.cols, g.k = (int)d.tokens, g.tile_cols = plan.shape.tile_cols;
     g.out = dweight, g.out_row = d.dweight_row, g.out_worker = d.dweight_worker;
-    g.splits = plan.splits, g.parts = plan.parts, g.part_rows = round_up(d.outs, kVocabTile), g.part_row = round_up(d.cols, kVocabTile);
+    g.splits = plan.shape.splits, g.parts = plan.parts, g.part_rows = round_up(d.outs, kVocabTile), g.part_row = round_up(d.cols, kVocabTile);
     RPS_TRY(launch_product(Product::kDweight, g, stream));
     if (g.parts != nullptr) RPS_TRY(launch_join(Product::kDweight, g, stream));
     return RPS_OK;

@@ -32,11 +32,9 @@ cudaError_t launch_after(Kernel kernel, dim3 grid, int threads, size_t shared, c
 }
 
 // ---------------------------------------------------------------------------------------------------- products
-// Token rows are padded to whole tiles, and the vocabulary goes through the loss in whole tiles; softmax statistics are kept for
-// each half of a tile's columns.
+// Token rows are padded to whole tiles, and the vocabulary goes through the loss in whole tiles.
 constexpr int kTokenTile = 256;
 constexpr int kVocabTile = 256;
-constexpr int kStatCols = 128;
 
 // An operand of a product: bf16 [worker][plane][rows][row stride].  fp32 values lie in three planes whose sum they are.
 struct Operand {
@@ -59,7 +57,7 @@ struct ProductParams {
     const int* count;   // [worker] tokens that take part, or NULL: all
     // kLse, kDlogits
     int v0, vocab;          // first row of the vocabulary in this piece; all of it
-    int stat_tiles;
+    int stat_cols, stat_tiles;  // softmax statistics are kept for every stat_cols (half a tile's) columns
     const int* target;      // [worker][tokens_padded]
     float2* part;           // [worker][stat_tiles][tokens_padded]: running maximum and sum
     float* hit;             // [worker][tokens_padded]: the target's logit
@@ -74,16 +72,17 @@ struct ProductParams {
     int64_t tokens;
     // The summed axis may be cut into `splits` runs of blocks, each with its own part [split][worker][part_rows][part_row]; over several
     // pieces of the vocabulary a part goes on growing (`add`).
-    int splits, add;
-    int tile_cols;                // kDhidden, kDweight: columns of a tile (launch_product's to set)
+    int splits, tile_cols;        // product_shape
+    int add;
     float* parts;
     int64_t part_rows, part_row;  // multiples of the tile
 };
 
-// How many runs to cut a product's summed axis into, for `tiles` tiles of `blocks` blocks of 64 each.
-int product_splits(int64_t tiles, int64_t blocks, int planes);
-int64_t product_tiles(int64_t m, int64_t n, int workers);
-int64_t product_blocks(int64_t k);
+// How a product is cut: columns of its tiles, and runs of its summed axis.
+struct ProductShape {
+    int tile_cols, splits;
+};
+ProductShape product_shape(int64_t m, int64_t n, int64_t k, int workers, int planes, bool may_split);
 
 cudaError_t launch_product(Product which, const ProductParams& prm, cudaStream_t stream);
 cudaError_t launch_join(Product which, const ProductParams& prm, cudaStream_t stream);  // the parts into `out`
@@ -109,7 +108,7 @@ struct LceParams {
     // forward's end
     const float2* part;
     const float* hit;
-    int64_t stat_tiles;
+    int64_t stat_tiles;  // as ProductParams
     float* loss;
     float* lse;
     float* sums;      // [n][lce_merge_blocks(tokens)]

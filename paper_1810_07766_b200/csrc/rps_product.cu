@@ -46,7 +46,7 @@ static_assert(kTileM == kTokenTile && kTileN == kVocabTile, "operands are padded
 // Rows leave through shared memory: a lane holds one row, and 32 lanes writing 16 bytes of 32 rows each would touch 32 lines at a time and
 // half a sector of each.  Instead 64 bytes of each of the warp's 32 rows are laid down (parts of 16 bytes, exchanged by the row's
 // number so that neither side has bank conflicts) and written out as 4 lanes to a row; rows that are not 16-byte aligned go out
-// element by element, still in the order of memory.  (Gradient of 8 fp32 weights of 10001 x 650, rows of 2600 bytes: 453 -> XXX us.)
+// element by element, still in the order of memory.  (Gradient of 8 fp32 weights of 10001 x 650, rows of 2600 bytes: 453 -> 225 us.)
 struct Staging {
     uint4 part[32][4];
     int64_t at[32];
@@ -56,6 +56,7 @@ struct Control {
     Staging staging[kEpilogueWarps];
     uint64_t full[kStages], empty[kStages], sum_full[2], sum_empty[2];
     uint32_t tensor_memory;
+    int count[RPS_MAX_WORKERS];      // tokens of each worker that take part
     int start[RPS_MAX_WORKERS + 1];  // first tile of each worker
 };
 
@@ -286,6 +287,7 @@ __device__ __forceinline__ void store_rows(Staging& stage, const float (&v)[kHal
     stage.at[threadIdx.x % 32] = at;
 #pragma unroll
     for (int c = 0; c < kHalf; c += kChunk) {
+        if (c >= cols) break;
         uint4 mine[4];
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
@@ -300,12 +302,13 @@ __device__ __forceinline__ void store_rows(Staging& stage, const float (&v)[kHal
 }
 
 // fp32 values as three planes of bf16 parts.
-__device__ __forceinline__ void store_parts(Staging& stage, float (&v)[kHalf], bf16* out, int64_t plane, int64_t at)
+__device__ __forceinline__ void store_parts(Staging& stage, float (&v)[kHalf], bf16* out, int64_t plane, int64_t at, int cols)
 {
     __syncwarp();
     stage.at[threadIdx.x % 32] = at;
 #pragma unroll
     for (int c = 0; c < kHalf; c += 32) {
+        if (c >= cols) break;
 #pragma unroll
         for (int q = 0; q < 3; ++q) {
             uint4 mine[4];
@@ -321,54 +324,92 @@ __device__ __forceinline__ void store_parts(Staging& stage, float (&v)[kHalf], b
                 }
                 word[j / 2] = two_bf16(part[0], part[1]);
             }
-            store_chunk<false, true>(stage, mine, out + q * plane, c, kHalf, true);
+            store_chunk<false, true>(stage, mine, out + q * plane, c, cols, true);
         }
     }
 }
 
+// What the epilogue needs to know of a row, read while the products are still on their way.
+struct RowInfo {
+    int target;   // kLse, kDlogits: less the first column of this warp
+    float2 info;  // kDlogits: lse and g
+    int64_t at;   // kDhidden, kDweight: offset of the row in `out`, -1 if it is not to be written
+    float scale;
+};
+
+template <Product WHICH>
+__device__ __forceinline__ RowInfo row_info(const ProductParams& prm, int w, int row, int n0, int count)
+{
+    RowInfo r{};
+    const bool in = row < (WHICH == Product::kDweight ? prm.m : count);
+    if constexpr (WHICH == Product::kLse || WHICH == Product::kDlogits) {
+        r.target = in ? __ldg(prm.target + w * prm.tokens_padded + row) - prm.v0 - n0 : -1;
+        if (WHICH == Product::kDlogits && in) r.info = __ldg(prm.info + w * prm.tokens_padded + row);
+    } else {
+        r.at = -1;
+        if (in && prm.parts == nullptr) r.at = w * prm.out_worker + (WHICH == Product::kDhidden ? (int64_t)__ldg(prm.rows + w * prm.tokens + row) : (int64_t)row) * prm.out_row + n0;
+        r.scale = prm.scale != nullptr ? __ldg(prm.scale + w) : 1.0f;
+    }
+    return r;
+}
+
 // One row's 128 columns of a tile.
 template <Product WHICH, int PLANES>
-__device__ __forceinline__ void epilogue(const ProductParams& prm, int w, int split, int row, int n0, int width, int count, float (&v)[kHalf], bool wide, Staging& stage)
+__device__ __forceinline__ void epilogue(const ProductParams& prm, int w, int split, int row, int n0, int width, int count, const RowInfo& info, float (&v)[kHalf], bool wide, Staging& stage)
 {
     const int cols = min(width, prm.n - n0);
     if (cols <= 0 && WHICH != Product::kDlogits) return;
     if constexpr (WHICH == Product::kLse) {
+        // in runs of 32 columns, as a narrow tile has fewer
         if (row >= count) return;
-        if (cols < kHalf) {
-#pragma unroll
-            for (int j = 0; j < kHalf; ++j)
-                if (j >= cols) v[j] = -INFINITY;
-        }
+        const int t = info.target;
         float top = -INFINITY, sum = 0.0f;
 #pragma unroll
-        for (int j = 0; j < kHalf; ++j) top = fmaxf(top, v[j]);
-        const float at = top == -INFINITY ? 0.0f : top * kLog2e;
-        const int t = prm.target[w * prm.tokens_padded + row] - prm.v0 - n0;
-        if (t >= 0 && t < kHalf) {
-            float hit = 0.0f;
+        for (int c = 0; c < kHalf; c += 32) {
+            if (c >= cols) break;
+            if (cols - c < 32) {
 #pragma unroll
-            for (int j = 0; j < kHalf; ++j)
-                if (j == t) hit = v[j];
-            prm.hit[w * prm.tokens_padded + row] = hit;
+                for (int j = c; j < c + 32; ++j)
+                    if (j >= cols) v[j] = -INFINITY;
+            }
+#pragma unroll
+            for (int j = c; j < c + 32; ++j) top = fmaxf(top, v[j]);
         }
+        const float at = top == -INFINITY ? 0.0f : top * kLog2e;
 #pragma unroll
-        for (int j = 0; j < kHalf; ++j) sum += exp2_fast(fmaf(v[j], kLog2e, -at));
-        prm.part[((int64_t)w * prm.stat_tiles + (prm.v0 + n0) / kStatCols) * prm.tokens_padded + row] = make_float2(top, sum);
+        for (int c = 0; c < kHalf; c += 32) {
+            if (c >= cols) break;
+            if (t >= c && t < min(c + 32, cols)) {
+                float hit = 0.0f;
+#pragma unroll
+                for (int j = c; j < c + 32; ++j)
+                    if (j == t) hit = v[j];
+                prm.hit[w * prm.tokens_padded + row] = hit;
+            }
+#pragma unroll
+            for (int j = c; j < c + 32; ++j) sum += exp2_fast(fmaf(v[j], kLog2e, -at));
+        }
+        prm.part[((int64_t)w * prm.stat_tiles + (prm.v0 + n0) / prm.stat_cols) * prm.tokens_padded + row] = make_float2(top, sum);
     } else if constexpr (WHICH == Product::kDlogits) {
         const bool in = row < count;
-        const float2 info = in ? prm.info[w * prm.tokens_padded + row] : make_float2(0.0f, 0.0f);
-        const int t = in ? prm.target[w * prm.tokens_padded + row] - prm.v0 - n0 : -1;
-        const int64_t at_dl = ((int64_t)w * PLANES * prm.tokens_padded + row) * prm.piece + n0;
-        const float at = info.x * kLog2e;
+        const int t = info.target;
+        // the product with dl over the tokens reads whole blocks of them: zeros behind the last one
+        const bool read = row < (count + kDepth - 1) / kDepth * kDepth;
+        const int64_t at_dl = read ? ((int64_t)w * PLANES * prm.tokens_padded + row) * prm.piece + n0 : -1;
+        const float at = info.info.x * kLog2e;
 #pragma unroll
-        for (int j = 0; j < kHalf; ++j) {
-            const float p = exp2_fast(fmaf(v[j], kLog2e, -at)) - (j == t ? 1.0f : 0.0f);
-            v[j] = in && j < cols ? info.y * p : 0.0f;
+        for (int c = 0; c < kHalf; c += 32) {
+            if (c >= width) break;
+#pragma unroll
+            for (int j = c; j < c + 32; ++j) {
+                const float p = exp2_fast(fmaf(v[j], kLog2e, -at)) - (j == t ? 1.0f : 0.0f);
+                v[j] = in && j < cols ? info.info.y * p : 0.0f;
+            }
         }
         if constexpr (PLANES == 1) {
-            store_rows<false, true>(stage, v, prm.dl, at_dl, kHalf, true);
+            store_rows<false, true>(stage, v, prm.dl, at_dl, width, true);
         } else {
-            store_parts(stage, v, prm.dl, prm.tokens_padded * prm.piece, at_dl);
+            store_parts(stage, v, prm.dl, prm.tokens_padded * prm.piece, at_dl, width);
         }
     } else {
         constexpr bool kHidden = WHICH == Product::kDhidden;
@@ -381,10 +422,9 @@ __device__ __forceinline__ void epilogue(const ProductParams& prm, int w, int sp
                 store_rows<false, true>(stage, v, prm.parts, at, width, true);
             return;
         }
-        const float g = prm.scale != nullptr ? prm.scale[w] : 1.0f;
-        const int64_t at = !in ? -1 : w * prm.out_worker + (kHidden ? (int64_t)prm.rows[w * prm.tokens + row] : (int64_t)row) * prm.out_row + n0;
+        const int64_t at = info.at;
 #pragma unroll
-        for (int j = 0; j < kHalf; ++j) v[j] *= g;
+        for (int j = 0; j < kHalf; ++j) v[j] *= info.scale;
         if constexpr (PLANES == 3)
             store_rows<false, false>(stage, v, static_cast<float*>(prm.out), at, cols, wide);
         else
@@ -426,20 +466,30 @@ __global__ void __launch_bounds__(kThreads, 1)
         asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.a) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.b) : "memory");
     }
-    // Columns of a tile.  Where they are a width that 256 does not divide, the tiles are made as narrow as their number allows (650
-    // columns: three of 224 instead of 256), as a tile's products take time by its columns.
-    const int tile_n = WHICH == Product::kDhidden || WHICH == Product::kDweight ? prm.tile_cols : kTileN, half_n = tile_n / 2;
+    const int tile_n = prm.tile_cols, half_n = tile_n / 2;
     const int n_tiles = (prm.n + tile_n - 1) / tile_n;
     after_the_kernel_before();
     if (warp == 2) {
-        // tiles of each worker: where the tokens are rows, only those that hold a token that takes part
+        // tiles of each worker (a lane to a worker): where the tokens are rows, only those that hold a token that takes part
         int total = 0;
-        for (int w = 0; w < prm.workers; ++w) {
-            const int rows = WHICH != Product::kDweight && prm.count != nullptr ? prm.count[w] : prm.m;
-            if (lane == 0) control.start[w] = total;
-            total += (rows + kTileM - 1) / kTileM * n_tiles;
+        for (int w0 = 0; w0 < prm.workers; w0 += 32) {
+            const int w = w0 + lane;
+            int count = 0, tiles = 0;
+            if (w < prm.workers) {
+                count = prm.count != nullptr ? __ldg(prm.count + w) : (WHICH == Product::kDweight ? prm.k : prm.m);
+                tiles = ((WHICH == Product::kDweight ? prm.m : count) + kTileM - 1) / kTileM * n_tiles;
+                control.count[w] = count;
+            }
+            int upto = tiles;
+#pragma unroll
+            for (int s = 1; s < 32; s *= 2) {
+                const int n = __shfl_up_sync(0xFFFFFFFFu, upto, s);
+                if (lane >= s) upto += n;
+            }
+            if (w < prm.workers) control.start[w + 1] = total + upto;
+            total += __shfl_sync(0xFFFFFFFFu, upto, 31);
         }
-        if (lane == 0) control.start[prm.workers] = total;
+        if (lane == 0) control.start[0] = 0;
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
@@ -463,7 +513,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         // columns of a row of tiles, for dl's sake
         const int m = kRowsFirst ? tile % m_tiles : tile / n_tiles, n = kRowsFirst ? tile / m_tiles : tile % n_tiles;
         t.m0 = m * kTileM, t.n0 = n * tile_n;
-        t.count = prm.count != nullptr ? prm.count[t.w] : (WHICH == Product::kDweight ? prm.k : prm.m);
+        t.count = control.count[t.w];
         const int k = WHICH == Product::kDweight ? t.count : prm.k;
         const int depth = (k + kDepth - 1) / kDepth, run = (depth + prm.splits - 1) / prm.splits;
         t.first = t.split * run;
@@ -487,7 +537,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     if (!fine) break;
                     const int kb = PLANES == 1 ? i : i / 3, plane = i - kb * PLANES, k0 = (t.first + kb) * kDepth;
                     const uint32_t bar = in_first_cta(smem_addr(&control.full[stage]));
-                    if (rank == 0) mbar_arrive_expect_tx(smem_addr(&control.full[stage]), kBOther && half_n <= 64 ? 2 * kStageBytes - kOperandBytes : 2 * kStageBytes);
+                    if (rank == 0) mbar_arrive_expect_tx(smem_addr(&control.full[stage]), 2 * (kOperandBytes + (kBOther ? (half_n > 64 ? kOperandBytes : kOperandBytes / 2) : half_n * kDepth * 2)));
                     const uint32_t a = base + stage * kStageBytes, b = a + kOperandBytes;
                     if (kAOther) {
                         load_box(a, &maps.a, m0, k0, plane, wa, bar);
@@ -576,6 +626,10 @@ __global__ void __launch_bounds__(kThreads, 1)
         int made = 0;
         for (int tile = blockIdx.x / 2; tile < total && fine; tile += pairs) {
             const Tile t = tile_at(tile);
+            const int row = t.m0 + (int)rank * 128 + quarter * 32 + lane, n0 = t.n0 + half * half_n;
+            const RowInfo info = row_info<WHICH>(prm, t.w, row, n0, t.count);
+            // a warp none of whose rows is wanted only keeps step
+            const bool idle = t.m0 + (int)rank * 128 + quarter * 32 >= (WHICH == Product::kDweight ? prm.m : WHICH == Product::kDlogits ? (t.count + kDepth - 1) / kDepth * kDepth : t.count);
             float v[kHalf];
             if (t.blocks == 0) {
 #pragma unroll
@@ -586,14 +640,14 @@ __global__ void __launch_bounds__(kThreads, 1)
                 fine = __all_sync(0xFFFFFFFFu, wait(smem_addr(&control.sum_full[buffer]), made >> 1 & 1));
                 if (!fine) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                take_sums(v, tensor_memory + ((uint32_t)(quarter * 32) << 16) + buffer * kTileN + half * half_n, kb > 0);
+                if (!idle) take_sums(v, tensor_memory + ((uint32_t)(quarter * 32) << 16) + buffer * kTileN + half * half_n, kb > 0);
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) arrive_cluster(in_first_cta(smem_addr(&control.sum_empty[buffer])));
                 ++made;
             }
             if (!fine) break;
-            epilogue<WHICH, PLANES>(prm, t.w, t.split, t.m0 + (int)rank * 128 + quarter * 32 + lane, t.n0 + half * half_n, half_n, t.count, v, wide, control.staging[warp - 2]);
+            if (!idle) epilogue<WHICH, PLANES>(prm, t.w, t.split, row, n0, half_n, t.count, info, v, wide, control.staging[warp - 2]);
         }
     }
     if (!fine && lane == 0) atomicExch(&g_gave_up, 1);
@@ -634,38 +688,43 @@ cudaError_t launch(const ProductParams& prm, cudaStream_t stream)
     ProductParams p = prm;
     if (p.k == 0) {  // nothing is read: the kernel writes zeros
         p.count = nullptr;
-    } else if (!encode_operand(&maps.a, p.a, p.planes, p.workers, a_other ? 64 : 128) || !encode_operand(&maps.b, p.b, p.planes, p.workers, b_other ? 64 : 128)) {
+    } else if (!encode_operand(&maps.a, p.a, p.planes, p.workers, a_other ? 64 : 128) || !encode_operand(&maps.b, p.b, p.planes, p.workers, b_other ? 64 : p.tile_cols / 2)) {
         return cudaErrorInvalidValue;
     }
     if (p.splits < 1) p.splits = 1;
-    p.tile_cols = (int)round_up(ceil_div(p.n, ceil_div(p.n, kTileN)), 32);
-    const int64_t tiles = product_tiles(p.m, p.n, p.workers) * p.splits;
+    const int64_t tiles = ceil_div(p.m, kTileM) * ceil_div(p.n, p.tile_cols) * p.workers * p.splits;
     const int pairs = (int)(tiles < sms / 2 ? tiles : sms / 2);
     return launch_after(rps_product_kernel<WHICH, PLANES>, dim3(2 * pairs), kThreads, kSharedBytes, stream, 2, p, maps);
 }
 
 }  // namespace
 
-int64_t product_tiles(int64_t m, int64_t n, int workers) { return ceil_div(m, kTileM) * ceil_div(n, kTileN) * workers; }
-
-int64_t product_blocks(int64_t k) { return ceil_div(k, kDepth); }
-
-// A product with fewer tiles than the 74 pairs and a long summed axis is cut, so that all pairs work.  In microseconds: a block takes a
-// pair 0.27 (the six products of parts of fp32: 1.6) and a tile's end 1; a part's 256 KB written and read 0.1, the launch that joins
-// them 5.  (48 tiles of 157 fp32 blocks: 312 us whole, 222 + 10 in three runs.  From 74 tiles on cutting only evens the last
-// round out, and the board's power, not the idle pairs, bounds it: 120 tiles of 1024 bf16 blocks took 745 us whole, 740 + 15 in three.)
-int product_splits(int64_t tiles, int64_t blocks, int planes)
+// A product with fewer tiles than the 74 pairs and a long summed axis is cut along it, so that all pairs work.  In microseconds: a block
+// takes a pair 0.27 (the six products of parts of fp32: 1.6) and a tile's end 1; a part's 256 KB written and read 0.1, the launch
+// that joins them 5.  (48 tiles of 157 fp32 blocks: 312 us whole, 222 + 10 in three runs.  From 74 tiles on cutting only evens the
+// last round out, and the board's power, not the idle pairs, bounds it: 120 tiles of 1024 bf16 blocks took 745 us whole, 740 + 15
+// in three.)
+//
+// The tiles' columns are a multiple of 32.  A width that 256 does not divide is cut as narrow as the number of its tiles allows (650
+// columns: three of 224 instead of 256), as a tile's products take time by its columns; and where the summed axis is not cut, as
+// long as twice the tiles still find an idle pair each, down to 64 columns, since a small call waits for one tile's copies and
+// its end.  (4 workers of 32 tokens, 1000
+// words, 256 columns: the four products of a step 39 us with tiles of 256, 32 us with 128 and 64.)
+ProductShape product_shape(int64_t m, int64_t n, int64_t k, int workers, int planes, bool may_split)
 {
     constexpr int64_t kPairs = 148 / 2;
+    const int64_t others = ceil_div(m > 0 ? m : 1, kTileM) * workers, blocks = ceil_div(k, kDepth);
+    int64_t across = ceil_div(n, kTileN);
     const double block = planes == 1 ? 0.27 : 1.6;
     int best = 1;
     double least = 0.0;
-    for (int s = 1; s <= 32 && (s == 1 || (tiles < kPairs && s * 4 <= blocks)); ++s) {
-        const double rounds = (double)ceil_div(tiles * s, kPairs);
-        const double cost = rounds * ((double)ceil_div(blocks, s) * block + 1.0) + (s > 1 ? 5.0 + 0.1 * (double)(tiles * s) : 0.0);
+    for (int s = 1; s <= 32 && (s == 1 || (may_split && across * others < kPairs && s * 4 <= blocks)); ++s) {
+        const int64_t items = across * others * s;
+        const double cost = (double)ceil_div(items, kPairs) * ((double)ceil_div(blocks, s) * block + 1.0) + (s > 1 ? 5.0 + 0.1 * (double)items : 0.0);
         if (s == 1 || cost < least) best = s, least = cost;
     }
-    return best;
+    while (best == 1 && across * 2 * others <= kPairs && n / (across * 2) >= 64) across *= 2;
+    return {(int)round_up(ceil_div(n, across), 32), best};
 }
 
 namespace {
