@@ -71,7 +71,7 @@ typedef struct rps_lce_desc {
     int64_t ignore_index;
     int64_t hidden_row, hidden_worker;   /* strides of hidden; hidden_row >= cols                        */
     int64_t weight_row, weight_worker;   /* strides of weight; weight_row >= cols                        */
-    int64_t dweight_row, dweight_worker; /* strides of dweight (backward only); dweight_row >= cols      */
+    int64_t dweight_row, dweight_worker; /* strides of dweight (backward only); cols <= dweight_row < 2^31 */
 } rps_lce_desc;
 
 /* Bytes of workspace that rps_lce_forward (backward = 0) or rps_lce_backward (backward = 1) wants.  Of the weight only
@@ -165,7 +165,7 @@ typedef struct rps_wgrad_desc {
     int32_t n;               /* workers, 1..RPS_MAX_WORKERS                           */
     int64_t tokens;          /* 0 <= tokens < 2^24                                    */
     int64_t outs, cols;      /* 1..2^24-1                                             */
-    int64_t dy_row, dy_worker, dweight_row, dweight_worker; /* strides; rows >= outs and >= cols */
+    int64_t dy_row, dy_worker, dweight_row, dweight_worker; /* strides; rows >= outs and >= cols, dweight_row < 2^31 */
 } rps_wgrad_desc;
 
 /* Of dy only the address counts. */

@@ -191,7 +191,7 @@ __global__ void __launch_bounds__(kMergeThreads) rps_lce_merge_kernel(const LceP
     };
     if (i < count) {
         const float2* part = prm.part + w * prm.stat_tiles * prm.tokens_padded + i;
-        constexpr int kAtATime = 4;
+        constexpr int kAtATime = 8;
         for (int64_t v = warp; v < prm.stat_tiles; v += kWarps * kAtATime) {
             float2 p[kAtATime];
 #pragma unroll

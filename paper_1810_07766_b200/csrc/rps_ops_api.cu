@@ -63,6 +63,7 @@ constexpr int64_t kMaxSize = (1ll << 24) - 1;
 int check_output_strides(const char* name, int n, int64_t rows, int64_t cols, int64_t row, int64_t worker)
 {
     if (row < cols) return fail(RPS_EINVAL, "%s: a row stride of %lld is less than the %lld columns", name, (long long)row, (long long)cols);
+    if (row >= 1ll << 31) return fail(RPS_EINVAL, "%s: a row stride of %lld", name, (long long)row);
     if (n > 1 && worker < (rows - 1) * row + cols && (worker < cols || row < (n - 1) * worker + cols))
         return fail(RPS_EINVAL, "%s: the workers' parts overlap (worker stride %lld)", name, (long long)worker);
     return RPS_OK;
@@ -131,8 +132,7 @@ LcePlan plan_lce(const rps_lce_desc& d, const void* weight, bool backward, void*
     ProductParams& g = plan.product;
     // in several pieces the tiles are whole, so that the pieces' statistics lie side by side
     g.tile_cols = plan.piece < whole ? kVocabTile : product_shape(d.tokens, d.vocab, d.cols, d.n, p.planes, false).tile_cols;
-    g.stat_cols = g.tile_cols / 2;
-    p.stat_tiles = ceil_div(d.vocab, g.stat_cols);
+    p.stat_tiles = ceil_div(d.vocab, g.tile_cols);
 
     Carver c{static_cast<unsigned char*>(workspace)};
     p.count = c.take<int>(p.n);

@@ -57,7 +57,7 @@ struct ProductParams {
     const int* count;   // [worker] tokens that take part, or NULL: all
     // kLse, kDlogits
     int v0, vocab;          // first row of the vocabulary in this piece; all of it
-    int stat_cols, stat_tiles;  // softmax statistics are kept for every stat_cols (half a tile's) columns
+    int stat_tiles;         // softmax statistics are kept for every tile's columns
     const int* target;      // [worker][tokens_padded]
     float2* part;           // [worker][stat_tiles][tokens_padded]: running maximum and sum
     float* hit;             // [worker][tokens_padded]: the target's logit
@@ -73,6 +73,7 @@ struct ProductParams {
     // The summed axis may be cut into `splits` runs of blocks, each with its own part [split][worker][part_rows][part_row]; over several
     // pieces of the vocabulary a part goes on growing (`add`).
     int splits, tile_cols;        // product_shape
+    int a_rows;                   // rows of A that a CTA copies (launch_product's to set)
     int add;
     float* parts;
     int64_t part_rows, part_row;  // multiples of the tile

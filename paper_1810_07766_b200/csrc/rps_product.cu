@@ -5,9 +5,11 @@
 // result in fp32.  Tensor memory has room for two tiles, so the epilogue of one runs under the products of the next.  The
 // pairs are persistent and take the tiles round robin.
 //
-// Roles in a CTA: warp 0 copies (TMA boxes of 64 columns, 128-byte swizzle, a ring of kStages), warp 1 issues the products
-// (first CTA only) and owns the tensor memory, warps 2..9 are the epilogue: two for each quarter of the 128 rows, each with
-// half of the columns, a row to a lane, so that a row's softmax statistics need no exchange between lanes.
+// Roles in a CTA: warp 0 copies (TMA boxes of 64 columns, 128-byte swizzle, a ring of 6 to 24 stages), warp 1 issues the products
+// (first CTA only) and owns the tensor memory, the others are the epilogue, a row to a lane, so that a row's softmax statistics need
+// no exchange between lanes.  bf16 operands have 16 such warps of 64 columns, which work on 32 columns at a time straight out of tensor
+// memory; fp32 operands 8 of 128 columns, held in registers while their segments (below) are added.  (With 8 warps of 128 columns
+// in registers for bf16, too few to issue while another waits, a tile's end took XXX us where it is all there is.)
 //
 // Operands are read as they lie in memory: with the summed axis contiguous, or (dl and W in dH = dl W, dl and H in dW = dl^T H) with
 // the other one contiguous, which the descriptors of the shared-memory tiles express; nothing is transposed.
@@ -15,6 +17,7 @@
 // fp32 operands are three bf16 parts each (24 significant bits); of the nine products of parts the six that reach 2^-24
 // of the result are made.  The three parts of a block lie in three stages of the ring, so each is copied once for its three products.
 #include <mutex>
+#include <type_traits>
 
 #include "rps_ops_kernels.h"
 #include "rps_tma.cuh"
@@ -27,12 +30,17 @@ using rps::mbar_init;
 using rps::smem_addr;
 
 constexpr int kTileM = 256, kTileN = 256, kDepth = 64;  // of a pair (kTileN at most); 64 bf16 are one 128-byte swizzled line
-constexpr int kHalf = kTileN / 2;  // columns of a warp of the epilogue, at most
-constexpr int kStages = 6;
-constexpr int kOperandBytes = 128 * kDepth * 2;  // one operand's part of a stage in one CTA
-constexpr int kStageBytes = 2 * kOperandBytes;
-constexpr int kEpilogueWarps = 8;
-constexpr int kThreads = 32 * (2 + kEpilogueWarps);
+constexpr int kOperandBytes = 128 * kDepth * 2;  // one operand's part of a stage in one CTA, at most
+constexpr int kRingBytes = 6 * 2 * kOperandBytes;
+constexpr int kMostStages = 24;                  // of narrower tiles and fewer rows more stages fit
+// Warps of the epilogue: two (fp32) or four (bf16) for each quarter of a CTA's 128 rows.
+template <int PLANES>
+struct Epilogue {
+    static constexpr int kParts = PLANES == 3 ? 2 : 4;
+    static constexpr int kWarps = 4 * kParts, kThreads = 32 * (2 + kWarps);
+    static constexpr int kCols = kTileN / kParts;  // of a warp, at most
+};
+constexpr int kMostEpilogueWarps = Epilogue<1>::kWarps;
 // The tensor cores cut an fp32 sum off after each step of 16 instead of rounding it, a bias that grows with the number of steps
 // (relative error of a 512-long sum of random terms: 5e-7).  Where fp32 accuracy is asked for, the summed axis goes
 // through in segments whose sums the epilogue adds in fp32, rounded: every 2 blocks of fp32 operands (48 steps), and every 16 blocks (64
@@ -49,18 +57,26 @@ static_assert(kTileM == kTokenTile && kTileN == kVocabTile, "operands are padded
 // element by element, still in the order of memory.  (Gradient of 8 fp32 weights of 10001 x 650, rows of 2600 bytes: 453 -> 225 us.)
 struct Staging {
     uint4 part[32][4];
+};
+struct StagingWithOffsets : Staging {  // fp32, whose 8 warps leave room for the rows' offsets; bf16 makes them anew from the rows' numbers
     int64_t at[32];
 };
 
 struct Control {
-    Staging staging[kEpilogueWarps];
-    uint64_t full[kStages], empty[kStages], sum_full[2], sum_empty[2];
+    union {
+        Staging staging[kMostEpilogueWarps];
+        StagingWithOffsets staging_f32[Epilogue<3>::kWarps];
+    };
+    uint64_t full[kMostStages], empty[kMostStages], sum_full[2], sum_empty[2];
+    uint64_t statistics[4][4];  // kLse, of each quarter of the rows and four tiles in turn: the warps' parts are there
     uint32_t tensor_memory;
     int count[RPS_MAX_WORKERS];      // tokens of each worker that take part
     int start[RPS_MAX_WORKERS + 1];  // first tile of each worker
 };
 
-constexpr int kSharedBytes = 1024 + kStages * kStageBytes + (int)sizeof(Control);
+constexpr int kSharedBytes = 1024 + kRingBytes + (int)sizeof(Control);
+// The products read 128 rows of A whatever part of them a stage holds; behind the last stage lies Control.
+static_assert(sizeof(Control) >= kOperandBytes, "reads past the ring stay in shared memory");
 
 // Set when a bounded wait gave up (rps_ops_check).
 __device__ int g_gave_up = 0;
@@ -90,9 +106,11 @@ __device__ __forceinline__ uint32_t in_first_cta(uint32_t addr)
     return r;
 }
 
+// Says that tensor memory has been read.  Relaxed: what has to come before it are the loads of tensor memory, which
+// tcgen05.fence::before_thread_sync orders; a release would wait for the stores of the tile before as well (4.6 -> XXX us a tile of stores).
 __device__ __forceinline__ void arrive_cluster(uint32_t bar)
 {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
 // Waits for the phase with the given parity; what the pair did before it is then visible.  Gives up after kWaitNs.
@@ -173,19 +191,20 @@ __device__ __forceinline__ void load_sums(float* v, uint32_t addr)
         : "memory");
 }
 
-// 128 columns of this lane's row: taken over, or added to those of the segments before.  (Of a narrower tile the last ones are whatever
+// COLS columns of this lane's row: taken over, or added to those of the segments before.  (Of a narrower tile the last ones are whatever
 // tensor memory holds; they are not stored.)
-__device__ __forceinline__ void take_sums(float (&v)[kHalf], uint32_t addr, bool add)
+template <int COLS>
+__device__ __forceinline__ void take_sums(float (&v)[COLS], uint32_t addr, bool add)
 {
     __syncwarp();
     if (!add) {
 #pragma unroll
-        for (int c = 0; c < kHalf; c += 16) load_sums(v + c, addr + c);
+        for (int c = 0; c < COLS; c += 16) load_sums(v + c, addr + c);
         asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
         return;
     }
 #pragma unroll
-    for (int c = 0; c < kHalf; c += 16) {
+    for (int c = 0; c < COLS; c += 16) {
         float r[16];
         load_sums(r, addr + c);
         asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
@@ -213,9 +232,42 @@ __device__ __forceinline__ uint32_t two_bf16(float lo, float hi)
 __device__ __forceinline__ void store_element(float* to, float e) { __stcg(to, e); }
 __device__ __forceinline__ void store_element(bf16* to, bf16 e) { __stcg(reinterpret_cast<unsigned short*>(to), __bfloat16_as_ushort(e)); }
 
+// Where a warp's rows go: lane's row `index` (-1: not written) of rows `stride` apart, from `out` on, which is this warp's first column.
+template <typename T>
+struct Rows {
+    T* out;
+    int stride;
+    int index;
+    int cols;   // that exist
+    bool wide;  // rows are 16-byte aligned
+};
+
+// Offset of row r of the warp, -1 if it is not written; all lanes ask.
+template <typename T>
+__device__ __forceinline__ int64_t row_offset(const Staging&, const Rows<T>& to, int r)
+{
+    const int index = __shfl_sync(0xFFFFFFFFu, to.index, r);
+    return index < 0 ? -1 : (int64_t)index * to.stride;
+}
+template <typename T>
+__device__ __forceinline__ int64_t row_offset(const StagingWithOffsets& stage, const Rows<T>&, int r)
+{
+    return stage.at[r];
+}
+template <typename T>
+__device__ __forceinline__ void set_offsets(Staging&, const Rows<T>&)
+{
+}
+template <typename T>
+__device__ __forceinline__ void set_offsets(StagingWithOffsets& stage, const Rows<T>& to)
+{
+    __syncwarp();
+    stage.at[threadIdx.x % 32] = to.index < 0 ? -1 : (int64_t)to.index * to.stride;
+}
+
 // 64 bytes of each of the warp's rows, from column `c` on.  Loads come before stores, several at a time.  ADD, WHOLE: see store_rows.
-template <bool ADD, bool WHOLE, typename T>
-__device__ __forceinline__ void store_chunk(Staging& stage, const uint4 (&mine)[4], T* out, int c, int cols, bool wide)
+template <bool ADD, bool WHOLE, typename T, typename Stage>
+__device__ __forceinline__ void store_chunk(Stage& stage, const uint4 (&mine)[4], const Rows<T>& to, int c)
 {
     constexpr int kChunk = 64 / sizeof(T), kPart = 16 / sizeof(T);  // columns
     const int lane = threadIdx.x % 32;
@@ -223,21 +275,21 @@ __device__ __forceinline__ void store_chunk(Staging& stage, const uint4 (&mine)[
 #pragma unroll
     for (int q = 0; q < 4; ++q) stage.part[lane][q ^ (lane >> 1 & 3)] = mine[q];
     __syncwarp();
-    if (WHOLE || wide) {
+    if (WHOLE || to.wide) {
         const int col = c + lane % 4 * kPart;
         uint4 word[4];
-        int64_t at[4];
+        int64_t row[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int r = lane / 4 + 8 * i;
             word[i] = stage.part[r][lane % 4 ^ (r >> 1 & 3)];
-            at[i] = stage.at[r];
+            row[i] = row_offset(stage, to, r);
         }
-        if (col >= cols) return;
+        if (col >= to.cols) return;
         if constexpr (ADD) {
             float4 old[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) old[i] = at[i] < 0 ? make_float4(0, 0, 0, 0) : __ldcg(reinterpret_cast<const float4*>(out + at[i] + col));
+            for (int i = 0; i < 4; ++i) old[i] = row[i] < 0 ? make_float4(0, 0, 0, 0) : __ldcg(reinterpret_cast<const float4*>(to.out + row[i] + col));
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 word[i] = make_uint4(__float_as_uint(__uint_as_float(word[i].x) + old[i].x), __float_as_uint(__uint_as_float(word[i].y) + old[i].y),
@@ -245,49 +297,47 @@ __device__ __forceinline__ void store_chunk(Staging& stage, const uint4 (&mine)[
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            if (at[i] < 0) continue;
-            T* to = out + at[i] + col;
-            if (WHOLE || col + kPart <= cols) {
-                __stcg(reinterpret_cast<uint4*>(to), word[i]);
+            if (row[i] < 0) continue;
+            T* at = to.out + row[i] + col;
+            if (WHOLE || col + kPart <= to.cols) {
+                __stcg(reinterpret_cast<uint4*>(at), word[i]);
             } else {
                 const T* e = reinterpret_cast<const T*>(&word[i]);
 #pragma unroll
                 for (int k = 0; k < kPart; ++k)
-                    if (col + k < cols) store_element(to + k, e[k]);
+                    if (col + k < to.cols) store_element(at + k, e[k]);
             }
         }
     } else {
         constexpr int kRows = 32 / kChunk, kAtATime = 8;  // rows that the warp writes at a time, an element to a lane: 2 of fp32, 1 of bf16
         const int col = lane % kChunk;
-        const bool there = c + col < cols;
+        const bool there = c + col < to.cols;
 #pragma unroll 1
         for (int r0 = 0; r0 < 32; r0 += kRows * kAtATime) {
             T e[kAtATime];
-            int64_t at[kAtATime];
+            int64_t row[kAtATime];
 #pragma unroll
             for (int i = 0; i < kAtATime; ++i) {
                 const int r = r0 + i * kRows + lane / kChunk;
-                at[i] = stage.at[r];
+                row[i] = row_offset(stage, to, r);
                 e[i] = reinterpret_cast<const T*>(&stage.part[r][col / kPart ^ (r >> 1 & 3)])[col % kPart];
             }
 #pragma unroll
             for (int i = 0; i < kAtATime; ++i)
-                if (at[i] >= 0 && there) store_element(out + at[i] + c + col, e[i]);
+                if (row[i] >= 0 && there) store_element(to.out + row[i] + c + col, e[i]);
         }
     }
 }
 
-// `at`: offset of this lane's row in `out`, or -1 if it is not to be written; `cols` of the 128 columns exist.  WHOLE: rows are 16-byte
-// aligned and `cols` a multiple of 16 bytes.  ADD: to what is there (fp32, WHOLE).
-template <bool ADD, bool WHOLE, typename T>
-__device__ __forceinline__ void store_rows(Staging& stage, const float (&v)[kHalf], T* out, int64_t at, int cols, bool wide)
+// The warp's rows.  WHOLE: they are 16-byte aligned and `cols` a multiple of 16 bytes.  ADD: to what is there (fp32, WHOLE).
+template <bool ADD, bool WHOLE, typename T, int COLS, typename Stage>
+__device__ __forceinline__ void store_rows(Stage& stage, const float (&v)[COLS], const Rows<T>& to)
 {
     constexpr int kChunk = 64 / sizeof(T), kPart = 16 / sizeof(T);
-    __syncwarp();
-    stage.at[threadIdx.x % 32] = at;
+    set_offsets(stage, to);
 #pragma unroll
-    for (int c = 0; c < kHalf; c += kChunk) {
-        if (c >= cols) break;
+    for (int c = 0; c < COLS; c += kChunk) {
+        if (c >= to.cols) break;
         uint4 mine[4];
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
@@ -297,20 +347,21 @@ __device__ __forceinline__ void store_rows(Staging& stage, const float (&v)[kHal
             else
                 mine[q] = make_uint4(two_bf16(f[0], f[1]), two_bf16(f[2], f[3]), two_bf16(f[4], f[5]), two_bf16(f[6], f[7]));
         }
-        store_chunk<ADD, WHOLE>(stage, mine, out, c, cols, wide);
+        store_chunk<ADD, WHOLE>(stage, mine, to, c);
     }
 }
 
 // fp32 values as three planes of bf16 parts.
-__device__ __forceinline__ void store_parts(Staging& stage, float (&v)[kHalf], bf16* out, int64_t plane, int64_t at, int cols)
+template <int COLS, typename Stage>
+__device__ __forceinline__ void store_parts(Stage& stage, float (&v)[COLS], Rows<bf16> to, int64_t plane)
 {
-    __syncwarp();
-    stage.at[threadIdx.x % 32] = at;
+    set_offsets(stage, to);
 #pragma unroll
-    for (int c = 0; c < kHalf; c += 32) {
-        if (c >= cols) break;
+    for (int c = 0; c < COLS; c += 32) {
+        if (c >= to.cols) break;
+        Rows<bf16> part_to = to;
 #pragma unroll
-        for (int q = 0; q < 3; ++q) {
+        for (int q = 0; q < 3; ++q, part_to.out += plane) {
             uint4 mine[4];
             uint32_t* word = reinterpret_cast<uint32_t*>(mine);
 #pragma unroll
@@ -324,7 +375,7 @@ __device__ __forceinline__ void store_parts(Staging& stage, float (&v)[kHalf], b
                 }
                 word[j / 2] = two_bf16(part[0], part[1]);
             }
-            store_chunk<false, true>(stage, mine, out + q * plane, c, cols, true);
+            store_chunk<false, true>(stage, mine, part_to, c);
         }
     }
 }
@@ -333,7 +384,7 @@ __device__ __forceinline__ void store_parts(Staging& stage, float (&v)[kHalf], b
 struct RowInfo {
     int target;   // kLse, kDlogits: less the first column of this warp
     float2 info;  // kDlogits: lse and g
-    int64_t at;   // kDhidden, kDweight: offset of the row in `out`, -1 if it is not to be written
+    int index;    // of the row where it is stored, -1 if it is not
     float scale;
 };
 
@@ -345,96 +396,117 @@ __device__ __forceinline__ RowInfo row_info(const ProductParams& prm, int w, int
     if constexpr (WHICH == Product::kLse || WHICH == Product::kDlogits) {
         r.target = in ? __ldg(prm.target + w * prm.tokens_padded + row) - prm.v0 - n0 : -1;
         if (WHICH == Product::kDlogits && in) r.info = __ldg(prm.info + w * prm.tokens_padded + row);
+        // the product with dl over the tokens reads whole blocks of them: zeros behind the last one
+        r.index = row < (count + kDepth - 1) / kDepth * kDepth ? row : -1;
     } else {
-        r.at = -1;
-        if (in && prm.parts == nullptr) r.at = w * prm.out_worker + (WHICH == Product::kDhidden ? (int64_t)__ldg(prm.rows + w * prm.tokens + row) : (int64_t)row) * prm.out_row + n0;
+        r.index = !in ? -1 : WHICH == Product::kDhidden && prm.parts == nullptr ? __ldg(prm.rows + w * prm.tokens + row) : row;
         r.scale = prm.scale != nullptr ? __ldg(prm.scale + w) : 1.0f;
     }
     return r;
 }
 
-// One row's 128 columns of a tile.
-template <Product WHICH, int PLANES>
-__device__ __forceinline__ void epilogue(const ProductParams& prm, int w, int split, int row, int n0, int width, int count, const RowInfo& info, float (&v)[kHalf], bool wide, Staging& stage)
+// kLse: a warp's columns of one row of a tile, `width` of them.  `turn`: tiles that the warp has had.  False if a wait gave up.
+template <int PLANES, int COLS>
+__device__ __forceinline__ bool statistics(const ProductParams& prm, int w, int row, int n0, int width, int count, const RowInfo& info, float (&v)[COLS],
+                                           Control& control, int quarter, int part, int turn)
+{
+    constexpr int kParts = Epilogue<PLANES>::kParts;
+    const int cols = min(width, prm.n - n0);
+    // in runs of 32 columns, as a narrow tile has fewer
+    const int t = info.target;
+    float top = -INFINITY, sum = 0.0f;
+#pragma unroll
+    for (int c = 0; c < COLS; c += 32) {
+        if (c >= cols) break;
+        if (cols - c < 32) {
+#pragma unroll
+            for (int j = c; j < c + 32; ++j)
+                if (j >= cols) v[j] = -INFINITY;
+        }
+#pragma unroll
+        for (int j = c; j < c + 32; ++j) top = fmaxf(top, v[j]);
+    }
+    const float at = top == -INFINITY ? 0.0f : top * kLog2e;
+#pragma unroll
+    for (int c = 0; c < COLS; c += 32) {
+        if (c >= cols) break;
+        if (t >= c && t < min(c + 32, cols)) {
+            float hit = 0.0f;
+#pragma unroll
+            for (int j = c; j < c + 32; ++j)
+                if (j == t) hit = v[j];
+            prm.hit[w * prm.tokens_padded + row] = hit;
+        }
+#pragma unroll
+        for (int j = c; j < c + 32; ++j) sum += exp2_fast(fmaf(v[j], kLog2e, -at));
+    }
+    // The warps of these rows put theirs together.  There is room for four tiles' in turn, as none of them can be more than two tiles
+    // ahead of another: tensor memory holds two.
+    static_assert(sizeof(control.staging) >= 4 * kParts * 128 * sizeof(float2), "unused here otherwise");
+    float2* row_statistics = reinterpret_cast<float2*>(control.staging) + (turn & 3) * kParts * 128;
+    const uint32_t there = smem_addr(&control.statistics[quarter][turn & 3]);
+    const int lane = threadIdx.x % 32, r = quarter * 32 + lane;
+    row_statistics[part * 128 + r] = make_float2(top, sum);
+    __syncwarp();
+    if (lane == 0) rps::mbar_arrive(there);
+    if (part != 0) return true;
+    if (!__all_sync(0xFFFFFFFFu, wait(there, turn >> 2 & 1))) return false;
+    if (row >= count) return true;
+    for (int k = 1; k < kParts; ++k) {
+        const float2 p = row_statistics[k * 128 + r];
+        const float m = fmaxf(top, p.x), from = m == -INFINITY ? 0.0f : m * kLog2e;
+        sum = fmaf(sum, exp2_fast(fmaf(top, kLog2e, -from)), p.y * exp2_fast(fmaf(p.x, kLog2e, -from)));
+        top = m;
+    }
+    prm.part[((int64_t)w * prm.stat_tiles + (prm.v0 + n0) / prm.tile_cols) * prm.tokens_padded + row] = make_float2(top, sum);
+    return true;
+}
+
+// The other products: columns n0.. of one row of a tile, `width` (at most COLS) of them.
+template <Product WHICH, int PLANES, int COLS, typename Stage>
+__device__ __forceinline__ void store_columns(const ProductParams& prm, int w, int split, int row, int n0, int width, int count, int target,
+                                              const RowInfo& info, float (&v)[COLS], bool wide, Stage& stage)
 {
     const int cols = min(width, prm.n - n0);
-    if (cols <= 0 && WHICH != Product::kDlogits) return;
-    if constexpr (WHICH == Product::kLse) {
-        // in runs of 32 columns, as a narrow tile has fewer
-        if (row >= count) return;
-        const int t = info.target;
-        float top = -INFINITY, sum = 0.0f;
-#pragma unroll
-        for (int c = 0; c < kHalf; c += 32) {
-            if (c >= cols) break;
-            if (cols - c < 32) {
-#pragma unroll
-                for (int j = c; j < c + 32; ++j)
-                    if (j >= cols) v[j] = -INFINITY;
-            }
-#pragma unroll
-            for (int j = c; j < c + 32; ++j) top = fmaxf(top, v[j]);
-        }
-        const float at = top == -INFINITY ? 0.0f : top * kLog2e;
-#pragma unroll
-        for (int c = 0; c < kHalf; c += 32) {
-            if (c >= cols) break;
-            if (t >= c && t < min(c + 32, cols)) {
-                float hit = 0.0f;
-#pragma unroll
-                for (int j = c; j < c + 32; ++j)
-                    if (j == t) hit = v[j];
-                prm.hit[w * prm.tokens_padded + row] = hit;
-            }
-#pragma unroll
-            for (int j = c; j < c + 32; ++j) sum += exp2_fast(fmaf(v[j], kLog2e, -at));
-        }
-        prm.part[((int64_t)w * prm.stat_tiles + (prm.v0 + n0) / prm.stat_cols) * prm.tokens_padded + row] = make_float2(top, sum);
-    } else if constexpr (WHICH == Product::kDlogits) {
+    if constexpr (WHICH == Product::kDlogits) {
         const bool in = row < count;
-        const int t = info.target;
-        // the product with dl over the tokens reads whole blocks of them: zeros behind the last one
-        const bool read = row < (count + kDepth - 1) / kDepth * kDepth;
-        const int64_t at_dl = read ? ((int64_t)w * PLANES * prm.tokens_padded + row) * prm.piece + n0 : -1;
         const float at = info.info.x * kLog2e;
 #pragma unroll
-        for (int c = 0; c < kHalf; c += 32) {
+        for (int c = 0; c < COLS; c += 32) {
             if (c >= width) break;
 #pragma unroll
             for (int j = c; j < c + 32; ++j) {
-                const float p = exp2_fast(fmaf(v[j], kLog2e, -at)) - (j == t ? 1.0f : 0.0f);
+                const float p = exp2_fast(fmaf(v[j], kLog2e, -at)) - (j == target ? 1.0f : 0.0f);
                 v[j] = in && j < cols ? info.info.y * p : 0.0f;
             }
         }
-        if constexpr (PLANES == 1) {
-            store_rows<false, true>(stage, v, prm.dl, at_dl, width, true);
-        } else {
-            store_parts(stage, v, prm.dl, prm.tokens_padded * prm.piece, at_dl, width);
-        }
+        const int64_t plane = prm.tokens_padded * prm.piece;
+        const Rows<bf16> to{prm.dl + w * PLANES * plane + n0, (int)prm.piece, info.index, width, true};
+        if constexpr (PLANES == 1)
+            store_rows<false, true>(stage, v, to);
+        else
+            store_parts(stage, v, to, plane);
     } else {
-        constexpr bool kHidden = WHICH == Product::kDhidden;
-        const bool in = row < (kHidden ? count : prm.m);
+        if (cols <= 0) return;
         if (prm.parts != nullptr) {
-            const int64_t at = in ? (((int64_t)split * prm.workers + w) * prm.part_rows + row) * prm.part_row + n0 : -1;
+            const Rows<float> to{prm.parts + ((int64_t)split * prm.workers + w) * prm.part_rows * prm.part_row + n0, (int)prm.part_row, info.index, width,
+                                 true};
             if (prm.add)
-                store_rows<true, true>(stage, v, prm.parts, at, width, true);
+                store_rows<true, true>(stage, v, to);
             else
-                store_rows<false, true>(stage, v, prm.parts, at, width, true);
+                store_rows<false, true>(stage, v, to);
             return;
         }
-        const int64_t at = info.at;
 #pragma unroll
-        for (int j = 0; j < kHalf; ++j) v[j] *= info.scale;
-        if constexpr (PLANES == 3)
-            store_rows<false, false>(stage, v, static_cast<float*>(prm.out), at, cols, wide);
-        else
-            store_rows<false, false>(stage, v, static_cast<bf16*>(prm.out), at, cols, wide);
+        for (int j = 0; j < COLS; ++j) v[j] *= info.scale;
+        using T = std::conditional_t<PLANES == 3, float, bf16>;
+        store_rows<false, false>(stage, v, Rows<T>{static_cast<T*>(prm.out) + w * prm.out_worker + n0, (int)prm.out_row, info.index, cols, wide});
     }
 }
 
 // ------------------------------------------------------------------------------------------------------------ kernel
 template <Product WHICH, int PLANES>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(Epilogue<PLANES>::kThreads, 1)
     rps_product_kernel(const __grid_constant__ ProductParams prm, const __grid_constant__ Maps maps)
 {
     constexpr bool kAOther = WHICH == Product::kDweight;                                  // A's rows are contiguous, not the summed axis
@@ -442,20 +514,21 @@ __global__ void __launch_bounds__(kThreads, 1)
     constexpr bool kRowsFirst = WHICH != Product::kDweight;                               // order of the tiles: see below
     extern __shared__ unsigned char raw[];
     const uint32_t base = (smem_addr(raw) + 1023) / 1024 * 1024;
-    unsigned char* const stages = raw + (base - smem_addr(raw));
-    Control& control = *reinterpret_cast<Control*>(stages + kStages * kStageBytes);
+    unsigned char* const ring = raw + (base - smem_addr(raw));
+    Control& control = *reinterpret_cast<Control*>(ring + kRingBytes);
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const uint32_t rank = cluster_rank();
 
     if (warp == 0 && lane == 0) {
-        for (int s = 0; s < kStages; ++s) {
+        for (int s = 0; s < kMostStages; ++s) {
             mbar_init(smem_addr(&control.full[s]), 1);
             mbar_init(smem_addr(&control.empty[s]), 1);
         }
         for (int s = 0; s < 2; ++s) {
             mbar_init(smem_addr(&control.sum_full[s]), 1);
-            mbar_init(smem_addr(&control.sum_empty[s]), 2 * kEpilogueWarps);
+            mbar_init(smem_addr(&control.sum_empty[s]), 2 * Epilogue<PLANES>::kWarps);
         }
+        for (int s = 0; s < 16; ++s) mbar_init(smem_addr(&control.statistics[s / 4][s % 4]), Epilogue<PLANES>::kParts);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) {
@@ -468,6 +541,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     const int tile_n = prm.tile_cols, half_n = tile_n / 2;
     const int n_tiles = (prm.n + tile_n - 1) / tile_n;
+    const uint32_t a_bytes = prm.a_rows * kDepth * 2, b_bytes = kBOther ? (half_n > 64 ? kOperandBytes : kOperandBytes / 2) : half_n * kDepth * 2;
+    const int stages = min(kMostStages, (int)(kRingBytes / (a_bytes + b_bytes)));
     after_the_kernel_before();
     if (warp == 2) {
         // tiles of each worker (a lane to a worker): where the tokens are rows, only those that hold a token that takes part
@@ -532,39 +607,48 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const Tile t = tile_at(tile);
                 const int m0 = t.m0 + rank * 128, n0 = t.n0 + rank * half_n;
                 const int wa = prm.a.worker != 0 ? t.w : 0, wb = prm.b.worker != 0 ? t.w : 0;
+                // a CTA's part that holds no row or column of the result is not copied: what the products read in its place reaches
+                // only results that are not stored
+                const int rows = WHICH == Product::kDweight ? prm.m : t.count;
+                const bool copy_a = m0 < rows, copy_b = n0 < prm.n;
+                const uint32_t bytes = (t.m0 + 128 < rows ? 2 : 1) * a_bytes + (t.n0 + half_n < prm.n ? 2 : 1) * b_bytes;
                 for (int i = 0; i < t.blocks * PLANES; ++i) {
                     fine = wait(smem_addr(&control.empty[stage]), phase ^ 1);
                     if (!fine) break;
                     const int kb = PLANES == 1 ? i : i / 3, plane = i - kb * PLANES, k0 = (t.first + kb) * kDepth;
                     const uint32_t bar = in_first_cta(smem_addr(&control.full[stage]));
-                    if (rank == 0) mbar_arrive_expect_tx(smem_addr(&control.full[stage]), 2 * (kOperandBytes + (kBOther ? (half_n > 64 ? kOperandBytes : kOperandBytes / 2) : half_n * kDepth * 2)));
-                    const uint32_t a = base + stage * kStageBytes, b = a + kOperandBytes;
-                    if (kAOther) {
-                        load_box(a, &maps.a, m0, k0, plane, wa, bar);
-                        load_box(a + kOperandBytes / 2, &maps.a, m0 + 64, k0, plane, wa, bar);
-                    } else {
-                        load_box(a, &maps.a, k0, m0, plane, wa, bar);
+                    if (rank == 0) mbar_arrive_expect_tx(smem_addr(&control.full[stage]), bytes);
+                    const uint32_t a = base + stage * (a_bytes + b_bytes), b = a + a_bytes;
+                    if (copy_a) {
+                        if (kAOther) {
+                            load_box(a, &maps.a, m0, k0, plane, wa, bar);
+                            load_box(a + kOperandBytes / 2, &maps.a, m0 + 64, k0, plane, wa, bar);
+                        } else {
+                            load_box(a, &maps.a, k0, m0, plane, wa, bar);
+                        }
                     }
-                    if (kBOther) {
-                        load_box(b, &maps.b, n0, k0, plane, wb, bar);
-                        if (half_n > 64) load_box(b + kOperandBytes / 2, &maps.b, n0 + 64, k0, plane, wb, bar);
-                    } else {
-                        load_box(b, &maps.b, k0, n0, plane, wb, bar);
+                    if (copy_b) {
+                        if (kBOther) {
+                            load_box(b, &maps.b, n0, k0, plane, wb, bar);
+                            if (half_n > 64) load_box(b + kOperandBytes / 2, &maps.b, n0 + 64, k0, plane, wb, bar);
+                        } else {
+                            load_box(b, &maps.b, k0, n0, plane, wb, bar);
+                        }
                     }
                     ++issued;
-                    if (++stage == kStages) stage = 0, phase ^= 1;
+                    if (++stage == stages) stage = 0, phase ^= 1;
                 }
             }
             if (fine) {
                 // the pair's arrivals on this CTA's barriers: all have come before it may end
-                for (int i = 0; i < kStages && fine; ++i) {
+                for (int i = 0; i < stages && fine; ++i) {
                     fine = wait(smem_addr(&control.empty[stage]), phase ^ 1);
-                    if (++stage == kStages) stage = 0, phase ^= 1;
+                    if (++stage == stages) stage = 0, phase ^= 1;
                 }
             } else if (rank == 0) {
-                // copies still on their way when a wait gave up: the last kStages of them at most
-                for (int i = issued > kStages ? issued - kStages : 0; i < issued; ++i)
-                    wait(smem_addr(&control.full[i % kStages]), i / kStages & 1);
+                // copies still on their way when a wait gave up: those of the last round of the ring at most
+                for (int i = issued > stages ? issued - stages : 0; i < issued; ++i)
+                    wait(smem_addr(&control.full[i % stages]), i / stages & 1);
             }
         }
     } else if (warp == 1) {
@@ -589,30 +673,27 @@ __global__ void __launch_bounds__(kThreads, 1)
                                      tile_descriptor(b + k * b_step, kBOther ? kOperandBytes / 2 : 16, 1024), descriptor, add || k > 0);
                     };
                     for (; kb < end; ++kb) {
-                        uint32_t at[PLANES];
-                        int s = stage;
-                        uint32_t ph = phase;
+                        uint32_t at[PLANES], freed[PLANES];
 #pragma unroll
                         for (int q = 0; q < PLANES; ++q) {
-                            fine = fine && wait(smem_addr(&control.full[s]), ph);
-                            at[q] = base + s * kStageBytes;
-                            if (++s == kStages) s = 0, ph ^= 1;
+                            fine = fine && wait(smem_addr(&control.full[stage]), phase);
+                            at[q] = base + stage * (a_bytes + b_bytes), freed[q] = smem_addr(&control.empty[stage]);
+                            if (++stage == stages) stage = 0, phase ^= 1;
                         }
                         if (!fine) break;
                         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                         if constexpr (PLANES == 1) {
-                            block(at[0], at[0] + kOperandBytes, kb > begin);
+                            block(at[0], at[0] + a_bytes, kb > begin);
                         } else {  // parts of A and B, the smallest products first
-                            block(at[2], at[0] + kOperandBytes, kb > begin);
-                            block(at[0], at[2] + kOperandBytes, true);
-                            block(at[1], at[1] + kOperandBytes, true);
-                            block(at[1], at[0] + kOperandBytes, true);
-                            block(at[0], at[1] + kOperandBytes, true);
-                            block(at[0], at[0] + kOperandBytes, true);
+                            block(at[2], at[0] + a_bytes, kb > begin);
+                            block(at[0], at[2] + a_bytes, true);
+                            block(at[1], at[1] + a_bytes, true);
+                            block(at[1], at[0] + a_bytes, true);
+                            block(at[0], at[1] + a_bytes, true);
+                            block(at[0], at[0] + a_bytes, true);
                         }
 #pragma unroll
-                        for (int q = 0; q < PLANES; ++q) commit_to_pair(smem_addr(&control.empty[(at[q] - base) / kStageBytes]));
-                        stage = s, phase = ph;
+                        for (int q = 0; q < PLANES; ++q) commit_to_pair(freed[q]);
                     }
                     if (!fine) break;
                     commit_to_pair(smem_addr(&control.sum_full[buffer]));
@@ -621,33 +702,62 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
         }
     } else {
-        const int quarter = warp % 4, half = (warp - 2) / 4;
+        constexpr int kCols = Epilogue<PLANES>::kCols;
+        const int quarter = warp % 4, part = (warp - 2) / 4, part_n = tile_n / Epilogue<PLANES>::kParts;
         const bool wide = (reinterpret_cast<uintptr_t>(prm.out) | (prm.out_row | prm.out_worker) * (PLANES == 3 ? 4 : 2)) % 16 == 0;
-        int made = 0;
+        int made = 0, turn = 0;
+        const auto summed = [&] {
+            fine = __all_sync(0xFFFFFFFFu, wait(smem_addr(&control.sum_full[made & 1]), made >> 1 & 1));
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            return fine;
+        };
+        const auto taken = [&] {
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) arrive_cluster(in_first_cta(smem_addr(&control.sum_empty[made & 1])));
+            ++made;
+        };
         for (int tile = blockIdx.x / 2; tile < total && fine; tile += pairs) {
             const Tile t = tile_at(tile);
-            const int row = t.m0 + (int)rank * 128 + quarter * 32 + lane, n0 = t.n0 + half * half_n;
+            const int row = t.m0 + (int)rank * 128 + quarter * 32 + lane, n0 = t.n0 + part * part_n;
             const RowInfo info = row_info<WHICH>(prm, t.w, row, n0, t.count);
             // a warp none of whose rows is wanted only keeps step
             const bool idle = t.m0 + (int)rank * 128 + quarter * 32 >= (WHICH == Product::kDweight ? prm.m : WHICH == Product::kDlogits ? (t.count + kDepth - 1) / kDepth * kDepth : t.count);
-            float v[kHalf];
-            if (t.blocks == 0) {
+            const uint32_t columns = tensor_memory + ((uint32_t)(quarter * 32) << 16) + part * part_n;
+            if constexpr (PLANES == 1 && WHICH != Product::kLse) {  // one segment
+                if (t.blocks > 0 && !summed()) break;
+#pragma unroll 1
+                for (int c = 0; c < part_n && !idle; c += 32) {
+                    float v[32];
+                    if (t.blocks > 0) {
+                        take_sums(v, columns + (made & 1) * kTileN + c, false);
+                        if (c + 32 >= part_n) taken();
+                    } else {
 #pragma unroll
-                for (int j = 0; j < kHalf; ++j) v[j] = 0.0f;
-            }
-            for (int kb = 0; kb < t.blocks; kb = min(kb + segment, t.blocks)) {
-                const int buffer = made & 1;
-                fine = __all_sync(0xFFFFFFFFu, wait(smem_addr(&control.sum_full[buffer]), made >> 1 & 1));
+                        for (int j = 0; j < 32; ++j) v[j] = 0.0f;
+                    }
+                    store_columns<WHICH, PLANES>(prm, t.w, t.split, row, n0 + c, min(32, part_n - c), t.count, info.target - c, info, v, wide,
+                                                 control.staging[warp - 2]);
+                }
+                if (t.blocks > 0 && idle) taken();
+            } else {
+                float v[kCols];
+                if (t.blocks == 0) {
+#pragma unroll
+                    for (int j = 0; j < kCols; ++j) v[j] = 0.0f;
+                }
+                for (int kb = 0; kb < t.blocks; kb = min(kb + segment, t.blocks)) {
+                    if (!summed()) break;
+                    if (!idle) take_sums(v, columns + (made & 1) * kTileN, kb > 0);
+                    taken();
+                }
                 if (!fine) break;
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                if (!idle) take_sums(v, tensor_memory + ((uint32_t)(quarter * 32) << 16) + buffer * kTileN + half * half_n, kb > 0);
-                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) arrive_cluster(in_first_cta(smem_addr(&control.sum_empty[buffer])));
-                ++made;
+                if (idle) continue;
+                if constexpr (WHICH == Product::kLse)
+                    fine = statistics<PLANES>(prm, t.w, row, n0, part_n, t.count, info, v, control, quarter, part, turn++);
+                else
+                    store_columns<WHICH, PLANES>(prm, t.w, t.split, row, n0, part_n, t.count, info.target, info, v, wide, control.staging_f32[warp - 2]);
             }
-            if (!fine) break;
-            if (!idle) epilogue<WHICH, PLANES>(prm, t.w, t.split, row, n0, half_n, t.count, info, v, wide, control.staging[warp - 2]);
         }
     }
     if (!fine && lane == 0) atomicExch(&g_gave_up, 1);
@@ -686,15 +796,16 @@ cudaError_t launch(const ProductParams& prm, cudaStream_t stream)
     Maps maps{};
     constexpr bool a_other = WHICH == Product::kDweight, b_other = WHICH == Product::kDweight || WHICH == Product::kDhidden;
     ProductParams p = prm;
+    if (p.splits < 1) p.splits = 1;
+    p.a_rows = a_other || p.m > 128 ? 128 : (int)round_up(p.m, 8);
     if (p.k == 0) {  // nothing is read: the kernel writes zeros
         p.count = nullptr;
-    } else if (!encode_operand(&maps.a, p.a, p.planes, p.workers, a_other ? 64 : 128) || !encode_operand(&maps.b, p.b, p.planes, p.workers, b_other ? 64 : p.tile_cols / 2)) {
+    } else if (!encode_operand(&maps.a, p.a, p.planes, p.workers, a_other ? 64 : p.a_rows) || !encode_operand(&maps.b, p.b, p.planes, p.workers, b_other ? 64 : p.tile_cols / 2)) {
         return cudaErrorInvalidValue;
     }
-    if (p.splits < 1) p.splits = 1;
     const int64_t tiles = ceil_div(p.m, kTileM) * ceil_div(p.n, p.tile_cols) * p.workers * p.splits;
     const int pairs = (int)(tiles < sms / 2 ? tiles : sms / 2);
-    return launch_after(rps_product_kernel<WHICH, PLANES>, dim3(2 * pairs), kThreads, kSharedBytes, stream, 2, p, maps);
+    return launch_after(rps_product_kernel<WHICH, PLANES>, dim3(2 * pairs), Epilogue<PLANES>::kThreads, kSharedBytes, stream, 2, p, maps);
 }
 
 }  // namespace

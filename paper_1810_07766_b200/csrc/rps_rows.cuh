@@ -42,8 +42,8 @@ __device__ __forceinline__ uint4 load_slice(const T* row, int c, int cols)
         for (int j = 0; j < 4; ++j) r[j] = c + j * kPer < cols ? __ldg(reinterpret_cast<const uint32_t*>(row + c + j * kPer)) : 0u;
         return make_uint4(r[0], r[1], r[2], r[3]);
     } else {
-        uint32_t r[4] = {};
         const unsigned short* half = reinterpret_cast<const unsigned short*>(row);
+        uint32_t r[4] = {};
 #pragma unroll
         for (int j = 0; j < 8; ++j)
             if (c + j < cols) r[j / 2] |= (uint32_t)__ldg(half + c + j) << (j % 2 * 16);
