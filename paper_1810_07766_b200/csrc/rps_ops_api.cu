@@ -131,7 +131,8 @@ LcePlan plan_lce(const rps_lce_desc& d, const void* weight, bool backward, void*
     if (plan.lay_out_weight) narrow(p.n * p.planes * p.cols_padded * 2);
     ProductParams& g = plan.product;
     // in several pieces the tiles are whole, so that the pieces' statistics lie side by side
-    g.tile_cols = plan.piece < whole ? kVocabTile : product_shape(d.tokens, d.vocab, d.cols, d.n, p.planes, false).tile_cols;
+    g.shaped(product_shape(d.tokens, d.vocab, d.cols, d.n, p.planes, false));
+    if (plan.piece < whole) g.tile_cols = kVocabTile;
     p.stat_tiles = ceil_div(d.vocab, g.tile_cols);
 
     Carver c{static_cast<unsigned char*>(workspace)};
@@ -272,14 +273,14 @@ extern "C" int rps_lce_backward(const rps_lce_desc* desc, const void* hidden, co
         if (d.tokens > 0) {
             g.a = h, g.b = weight_rows, g.m = (int)d.tokens, g.n = (int)rows, g.k = (int)d.cols;
             RPS_TRY(launch_product(Product::kDlogits, g, stream));
-            g.a = dl, g.n = (int)d.cols, g.k = (int)rows, g.tile_cols = plan.hidden_shape.tile_cols;
-            g.splits = plan.hidden_shape.splits, g.parts = plan.hidden_parts, g.part_rows = p.tokens_padded, g.add = v0 > 0;
+            g.a = dl, g.n = (int)d.cols, g.k = (int)rows, g.shaped(plan.hidden_shape);
+            g.parts = plan.hidden_parts, g.part_rows = p.tokens_padded, g.add = v0 > 0;
             g.out = dhidden, g.out_row = d.cols, g.out_worker = d.tokens * d.cols;
             RPS_TRY(launch_product(Product::kDhidden, g, stream));
             if (g.parts != nullptr && v0 + rows == d.vocab) RPS_TRY(launch_join(Product::kDhidden, g, stream));
         }
-        g.a = dl, g.b = h, g.m = (int)rows, g.n = (int)d.cols, g.k = (int)d.tokens, g.tile_cols = plan.weight_shape.tile_cols;
-        g.splits = plan.weight_shape.splits, g.parts = plan.weight_parts, g.part_rows = plan.piece, g.add = 0;
+        g.a = dl, g.b = h, g.m = (int)rows, g.n = (int)d.cols, g.k = (int)d.tokens, g.shaped(plan.weight_shape);
+        g.parts = plan.weight_parts, g.part_rows = plan.piece, g.add = 0;
         g.out = static_cast<unsigned char*>(dweight) + v0 * d.dweight_row * (p.f32 ? 4 : 2), g.out_row = d.dweight_row, g.out_worker = d.dweight_worker;
         RPS_TRY(launch_product(Product::kDweight, g, stream));
         if (g.parts != nullptr) RPS_TRY(launch_join(Product::kDweight, g, stream));
@@ -512,9 +513,9 @@ extern "C" int rps_packed_wgrad(const rps_wgrad_desc* desc, const void* dy, cons
     }
     ProductParams g{};
     g.a = plan.dy, g.b = plan.x, g.workers = d.n, g.planes = d.dtype == RPS_F32 ? 3 : 1;
-    g.m = (int)d.outs, g.n = (int)d.cols, g.k = (int)d.tokens, g.tile_cols = plan.shape.tile_cols;
+    g.m = (int)d.outs, g.n = (int)d.cols, g.k = (int)d.tokens, g.shaped(plan.shape);
     g.out = dweight, g.out_row = d.dweight_row, g.out_worker = d.dweight_worker;
-    g.splits = plan.shape.splits, g.parts = plan.parts, g.part_rows = round_up(d.outs, kVocabTile), g.part_row = round_up(d.cols, kVocabTile);
+    g.parts = plan.parts, g.part_rows = round_up(d.outs, kVocabTile), g.part_row = round_up(d.cols, kVocabTile);
     RPS_TRY(launch_product(Product::kDweight, g, stream));
     if (g.parts != nullptr) RPS_TRY(launch_join(Product::kDweight, g, stream));
     return RPS_OK;

@@ -50,6 +50,11 @@ enum class Product {
     kDweight   // A = dl or dy [k][m], B = hidden or x [k][n]
 };
 
+// How a product is cut: columns of its tiles, runs of its summed axis, and CTAs that make a tile (1 or 2).
+struct ProductShape {
+    int tile_cols, splits, ctas;
+};
+
 struct ProductParams {
     Operand a, b;
     int workers, planes;  // three planes: fp32 operands and results, one: bf16
@@ -72,17 +77,14 @@ struct ProductParams {
     int64_t tokens;
     // The summed axis may be cut into `splits` runs of blocks, each with its own part [split][worker][part_rows][part_row]; over several
     // pieces of the vocabulary a part goes on growing (`add`).
-    int splits, tile_cols;        // product_shape
+    int splits, tile_cols, ctas;  // product_shape
+    void shaped(const ProductShape& s) { tile_cols = s.tile_cols, splits = s.splits, ctas = s.ctas; }
     int a_rows;                   // rows of A that a CTA copies (launch_product's to set)
     int add;
     float* parts;
     int64_t part_rows, part_row;  // multiples of the tile
 };
 
-// How a product is cut: columns of its tiles, and runs of its summed axis.
-struct ProductShape {
-    int tile_cols, splits;
-};
 ProductShape product_shape(int64_t m, int64_t n, int64_t k, int workers, int planes, bool may_split);
 
 cudaError_t launch_product(Product which, const ProductParams& prm, cudaStream_t stream);

@@ -1,6 +1,6 @@
 // Matrix products of the training operators on the tensor cores, with their epilogues.
 //
-// A pair of CTAs (a cluster of two, on neighbouring SMs) makes one 256 x 256 tile: each CTA stages 128 rows of A and half of B's 256
+// A pair of CTAs (a cluster of two, on neighbouring SMs) makes one 256 x 256 tile (or, product_shape, a CTA alone one of 128 x 256): each CTA stages 128 rows of A and half of B's 256
 // columns, one thread of the first CTA issues the pair's tcgen05.mma, and each CTA's tensor memory holds its 128 rows of the
 // result in fp32.  Tensor memory has room for two tiles, so the epilogue of one runs under the products of the next.  The
 // pairs are persistent and take the tiles round robin.
@@ -29,8 +29,9 @@ using rps::mbar_arrive_expect_tx;
 using rps::mbar_init;
 using rps::smem_addr;
 
-constexpr int kTileM = 256, kTileN = 256, kDepth = 64;  // of a pair (kTileN at most); 64 bf16 are one 128-byte swizzled line
-constexpr int kOperandBytes = 128 * kDepth * 2;  // one operand's part of a stage in one CTA, at most
+constexpr int kTileN = 256, kDepth = 64;  // columns of a tile at most, and of the summed axis at a time; 64 bf16 are one 128-byte swizzled line
+constexpr int kOperandBytes = 128 * kDepth * 2;  // 128 rows of an operand in a stage
+constexpr int kBoxBytes = 64 * kDepth * 2;       // 64 columns of an operand whose summed axis is not the contiguous one
 constexpr int kRingBytes = 6 * 2 * kOperandBytes;
 constexpr int kMostStages = 24;                  // of narrower tiles and fewer rows more stages fit
 // Warps of the epilogue: two (fp32) or four (bf16) for each quarter of a CTA's 128 rows.
@@ -49,7 +50,7 @@ constexpr int kMostEpilogueWarps = Epilogue<1>::kWarps;
 constexpr int kSegmentF32 = 2, kSegmentStatistics = 16;  // in blocks of kDepth
 constexpr uint64_t kWaitNs = 2000000000ull;
 
-static_assert(kTileM == kTokenTile && kTileN == kVocabTile, "operands are padded to whole tiles");
+static_assert(kTileN == kVocabTile && kTokenTile % 256 == 0, "operands are padded to whole tiles");
 
 // Rows leave through shared memory: a lane holds one row, and 32 lanes writing 16 bytes of 32 rows each would touch 32 lines at a time and
 // half a sector of each.  Instead 64 bytes of each of the warp's 32 rows are laid down (parts of 16 bytes, exchanged by the row's
@@ -138,46 +139,86 @@ __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity)
 }
 
 // One box into this CTA's shared memory; its bytes are counted on the first CTA's barrier.
+template <int CTAS>
 __device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, int x, int y, int plane, int worker, uint32_t bar)
 {
-    asm volatile(
-        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3, %4, "
-        "%5}], [%6];" ::"r"(dst),
-        "l"(map), "r"(x), "r"(y), "r"(plane), "r"(worker), "r"(bar)
-        : "memory");
+    if constexpr (CTAS == 2)
+        asm volatile(
+            "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3, %4, "
+            "%5}], [%6];" ::"r"(dst),
+            "l"(map), "r"(x), "r"(y), "r"(plane), "r"(worker), "r"(bar)
+            : "memory");
+    else
+        asm volatile(
+            "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
+            "l"(map), "r"(x), "r"(y), "r"(plane), "r"(worker), "r"(bar)
+            : "memory");
 }
 
-// Descriptor of a shared-memory tile with the 128-byte swizzle: start address and the two strides in units of 16 bytes, the
-// constant 1 at bit 46, layout 2 (128-byte swizzle) at bit 61.  Summed axis contiguous: `stride` leads from 8 rows to the
-// next 8.  Other axis contiguous: `stride` leads from 8 steps of the summed axis to the next 8, `lead` from one 64-wide box to the next.
-__device__ __forceinline__ uint64_t tile_descriptor(uint32_t addr, uint32_t lead, uint32_t stride)
+// Descriptor of a shared-memory tile with the 128-byte swizzle: start address and two strides in units of 16 bytes, the constant 1 at
+// bit 46, layout 2 (128-byte swizzle) at bit 61.  Summed axis contiguous: the stride at bit 32 leads from 8 rows to the next 8.
+// Other axis contiguous: it leads from 8 steps of the summed axis to the next 8, and the one at bit 16 from one 64-wide box to the
+// next.  The upper word is the same for all, and in the lower one tiles and their parts lie a constant apart.
+constexpr uint32_t kDescriptorHigh = 1024 / 16 | 1u << 14 | 2u << 29;
+
+__device__ __forceinline__ uint32_t descriptor_low(uint32_t addr, bool other) { return addr >> 4 | (uint32_t)(other ? kBoxBytes / 16 : 1) << 16; }
+
+// fp32 sums of bf16 products, rows x tile_n.
+__device__ __forceinline__ uint32_t instruction_descriptor(bool a_other, bool b_other, int rows, int tile_n)
 {
-    return (uint64_t)((addr >> 4) & 0x3FFF) | (uint64_t)((lead >> 4) & 0x3FFF) << 16 | (uint64_t)((stride >> 4) & 0x3FFF) << 32 | 1ull << 46 |
-           2ull << 61;
+    return 1u << 4 | 1u << 7 | 1u << 10 | (a_other ? 1u : 0u) << 15 | (b_other ? 1u : 0u) << 16 | (uint32_t)(tile_n / 8) << 17 | (uint32_t)(rows / 16) << 24;
 }
 
-// fp32 sums of bf16 products, 256 x tile_n over the pair.
-__device__ __forceinline__ uint32_t instruction_descriptor(bool a_other, bool b_other, int tile_n)
+// `a`, `b`: lower words of the descriptors.
+template <int CTAS>
+__device__ __forceinline__ void multiply(uint32_t sum, uint32_t a, uint32_t b, uint32_t descriptor, bool add)
 {
-    return 1u << 4 | 1u << 7 | 1u << 10 | (a_other ? 1u : 0u) << 15 | (b_other ? 1u : 0u) << 16 | (uint32_t)(tile_n / 8) << 17 |
-           (uint32_t)(kTileM / 16) << 24;
+    if constexpr (CTAS == 2)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\tsetp.ne.u32 p, %5, 0;\n\tmov.b64 da, {%1, %3};\n\tmov.b64 db, {%2, %3};\n\t"
+            "tcgen05.mma.cta_group::2.kind::f16 [%0], da, db, %4, p;\n\t}" ::"r"(sum),
+            "r"(a), "r"(b), "n"(kDescriptorHigh), "r"(descriptor), "r"((uint32_t)add)
+            : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\tsetp.ne.u32 p, %5, 0;\n\tmov.b64 da, {%1, %3};\n\tmov.b64 db, {%2, %3};\n\t"
+            "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, p;\n\t}" ::"r"(sum),
+            "r"(a), "r"(b), "n"(kDescriptorHigh), "r"(descriptor), "r"((uint32_t)add)
+            : "memory");
 }
 
-__device__ __forceinline__ void multiply(uint32_t sum, uint64_t a, uint64_t b, uint32_t descriptor, bool add)
+// Arrives on the barrier at this offset (in both CTAs of a pair) once the products issued so far are done.
+template <int CTAS>
+__device__ __forceinline__ void commit(uint32_t bar)
 {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(sum),
-        "l"(a), "l"(b), "r"(descriptor), "r"((uint32_t)add)
-        : "memory");
+    if constexpr (CTAS == 2)
+        asm volatile(
+            "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3)
+            : "memory");
+    else
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
 
-// Arrives on the barrier at this offset in both CTAs once the products issued so far are done.
-__device__ __forceinline__ void commit_to_pair(uint32_t bar)
+// All 512 columns of tensor memory, for the whole kernel.
+template <int CTAS>
+__device__ __forceinline__ void take_tensor_memory(uint32_t address_to)
 {
-    asm volatile(
-        "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3)
-        : "memory");
+    if constexpr (CTAS == 2) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(address_to) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+    } else {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(address_to) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+}
+
+template <int CTAS>
+__device__ __forceinline__ void free_tensor_memory(uint32_t address)
+{
+    if constexpr (CTAS == 2)
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(address) : "memory");
+    else
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(address) : "memory");
 }
 
 // 16 columns of this lane's row.
@@ -194,7 +235,7 @@ __device__ __forceinline__ void load_sums(float* v, uint32_t addr)
 // COLS columns of this lane's row: taken over, or added to those of the segments before.  (Of a narrower tile the last ones are whatever
 // tensor memory holds; they are not stored.)
 template <int COLS>
-__device__ __forceinline__ void take_sums(float (&v)[COLS], uint32_t addr, bool add)
+__device__ __forceinline__ void take_sums(float (&v)[COLS], uint32_t addr, bool add, int width)
 {
     __syncwarp();
     if (!add) {
@@ -205,6 +246,7 @@ __device__ __forceinline__ void take_sums(float (&v)[COLS], uint32_t addr, bool 
     }
 #pragma unroll
     for (int c = 0; c < COLS; c += 16) {
+        if (c >= width) break;
         float r[16];
         load_sums(r, addr + c);
         asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
@@ -505,19 +547,20 @@ __device__ __forceinline__ void store_columns(const ProductParams& prm, int w, i
 }
 
 // ------------------------------------------------------------------------------------------------------------ kernel
-template <Product WHICH, int PLANES>
+template <Product WHICH, int PLANES, int CTAS>
 __global__ void __launch_bounds__(Epilogue<PLANES>::kThreads, 1)
     rps_product_kernel(const __grid_constant__ ProductParams prm, const __grid_constant__ Maps maps)
 {
     constexpr bool kAOther = WHICH == Product::kDweight;                                  // A's rows are contiguous, not the summed axis
     constexpr bool kBOther = WHICH == Product::kDweight || WHICH == Product::kDhidden;
     constexpr bool kRowsFirst = WHICH != Product::kDweight;                               // order of the tiles: see below
+    constexpr int kRows = 128 * CTAS;  // of a tile
     extern __shared__ unsigned char raw[];
     const uint32_t base = (smem_addr(raw) + 1023) / 1024 * 1024;
     unsigned char* const ring = raw + (base - smem_addr(raw));
     Control& control = *reinterpret_cast<Control*>(ring + kRingBytes);
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const uint32_t rank = cluster_rank();
+    const uint32_t rank = CTAS == 2 ? cluster_rank() : 0;
 
     if (warp == 0 && lane == 0) {
         for (int s = 0; s < kMostStages; ++s) {
@@ -526,22 +569,19 @@ __global__ void __launch_bounds__(Epilogue<PLANES>::kThreads, 1)
         }
         for (int s = 0; s < 2; ++s) {
             mbar_init(smem_addr(&control.sum_full[s]), 1);
-            mbar_init(smem_addr(&control.sum_empty[s]), 2 * Epilogue<PLANES>::kWarps);
+            mbar_init(smem_addr(&control.sum_empty[s]), CTAS * Epilogue<PLANES>::kWarps);
         }
         for (int s = 0; s < 16; ++s) mbar_init(smem_addr(&control.statistics[s / 4][s % 4]), Epilogue<PLANES>::kParts);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&control.tensor_memory)) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
-    }
+    if (warp == 1) take_tensor_memory<CTAS>(smem_addr(&control.tensor_memory));
     if (warp == 0 && lane == 0) {
         asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.a) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.b) : "memory");
     }
-    const int tile_n = prm.tile_cols, half_n = tile_n / 2;
+    const int tile_n = prm.tile_cols, own_n = tile_n / CTAS;  // columns of B that a CTA copies
     const int n_tiles = (prm.n + tile_n - 1) / tile_n;
-    const uint32_t a_bytes = prm.a_rows * kDepth * 2, b_bytes = kBOther ? (half_n > 64 ? kOperandBytes : kOperandBytes / 2) : half_n * kDepth * 2;
+    const uint32_t a_bytes = prm.a_rows * kDepth * 2, b_bytes = kBOther ? (own_n + 63) / 64 * (kBoxBytes) : own_n * kDepth * 2;
     const int stages = min(kMostStages, (int)(kRingBytes / (a_bytes + b_bytes)));
     after_the_kernel_before();
     if (warp == 2) {
@@ -552,7 +592,7 @@ __global__ void __launch_bounds__(Epilogue<PLANES>::kThreads, 1)
             int count = 0, tiles = 0;
             if (w < prm.workers) {
                 count = prm.count != nullptr ? __ldg(prm.count + w) : (WHICH == Product::kDweight ? prm.k : prm.m);
-                tiles = ((WHICH == Product::kDweight ? prm.m : count) + kTileM - 1) / kTileM * n_tiles;
+                tiles = ((WHICH == Product::kDweight ? prm.m : count) + kRows - 1) / kRows * n_tiles;
                 control.count[w] = count;
             }
             int upto = tiles;
@@ -568,11 +608,11 @@ __global__ void __launch_bounds__(Epilogue<PLANES>::kThreads, 1)
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
-    cluster_sync();
+    if constexpr (CTAS == 2) cluster_sync();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tensor_memory = control.tensor_memory;
 
-    const int tiles = control.start[prm.workers], pairs = gridDim.x / 2, total = tiles * prm.splits;
+    const int tiles = control.start[prm.workers], groups = gridDim.x / CTAS, total = tiles * prm.splits;
     struct Tile {
         int w, split, m0, n0, count, first, blocks;  // blocks of the summed axis: the first one and how many
     };
@@ -587,7 +627,7 @@ __global__ void __launch_bounds__(Epilogue<PLANES>::kThreads, 1)
         // kLse, kDlogits: all rows of a column of tiles before the next one, so that the weight is read from memory once; kDweight: all
         // columns of a row of tiles, for dl's sake
         const int m = kRowsFirst ? tile % m_tiles : tile / n_tiles, n = kRowsFirst ? tile / m_tiles : tile % n_tiles;
-        t.m0 = m * kTileM, t.n0 = n * tile_n;
+        t.m0 = m * kRows, t.n0 = n * tile_n;
         t.count = control.count[t.w];
         const int k = WHICH == Product::kDweight ? t.count : prm.k;
         const int depth = (k + kDepth - 1) / kDepth, run = (depth + prm.splits - 1) / prm.splits;
@@ -603,15 +643,15 @@ __global__ void __launch_bounds__(Epilogue<PLANES>::kThreads, 1)
         if (lane == 0) {
             int stage = 0, issued = 0;
             uint32_t phase = 0;
-            for (int tile = blockIdx.x / 2; tile < total && fine; tile += pairs) {
+            for (int tile = blockIdx.x / CTAS; tile < total && fine; tile += groups) {
                 const Tile t = tile_at(tile);
-                const int m0 = t.m0 + rank * 128, n0 = t.n0 + rank * half_n;
+                const int m0 = t.m0 + rank * 128, n0 = t.n0 + rank * own_n;
                 const int wa = prm.a.worker != 0 ? t.w : 0, wb = prm.b.worker != 0 ? t.w : 0;
                 // a CTA's part that holds no row or column of the result is not copied: what the products read in its place reaches
                 // only results that are not stored
                 const int rows = WHICH == Product::kDweight ? prm.m : t.count;
                 const bool copy_a = m0 < rows, copy_b = n0 < prm.n;
-                const uint32_t bytes = (t.m0 + 128 < rows ? 2 : 1) * a_bytes + (t.n0 + half_n < prm.n ? 2 : 1) * b_bytes;
+                const uint32_t bytes = (CTAS == 2 && t.m0 + 128 < rows ? 2 : 1) * a_bytes + (CTAS == 2 && t.n0 + own_n < prm.n ? 2 : 1) * b_bytes;
                 for (int i = 0; i < t.blocks * PLANES; ++i) {
                     fine = wait(smem_addr(&control.empty[stage]), phase ^ 1);
                     if (!fine) break;
@@ -621,18 +661,17 @@ __global__ void __launch_bounds__(Epilogue<PLANES>::kThreads, 1)
                     const uint32_t a = base + stage * (a_bytes + b_bytes), b = a + a_bytes;
                     if (copy_a) {
                         if (kAOther) {
-                            load_box(a, &maps.a, m0, k0, plane, wa, bar);
-                            load_box(a + kOperandBytes / 2, &maps.a, m0 + 64, k0, plane, wa, bar);
+                            load_box<CTAS>(a, &maps.a, m0, k0, plane, wa, bar);
+                            load_box<CTAS>(a + kBoxBytes, &maps.a, m0 + 64, k0, plane, wa, bar);
                         } else {
-                            load_box(a, &maps.a, k0, m0, plane, wa, bar);
+                            load_box<CTAS>(a, &maps.a, k0, m0, plane, wa, bar);
                         }
                     }
                     if (copy_b) {
                         if (kBOther) {
-                            load_box(b, &maps.b, n0, k0, plane, wb, bar);
-                            if (half_n > 64) load_box(b + kOperandBytes / 2, &maps.b, n0 + 64, k0, plane, wb, bar);
+                            for (int c = 0; c < own_n; c += 64) load_box<CTAS>(b + c / 64 * kBoxBytes, &maps.b, n0 + c, k0, plane, wb, bar);
                         } else {
-                            load_box(b, &maps.b, k0, n0, plane, wb, bar);
+                            load_box<CTAS>(b, &maps.b, k0, n0, plane, wb, bar);
                         }
                     }
                     ++issued;
@@ -653,12 +692,13 @@ __global__ void __launch_bounds__(Epilogue<PLANES>::kThreads, 1)
         }
     } else if (warp == 1) {
         if (rank == 0 && lane == 0) {
-            const uint32_t descriptor = instruction_descriptor(kAOther, kBOther, tile_n);
+            const uint32_t descriptor = instruction_descriptor(kAOther, kBOther, kRows, tile_n);
             // one product covers 16 of the summed axis: 32 bytes further along swizzled rows, or 16 rows of 128 bytes further
-            constexpr uint32_t a_step = kAOther ? 2048 : 32, b_step = kBOther ? 2048 : 32;
+            constexpr uint32_t a_step = (kAOther ? 2048 : 32) / 16, b_step = (kBOther ? 2048 : 32) / 16;
+            const uint32_t a_first = descriptor_low(base, kAOther), b_first = descriptor_low(base + a_bytes, kBOther), stage_step = (a_bytes + b_bytes) / 16;
             int stage = 0, made = 0;
             uint32_t phase = 0;
-            for (int tile = blockIdx.x / 2; tile < total && fine; tile += pairs) {
+            for (int tile = blockIdx.x / CTAS; tile < total && fine; tile += groups) {
                 const Tile t = tile_at(tile);
                 for (int kb = 0; kb < t.blocks && fine;) {
                     const int buffer = made & 1, begin = kb, end = min(kb + segment, t.blocks);
@@ -668,35 +708,34 @@ __global__ void __launch_bounds__(Epilogue<PLANES>::kThreads, 1)
                     const uint32_t sum = tensor_memory + buffer * kTileN;
                     const auto block = [&](uint32_t a, uint32_t b, bool add) {
 #pragma unroll
-                        for (int k = 0; k < kDepth / 16; ++k)
-                            multiply(sum, tile_descriptor(a + k * a_step, kAOther ? kOperandBytes / 2 : 16, 1024),
-                                     tile_descriptor(b + k * b_step, kBOther ? kOperandBytes / 2 : 16, 1024), descriptor, add || k > 0);
+                        for (int k = 0; k < kDepth / 16; ++k) multiply<CTAS>(sum, a + k * a_step, b + k * b_step, descriptor, add || k > 0);
                     };
                     for (; kb < end; ++kb) {
-                        uint32_t at[PLANES], freed[PLANES];
+                        uint32_t a[PLANES], b[PLANES], freed[PLANES];
 #pragma unroll
                         for (int q = 0; q < PLANES; ++q) {
                             fine = fine && wait(smem_addr(&control.full[stage]), phase);
-                            at[q] = base + stage * (a_bytes + b_bytes), freed[q] = smem_addr(&control.empty[stage]);
+                            a[q] = a_first + stage * stage_step, b[q] = b_first + stage * stage_step, freed[q] = smem_addr(&control.empty[stage]);
                             if (++stage == stages) stage = 0, phase ^= 1;
                         }
                         if (!fine) break;
                         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                         if constexpr (PLANES == 1) {
-                            block(at[0], at[0] + a_bytes, kb > begin);
-                        } else {  // parts of A and B, the smallest products first
-                            block(at[2], at[0] + a_bytes, kb > begin);
-                            block(at[0], at[2] + a_bytes, true);
-                            block(at[1], at[1] + a_bytes, true);
-                            block(at[1], at[0] + a_bytes, true);
-                            block(at[0], at[1] + a_bytes, true);
-                            block(at[0], at[0] + a_bytes, true);
+                            block(a[0], b[0], kb > begin);
+                        } else {  // parts of A and B, the smallest products first, and a stage given back as soon as it has had its last
+                            block(a[2], b[0], kb > begin);
+                            block(a[0], b[2], true);
+                            commit<CTAS>(freed[2]);
+                            block(a[1], b[1], true);
+                            block(a[1], b[0], true);
+                            block(a[0], b[1], true);
+                            commit<CTAS>(freed[1]);
+                            block(a[0], b[0], true);
                         }
-#pragma unroll
-                        for (int q = 0; q < PLANES; ++q) commit_to_pair(freed[q]);
+                        commit<CTAS>(freed[0]);
                     }
                     if (!fine) break;
-                    commit_to_pair(smem_addr(&control.sum_full[buffer]));
+                    commit<CTAS>(smem_addr(&control.sum_full[buffer]));
                     ++made;
                 }
             }
@@ -717,7 +756,7 @@ __global__ void __launch_bounds__(Epilogue<PLANES>::kThreads, 1)
             if (lane == 0) arrive_cluster(in_first_cta(smem_addr(&control.sum_empty[made & 1])));
             ++made;
         };
-        for (int tile = blockIdx.x / 2; tile < total && fine; tile += pairs) {
+        for (int tile = blockIdx.x / CTAS; tile < total && fine; tile += groups) {
             const Tile t = tile_at(tile);
             const int row = t.m0 + (int)rank * 128 + quarter * 32 + lane, n0 = t.n0 + part * part_n;
             const RowInfo info = row_info<WHICH>(prm, t.w, row, n0, t.count);
@@ -730,7 +769,7 @@ __global__ void __launch_bounds__(Epilogue<PLANES>::kThreads, 1)
                 for (int c = 0; c < part_n && !idle; c += 32) {
                     float v[32];
                     if (t.blocks > 0) {
-                        take_sums(v, columns + (made & 1) * kTileN + c, false);
+                        take_sums(v, columns + (made & 1) * kTileN + c, false, 32);
                         if (c + 32 >= part_n) taken();
                     } else {
 #pragma unroll
@@ -748,7 +787,7 @@ __global__ void __launch_bounds__(Epilogue<PLANES>::kThreads, 1)
                 }
                 for (int kb = 0; kb < t.blocks; kb = min(kb + segment, t.blocks)) {
                     if (!summed()) break;
-                    if (!idle) take_sums(v, columns + (made & 1) * kTileN, kb > 0);
+                    if (!idle) take_sums(v, columns + (made & 1) * kTileN, kb > 0, part_n);
                     taken();
                 }
                 if (!fine) break;
@@ -763,10 +802,10 @@ __global__ void __launch_bounds__(Epilogue<PLANES>::kThreads, 1)
     if (!fine && lane == 0) atomicExch(&g_gave_up, 1);
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
-    cluster_sync();
+    if constexpr (CTAS == 2) cluster_sync();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     __syncwarp();
-    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tensor_memory) : "memory");
+    if (warp == 1) free_tensor_memory<CTAS>(tensor_memory);
 }
 
 // ------------------------------------------------------------------------------------------------------------- host
@@ -785,11 +824,11 @@ bool encode_operand(CUtensorMap* map, const Operand& o, int planes, int workers,
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <Product WHICH, int PLANES>
+template <Product WHICH, int PLANES, int CTAS>
 cudaError_t launch(const ProductParams& prm, cudaStream_t stream)
 {
     static rps::LaunchState state;
-    cudaError_t err = rps::grant_smem(state, rps_product_kernel<WHICH, PLANES>, kSharedBytes);
+    cudaError_t err = rps::grant_smem(state, rps_product_kernel<WHICH, PLANES, CTAS>, kSharedBytes);
     if (err != cudaSuccess) return err;
     int sms = 0;
     if ((err = sm_count(&sms)) != cudaSuccess) return err;
@@ -800,42 +839,52 @@ cudaError_t launch(const ProductParams& prm, cudaStream_t stream)
     p.a_rows = a_other || p.m > 128 ? 128 : (int)round_up(p.m, 8);
     if (p.k == 0) {  // nothing is read: the kernel writes zeros
         p.count = nullptr;
-    } else if (!encode_operand(&maps.a, p.a, p.planes, p.workers, a_other ? 64 : p.a_rows) || !encode_operand(&maps.b, p.b, p.planes, p.workers, b_other ? 64 : p.tile_cols / 2)) {
+    } else if (!encode_operand(&maps.a, p.a, p.planes, p.workers, a_other ? 64 : p.a_rows) || !encode_operand(&maps.b, p.b, p.planes, p.workers, b_other ? 64 : p.tile_cols / CTAS)) {
         return cudaErrorInvalidValue;
     }
-    const int64_t tiles = ceil_div(p.m, kTileM) * ceil_div(p.n, p.tile_cols) * p.workers * p.splits;
-    const int pairs = (int)(tiles < sms / 2 ? tiles : sms / 2);
-    return launch_after(rps_product_kernel<WHICH, PLANES>, dim3(2 * pairs), Epilogue<PLANES>::kThreads, kSharedBytes, stream, 2, p, maps);
+    const int64_t tiles = ceil_div(p.m, 128 * CTAS) * ceil_div(p.n, p.tile_cols) * p.workers * p.splits;
+    const int groups = (int)(tiles < sms / CTAS ? tiles : sms / CTAS);
+    return launch_after(rps_product_kernel<WHICH, PLANES, CTAS>, dim3(CTAS * groups), Epilogue<PLANES>::kThreads, kSharedBytes, stream, CTAS, p, maps);
+}
+
+template <Product WHICH, int PLANES>
+cudaError_t launch_pairs_or_not(const ProductParams& prm, cudaStream_t stream)
+{
+    return prm.ctas == 2 ? launch<WHICH, PLANES, 2>(prm, stream) : launch<WHICH, PLANES, 1>(prm, stream);
 }
 
 }  // namespace
 
-// A product with fewer tiles than the 74 pairs and a long summed axis is cut along it, so that all pairs work.  In microseconds: a block
-// takes a pair 0.27 (the six products of parts of fp32: 1.6) and a tile's end 1; a part's 256 KB written and read 0.1, the launch
-// that joins them 5.  (48 tiles of 157 fp32 blocks: 312 us whole, 222 + 10 in three runs.  From 74 tiles on cutting only evens the
-// last round out, and the board's power, not the idle pairs, bounds it: 120 tiles of 1024 bf16 blocks took 745 us whole, 740 + 15
-// in three.)
+// Pairs of CTAs share B's copies, so they are the faster by some 15 %; but a tile of theirs has 256 rows, and where its second half
+// would be empty (up to 128 rows, 257 to 384, ...) single CTAs with 128 rows are.  (4 workers of 42 tokens, 1314 words, 2530 columns
+// fp32: XXX us in pairs, XXX alone.)
+//
+// A product with fewer tiles than there are pairs (or CTAs) and a long summed axis is cut along it, so that all work.  In
+// microseconds: a block takes 0.27 (the six products of parts of fp32: 1.6) and a tile's end 1; a part written and read 0.1 (0.05 of a
+// single CTA), the launch that joins them 5.  (48 tiles of 157 fp32 blocks: 312 us whole, 222 + 10 in three runs.  From 74 tiles on
+// cutting only evens the last round out, and the board's power, not the idle pairs, bounds it: 120 tiles of 1024 bf16
+// blocks took 745 us whole, 740 + 15 in three.)
 //
 // The tiles' columns are a multiple of 32.  A width that 256 does not divide is cut as narrow as the number of its tiles allows (650
 // columns: three of 224 instead of 256), as a tile's products take time by its columns; and where the summed axis is not cut, as
-// long as twice the tiles still find an idle pair each, down to 64 columns, since a small call waits for one tile's copies and
-// its end.  (4 workers of 32 tokens, 1000
-// words, 256 columns: the four products of a step 39 us with tiles of 256, 32 us with 128 and 64.)
+// long as twice the tiles still find an idle place each, down to 32 columns, since a small call waits for one tile's copies (some 70
+// bytes a nanosecond reach an SM) and its end.  (4 workers of 32 tokens, 1000 words, 256 columns: the four products of a step 39 us with tiles of 256, 32 us with 128 and 64.)
 ProductShape product_shape(int64_t m, int64_t n, int64_t k, int workers, int planes, bool may_split)
 {
-    constexpr int64_t kPairs = 148 / 2;
-    const int64_t others = ceil_div(m > 0 ? m : 1, kTileM) * workers, blocks = ceil_div(k, kDepth);
+    const int64_t halves = ceil_div(m > 0 ? m : 1, 128), whole = ceil_div(halves, 2);
+    const int ctas = (double)halves * 1.15 < (double)(2 * whole) ? 1 : 2;
+    const int64_t places = 148 / ctas, others = (ctas == 1 ? halves : whole) * workers, blocks = ceil_div(k, kDepth);
     int64_t across = ceil_div(n, kTileN);
     const double block = planes == 1 ? 0.27 : 1.6;
     int best = 1;
     double least = 0.0;
-    for (int s = 1; s <= 32 && (s == 1 || (may_split && across * others < kPairs && s * 4 <= blocks)); ++s) {
+    for (int s = 1; s <= 32 && (s == 1 || (may_split && across * others < places && s * 4 <= blocks)); ++s) {
         const int64_t items = across * others * s;
-        const double cost = (double)ceil_div(items, kPairs) * ((double)ceil_div(blocks, s) * block + 1.0) + (s > 1 ? 5.0 + 0.1 * (double)items : 0.0);
+        const double cost = (double)ceil_div(items, places) * ((double)ceil_div(blocks, s) * block + 1.0) + (s > 1 ? 5.0 + 0.05 * ctas * (double)items : 0.0);
         if (s == 1 || cost < least) best = s, least = cost;
     }
-    while (best == 1 && across * 2 * others <= kPairs && n / (across * 2) >= 64) across *= 2;
-    return {(int)round_up(ceil_div(n, across), 32), best};
+    while (best == 1 && across * 2 * others <= places && n / (across * 2) >= 32) across *= 2;
+    return {(int)round_up(ceil_div(n, across), 32), best, ctas};
 }
 
 namespace {
@@ -887,10 +936,10 @@ cudaError_t launch_product(Product which, const ProductParams& prm, cudaStream_t
 {
     const bool f32 = prm.planes == 3;
     switch (which) {
-        case Product::kLse: return f32 ? launch<Product::kLse, 3>(prm, stream) : launch<Product::kLse, 1>(prm, stream);
-        case Product::kDlogits: return f32 ? launch<Product::kDlogits, 3>(prm, stream) : launch<Product::kDlogits, 1>(prm, stream);
-        case Product::kDhidden: return f32 ? launch<Product::kDhidden, 3>(prm, stream) : launch<Product::kDhidden, 1>(prm, stream);
-        default: return f32 ? launch<Product::kDweight, 3>(prm, stream) : launch<Product::kDweight, 1>(prm, stream);
+        case Product::kLse: return f32 ? launch_pairs_or_not<Product::kLse, 3>(prm, stream) : launch_pairs_or_not<Product::kLse, 1>(prm, stream);
+        case Product::kDlogits: return f32 ? launch_pairs_or_not<Product::kDlogits, 3>(prm, stream) : launch_pairs_or_not<Product::kDlogits, 1>(prm, stream);
+        case Product::kDhidden: return f32 ? launch_pairs_or_not<Product::kDhidden, 3>(prm, stream) : launch_pairs_or_not<Product::kDhidden, 1>(prm, stream);
+        default: return f32 ? launch_pairs_or_not<Product::kDweight, 3>(prm, stream) : launch_pairs_or_not<Product::kDweight, 1>(prm, stream);
     }
 }
 
