@@ -166,6 +166,9 @@ typedef struct rps_wgrad_desc {
     int64_t tokens;          /* 0 <= tokens < 2^24                                    */
     int64_t outs, cols;      /* 1..2^24-1                                             */
     int64_t dy_row, dy_worker, dweight_row, dweight_worker; /* strides; rows >= outs and >= cols, dweight_row < 2^31 */
+    int32_t wait_limit_ms;   /* every wait of the product's kernel on data gives up after this many milliseconds (0 = 2000) */
+    int32_t withhold_copies; /* test aid for that: 1 = the kernel issues no copies, so its waits run out, the result is not
+                                written and rps_ops_check reports it; 0 otherwise                                           */
 } rps_wgrad_desc;
 
 /* Of dy only the address counts. */
@@ -173,7 +176,7 @@ int rps_wgrad_workspace(const rps_wgrad_desc* desc, const void* dy, size_t* byte
 int rps_packed_wgrad(const rps_wgrad_desc* desc, const void* dy, const int8_t* codes, const float* scales, void* dweight,
                      void* workspace, size_t workspace_bytes, void* cuda_stream);
 
-/* Every wait of the matrix-product kernels on data is bounded (two seconds); one that gives up ends its kernel early.
+/* Every wait of the matrix-product kernels on data is bounded (two seconds, unless a description says otherwise); one that gives up ends its kernel early.
  * rps_ops_check synchronises the stream and returns RPS_ECUDA if that happened on the current device since the last check. */
 int rps_ops_check(void* cuda_stream);
 

@@ -452,6 +452,8 @@ int check_wgrad(const rps_wgrad_desc* d)
     if (d->outs < 1 || d->outs > kMaxSize || d->cols < 1 || d->cols > kMaxSize)
         return fail(RPS_EINVAL, "outs = %lld, cols = %lld", (long long)d->outs, (long long)d->cols);
     if (d->n * d->tokens >= 1ll << 31) return fail(RPS_EINVAL, "n * tokens = %lld", (long long)(d->n * d->tokens));
+    if (d->wait_limit_ms < 0 || d->withhold_copies < 0 || d->withhold_copies > 1)
+        return fail(RPS_EINVAL, "wait_limit_ms = %d, withhold_copies = %d", d->wait_limit_ms, d->withhold_copies);
     if (d->dy_row < d->outs || d->dy_worker < 0) return fail(RPS_EINVAL, "strides of dy (%lld, %lld)", (long long)d->dy_worker, (long long)d->dy_row);
     return check_output_strides("dweight", d->n, d->outs, d->cols, d->dweight_row, d->dweight_worker);
 }
@@ -513,7 +515,7 @@ extern "C" int rps_packed_wgrad(const rps_wgrad_desc* desc, const void* dy, cons
     }
     ProductParams g{};
     g.a = plan.dy, g.b = plan.x, g.workers = d.n, g.planes = d.dtype == RPS_F32 ? 3 : 1;
-    g.m = (int)d.outs, g.n = (int)d.cols, g.k = (int)d.tokens, g.shaped(plan.shape);
+    g.m = (int)d.outs, g.n = (int)d.cols, g.k = (int)d.tokens, g.shaped(plan.shape), g.wait_limit_ms = d.wait_limit_ms, g.withhold_copies = d.withhold_copies;
     g.out = dweight, g.out_row = d.dweight_row, g.out_worker = d.dweight_worker;
     g.parts = plan.parts, g.part_rows = round_up(d.outs, kVocabTile), g.part_row = round_up(d.cols, kVocabTile);
     RPS_TRY(launch_product(Product::kDweight, g, stream));

@@ -79,6 +79,7 @@ struct ProductParams {
     // pieces of the vocabulary a part goes on growing (`add`).
     int splits, tile_cols, ctas;  // product_shape
     void shaped(const ProductShape& s) { tile_cols = s.tile_cols, splits = s.splits, ctas = s.ctas; }
+    int wait_limit_ms, withhold_copies;  // 0: the default; see rps_wgrad_desc
     int a_rows;                   // rows of A that a CTA copies (launch_product's to set)
     int add;
     float* parts;

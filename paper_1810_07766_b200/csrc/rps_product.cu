@@ -48,7 +48,6 @@ constexpr int kMostEpilogueWarps = Epilogue<1>::kWarps;
 // steps) for the softmax statistics of bf16 operands.  Adding a segment takes the epilogue about 600 cycles under the 6144 or 8192
 // cycles of the products of the next one.
 constexpr int kSegmentF32 = 2, kSegmentStatistics = 16;  // in blocks of kDepth
-constexpr uint64_t kWaitNs = 2000000000ull;
 
 static_assert(kTileN == kVocabTile && kTokenTile % 256 == 0, "operands are padded to whole tiles");
 
@@ -114,7 +113,7 @@ __device__ __forceinline__ void arrive_cluster(uint32_t bar)
     asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
-// Waits for the phase with the given parity; what the pair did before it is then visible.  Gives up after kWaitNs.
+// Waits for the phase with the given parity; what the pair did before it is then visible.  Gives up after limit_ns.
 __device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity)
 {
     uint32_t done;
@@ -128,13 +127,13 @@ __device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity)
     return done != 0;
 }
 
-__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity)
+__device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, uint64_t limit_ns)
 {
     if (try_wait(bar, parity)) return true;
     const uint64_t start = rps::global_timer_ns();
 #pragma unroll 1
     while (!try_wait(bar, parity))
-        if (rps::global_timer_ns() - start > kWaitNs) return false;
+        if (rps::global_timer_ns() - start > limit_ns) return false;
     return true;
 }
 
@@ -450,7 +449,7 @@ __device__ __forceinline__ RowInfo row_info(const ProductParams& prm, int w, int
 // kLse: a warp's columns of one row of a tile, `width` of them.  `turn`: tiles that the warp has had.  False if a wait gave up.
 template <int PLANES, int COLS>
 __device__ __forceinline__ bool statistics(const ProductParams& prm, int w, int row, int n0, int width, int count, const RowInfo& info, float (&v)[COLS],
-                                           Control& control, int quarter, int part, int turn)
+                                           Control& control, int quarter, int part, int turn, uint64_t limit_ns)
 {
     constexpr int kParts = Epilogue<PLANES>::kParts;
     const int cols = min(width, prm.n - n0);
@@ -492,7 +491,7 @@ __device__ __forceinline__ bool statistics(const ProductParams& prm, int w, int 
     __syncwarp();
     if (lane == 0) rps::mbar_arrive(there);
     if (part != 0) return true;
-    if (!__all_sync(0xFFFFFFFFu, wait(there, turn >> 2 & 1))) return false;
+    if (!__all_sync(0xFFFFFFFFu, wait_for(there, turn >> 2 & 1, limit_ns))) return false;
     if (row >= count) return true;
     for (int k = 1; k < kParts; ++k) {
         const float2 p = row_statistics[k * 128 + r];
@@ -638,6 +637,8 @@ __global__ void __launch_bounds__(Epilogue<PLANES>::kThreads, 1)
     // blocks to a segment
     const int segment = PLANES == 3 ? kSegmentF32 : WHICH == Product::kLse ? kSegmentStatistics : 1 << 30;
     bool fine = true;
+    const uint64_t limit_ns = prm.wait_limit_ms > 0 ? (uint64_t)prm.wait_limit_ms * 1000000u : rps::kDefaultWaitLimitNs;
+    const auto wait = [&](uint32_t bar, uint32_t parity) { return wait_for(bar, parity, limit_ns); };
 
     if (warp == 0) {
         if (lane == 0) {
@@ -652,7 +653,7 @@ __global__ void __launch_bounds__(Epilogue<PLANES>::kThreads, 1)
                 const int rows = WHICH == Product::kDweight ? prm.m : t.count;
                 const bool copy_a = m0 < rows, copy_b = n0 < prm.n;
                 const uint32_t bytes = (CTAS == 2 && t.m0 + 128 < rows ? 2 : 1) * a_bytes + (CTAS == 2 && t.n0 + own_n < prm.n ? 2 : 1) * b_bytes;
-                for (int i = 0; i < t.blocks * PLANES; ++i) {
+                for (int i = 0; i < t.blocks * PLANES && prm.withhold_copies == 0; ++i) {
                     fine = wait(smem_addr(&control.empty[stage]), phase ^ 1);
                     if (!fine) break;
                     const int kb = PLANES == 1 ? i : i / 3, plane = i - kb * PLANES, k0 = (t.first + kb) * kDepth;
@@ -793,7 +794,7 @@ __global__ void __launch_bounds__(Epilogue<PLANES>::kThreads, 1)
                 if (!fine) break;
                 if (idle) continue;
                 if constexpr (WHICH == Product::kLse)
-                    fine = statistics<PLANES>(prm, t.w, row, n0, part_n, t.count, info, v, control, quarter, part, turn++);
+                    fine = statistics<PLANES>(prm, t.w, row, n0, part_n, t.count, info, v, control, quarter, part, turn++, limit_ns);
                 else
                     store_columns<WHICH, PLANES>(prm, t.w, t.split, row, n0, part_n, t.count, info.target, info, v, wide, control.staging_f32[warp - 2]);
             }

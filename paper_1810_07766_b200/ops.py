@@ -51,7 +51,8 @@ class rps_norm_desc(ctypes.Structure):
 
 class rps_wgrad_desc(ctypes.Structure):
     _fields_ = [("dtype", _i32), ("n", _i32), ("tokens", _i64), ("outs", _i64), ("cols", _i64), ("dy_row", _i64),
-                ("dy_worker", _i64), ("dweight_row", _i64), ("dweight_worker", _i64)]
+                ("dy_worker", _i64), ("dweight_row", _i64), ("dweight_worker", _i64), ("wait_limit_ms", _i32),
+                ("withhold_copies", _i32)]
 
 
 _lib = None

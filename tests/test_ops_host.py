@@ -123,7 +123,7 @@ def test_pack_and_wgrad_arguments_are_refused(lib):
     size = ctypes.c_size_t()
     assert lib.rps_wgrad_workspace(ctypes.byref(desc()), None, ctypes.byref(size)) == 0 and size.value > 0
     for change in ({"dtype": 2}, {"n": 0}, {"tokens": -1}, {"outs": 0}, {"cols": 0}, {"dy_row": 7}, {"dy_worker": -1}, {"dweight_row": 9},
-                   {"dweight_worker": 79}):
+                   {"dweight_worker": 79}, {"dweight_row": 1 << 31, "dweight_worker": 1 << 40}, {"wait_limit_ms": -1}, {"withhold_copies": 2}):
         assert lib.rps_wgrad_workspace(ctypes.byref(desc(**change)), None, ctypes.byref(size)) == -1, change
     assert lib.rps_packed_wgrad(ctypes.byref(desc()), one, one, one, None, one, size.value, None) == -1
     assert lib.rps_packed_wgrad(ctypes.byref(desc()), one, one, one, one, one, size.value - 1, None) == -1
