@@ -132,7 +132,10 @@ LcePlan plan_lce(const rps_lce_desc& d, const void* weight, bool backward, void*
     ProductParams& g = plan.product;
     // in several pieces the tiles are whole, so that the pieces' statistics lie side by side
     g.shaped(product_shape(d.tokens, d.vocab, d.cols, d.n, p.planes, false));
-    if (plan.piece < whole) g.tile_cols = kVocabTile;
+    if (plan.piece < whole)
+        g.tile_cols = kVocabTile;
+    else
+        plan.piece = round_up(d.vocab, g.tile_cols);  // dl is written in whole tiles
     p.stat_tiles = ceil_div(d.vocab, g.tile_cols);
 
     Carver c{static_cast<unsigned char*>(workspace)};
@@ -145,12 +148,11 @@ LcePlan plan_lce(const rps_lce_desc& d, const void* weight, bool backward, void*
         p.info = c.take<float2>(p.n * p.tokens_padded);
         plan.dl = c.take<bf16>(p.n * p.planes * p.tokens_padded * plan.piece);
         p.scale = c.take<float>(p.n);
-        const int64_t part_row = round_up(p.cols, kVocabTile);
         plan.hidden_shape = product_shape(d.tokens, d.cols, plan.piece < d.vocab ? plan.piece : d.vocab, p.n, p.planes, true);
-        if (plan.piece < whole || plan.hidden_shape.splits > 1)
-            plan.hidden_parts = c.take<float>(plan.hidden_shape.splits * p.n * p.tokens_padded * part_row);
+        if (plan.piece < d.vocab || plan.hidden_shape.splits > 1)
+            plan.hidden_parts = c.take<float>(plan.hidden_shape.splits * p.n * p.tokens_padded * round_up(p.cols, plan.hidden_shape.tile_cols));
         plan.weight_shape = product_shape(plan.piece < d.vocab ? plan.piece : d.vocab, d.cols, d.tokens, p.n, p.planes, true);
-        if (plan.weight_shape.splits > 1) plan.weight_parts = c.take<float>(plan.weight_shape.splits * p.n * plan.piece * part_row);
+        if (plan.weight_shape.splits > 1) plan.weight_parts = c.take<float>(plan.weight_shape.splits * p.n * plan.piece * round_up(p.cols, plan.weight_shape.tile_cols));
     } else {
         p.done = c.take<int>(p.n);
         p.sums = c.take<float>(p.n * lce_merge_blocks(p.tokens));
@@ -163,7 +165,7 @@ LcePlan plan_lce(const rps_lce_desc& d, const void* weight, bool backward, void*
     g.vocab = (int)p.vocab, g.stat_tiles = (int)p.stat_tiles, g.target = p.target;
     g.part = const_cast<float2*>(p.part), g.hit = const_cast<float*>(p.hit), g.info = p.info, g.dl = plan.dl;
     g.tokens_padded = p.tokens_padded, g.piece = plan.piece, g.rows = p.rows, g.tokens = p.tokens;
-    g.part_row = round_up(p.cols, kVocabTile), g.scale = p.scale;
+    g.scale = p.scale;
     return plan;
 }
 
@@ -274,13 +276,13 @@ extern "C" int rps_lce_backward(const rps_lce_desc* desc, const void* hidden, co
             g.a = h, g.b = weight_rows, g.m = (int)d.tokens, g.n = (int)rows, g.k = (int)d.cols;
             RPS_TRY(launch_product(Product::kDlogits, g, stream));
             g.a = dl, g.n = (int)d.cols, g.k = (int)rows, g.shaped(plan.hidden_shape);
-            g.parts = plan.hidden_parts, g.part_rows = p.tokens_padded, g.add = v0 > 0;
+            g.parts = plan.hidden_parts, g.part_rows = p.tokens_padded, g.part_row = round_up(d.cols, g.tile_cols), g.add = v0 > 0;
             g.out = dhidden, g.out_row = d.cols, g.out_worker = d.tokens * d.cols;
             RPS_TRY(launch_product(Product::kDhidden, g, stream));
             if (g.parts != nullptr && v0 + rows == d.vocab) RPS_TRY(launch_join(Product::kDhidden, g, stream));
         }
         g.a = dl, g.b = h, g.m = (int)rows, g.n = (int)d.cols, g.k = (int)d.tokens, g.shaped(plan.weight_shape);
-        g.parts = plan.weight_parts, g.part_rows = plan.piece, g.add = 0;
+        g.parts = plan.weight_parts, g.part_rows = plan.piece, g.part_row = round_up(d.cols, g.tile_cols), g.add = 0;
         g.out = static_cast<unsigned char*>(dweight) + v0 * d.dweight_row * (p.f32 ? 4 : 2), g.out_row = d.dweight_row, g.out_worker = d.dweight_worker;
         RPS_TRY(launch_product(Product::kDweight, g, stream));
         if (g.parts != nullptr) RPS_TRY(launch_join(Product::kDweight, g, stream));
@@ -481,7 +483,7 @@ WgradPlan plan_wgrad(const rps_wgrad_desc& d, const void* dy, void* workspace)
         q.src_row = d.dy_row, q.src_worker = d.dy_worker, q.dst = to, q.dst_row = row, q.dst_plane = plane, q.dst_worker = planes * plane;
     }
     plan.shape = product_shape(d.outs, d.cols, d.tokens, d.n, planes, true);
-    if (plan.shape.splits > 1) plan.parts = c.take<float>(plan.shape.splits * d.n * round_up(d.outs, kVocabTile) * round_up(d.cols, kVocabTile));
+    if (plan.shape.splits > 1) plan.parts = c.take<float>(plan.shape.splits * d.n * round_up(d.outs, kVocabTile) * round_up(d.cols, plan.shape.tile_cols));
     plan.bytes = c.used;
     return plan;
 }
@@ -517,7 +519,7 @@ extern "C" int rps_packed_wgrad(const rps_wgrad_desc* desc, const void* dy, cons
     g.a = plan.dy, g.b = plan.x, g.workers = d.n, g.planes = d.dtype == RPS_F32 ? 3 : 1;
     g.m = (int)d.outs, g.n = (int)d.cols, g.k = (int)d.tokens, g.shaped(plan.shape), g.wait_limit_ms = d.wait_limit_ms, g.withhold_copies = d.withhold_copies;
     g.out = dweight, g.out_row = d.dweight_row, g.out_worker = d.dweight_worker;
-    g.parts = plan.parts, g.part_rows = round_up(d.outs, kVocabTile), g.part_row = round_up(d.cols, kVocabTile);
+    g.parts = plan.parts, g.part_rows = round_up(d.outs, kVocabTile), g.part_row = round_up(d.cols, g.tile_cols);
     RPS_TRY(launch_product(Product::kDweight, g, stream));
     if (g.parts != nullptr) RPS_TRY(launch_join(Product::kDweight, g, stream));
     return RPS_OK;

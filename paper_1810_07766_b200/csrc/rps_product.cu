@@ -16,6 +16,7 @@
 //
 // fp32 operands are three bf16 parts each (24 significant bits); of the nine products of parts the six that reach 2^-24
 // of the result are made.  The three parts of a block lie in three stages of the ring, so each is copied once for its three products.
+#include <algorithm>
 #include <mutex>
 #include <type_traits>
 
@@ -866,10 +867,11 @@ cudaError_t launch_pairs_or_not(const ProductParams& prm, cudaStream_t stream)
 // cutting only evens the last round out, and the board's power, not the idle pairs, bounds it: 120 tiles of 1024 bf16
 // blocks took 745 us whole, 740 + 15 in three.)
 //
-// The tiles' columns are a multiple of 32.  A width that 256 does not divide is cut as narrow as the number of its tiles allows (650
-// columns: three of 224 instead of 256), as a tile's products take time by its columns; and where the summed axis is not cut, as
-// long as twice the tiles still find an idle place each, down to 32 columns, since a small call waits for one tile's copies (some 70
-// bytes a nanosecond reach an SM) and its end.  (4 workers of 32 tokens, 1000 words, 256 columns: the four products of a step 39 us with tiles of 256, 32 us with 128 and 64.)
+// The tiles' columns are a multiple of 32: as few as their number allows (650 columns are three of 224 instead of 256); and up to two
+// rounds so few that rounds x time of a tile is least.  Half of a tile's time is A's, whose copies are the same for any width (a
+// quarter of fp32's, where each copy has three products), and half B's.  So 76 tiles of 192 become 114 of 128 (two workers' 1048 x 4735 x 345 fp32: 65 -> 49 us), and a
+// small call's tiles so narrow that every place has one.  (Of many rounds the widest are best: 8192 x 8192 x 2048 bf16 in 4 rounds of
+// 256 columns 184 us, in 5 of 192 246 us.)  (4 workers of 32 tokens, 1000 words, 256 columns: the four products of a step 39 us with tiles of 256, 32 us with 128 and 64.)
 ProductShape product_shape(int64_t m, int64_t n, int64_t k, int workers, int planes, bool may_split)
 {
     const int64_t halves = ceil_div(m > 0 ? m : 1, 128), whole = ceil_div(halves, 2);
@@ -884,7 +886,16 @@ ProductShape product_shape(int64_t m, int64_t n, int64_t k, int workers, int pla
         const double cost = (double)ceil_div(items, places) * ((double)ceil_div(blocks, s) * block + 1.0) + (s > 1 ? 5.0 + 0.05 * ctas * (double)items : 0.0);
         if (s == 1 || cost < least) best = s, least = cost;
     }
-    while (best == 1 && across * 2 * others <= places && n / (across * 2) >= 32) across *= 2;
+    if (best == 1) {
+        const int64_t fewest = across, idle = std::max(across, std::min(places / others, n / 32));
+        double shortest = 0.0;
+        for (int64_t a = fewest; a <= (fewest * others <= 2 * places ? std::max(idle, fewest + 8) : fewest); a = a < fewest + 8 ? a + 1 : idle > a ? idle : a + 1) {
+            const int64_t tile = round_up(ceil_div(n, a), 32), tiles = ceil_div(n, tile);
+            const double part = (double)tile / kTileN, products = planes == 1 ? 0.5 + 0.5 * part : 0.25 + 0.75 * part;
+            const double cost = (double)ceil_div(tiles * others, places) * ((double)blocks * block * products + part + 0.5);
+            if (a == fewest || cost < shortest) across = a, shortest = cost;
+        }
+    }
     return {(int)round_up(ceil_div(n, across), 32), best, ctas};
 }
 
