@@ -203,10 +203,18 @@ __global__ void __launch_bounds__(kMergeThreads) rps_lce_merge_kernel(const LceP
     }
     parts[warp][lane] = make_float2(top, sum);
     __syncthreads();
+    // four warps take four parts each, then one the four
+    if (warp < 4) {
+#pragma unroll
+        for (int k = 1; k < kWarps / 4; ++k) join(parts[warp + 4 * k][lane]);
+        parts[warp][lane] = make_float2(top, sum);
+    }
+    __syncthreads();
     if (warp != 0) return;
     float loss = 0.0f;
     if (i < count) {
-        for (int k = 1; k < kWarps; ++k) join(parts[k][lane]);
+#pragma unroll
+        for (int k = 1; k < 4; ++k) join(parts[k][lane]);
         const float lse = top + logf(sum);
         loss = lse - prm.hit[w * prm.tokens_padded + i];
         const int64_t t = prm.rows[w * prm.tokens + i];

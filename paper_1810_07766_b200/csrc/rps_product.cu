@@ -393,7 +393,8 @@ __device__ __forceinline__ void store_rows(Stage& stage, const float (&v)[COLS],
     }
 }
 
-// fp32 values as three planes of bf16 parts.
+// fp32 values as three planes of bf16 parts: the leading 8 bits of what the parts before leave, cut off.  (A NaN is one in all of them, an
+// infinity becomes NaN in the second: what they are summed into is NaN either way.)
 template <int COLS, typename Stage>
 __device__ __forceinline__ void store_parts(Stage& stage, float (&v)[COLS], Rows<bf16> to, int64_t plane)
 {
@@ -408,14 +409,14 @@ __device__ __forceinline__ void store_parts(Stage& stage, float (&v)[COLS], Rows
             uint32_t* word = reinterpret_cast<uint32_t*>(mine);
 #pragma unroll
             for (int j = 0; j < 32; j += 2) {
-                float part[2];
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    float& f = v[c + j + k];
-                    part[k] = q < 2 ? leading_bits(f) : f;
-                    if (q < 2) f = rest_of(f, part[k]);
+                float &f0 = v[c + j], &f1 = v[c + j + 1];
+                if (q < 2) {
+                    const uint32_t lead0 = __float_as_uint(f0) & 0xFFFF0000u, lead1 = __float_as_uint(f1) & 0xFFFF0000u;
+                    word[j / 2] = __byte_perm(lead0, lead1, 0x7632);
+                    f0 -= __uint_as_float(lead0), f1 -= __uint_as_float(lead1);
+                } else {
+                    word[j / 2] = two_bf16(f0, f1);
                 }
-                word[j / 2] = two_bf16(part[0], part[1]);
             }
             store_chunk<false, true>(stage, mine, part_to, c);
         }
