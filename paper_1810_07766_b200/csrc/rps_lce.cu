@@ -10,21 +10,23 @@ namespace {
 constexpr int kSelectThreads = 1024;
 constexpr int kMergeThreads = 512, kMergeRows = 32;
 constexpr int kRowThreads = 256;
+constexpr int kFewTokens = 4 * kRowThreads;
 
-// One CTA per worker.  rows[] becomes a permutation of the worker's tokens: those that take part in their order, then
-// the ignored ones.  A thread takes four tokens at a time; a scan over the lanes and one over the warps give each its place.
-__global__ void __launch_bounds__(kSelectThreads) rps_lce_select_kernel(const LceParams prm)
+// The worker's tokens in a new order: those that take part in theirs, then the ignored ones.  A thread takes four tokens at a time; a
+// scan over the lanes and one over the warps give each its place.  Returns how many take part; `write`: also what later kernels
+// need of it goes out; row_of (or NULL): the order, for this CTA.
+template <int THREADS>
+__device__ __forceinline__ int select_tokens(const LceParams& prm, int w, bool write, int* row_of)
 {
-    after_the_kernel_before();
-    constexpr int kEach = 4, kWarps = kSelectThreads / 32;
-    static_assert(kWarps == 32, "a lane for each warp's count");
+    constexpr int kEach = 4, kWarps = THREADS / 32;
+    static_assert(kWarps <= 32, "a lane for each warp's count");
     __shared__ int warp_count[kWarps];
-    const int w = blockIdx.x, lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     const int64_t* targets = prm.targets + w * prm.tokens;
     int* rows = prm.rows + w * prm.tokens;
     const int64_t padded = w * prm.tokens_padded;
     int kept = 0;
-    for (int64_t t0 = 0; t0 < prm.tokens; t0 += kSelectThreads * kEach) {
+    for (int64_t t0 = 0; t0 < prm.tokens; t0 += THREADS * kEach) {
         const int64_t t = t0 + threadIdx.x * kEach;
         int64_t y[kEach];
         int mine = 0;
@@ -41,49 +43,62 @@ __global__ void __launch_bounds__(kSelectThreads) rps_lce_select_kernel(const Lc
         }
         if (lane == 31) warp_count[warp] = upto;
         __syncthreads();
-        int warps_upto = warp_count[lane];
+        int warps_upto = lane < kWarps ? warp_count[lane] : 0;
 #pragma unroll
         for (int s = 1; s < 32; s *= 2) {
             const int n = __shfl_up_sync(0xFFFFFFFFu, warps_upto, s);
             if (lane >= s) warps_upto += n;
         }
-        int at = kept + upto - mine + (warp > 0 ? __shfl_sync(0xFFFFFFFFu, warps_upto, warp - 1) : 0);
+        const int before = __shfl_sync(0xFFFFFFFFu, warps_upto, warp > 0 ? warp - 1 : 0);
+        int at = kept + upto - mine + (warp > 0 ? before : 0);
         kept += __shfl_sync(0xFFFFFFFFu, warps_upto, 31);
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
             if (t + j >= prm.tokens) break;
-            if (y[j] != prm.ignore_index) {
-                const bool names_a_row = y[j] >= 0 && y[j] < prm.vocab;
-                rows[at] = (int)t + j;
-                prm.target[padded + at] = names_a_row ? (int)y[j] : -1;
-                if (prm.backward) {
-                    const float g = prm.reduction == RPS_REDUCE_NONE ? prm.dloss[w * prm.tokens + t + j] : 1.0f;
-                    prm.info[padded + at] = make_float2(prm.lse_in[w * prm.tokens + t + j], names_a_row ? g : nanf(""));
-                } else {
-                    const_cast<float*>(prm.hit)[padded + at] = names_a_row ? 0.0f : nanf("");
-                }
-                ++at;
-            } else {
-                // filled from the end, so that the places do not depend on the count: ignored token number i lies i from the end
-                rows[prm.tokens - 1 - ((int)t + j - at)] = (int)t + j;
-                if (!prm.backward) {
+            const bool in = y[j] != prm.ignore_index;
+            // ignored tokens are filled in from the end, so that the places do not depend on the count: number i lies i from the end
+            const int place = in ? at : (int)prm.tokens - 1 - ((int)t + j - at);
+            if (row_of != nullptr) row_of[place] = (int)t + j;
+            if (write) {
+                rows[place] = (int)t + j;
+                if (in) {
+                    const bool names_a_row = y[j] >= 0 && y[j] < prm.vocab;
+                    prm.target[padded + at] = names_a_row ? (int)y[j] : -1;
+                    if (prm.backward) {
+                        const float g = prm.reduction == RPS_REDUCE_NONE ? prm.dloss[w * prm.tokens + t + j] : 1.0f;
+                        prm.info[padded + at] = make_float2(prm.lse_in[w * prm.tokens + t + j], names_a_row ? g : nanf(""));
+                    } else {
+                        const_cast<float*>(prm.hit)[padded + at] = names_a_row ? 0.0f : nanf("");
+                    }
+                } else if (!prm.backward) {
                     prm.lse[w * prm.tokens + t + j] = 0.0f;
                     if (prm.reduction == RPS_REDUCE_NONE) prm.loss[w * prm.tokens + t + j] = 0.0f;
                 }
             }
+            if (in) ++at;
         }
         __syncthreads();
     }
-    if (threadIdx.x != 0) return;
-    prm.count[w] = kept;
-    if (prm.backward) {
-        // A factor that all rows share stays out of dl: near a token's target dl is p - 1, which bf16 holds all but exactly, and
-        // (p - 1) times a factor it does not (relative error of the gradients: 2.7e-3 -> 1.7e-3, 1.65e-3 of it the rounding of the result).
-        prm.scale[w] = prm.reduction == RPS_REDUCE_NONE || kept == 0 ? 1.0f : prm.reduction == RPS_REDUCE_MEAN ? prm.dloss[w] / (float)kept : prm.dloss[w];
-    } else {
-        prm.done[w] = 0;
-        if (kept == 0 && prm.reduction != RPS_REDUCE_NONE) prm.loss[w] = 0.0f;
+    if (threadIdx.x == 0 && write) {
+        prm.count[w] = kept;
+        if (prm.backward) {
+            // A factor that all rows share stays out of dl: near a token's target dl is p - 1, which bf16 holds all but exactly, and
+            // (p - 1) times a factor it does not (relative error of the gradients: 2.7e-3 -> 1.7e-3, 1.65e-3 of it the rounding of the
+            // result).
+            prm.scale[w] = prm.reduction == RPS_REDUCE_NONE || kept == 0 ? 1.0f : prm.reduction == RPS_REDUCE_MEAN ? prm.dloss[w] / (float)kept : prm.dloss[w];
+        } else {
+            prm.done[w] = 0;
+            if (kept == 0 && prm.reduction != RPS_REDUCE_NONE) prm.loss[w] = 0.0f;
+        }
     }
+    return kept;
+}
+
+// One CTA per worker.
+__global__ void __launch_bounds__(kSelectThreads) rps_lce_select_kernel(const LceParams prm)
+{
+    after_the_kernel_before();
+    select_tokens<kSelectThreads>(prm, blockIdx.x, true, nullptr);
 }
 
 // Eight columns from c on, as fp32; zero from `cols` on.
@@ -114,22 +129,26 @@ __device__ __forceinline__ void store_parts(bf16* dst, int64_t plane, const floa
     }
 }
 
-// A warp to a row.
-template <typename T, int ALIGN>
+// Rows of hidden laid out in the new order, a warp to a row.  SELECT (at most kFewTokens): every CTA finds the order out for itself, the
+// first one of a worker also for the kernels to come, which saves a launch (one / two, us: 1 token 2.5 / 5.1; 1000 tokens x 256 bf16
+// 3.3 / 5.7; of 8 workers x 512 bf16 8.2 / 8.5, x 1024 fp32 18.7 / 20.0: with more rows the order is found too often to gain by it).
+template <typename T, int ALIGN, bool SELECT>
 __global__ void __launch_bounds__(kRowThreads) rps_lce_gather_kernel(const LceParams prm)
 {
     after_the_kernel_before();
+    __shared__ int row_of[SELECT ? kFewTokens : 1];
     const int w = blockIdx.y, lane = threadIdx.x % 32;
     const int64_t i = (int64_t)blockIdx.x * (kRowThreads / 32) + threadIdx.x / 32;
-    const int count = prm.count[w], D = (int)prm.cols;
+    const int count = SELECT ? select_tokens<kRowThreads>(prm, w, blockIdx.x == 0, row_of) : prm.count[w], D = (int)prm.cols;
     const bool in = i < count;
+    const int64_t token = i < prm.tokens ? (SELECT ? row_of[i] : prm.rows[w * prm.tokens + i]) : 0;
     if (!in && i < prm.tokens && prm.backward) {  // an ignored token's gradient
-        T* out = static_cast<T*>(prm.dhidden) + (w * prm.tokens + prm.rows[w * prm.tokens + i]) * prm.cols;
+        T* out = static_cast<T*>(prm.dhidden) + (w * prm.tokens + token) * prm.cols;
         for (int c = lane; c < D; c += 32) out[c] = from_float<T>(0.0f);
     }
-    // products read whole token tiles: the rows behind the last one are cleared
-    if (i >= (count + kTokenTile - 1) / kTokenTile * kTokenTile) return;
-    const T* src = static_cast<const T*>(prm.hidden) + w * prm.hidden_worker + (in ? prm.rows[w * prm.tokens + i] : 0) * prm.hidden_row;
+    // the product with dl over the tokens reads whole blocks of rows: those behind the last one are cleared
+    if (i >= (count + kTokenBlock - 1) / kTokenBlock * kTokenBlock) return;
+    const T* src = static_cast<const T*>(prm.hidden) + w * prm.hidden_worker + (in ? token : 0) * prm.hidden_row;
     bf16* dst = prm.packed + (w * prm.planes * prm.tokens_padded + i) * prm.cols_padded;
     const int64_t plane = prm.tokens_padded * prm.cols_padded;
 #pragma unroll 4
@@ -245,12 +264,14 @@ int aligned_source(const void* p, int64_t cols, int64_t row, int64_t worker)
     return std::min(alignment<T>(p, cols, row), alignment<T>(p, cols, worker));
 }
 
-template <typename T>
+template <typename T, bool SELECT>
 cudaError_t gather(const LceParams& prm, cudaStream_t stream)
 {
-    const dim3 grid((unsigned)ceil_div(prm.tokens_padded, kRowThreads / 32), (unsigned)prm.n);
+    const dim3 grid((unsigned)ceil_div(round_up(prm.tokens, kTokenBlock), kRowThreads / 32), (unsigned)prm.n);
     const int align = aligned_source<T>(prm.hidden, prm.cols, prm.hidden_row, prm.hidden_worker);
-    const auto kernel = align == 16 ? rps_lce_gather_kernel<T, 16> : align == 4 ? rps_lce_gather_kernel<T, 4> : rps_lce_gather_kernel<T, sizeof(T)>;
+    const auto kernel = align == 16  ? rps_lce_gather_kernel<T, 16, SELECT>
+                        : align == 4 ? rps_lce_gather_kernel<T, 4, SELECT>
+                                     : rps_lce_gather_kernel<T, sizeof(T), SELECT>;
     return launch_after(kernel, grid, kRowThreads, 0, stream, 1, prm);
 }
 
@@ -269,14 +290,12 @@ cudaError_t planes(const PlanesParams& prm, cudaStream_t stream)
 
 }  // namespace
 
-cudaError_t launch_lce_select(const LceParams& prm, cudaStream_t stream)
+cudaError_t launch_lce_rows(const LceParams& prm, cudaStream_t stream)
 {
-    return launch_after(rps_lce_select_kernel, dim3((unsigned)prm.n), kSelectThreads, 0, stream, 1, prm);
-}
-
-cudaError_t launch_lce_gather(const LceParams& prm, cudaStream_t stream)
-{
-    return prm.f32 ? gather<float>(prm, stream) : gather<bf16>(prm, stream);
+    if (prm.tokens > 0 && prm.tokens <= kFewTokens) return prm.f32 ? gather<float, true>(prm, stream) : gather<bf16, true>(prm, stream);
+    const cudaError_t err = launch_after(rps_lce_select_kernel, dim3((unsigned)prm.n), kSelectThreads, 0, stream, 1, prm);
+    if (err != cudaSuccess || prm.tokens == 0) return err;
+    return prm.f32 ? gather<float, false>(prm, stream) : gather<bf16, false>(prm, stream);
 }
 
 int64_t lce_merge_blocks(int64_t tokens) { return ceil_div(tokens, kMergeRows); }

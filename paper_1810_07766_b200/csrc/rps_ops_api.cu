@@ -228,9 +228,8 @@ extern "C" int rps_lce_forward(const rps_lce_desc* desc, const void* hidden, con
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     LceParams& p = plan.p;
     p.targets = targets, p.hidden = hidden, p.loss = loss, p.lse = lse;
-    RPS_TRY(launch_lce_select(p, stream));
+    RPS_TRY(launch_lce_rows(p, stream));
     if (d.tokens == 0) return RPS_OK;
-    RPS_TRY(launch_lce_gather(p, stream));
     ProductParams g = plan.product;
     g.a = hidden_operand(p);
     g.m = (int)d.tokens, g.k = (int)d.cols;
@@ -260,8 +259,7 @@ extern "C" int rps_lce_backward(const rps_lce_desc* desc, const void* hidden, co
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     LceParams& p = plan.p;
     p.targets = targets, p.hidden = hidden, p.lse_in = lse, p.dloss = dloss, p.dhidden = dhidden;
-    RPS_TRY(launch_lce_select(p, stream));
-    if (d.tokens > 0) RPS_TRY(launch_lce_gather(p, stream));
+    RPS_TRY(launch_lce_rows(p, stream));
     const Operand h = hidden_operand(p);
     for (int64_t v0 = 0; v0 < d.vocab; v0 += plan.piece) {
         const int64_t rows = d.vocab - v0 < plan.piece ? d.vocab - v0 : plan.piece;

@@ -34,6 +34,7 @@ cudaError_t launch_after(Kernel kernel, dim3 grid, int threads, size_t shared, c
 // ---------------------------------------------------------------------------------------------------- products
 // Token rows are padded to whole tiles, and the vocabulary goes through the loss in whole tiles.
 constexpr int kTokenTile = 256;
+constexpr int kTokenBlock = 64;  // of tokens as a summed axis
 constexpr int kVocabTile = 256;
 
 // An operand of a product: bf16 [worker][plane][rows][row stride].  fp32 values lie in three planes whose sum they are.
@@ -119,8 +120,8 @@ struct LceParams {
     int* done;        // [n]
 };
 
-cudaError_t launch_lce_select(const LceParams& prm, cudaStream_t stream);
-cudaError_t launch_lce_gather(const LceParams& prm, cudaStream_t stream);
+// Which tokens take part, and their rows laid out.
+cudaError_t launch_lce_rows(const LceParams& prm, cudaStream_t stream);
 int64_t lce_merge_blocks(int64_t tokens);
 cudaError_t launch_lce_merge(const LceParams& prm, cudaStream_t stream);
 

@@ -51,7 +51,7 @@ constexpr int kMostEpilogueWarps = Epilogue<1>::kWarps;
 // x 10001 x 650 fp32 256 -> 238 us, errors of the gradients 6e-7 -> 9e-7; not taken.)
 constexpr int kSegmentF32 = 2, kSegmentStatistics = 16;  // in blocks of kDepth
 
-static_assert(kTileN == kVocabTile && kTokenTile % 256 == 0, "operands are padded to whole tiles");
+static_assert(kTileN == kVocabTile && kTokenTile % 256 == 0 && kTokenBlock == kDepth, "operands are padded to whole tiles");
 
 // Rows leave through shared memory: a lane holds one row, and 32 lanes writing 16 bytes of 32 rows each would touch 32 lines at a time and
 // half a sector of each.  Instead 64 bytes of each of the warp's 32 rows are laid down (parts of 16 bytes, exchanged by the row's
