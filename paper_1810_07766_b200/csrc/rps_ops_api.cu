@@ -121,6 +121,27 @@ LcePlan plan_lce(const rps_lce_desc& d, const void* weight, bool backward, void*
     p.vocab = d.vocab, p.cols = d.cols, p.cols_padded = round_up(d.cols, 8), p.ignore_index = d.ignore_index;
     p.hidden_row = d.hidden_row, p.hidden_worker = d.hidden_worker;
     plan.lay_out_weight = p.f32 || !aligned_matrix(weight, d.weight_row, d.weight_worker);
+    plan_lce_dot(&p);
+    if (p.dot_rows > 0) {
+        Carver c{static_cast<unsigned char*>(workspace)};
+        p.count = c.take<int>(p.n);
+        p.rows = c.take<int>(p.n * p.tokens);
+        p.target = c.take<int>(p.n * p.tokens_padded);
+        if (backward) {
+            p.info = c.take<float2>(p.n * p.tokens_padded);
+            p.scale = c.take<float>(p.n);
+            p.dot_dl = c.take<float>(p.n * p.vocab * p.dot_rows);
+            p.dot_parts = c.take<float>(p.dot_ranges * p.n * p.dot_rows * round_up(p.cols, 4));
+        } else {
+            p.done = c.take<int>(p.n);
+            p.sums = c.take<float>(p.n * lce_merge_blocks(p.tokens));
+            p.stat_tiles = p.dot_blocks;
+            p.part = c.take<float2>(p.n * p.stat_tiles * p.tokens_padded);
+            p.hit = c.take<float>(p.n * p.tokens_padded);
+        }
+        plan.bytes = c.used;
+        return plan;
+    }
     const int64_t whole = round_up(d.vocab, kVocabTile);
     plan.piece = whole;
     const auto narrow = [&](int64_t bytes_per_column) {
@@ -228,6 +249,12 @@ extern "C" int rps_lce_forward(const rps_lce_desc* desc, const void* hidden, con
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     LceParams& p = plan.p;
     p.targets = targets, p.hidden = hidden, p.loss = loss, p.lse = lse;
+    if (p.dot_rows > 0) {
+        p.weight = weight, p.weight_row = d.weight_row, p.weight_worker = d.weight_worker;
+        RPS_TRY(launch_lce_dot(p, stream));
+        RPS_TRY(launch_lce_merge(p, stream));
+        return RPS_OK;
+    }
     RPS_TRY(launch_lce_rows(p, stream));
     if (d.tokens == 0) return RPS_OK;
     ProductParams g = plan.product;
@@ -259,6 +286,19 @@ extern "C" int rps_lce_backward(const rps_lce_desc* desc, const void* hidden, co
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     LceParams& p = plan.p;
     p.targets = targets, p.hidden = hidden, p.lse_in = lse, p.dloss = dloss, p.dhidden = dhidden;
+    if (p.dot_rows > 0) {
+        p.weight = weight, p.weight_row = d.weight_row, p.weight_worker = d.weight_worker;
+        p.dweight = dweight, p.dweight_row = d.dweight_row, p.dweight_worker = d.dweight_worker;
+        RPS_TRY(launch_lce_dot(p, stream));
+        RPS_TRY(launch_lce_dot_grads(p, stream));
+        ProductParams g{};
+        g.workers = p.n, g.planes = p.planes, g.count = p.count, g.rows = p.rows, g.tokens = p.tokens, g.scale = p.scale;
+        g.m = (int)d.tokens, g.n = (int)d.cols, g.splits = p.dot_ranges;
+        g.parts = p.dot_parts, g.part_rows = p.dot_rows, g.part_row = round_up(d.cols, 4);
+        g.out = dhidden, g.out_row = d.cols, g.out_worker = d.tokens * d.cols;
+        RPS_TRY(launch_join(Product::kDhidden, g, stream));
+        return RPS_OK;
+    }
     RPS_TRY(launch_lce_rows(p, stream));
     const Operand h = hidden_operand(p);
     for (int64_t v0 = 0; v0 < d.vocab; v0 += plan.piece) {

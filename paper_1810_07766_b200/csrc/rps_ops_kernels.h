@@ -118,7 +118,20 @@ struct LceParams {
     float* lse;
     float* sums;      // [n][lce_merge_blocks(tokens)]
     int* done;        // [n]
+    // a few tokens (dot_rows > 0): see rps_lce_dot.cu
+    int dot_rows, dot_blocks;          // room for tokens in dot_dl; CTAs of each worker that make logits
+    int dot_ranges, dot_wide, dot_high;  // of the gradients: ranges of the vocabulary; warps of a CTA along a row and over rows
+    const void* weight;
+    int64_t weight_row, weight_worker;
+    void* dweight;
+    int64_t dweight_row, dweight_worker;
+    float* dot_dl;                     // [n][vocab][dot_rows]
+    float* dot_parts;                  // [ranges][n][dot_rows][round_up(cols, 4)]: of dhidden
 };
+// Whether so few tokens go through dot products, and how; the rest of prm is set.
+void plan_lce_dot(LceParams* prm);
+cudaError_t launch_lce_dot(const LceParams& prm, cudaStream_t stream);         // statistics, or (backward) dl
+cudaError_t launch_lce_dot_grads(const LceParams& prm, cudaStream_t stream);   // dweight, and dhidden's parts
 
 // Which tokens take part, and their rows laid out.
 cudaError_t launch_lce_rows(const LceParams& prm, cudaStream_t stream);
@@ -179,6 +192,15 @@ cudaError_t launch_norm_backward(const NormParams& prm, cudaStream_t stream);
 __device__ __forceinline__ void after_the_kernel_before()
 {
     asm volatile("griddepcontrol.launch_dependents;\n\tgriddepcontrol.wait;" ::: "memory");
+}
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+__device__ __forceinline__ float exp2_fast(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
 }
 
 template <typename T>
