@@ -865,31 +865,38 @@ cudaError_t launch_pairs_or_not(const ProductParams& prm, cudaStream_t stream)
 // quarter of fp32's, where each copy has three products), and half B's.  So 76 tiles of 192 become 114 of 128 (two workers' 1048 x 4735 x 345 fp32: 65 -> 49 us), and a
 // small call's tiles so narrow that every place has one.  (Of many rounds the widest are best: 8192 x 8192 x 2048 bf16 in 4 rounds of
 // 256 columns 184 us, in 5 of 192 246 us.)  (4 workers of 32 tokens, 1000 words, 256 columns: the four products of a step 39 us with tiles of 256, 32 us with 128 and 64.)
+double block_time(int planes, int ctas, double tile)
+{
+    if (planes == 1) return 0.27 * (0.5 + 0.5 * tile / kTileN);
+    if (ctas == 2) return std::max(1.05, 0.45 + 0.0047 * tile);
+    return tile <= 128 ? std::max(1.03, 0.86 + 0.0027 * tile) : 0.0133 * tile;
+}
+
 ProductShape product_shape(int64_t m, int64_t n, int64_t k, int workers, int planes, bool may_split)
 {
     const int64_t halves = ceil_div(m > 0 ? m : 1, 128), whole = ceil_div(halves, 2);
     const int ctas = halves == 1 ? 1 : 2;
     const int64_t places = 148 / ctas, others = (ctas == 1 ? halves : whole) * workers, blocks = ceil_div(k, kDepth);
-    int64_t across = ceil_div(n, kTileN);
-    const double block = planes == 1 ? 0.27 : 1.6;
-    int best = 1;
+    const int64_t fewest = ceil_div(n, kTileN);
+    ProductShape best{};
     double least = 0.0;
-    for (int s = 1; s <= 32 && (s == 1 || (may_split && across * others < places && s * 4 <= blocks)); ++s) {
-        const int64_t items = across * others * s;
-        const double cost = (double)ceil_div(items, places) * ((double)ceil_div(blocks, s) * block + 1.0) + (s > 1 ? 5.0 + 0.05 * ctas * (double)items : 0.0);
-        if (s == 1 || cost < least) best = s, least = cost;
-    }
-    if (best == 1) {
-        const int64_t fewest = across, idle = std::max(across, std::min(places / others, n / 32));
-        double shortest = 0.0;
-        for (int64_t a = fewest; a <= (fewest * others <= 2 * places ? std::max(idle, fewest + 8) : fewest); a = a < fewest + 8 ? a + 1 : idle > a ? idle : a + 1) {
-            const int64_t tile = round_up(ceil_div(n, a), 32), tiles = ceil_div(n, tile);
-            const double part = (double)tile / kTileN, products = planes == 1 ? 0.5 + 0.5 * part : 0.25 + 0.75 * part;
-            const double cost = (double)ceil_div(tiles * others, places) * ((double)blocks * block * products + part + 0.5);
-            if (a == fewest || cost < shortest) across = a, shortest = cost;
+    const auto consider = [&](int64_t across) {
+        const int64_t tile = round_up(ceil_div(n, across), 32), tiles = ceil_div(n, tile) * others;
+        const double part = (double)tile / kTileN, block = block_time(planes, ctas, (double)tile);
+        for (int s = 1; s <= 32 && (s == 1 || (may_split && tiles < places && s * 4 <= blocks)); ++s) {
+            const double cost = (double)ceil_div(tiles * s, places) * ((double)ceil_div(blocks, s) * block + part + 0.5) +
+                                (s > 1 ? 5.0 + 0.05 * ctas * part * (double)(tiles * s) : 0.0);
+            if (best.ctas == 0 || cost < least) best = {(int)tile, s, ctas}, least = cost;
         }
+    };
+    // whole tiles, halves of them, up to eight more in a row, and one for every place
+    consider(fewest);
+    if (fewest * others <= 2 * places) {
+        for (int64_t a = fewest + 1; a < fewest + 8; ++a) consider(a);
+        consider(std::max(fewest, std::min(places / others, n / 32)));
     }
-    return {(int)round_up(ceil_div(n, across), 32), best, ctas};
+    if (planes == 3 && ctas == 1) consider(2 * fewest);
+    return best;
 }
 
 namespace {
