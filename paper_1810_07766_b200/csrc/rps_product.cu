@@ -39,10 +39,16 @@ constexpr int kMostStages = 24;                  // of narrower tiles and fewer 
 template <int PLANES>
 struct Epilogue {
     static constexpr int kParts = PLANES == 3 ? 2 : 4;
-    static constexpr int kWarps = 4 * kParts, kThreads = 32 * (2 + kWarps);
+    static constexpr int kWarps = 4 * kParts;
+    // Warps 0 and 1 issue copies and products; with fp32 the epilogue's are groups of four, whose registers are shared out anew.
+    static constexpr int kFirst = PLANES == 3 ? 4 : 2, kThreads = 32 * (kFirst + kWarps);
     static constexpr int kCols = kTileN / kParts;  // of a warp, at most
 };
 constexpr int kMostEpilogueWarps = Epilogue<1>::kWarps;
+// Registers of a thread with fp32, whose 128 columns a row left too few of the 168 that all threads alike can have, and what is spilled is far
+// away: nearly all of the SM's memory is shared memory here.  (The gradient above 219 -> 186 us, 3 of 5534 x 1020 32 -> 28.)
+constexpr int kLaunchRegisters = 168, kIssueRegisters = 72, kEpilogueRegisters = 216;
+static_assert(4 * kIssueRegisters + Epilogue<3>::kWarps * kEpilogueRegisters <= Epilogue<3>::kThreads / 32 * kLaunchRegisters, "the block's own");
 // The tensor cores cut an fp32 sum off after each step of 16 instead of rounding it, a bias that grows with the number of steps
 // (relative error of a 512-long sum of random terms: 5e-7).  Where fp32 accuracy is asked for, the summed axis goes
 // through in segments whose sums the epilogue adds in fp32, rounded: every 2 blocks of fp32 operands (48 steps), and every 16 blocks (64
@@ -56,7 +62,7 @@ static_assert(kTileN == kVocabTile && kTokenTile % 256 == 0 && kTokenBlock == kD
 // Rows leave through shared memory: a lane holds one row, and 32 lanes writing 16 bytes of 32 rows each would touch 32 lines at a time and
 // half a sector of each.  Instead 64 bytes of each of the warp's 32 rows are laid down (parts of 16 bytes, exchanged by the row's
 // number so that neither side has bank conflicts) and written out as 4 lanes to a row; rows that are not 16-byte aligned go out
-// element by element, still in the order of memory.  (Gradient of 8 fp32 weights of 10001 x 650, rows of 2600 bytes: 453 -> 225 us.)
+// element by element, still in the order of memory.  (Gradient of 8 fp32 weights of 10001 x 650, rows of 2600 bytes: 453 -> 186 us.)
 struct Staging {
     uint4 part[32][4];
 };
@@ -274,6 +280,8 @@ struct Rows {
     int index;
     int cols;   // that exist
     bool wide;  // rows are 16-byte aligned
+    int top;    // kDweight: the warp's first row, the others follow it
+    int rows;   // of them that exist
 };
 
 // Offset of row r of the warp, -1 if it is not written; all lanes ask.
@@ -299,8 +307,8 @@ __device__ __forceinline__ void set_offsets(StagingWithOffsets& stage, const Row
     stage.at[threadIdx.x % 32] = to.index < 0 ? -1 : (int64_t)to.index * to.stride;
 }
 
-// 64 bytes of each of the warp's rows, from column `c` on.  Loads come before stores, several at a time.  ADD, WHOLE: see store_rows.
-template <bool ADD, bool WHOLE, typename T, typename Stage>
+// 64 bytes of each of the warp's rows, from column `c` on.  Loads come before stores, several at a time.  ADD, WHOLE, RUN: see store_rows.
+template <bool ADD, bool WHOLE, bool RUN, typename T, typename Stage>
 __device__ __forceinline__ void store_chunk(Stage& stage, const uint4 (&mine)[4], const Rows<T>& to, int c)
 {
     constexpr int kChunk = 64 / sizeof(T), kPart = 16 / sizeof(T);  // columns
@@ -343,32 +351,50 @@ __device__ __forceinline__ void store_chunk(Stage& stage, const uint4 (&mine)[4]
             }
         }
     } else {
-        constexpr int kRows = 32 / kChunk, kAtATime = 8;  // rows that the warp writes at a time, an element to a lane: 2 of fp32, 1 of bf16
-        const int col = lane % kChunk;
+        // an element to a lane, rows kRows at a time (2 of fp32, 1 of bf16)
+        constexpr int kRows = 32 / kChunk, kAtATime = 8;
+        const int col = lane % kChunk, below = lane / kChunk;
         const bool there = c + col < to.cols;
+        if constexpr (RUN) {
+            T* at = to.out + (int64_t)(to.top + below) * to.stride + c + col;
 #pragma unroll 1
-        for (int r0 = 0; r0 < 32; r0 += kRows * kAtATime) {
-            T e[kAtATime];
-            int64_t row[kAtATime];
+            for (int r0 = 0; r0 < 32; r0 += kRows * kAtATime) {
+                T e[kAtATime];
 #pragma unroll
-            for (int i = 0; i < kAtATime; ++i) {
-                const int r = r0 + i * kRows + lane / kChunk;
-                row[i] = row_offset(stage, to, r);
-                e[i] = reinterpret_cast<const T*>(&stage.part[r][col / kPart ^ (r >> 1 & 3)])[col % kPart];
+                for (int i = 0; i < kAtATime; ++i) {
+                    const int r = r0 + i * kRows + below;
+                    e[i] = reinterpret_cast<const T*>(&stage.part[r][col / kPart ^ (r >> 1 & 3)])[col % kPart];
+                }
+#pragma unroll
+                for (int i = 0; i < kAtATime; ++i, at += (int64_t)kRows * to.stride)
+                    if (r0 + i * kRows + below < to.rows && there) store_element(at, e[i]);
             }
+        } else {
+#pragma unroll 1
+            for (int r0 = 0; r0 < 32; r0 += kRows * kAtATime) {
+                T e[kAtATime];
+                int64_t row[kAtATime];
 #pragma unroll
-            for (int i = 0; i < kAtATime; ++i)
-                if (row[i] >= 0 && there) store_element(to.out + row[i] + c + col, e[i]);
+                for (int i = 0; i < kAtATime; ++i) {
+                    const int r = r0 + i * kRows + below;
+                    row[i] = row_offset(stage, to, r);
+                    e[i] = reinterpret_cast<const T*>(&stage.part[r][col / kPart ^ (r >> 1 & 3)])[col % kPart];
+                }
+#pragma unroll
+                for (int i = 0; i < kAtATime; ++i)
+                    if (row[i] >= 0 && there) store_element(to.out + row[i] + c + col, e[i]);
+            }
         }
     }
 }
 
-// The warp's rows.  WHOLE: they are 16-byte aligned and `cols` a multiple of 16 bytes.  ADD: to what is there (fp32, WHOLE).
-template <bool ADD, bool WHOLE, typename T, int COLS, typename Stage>
+// The warp's rows.  WHOLE: they are 16-byte aligned and `cols` a multiple of 16 bytes.  ADD: to what is there (fp32, WHOLE).  RUN: they follow
+// one another from to.top on, so that a row's place needs no looking up (3 bf16 gradients of 5534 x 2047: 52 -> 33 us).
+template <bool ADD, bool WHOLE, bool RUN, typename T, int COLS, typename Stage>
 __device__ __forceinline__ void store_rows(Stage& stage, const float (&v)[COLS], const Rows<T>& to)
 {
     constexpr int kChunk = 64 / sizeof(T), kPart = 16 / sizeof(T);
-    set_offsets(stage, to);
+    if (WHOLE || !RUN || to.wide) set_offsets(stage, to);
 #pragma unroll
     for (int c = 0; c < COLS; c += kChunk) {
         if (c >= to.cols) break;
@@ -381,7 +407,7 @@ __device__ __forceinline__ void store_rows(Stage& stage, const float (&v)[COLS],
             else
                 mine[q] = make_uint4(two_bf16(f[0], f[1]), two_bf16(f[2], f[3]), two_bf16(f[4], f[5]), two_bf16(f[6], f[7]));
         }
-        store_chunk<ADD, WHOLE>(stage, mine, to, c);
+        store_chunk<ADD, WHOLE, RUN>(stage, mine, to, c);
     }
 }
 
@@ -410,7 +436,7 @@ __device__ __forceinline__ void store_parts(Stage& stage, float (&v)[COLS], Rows
                     word[j / 2] = two_bf16(f0, f1);
                 }
             }
-            store_chunk<false, true>(stage, mine, part_to, c);
+            store_chunk<false, true, false>(stage, mine, part_to, c);
         }
     }
 }
@@ -516,26 +542,28 @@ __device__ __forceinline__ void store_columns(const ProductParams& prm, int w, i
             }
         }
         const int64_t plane = prm.tokens_padded * prm.piece;
-        const Rows<bf16> to{prm.dl + w * PLANES * plane + n0, (int)prm.piece, info.index, width, true};
+        const Rows<bf16> to{prm.dl + w * PLANES * plane + n0, (int)prm.piece, info.index, width, true, 0, 0};
         if constexpr (PLANES == 1)
-            store_rows<false, true>(stage, v, to);
+            store_rows<false, true, false>(stage, v, to);
         else
             store_parts(stage, v, to, plane);
     } else {
         if (cols <= 0) return;
         if (prm.parts != nullptr) {
             const Rows<float> to{prm.parts + ((int64_t)split * prm.workers + w) * prm.part_rows * prm.part_row + n0, (int)prm.part_row, info.index, width,
-                                 true};
+                                 true, 0, 0};
             if (prm.add)
-                store_rows<true, true>(stage, v, to);
+                store_rows<true, true, false>(stage, v, to);
             else
-                store_rows<false, true>(stage, v, to);
+                store_rows<false, true, false>(stage, v, to);
             return;
         }
 #pragma unroll
         for (int j = 0; j < COLS; ++j) v[j] *= info.scale;
         using T = std::conditional_t<PLANES == 3, float, bf16>;
-        store_rows<false, false>(stage, v, Rows<T>{static_cast<T*>(prm.out) + w * prm.out_worker + n0, (int)prm.out_row, info.index, cols, wide});
+        const int top = row - (int)(threadIdx.x % 32);
+        store_rows<false, false, WHICH == Product::kDweight>(
+            stage, v, Rows<T>{static_cast<T*>(prm.out) + w * prm.out_worker + n0, (int)prm.out_row, info.index, cols, wide, top, min(32, prm.m - top)});
     }
 }
 
@@ -634,110 +662,114 @@ __global__ void __launch_bounds__(Epilogue<PLANES>::kThreads, 1)
     const uint64_t limit_ns = prm.wait_limit_ms > 0 ? (uint64_t)prm.wait_limit_ms * 1000000u : rps::kDefaultWaitLimitNs;
     const auto wait = [&](uint32_t bar, uint32_t parity) { return wait_for(bar, parity, limit_ns); };
 
-    if (warp == 0) {
-        if (lane == 0) {
-            int stage = 0, issued = 0;
-            uint32_t phase = 0;
-            for (int tile = blockIdx.x / CTAS; tile < total && fine; tile += groups) {
-                const Tile t = tile_at(tile);
-                const int m0 = t.m0 + rank * 128, n0 = t.n0 + rank * own_n;
-                const int wa = prm.a.worker != 0 ? t.w : 0, wb = prm.b.worker != 0 ? t.w : 0;
-                // a CTA's part that holds no row or column of the result is not copied: what the products read in its place reaches
-                // only results that are not stored
-                const int rows = WHICH == Product::kDweight ? prm.m : t.count;
-                const bool copy_a = m0 < rows, copy_b = n0 < prm.n;
-                const uint32_t bytes = (CTAS == 2 && t.m0 + 128 < rows ? 2 : 1) * a_bytes + (CTAS == 2 && t.n0 + own_n < prm.n ? 2 : 1) * b_bytes;
-                for (int i = 0; i < t.blocks * PLANES && prm.withhold_copies == 0; ++i) {
-                    fine = wait(smem_addr(&control.empty[stage]), phase ^ 1);
-                    if (!fine) break;
-                    const int kb = PLANES == 1 ? i : i / 3, plane = i - kb * PLANES, k0 = (t.first + kb) * kDepth;
-                    const uint32_t bar = in_first_cta(smem_addr(&control.full[stage]));
-                    if (rank == 0) mbar_arrive_expect_tx(smem_addr(&control.full[stage]), bytes);
-                    const uint32_t a = base + stage * (a_bytes + b_bytes), b = a + a_bytes;
-                    if (copy_a) {
-                        if (kAOther) {
-                            load_box<CTAS>(a, &maps.a, m0, k0, plane, wa, bar);
-                            load_box<CTAS>(a + kBoxBytes, &maps.a, m0 + 64, k0, plane, wa, bar);
-                        } else {
-                            load_box<CTAS>(a, &maps.a, k0, m0, plane, wa, bar);
+    if (warp < Epilogue<PLANES>::kFirst) {
+        if constexpr (PLANES == 3) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kIssueRegisters));
+        if (warp == 0) {
+            if (lane == 0) {
+                int stage = 0, issued = 0;
+                uint32_t phase = 0;
+                for (int tile = blockIdx.x / CTAS; tile < total && fine; tile += groups) {
+                    const Tile t = tile_at(tile);
+                    const int m0 = t.m0 + rank * 128, n0 = t.n0 + rank * own_n;
+                    const int wa = prm.a.worker != 0 ? t.w : 0, wb = prm.b.worker != 0 ? t.w : 0;
+                    // a CTA's part that holds no row or column of the result is not copied: what the products read in its place reaches
+                    // only results that are not stored
+                    const int rows = WHICH == Product::kDweight ? prm.m : t.count;
+                    const bool copy_a = m0 < rows, copy_b = n0 < prm.n;
+                    const uint32_t bytes = (CTAS == 2 && t.m0 + 128 < rows ? 2 : 1) * a_bytes + (CTAS == 2 && t.n0 + own_n < prm.n ? 2 : 1) * b_bytes;
+                    for (int i = 0; i < t.blocks * PLANES && prm.withhold_copies == 0; ++i) {
+                        fine = wait(smem_addr(&control.empty[stage]), phase ^ 1);
+                        if (!fine) break;
+                        const int kb = PLANES == 1 ? i : i / 3, plane = i - kb * PLANES, k0 = (t.first + kb) * kDepth;
+                        const uint32_t bar = in_first_cta(smem_addr(&control.full[stage]));
+                        if (rank == 0) mbar_arrive_expect_tx(smem_addr(&control.full[stage]), bytes);
+                        const uint32_t a = base + stage * (a_bytes + b_bytes), b = a + a_bytes;
+                        if (copy_a) {
+                            if (kAOther) {
+                                load_box<CTAS>(a, &maps.a, m0, k0, plane, wa, bar);
+                                load_box<CTAS>(a + kBoxBytes, &maps.a, m0 + 64, k0, plane, wa, bar);
+                            } else {
+                                load_box<CTAS>(a, &maps.a, k0, m0, plane, wa, bar);
+                            }
                         }
-                    }
-                    if (copy_b) {
-                        if (kBOther) {
-                            for (int c = 0; c < own_n; c += 64) load_box<CTAS>(b + c / 64 * kBoxBytes, &maps.b, n0 + c, k0, plane, wb, bar);
-                        } else {
-                            load_box<CTAS>(b, &maps.b, k0, n0, plane, wb, bar);
+                        if (copy_b) {
+                            if (kBOther) {
+                                for (int c = 0; c < own_n; c += 64) load_box<CTAS>(b + c / 64 * kBoxBytes, &maps.b, n0 + c, k0, plane, wb, bar);
+                            } else {
+                                load_box<CTAS>(b, &maps.b, k0, n0, plane, wb, bar);
+                            }
                         }
+                        ++issued;
+                        if (++stage == stages) stage = 0, phase ^= 1;
                     }
-                    ++issued;
-                    if (++stage == stages) stage = 0, phase ^= 1;
+                }
+                if (fine) {
+                    // the pair's arrivals on this CTA's barriers: all have come before it may end
+                    for (int i = 0; i < stages && fine; ++i) {
+                        fine = wait(smem_addr(&control.empty[stage]), phase ^ 1);
+                        if (++stage == stages) stage = 0, phase ^= 1;
+                    }
+                } else if (rank == 0) {
+                    // copies still on their way when a wait gave up: those of the last round of the ring at most
+                    for (int i = issued > stages ? issued - stages : 0; i < issued; ++i)
+                        wait(smem_addr(&control.full[i % stages]), i / stages & 1);
                 }
             }
-            if (fine) {
-                // the pair's arrivals on this CTA's barriers: all have come before it may end
-                for (int i = 0; i < stages && fine; ++i) {
-                    fine = wait(smem_addr(&control.empty[stage]), phase ^ 1);
-                    if (++stage == stages) stage = 0, phase ^= 1;
-                }
-            } else if (rank == 0) {
-                // copies still on their way when a wait gave up: those of the last round of the ring at most
-                for (int i = issued > stages ? issued - stages : 0; i < issued; ++i)
-                    wait(smem_addr(&control.full[i % stages]), i / stages & 1);
-            }
-        }
-    } else if (warp == 1) {
-        if (rank == 0 && lane == 0) {
-            const uint32_t descriptor = instruction_descriptor(kAOther, kBOther, kRows, tile_n);
-            // one product covers 16 of the summed axis: 32 bytes further along swizzled rows, or 16 rows of 128 bytes further
-            constexpr uint32_t a_step = (kAOther ? 2048 : 32) / 16, b_step = (kBOther ? 2048 : 32) / 16;
-            const uint32_t a_first = descriptor_low(base, kAOther), b_first = descriptor_low(base + a_bytes, kBOther), stage_step = (a_bytes + b_bytes) / 16;
-            int stage = 0, made = 0;
-            uint32_t phase = 0;
-            for (int tile = blockIdx.x / CTAS; tile < total && fine; tile += groups) {
-                const Tile t = tile_at(tile);
-                for (int kb = 0; kb < t.blocks && fine;) {
-                    const int buffer = made & 1, begin = kb, end = min(kb + segment, t.blocks);
-                    fine = wait(smem_addr(&control.sum_empty[buffer]), (made >> 1 & 1) ^ 1);
-                    if (!fine) break;
-                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint32_t sum = tensor_memory + buffer * kTileN;
-                    const auto block = [&](uint32_t a, uint32_t b, bool add) {
-#pragma unroll
-                        for (int k = 0; k < kDepth / 16; ++k) multiply<CTAS>(sum, a + k * a_step, b + k * b_step, descriptor, add || k > 0);
-                    };
-                    for (; kb < end; ++kb) {
-                        uint32_t a[PLANES], b[PLANES], freed[PLANES];
-#pragma unroll
-                        for (int q = 0; q < PLANES; ++q) {
-                            fine = fine && wait(smem_addr(&control.full[stage]), phase);
-                            a[q] = a_first + stage * stage_step, b[q] = b_first + stage * stage_step, freed[q] = smem_addr(&control.empty[stage]);
-                            if (++stage == stages) stage = 0, phase ^= 1;
-                        }
+        } else if (warp == 1) {
+            if (rank == 0 && lane == 0) {
+                const uint32_t descriptor = instruction_descriptor(kAOther, kBOther, kRows, tile_n);
+                // one product covers 16 of the summed axis: 32 bytes further along swizzled rows, or 16 rows of 128 bytes further
+                constexpr uint32_t a_step = (kAOther ? 2048 : 32) / 16, b_step = (kBOther ? 2048 : 32) / 16;
+                const uint32_t a_first = descriptor_low(base, kAOther), b_first = descriptor_low(base + a_bytes, kBOther), stage_step = (a_bytes + b_bytes) / 16;
+                int stage = 0, made = 0;
+                uint32_t phase = 0;
+                for (int tile = blockIdx.x / CTAS; tile < total && fine; tile += groups) {
+                    const Tile t = tile_at(tile);
+                    for (int kb = 0; kb < t.blocks && fine;) {
+                        const int buffer = made & 1, begin = kb, end = min(kb + segment, t.blocks);
+                        fine = wait(smem_addr(&control.sum_empty[buffer]), (made >> 1 & 1) ^ 1);
                         if (!fine) break;
                         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                        if constexpr (PLANES == 1) {
-                            block(a[0], b[0], kb > begin);
-                        } else {  // parts of A and B, the smallest products first, and a stage given back as soon as it has had its last
-                            block(a[2], b[0], kb > begin);
-                            block(a[0], b[2], true);
-                            commit<CTAS>(freed[2]);
-                            block(a[1], b[1], true);
-                            block(a[1], b[0], true);
-                            block(a[0], b[1], true);
-                            commit<CTAS>(freed[1]);
-                            block(a[0], b[0], true);
+                        const uint32_t sum = tensor_memory + buffer * kTileN;
+                        const auto block = [&](uint32_t a, uint32_t b, bool add) {
+#pragma unroll
+                            for (int k = 0; k < kDepth / 16; ++k) multiply<CTAS>(sum, a + k * a_step, b + k * b_step, descriptor, add || k > 0);
+                        };
+                        for (; kb < end; ++kb) {
+                            uint32_t a[PLANES], b[PLANES], freed[PLANES];
+#pragma unroll
+                            for (int q = 0; q < PLANES; ++q) {
+                                fine = fine && wait(smem_addr(&control.full[stage]), phase);
+                                a[q] = a_first + stage * stage_step, b[q] = b_first + stage * stage_step, freed[q] = smem_addr(&control.empty[stage]);
+                                if (++stage == stages) stage = 0, phase ^= 1;
+                            }
+                            if (!fine) break;
+                            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                            if constexpr (PLANES == 1) {
+                                block(a[0], b[0], kb > begin);
+                            } else {  // parts of A and B, the smallest products first, and a stage given back as soon as it has had its last
+                                block(a[2], b[0], kb > begin);
+                                block(a[0], b[2], true);
+                                commit<CTAS>(freed[2]);
+                                block(a[1], b[1], true);
+                                block(a[1], b[0], true);
+                                block(a[0], b[1], true);
+                                commit<CTAS>(freed[1]);
+                                block(a[0], b[0], true);
+                            }
+                            commit<CTAS>(freed[0]);
                         }
-                        commit<CTAS>(freed[0]);
+                        if (!fine) break;
+                        commit<CTAS>(smem_addr(&control.sum_full[buffer]));
+                        ++made;
                     }
-                    if (!fine) break;
-                    commit<CTAS>(smem_addr(&control.sum_full[buffer]));
-                    ++made;
                 }
             }
         }
     } else {
+        if constexpr (PLANES == 3) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kEpilogueRegisters));
         constexpr int kCols = Epilogue<PLANES>::kCols;
-        const int quarter = warp % 4, part = (warp - 2) / 4, part_n = tile_n / Epilogue<PLANES>::kParts;
+        const int quarter = warp % 4, part = (warp - Epilogue<PLANES>::kFirst) / 4, part_n = tile_n / Epilogue<PLANES>::kParts;
         const bool wide = (reinterpret_cast<uintptr_t>(prm.out) | (prm.out_row | prm.out_worker) * (PLANES == 3 ? 4 : 2)) % 16 == 0;
         int made = 0, turn = 0;
         const auto summed = [&] {
@@ -771,7 +803,7 @@ __global__ void __launch_bounds__(Epilogue<PLANES>::kThreads, 1)
                         for (int j = 0; j < 32; ++j) v[j] = 0.0f;
                     }
                     store_columns<WHICH, PLANES>(prm, t.w, t.split, row, n0 + c, min(32, part_n - c), t.count, info.target - c, info, v, wide,
-                                                 control.staging[warp - 2]);
+                                                 control.staging[warp - Epilogue<PLANES>::kFirst]);
                 }
                 if (t.blocks > 0 && idle) taken();
             } else {
@@ -790,7 +822,7 @@ __global__ void __launch_bounds__(Epilogue<PLANES>::kThreads, 1)
                 if constexpr (WHICH == Product::kLse)
                     fine = statistics<PLANES>(prm, t.w, row, n0, part_n, t.count, info, v, control, quarter, part, turn++, limit_ns);
                 else
-                    store_columns<WHICH, PLANES>(prm, t.w, t.split, row, n0, part_n, t.count, info.target, info, v, wide, control.staging_f32[warp - 2]);
+                    store_columns<WHICH, PLANES>(prm, t.w, t.split, row, n0, part_n, t.count, info.target, info, v, wide, control.staging_f32[warp - Epilogue<PLANES>::kFirst]);
             }
         }
     }
@@ -819,12 +851,24 @@ bool encode_operand(CUtensorMap* map, const Operand& o, int planes, int workers,
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// 0 if they cannot be asked for.
+template <typename Kernel>
+int registers_of(Kernel kernel)
+{
+    cudaFuncAttributes attributes{};
+    return cudaFuncGetAttributes(&attributes, kernel) == cudaSuccess ? attributes.numRegs : 0;
+}
+
 template <Product WHICH, int PLANES, int CTAS>
 cudaError_t launch(const ProductParams& prm, cudaStream_t stream)
 {
     static rps::LaunchState state;
     cudaError_t err = rps::grant_smem(state, rps_product_kernel<WHICH, PLANES, CTAS>, kSharedBytes);
     if (err != cudaSuccess) return err;
+    if constexpr (PLANES == 3) {  // the epilogue waits for registers that a smaller launch would never have
+        static const int registers = registers_of(rps_product_kernel<WHICH, PLANES, CTAS>);
+        if (registers != kLaunchRegisters) return cudaErrorLaunchOutOfResources;
+    }
     int sms = 0;
     if ((err = sm_count(&sms)) != cudaSuccess) return err;
     Maps maps{};
