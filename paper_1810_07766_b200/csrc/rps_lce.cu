@@ -6,7 +6,7 @@ namespace rps_ops {
 namespace {
 
 constexpr int kSelectThreads = 1024;
-constexpr int kMergeThreads = 512, kMergeRows = 32;
+constexpr int kMergeThreads = 512, kMergeRows = 8, kManyMergeRows = 32;
 constexpr int kRowThreads = 256;
 constexpr int kFewTokens = 4 * kRowThreads;
 
@@ -55,12 +55,13 @@ __global__ void __launch_bounds__(kRowThreads) rps_lce_gather_kernel(const LcePa
     __shared__ int row_of[SELECT ? kFewTokens : 1];
     const int w = blockIdx.y, lane = threadIdx.x % 32;
     const int64_t i = (int64_t)blockIdx.x * (kRowThreads / 32) + threadIdx.x / 32;
-    const int count = SELECT ? select_tokens<kRowThreads>(prm, w, blockIdx.x == 0, row_of) : prm.count[w], D = (int)prm.cols;
+    const int count = SELECT ? select_tokens<kRowThreads>(prm, w, blockIdx.x == 0 && blockIdx.z == 0, row_of) : prm.count[w], D = (int)prm.cols;
     const bool in = i < count;
+    const int c0 = (blockIdx.z * 32 + lane) * 8, step = gridDim.z * 256;
     const int64_t token = i < prm.tokens ? (SELECT ? row_of[i] : prm.rows[w * prm.tokens + i]) : 0;
     if (!in && i < prm.tokens && prm.backward) {  // an ignored token's gradient
         T* out = static_cast<T*>(prm.dhidden) + (w * prm.tokens + token) * prm.cols;
-        for (int c = lane; c < D; c += 32) out[c] = from_float<T>(0.0f);
+        for (int c = blockIdx.z * 32 + lane; c < D; c += gridDim.z * 32) out[c] = from_float<T>(0.0f);
     }
     // the product with dl over the tokens reads whole blocks of rows: those behind the last one are cleared
     if (i >= (count + kTokenBlock - 1) / kTokenBlock * kTokenBlock) return;
@@ -68,7 +69,7 @@ __global__ void __launch_bounds__(kRowThreads) rps_lce_gather_kernel(const LcePa
     bf16* dst = prm.packed + (w * prm.planes * prm.tokens_padded + i) * prm.cols_padded;
     const int64_t plane = prm.tokens_padded * prm.cols_padded;
 #pragma unroll 4
-    for (int c = lane * 8; c < prm.cols_padded; c += 256) {
+    for (int c = c0; c < prm.cols_padded; c += step) {
         float v[8];
         load_eight<T, ALIGN>(src, c, in ? D : 0, v);
         store_parts<T>(dst + c, plane, v);
@@ -106,18 +107,20 @@ __global__ void __launch_bounds__(kRowThreads) rps_planes_kernel(const PlanesPar
     }
 }
 
-// Joins the (maximum, sum) pairs of a row's vocabulary tiles: a CTA for 32 rows, a lane to a row so that reads are whole lines, the tiles
-// dealt to the 16 warps.  (One thread for all tiles of a row took 248 us for 4096 rows of 1024 tiles.)  The sum over a worker's
-// rows is made of the CTAs' sums by the one that finishes last, always in the same order.
+// Joins the (maximum, sum) pairs of a row's vocabulary tiles: a CTA for ROWS rows, whose pairs of a tile lie together, and 32 / ROWS tiles to a
+// warp at a time.  The sum over a worker's rows is made of the CTAs' sums by the one that finishes last, always in the same order.  8 rows
+// fill the SMs where 32 would not (4096 rows of 512 tiles 16 us against 25, 2048 of 196 6.0 against 10.4); where they would, fewer CTAs
+// to wait for are better (8192 rows of 32 tiles 13.1 against 7.7).
+template <int ROWS>
 __global__ void __launch_bounds__(kMergeThreads) rps_lce_merge_kernel(const LceParams prm)
 {
     after_the_kernel_before();
-    constexpr int kWarps = kMergeThreads / 32;
-    __shared__ float2 parts[kWarps][32];
+    constexpr int kSets = kMergeThreads / ROWS;  // of tiles
+    __shared__ float2 parts[kMergeThreads / 32][ROWS];
     const int w = blockIdx.y, count = prm.count[w], lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-    const int blocks = (count + kMergeRows - 1) / kMergeRows;
+    const int blocks = (count + ROWS - 1) / ROWS;
     if ((int)blockIdx.x >= blocks) return;
-    const int i = blockIdx.x * kMergeRows + lane;
+    const int i = blockIdx.x * ROWS + threadIdx.x % ROWS;
     float top = -INFINITY, sum = 0.0f;
     const auto join = [&](float2 p) {
         const float m = fmaxf(top, p.x), at = m == -INFINITY ? 0.0f : m;
@@ -127,29 +130,28 @@ __global__ void __launch_bounds__(kMergeThreads) rps_lce_merge_kernel(const LceP
     if (i < count) {
         const float2* part = prm.part + w * prm.stat_tiles * prm.tokens_padded + i;
         constexpr int kAtATime = 8;
-        for (int64_t v = warp; v < prm.stat_tiles; v += kWarps * kAtATime) {
+        for (int64_t v = threadIdx.x / ROWS; v < prm.stat_tiles; v += kSets * kAtATime) {
             float2 p[kAtATime];
 #pragma unroll
             for (int k = 0; k < kAtATime; ++k)
-                p[k] = v + k * kWarps < prm.stat_tiles ? __ldcs(part + (v + k * kWarps) * prm.tokens_padded) : make_float2(-INFINITY, 0.0f);
+                p[k] = v + k * kSets < prm.stat_tiles ? __ldcs(part + (v + k * kSets) * prm.tokens_padded) : make_float2(-INFINITY, 0.0f);
 #pragma unroll
             for (int k = 0; k < kAtATime; ++k) join(p[k]);
         }
     }
-    parts[warp][lane] = make_float2(top, sum);
-    __syncthreads();
-    // four warps take four parts each, then one the four
-    if (warp < 4) {
 #pragma unroll
-        for (int k = 1; k < kWarps / 4; ++k) join(parts[warp + 4 * k][lane]);
-        parts[warp][lane] = make_float2(top, sum);
-    }
+    for (int s = ROWS; s < 32; s *= 2) join(make_float2(__shfl_xor_sync(0xFFFFFFFFu, top, s), __shfl_xor_sync(0xFFFFFFFFu, sum, s)));
+    if (lane < ROWS) parts[warp][lane] = make_float2(top, sum);
     __syncthreads();
     if (warp != 0) return;
-    float loss = 0.0f;
-    if (i < count) {
+    // each lane some of the warps' pairs of a row, then the lanes of the row
+    top = -INFINITY, sum = 0.0f;
 #pragma unroll
-        for (int k = 1; k < 4; ++k) join(parts[k][lane]);
+    for (int k = 0; k < ROWS * kMergeThreads / 32 / 32; ++k) join(parts[lane / ROWS + k * (32 / ROWS)][lane % ROWS]);
+#pragma unroll
+    for (int s = ROWS; s < 32; s *= 2) join(make_float2(__shfl_xor_sync(0xFFFFFFFFu, top, s), __shfl_xor_sync(0xFFFFFFFFu, sum, s)));
+    float loss = 0.0f;
+    if (i < count && lane < ROWS) {
         const float lse = top + logf(sum);
         loss = lse - prm.hit[w * prm.tokens_padded + i];
         const int64_t t = prm.rows[w * prm.tokens + i];
@@ -177,7 +179,10 @@ __global__ void __launch_bounds__(kMergeThreads) rps_lce_merge_kernel(const LceP
 template <typename T, bool SELECT>
 cudaError_t gather(const LceParams& prm, cudaStream_t stream)
 {
-    const dim3 grid((unsigned)ceil_div(round_up(prm.tokens, kTokenBlock), kRowThreads / 32), (unsigned)prm.n);
+    const int64_t rows = ceil_div(round_up(prm.tokens, kTokenBlock), kRowThreads / 32), places = 148 * 4;
+    // few rows share their columns out, instead of a warp's turns along each (4 workers of 42 rows of 2530 fp32: 25 -> 6.5 us)
+    const int64_t along = std::max<int64_t>(1, std::min(ceil_div(prm.cols_padded, 256), places / (rows * prm.n)));
+    const dim3 grid((unsigned)rows, (unsigned)prm.n, (unsigned)along);
     const int align = aligned_source<T>(prm.hidden, prm.cols, prm.hidden_row, prm.hidden_worker);
     const auto kernel = align == 16  ? rps_lce_gather_kernel<T, 16, SELECT>
                         : align == 4 ? rps_lce_gather_kernel<T, 4, SELECT>
@@ -212,8 +217,9 @@ int64_t lce_merge_blocks(int64_t tokens) { return ceil_div(tokens, kMergeRows); 
 
 cudaError_t launch_lce_merge(const LceParams& prm, cudaStream_t stream)
 {
-    const dim3 grid((unsigned)lce_merge_blocks(prm.tokens), (unsigned)prm.n);
-    return launch_after(rps_lce_merge_kernel, grid, kMergeThreads, 0, stream, 1, prm);
+    const int64_t many = ceil_div(prm.tokens, kManyMergeRows);
+    if (many * prm.n >= 148) return launch_after(rps_lce_merge_kernel<kManyMergeRows>, dim3((unsigned)many, (unsigned)prm.n), kMergeThreads, 0, stream, 1, prm);
+    return launch_after(rps_lce_merge_kernel<kMergeRows>, dim3((unsigned)lce_merge_blocks(prm.tokens), (unsigned)prm.n), kMergeThreads, 0, stream, 1, prm);
 }
 
 cudaError_t launch_planes(const PlanesParams& prm, cudaStream_t stream)
