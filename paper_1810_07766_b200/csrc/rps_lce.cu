@@ -86,7 +86,7 @@ __global__ void __launch_bounds__(kRowThreads) rps_planes_kernel(const PlanesPar
     const uint32_t step = gridDim.x * kRowThreads;
     const T* src = static_cast<const T*>(prm.src) + w * prm.src_worker;
     bf16* dst = prm.dst + w * prm.dst_worker;
-    constexpr int kAtATime = 2;
+    constexpr int kAtATime = 4;
     for (uint64_t u0 = blockIdx.x * kRowThreads + threadIdx.x; u0 < total; u0 += (uint64_t)step * kAtATime) {
         float v[kAtATime][8];
         uint32_t row[kAtATime];

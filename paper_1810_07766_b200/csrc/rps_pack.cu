@@ -134,8 +134,8 @@ __global__ void __launch_bounds__(kThreads) rps_unpack_planes_kernel(const PackP
         for (int i = 0; i < kUnits; ++i) {
             if (u0 + (uint64_t)i * step >= units) break;
             if (at[i].c >= prm.dst_row) continue;
-            const int64_t w = at[i].row / prm.tokens;
-            bf16* dst = prm.planes_out + w * prm.dst_worker + (at[i].row - w * prm.tokens) * prm.dst_row + at[i].c;
+            const uint32_t row = (uint32_t)at[i].row, w = row / (uint32_t)prm.tokens;  // both below 2^32
+            bf16* dst = prm.planes_out + w * prm.dst_worker + (int64_t)(row - w * (uint32_t)prm.tokens) * prm.dst_row + at[i].c;
             float v[W];
             codes[i].values(scale[i], v);
             if constexpr (sizeof(T) == 2) {
