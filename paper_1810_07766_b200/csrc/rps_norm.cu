@@ -416,13 +416,23 @@ __global__ void __launch_bounds__(512) rps_norm_reduce_kernel(const NormParams p
     }
 }
 
-// Threads of a CTA and CTAs of a cluster for a row of `slices` 16-byte slices: the fewest threads (a power of two of
-// warps) that hold it, up to 512, then a cluster.
-void shape_of_row(int64_t slices, int* threads, int* cluster)
+// Threads of a CTA and CTAs of a cluster for a row of `slices` 16-byte slices: the fewest threads (a power of two of warps) that hold it, up
+// to 512, then a cluster.  `most` threads are resident on an SM at once, and a row of
+// a cluster of 3 or 4 takes 1.6 times as long as one of 2 (3.7 us forward, 2.5 backward: its sums go from CTA to CTA twice), so the cluster that
+// has most rows through in a given time is taken.  (2200 rows of 4488 fp32, forward + backward: 4 CTAs of 512 threads 174 + 253 us, 3
+// of 384 131 + 172, 4 of 288 and 3 of 384 114 + 152; 3126 rows of 4840 bf16: 2 of 512 84 + 104, 2 of 320 63 + 91, 3 of 224 124 backward.)
+void shape_of_row(int64_t slices, int most, int* threads, int* cluster)
 {
     *threads = 32, *cluster = 1;
     while (*threads < kMostThreads && *threads < slices) *threads *= 2;
-    while (*threads * *cluster < slices) *cluster *= 2;
+    if (*threads >= slices) return;
+    double best = 0.0;
+    for (int c = 2; c <= 8; ++c) {
+        const int64_t each = round_up(ceil_div(slices, c), 32);
+        if (each > kMostThreads) continue;
+        const double rate = (double)(148 * (most / each) / c) / (c == 2 ? 1.0 : 1.6 + 0.25 * std::max(0, c - 4));
+        if (rate > best) best = rate, *threads = (int)each, *cluster = c;
+    }
 }
 
 // `arrays` slices of each of kSlots rows to a thread in shared memory.
@@ -468,7 +478,7 @@ cudaError_t forward(NormParams prm, cudaStream_t stream)
 {
     const bool pack = prm.f_codes != nullptr;
     int threads = 0, sms = 0;
-    shape_of_row(ceil_div(pack ? prm.pitch : prm.cols, Slice<T>::kWidth), &threads, &prm.cluster);
+    shape_of_row(ceil_div(pack ? prm.pitch : prm.cols, Slice<T>::kWidth), kForwardThreads, &threads, &prm.cluster);
     cudaError_t err = sm_count(&sms);
     if (err != cudaSuccess) return err;
     const int align = common_alignment<T>(prm);
@@ -484,7 +494,7 @@ template <typename T>
 cudaError_t backward(NormParams prm, cudaStream_t stream)
 {
     int threads = 0;
-    shape_of_row(ceil_div(prm.cols, Slice<T>::kWidth), &threads, &prm.cluster);
+    shape_of_row(ceil_div(prm.cols, Slice<T>::kWidth), kBackwardThreads, &threads, &prm.cluster);
     const int align = common_alignment<T>(prm);
     const dim3 grid((unsigned)(prm.blocks * prm.cluster), (unsigned)prm.n);
     constexpr int kLeast = sizeof(T);
@@ -506,7 +516,7 @@ cudaError_t backward(NormParams prm, cudaStream_t stream)
 void plan_norm_backward(NormParams* prm)
 {
     int threads = 0, cluster = 0;
-    shape_of_row(ceil_div(prm->cols, prm->f32 ? Slice<float>::kWidth : Slice<bf16>::kWidth), &threads, &cluster);
+    shape_of_row(ceil_div(prm->cols, prm->f32 ? Slice<float>::kWidth : Slice<bf16>::kWidth), kBackwardThreads, &threads, &cluster);
     // as many blocks over all workers as are resident at once (512 threads of each of the 148 SMs); of the two nearest ways
     // to cut the rows the one whose longest SM has fewer of them
     int64_t want = (int64_t)148 * (kBackwardThreads / threads) / cluster / prm->n;
