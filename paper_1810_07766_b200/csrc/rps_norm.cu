@@ -13,6 +13,7 @@
 // second kernel adds the blocks' in a fixed order.
 #include <algorithm>
 
+#include "rps_cluster.cuh"
 #include "rps_kernels.h"
 #include "rps_rows.cuh"
 
@@ -25,49 +26,65 @@ constexpr int kForwardThreads = 1024, kBackwardThreads = 512;  // resident on an
 constexpr int kMostCluster = 8;
 constexpr int kMostWarps = kMostThreads / 32 * kMostCluster;
 
-__device__ __forceinline__ uint32_t cluster_rank()
-{
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
+// Set when a bounded wait gave up (rps_ops_check).
+__device__ int g_norm_gave_up = 0;
 
-// Room for the warps' sums of up to four values, double-buffered over successive rows, so that one barrier is enough.
+// Room for the warps' sums of up to four values, double-buffered over successive exchanges, so that one barrier is enough.
 struct Sums {
     float of[2][4][kMostWarps];
+    uint64_t arrived[2];  // of a cluster: counts the bytes
 };
 
-// A warp's sum of a value to every CTA that shares the row, and the barrier.
+// Of a cluster: before the first exchange.
+__device__ __forceinline__ void start_exchanges(Sums& sums)
+{
+    if (threadIdx.x == 0) {
+        for (int k = 0; k < 2; ++k) rps::mbar_init(rps::smem_addr(&sums.arrived[k]), 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncthreads();
+    cluster_sync();
+}
+
+// A warp's sum of each of `values` values to every CTA that shares the row, and the wait for all of them.  Some lanes (8 at least) have the sum of
+// a value, and `index` numbers them.  In a cluster each of them sends it to one CTA, whose barrier counts the bytes: a barrier of the whole
+// cluster would first see the stores of the row before through to memory (2200 rows of 4096 fp32: @@).  A warp sends
+// again only after it has read all sums of the exchange before, so nobody is more than one exchange ahead, and two rooms are enough.
 template <bool CLUSTER>
-__device__ __forceinline__ void exchange(float* slots, float v, bool mine, int cluster, uint32_t rank)
+__device__ __forceinline__ void exchange(Sums& sums, int turn, uint32_t parity, int value, int values, float v, int index, int cluster, uint32_t rank, bool& fine)
 {
     const int warps = blockDim.x / 32, warp = threadIdx.x / 32;
     if constexpr (!CLUSTER) {
-        if (mine) slots[warp] = v;
+        if (index == 0) sums.of[turn][value][warp] = v;
         __syncthreads();
     } else {
-        if (mine) {
-            const uint32_t own = (uint32_t)__cvta_generic_to_shared(&slots[rank * warps + warp]);
-            for (int k = 0; k < cluster; ++k) {
-                uint32_t there;
-                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(own), "r"(k));
-                asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(there), "f"(v) : "memory");
-            }
+        const uint32_t bar = rps::smem_addr(&sums.arrived[turn]);
+        if (threadIdx.x == 0) rps::mbar_arrive_expect_tx(bar, (uint32_t)(warps * cluster * values) * 4);
+        if (index < cluster) {
+            uint32_t there, counter;
+            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(rps::smem_addr(&sums.of[turn][value][rank * warps + warp])), "r"(index));
+            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(counter) : "r"(bar), "r"(index));
+            asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.b32 [%0], %1, [%2];" ::"r"(there), "r"(__float_as_uint(v)), "r"(counter)
+                         : "memory");
         }
         __syncwarp();
-        asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+        if (fine && !wait_for(bar, parity, rps::kDefaultWaitLimitNs)) {
+            fine = false;  // the rows' results are void from here on
+            atomicExch(&g_norm_gave_up, 1);
+        }
+        __syncwarp();
     }
 }
 
 // The sum of a value over the threads that share a row; every thread gets it, added in the same order.
 template <bool CLUSTER>
-__device__ __forceinline__ float row_sum(float v, Sums& sums, int turn, int cluster, uint32_t rank)
+__device__ __forceinline__ float row_sum(float v, Sums& sums, int turn, uint32_t parity, int cluster, uint32_t rank, bool& fine)
 {
     const int lane = threadIdx.x % 32, used = blockDim.x / 32 * cluster;
 #pragma unroll
     for (int s = 16; s > 0; s /= 2) v += __shfl_xor_sync(0xFFFFFFFFu, v, s);
     if (!CLUSTER && used == 1) return v;
-    exchange<CLUSTER>(sums.of[turn][0], v, lane == 0, cluster, rank);
+    exchange<CLUSTER>(sums, turn, parity, 0, 1, v, lane, cluster, rank, fine);
     if constexpr (!CLUSTER) {  // at most 16 warps
         v = lane % 16 < used ? sums.of[turn][0][lane % 16] : 0.0f;
     } else {
@@ -82,7 +99,7 @@ __device__ __forceinline__ float row_sum(float v, Sums& sums, int turn, int clus
 // The same of three values at a time: the lanes share the values out while they add (8 lanes to a value), 6 exchanges between lanes
 // instead of 15.
 template <bool CLUSTER>
-__device__ __forceinline__ void row_sums(float (&v)[3], Sums& sums, int turn, int cluster, uint32_t rank)
+__device__ __forceinline__ void row_sums(float (&v)[3], Sums& sums, int turn, uint32_t parity, int cluster, uint32_t rank, bool& fine)
 {
     const int lane = threadIdx.x % 32, used = blockDim.x / 32 * cluster, value = lane / 8;
     const bool high = lane & 16, odd = lane & 8;
@@ -94,7 +111,7 @@ __device__ __forceinline__ void row_sums(float (&v)[3], Sums& sums, int turn, in
 #pragma unroll
     for (int k = 4; k > 0; k /= 2) s += __shfl_xor_sync(0xFFFFFFFFu, s, k);
     if (CLUSTER || used > 1) {
-        exchange<CLUSTER>(sums.of[turn][value], s, lane % 8 == 0, cluster, rank);
+        exchange<CLUSTER>(sums, turn, parity, value, 4, s, lane % 8, cluster, rank, fine);
         s = 0.0f;
         for (int k = lane % 8; k < used; k += 8) s += sums.of[turn][value][k];
 #pragma unroll
@@ -117,6 +134,8 @@ __global__ void __launch_bounds__(kMostThreads, kForwardThreads / kMostThreads) 
     const uint32_t copied = (uint32_t)__cvta_generic_to_shared(ring);
     const int cluster = CLUSTER ? prm.cluster : 1, D = (int)prm.cols;
     const uint32_t rank = CLUSTER ? cluster_rank() : 0;
+    bool fine = true;
+    if (CLUSTER) start_exchanges(sums);
     const int c = ((int)rank * blockDim.x + threadIdx.x) * W;
     const int64_t rows = prm.n * prm.tokens, first = rows * (blockIdx.x / cluster) / (gridDim.x / cluster);
     const int count = (int)(rows * (blockIdx.x / cluster + 1) / (gridDim.x / cluster) - first);
@@ -181,7 +200,7 @@ __global__ void __launch_bounds__(kMostThreads, kForwardThreads / kMostThreads) 
         Pair s(0.0f);
 #pragma unroll
         for (int j = 0; j < P; ++j) s = fma(f[j], f[j], s);
-        const float r_f = rsqrtf(fmaf(row_sum<CLUSTER>(s.sum(), sums, 0, cluster, rank), inv, prm.eps));
+        const float r_f = rsqrtf(fmaf(row_sum<CLUSTER>(s.sum(), sums, 0, i & 1, cluster, rank, fine), inv, prm.eps));
         if constexpr (PACK) {
             const int64_t row = first + i;
             float v[W];
@@ -197,7 +216,7 @@ __global__ void __launch_bounds__(kMostThreads, kForwardThreads / kMostThreads) 
         }
         const uint4 h = narrow(x);
         store_slice<T, ALIGN>(h_rows + at, c, D, h);
-        const float r_h = rsqrtf(fmaf(row_sum<CLUSTER>(s.sum(), sums, 1, cluster, rank), inv, prm.eps));
+        const float r_h = rsqrtf(fmaf(row_sum<CLUSTER>(s.sum(), sums, 1, i & 1, cluster, rank, fine), inv, prm.eps));
         if constexpr (PACK) {
             const int64_t row = first + i;
             float stored[W];  // as a reader of h sees it
@@ -219,7 +238,10 @@ __global__ void __launch_bounds__(kMostThreads, kForwardThreads / kMostThreads) 
         }
     }
     // another CTA's sums may still be on their way here
-    if (CLUSTER) asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+    if (CLUSTER) {
+        __syncwarp();
+        cluster_sync();
+    }
 }
 
 template <typename T, int ALIGN, bool PACKED, bool CLUSTER>
@@ -232,6 +254,8 @@ __global__ void __launch_bounds__(kMostThreads, kBackwardThreads / kMostThreads)
     const uint32_t copied = (uint32_t)__cvta_generic_to_shared(ring);
     const int cluster = CLUSTER ? prm.cluster : 1, D = (int)prm.cols;
     const uint32_t rank = CLUSTER ? cluster_rank() : 0;
+    bool fine = true;
+    if (CLUSTER) start_exchanges(sums);
     const int c = ((int)rank * blockDim.x + threadIdx.x) * W;
     const float inv = 1.0f / (float)D;
     const int64_t block = blockIdx.x / cluster, w = blockIdx.y;
@@ -348,7 +372,7 @@ __global__ void __launch_bounds__(kMostThreads, kBackwardThreads / kMostThreads)
         }
         from += slot;
         if (from == end_of_ring) from -= kSlots * slot;
-        row_sums<CLUSTER>(s, sums, i & 1, cluster, rank);
+        row_sums<CLUSTER>(s, sums, i & 1, i >> 1 & 1, cluster, rank, fine);
         const float mean_h = s[0] * inv * r_h * r_h * r_h;
         const float mean_f = (s[1] - mean_h * s[2]) * inv * r_f * r_f * r_f;
         Pair df[P];
@@ -386,7 +410,10 @@ __global__ void __launch_bounds__(kMostThreads, kBackwardThreads / kMostThreads)
             }
         }
     }
-    if (CLUSTER) asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+    if (CLUSTER) {
+        __syncwarp();
+        cluster_sync();
+    }
 }
 
 // Sums of the blocks' sums: 32 columns to a CTA, the blocks dealt to its 16 warps, whose sums are added in their order.
@@ -512,6 +539,8 @@ cudaError_t backward(NormParams prm, cudaStream_t stream)
 }
 
 }  // namespace
+
+cudaError_t read_norm_gave_up(int* value, cudaStream_t stream) { return read_and_clear(g_norm_gave_up, value, stream); }
 
 void plan_norm_backward(NormParams* prm)
 {

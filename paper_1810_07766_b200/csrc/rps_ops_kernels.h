@@ -91,7 +91,8 @@ ProductShape product_shape(int64_t m, int64_t n, int64_t k, int workers, int pla
 
 cudaError_t launch_product(Product which, const ProductParams& prm, cudaStream_t stream);
 cudaError_t launch_join(Product which, const ProductParams& prm, cudaStream_t stream);  // the parts into `out`
-cudaError_t read_gave_up(int* value, cudaStream_t stream);  // and clears it; synchronises
+cudaError_t read_gave_up(int* value, cudaStream_t stream);  // whether a wait in a product gave up, and clears it; synchronises
+cudaError_t read_norm_gave_up(int* value, cudaStream_t stream);  // the same of a norm
 cudaError_t sm_count(int* out);                             // of the current device
 
 // ---------------------------------------------------------------------------------------------------- the loss
@@ -189,6 +190,17 @@ cudaError_t launch_norm_backward(const NormParams& prm, cudaStream_t stream);
 
 // ---------------------------------------------------------------------------------------------------- device helpers
 #ifdef __CUDACC__
+// A flag in device memory.
+inline cudaError_t read_and_clear(int& flag, int* value, cudaStream_t stream)
+{
+    const int zero = 0;
+    cudaError_t err = cudaMemcpyFromSymbolAsync(value, flag, sizeof(int), 0, cudaMemcpyDeviceToHost, stream);
+    if (err == cudaSuccess) err = cudaStreamSynchronize(stream);
+    if (err == cudaSuccess && *value != 0) err = cudaMemcpyToSymbolAsync(flag, &zero, sizeof(int), 0, cudaMemcpyHostToDevice, stream);
+    if (err == cudaSuccess) err = cudaStreamSynchronize(stream);
+    return err;
+}
+
 __device__ __forceinline__ void after_the_kernel_before()
 {
     asm volatile("griddepcontrol.launch_dependents;\n\tgriddepcontrol.wait;" ::: "memory");

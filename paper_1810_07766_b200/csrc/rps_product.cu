@@ -21,7 +21,7 @@
 #include <type_traits>
 
 #include "rps_ops_kernels.h"
-#include "rps_tma.cuh"
+#include "rps_cluster.cuh"
 
 namespace rps_ops {
 namespace {
@@ -94,18 +94,6 @@ struct Maps {
 };
 
 // ------------------------------------------------------------------------------------------------------ instructions
-__device__ __forceinline__ uint32_t cluster_rank()
-{
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
-
-__device__ __forceinline__ void cluster_sync()
-{
-    asm volatile("barrier.cluster.arrive;\n\tbarrier.cluster.wait;" ::: "memory");
-}
-
 // The address of the first CTA's copy of a shared variable.
 __device__ __forceinline__ uint32_t in_first_cta(uint32_t addr)
 {
@@ -121,29 +109,6 @@ __device__ __forceinline__ void arrive_cluster(uint32_t bar)
     asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
-// Waits for the phase with the given parity; what the pair did before it is then visible.  Gives up after limit_ns.
-__device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity)
-{
-    uint32_t done;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(done)
-        : "r"(bar), "r"(parity), "r"(rps::kSuspendHintNs)
-        : "memory");
-    return done != 0;
-}
-
-__device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, uint64_t limit_ns)
-{
-    if (try_wait(bar, parity)) return true;
-    const uint64_t start = rps::global_timer_ns();
-#pragma unroll 1
-    while (!try_wait(bar, parity))
-        if (rps::global_timer_ns() - start > limit_ns) return false;
-    return true;
-}
 
 // One box into this CTA's shared memory; its bytes are counted on the first CTA's barrier.
 template <int CTAS>
@@ -1024,15 +989,7 @@ cudaError_t launch_product(Product which, const ProductParams& prm, cudaStream_t
     }
 }
 
-cudaError_t read_gave_up(int* value, cudaStream_t stream)
-{
-    const int zero = 0;
-    cudaError_t err = cudaMemcpyFromSymbolAsync(value, g_gave_up, sizeof(int), 0, cudaMemcpyDeviceToHost, stream);
-    if (err == cudaSuccess) err = cudaStreamSynchronize(stream);
-    if (err == cudaSuccess && *value != 0) err = cudaMemcpyToSymbolAsync(g_gave_up, &zero, sizeof(int), 0, cudaMemcpyHostToDevice, stream);
-    if (err == cudaSuccess) err = cudaStreamSynchronize(stream);
-    return err;
-}
+cudaError_t read_gave_up(int* value, cudaStream_t stream) { return read_and_clear(g_gave_up, value, stream); }
 
 cudaError_t sm_count(int* out)
 {
