@@ -48,7 +48,7 @@ __device__ __forceinline__ void start_exchanges(Sums& sums)
 
 // A warp's sum of each of `values` values to every CTA that shares the row, and the wait for all of them.  Some lanes (8 at least) have the sum of
 // a value, and `index` numbers them.  In a cluster each of them sends it to one CTA, whose barrier counts the bytes: a barrier of the whole
-// cluster would first see the stores of the row before through to memory (2200 rows of 4096 fp32: @@).  A warp sends
+// cluster would first see the stores of the row before through to memory (2200 rows of 4096 fp32: 56 + 74 us, 43 + 57 so).  A warp sends
 // again only after it has read all sums of the exchange before, so nobody is more than one exchange ahead, and two rooms are enough.
 template <bool CLUSTER>
 __device__ __forceinline__ void exchange(Sums& sums, int turn, uint32_t parity, int value, int values, float v, int index, int cluster, uint32_t rank, bool& fine)
@@ -445,9 +445,10 @@ __global__ void __launch_bounds__(512) rps_norm_reduce_kernel(const NormParams p
 
 // Threads of a CTA and CTAs of a cluster for a row of `slices` 16-byte slices: the fewest threads (a power of two of warps) that hold it, up
 // to 512, then a cluster.  `most` threads are resident on an SM at once, and a row of
-// a cluster of 3 or 4 takes 1.6 times as long as one of 2 (3.7 us forward, 2.5 backward: its sums go from CTA to CTA twice), so the cluster that
-// has most rows through in a given time is taken.  (2200 rows of 4488 fp32, forward + backward: 4 CTAs of 512 threads 174 + 253 us, 3
-// of 384 131 + 172, 4 of 288 and 3 of 384 114 + 152; 3126 rows of 4840 bf16: 2 of 512 84 + 104, 2 of 320 63 + 91, 3 of 224 124 backward.)
+// a cluster of 3 or 4 takes 1.4 to 1.7 times as long as one of 2 (2.9 us forward, 1.9 backward: its sums go from CTA to CTA twice, or
+// once), so the cluster that has most rows through in a given time is taken.  (2200 rows of 4488 fp32, forward and backward: 4 CTAs of 288 threads and
+// 3 of 384 80 + 117 us; with 4 of 512 for both and slower exchanges 174 + 253.  3126 rows of 4840 bf16, both: 2 of 320 121, backward by 4 of
+// 160 instead 141.)
 void shape_of_row(int64_t slices, int most, int* threads, int* cluster)
 {
     *threads = 32, *cluster = 1;
