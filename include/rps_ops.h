@@ -119,6 +119,10 @@ typedef struct rps_norm_desc {
     int64_t post_worker, pre_worker, gate_worker;    /* strides between workers       */
     double scale;            /* finite                                                */
     double eps;              /* >= 0                                                  */
+    int32_t wait_limit_ms;   /* rows wider than a CTA holds (8 KB) are shared by CTAs that wait for one another's sums; every such
+                                wait gives up after this many milliseconds (0 = 2000) */
+    int32_t withhold_sums;   /* test aid for that: 1 = one CTA of each row sends no sums, so the others' waits run out, the rows'
+                                results are not written and rps_ops_check reports it; 0 otherwise */
 } rps_norm_desc;
 
 /* r_f, r_h: float [n][tokens], written for the backward pass; both may be NULL together.  f_codes, f_scales, h_codes,
@@ -176,8 +180,10 @@ int rps_wgrad_workspace(const rps_wgrad_desc* desc, const void* dy, size_t* byte
 int rps_packed_wgrad(const rps_wgrad_desc* desc, const void* dy, const int8_t* codes, const float* scales, void* dweight,
                      void* workspace, size_t workspace_bytes, void* cuda_stream);
 
-/* Every wait of the matrix-product kernels on data is bounded (two seconds, unless a description says otherwise); one that gives up ends its kernel early.
- * rps_ops_check synchronises the stream and returns RPS_ECUDA if that happened on the current device since the last check. */
+/* Every wait inside a kernel is bounded (two seconds, unless a description says otherwise): those of the matrix products on data, and those of the
+ * norms whose rows are shared by several CTAs on one another's sums.  One that gives up ends its kernel early; what the call had
+ * not written by then is not written, and what it has written is not valid.  rps_ops_check synchronises the stream and returns
+ * RPS_ECUDA if that happened on the current device since the last check. */
 int rps_ops_check(void* cuda_stream);
 
 /* Reason for the last failure of a function of this file on the calling thread ("" if none). */

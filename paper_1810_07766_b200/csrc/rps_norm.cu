@@ -46,12 +46,28 @@ __device__ __forceinline__ void start_exchanges(Sums& sums)
     cluster_sync();
 }
 
+// Of a cluster: after the last one.  No CTA may end while another's sums may still be on their way to it.  Where all waits were met they have
+// arrived; after one that ran out (its CTA may have had some of them sent just now) they are given time, once nobody sends any more.
+__device__ __forceinline__ void end_exchanges(bool fine)
+{
+    if (!fine) {
+        copies_arrived<0>();
+        if (threadIdx.x % 32 == 0) atomicExch(&g_norm_gave_up, 1);
+    }
+    __syncwarp();
+    cluster_sync();
+    if (!fine) __nanosleep(200000);
+}
+
 // A warp's sum of each of `values` values to every CTA that shares the row, and the wait for all of them.  Some lanes (8 at least) have the sum of
 // a value, and `index` numbers them.  In a cluster each of them sends it to one CTA, whose barrier counts the bytes: a barrier of the whole
 // cluster would first see the stores of the row before through to memory (2200 rows of 4096 fp32: 56 + 74 us, 43 + 57 so).  A warp sends
 // again only after it has read all sums of the exchange before, so nobody is more than one exchange ahead, and two rooms are enough.
+// A warp whose wait runs out (fine = false, for all of its lanes) is done: it neither arrives nor sends again, as a barrier must not be
+// arrived on twice in a phase, and so the others' waits run out one exchange later at most.
 template <bool CLUSTER>
-__device__ __forceinline__ void exchange(Sums& sums, int turn, uint32_t parity, int value, int values, float v, int index, int cluster, uint32_t rank, bool& fine)
+__device__ __forceinline__ void exchange(const NormParams& prm, Sums& sums, int turn, uint32_t parity, int value, int values, float v, int index, int cluster,
+                                         uint32_t rank, bool& fine)
 {
     const int warps = blockDim.x / 32, warp = threadIdx.x / 32;
     if constexpr (!CLUSTER) {
@@ -60,7 +76,7 @@ __device__ __forceinline__ void exchange(Sums& sums, int turn, uint32_t parity, 
     } else {
         const uint32_t bar = rps::smem_addr(&sums.arrived[turn]);
         if (threadIdx.x == 0) rps::mbar_arrive_expect_tx(bar, (uint32_t)(warps * cluster * values) * 4);
-        if (index < cluster) {
+        if (index < cluster && (prm.withhold_sums == 0 || rank + 1 < (uint32_t)cluster)) {
             uint32_t there, counter;
             asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(rps::smem_addr(&sums.of[turn][value][rank * warps + warp])), "r"(index));
             asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(counter) : "r"(bar), "r"(index));
@@ -68,23 +84,19 @@ __device__ __forceinline__ void exchange(Sums& sums, int turn, uint32_t parity, 
                          : "memory");
         }
         __syncwarp();
-        if (fine && !wait_for(bar, parity, rps::kDefaultWaitLimitNs)) {
-            fine = false;  // the rows' results are void from here on
-            atomicExch(&g_norm_gave_up, 1);
-        }
-        __syncwarp();
+        fine = __all_sync(0xFFFFFFFFu, wait_for(bar, parity, prm.wait_limit_ms > 0 ? (uint64_t)prm.wait_limit_ms * 1000000u : rps::kDefaultWaitLimitNs));
     }
 }
 
 // The sum of a value over the threads that share a row; every thread gets it, added in the same order.
 template <bool CLUSTER>
-__device__ __forceinline__ float row_sum(float v, Sums& sums, int turn, uint32_t parity, int cluster, uint32_t rank, bool& fine)
+__device__ __forceinline__ float row_sum(const NormParams& prm, float v, Sums& sums, int turn, uint32_t parity, int cluster, uint32_t rank, bool& fine)
 {
     const int lane = threadIdx.x % 32, used = blockDim.x / 32 * cluster;
 #pragma unroll
     for (int s = 16; s > 0; s /= 2) v += __shfl_xor_sync(0xFFFFFFFFu, v, s);
     if (!CLUSTER && used == 1) return v;
-    exchange<CLUSTER>(sums, turn, parity, 0, 1, v, lane, cluster, rank, fine);
+    exchange<CLUSTER>(prm, sums, turn, parity, 0, 1, v, lane, cluster, rank, fine);
     if constexpr (!CLUSTER) {  // at most 16 warps
         v = lane % 16 < used ? sums.of[turn][0][lane % 16] : 0.0f;
     } else {
@@ -99,7 +111,7 @@ __device__ __forceinline__ float row_sum(float v, Sums& sums, int turn, uint32_t
 // The same of three values at a time: the lanes share the values out while they add (8 lanes to a value), 6 exchanges between lanes
 // instead of 15.
 template <bool CLUSTER>
-__device__ __forceinline__ void row_sums(float (&v)[3], Sums& sums, int turn, uint32_t parity, int cluster, uint32_t rank, bool& fine)
+__device__ __forceinline__ void row_sums(const NormParams& prm, float (&v)[3], Sums& sums, int turn, uint32_t parity, int cluster, uint32_t rank, bool& fine)
 {
     const int lane = threadIdx.x % 32, used = blockDim.x / 32 * cluster, value = lane / 8;
     const bool high = lane & 16, odd = lane & 8;
@@ -111,7 +123,7 @@ __device__ __forceinline__ void row_sums(float (&v)[3], Sums& sums, int turn, ui
 #pragma unroll
     for (int k = 4; k > 0; k /= 2) s += __shfl_xor_sync(0xFFFFFFFFu, s, k);
     if (CLUSTER || used > 1) {
-        exchange<CLUSTER>(sums, turn, parity, value, 4, s, lane % 8, cluster, rank, fine);
+        exchange<CLUSTER>(prm, sums, turn, parity, value, 4, s, lane % 8, cluster, rank, fine);
         s = 0.0f;
         for (int k = lane % 8; k < used; k += 8) s += sums.of[turn][value][k];
 #pragma unroll
@@ -200,7 +212,8 @@ __global__ void __launch_bounds__(kMostThreads, kForwardThreads / kMostThreads) 
         Pair s(0.0f);
 #pragma unroll
         for (int j = 0; j < P; ++j) s = fma(f[j], f[j], s);
-        const float r_f = rsqrtf(fmaf(row_sum<CLUSTER>(s.sum(), sums, 0, i & 1, cluster, rank, fine), inv, prm.eps));
+        const float r_f = rsqrtf(fmaf(row_sum<CLUSTER>(prm, s.sum(), sums, 0, i & 1, cluster, rank, fine), inv, prm.eps));
+        if (CLUSTER && !fine) break;
         if constexpr (PACK) {
             const int64_t row = first + i;
             float v[W];
@@ -216,7 +229,8 @@ __global__ void __launch_bounds__(kMostThreads, kForwardThreads / kMostThreads) 
         }
         const uint4 h = narrow(x);
         store_slice<T, ALIGN>(h_rows + at, c, D, h);
-        const float r_h = rsqrtf(fmaf(row_sum<CLUSTER>(s.sum(), sums, 1, i & 1, cluster, rank, fine), inv, prm.eps));
+        const float r_h = rsqrtf(fmaf(row_sum<CLUSTER>(prm, s.sum(), sums, 1, i & 1, cluster, rank, fine), inv, prm.eps));
+        if (CLUSTER && !fine) break;
         if constexpr (PACK) {
             const int64_t row = first + i;
             float stored[W];  // as a reader of h sees it
@@ -237,11 +251,7 @@ __global__ void __launch_bounds__(kMostThreads, kForwardThreads / kMostThreads) 
             prm.r_h[first + i] = r_h;
         }
     }
-    // another CTA's sums may still be on their way here
-    if (CLUSTER) {
-        __syncwarp();
-        cluster_sync();
-    }
+    if (CLUSTER) end_exchanges(fine);
 }
 
 template <typename T, int ALIGN, bool PACKED, bool CLUSTER>
@@ -372,7 +382,8 @@ __global__ void __launch_bounds__(kMostThreads, kBackwardThreads / kMostThreads)
         }
         from += slot;
         if (from == end_of_ring) from -= kSlots * slot;
-        row_sums<CLUSTER>(s, sums, i & 1, i >> 1 & 1, cluster, rank, fine);
+        row_sums<CLUSTER>(prm, s, sums, i & 1, i >> 1 & 1, cluster, rank, fine);
+        if (CLUSTER && !fine) break;
         const float mean_h = s[0] * inv * r_h * r_h * r_h;
         const float mean_f = (s[1] - mean_h * s[2]) * inv * r_f * r_f * r_f;
         Pair df[P];
@@ -410,10 +421,7 @@ __global__ void __launch_bounds__(kMostThreads, kBackwardThreads / kMostThreads)
             }
         }
     }
-    if (CLUSTER) {
-        __syncwarp();
-        cluster_sync();
-    }
+    if (CLUSTER) end_exchanges(fine);
 }
 
 // Sums of the blocks' sums: 32 columns to a CTA, the blocks dealt to its 16 warps, whose sums are added in their order.

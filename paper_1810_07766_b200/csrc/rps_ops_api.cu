@@ -343,6 +343,8 @@ int check_norm(const rps_norm_desc* d)
     if (d->gates < 1 || (d->tokens > 0 ? d->tokens % d->gates != 0 : d->gates != 1))
         return fail(RPS_EINVAL, "gates = %lld does not divide tokens = %lld", (long long)d->gates, (long long)d->tokens);
     if (d->post_worker < 0 || d->pre_worker < 0 || d->gate_worker < 0) return fail(RPS_EINVAL, "negative stride between workers");
+    if (d->wait_limit_ms < 0 || d->withhold_sums < 0 || d->withhold_sums > 1)
+        return fail(RPS_EINVAL, "wait_limit_ms = %d, withhold_sums = %d", d->wait_limit_ms, d->withhold_sums);
     if (!std::isfinite(d->scale) || !std::isfinite(d->eps) || d->eps < 0) return fail(RPS_EINVAL, "scale = %g, eps = %g", d->scale, d->eps);
     return RPS_OK;
 }
@@ -355,6 +357,7 @@ NormParams norm_params(const rps_norm_desc& d)
     p.post_worker = d.post_worker, p.pre_worker = d.pre_worker, p.gate_worker = d.gate_worker;
     p.scale = (float)d.scale, p.eps = (float)d.eps;
     p.pitch = rps_pack_pitch(d.cols), p.groups = ceil_div(d.cols, RPS_PACK_GROUP);
+    p.wait_limit_ms = d.wait_limit_ms, p.withhold_sums = d.withhold_sums;
     if (d.tokens > 0) plan_norm_backward(&p);
     return p;
 }

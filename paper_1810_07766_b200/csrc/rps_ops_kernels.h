@@ -183,6 +183,7 @@ struct NormParams {
     // or hold whole groups (chunks == 0)
     int64_t rows_per_block, blocks, chunks;
     float* partial;  // [n][blocks][3][cols]: dpost, dpre, dgate
+    int wait_limit_ms, withhold_sums;  // 0: the default; see rps_norm_desc
 };
 void plan_norm_backward(NormParams* prm);
 cudaError_t launch_norm_forward(const NormParams& prm, cudaStream_t stream);

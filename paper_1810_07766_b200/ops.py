@@ -46,7 +46,8 @@ class rps_lce_desc(ctypes.Structure):
 
 class rps_norm_desc(ctypes.Structure):
     _fields_ = [("dtype", _i32), ("n", _i32), ("tokens", _i64), ("cols", _i64), ("gates", _i64), ("post_worker", _i64),
-                ("pre_worker", _i64), ("gate_worker", _i64), ("scale", _dbl), ("eps", _dbl)]
+                ("pre_worker", _i64), ("gate_worker", _i64), ("scale", _dbl), ("eps", _dbl), ("wait_limit_ms", _i32),
+                ("withhold_sums", _i32)]
 
 
 class rps_wgrad_desc(ctypes.Structure):
