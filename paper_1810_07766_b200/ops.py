@@ -498,6 +498,7 @@ def gated_residual_norm_forward(x: torch.Tensor, f: torch.Tensor, gate: torch.Te
     if keep not in ("values", "int8"):
         raise ValueError('keep must be "values" or "int8"')
     device = _device_of(x=x, f=f, gate=gate, post=post, pre=pre)
+    scale, eps = float(scale), float(eps)  # a number held in a tensor too: plans are kept by values, never by what holds one
     desc, between, r_layout, _, _ = _norm_plan(x, gate, post, pre, scale, eps)
     _same("f", f, x)
     h, y = torch.empty_like(x), torch.empty_like(x)
@@ -519,7 +520,7 @@ def gated_residual_norm_backward(dh: Optional[torch.Tensor], dy: torch.Tensor, k
     """(dx, df, dgate, dpost, dpre) for the gradients dh (None: none reaches h but through y) and dy of the forward call's h
     and y (``rps_norm_backward``)."""
     device = _device_of(dy=dy, gate=gate, post=post, pre=pre, r=kept.r)
-    desc, between, r_layout, size, ws_layout = _norm_plan(dy, gate, post, pre, scale, kept.eps)
+    desc, between, r_layout, size, ws_layout = _norm_plan(dy, gate, post, pre, float(scale), float(kept.eps))
     if dh is not None:
         _device_of(dy=dy, dh=dh)
         _same("dh", dh, dy)
@@ -578,4 +579,7 @@ class _GatedResidualNorm(torch.autograd.Function):
 def gated_residual_norm(x: torch.Tensor, f: torch.Tensor, gate: torch.Tensor, post: torch.Tensor, pre: torch.Tensor, *,
                         scale: float = 1.0, eps: float = 1e-6, keep: str = "values") -> Tuple[torch.Tensor, torch.Tensor]:
     """Differentiable ``gated_residual_norm_forward``: (h, y)."""
-    return _GatedResidualNorm.apply(x, f, gate, post, pre, scale, eps, keep)
+    for name, v in (("scale", scale), ("eps", eps)):
+        if isinstance(v, torch.Tensor) and v.requires_grad and torch.is_grad_enabled():
+            raise ValueError(f"{name} gets no gradient: a learned factor belongs into gate or post")
+    return _GatedResidualNorm.apply(x, f, gate, post, pre, float(scale), float(eps), keep)
