@@ -432,6 +432,9 @@ def linear_8bit(x: torch.Tensor, weight: torch.Tensor) -> torch.Tensor:
     or both without ``n``.  The two plain products are PyTorch's."""
     if x.dim() != weight.dim() or x.dim() not in (2, 3):
         raise ValueError("x must be [n, tokens, cols] with weight [n, outs, cols], or [tokens, cols] with [outs, cols]")
+    _device_of(x=x, weight=weight)
+    _check("x", x, None, tuple(x.shape))
+    _check("weight", weight, x, tuple(x.shape[:-2]) + (weight.shape[-2], x.shape[-1]))
     return _Linear8bit.apply(x, weight)
 
 

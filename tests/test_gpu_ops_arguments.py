@@ -41,3 +41,17 @@ def test_a_scale_that_wants_a_gradient_is_refused(ops):  # noqa: F811
     s = norm_inputs("f32", 1, 8, 40, 1)
     with pytest.raises(ValueError, match="scale"):
         ops.gated_residual_norm(*(s[k] for k in ("x", "f", "gate", "post", "pre")), scale=torch.tensor(0.5, requires_grad=True))
+
+
+@pytest.mark.parametrize("x,weight", [((1, 5, 8), (2, 6, 8)), ((2, 5, 8), (1, 6, 8)), ((5, 8), (6, 9)), ((2, 5, 8), (3, 6, 8))])
+def test_linear_8bit_of_shapes_that_do_not_go_together(ops, x, weight):  # noqa: F811
+    """Refused before the product, not at its gradient."""
+    with pytest.raises(ValueError, match="weight"):
+        ops.linear_8bit(torch.ones(x, device="cuda"), torch.ones(weight, device="cuda"))
+
+
+def test_linear_8bit_of_two_types_or_places(ops):  # noqa: F811
+    x, w = torch.ones(5, 8, device="cuda"), torch.ones(6, 8, device="cuda")
+    for a, b in ((x.bfloat16(), w), (x, w.bfloat16()), (x.double(), w.double()), (x, w.cpu()), (x.cpu(), w)):
+        with pytest.raises(ValueError):
+            ops.linear_8bit(a, b)
