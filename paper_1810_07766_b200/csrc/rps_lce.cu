@@ -82,7 +82,7 @@ __global__ void __launch_bounds__(kRowThreads) rps_planes_kernel(const PlanesPar
 {
     after_the_kernel_before();
     const int w = blockIdx.y, per_row = (int)(prm.dst_row / 8);
-    const uint32_t total = (uint32_t)(prm.rows * per_row);  // below 2^32: the matrix has 16 bytes for each
+    const uint32_t total = (uint32_t)(prm.rows * per_row);  // below 2^32 (launch_planes)
     const uint32_t step = gridDim.x * kRowThreads;
     const T* src = static_cast<const T*>(prm.src) + w * prm.src_worker;
     bf16* dst = prm.dst + w * prm.dst_worker;
@@ -222,9 +222,18 @@ cudaError_t launch_lce_merge(const LceParams& prm, cudaStream_t stream)
     return launch_after(rps_lce_merge_kernel<kMergeRows>, dim3((unsigned)lce_merge_blocks(prm.tokens), (unsigned)prm.n), kMergeThreads, 0, stream, 1, prm);
 }
 
+// A launch counts its pieces of 16 bytes in 32 bits, so a matrix of 64 GiB and more takes several.
 cudaError_t launch_planes(const PlanesParams& prm, cudaStream_t stream)
 {
-    return prm.f32 ? planes<float>(prm, stream) : planes<bf16>(prm, stream);
+    const int64_t most = ((1ll << 32) - 1) / (prm.dst_row / 8);
+    for (int64_t row = 0; row < prm.rows; row += most) {
+        PlanesParams q = prm;
+        q.rows = std::min(most, prm.rows - row);
+        q.src = static_cast<const unsigned char*>(prm.src) + row * prm.src_row * (prm.f32 ? 4 : 2), q.dst = prm.dst + row * prm.dst_row;
+        const cudaError_t err = q.f32 ? planes<float>(q, stream) : planes<bf16>(q, stream);
+        if (err != cudaSuccess) return err;
+    }
+    return cudaSuccess;
 }
 
 }  // namespace rps_ops
