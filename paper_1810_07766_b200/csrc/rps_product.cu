@@ -56,6 +56,9 @@ static_assert(4 * kIssueRegisters + Epilogue<3>::kWarps * kEpilogueRegisters <= 
 // cycles of the products of the next one.  (Segments of 4 blocks for dl, whose tiles' ends then hold the next products up less: 8 x 500
 // x 10001 x 650 fp32 256 -> 238 us, errors of the gradients 6e-7 -> 9e-7; not taken.)
 constexpr int kSegmentF32 = 2, kSegmentStatistics = 16;  // in blocks of kDepth
+// bf16 results are rounded to 2^-9 of their size anyhow, but not after any number of steps: of a sum of terms of one sign each step cuts off 1e-7 of
+// what it ends at (measured over 2^19 tokens: 3.2e-3 in one run, 1.3e-4 in runs of 2048 steps, which are these).
+constexpr int kSegmentBf16 = 512;  // LONG: a kernel of its own, as the sums between segments take the registers of the others' epilogue
 
 static_assert(kTileN == kVocabTile && kTokenTile % 256 == 0 && kTokenBlock == kDepth, "operands are padded to whole tiles");
 
@@ -81,6 +84,15 @@ struct Control {
     int count[RPS_MAX_WORKERS];      // tokens of each worker that take part
     int start[RPS_MAX_WORKERS + 1];  // first tile of each worker
 };
+
+template <int PLANES>
+__device__ __forceinline__ auto& staging_of(Control& control)
+{
+    if constexpr (PLANES == 3)
+        return control.staging_f32;
+    else
+        return control.staging;
+}
 
 constexpr int kSharedBytes = 1024 + kRingBytes + (int)sizeof(Control);
 // The products read 128 rows of A whatever part of them a stage holds; behind the last stage lies Control.
@@ -533,7 +545,7 @@ __device__ __forceinline__ void store_columns(const ProductParams& prm, int w, i
 }
 
 // ------------------------------------------------------------------------------------------------------------ kernel
-template <Product WHICH, int PLANES, int CTAS>
+template <Product WHICH, int PLANES, int CTAS, bool LONG>
 __global__ void __launch_bounds__(Epilogue<PLANES>::kThreads, 1)
     rps_product_kernel(const __grid_constant__ ProductParams prm, const __grid_constant__ Maps maps)
 {
@@ -622,7 +634,7 @@ __global__ void __launch_bounds__(Epilogue<PLANES>::kThreads, 1)
         return t;
     };
     // blocks to a segment
-    const int segment = PLANES == 3 ? kSegmentF32 : WHICH == Product::kLse ? kSegmentStatistics : 1 << 30;
+    const int segment = PLANES == 3 ? kSegmentF32 : WHICH == Product::kLse ? kSegmentStatistics : LONG ? kSegmentBf16 : 1 << 30;
     bool fine = true;
     const uint64_t limit_ns = prm.wait_limit_ms > 0 ? (uint64_t)prm.wait_limit_ms * 1000000u : rps::kDefaultWaitLimitNs;
     const auto wait = [&](uint32_t bar, uint32_t parity) { return wait_for(bar, parity, limit_ns); };
@@ -755,7 +767,8 @@ __global__ void __launch_bounds__(Epilogue<PLANES>::kThreads, 1)
             // a warp none of whose rows is wanted only keeps step
             const bool idle = t.m0 + (int)rank * 128 + quarter * 32 >= (WHICH == Product::kDweight ? prm.m : WHICH == Product::kDlogits ? (t.count + kDepth - 1) / kDepth * kDepth : t.count);
             const uint32_t columns = tensor_memory + ((uint32_t)(quarter * 32) << 16) + part * part_n;
-            if constexpr (PLANES == 1 && WHICH != Product::kLse) {  // one segment
+            auto& staging = staging_of<PLANES>(control)[warp - Epilogue<PLANES>::kFirst];
+            if constexpr (PLANES == 1 && WHICH != Product::kLse && !LONG) {  // one segment
                 if (t.blocks > 0 && !summed()) break;
 #pragma unroll 1
                 for (int c = 0; c < part_n && !idle; c += 32) {
@@ -767,8 +780,7 @@ __global__ void __launch_bounds__(Epilogue<PLANES>::kThreads, 1)
 #pragma unroll
                         for (int j = 0; j < 32; ++j) v[j] = 0.0f;
                     }
-                    store_columns<WHICH, PLANES>(prm, t.w, t.split, row, n0 + c, min(32, part_n - c), t.count, info.target - c, info, v, wide,
-                                                 control.staging[warp - Epilogue<PLANES>::kFirst]);
+                    store_columns<WHICH, PLANES>(prm, t.w, t.split, row, n0 + c, min(32, part_n - c), t.count, info.target - c, info, v, wide, staging);
                 }
                 if (t.blocks > 0 && idle) taken();
             } else {
@@ -787,7 +799,7 @@ __global__ void __launch_bounds__(Epilogue<PLANES>::kThreads, 1)
                 if constexpr (WHICH == Product::kLse)
                     fine = statistics<PLANES>(prm, t.w, row, n0, part_n, t.count, info, v, control, quarter, part, turn++, limit_ns);
                 else
-                    store_columns<WHICH, PLANES>(prm, t.w, t.split, row, n0, part_n, t.count, info.target, info, v, wide, control.staging_f32[warp - Epilogue<PLANES>::kFirst]);
+                    store_columns<WHICH, PLANES>(prm, t.w, t.split, row, n0, part_n, t.count, info.target, info, v, wide, staging);
             }
         }
     }
@@ -824,14 +836,14 @@ int registers_of(Kernel kernel)
     return cudaFuncGetAttributes(&attributes, kernel) == cudaSuccess ? attributes.numRegs : 0;
 }
 
-template <Product WHICH, int PLANES, int CTAS>
+template <Product WHICH, int PLANES, int CTAS, bool LONG>
 cudaError_t launch(const ProductParams& prm, cudaStream_t stream)
 {
     static rps::LaunchState state;
-    cudaError_t err = rps::grant_smem(state, rps_product_kernel<WHICH, PLANES, CTAS>, kSharedBytes);
+    cudaError_t err = rps::grant_smem(state, rps_product_kernel<WHICH, PLANES, CTAS, LONG>, kSharedBytes);
     if (err != cudaSuccess) return err;
     if constexpr (PLANES == 3) {  // the epilogue waits for registers that a smaller launch would never have
-        static const int registers = registers_of(rps_product_kernel<WHICH, PLANES, CTAS>);
+        static const int registers = registers_of(rps_product_kernel<WHICH, PLANES, CTAS, LONG>);
         if (registers != kLaunchRegisters) return cudaErrorLaunchOutOfResources;
     }
     int sms = 0;
@@ -848,13 +860,17 @@ cudaError_t launch(const ProductParams& prm, cudaStream_t stream)
     }
     const int64_t tiles = ceil_div(p.m, 128 * CTAS) * ceil_div(p.n, p.tile_cols) * p.workers * p.splits;
     const int groups = (int)(tiles < sms / CTAS ? tiles : sms / CTAS);
-    return launch_after(rps_product_kernel<WHICH, PLANES, CTAS>, dim3(CTAS * groups), Epilogue<PLANES>::kThreads, kSharedBytes, stream, CTAS, p, maps);
+    return launch_after(rps_product_kernel<WHICH, PLANES, CTAS, LONG>, dim3(CTAS * groups), Epilogue<PLANES>::kThreads, kSharedBytes, stream, CTAS, p, maps);
 }
 
 template <Product WHICH, int PLANES>
 cudaError_t launch_pairs_or_not(const ProductParams& prm, cudaStream_t stream)
 {
-    return prm.ctas == 2 ? launch<WHICH, PLANES, 2>(prm, stream) : launch<WHICH, PLANES, 1>(prm, stream);
+    if constexpr (PLANES == 1 && WHICH != Product::kLse) {  // the others have segments in any case
+        const int64_t run = ceil_div(ceil_div(prm.k, kDepth), std::max(prm.splits, 1));
+        if (run > kSegmentBf16) return prm.ctas == 2 ? launch<WHICH, PLANES, 2, true>(prm, stream) : launch<WHICH, PLANES, 1, true>(prm, stream);
+    }
+    return prm.ctas == 2 ? launch<WHICH, PLANES, 2, false>(prm, stream) : launch<WHICH, PLANES, 1, false>(prm, stream);
 }
 
 }  // namespace

@@ -3,9 +3,51 @@ with more pieces than 32 bits count."""
 import pytest
 import torch
 
-from test_gpu_ops_loss import E32, ops  # noqa: F401
+from test_gpu_ops_loss import E32, check, inputs, ops  # noqa: F401
 
 pytestmark = pytest.mark.gpu
+
+
+def test_sums_over_many_tokens_are_not_cut_off(ops):  # noqa: F811
+    """The tensor cores cut a sum off after each 16 terms.  2^19 tokens are 32768 such steps, which of a sum of terms of one sign take 3.2e-3 in one
+    run; in runs of a few thousand steps it has to be 2.4e-4 at most, far below the rounding of a bf16 result (2e-3).  That rounding averages out
+    here: the results' sizes are spread over a factor of four."""
+    T, O, D = 1 << 19, 2304, 2304
+    g = torch.Generator(device="cuda").manual_seed(1)
+    dy = torch.empty(T, O, dtype=torch.bfloat16, device="cuda")
+    codes = torch.empty(T, D, dtype=torch.int8, device="cuda")
+    scales = torch.full((T, D // 128), 2.0 ** -7, device="cuda")
+    up = torch.linspace(1, 2, O, device="cuda")
+    want = torch.zeros(O, D, dtype=torch.float64, device="cuda")
+    for t in range(0, T, 1 << 15):
+        part = slice(t, t + (1 << 15))
+        dy[part] = (torch.rand(1 << 15, O, generator=g, device="cuda") * 0.5 + 0.5) * up
+        codes[part] = ((torch.rand(1 << 15, D, generator=g, device="cuda") * 30 + 30) * up).to(torch.int8)
+        want += dy[part].double().T @ (codes[part].double() * 2.0 ** -7)
+    got = ops.packed_weight_grad(dy, ops.PackedActivation(codes, scales, D, torch.bfloat16))
+    off = got.double() / want - 1
+    assert abs(float(off.mean())) <= 2.4e-4, float(off.mean())
+    assert float(off.abs().max()) <= 2.0 ** -8 + 5e-4
+
+
+def test_long_sums_of_odd_widths(ops):  # noqa: F811
+    """Sums of more steps than one run holds, into rows that are not 16-byte aligned and past their last column."""
+    T, O, D = 66000, 2303, 2311
+    g = torch.Generator(device="cuda").manual_seed(6)
+    dy = torch.randn(1, T, O, generator=g, device="cuda").bfloat16()
+    p = ops.pack_activation(torch.randn(1, T, D, generator=g, device="cuda").bfloat16())
+    x = ops.unpack_activation(p).double()   # as the product takes them: rounded to bf16
+    out = torch.full((1, O, D + 1), 7.0, dtype=torch.bfloat16, device="cuda")
+    ops.packed_weight_grad(dy, p, dweight=out[:, :, :D])
+    want, size = dy[0].double().T @ x[0], dy[0].double().abs().T @ x[0].abs()
+    assert (out[:, :, D] == 7).all()
+    assert ((out[0, :, :D] - want).abs() <= 4096 * E32 * size + 2.0 ** -8 * want.abs()).all()
+    assert (out[0, :, :D] - want).norm() <= 2.0 ** -8 * want.norm()
+
+
+@pytest.mark.parametrize("T,V,D", [(2048, 70000, 2560), (5, 40, 70000)])  # dhidden sums over the words, logits over the columns
+def test_long_sums_of_the_loss(ops, T, V, D):  # noqa: F811
+    check(ops, "bf16", *inputs("bf16", 1, T, V, D, seed=7))
 
 
 def test_operands_of_more_than_2_to_the_32_pieces(ops):  # noqa: F811
