@@ -143,7 +143,7 @@ __global__ void __launch_bounds__(kThreads, kResident<ROWS>) rps_lce_dot_kernel(
     const int target = in && y >= 0 && y < V ? (int)y : -1;
     float lse = 0.0f, g = 0.0f, top = -INFINITY, sum = 0.0f;
     if (BACKWARD && in) {
-        lse = prm.lse_in[token] * kLog2e;
+        lse = prm.lse_in[token];
         g = target < 0 ? nanf("") : prm.reduction == RPS_REDUCE_NONE ? prm.dloss[token] : 1.0f;
     }
     __syncthreads();
@@ -184,7 +184,7 @@ __global__ void __launch_bounds__(kThreads, kResident<ROWS>) rps_lce_dot_kernel(
         const float l = logit[0];
         if (at >= end) continue;
         if constexpr (BACKWARD) {
-            const float p = exp2_fast(fmaf(l, kLog2e, -lse)) - (at == target ? 1.0f : 0.0f);
+            const float p = exp_of_difference(l, lse) - (at == target ? 1.0f : 0.0f);
             if (first) prm.dot_dl[((int64_t)w * V + at) * ROWS + t] = in ? g * p : 0.0f;
         } else if (in) {
             if (at == target && first) const_cast<float*>(prm.hit)[w * prm.tokens_padded + t] = l;

@@ -20,8 +20,8 @@
 #include <mutex>
 #include <type_traits>
 
-#include "rps_ops_kernels.h"
 #include "rps_cluster.cuh"
+#include "rps_rows.cuh"
 
 namespace rps_ops {
 namespace {
@@ -464,7 +464,8 @@ __device__ __forceinline__ bool statistics(const ProductParams& prm, int w, int 
 #pragma unroll
         for (int j = c; j < c + 32; ++j) top = fmaxf(top, v[j]);
     }
-    const float at = top == -INFINITY ? 0.0f : top * kLog2e;
+    const float at = top == -INFINITY ? 0.0f : top;
+    Pair total(0.0f);
 #pragma unroll
     for (int c = 0; c < COLS; c += 32) {
         if (c >= cols) break;
@@ -476,8 +477,9 @@ __device__ __forceinline__ bool statistics(const ProductParams& prm, int w, int 
             prm.hit[w * prm.tokens_padded + row] = hit;
         }
 #pragma unroll
-        for (int j = c; j < c + 32; ++j) sum += exp2_fast(fmaf(v[j], kLog2e, -at));
+        for (int j = c; j < c + 32; j += 2) total = total + exp_of_difference(Pair(v[j], v[j + 1]), at);
     }
+    sum = total.sum();
     // The warps of these rows put theirs together.  There is room for four tiles' in turn, as none of them can be more than two tiles
     // ahead of another: tensor memory holds two.
     static_assert(sizeof(control.staging) >= 4 * kParts * 128 * sizeof(float2), "unused here otherwise");
@@ -492,8 +494,8 @@ __device__ __forceinline__ bool statistics(const ProductParams& prm, int w, int 
     if (row >= count) return true;
     for (int k = 1; k < kParts; ++k) {
         const float2 p = row_statistics[k * 128 + r];
-        const float m = fmaxf(top, p.x), from = m == -INFINITY ? 0.0f : m * kLog2e;
-        sum = fmaf(sum, exp2_fast(fmaf(top, kLog2e, -from)), p.y * exp2_fast(fmaf(p.x, kLog2e, -from)));
+        const float m = fmaxf(top, p.x), from = m == -INFINITY ? 0.0f : m;
+        sum = fmaf(sum, exp_of_difference(top, from), p.y * exp_of_difference(p.x, from));
         top = m;
     }
     prm.part[((int64_t)w * prm.stat_tiles + (prm.v0 + n0) / prm.tile_cols) * prm.tokens_padded + row] = make_float2(top, sum);
@@ -508,13 +510,12 @@ __device__ __forceinline__ void store_columns(const ProductParams& prm, int w, i
     const int cols = min(width, prm.n - n0);
     if constexpr (WHICH == Product::kDlogits) {
         const bool in = row < count;
-        const float at = info.info.x * kLog2e;
 #pragma unroll
         for (int c = 0; c < COLS; c += 32) {
             if (c >= width) break;
 #pragma unroll
             for (int j = c; j < c + 32; ++j) {
-                const float p = exp2_fast(fmaf(v[j], kLog2e, -at)) - (j == target ? 1.0f : 0.0f);
+                const float p = exp_of_difference(v[j], info.info.x) - (j == target ? 1.0f : 0.0f);
                 v[j] = in && j < cols ? info.info.y * p : 0.0f;
             }
         }

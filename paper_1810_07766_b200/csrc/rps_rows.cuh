@@ -137,6 +137,25 @@ __device__ __forceinline__ Pair fma(const Pair& a, const Pair& b, const Pair& c)
     return r;
 }
 
+__device__ __forceinline__ Pair operator+(const Pair& a, const Pair& b)
+{
+    Pair r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.bits) : "l"(a.bits), "l"(b.bits));
+    return r;
+}
+
+// exp(v - at).  The difference comes before the factor: v * log2(e) - at * log2(e) is off by a unit of the products' last place, which beyond 2^30
+// is outside the exponent's range, so that a row's largest logit gave infinity or zero instead of one.
+__device__ __forceinline__ float exp_of_difference(float v, float at) { return exp2_fast((v - at) * kLog2e); }
+
+// The same of two values.
+__device__ __forceinline__ Pair exp_of_difference(const Pair& v, float at)
+{
+    float a, b;
+    ((v + Pair(-at)) * Pair(kLog2e)).get(a, b);
+    return Pair(exp2_fast(a), exp2_fast(b));
+}
+
 __device__ __forceinline__ void widen(const uint4& s, Pair (&v)[2])
 {
     v[0] = Pair(__uint_as_float(s.x), __uint_as_float(s.y)), v[1] = Pair(__uint_as_float(s.z), __uint_as_float(s.w));

@@ -8,6 +8,17 @@ from test_gpu_ops_loss import E32, check, inputs, ops  # noqa: F401
 pytestmark = pytest.mark.gpu
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [1, 3, 40, 300])
+@pytest.mark.parametrize("spread", [1e6, 1e10, 1e15])
+def test_logits_of_any_size(ops, dtype, T, spread):  # noqa: F811
+    """Where the largest logit is beyond 2^30, a unit of its last place is beyond the exponent's range: differences have to be formed
+    before anything is scaled.  (All but one of a row's probabilities are zero, so the gradients are exact.)"""
+    h, w, y = inputs(dtype, 2, T, 500, 48, seed=T, spread=spread)
+    loss, lse, dh, dw = check(ops, dtype, h, w, y)
+    assert torch.isfinite(loss).all() and torch.isfinite(dh).all() and torch.isfinite(dw).all()
+
+
 def test_sums_over_many_tokens_are_not_cut_off(ops):  # noqa: F811
     """The tensor cores cut a sum off after each 16 terms.  2^19 tokens are 32768 such steps, which of a sum of terms of one sign take 3.2e-3 in one
     run; in runs of a few thousand steps it has to be 2.4e-4 at most, far below the rounding of a bf16 result (2e-3).  That rounding averages out
