@@ -19,7 +19,8 @@
  *     outside it (the first call on a device asks the driver for attributes).
  *   - dtype is an rps_dtype: RPS_F32 or RPS_BF16, one type for all arrays of a call that are not said to be something
  *     else.  Sums, statistics and accumulators are fp32; a bf16 result is rounded once, at the store, unless a comment
- *     says otherwise.  Results do not depend on the order in which blocks run: no call uses floating-point atomics.
+ *     says otherwise.  Infinities and NaN go through matrix products as they do through fp32 arithmetic, but for two cases of RPS_F32:
+ *     an infinity times an infinity is NaN, and where dloss is infinite the gradients are either infinite or NaN.  Results do not depend on the order in which blocks run: no call uses floating-point atomics.
  *   - Strides are in elements, and the innermost axis is always contiguous.  Sizes may be zero where a comment says so.
  */
 #ifndef RPS_OPS_H

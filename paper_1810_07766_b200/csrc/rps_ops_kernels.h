@@ -231,19 +231,15 @@ template <>
 __device__ __forceinline__ bf16 from_float<bf16>(float v) { return __float2bfloat16_rn(v); }
 
 // An fp32 value is the sum of three bf16 values exactly: each is the leading 8 bits of what the ones before it leave, cut off
-// rather than rounded so that none can overflow.  An infinity or a NaN stays in the first one and the others are zero.
-__device__ __forceinline__ float leading_bits(float v)
-{
-    const uint32_t bits = __float_as_uint(v);
-    // a NaN whose payload lies in the bits cut off stays one
-    return __uint_as_float(v != v ? bits | 0x00400000u : bits & 0xFFFF0000u);
-}
-
-__device__ __forceinline__ float rest_of(float v, float lead) { return fabsf(v) <= 3.402823466e38f ? v - lead : 0.0f; }
+// rather than rounded so that none can overflow.  An infinity or a NaN is the third one, after zeros: of the products made the third part takes
+// part in that with the other operand's first one alone, so that an infinity times a number is an infinity, and none meets a part that
+// happens to be zero.
+__device__ __forceinline__ float leading_bits(float v) { return __uint_as_float(__float_as_uint(v) & 0xFFFF0000u); }
 
 __device__ __forceinline__ void split_planes(float v, bf16 (&p)[3])
 {
-    const float lead = leading_bits(v), rest = rest_of(v, lead), mid = leading_bits(rest);
+    const bool finite = fabsf(v) <= 3.402823466e38f;
+    const float lead = finite ? leading_bits(v) : 0.0f, rest = v - lead, mid = finite ? leading_bits(rest) : 0.0f;
     p[0] = __float2bfloat16_rn(lead);  // exact, as the next one
     p[1] = __float2bfloat16_rn(mid);
     p[2] = __float2bfloat16_rn(rest - mid);

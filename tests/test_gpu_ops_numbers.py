@@ -3,7 +3,7 @@ with more pieces than 32 bits count."""
 import pytest
 import torch
 
-from test_gpu_ops_loss import E32, check, inputs, ops  # noqa: F401
+from test_gpu_ops_loss import E32, TYPES, check, inputs, ops  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -59,6 +59,25 @@ def test_long_sums_of_odd_widths(ops):  # noqa: F811
 @pytest.mark.parametrize("T,V,D", [(2048, 70000, 2560), (5, 40, 70000)])  # dhidden sums over the words, logits over the columns
 def test_long_sums_of_the_loss(ops, T, V, D):  # noqa: F811
     check(ops, "bf16", *inputs("bf16", 1, T, V, D, seed=7))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [3, 200])
+def test_infinities_go_through_products(ops, dtype, T):  # noqa: F811
+    """An infinity times a number is an infinity of the product's sign, times zero it is NaN; nothing else is touched."""
+    O, D = 40, 260
+    g = torch.Generator(device="cuda").manual_seed(3)
+    dy = torch.randn(1, T, O, generator=g, device="cuda").to(TYPES[dtype])
+    p = ops.pack_activation(torch.randn(1, T, D, generator=g, device="cuda").to(TYPES[dtype]))
+    dy[0, 1, 3], dy[0, T - 1, 7], dy[0, 0, 9] = float("inf"), float("-inf"), float("nan")
+    kept = ops.unpack_activation(p)
+    want, got = dy.double().mT @ kept.double(), ops.packed_weight_grad(dy, p)
+    rows = torch.ones(O, dtype=torch.bool)
+    rows[[3, 7, 9]] = False
+    assert torch.isfinite(got[0, rows.cuda()]).all()
+    assert torch.isinf(want[0, 3]).any() and torch.isnan(want[0, 3]).sum() <= D // 4
+    for o in (3, 7, 9):
+        assert torch.equal(got[0, o].double().nan_to_num(nan=5.0), want[0, o].nan_to_num(nan=5.0)), o
 
 
 def test_operands_of_more_than_2_to_the_32_pieces(ops):  # noqa: F811
