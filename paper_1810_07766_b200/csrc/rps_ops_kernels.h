@@ -230,19 +230,35 @@ __device__ __forceinline__ float from_float<float>(float v) { return v; }
 template <>
 __device__ __forceinline__ bf16 from_float<bf16>(float v) { return __float2bfloat16_rn(v); }
 
-// An fp32 value is the sum of three bf16 values exactly: each is the leading 8 bits of what the ones before it leave, cut off
-// rather than rounded so that none can overflow.  An infinity or a NaN is the third one, after zeros: of the products made the third part takes
-// part in that with the other operand's first one alone, so that an infinity times a number is an infinity, and none meets a part that
-// happens to be zero.
-__device__ __forceinline__ float leading_bits(float v) { return __uint_as_float(__float_as_uint(v) & 0xFFFF0000u); }
-
-__device__ __forceinline__ void split_planes(float v, bf16 (&p)[3])
+// Two values as bf16, rounded to nearest; what would round to infinity becomes the largest number.
+__device__ __forceinline__ uint32_t nearest_two_bf16(float lo, float hi)
 {
-    const bool finite = fabsf(v) <= 3.402823466e38f;
-    const float lead = finite ? leading_bits(v) : 0.0f, rest = v - lead, mid = finite ? leading_bits(rest) : 0.0f;
-    p[0] = __float2bfloat16_rn(lead);  // exact, as the next one
-    p[1] = __float2bfloat16_rn(mid);
-    p[2] = __float2bfloat16_rn(rest - mid);
+    uint32_t r;
+    asm("cvt.rn.satfinite.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+__device__ __forceinline__ uint32_t two_bf16(float lo, float hi)
+{
+    const __nv_bfloat162 p = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&p);
+}
+
+// An fp32 value is the sum of three bf16 values exactly: each is the nearest to what the ones before it leave, so that what the last two
+// leave out of a product has no sign in common with it.  (Cut off instead of rounded, the parts are up to twice as large, and the products of
+// parts that are not made reach 2^-21 of the result, always with its sign; rounded 2^-24.)  An infinity or a NaN is the third one, after
+// zeros: of the products made the third part takes part in that with the other operand's first one alone, so that an infinity times a
+// number is an infinity, and none meets a part that happens to be zero.  Two values at a time, as words.
+__device__ __forceinline__ void split_two(float a, float b, uint32_t (&parts)[3])
+{
+    const bool finite_a = fabsf(a) <= 3.402823466e38f, finite_b = fabsf(b) <= 3.402823466e38f;
+    float x = finite_a ? a : 0.0f, y = finite_b ? b : 0.0f;
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        parts[q] = nearest_two_bf16(x, y);
+        x -= __uint_as_float(parts[q] << 16), y -= __uint_as_float(parts[q] & 0xFFFF0000u);
+    }
+    parts[2] = two_bf16(finite_a ? x : a, finite_b ? y : b);
 }
 #endif
 

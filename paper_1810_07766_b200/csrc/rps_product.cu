@@ -14,8 +14,8 @@
 // Operands are read as they lie in memory: with the summed axis contiguous, or (dl and W in dH = dl W, dl and H in dW = dl^T H) with
 // the other one contiguous, which the descriptors of the shared-memory tiles express; nothing is transposed.
 //
-// fp32 operands are three bf16 parts each (24 significant bits); of the nine products of parts the six that reach 2^-24
-// of the result are made.  The three parts of a block lie in three stages of the ring, so each is copied once for its three products.
+// fp32 operands are three bf16 parts each (24 significant bits); of the nine products of parts six are made, and the others are below 2^-24 of
+// the result (split_two).  The three parts of a block lie in three stages of the ring, so each is copied once for its three products.
 #include <algorithm>
 #include <mutex>
 #include <type_traits>
@@ -240,12 +240,6 @@ __device__ __forceinline__ void take_sums(float (&v)[COLS], uint32_t addr, bool 
 }
 
 // --------------------------------------------------------------------------------------------------------- epilogues
-__device__ __forceinline__ uint32_t two_bf16(float lo, float hi)
-{
-    const __nv_bfloat162 p = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t*>(&p);
-}
-
 __device__ __forceinline__ void store_element(float* to, float e) { __stcg(to, e); }
 __device__ __forceinline__ void store_element(bf16* to, bf16 e) { __stcg(reinterpret_cast<unsigned short*>(to), __bfloat16_as_ushort(e)); }
 
@@ -388,8 +382,8 @@ __device__ __forceinline__ void store_rows(Stage& stage, const float (&v)[COLS],
     }
 }
 
-// fp32 values as three planes of bf16 parts: the leading 8 bits of what the parts before leave, cut off.  (A NaN is one in all of them, an
-// infinity becomes NaN in the second: what they are summed into is NaN either way.)
+// fp32 values as three planes of bf16 parts, as split_two makes them but for infinities (of an infinite dloss alone), whose first parts are the largest
+// number: what they are summed into is infinite or NaN.
 template <int COLS, typename Stage>
 __device__ __forceinline__ void store_parts(Stage& stage, float (&v)[COLS], Rows<bf16> to, int64_t plane)
 {
@@ -406,9 +400,8 @@ __device__ __forceinline__ void store_parts(Stage& stage, float (&v)[COLS], Rows
             for (int j = 0; j < 32; j += 2) {
                 float &f0 = v[c + j], &f1 = v[c + j + 1];
                 if (q < 2) {
-                    const uint32_t lead0 = __float_as_uint(f0) & 0xFFFF0000u, lead1 = __float_as_uint(f1) & 0xFFFF0000u;
-                    word[j / 2] = __byte_perm(lead0, lead1, 0x7632);
-                    f0 -= __uint_as_float(lead0), f1 -= __uint_as_float(lead1);
+                    word[j / 2] = nearest_two_bf16(f0, f1);
+                    f0 -= __uint_as_float(word[j / 2] << 16), f1 -= __uint_as_float(word[j / 2] & 0xFFFF0000u);
                 } else {
                     word[j / 2] = two_bf16(f0, f1);
                 }

@@ -233,19 +233,11 @@ int alignment(const void* p, int64_t cols, int64_t stride)
 // Eight fp32 values as three slices of bf16 parts that add up to them.
 __device__ __forceinline__ void split_slice(const float (&v)[8], uint4 (&parts)[3])
 {
-    uint32_t r[3][4];
+    uint32_t r[4][3];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        bf16 p[3];
-        split_planes(v[j], p);
+    for (int j = 0; j < 4; ++j) split_two(v[2 * j], v[2 * j + 1], r[j]);
 #pragma unroll
-        for (int q = 0; q < 3; ++q) {
-            const uint32_t bits = __bfloat16_as_ushort(p[q]);
-            r[q][j / 2] = j % 2 == 0 ? bits : r[q][j / 2] | bits << 16;
-        }
-    }
-#pragma unroll
-    for (int q = 0; q < 3; ++q) parts[q] = make_uint4(r[q][0], r[q][1], r[q][2], r[q][3]);
+    for (int q = 0; q < 3; ++q) parts[q] = make_uint4(r[0][q], r[1][q], r[2][q], r[3][q]);
 }
 
 constexpr float kSmallestPacked = 0x1p-100f;  // a group with nothing larger is kept as zeros: 127 / max stays finite

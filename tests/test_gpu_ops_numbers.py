@@ -61,6 +61,28 @@ def test_long_sums_of_the_loss(ops, T, V, D):  # noqa: F811
     check(ops, "bf16", *inputs("bf16", 1, T, V, D, seed=7))
 
 
+def test_fp32_products_keep_fp32_accuracy(ops):  # noqa: F811
+    """A single token, so that each result is one product.  With three parts that are each rounded to nearest the six products made
+    leave out at most 2^-24 of it; the last of their sums may be cut off by a unit, 2^-23."""
+    g = torch.Generator(device="cuda").manual_seed(2)
+    dy, x = torch.randn(1, 1, 2000, generator=g, device="cuda"), torch.randn(1, 1, 1920, generator=g, device="cuda")
+    # every value of a group has a different exponent and all 24 bits
+    p = ops.PackedActivation(torch.randint(1, 128, (1, 1, 1920), generator=g, device="cuda").to(torch.int8), x.abs()[..., :15].contiguous(), 1920, torch.float32)
+    kept = ops.unpack_activation(p).double()
+    got, want = ops.packed_weight_grad(dy, p).double(), dy.double().mT @ kept
+    assert float((got / want - 1).abs().max()) <= 2.0 ** -22
+
+
+@pytest.mark.parametrize("size,scale", [(3.4028e38, 1e-30), (3.3961e38, 2.0 ** -7), (1e30, 1e-30), (2.0 ** -108, 1.0)])
+def test_fp32_products_of_the_largest_and_smallest_values(ops, size, scale):  # noqa: F811
+    """Values that round to infinity as bf16, and values whose last part is the smallest that bf16 has: the bound of the test before."""
+    dy = torch.full((1, 1, 64), size, device="cuda") * torch.linspace(0.9999, 1, 64, device="cuda")
+    p = ops.PackedActivation((torch.arange(64, device="cuda") - 32).to(torch.int8)[None, None], torch.full((1, 1, 1), scale, device="cuda"), 64, torch.float32)
+    got, want = ops.packed_weight_grad(dy, p).double(), dy.double().mT @ ops.unpack_activation(p).double()
+    fits = want.abs() < 3.4e38
+    assert fits[..., 31].all() and ((got - want).abs()[fits] <= 2.0 ** -22 * want.abs()[fits]).all()
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("T", [3, 200])
 def test_infinities_go_through_products(ops, dtype, T):  # noqa: F811
