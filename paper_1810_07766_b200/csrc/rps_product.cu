@@ -17,6 +17,7 @@
 // fp32 operands are three bf16 parts each (24 significant bits); of the nine products of parts six are made, and the others are below 2^-24 of
 // the result (split_two).  The three parts of a block lie in three stages of the ring, so each is copied once for its three products.
 #include <algorithm>
+#include <atomic>
 #include <mutex>
 #include <type_traits>
 
@@ -822,12 +823,19 @@ bool encode_operand(CUtensorMap* map, const Operand& o, int planes, int workers,
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// 0 if they cannot be asked for.
+// Whether the kernel was compiled to the registers that its epilogue shares out anew: it would wait for ever for those that a smaller launch does not have.
+// `known` keeps the number once it has been asked for; a question that fails is asked again.
 template <typename Kernel>
-int registers_of(Kernel kernel)
+cudaError_t check_registers(std::atomic<int>& known, Kernel kernel)
 {
-    cudaFuncAttributes attributes{};
-    return cudaFuncGetAttributes(&attributes, kernel) == cudaSuccess ? attributes.numRegs : 0;
+    int registers = known.load(std::memory_order_relaxed);
+    if (registers == 0) {
+        cudaFuncAttributes attributes{};
+        const cudaError_t err = cudaFuncGetAttributes(&attributes, kernel);
+        if (err != cudaSuccess) return err;
+        known.store(registers = attributes.numRegs, std::memory_order_relaxed);
+    }
+    return registers == kLaunchRegisters ? cudaSuccess : cudaErrorInvalidKernelImage;
 }
 
 template <Product WHICH, int PLANES, int CTAS, bool LONG>
@@ -836,9 +844,9 @@ cudaError_t launch(const ProductParams& prm, cudaStream_t stream)
     static rps::LaunchState state;
     cudaError_t err = rps::grant_smem(state, rps_product_kernel<WHICH, PLANES, CTAS, LONG>, kSharedBytes);
     if (err != cudaSuccess) return err;
-    if constexpr (PLANES == 3) {  // the epilogue waits for registers that a smaller launch would never have
-        static const int registers = registers_of(rps_product_kernel<WHICH, PLANES, CTAS, LONG>);
-        if (registers != kLaunchRegisters) return cudaErrorLaunchOutOfResources;
+    if constexpr (PLANES == 3) {
+        static std::atomic<int> registers{0};
+        if ((err = check_registers(registers, rps_product_kernel<WHICH, PLANES, CTAS, LONG>)) != cudaSuccess) return err;
     }
     int sms = 0;
     if ((err = sm_count(&sms)) != cudaSuccess) return err;
