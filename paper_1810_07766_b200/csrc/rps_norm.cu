@@ -22,7 +22,11 @@ namespace {
 
 constexpr int kMostThreads = 512;
 constexpr int kSlots = 4, kAhead = kSlots - 1;      // rows in shared memory: this one and those ahead
-constexpr int kForwardThreads = 1024, kBackwardThreads = 512;  // resident on an SM: 48 KB and 40 KB of slots for each row
+// Threads on an SM at once, by registers.  By shared memory (the slots, the sums' 4 KB and 1 KB of the system for each CTA of 228 KB) so many CTAs
+// of 256 threads and more fit too; of narrower ones fewer: forward 7 of 8 of 128 threads, 13 of 16 of 64 and 20 of 32 of 32, backward 15 of 16 of
+// 32; the others follow when places get free.  (Room for the sums of one CTA's warps alone, and grids of what then fits: 4 x 24108 x 85 bf16
+// forward 55 -> 60 us, backward 161 -> 140; 65536 x 256 bf16 140 -> 141, 194 -> 201; 32768 x 1024 152 -> 154, 196 -> 196.)
+constexpr int kForwardThreads = 1024, kBackwardThreads = 512;
 constexpr int kMostCluster = 8;
 constexpr int kMostWarps = kMostThreads / 32 * kMostCluster;
 
@@ -452,11 +456,13 @@ __global__ void __launch_bounds__(512) rps_norm_reduce_kernel(const NormParams p
 }
 
 // Threads of a CTA and CTAs of a cluster for a row of `slices` 16-byte slices: the fewest threads (a power of two of warps) that hold it, up
-// to 512, then a cluster.  `most` threads are resident on an SM at once, and a row of
-// a cluster of 3 or 4 takes 1.4 to 1.7 times as long as one of 2 (2.9 us forward, 1.9 backward: its sums go from CTA to CTA twice, or
-// once), so the cluster that has most rows through in a given time is taken.  (2200 rows of 4488 fp32, forward and backward: 4 CTAs of 288 threads and
-// 3 of 384 80 + 117 us; with 4 of 512 for both and slower exchanges 174 + 253.  3126 rows of 4840 bf16, both: 2 of 320 121, backward by 4 of
-// 160 instead 141.)
+// to 512, then a cluster.  About `most` threads are resident on an SM at once, and a row of a cluster of 3 to 8 takes some 1.7 times as long as
+// one of 2, whatever their number (its sums go from CTA to CTA twice, or backward once), so the cluster that has most rows through in a given
+// time is taken.  2200 rows of fp32 in us, what is taken first:
+//   4488 columns  forward 6 CTAs of 192 threads 72, 5 of 256 75, 4 of 288 77, 8 of 160 79, 3 of 384 86
+//                 backward 5 of 256 116, 8 of 160 121, 6 of 192 123, 3 of 384 134, 4 of 288 146
+//   6200 columns  backward 7 of 224 171, 8 of 224 191, 4 of 416 196, 5 of 320 204, 6 of 288 235
+//   2100 columns  backward 2 of 288 41, 6 of 96 54
 void shape_of_row(int64_t slices, int most, int* threads, int* cluster)
 {
     *threads = 32, *cluster = 1;
@@ -466,7 +472,7 @@ void shape_of_row(int64_t slices, int most, int* threads, int* cluster)
     for (int c = 2; c <= 8; ++c) {
         const int64_t each = round_up(ceil_div(slices, c), 32);
         if (each > kMostThreads) continue;
-        const double rate = (double)(148 * (most / each) / c) / (c == 2 ? 1.0 : 1.6 + 0.25 * std::max(0, c - 4));
+        const double rate = (double)(148 * (most / each) / c) / (c == 2 ? 1.0 : 1.7);
         if (rate > best) best = rate, *threads = (int)each, *cluster = c;
     }
 }

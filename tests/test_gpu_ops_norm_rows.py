@@ -7,13 +7,12 @@ from test_gpu_ops_norm_pack import check_norm, norm_inputs, ops  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
-# A cluster of c CTAs of t threads holds rows of up to 4 c t fp32 or 8 c t bf16 columns; 148 SMs have 1024 (forward) and 512 (backward) threads at
-# once, so each of these gives every cluster 3 to 20 rows.  Clusters of 2 to 8 CTAs, whole and ragged last slices.
-CLUSTERS = [("f32", 1, 700, 2052, 1), ("f32", 2, 301, 4096, 7), ("f32", 3, 200, 4488, 1), ("f32", 1, 300, 5124, 300), ("f32", 1, 150, 6148, 1),
-            ("f32", 2, 90, 8192, 1), ("f32", 1, 120, 10243, 4), ("f32", 1, 110, 12300, 1), ("f32", 2, 60, 16384, 60), ("bf16", 1, 500, 4104, 1),
-            ("bf16", 2, 350, 5001, 1), ("bf16", 3, 140, 8200, 2), ("bf16", 1, 150, 12298, 1), ("bf16", 2, 100, 16384, 10)]
+# Rows over clusters of 2 to 8 CTAs, whole and ragged last slices; each cluster has 3 to 15 of them.
+CLUSTERS = [("f32", 1, 1200, 2052, 1), ("f32", 2, 301, 4096, 7), ("f32", 3, 200, 4488, 1), ("f32", 1, 600, 5400, 300), ("f32", 1, 500, 6148, 1),
+            ("f32", 2, 130, 8192, 1), ("f32", 1, 300, 10243, 4), ("f32", 1, 220, 12300, 1), ("f32", 2, 60, 16384, 60), ("bf16", 1, 1100, 4104, 1),
+            ("bf16", 2, 350, 5001, 1), ("bf16", 3, 200, 8200, 2), ("bf16", 1, 400, 12298, 1), ("bf16", 2, 120, 16384, 10)]
 # Rows of one CTA each: more than the ring's four slots, at each of the three alignments; the workers' rows end inside a CTA's.
-CTAS = [("f32", 3, 700, 2048, 1), ("f32", 3, 1100, 1001, 1100), ("f32", 5, 1900, 250, 10), ("f32", 3, 9500, 64, 1), ("bf16", 3, 700, 4096, 7),
+CTAS = [("f32", 3, 700, 2048, 1), ("f32", 3, 1100, 1001, 1100), ("f32", 5, 2500, 250, 10), ("f32", 3, 9500, 64, 1), ("bf16", 3, 700, 4096, 7),
         ("bf16", 3, 700, 4095, 1), ("bf16", 3, 1100, 2002, 2), ("bf16", 5, 2000, 333, 2000), ("bf16", 3, 9500, 85, 1), ("bf16", 7, 1500, 1000, 3)]
 
 
