@@ -179,7 +179,7 @@ __global__ void __launch_bounds__(kMergeThreads) rps_lce_merge_kernel(const LceP
 template <typename T, bool SELECT>
 cudaError_t gather(const LceParams& prm, cudaStream_t stream)
 {
-    const int64_t rows = ceil_div(round_up(prm.tokens, kTokenBlock), kRowThreads / 32), places = 148 * 4;
+    const int64_t rows = ceil_div(round_up(prm.tokens, kTokenBlock), kRowThreads / 32), places = kSms * 4;
     // few rows share their columns out, instead of a warp's turns along each (4 workers of 42 rows of 2530 fp32: 25 -> 6.5 us)
     const int64_t along = std::max<int64_t>(1, std::min(ceil_div(prm.cols_padded, 256), places / (rows * prm.n)));
     const dim3 grid((unsigned)rows, (unsigned)prm.n, (unsigned)along);
@@ -218,7 +218,7 @@ int64_t lce_merge_blocks(int64_t tokens) { return ceil_div(tokens, kMergeRows); 
 cudaError_t launch_lce_merge(const LceParams& prm, cudaStream_t stream)
 {
     const int64_t many = ceil_div(prm.tokens, kManyMergeRows);
-    if (many * prm.n >= 148) return launch_after(rps_lce_merge_kernel<kManyMergeRows>, dim3((unsigned)many, (unsigned)prm.n), kMergeThreads, 0, stream, 1, prm);
+    if (many * prm.n >= kSms) return launch_after(rps_lce_merge_kernel<kManyMergeRows>, dim3((unsigned)many, (unsigned)prm.n), kMergeThreads, 0, stream, 1, prm);
     return launch_after(rps_lce_merge_kernel<kMergeRows>, dim3((unsigned)lce_merge_blocks(prm.tokens), (unsigned)prm.n), kMergeThreads, 0, stream, 1, prm);
 }
 

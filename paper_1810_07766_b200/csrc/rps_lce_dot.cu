@@ -350,10 +350,10 @@ void plan_lce_dot(LceParams* prm)
     if (prm->tokens < 1 || prm->tokens > (prm->f32 ? kMostTokensF32 : kMostTokens) || (int64_t)rows * chunks * chunk * 4 > kMostHiddenBytes) return;
     const auto within = [](int64_t x, int64_t most) { return (int)std::max<int64_t>(1, std::min(x, most)); };
     prm->dot_rows = rows;
-    prm->dot_blocks = within(ceil_div(prm->vocab, kWarps * kRowsAtATime), 148 * (rows <= 2 ? kResident<1> : kResident<4>) / prm->n);
+    prm->dot_blocks = within(ceil_div(prm->vocab, kWarps * kRowsAtATime), kSms * (rows <= 2 ? kResident<1> : kResident<4>) / prm->n);
     const int across = (int)ceil_div(chunks, kWarps);
     prm->dot_wide = (int)ceil_div(chunks, across), prm->dot_high = kWarps / prm->dot_wide;
-    prm->dot_ranges = within(ceil_div(prm->vocab, 16 * prm->dot_high), 2 * 148 / (across * prm->n));
+    prm->dot_ranges = within(ceil_div(prm->vocab, 16 * prm->dot_high), 2 * kSms / (across * prm->n));
 }
 
 cudaError_t launch_lce_dot(const LceParams& prm, cudaStream_t stream)

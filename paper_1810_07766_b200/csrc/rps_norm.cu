@@ -472,7 +472,7 @@ void shape_of_row(int64_t slices, int most, int* threads, int* cluster)
     for (int c = 2; c <= 8; ++c) {
         const int64_t each = round_up(ceil_div(slices, c), 32);
         if (each > kMostThreads) continue;
-        const double rate = (double)(148 * (most / each) / c) / (c == 2 ? 1.0 : 1.7);
+        const double rate = (double)(kSms * (most / each) / c) / (c == 2 ? 1.0 : 1.7);
         if (rate > best) best = rate, *threads = (int)each, *cluster = c;
     }
 }
@@ -561,9 +561,9 @@ void plan_norm_backward(NormParams* prm)
 {
     int threads = 0, cluster = 0;
     shape_of_row(ceil_div(prm->cols, prm->f32 ? Slice<float>::kWidth : Slice<bf16>::kWidth), kBackwardThreads, &threads, &cluster);
-    // as many blocks over all workers as are resident at once (512 threads of each of the 148 SMs); of the two nearest ways
+    // as many blocks over all workers as are resident at once (512 threads of each SM); of the two nearest ways
     // to cut the rows the one whose longest SM has fewer of them
-    int64_t want = (int64_t)148 * (kBackwardThreads / threads) / cluster / prm->n;
+    int64_t want = (int64_t)kSms * (kBackwardThreads / threads) / cluster / prm->n;
     if (want < 1) want = 1;
     const int64_t rows = prm->rows_per_gate, target = ceil_div(prm->tokens, want);
     const bool whole = rows <= target;

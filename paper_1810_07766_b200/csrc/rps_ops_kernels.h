@@ -11,6 +11,10 @@ namespace rps_ops {
 
 using bf16 = __nv_bfloat16;
 
+// Of a B200.  Plans are made without asking the device, so that workspaces have the sizes that the calls then count on; a launch that has to know
+// how many there are asks sm_count.
+constexpr int kSms = 148;
+
 inline int64_t round_up(int64_t a, int64_t b) { return (a + b - 1) / b * b; }
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 

@@ -903,7 +903,7 @@ ProductShape product_shape(int64_t m, int64_t n, int64_t k, int workers, int pla
 {
     const int64_t halves = ceil_div(m > 0 ? m : 1, 128), whole = ceil_div(halves, 2);
     const int ctas = halves == 1 ? 1 : 2;
-    const int64_t places = 148 / ctas, others = (ctas == 1 ? halves : whole) * workers, blocks = ceil_div(k, kDepth);
+    const int64_t places = kSms / ctas, others = (ctas == 1 ? halves : whole) * workers, blocks = ceil_div(k, kDepth);
     const int64_t fewest = ceil_div(n, kTileN);
     ProductShape best{};
     double least = 0.0;
@@ -983,7 +983,7 @@ cudaError_t join(const ProductParams& prm, cudaStream_t stream)
     const int64_t rows = ceil_div(prm.m, 8), across = std::min<int64_t>(ceil_div(prm.n, 128), 65535);
     if (prm.splits >= 8 && across * 128 >= prm.n)
         return launch_after(rps_join_kernel<T, HIDDEN, true>, dim3((unsigned)prm.m, (unsigned)prm.workers, (unsigned)across), 256, 0, stream, 1, prm);
-    const int64_t along = std::max<int64_t>(1, std::min(across, 148 * 8 / (rows * prm.workers)));  // few rows share their columns out (182 of 2253: 30 -> 5 us)
+    const int64_t along = std::max<int64_t>(1, std::min(across, kSms * 8 / (rows * prm.workers)));  // few rows share their columns out (182 of 2253: 30 -> 5 us)
     return launch_after(rps_join_kernel<T, HIDDEN, false>, dim3((unsigned)rows, (unsigned)prm.workers, (unsigned)along), 256, 0, stream, 1, prm);
 }
 
