@@ -19,8 +19,11 @@
  *     outside it (the first call on a device asks the driver for attributes).
  *   - dtype is an rps_dtype: RPS_F32 or RPS_BF16, one type for all arrays of a call that are not said to be something
  *     else.  Sums, statistics and accumulators are fp32; a bf16 result is rounded once, at the store, unless a comment
- *     says otherwise.  Infinities and NaN go through matrix products as they do through fp32 arithmetic, but for two cases of RPS_F32:
- *     an infinity times an infinity is NaN, and where dloss is infinite the gradients are either infinite or NaN.  Results do not depend on the order in which blocks run: no call uses floating-point atomics.
+ *     says otherwise.  The tensor cores cut their sums off instead of rounding them, so those go through in runs that are added in
+ *     fp32, rounded: of 128 terms with RPS_F32 (whose products leave out less than 2^-24 of themselves), of 1024 for the loss and
+ *     32768 for the gradients with RPS_BF16.  Infinities and NaN go through matrix products as they do through fp32 arithmetic,
+ *     but for two cases of RPS_F32: an infinity times an infinity is NaN, and where dloss is infinite the gradients are either
+ *     infinite or NaN.  Results do not depend on the order in which blocks run: no call uses floating-point atomics.
  *   - Strides are in elements, and the innermost axis is always contiguous.  Sizes may be zero where a comment says so.
  */
 #ifndef RPS_OPS_H
@@ -107,14 +110,15 @@ int rps_lce_backward(const rps_lce_desc* desc, const void* hidden, const void* w
  *   dgate = sum scale * u * t,  dpost = sum scale * gate * t * f * r(f),  dpre = sum dy * h * r(h)
  *
  * x, f, h, y and their gradients are dense [n][tokens][cols]; post and pre are [n][cols] with a stride between workers,
- * gate is [n][gates][cols] with a stride between workers.  The backward pass reads f and h either as they were or as
- * 8-bit codes with scales (rps_pack), which the forward pass writes along the way when it is given room for them; r(f) and
- * r(h) are always those of the values before packing.  tokens may be 0.
+ * gate is [n][gates][cols] with a stride between workers.  The backward pass reads f and h either as they are stored (h of
+ * RPS_BF16 rounded, that is, while r(h) and y are made of h before it is) or as 8-bit codes of that with scales (rps_pack), which the
+ * forward pass writes along the way when it is given room for them; r(f) and r(h) are always those of the values before rounding and
+ * packing.  tokens may be 0; n * tokens < 2^31.
  * ------------------------------------------------------------------------------------------------------------------ */
 typedef struct rps_norm_desc {
     int32_t dtype;
     int32_t n;               /* workers, 1..RPS_MAX_WORKERS                           */
-    int64_t tokens;          /* tokens of a worker, 0 <= tokens < 2^31                */
+    int64_t tokens;          /* tokens of a worker, 0 <= n * tokens < 2^31            */
     int64_t cols;            /* 1..RPS_MAX_NORM_COLS                                  */
     int64_t gates;           /* rows of gate, a divisor of tokens (1 if tokens is 0)  */
     int64_t post_worker, pre_worker, gate_worker;    /* strides between workers       */
@@ -168,7 +172,7 @@ int rps_unpack(int dtype, int64_t rows, int64_t cols, const int8_t* codes, const
 typedef struct rps_wgrad_desc {
     int32_t dtype;           /* of dy and dweight                                     */
     int32_t n;               /* workers, 1..RPS_MAX_WORKERS                           */
-    int64_t tokens;          /* 0 <= tokens < 2^24                                    */
+    int64_t tokens;          /* 0 <= tokens < 2^24, n * tokens < 2^31                 */
     int64_t outs, cols;      /* 1..2^24-1                                             */
     int64_t dy_row, dy_worker, dweight_row, dweight_worker; /* strides; rows >= outs and >= cols, dweight_row < 2^31 */
     int32_t wait_limit_ms;   /* every wait of the product's kernel on data gives up after this many milliseconds (0 = 2000) */

@@ -24,10 +24,14 @@ constexpr int kMostThreads = 512;
 constexpr int kSlots = 4, kAhead = kSlots - 1;      // rows in shared memory: this one and those ahead
 // Threads on an SM at once, by registers.  By shared memory (the slots, the sums' 4 KB and 1 KB of the system for each CTA of 228 KB) so many CTAs
 // of 256 threads and more fit too; of narrower ones fewer: forward 7 of 8 of 128 threads, 13 of 16 of 64 and 20 of 32 of 32, backward 15 of 16 of
-// 32; the others follow when places get free.  (Room for the sums of one CTA's warps alone, and grids of what then fits: 4 x 24108 x 85 bf16
-// forward 55 -> 60 us, backward 161 -> 140; 65536 x 256 bf16 140 -> 141, 194 -> 201; 32768 x 1024 152 -> 154, 196 -> 196.)
+// 32; the others follow when places get free.  (With room for the sums of one CTA's warps alone, so that all but the last forward ones fit: 4 x 24108 x 85
+// bf16 forward 54 -> 57 us, backward 170 -> 151; 65536 x 256 37 -> 39, 96 -> 92; 30000 x 500 fp32 60 -> 65, 104 -> 104; 32768 x 512 bf16 with 8-bit copies
+// 50 -> 44, 72 -> 72.)
 constexpr int kForwardThreads = 1024, kBackwardThreads = 512;
 constexpr int kMostCluster = 8;
+// Of the slots in shared memory, whatever lies before them: copies of 16 bytes whose neighbours in a warp start off a 128-byte line are far slower
+// (16 bytes off: 16384 x 4096 bf16 backward 196 -> 220 us, 32768 x 1024 55 + 109 -> 151 + 192, 65536 x 256 36 + 95 -> 140 + 194).
+constexpr int kLine = 128;
 constexpr int kMostWarps = kMostThreads / 32 * kMostCluster;
 
 // Set when a bounded wait gave up (rps_ops_check).
@@ -65,7 +69,7 @@ __device__ __forceinline__ void end_exchanges(bool fine)
 
 // A warp's sum of each of `values` values to every CTA that shares the row, and the wait for all of them.  Some lanes (8 at least) have the sum of
 // a value, and `index` numbers them.  In a cluster each of them sends it to one CTA, whose barrier counts the bytes: a barrier of the whole
-// cluster would first see the stores of the row before through to memory (2200 rows of 4096 fp32: 56 + 74 us, 43 + 57 so).  A warp sends
+// cluster would first see the stores of the row before through to memory (2200 rows of 4096 fp32: 52 + 70 us, 38 + 51 so).  A warp sends
 // again only after it has read all sums of the exchange before, so nobody is more than one exchange ahead, and two rooms are enough.
 // A warp whose wait runs out (fine = false, for all of its lanes) is done: it neither arrives nor sends again, as a barrier must not be
 // arrived on twice in a phase, and so the others' waits run out one exchange later at most.
@@ -145,7 +149,7 @@ __global__ void __launch_bounds__(kMostThreads, kForwardThreads / kMostThreads) 
 {
     after_the_kernel_before();
     constexpr int W = Slice<T>::kWidth, P = W / 2;
-    extern __shared__ uint4 ring[];
+    extern __shared__ __align__(kLine) uint4 ring[];
     __shared__ Sums sums;
     const uint32_t copied = (uint32_t)__cvta_generic_to_shared(ring);
     const int cluster = CLUSTER ? prm.cluster : 1, D = (int)prm.cols;
@@ -263,7 +267,7 @@ __global__ void __launch_bounds__(kMostThreads, kBackwardThreads / kMostThreads)
 {
     after_the_kernel_before();
     constexpr int W = Slice<T>::kWidth, P = W / 2;
-    extern __shared__ uint4 ring[];
+    extern __shared__ __align__(kLine) uint4 ring[];
     __shared__ Sums sums;
     const uint32_t copied = (uint32_t)__cvta_generic_to_shared(ring);
     const int cluster = CLUSTER ? prm.cluster : 1, D = (int)prm.cols;
@@ -459,10 +463,10 @@ __global__ void __launch_bounds__(512) rps_norm_reduce_kernel(const NormParams p
 // to 512, then a cluster.  About `most` threads are resident on an SM at once, and a row of a cluster of 3 to 8 takes some 1.7 times as long as
 // one of 2, whatever their number (its sums go from CTA to CTA twice, or backward once), so the cluster that has most rows through in a given
 // time is taken.  2200 rows of fp32 in us, what is taken first:
-//   4488 columns  forward 6 CTAs of 192 threads 72, 5 of 256 75, 4 of 288 77, 8 of 160 79, 3 of 384 86
-//                 backward 5 of 256 116, 8 of 160 121, 6 of 192 123, 3 of 384 134, 4 of 288 146
-//   6200 columns  backward 7 of 224 171, 8 of 224 191, 4 of 416 196, 5 of 320 204, 6 of 288 235
-//   2100 columns  backward 2 of 288 41, 6 of 96 54
+//   4488 columns  forward 6 CTAs of 192 threads 64, 5 of 256 67, 4 of 288 69, 8 of 160 72, 3 of 384 78
+//                 backward 5 of 256 103, 6 of 192 108, 8 of 160 108, 3 of 384 116, 4 of 288 130
+//   6200 columns  backward 7 of 224 150, 8 of 224 167, 4 of 416 168, 5 of 320 180, 6 of 288 207
+//   2100 columns  backward 2 of 288 39, 6 of 96 51
 void shape_of_row(int64_t slices, int most, int* threads, int* cluster)
 {
     *threads = 32, *cluster = 1;

@@ -497,7 +497,8 @@ def gated_residual_norm_forward(x: torch.Tensor, f: torch.Tensor, gate: torch.Te
 
     x, f ``[n, tokens, cols]``; post, pre ``[n, cols]``; gate ``[n, gates, cols]``, gates a divisor of tokens (consecutive tokens
     share a row: 1 for a gate of each channel, tokens for one of each token); all without ``n`` for a single worker.
-    keep: "values" (kept holds f and h themselves), "int8" (8-bit copies, written along the way)."""
+    keep: "values" (kept holds f and h themselves: a bfloat16 h as it is rounded), "int8" (8-bit copies, written along the way).
+    scale and eps are numbers and get no gradient."""
     if keep not in ("values", "int8"):
         raise ValueError('keep must be "values" or "int8"')
     device = _device_of(x=x, f=f, gate=gate, post=post, pre=pre)
