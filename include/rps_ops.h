@@ -185,6 +185,36 @@ int rps_wgrad_workspace(const rps_wgrad_desc* desc, const void* dy, size_t* byte
 int rps_packed_wgrad(const rps_wgrad_desc* desc, const void* dy, const int8_t* codes, const float* scales, void* dweight,
                      void* workspace, size_t workspace_bytes, void* cuda_stream);
 
+/* ------------------------------------------------------------------------------------------------------------------
+ * Rows of a table looked up by token, and the table's gradient, for each worker by itself.
+ *
+ *   out[t] = scale * weight[tokens[t]],   dweight[v] = scale * sum over t with tokens[t] == v of dout[t]
+ *
+ * Tokens that are ignore_index take no part: their row of out is 0, and their row of dout is not read.  Any other token
+ * outside 0..vocab-1 is a mistake of the caller that the host cannot see: its row of out is NaN, and no row of dweight is its own.
+ * The gradient's sums go through the tokens in their order (by tiles where a word is frequent), in fp32, and are rounded once.
+ * tokens: int64 [n][tokens], dense.  out, dout: [n][tokens][cols], dense.  tokens may be 0; n * tokens < 2^31.
+ * ------------------------------------------------------------------------------------------------------------------ */
+typedef struct rps_embed_desc {
+    int32_t dtype;          /* of weight, out, dout, dweight                                              */
+    int32_t n;              /* workers, 1..RPS_MAX_WORKERS                                                */
+    int32_t accumulate;     /* backward: 0 = dweight is written whole, 1 = added to (rows without a token are not touched);
+                               for a table that is also the weight of the output layer, whose gradient is there already */
+    int32_t reserved;       /* 0 */
+    int64_t tokens;         /* tokens of a worker, 0 <= tokens < 2^24                                     */
+    int64_t vocab;          /* rows of weight, 1 <= vocab < 2^30                                          */
+    int64_t cols;           /* 1 <= cols < 2^24                                                           */
+    int64_t ignore_index;
+    int64_t weight_row, weight_worker;    /* strides of weight (forward); weight_row >= cols              */
+    int64_t dweight_row, dweight_worker;  /* strides of dweight (backward); cols <= dweight_row < 2^31    */
+    double scale;           /* finite                                                                     */
+} rps_embed_desc;
+
+int rps_embed_forward(const rps_embed_desc* desc, const int64_t* tokens, const void* weight, void* out, void* cuda_stream);
+int rps_embed_workspace(const rps_embed_desc* desc, size_t* bytes); /* of rps_embed_backward */
+int rps_embed_backward(const rps_embed_desc* desc, const int64_t* tokens, const void* dout, void* dweight, void* workspace,
+                       size_t workspace_bytes, void* cuda_stream);
+
 /* Every wait inside a kernel is bounded (two seconds, unless a description says otherwise): those of the matrix products on data, and those of the
  * norms whose rows are shared by several CTAs on one another's sums.  One that gives up ends its kernel early; what the call had
  * not written by then is not written, and what it has written is not valid.  rps_ops_check synchronises the stream and returns

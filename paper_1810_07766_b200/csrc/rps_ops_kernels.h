@@ -193,6 +193,30 @@ void plan_norm_backward(NormParams* prm);
 cudaError_t launch_norm_forward(const NormParams& prm, cudaStream_t stream);
 cudaError_t launch_norm_backward(const NormParams& prm, cudaStream_t stream);
 
+// ---------------------------------------------------------------------------------------------------- embedding
+struct EmbedParams {
+    int f32, n, accumulate;
+    float scale;
+    int64_t count, vocab, cols, ignore_index;  // count: tokens of a worker
+    const int64_t* tokens;
+    const void* weight;
+    int64_t weight_row, weight_worker;
+    void* out;
+    const void* dout;
+    void* dweight;
+    int64_t dweight_row, dweight_worker;
+    // backward (plan_embed): the tokens sorted by row, in one of two places each
+    int key_bits, digit_bits, sorted;  // sorted: which place
+    int64_t sort_blocks;               // CTAs that sort a worker's tokens; 0: one, in shared memory
+    uint32_t *keys[2], *from[2];       // [n][count]
+    uint32_t* counts;                  // [n][256][sort_blocks]
+    int64_t tile, tiles, part_row;     // sorted tokens of a tile; of a worker
+    float* parts;                      // [n][tiles][2][part_row]: sums of runs that cross tiles: from the tile before, into the next
+};
+void plan_embed(EmbedParams* prm);
+cudaError_t launch_embed_lookup(const EmbedParams& prm, cudaStream_t stream);
+cudaError_t launch_embed_gradient(const EmbedParams& prm, cudaStream_t stream);
+
 // ---------------------------------------------------------------------------------------------------- device helpers
 #ifdef __CUDACC__
 // A flag in device memory.

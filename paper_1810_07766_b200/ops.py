@@ -32,6 +32,7 @@ _DTYPE = {torch.float32: RPS_F32, torch.bfloat16: RPS_BF16}
 SYMBOLS = (
     "rps_lce_workspace", "rps_lce_forward", "rps_lce_backward", "rps_norm_forward", "rps_norm_workspace",
     "rps_norm_backward", "rps_pack_pitch", "rps_pack", "rps_unpack", "rps_wgrad_workspace", "rps_packed_wgrad",
+    "rps_embed_forward", "rps_embed_workspace", "rps_embed_backward",
     "rps_ops_check", "rps_ops_last_error",
 )
 
@@ -56,6 +57,12 @@ class rps_wgrad_desc(ctypes.Structure):
                 ("withhold_copies", _i32)]
 
 
+class rps_embed_desc(ctypes.Structure):
+    _fields_ = [("dtype", _i32), ("n", _i32), ("accumulate", _i32), ("reserved", _i32), ("tokens", _i64), ("vocab", _i64), ("cols", _i64),
+                ("ignore_index", _i64), ("weight_row", _i64), ("weight_worker", _i64), ("dweight_row", _i64), ("dweight_worker", _i64),
+                ("scale", _dbl)]
+
+
 _lib = None
 
 
@@ -64,7 +71,7 @@ def _library() -> ctypes.CDLL:
     if _lib is None:
         lib = binding.load_library()
         vp, cint, size = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t
-        lce, norm, wgrad = (ctypes.POINTER(t) for t in (rps_lce_desc, rps_norm_desc, rps_wgrad_desc))
+        lce, norm, wgrad, embed = (ctypes.POINTER(t) for t in (rps_lce_desc, rps_norm_desc, rps_wgrad_desc, rps_embed_desc))
         sizep = ctypes.POINTER(size)
         sig = {
             "rps_lce_workspace": (cint, [lce, vp, cint, sizep]),
@@ -78,6 +85,9 @@ def _library() -> ctypes.CDLL:
             "rps_unpack": (cint, [cint, _i64, _i64, vp, vp, vp, _i64, vp]),
             "rps_wgrad_workspace": (cint, [wgrad, vp, sizep]),
             "rps_packed_wgrad": (cint, [wgrad] + [vp] * 5 + [size, vp]),
+            "rps_embed_forward": (cint, [embed] + [vp] * 4),
+            "rps_embed_workspace": (cint, [embed, sizep]),
+            "rps_embed_backward": (cint, [embed] + [vp] * 4 + [size, vp]),
             "rps_ops_check": (cint, [vp]),
             "rps_ops_last_error": (ctypes.c_char_p, []),
         }
@@ -587,3 +597,96 @@ def gated_residual_norm(x: torch.Tensor, f: torch.Tensor, gate: torch.Tensor, po
         if isinstance(v, torch.Tensor) and v.requires_grad and torch.is_grad_enabled():
             raise ValueError(f"{name} gets no gradient: a learned factor belongs into gate or post")
     return _GatedResidualNorm.apply(x, f, gate, post, pre, float(scale), float(eps), keep)
+
+
+# ----------------------------------------------------------------------------------------------------------- embedding
+def _finite(name: str, value) -> float:
+    if isinstance(value, torch.Tensor) and value.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{name} gets no gradient: it has to be a number")
+    return float(value)
+
+
+def _tokens_of(tokens: torch.Tensor) -> Tuple[Tuple[int, ...], int, int]:
+    """(leading axes, workers, tokens) of int64 tokens."""
+    if tokens.dim() not in (1, 2) or tokens.dtype != torch.int64:
+        raise ValueError(f"tokens must be an int64 tensor [n, tokens] or [tokens], not {tokens.dtype} of {tuple(tokens.shape)}")
+    lead = tuple(tokens.shape[:-1])
+    return lead, lead[0] if lead else 1, tokens.shape[-1]
+
+
+def embedding_forward(tokens: torch.Tensor, weight: torch.Tensor, *, scale: float = 1.0, ignore_index: int = -100) -> torch.Tensor:
+    """``scale * weight[tokens]`` (``rps_embed_forward``): tokens int64 ``[n, tokens]``, weight ``[n, vocab, cols]``, the result
+    ``[n, tokens, cols]`` (all without ``n`` for a single worker).  Ignored tokens have rows of zeros."""
+    device = _device_of(tokens=tokens, weight=weight)
+    scale = float(scale)
+    key = ("embed", tokens.dtype, tokens.shape, weight.dtype, weight.shape, weight.stride(), scale, ignore_index)
+    plan = _plans.get(key)
+    if plan is None:
+        lead, n, count = _tokens_of(tokens)
+        if weight.dim() != len(lead) + 2:
+            raise ValueError("weight must be [n, vocab, cols] with tokens [n, tokens], or [vocab, cols] with [tokens]")
+        vocab, cols = weight.shape[-2:]
+        _check("weight", weight, None, lead + (vocab, cols))
+        d = rps_embed_desc(dtype=_DTYPE[weight.dtype], n=n, tokens=count, vocab=vocab, cols=cols, ignore_index=ignore_index, scale=scale)
+        d.weight_row, d.weight_worker = _matrix_strides("weight", weight)
+        plan = _keep(key, (ctypes.byref(d), _dense_layout(lead + (count, cols))))
+    tokens = tokens.contiguous()
+    out = _new(plan[1], weight.dtype, weight.device)
+    _call("rps_embed_forward", device, plan[0], tokens.data_ptr(), weight.data_ptr(), out.data_ptr(), _stream(device))
+    return out
+
+
+def embedding_backward(dout: torch.Tensor, tokens: torch.Tensor, vocab: int, *, scale: float = 1.0, ignore_index: int = -100,
+                       dweight: Optional[torch.Tensor] = None, accumulate: bool = False) -> torch.Tensor:
+    """Gradient ``[n, vocab, cols]`` of the table for the gradient dout ``[n, tokens, cols]`` of the forward call's result
+    (``rps_embed_backward``).  ``dweight``, if given, may be strided as in ``linear_cross_entropy_backward``; it is written, or with
+    ``accumulate`` added to: for a table that is also the output layer's weight, whose gradient is there already."""
+    device = _device_of(dout=dout, tokens=tokens)
+    if dweight is not None:
+        _device_of(dout=dout, dweight=dweight)
+    elif accumulate:
+        raise ValueError("accumulate needs a dweight to add to")
+    scale, accumulate = float(scale), bool(accumulate)
+    key = ("dembed", dout.dtype, dout.shape, dout.stride(), tokens.dtype, tokens.shape, vocab, scale, ignore_index, accumulate) + (
+        () if dweight is None else (dweight.dtype, dweight.shape, dweight.stride()))
+    plan = _plans.get(key)
+    if plan is None:
+        lead, n, count = _tokens_of(tokens)
+        if dout.dim() != len(lead) + 2:
+            raise ValueError("dout must be [n, tokens, cols] with tokens [n, tokens], or [tokens, cols] with [tokens]")
+        cols = dout.shape[-1]
+        _check("dout", dout, None, lead + (count, cols))
+        _dense("dout", dout)
+        d = rps_embed_desc(dtype=_DTYPE[dout.dtype], n=n, accumulate=accumulate, tokens=count, vocab=vocab, cols=cols, ignore_index=ignore_index, scale=scale,
+                           dweight_row=cols, dweight_worker=vocab * cols)
+        if dweight is not None:
+            _check("dweight", dweight, dout, lead + (vocab, cols))
+            d.dweight_row, d.dweight_worker = _matrix_strides("dweight", dweight)
+        size = ctypes.c_size_t()
+        _call("rps_embed_workspace", device, ctypes.byref(d), ctypes.byref(size))
+        plan = _keep(key, (ctypes.byref(d), _dense_layout(lead + (vocab, cols)), size.value, _dense_layout((size.value,))))
+    desc, layout, size, ws_layout = plan
+    tokens = tokens.contiguous()
+    if dweight is None:
+        dweight = _new(layout, dout.dtype, dout.device)
+    ws = _new(ws_layout, torch.uint8, dout.device)
+    _call("rps_embed_backward", device, desc, tokens.data_ptr(), dout.data_ptr(), dweight.data_ptr(), ws.data_ptr(), size, _stream(device))
+    return dweight
+
+
+class _Embedding(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, tokens, weight, scale, ignore_index):
+        ctx.save_for_backward(tokens)
+        ctx.vocab, ctx.settings = weight.shape[-2], {"scale": scale, "ignore_index": ignore_index}
+        return embedding_forward(tokens, weight, scale=scale, ignore_index=ignore_index)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dout):
+        return None, embedding_backward(dout.contiguous(), *ctx.saved_tensors, ctx.vocab, **ctx.settings), None, None
+
+
+def embedding(tokens: torch.Tensor, weight: torch.Tensor, *, scale: float = 1.0, ignore_index: int = -100) -> torch.Tensor:
+    """Differentiable ``embedding_forward``."""
+    return _Embedding.apply(tokens, weight, _finite("scale", scale), ignore_index)
