@@ -37,7 +37,9 @@ extern "C" {
 
 enum {
     RPS_PACK_GROUP = 128,       /* consecutive columns of a row that share one scale in 8-bit activations */
-    RPS_MAX_NORM_COLS = 16384   /* widest row of rps_norm_forward / rps_norm_backward                     */
+    RPS_MAX_NORM_COLS = 16384,  /* widest row of rps_norm_forward / rps_norm_backward                     */
+    RPS_MAX_TOP = 256,          /* most logits of a token that a teacher keeps for rps_distil_...         */
+    RPS_MAX_HEAD_COLS = 128     /* widest key or value of a head of rps_linear_attention_...              */
 };
 
 /* ------------------------------------------------------------------------------------------------------------------
@@ -93,6 +95,48 @@ int rps_lce_forward(const rps_lce_desc* desc, const void* hidden, const void* we
 int rps_lce_backward(const rps_lce_desc* desc, const void* hidden, const void* weight, const int64_t* targets,
                      const float* lse, const float* dloss, void* dhidden, void* dweight, void* workspace,
                      size_t workspace_bytes, void* cuda_stream);
+
+/* ------------------------------------------------------------------------------------------------------------------
+ * Distillation: how far the softmax of a linear layer over a large vocabulary is from a teacher of which the largest logits have
+ * been kept, without keeping the student's logits.  With tau the temperature and l as above, for each token
+ *
+ *   q_j  = exp(top_logits[j] / tau) / (sum of those over the token's entries j)
+ *   lse  = tau * log sum_v exp(l[v] / tau)                             (the soft maximum of the logits)
+ *   p[v] = exp((l[v] - lse) / tau)
+ *   loss = tau^2 * sum_j q_j * (log q_j - log p[top_ids[j]])
+ *   dl[v] = g * tau * (p[v] - sum of q_j with top_ids[j] == v),   dhidden = dl * weight,   dweight = dl^T * hidden
+ *
+ * An entry whose id is ignore_index, or whose logit is minus infinity, is none.  A token without entries takes no part: its row of hidden
+ * is not read, its loss and lse are 0 and its row of dhidden is 0; RPS_REDUCE_MEAN divides by the number of the others.  An id that is neither
+ * ignore_index nor in 0..vocab-1, or a logit that is NaN or infinity, is a mistake of the caller that the host cannot see: it gives that
+ * token's loss, and every gradient it takes part in, the value NaN.  A word may be in several entries, which count one by one.
+ * dl is rounded as in the cross entropy above.
+ * ------------------------------------------------------------------------------------------------------------------ */
+typedef struct rps_distil_desc {
+    int32_t dtype;         /* of hidden, weight, dhidden, dweight                                        */
+    int32_t reduction;     /* rps_reduction                                                              */
+    int32_t n;             /* workers, 1..RPS_MAX_WORKERS                                                */
+    int32_t top_dtype;     /* rps_dtype of top_logits                                                    */
+    int64_t tokens;        /* tokens of a worker, 0 <= tokens < 2^24, n * tokens < 2^31                  */
+    int64_t vocab;         /* rows of weight, 1 <= vocab < 2^30                                          */
+    int64_t cols;          /* width of hidden and weight, 1 <= cols < 2^24                               */
+    int64_t top;           /* entries of a token, 1..RPS_MAX_TOP                                         */
+    int64_t ignore_index;
+    int64_t hidden_row, hidden_worker;   /* strides as in rps_lce_desc                                   */
+    int64_t weight_row, weight_worker;
+    int64_t dweight_row, dweight_worker;
+    double temperature;    /* 1e-6..1e6                                                                  */
+} rps_distil_desc;
+
+/* As rps_lce_workspace. */
+int rps_distil_workspace(const rps_distil_desc* desc, const void* weight, int backward, size_t* bytes);
+
+/* top_ids: int64 [n][tokens][top], dense.  top_logits: the same in top_dtype.  The others as in rps_lce_forward and rps_lce_backward. */
+int rps_distil_forward(const rps_distil_desc* desc, const void* hidden, const void* weight, const int64_t* top_ids, const void* top_logits,
+                       float* loss, float* lse, void* workspace, size_t workspace_bytes, void* cuda_stream);
+int rps_distil_backward(const rps_distil_desc* desc, const void* hidden, const void* weight, const int64_t* top_ids,
+                        const void* top_logits, const float* lse, const float* dloss, void* dhidden, void* dweight, void* workspace,
+                        size_t workspace_bytes, void* cuda_stream);
 
 /* ------------------------------------------------------------------------------------------------------------------
  * The step between two blocks of a network: norm after the block, gate, residual scale, residual sum, norm before the
@@ -214,6 +258,62 @@ int rps_embed_forward(const rps_embed_desc* desc, const int64_t* tokens, const v
 int rps_embed_workspace(const rps_embed_desc* desc, size_t* bytes); /* of rps_embed_backward */
 int rps_embed_backward(const rps_embed_desc* desc, const int64_t* tokens, const void* dout, void* dweight, void* workspace,
                        size_t workspace_bytes, void* cuda_stream);
+
+/* ------------------------------------------------------------------------------------------------------------------
+ * Linear attention with a decay r = exp(log_decay) for each head, over the sequences of each worker.  For each head of a sequence
+ *
+ *   S_t = r S_(t-1) + k_t^T v_t,   out_t = scale * q_t S_t          S: [key_cols][value_cols], S before the first token: state_in
+ *
+ * and with R_t the gradient that reaches S_t (R after the last token: dstate_out)
+ *
+ *   R_t = r R_(t+1) + scale * q_t^T dout_t,   dq_t = scale * dout_t S_t^T,   dk_t = v_t R_t^T,   dv_t = k_t R_t,   dstate_in = r R_0
+ *
+ * (R_(t+1) taken without its factor r for the last token).  Sequences go through in chunks of 64 tokens, whose part of the sums is made
+ * as masked products; so an infinity or a NaN at a token may also reach results of the other tokens of its chunk.
+ *
+ * States are fp32, [n][sequences][heads][key_cols][value_cols], dense.  With RPS_BF16 the results that are bf16 are made of products of bf16 (of the masked
+ * scores, and of S where it meets a q, rounded); what is added to a state has 17 bits or more.
+ * log_decay: float [n][heads], at most 0 (minus infinity: r = 0); a positive one or a NaN makes its head's results NaN.  It gets no gradient.
+ * lengths: int64 [n][sequences], dense, or NULL (all tokens): only the first `length` tokens of a sequence take part (a length outside
+ * 0..tokens counts as the nearest of them).  The others are not read, their rows of out, dq, dk and dv are 0, and states are those after the
+ * last token that takes part.
+ * q, k, v and dout are [n][sequences][tokens][heads][cols] at any strides of the outer axes (parts of one projection's output, say); out, dq,
+ * dk and dv are dense in this order.  sequences and tokens may be 0.
+ * ------------------------------------------------------------------------------------------------------------------ */
+typedef struct rps_axis_strides {
+    int64_t worker, sequence, token, head;
+} rps_axis_strides;
+
+typedef struct rps_linear_attention_desc {
+    int32_t dtype;          /* of q, k, v, out, dout, dq, dk, dv                        */
+    int32_t n;              /* workers, 1..RPS_MAX_WORKERS                              */
+    int32_t heads;          /* 1..65535                                                 */
+    int32_t reserved;       /* 0                                                        */
+    int64_t sequences;      /* of a worker; n * sequences * heads < 2^28                */
+    int64_t tokens;         /* of a sequence, 0 <= tokens < 2^31                        */
+    int64_t key_cols, value_cols;   /* of a head, 1..RPS_MAX_HEAD_COLS                  */
+    rps_axis_strides q, k, v, dout; /* not negative (dout: backward only)               */
+    double scale;           /* finite                                                   */
+} rps_linear_attention_desc;
+
+/* Bytes of workspace that rps_linear_attention_forward (backward = 0) or _backward (backward = 1) wants. */
+int rps_linear_attention_workspace(const rps_linear_attention_desc* desc, int backward, size_t* bytes);
+
+/* state_in NULL: zeros.  state_out NULL: not wanted; it may not overlap state_in. */
+int rps_linear_attention_forward(const rps_linear_attention_desc* desc, const void* q, const void* k, const void* v,
+                                 const float* log_decay, const int64_t* lengths, const float* state_in, void* out,
+                                 float* state_out, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* dstate_out NULL: zeros.  dstate_in NULL: not wanted; it may not overlap dstate_out. */
+int rps_linear_attention_backward(const rps_linear_attention_desc* desc, const void* dout, const float* dstate_out, const void* q,
+                                  const void* k, const void* v, const float* log_decay, const int64_t* lengths,
+                                  const float* state_in, void* dq, void* dk, void* dv, float* dstate_in, void* workspace,
+                                  size_t workspace_bytes, void* cuda_stream);
+
+/* One token of every sequence (desc->tokens is 1, and the token strides count for nothing): out and the state after it, in fp32 throughout.
+ * state_out may be state_in itself, and may not overlap it otherwise. */
+int rps_linear_attention_step(const rps_linear_attention_desc* desc, const void* q, const void* k, const void* v, const float* log_decay,
+                              const float* state_in, void* out, float* state_out, void* cuda_stream);
 
 /* Every wait inside a kernel is bounded (two seconds, unless a description says otherwise): those of the matrix products on data, and those of the
  * norms whose rows are shared by several CTAs on one another's sums.  One that gives up ends its kernel early; what the call had

@@ -111,7 +111,9 @@ __global__ void __launch_bounds__(kRowThreads) rps_planes_kernel(const PlanesPar
 // warp at a time.  The sum over a worker's rows is made of the CTAs' sums by the one that finishes last, always in the same order.  8 rows
 // fill the SMs where 32 would not (4096 rows of 512 tiles 16 us against 25, 2048 of 196 6.0 against 10.4); where they would, fewer CTAs
 // to wait for are better (8192 rows of 32 tiles 13.1 against 7.7).
-template <int ROWS>
+// TOP: a row's loss is its divergence from the teacher, with the logits z of its entries, q their probabilities and lse the soft maximum of z:
+// tau^2 sum q (log q - (z - lse) / tau).
+template <int ROWS, bool TOP>
 __global__ void __launch_bounds__(kMergeThreads) rps_lce_merge_kernel(const LceParams prm)
 {
     after_the_kernel_before();
@@ -124,7 +126,8 @@ __global__ void __launch_bounds__(kMergeThreads) rps_lce_merge_kernel(const LceP
     float top = -INFINITY, sum = 0.0f;
     const auto join = [&](float2 p) {
         const float m = fmaxf(top, p.x), at = m == -INFINITY ? 0.0f : m;
-        sum = sum * __expf(top - at) + p.y * __expf(p.x - at);
+        const float factor = TOP ? prm.sharpness : 1.0f;
+        sum = sum * __expf((top - at) * factor) + p.y * __expf((p.x - at) * factor);
         top = m;
     };
     if (i < count) {
@@ -150,11 +153,24 @@ __global__ void __launch_bounds__(kMergeThreads) rps_lce_merge_kernel(const LceP
     for (int k = 0; k < ROWS * kMergeThreads / 32 / 32; ++k) join(parts[lane / ROWS + k * (32 / ROWS)][lane % ROWS]);
 #pragma unroll
     for (int s = ROWS; s < 32; s *= 2) join(make_float2(__shfl_xor_sync(0xFFFFFFFFu, top, s), __shfl_xor_sync(0xFFFFFFFFu, sum, s)));
-    float loss = 0.0f;
+    float loss = 0.0f, apart = 0.0f;
+    const float lse = TOP ? top + prm.factor * logf(sum) : top + logf(sum);
+    if constexpr (TOP) {
+        // the lanes of a row share its entries
+        if (i < count) {
+            const int64_t first = (w * prm.tokens + prm.rows[w * prm.tokens + i]) * prm.top;
+#pragma unroll 4
+            for (int e = lane / ROWS; e < prm.top; e += 32 / ROWS) {
+                const float q = prm.entry_weight[first + e];
+                if (q != 0.0f) apart = fmaf(q, lse - prm.entry_logit[first + e], apart);  // the logits of the others are not there
+            }
+        }
+#pragma unroll
+        for (int s = ROWS; s < 32; s *= 2) apart += __shfl_xor_sync(0xFFFFFFFFu, apart, s);
+    }
     if (i < count && lane < ROWS) {
-        const float lse = top + logf(sum);
-        loss = lse - prm.hit[w * prm.tokens_padded + i];
         const int64_t t = prm.rows[w * prm.tokens + i];
+        loss = TOP ? prm.factor * fmaf(prm.factor, prm.entropy[w * prm.tokens + t], apart) : lse - prm.hit[w * prm.tokens_padded + i];
         prm.lse[w * prm.tokens + t] = lse;
         if (prm.reduction == RPS_REDUCE_NONE) prm.loss[w * prm.tokens + t] = loss;
     }
@@ -218,8 +234,12 @@ int64_t lce_merge_blocks(int64_t tokens) { return ceil_div(tokens, kMergeRows); 
 cudaError_t launch_lce_merge(const LceParams& prm, cudaStream_t stream)
 {
     const int64_t many = ceil_div(prm.tokens, kManyMergeRows);
-    if (many * prm.n >= kSms) return launch_after(rps_lce_merge_kernel<kManyMergeRows>, dim3((unsigned)many, (unsigned)prm.n), kMergeThreads, 0, stream, 1, prm);
-    return launch_after(rps_lce_merge_kernel<kMergeRows>, dim3((unsigned)lce_merge_blocks(prm.tokens), (unsigned)prm.n), kMergeThreads, 0, stream, 1, prm);
+    if (many * prm.n >= kSms) {
+        const auto kernel = prm.top > 0 ? rps_lce_merge_kernel<kManyMergeRows, true> : rps_lce_merge_kernel<kManyMergeRows, false>;
+        return launch_after(kernel, dim3((unsigned)many, (unsigned)prm.n), kMergeThreads, 0, stream, 1, prm);
+    }
+    const auto kernel = prm.top > 0 ? rps_lce_merge_kernel<kMergeRows, true> : rps_lce_merge_kernel<kMergeRows, false>;
+    return launch_after(kernel, dim3((unsigned)lce_merge_blocks(prm.tokens), (unsigned)prm.n), kMergeThreads, 0, stream, 1, prm);
 }
 
 // A launch counts its pieces of 16 bytes in 32 bits, so a matrix of 64 GiB and more takes several.

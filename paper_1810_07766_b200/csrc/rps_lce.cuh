@@ -80,7 +80,7 @@ __device__ __forceinline__ int select_tokens(const LceParams& prm, int w, bool w
             // A factor that all rows share stays out of dl: near a token's target dl is p - 1, which bf16 holds all but exactly, and
             // (p - 1) times a factor it does not (relative error of the gradients: 2.7e-3 -> 1.7e-3, 1.65e-3 of it the rounding of the
             // result).
-            prm.scale[w] = prm.reduction == RPS_REDUCE_NONE || kept == 0 ? 1.0f : prm.reduction == RPS_REDUCE_MEAN ? prm.dloss[w] / (float)kept : prm.dloss[w];
+            prm.scale[w] = prm.factor * (prm.reduction == RPS_REDUCE_NONE || kept == 0 ? 1.0f : prm.reduction == RPS_REDUCE_MEAN ? prm.dloss[w] / (float)kept : prm.dloss[w]);
         } else {
             prm.done[w] = 0;
             if (kept == 0 && prm.reduction != RPS_REDUCE_NONE) prm.loss[w] = 0.0f;

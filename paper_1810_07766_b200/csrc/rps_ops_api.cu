@@ -47,6 +47,7 @@ struct LcePlan {
     float* hidden_parts = nullptr;
     float* weight_parts = nullptr;
     ProductShape hidden_shape{}, weight_shape{};
+    TeacherParams teacher{};  // distillation
     size_t bytes = 0;
 };
 
@@ -64,7 +65,8 @@ int check_lce(const rps_lce_desc* d)
     return RPS_OK;
 }
 
-LcePlan plan_lce(const rps_lce_desc& d, const void* weight, bool backward, void* workspace)
+// top > 0: distillation.
+LcePlan plan_lce(const rps_lce_desc& d, const void* weight, bool backward, void* workspace, int top = 0, double temperature = 1.0)
 {
     LcePlan plan;
     LceParams& p = plan.p;
@@ -73,7 +75,8 @@ LcePlan plan_lce(const rps_lce_desc& d, const void* weight, bool backward, void*
     p.vocab = d.vocab, p.cols = d.cols, p.cols_padded = round_up(d.cols, 8), p.ignore_index = d.ignore_index;
     p.hidden_row = d.hidden_row, p.hidden_worker = d.hidden_worker;
     plan.lay_out_weight = p.f32 || !aligned_matrix(weight, d.weight_row, d.weight_worker);
-    plan_lce_dot(&p);
+    p.top = top, p.factor = (float)temperature, p.sharpness = (float)(1.0 / temperature);
+    if (top == 0) plan_lce_dot(&p);
     if (p.dot_rows > 0) {
         Carver c{static_cast<unsigned char*>(workspace)};
         p.count = c.take<int>(p.n);
@@ -132,6 +135,19 @@ LcePlan plan_lce(const rps_lce_desc& d, const void* weight, bool backward, void*
         p.part = c.take<float2>(p.n * p.stat_tiles * p.tokens_padded);
         p.hit = c.take<float>(p.n * p.tokens_padded);
     }
+    if (top > 0) {
+        TeacherParams& t = plan.teacher;
+        t.n = p.n, t.top = top, t.tokens = p.tokens, t.vocab = p.vocab, t.sharpness = p.sharpness;
+        t.entry_id = c.take<int>(p.n * p.tokens * top);
+        t.entry_weight = c.take<float>(p.n * p.tokens * top);
+        t.targets = c.take<int64_t>(p.n * p.tokens);
+        if (!backward) {
+            t.entropy = c.take<float>(p.n * p.tokens);
+            g.entry_logit = c.take<float>(p.n * p.tokens * top);
+        }
+        g.top = top, g.sharpness = p.sharpness, g.entry_id = t.entry_id, g.entry_weight = t.entry_weight;
+        p.targets = t.targets, p.entropy = t.entropy, p.entry_id = t.entry_id, p.entry_weight = t.entry_weight, p.entry_logit = g.entry_logit;
+    }
     plan.bytes = c.used;
 
     g.workers = p.n, g.planes = p.planes, g.count = p.count;
@@ -188,6 +204,59 @@ extern "C" int rps_lce_workspace(const rps_lce_desc* desc, const void* weight, i
     return RPS_OK;
 }
 
+namespace {
+
+// The products of a forward pass, once the plan knows its arrays and the tokens that take part have been sorted out.
+int lce_statistics(const rps_lce_desc& d, const LcePlan& plan, const void* weight, cudaStream_t stream)
+{
+    const LceParams& p = plan.p;
+    ProductParams g = plan.product;
+    g.a = hidden_operand(p);
+    g.m = (int)d.tokens, g.k = (int)d.cols;
+    for (int64_t v0 = 0; v0 < d.vocab; v0 += plan.piece) {
+        const int64_t rows = d.vocab - v0 < plan.piece ? d.vocab - v0 : plan.piece;
+        if (int rc = weight_operand(d, plan, weight, v0, rows, &g.b, stream)) return rc;
+        g.v0 = (int)v0, g.n = (int)rows;
+        RPS_TRY(launch_product(p.top > 0 ? Product::kTopLse : Product::kLse, g, stream));
+    }
+    RPS_TRY(launch_lce_merge(p, stream));
+    return RPS_OK;
+}
+
+// Those of a backward pass.
+int lce_gradients(const rps_lce_desc& d, const LcePlan& plan, const void* weight, void* dhidden, void* dweight, cudaStream_t stream)
+{
+    const LceParams& p = plan.p;
+    const Operand h = hidden_operand(p);
+    for (int64_t v0 = 0; v0 < d.vocab; v0 += plan.piece) {
+        const int64_t rows = d.vocab - v0 < plan.piece ? d.vocab - v0 : plan.piece;
+        const int64_t tiled = round_up(rows, plan.product.tile_cols);  // dl is written (zeros behind the last row) in whole tiles
+        Operand weight_rows;
+        if (int rc = weight_operand(d, plan, weight, v0, rows, &weight_rows, stream)) return rc;
+        const int64_t plane = p.tokens_padded * plan.piece;
+        const Operand dl{plan.dl, p.planes * plane, plane, plan.piece, p.tokens_padded, tiled};
+        ProductParams g = plan.product;
+        g.v0 = (int)v0;
+        if (d.tokens > 0) {
+            g.a = h, g.b = weight_rows, g.m = (int)d.tokens, g.n = (int)rows, g.k = (int)d.cols;
+            RPS_TRY(launch_product(p.top > 0 ? Product::kTopDlogits : Product::kDlogits, g, stream));
+            g.a = dl, g.n = (int)d.cols, g.k = (int)rows, g.shaped(plan.hidden_shape);
+            g.parts = plan.hidden_parts, g.part_rows = p.tokens_padded, g.part_row = round_up(d.cols, g.tile_cols), g.add = v0 > 0;
+            g.out = dhidden, g.out_row = d.cols, g.out_worker = d.tokens * d.cols;
+            RPS_TRY(launch_product(Product::kDhidden, g, stream));
+            if (g.parts != nullptr && v0 + rows == d.vocab) RPS_TRY(launch_join(Product::kDhidden, g, stream));
+        }
+        g.a = dl, g.b = h, g.m = (int)rows, g.n = (int)d.cols, g.k = (int)d.tokens, g.shaped(plan.weight_shape);
+        g.parts = plan.weight_parts, g.part_rows = plan.piece, g.part_row = round_up(d.cols, g.tile_cols), g.add = 0;
+        g.out = static_cast<unsigned char*>(dweight) + v0 * d.dweight_row * (p.f32 ? 4 : 2), g.out_row = d.dweight_row, g.out_worker = d.dweight_worker;
+        RPS_TRY(launch_product(Product::kDweight, g, stream));
+        if (g.parts != nullptr) RPS_TRY(launch_join(Product::kDweight, g, stream));
+    }
+    return RPS_OK;
+}
+
+}  // namespace
+
 extern "C" int rps_lce_forward(const rps_lce_desc* desc, const void* hidden, const void* weight, const int64_t* targets,
                                float* loss, float* lse, void* workspace, size_t workspace_bytes, void* cuda_stream)
 {
@@ -209,18 +278,7 @@ extern "C" int rps_lce_forward(const rps_lce_desc* desc, const void* hidden, con
         return RPS_OK;
     }
     RPS_TRY(launch_lce_rows(p, stream));
-    if (d.tokens == 0) return RPS_OK;
-    ProductParams g = plan.product;
-    g.a = hidden_operand(p);
-    g.m = (int)d.tokens, g.k = (int)d.cols;
-    for (int64_t v0 = 0; v0 < d.vocab; v0 += plan.piece) {
-        const int64_t rows = d.vocab - v0 < plan.piece ? d.vocab - v0 : plan.piece;
-        if (int rc = weight_operand(d, plan, weight, v0, rows, &g.b, stream)) return rc;
-        g.v0 = (int)v0, g.n = (int)rows;
-        RPS_TRY(launch_product(Product::kLse, g, stream));
-    }
-    RPS_TRY(launch_lce_merge(p, stream));
-    return RPS_OK;
+    return d.tokens == 0 ? RPS_OK : lce_statistics(d, plan, weight, stream);
 }
 
 extern "C" int rps_lce_backward(const rps_lce_desc* desc, const void* hidden, const void* weight, const int64_t* targets,
@@ -253,32 +311,87 @@ extern "C" int rps_lce_backward(const rps_lce_desc* desc, const void* hidden, co
         return RPS_OK;
     }
     RPS_TRY(launch_lce_rows(p, stream));
-    const Operand h = hidden_operand(p);
-    for (int64_t v0 = 0; v0 < d.vocab; v0 += plan.piece) {
-        const int64_t rows = d.vocab - v0 < plan.piece ? d.vocab - v0 : plan.piece;
-        const int64_t tiled = round_up(rows, plan.product.tile_cols);  // dl is written (zeros behind the last row) in whole tiles
-        Operand weight_rows;
-        if (int rc = weight_operand(d, plan, weight, v0, rows, &weight_rows, stream)) return rc;
-        const int64_t plane = p.tokens_padded * plan.piece;
-        const Operand dl{plan.dl, p.planes * plane, plane, plan.piece, p.tokens_padded, tiled};
-        ProductParams g = plan.product;
-        g.v0 = (int)v0;
-        if (d.tokens > 0) {
-            g.a = h, g.b = weight_rows, g.m = (int)d.tokens, g.n = (int)rows, g.k = (int)d.cols;
-            RPS_TRY(launch_product(Product::kDlogits, g, stream));
-            g.a = dl, g.n = (int)d.cols, g.k = (int)rows, g.shaped(plan.hidden_shape);
-            g.parts = plan.hidden_parts, g.part_rows = p.tokens_padded, g.part_row = round_up(d.cols, g.tile_cols), g.add = v0 > 0;
-            g.out = dhidden, g.out_row = d.cols, g.out_worker = d.tokens * d.cols;
-            RPS_TRY(launch_product(Product::kDhidden, g, stream));
-            if (g.parts != nullptr && v0 + rows == d.vocab) RPS_TRY(launch_join(Product::kDhidden, g, stream));
-        }
-        g.a = dl, g.b = h, g.m = (int)rows, g.n = (int)d.cols, g.k = (int)d.tokens, g.shaped(plan.weight_shape);
-        g.parts = plan.weight_parts, g.part_rows = plan.piece, g.part_row = round_up(d.cols, g.tile_cols), g.add = 0;
-        g.out = static_cast<unsigned char*>(dweight) + v0 * d.dweight_row * (p.f32 ? 4 : 2), g.out_row = d.dweight_row, g.out_worker = d.dweight_worker;
-        RPS_TRY(launch_product(Product::kDweight, g, stream));
-        if (g.parts != nullptr) RPS_TRY(launch_join(Product::kDweight, g, stream));
-    }
+    return lce_gradients(d, plan, weight, dhidden, dweight, stream);
+}
+
+// ------------------------------------------------------------------------------------------------------------ distillation
+namespace {
+
+// The description of the loss that goes with it: the same arrays but for the targets.
+int check_distil(const rps_distil_desc* d, rps_lce_desc* lce)
+{
+    if (d == nullptr) return fail(RPS_EINVAL, "desc is NULL");
+    *lce = {d->dtype, d->reduction, d->n, d->tokens, d->vocab, d->cols, kNoTeacher, d->hidden_row, d->hidden_worker, d->weight_row, d->weight_worker, d->dweight_row,
+            d->dweight_worker};
+    if (int rc = check_lce(lce)) return rc;
+    if (d->top_dtype != RPS_F32 && d->top_dtype != RPS_BF16) return fail(RPS_EINVAL, "top_dtype %d is neither RPS_F32 nor RPS_BF16", d->top_dtype);
+    if (d->top < 1) return fail(RPS_EINVAL, "top = %lld", (long long)d->top);
+    if (d->top > RPS_MAX_TOP) return fail(RPS_ELIMIT, "top = %lld; up to %d logits of a token are possible", (long long)d->top, (int)RPS_MAX_TOP);
+    if (d->n * d->tokens >= 1ll << 31) return fail(RPS_EINVAL, "n * tokens = %lld", (long long)(d->n * d->tokens));
+    // 1 / temperature and its square stay far from the ends of fp32
+    if (!(d->temperature >= 1e-6 && d->temperature <= 1e6)) return fail(RPS_EINVAL, "temperature = %g; 1e-6..1e6 are possible", d->temperature);
     return RPS_OK;
+}
+
+// The teacher's probabilities, and which tokens take part.
+int sort_out(const rps_distil_desc& d, const LcePlan& plan, const int64_t* top_ids, const void* top_logits, cudaStream_t stream)
+{
+    if (d.tokens > 0) {
+        TeacherParams t = plan.teacher;
+        t.ids = top_ids, t.logits = top_logits, t.top_f32 = d.top_dtype == RPS_F32, t.ignore_index = d.ignore_index;
+        RPS_TRY(launch_teacher(t, stream));
+    }
+    RPS_TRY(launch_lce_rows(plan.p, stream));
+    return RPS_OK;
+}
+
+}  // namespace
+
+extern "C" int rps_distil_workspace(const rps_distil_desc* desc, const void* weight, int backward, size_t* bytes)
+{
+    start();
+    if (bytes == nullptr) return fail(RPS_EINVAL, "bytes is NULL");
+    rps_lce_desc lce;
+    if (int rc = check_distil(desc, &lce)) return rc;
+    *bytes = plan_lce(lce, weight, backward != 0, nullptr, (int)desc->top, desc->temperature).bytes;
+    return RPS_OK;
+}
+
+extern "C" int rps_distil_forward(const rps_distil_desc* desc, const void* hidden, const void* weight, const int64_t* top_ids, const void* top_logits,
+                                  float* loss, float* lse, void* workspace, size_t workspace_bytes, void* cuda_stream)
+{
+    start();
+    rps_lce_desc d;
+    if (int rc = check_distil(desc, &d)) return rc;
+    if (weight == nullptr || (d.tokens > 0 && (hidden == nullptr || top_ids == nullptr || top_logits == nullptr || lse == nullptr)) ||
+        (loss == nullptr && (d.tokens > 0 || d.reduction != RPS_REDUCE_NONE)))
+        return fail(RPS_EINVAL, "NULL array");
+    LcePlan plan = plan_lce(d, weight, false, workspace, (int)desc->top, desc->temperature);
+    if (int rc = check_workspace(workspace, workspace_bytes, plan.bytes)) return rc;
+    const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    plan.p.hidden = hidden, plan.p.loss = loss, plan.p.lse = lse;
+    if (int rc = sort_out(*desc, plan, top_ids, top_logits, stream)) return rc;
+    return d.tokens == 0 ? RPS_OK : lce_statistics(d, plan, weight, stream);
+}
+
+extern "C" int rps_distil_backward(const rps_distil_desc* desc, const void* hidden, const void* weight, const int64_t* top_ids, const void* top_logits,
+                                   const float* lse, const float* dloss, void* dhidden, void* dweight, void* workspace, size_t workspace_bytes,
+                                   void* cuda_stream)
+{
+    start();
+    rps_lce_desc d;
+    if (int rc = check_distil(desc, &d)) return rc;
+    if (int rc = check_output_strides("dweight", d.n, d.vocab, d.cols, d.dweight_row, d.dweight_worker)) return rc;
+    if (weight == nullptr || dweight == nullptr ||
+        (d.tokens > 0 && (hidden == nullptr || top_ids == nullptr || top_logits == nullptr || lse == nullptr || dhidden == nullptr)) ||
+        (dloss == nullptr && (d.tokens > 0 || d.reduction != RPS_REDUCE_NONE)))
+        return fail(RPS_EINVAL, "NULL array");
+    LcePlan plan = plan_lce(d, weight, true, workspace, (int)desc->top, desc->temperature);
+    if (int rc = check_workspace(workspace, workspace_bytes, plan.bytes)) return rc;
+    const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    plan.p.hidden = hidden, plan.p.lse_in = lse, plan.p.dloss = dloss, plan.p.dhidden = dhidden;
+    if (int rc = sort_out(*desc, plan, top_ids, top_logits, stream)) return rc;
+    return lce_gradients(d, plan, weight, dhidden, dweight, stream);
 }
 
 // ------------------------------------------------------------------------------------------------------------ norm

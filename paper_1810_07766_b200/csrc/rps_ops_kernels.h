@@ -51,6 +51,8 @@ struct Operand {
 enum class Product {
     kLse,      // A = hidden [m][k], B = weight [n][k]: softmax statistics of each row over a tile of columns
     kDlogits,  // the same product: dl = g (exp(l - lse) - [v == target]) into planes
+    kTopLse,   // kLse of logits times `sharpness`, and the logits of each row's entries
+    kTopDlogits,  // kDlogits of them, less the probabilities of the row's entries instead of a target's one
     kDhidden,  // A = dl [m][k], B = weight [k][n]: a sum over pieces of the vocabulary, then scattered to the tokens' rows
     kDweight   // A = dl or dy [k][m], B = hidden or x [k][n]
 };
@@ -73,6 +75,12 @@ struct ProductParams {
     float* hit;             // [worker][tokens_padded]: the target's logit
     const float2* info;     // [worker][tokens_padded]: lse, g
     bf16* dl;               // [worker][plane][tokens_padded][piece]
+    // kTopLse, kTopDlogits: up to `top` entries of each token, by rising row of the weight (behind the last: the largest int)
+    int top;
+    float sharpness;
+    const int* entry_id;       // [worker][tokens][top]
+    const float* entry_weight; // their probabilities
+    float* entry_logit;        // written by kTopLse
     int64_t tokens_padded, piece;
     // kDhidden, kDweight: the result, scaled and in the caller's type, or (part != NULL) fp32 parts of it that launch_join adds up
     void* out;
@@ -119,6 +127,12 @@ struct LceParams {
     const float2* part;
     const float* hit;
     int64_t stat_tiles;  // as ProductParams
+    float factor, sharpness;  // of the loss's gradient, and of the logits: 1 but for distillation
+    // distillation (top > 0): see ProductParams
+    int top;
+    const float* entropy;     // [n][tokens]: sum of p log p over the entries
+    const int* entry_id;
+    const float *entry_weight, *entry_logit;
     float* loss;
     float* lse;
     float* sums;      // [n][lce_merge_blocks(tokens)]
@@ -138,10 +152,25 @@ void plan_lce_dot(LceParams* prm);
 cudaError_t launch_lce_dot(const LceParams& prm, cudaStream_t stream);         // statistics, or (backward) dl
 cudaError_t launch_lce_dot_grads(const LceParams& prm, cudaStream_t stream);   // dweight, and dhidden's parts
 
+// Distillation's teacher: its entries' probabilities, sorted by row of the weight, and which tokens have any.
+struct TeacherParams {
+    int n, top, top_f32;
+    int64_t tokens, vocab, ignore_index;
+    float sharpness;
+    const int64_t* ids;     // [n][tokens][top]
+    const void* logits;
+    int* entry_id;          // as ProductParams
+    float* entry_weight;
+    float* entropy;         // [n][tokens], or NULL
+    int64_t* targets;       // [n][tokens]: 0, kNoTeacher for a token without entries, -1 for one whose entries are no distribution
+};
+constexpr int64_t kNoTeacher = -100;
+cudaError_t launch_teacher(const TeacherParams& prm, cudaStream_t stream);
+
 // Which tokens take part, and their rows laid out.
 cudaError_t launch_lce_rows(const LceParams& prm, cudaStream_t stream);
 int64_t lce_merge_blocks(int64_t tokens);
-cudaError_t launch_lce_merge(const LceParams& prm, cudaStream_t stream);
+cudaError_t launch_lce_merge(const LceParams& prm, cudaStream_t stream);  // the loss, or (top > 0) the divergence from the teacher
 
 // Lays the rows of a matrix of each worker out as planes; columns past `cols` become zero.
 struct PlanesParams {
@@ -216,6 +245,41 @@ struct EmbedParams {
 void plan_embed(EmbedParams* prm);
 cudaError_t launch_embed_lookup(const EmbedParams& prm, cudaStream_t stream);
 cudaError_t launch_embed_gradient(const EmbedParams& prm, cudaStream_t stream);
+
+// ---------------------------------------------------------------------------------------------------- linear attention
+constexpr int kMixChunk = 64, kMixMaxCols = RPS_MAX_HEAD_COLS, kMixSegments = 64;
+
+// [worker][sequence][token][head][cols]; strides
+struct MixOperand {
+    const void* base;
+    int64_t worker, sequence, token, head;
+};
+
+// One form (rps_mix.cu).
+struct MixTerm {
+    MixOperand x, y, z;
+    void* out;              // [worker][sequence][token][head][b], dense
+    int a, b, reversed;     // columns of x and y, and of z; whether time runs backwards
+    const float* state_in;  // a * b of each unit, or NULL: zeros
+    float* state_out;       // or NULL
+    int64_t state_a, state_b;  // strides of the states' elements
+    float score_scale, state_scale, update_scale;  // of x . y, of x W, and of what is added to W
+};
+
+struct MixParams {
+    int f32, n, heads, terms;
+    int64_t sequences, tokens;
+    const int64_t* lengths;   // [n][sequences], or NULL
+    const float* log_decay;   // [n][heads]
+    MixTerm term[3];
+    // plan_mix
+    int64_t units, segment_tokens, state_room;
+    int columns, segments, join_blocks;
+    float* segment_states;    // [term][unit][segment][state_room] (segments > 1)
+};
+void plan_mix(MixParams* prm);
+cudaError_t launch_mix(const MixParams& prm, cudaStream_t stream);
+cudaError_t launch_mix_step(const MixParams& prm, cudaStream_t stream);
 
 // ---------------------------------------------------------------------------------------------------- device helpers
 #ifdef __CUDACC__

@@ -412,22 +412,55 @@ __device__ __forceinline__ void store_parts(Stage& stage, float (&v)[COLS], Rows
     }
 }
 
+template <Product WHICH>
+constexpr bool kTop = WHICH == Product::kTopLse || WHICH == Product::kTopDlogits;
+template <Product WHICH>
+constexpr bool kStatistics = WHICH == Product::kLse || WHICH == Product::kTopLse;
+template <Product WHICH>
+constexpr bool kGradient = WHICH == Product::kDlogits || WHICH == Product::kTopDlogits;
+
 // What the epilogue needs to know of a row, read while the products are still on their way.
 struct RowInfo {
     int target;   // kLse, kDlogits: less the first column of this warp
-    float2 info;  // kDlogits: lse and g
+    float2 info;  // kDlogits, kTopDlogits: lse and g
     int index;    // of the row where it is stored, -1 if it is not
     float scale;
+    // kTopLse, kTopDlogits: the row's entries, the next of them from this warp's columns on, and its column (the largest int: none)
+    int64_t entries;
+    int next, next_col;
 };
+
+__device__ __forceinline__ int entry_column(const ProductParams& prm, const RowInfo& r, int first)
+{
+    return r.next < prm.top ? __ldg(prm.entry_id + r.entries + r.next) - first : 0x7FFFFFFF;
+}
 
 template <Product WHICH>
 __device__ __forceinline__ RowInfo row_info(const ProductParams& prm, int w, int row, int n0, int count)
 {
     RowInfo r{};
     const bool in = row < (WHICH == Product::kDweight ? prm.m : count);
-    if constexpr (WHICH == Product::kLse || WHICH == Product::kDlogits) {
-        r.target = in ? __ldg(prm.target + w * prm.tokens_padded + row) - prm.v0 - n0 : -1;
-        if (WHICH == Product::kDlogits && in) r.info = __ldg(prm.info + w * prm.tokens_padded + row);
+    if constexpr (kStatistics<WHICH> || kGradient<WHICH>) {
+        if constexpr (kTop<WHICH>) {
+            r.next = prm.top, r.next_col = 0x7FFFFFFF;
+            if (in) {
+                r.entries = (w * prm.tokens + __ldg(prm.rows + w * prm.tokens + row)) * prm.top;
+                const int first = prm.v0 + n0;
+                int low = 0, high = prm.top;
+                while (low < high) {
+                    const int middle = (low + high) / 2;
+                    if (__ldg(prm.entry_id + r.entries + middle) < first)
+                        low = middle + 1;
+                    else
+                        high = middle;
+                }
+                r.next = low;
+                r.next_col = entry_column(prm, r, first);
+            }
+        } else {
+            r.target = in ? __ldg(prm.target + w * prm.tokens_padded + row) - prm.v0 - n0 : -1;
+        }
+        if (kGradient<WHICH> && in) r.info = __ldg(prm.info + w * prm.tokens_padded + row);
         // the product with dl over the tokens reads whole blocks of them: zeros behind the last one
         r.index = row < (count + kDepth - 1) / kDepth * kDepth ? row : -1;
     } else {
@@ -437,15 +470,16 @@ __device__ __forceinline__ RowInfo row_info(const ProductParams& prm, int w, int
     return r;
 }
 
-// kLse: a warp's columns of one row of a tile, `width` of them.  `turn`: tiles that the warp has had.  False if a wait gave up.
-template <int PLANES, int COLS>
-__device__ __forceinline__ bool statistics(const ProductParams& prm, int w, int row, int n0, int width, int count, const RowInfo& info, float (&v)[COLS],
+// kLse, kTopLse: a warp's columns of one row of a tile, `width` of them.  `turn`: tiles that the warp has had.  False if a wait gave up.
+template <Product WHICH, int PLANES, int COLS>
+__device__ __forceinline__ bool statistics(const ProductParams& prm, int w, int row, int n0, int width, int count, RowInfo& info, float (&v)[COLS],
                                            Control& control, int quarter, int part, int turn, uint64_t limit_ns)
 {
     constexpr int kParts = Epilogue<PLANES>::kParts;
     const int cols = min(width, prm.n - n0);
     // in runs of 32 columns, as a narrow tile has fewer
-    const int t = info.target;
+    const int t = kTop<WHICH> ? -1 : info.target;
+    const float factor = kTop<WHICH> ? prm.sharpness * kLog2e : kLog2e;
     float top = -INFINITY, sum = 0.0f;
 #pragma unroll
     for (int c = 0; c < COLS; c += 32) {
@@ -471,7 +505,18 @@ __device__ __forceinline__ bool statistics(const ProductParams& prm, int w, int 
             prm.hit[w * prm.tokens_padded + row] = hit;
         }
 #pragma unroll
-        for (int j = c; j < c + 32; j += 2) total = total + exp_of_difference(Pair(v[j], v[j + 1]), at);
+        for (int j = c; j < c + 32; j += 2) total = total + exp_of_difference(Pair(v[j], v[j + 1]), at, factor);
+    }
+    if constexpr (kTop<WHICH>) {
+        while (info.next_col < cols) {
+            float logit = 0.0f;
+#pragma unroll
+            for (int j = 0; j < COLS; ++j)
+                if (j == info.next_col) logit = v[j];
+            prm.entry_logit[info.entries + info.next] = logit;
+            ++info.next;
+            info.next_col = entry_column(prm, info, prm.v0 + n0);
+        }
     }
     sum = total.sum();
     // The warps of these rows put theirs together.  There is room for four tiles' in turn, as none of them can be more than two tiles
@@ -489,27 +534,41 @@ __device__ __forceinline__ bool statistics(const ProductParams& prm, int w, int 
     for (int k = 1; k < kParts; ++k) {
         const float2 p = row_statistics[k * 128 + r];
         const float m = fmaxf(top, p.x), from = m == -INFINITY ? 0.0f : m;
-        sum = fmaf(sum, exp_of_difference(top, from), p.y * exp_of_difference(p.x, from));
+        sum = fmaf(sum, exp_of_difference(top, from, factor), p.y * exp_of_difference(p.x, from, factor));
         top = m;
     }
     prm.part[((int64_t)w * prm.stat_tiles + (prm.v0 + n0) / prm.tile_cols) * prm.tokens_padded + row] = make_float2(top, sum);
     return true;
 }
 
-// The other products: columns n0.. of one row of a tile, `width` (at most COLS) of them.
+// The other products: columns n0.. of one row of a tile, `width` (at most COLS) of them, the first of them being this warp's column c0.
 template <Product WHICH, int PLANES, int COLS, typename Stage>
-__device__ __forceinline__ void store_columns(const ProductParams& prm, int w, int split, int row, int n0, int width, int count, int target,
-                                              const RowInfo& info, float (&v)[COLS], bool wide, Stage& stage)
+__device__ __forceinline__ void store_columns(const ProductParams& prm, int w, int split, int row, int n0, int width, int count, int c0,
+                                              RowInfo& info, float (&v)[COLS], bool wide, Stage& stage)
 {
     const int cols = min(width, prm.n - n0);
-    if constexpr (WHICH == Product::kDlogits) {
+    if constexpr (kGradient<WHICH>) {
         const bool in = row < count;
+        const int target = kTop<WHICH> ? -1 : info.target - c0;
+        if constexpr (kTop<WHICH>) {
+            const float factor = prm.sharpness * kLog2e;
+#pragma unroll
+            for (int j = 0; j < COLS; ++j) v[j] = exp_of_difference(v[j], info.info.x, factor);
+            while (info.next_col - c0 < cols) {
+                const float q = __ldg(prm.entry_weight + info.entries + info.next);
+#pragma unroll
+                for (int j = 0; j < COLS; ++j)
+                    if (j == info.next_col - c0) v[j] -= q;
+                ++info.next;
+                info.next_col = entry_column(prm, info, prm.v0 + n0 - c0);
+            }
+        }
 #pragma unroll
         for (int c = 0; c < COLS; c += 32) {
             if (c >= width) break;
 #pragma unroll
             for (int j = c; j < c + 32; ++j) {
-                const float p = exp_of_difference(v[j], info.info.x) - (j == target ? 1.0f : 0.0f);
+                const float p = kTop<WHICH> ? v[j] : exp_of_difference(v[j], info.info.x) - (j == target ? 1.0f : 0.0f);
                 v[j] = in && j < cols ? info.info.y * p : 0.0f;
             }
         }
@@ -629,7 +688,7 @@ __global__ void __launch_bounds__(Epilogue<PLANES>::kThreads, 1)
         return t;
     };
     // blocks to a segment
-    const int segment = PLANES == 3 ? kSegmentF32 : WHICH == Product::kLse ? kSegmentStatistics : LONG ? kSegmentBf16 : 1 << 30;
+    const int segment = PLANES == 3 ? kSegmentF32 : kStatistics<WHICH> ? kSegmentStatistics : LONG ? kSegmentBf16 : 1 << 30;
     bool fine = true;
     const uint64_t limit_ns = prm.wait_limit_ms > 0 ? (uint64_t)prm.wait_limit_ms * 1000000u : rps::kDefaultWaitLimitNs;
     const auto wait = [&](uint32_t bar, uint32_t parity) { return wait_for(bar, parity, limit_ns); };
@@ -758,12 +817,12 @@ __global__ void __launch_bounds__(Epilogue<PLANES>::kThreads, 1)
         for (int tile = blockIdx.x / CTAS; tile < total && fine; tile += groups) {
             const Tile t = tile_at(tile);
             const int row = t.m0 + (int)rank * 128 + quarter * 32 + lane, n0 = t.n0 + part * part_n;
-            const RowInfo info = row_info<WHICH>(prm, t.w, row, n0, t.count);
+            RowInfo info = row_info<WHICH>(prm, t.w, row, n0, t.count);
             // a warp none of whose rows is wanted only keeps step
-            const bool idle = t.m0 + (int)rank * 128 + quarter * 32 >= (WHICH == Product::kDweight ? prm.m : WHICH == Product::kDlogits ? (t.count + kDepth - 1) / kDepth * kDepth : t.count);
+            const bool idle = t.m0 + (int)rank * 128 + quarter * 32 >= (WHICH == Product::kDweight ? prm.m : kGradient<WHICH> ? (t.count + kDepth - 1) / kDepth * kDepth : t.count);
             const uint32_t columns = tensor_memory + ((uint32_t)(quarter * 32) << 16) + part * part_n;
             auto& staging = staging_of<PLANES>(control)[warp - Epilogue<PLANES>::kFirst];
-            if constexpr (PLANES == 1 && WHICH != Product::kLse && !LONG) {  // one segment
+            if constexpr (PLANES == 1 && !kStatistics<WHICH> && !LONG) {  // one segment
                 if (t.blocks > 0 && !summed()) break;
 #pragma unroll 1
                 for (int c = 0; c < part_n && !idle; c += 32) {
@@ -775,7 +834,7 @@ __global__ void __launch_bounds__(Epilogue<PLANES>::kThreads, 1)
 #pragma unroll
                         for (int j = 0; j < 32; ++j) v[j] = 0.0f;
                     }
-                    store_columns<WHICH, PLANES>(prm, t.w, t.split, row, n0 + c, min(32, part_n - c), t.count, info.target - c, info, v, wide, staging);
+                    store_columns<WHICH, PLANES>(prm, t.w, t.split, row, n0 + c, min(32, part_n - c), t.count, c, info, v, wide, staging);
                 }
                 if (t.blocks > 0 && idle) taken();
             } else {
@@ -791,10 +850,10 @@ __global__ void __launch_bounds__(Epilogue<PLANES>::kThreads, 1)
                 }
                 if (!fine) break;
                 if (idle) continue;
-                if constexpr (WHICH == Product::kLse)
-                    fine = statistics<PLANES>(prm, t.w, row, n0, part_n, t.count, info, v, control, quarter, part, turn++, limit_ns);
+                if constexpr (kStatistics<WHICH>)
+                    fine = statistics<WHICH, PLANES>(prm, t.w, row, n0, part_n, t.count, info, v, control, quarter, part, turn++, limit_ns);
                 else
-                    store_columns<WHICH, PLANES>(prm, t.w, t.split, row, n0, part_n, t.count, info.target, info, v, wide, staging);
+                    store_columns<WHICH, PLANES>(prm, t.w, t.split, row, n0, part_n, t.count, 0, info, v, wide, staging);
             }
         }
     }
@@ -868,7 +927,7 @@ cudaError_t launch(const ProductParams& prm, cudaStream_t stream)
 template <Product WHICH, int PLANES>
 cudaError_t launch_pairs_or_not(const ProductParams& prm, cudaStream_t stream)
 {
-    if constexpr (PLANES == 1 && WHICH != Product::kLse) {  // the others have segments in any case
+    if constexpr (PLANES == 1 && !kStatistics<WHICH>) {  // the others have segments in any case
         const int64_t run = ceil_div(ceil_div(prm.k, kDepth), std::max(prm.splits, 1));
         if (run > kSegmentBf16) return prm.ctas == 2 ? launch<WHICH, PLANES, 2, true>(prm, stream) : launch<WHICH, PLANES, 1, true>(prm, stream);
     }
@@ -1002,6 +1061,8 @@ cudaError_t launch_product(Product which, const ProductParams& prm, cudaStream_t
     switch (which) {
         case Product::kLse: return f32 ? launch_pairs_or_not<Product::kLse, 3>(prm, stream) : launch_pairs_or_not<Product::kLse, 1>(prm, stream);
         case Product::kDlogits: return f32 ? launch_pairs_or_not<Product::kDlogits, 3>(prm, stream) : launch_pairs_or_not<Product::kDlogits, 1>(prm, stream);
+        case Product::kTopLse: return f32 ? launch_pairs_or_not<Product::kTopLse, 3>(prm, stream) : launch_pairs_or_not<Product::kTopLse, 1>(prm, stream);
+        case Product::kTopDlogits: return f32 ? launch_pairs_or_not<Product::kTopDlogits, 3>(prm, stream) : launch_pairs_or_not<Product::kTopDlogits, 1>(prm, stream);
         case Product::kDhidden: return f32 ? launch_pairs_or_not<Product::kDhidden, 3>(prm, stream) : launch_pairs_or_not<Product::kDhidden, 1>(prm, stream);
         default: return f32 ? launch_pairs_or_not<Product::kDweight, 3>(prm, stream) : launch_pairs_or_not<Product::kDweight, 1>(prm, stream);
     }

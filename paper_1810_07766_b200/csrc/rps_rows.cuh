@@ -146,13 +146,14 @@ __device__ __forceinline__ Pair operator+(const Pair& a, const Pair& b)
 
 // exp(v - at).  The difference comes before the factor: v * log2(e) - at * log2(e) is off by a unit of the products' last place, which beyond 2^30
 // is outside the exponent's range, so that a row's largest logit gave infinity or zero instead of one.
-__device__ __forceinline__ float exp_of_difference(float v, float at) { return exp2_fast((v - at) * kLog2e); }
+// `factor`: log2(e), or that times what the difference is multiplied by.
+__device__ __forceinline__ float exp_of_difference(float v, float at, float factor = kLog2e) { return exp2_fast((v - at) * factor); }
 
 // The same of two values.
-__device__ __forceinline__ Pair exp_of_difference(const Pair& v, float at)
+__device__ __forceinline__ Pair exp_of_difference(const Pair& v, float at, float factor = kLog2e)
 {
     float a, b;
-    ((v + Pair(-at)) * Pair(kLog2e)).get(a, b);
+    ((v + Pair(-at)) * Pair(factor)).get(a, b);
     return Pair(exp2_fast(a), exp2_fast(b));
 }
 

@@ -25,14 +25,17 @@ from .binding import RPS_BF16, RPS_F32, RPS_OK, RPSError
 
 GROUP = 128               # columns that share a scale in 8-bit activations (RPS_PACK_GROUP)
 MAX_NORM_COLS = 16384     # RPS_MAX_NORM_COLS
+MAX_HEAD_COLS = 128       # RPS_MAX_HEAD_COLS
+MAX_TOP = 256             # RPS_MAX_TOP
 _REDUCTION = {"none": 0, "sum": 1, "mean": 2}
 _DTYPE = {torch.float32: RPS_F32, torch.bfloat16: RPS_BF16}
 
 # every symbol include/rps_ops.h declares
 SYMBOLS = (
-    "rps_lce_workspace", "rps_lce_forward", "rps_lce_backward", "rps_norm_forward", "rps_norm_workspace",
+    "rps_lce_workspace", "rps_lce_forward", "rps_lce_backward", "rps_distil_workspace", "rps_distil_forward", "rps_distil_backward", "rps_norm_forward", "rps_norm_workspace",
     "rps_norm_backward", "rps_pack_pitch", "rps_pack", "rps_unpack", "rps_wgrad_workspace", "rps_packed_wgrad",
-    "rps_embed_forward", "rps_embed_workspace", "rps_embed_backward",
+    "rps_embed_forward", "rps_embed_workspace", "rps_embed_backward", "rps_linear_attention_workspace",
+    "rps_linear_attention_forward", "rps_linear_attention_backward", "rps_linear_attention_step",
     "rps_ops_check", "rps_ops_last_error",
 )
 
@@ -43,6 +46,12 @@ class rps_lce_desc(ctypes.Structure):
     _fields_ = [("dtype", _i32), ("reduction", _i32), ("n", _i32), ("tokens", _i64), ("vocab", _i64), ("cols", _i64),
                 ("ignore_index", _i64), ("hidden_row", _i64), ("hidden_worker", _i64), ("weight_row", _i64),
                 ("weight_worker", _i64), ("dweight_row", _i64), ("dweight_worker", _i64)]
+
+
+class rps_distil_desc(ctypes.Structure):
+    _fields_ = [("dtype", _i32), ("reduction", _i32), ("n", _i32), ("top_dtype", _i32), ("tokens", _i64), ("vocab", _i64), ("cols", _i64), ("top", _i64),
+                ("ignore_index", _i64), ("hidden_row", _i64), ("hidden_worker", _i64), ("weight_row", _i64), ("weight_worker", _i64), ("dweight_row", _i64),
+                ("dweight_worker", _i64), ("temperature", _dbl)]
 
 
 class rps_norm_desc(ctypes.Structure):
@@ -63,6 +72,16 @@ class rps_embed_desc(ctypes.Structure):
                 ("scale", _dbl)]
 
 
+class rps_axis_strides(ctypes.Structure):
+    _fields_ = [("worker", _i64), ("sequence", _i64), ("token", _i64), ("head", _i64)]
+
+
+class rps_linear_attention_desc(ctypes.Structure):
+    _fields_ = [("dtype", _i32), ("n", _i32), ("heads", _i32), ("reserved", _i32), ("sequences", _i64), ("tokens", _i64), ("key_cols", _i64),
+                ("value_cols", _i64), ("q", rps_axis_strides), ("k", rps_axis_strides), ("v", rps_axis_strides), ("dout", rps_axis_strides),
+                ("scale", _dbl)]
+
+
 _lib = None
 
 
@@ -71,12 +90,16 @@ def _library() -> ctypes.CDLL:
     if _lib is None:
         lib = binding.load_library()
         vp, cint, size = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t
-        lce, norm, wgrad, embed = (ctypes.POINTER(t) for t in (rps_lce_desc, rps_norm_desc, rps_wgrad_desc, rps_embed_desc))
+        lce, distil, norm, wgrad, embed, attention = (
+            ctypes.POINTER(t) for t in (rps_lce_desc, rps_distil_desc, rps_norm_desc, rps_wgrad_desc, rps_embed_desc, rps_linear_attention_desc))
         sizep = ctypes.POINTER(size)
         sig = {
             "rps_lce_workspace": (cint, [lce, vp, cint, sizep]),
             "rps_lce_forward": (cint, [lce] + [vp] * 6 + [size, vp]),
             "rps_lce_backward": (cint, [lce] + [vp] * 8 + [size, vp]),
+            "rps_distil_workspace": (cint, [distil, vp, cint, sizep]),
+            "rps_distil_forward": (cint, [distil] + [vp] * 7 + [size, vp]),
+            "rps_distil_backward": (cint, [distil] + [vp] * 9 + [size, vp]),
             "rps_norm_forward": (cint, [norm] + [vp] * 14),
             "rps_norm_workspace": (cint, [norm, sizep]),
             "rps_norm_backward": (cint, [norm] + [vp] * 17 + [size, vp]),
@@ -88,6 +111,10 @@ def _library() -> ctypes.CDLL:
             "rps_embed_forward": (cint, [embed] + [vp] * 4),
             "rps_embed_workspace": (cint, [embed, sizep]),
             "rps_embed_backward": (cint, [embed] + [vp] * 4 + [size, vp]),
+            "rps_linear_attention_workspace": (cint, [attention, cint, sizep]),
+            "rps_linear_attention_forward": (cint, [attention] + [vp] * 9 + [size, vp]),
+            "rps_linear_attention_backward": (cint, [attention] + [vp] * 13 + [size, vp]),
+            "rps_linear_attention_step": (cint, [attention] + [vp] * 8),
             "rps_ops_check": (cint, [vp]),
             "rps_ops_last_error": (ctypes.c_char_p, []),
         }
@@ -193,6 +220,12 @@ def _parameter_stride(name: str, t: torch.Tensor) -> int:
     if not part.is_contiguous():
         raise ValueError(f"each worker's part of {name} must be contiguous")
     return t.stride(0) if t.shape[0] > 1 else 0
+
+
+def _finite(name: str, value) -> float:
+    if isinstance(value, torch.Tensor) and value.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{name} gets no gradient: it has to be a number")
+    return float(value)
 
 
 # ------------------------------------------------------------------------------------------------------------ the loss
@@ -307,6 +340,115 @@ def linear_cross_entropy(hidden: torch.Tensor, weight: torch.Tensor, targets: to
                          reduction: str = "mean") -> torch.Tensor:
     """Differentiable ``linear_cross_entropy_forward``: the loss alone."""
     return _LinearCrossEntropy.apply(hidden, weight, targets, ignore_index, reduction)
+
+
+# --------------------------------------------------------------------------------------------------------- distillation
+def _distil_plan(hidden, weight, top_ids, top_logits, temperature, ignore_index, reduction, dweight=None) -> _LcePlan:
+    at = weight.data_ptr() & 15
+    key = ("distil", hidden.dtype, hidden.shape, hidden.stride(), weight.dtype, weight.shape, weight.stride(), at, top_ids.dtype, top_ids.shape, top_logits.dtype,
+           top_logits.shape, temperature, ignore_index, reduction) + (() if dweight is None else (dweight.dtype, dweight.shape, dweight.stride()))
+    plan = _plans.get(key)
+    if plan is not None:
+        return plan
+    if reduction not in _REDUCTION:
+        raise ValueError(f"reduction must be one of {sorted(_REDUCTION)}")
+    if hidden.dim() not in (2, 3):
+        raise ValueError("hidden must be a tensor [n, tokens, cols] or [tokens, cols]")
+    lead = tuple(hidden.shape[:-2])
+    tokens, cols = hidden.shape[-2:]
+    _check("hidden", hidden, None, tuple(hidden.shape))
+    if weight.dim() != hidden.dim():
+        raise ValueError("weight must be [n, vocab, cols] with hidden [n, tokens, cols], or [vocab, cols] with [tokens, cols]")
+    vocab = weight.shape[-2]
+    _check("weight", weight, hidden, lead + (vocab, cols))
+    if top_ids.dtype != torch.int64 or top_ids.dim() != hidden.dim() or tuple(top_ids.shape[:-1]) != lead + (tokens,):
+        raise ValueError(f"top_ids must be int64 of shape {lead + (tokens, 'top')}, not {top_ids.dtype} of {tuple(top_ids.shape)}")
+    _check("top_logits", top_logits, None, tuple(top_ids.shape))
+    d = rps_distil_desc(dtype=_DTYPE[hidden.dtype], reduction=_REDUCTION[reduction], n=lead[0] if lead else 1, top_dtype=_DTYPE[top_logits.dtype], tokens=tokens,
+                        vocab=vocab, cols=cols, top=top_ids.shape[-1], ignore_index=ignore_index, temperature=temperature)
+    d.hidden_row, d.hidden_worker = _matrix_strides("hidden", hidden)
+    d.weight_row, d.weight_worker = _matrix_strides("weight", weight)
+    if dweight is not None:
+        _check("dweight", dweight, hidden, tuple(weight.shape))
+        d.dweight_row, d.dweight_worker = _matrix_strides("dweight", dweight)
+    else:
+        d.dweight_row, d.dweight_worker = cols, vocab * cols
+    sizes = []
+    for backward in (0, 1):
+        size = ctypes.c_size_t()
+        _call("rps_distil_workspace", hidden.get_device(), ctypes.byref(d), at, backward, ctypes.byref(size))
+        sizes.append(size.value)
+    each = _dense_layout(lead + (tokens,))
+    return _keep(key, _LcePlan(ctypes.byref(d), each, each if reduction == "none" else _dense_layout(lead), _dense_layout(hidden.shape),
+                               _dense_layout(weight.shape), tuple(sizes), tuple(_dense_layout((size,)) for size in sizes)))
+
+
+def linear_distillation_forward(hidden: torch.Tensor, weight: torch.Tensor, top_ids: torch.Tensor, top_logits: torch.Tensor, *, temperature: float = 1.0,
+                                ignore_index: int = -100, reduction: str = "mean") -> Tuple[torch.Tensor, torch.Tensor]:
+    """(loss, lse): ``temperature ** 2`` times the divergence of ``softmax(hidden @ weight.T / temperature)`` from a teacher's
+    ``softmax(top_logits / temperature)`` over the words top_ids (``rps_distil_forward``).
+
+    hidden ``[n, tokens, cols]``, weight ``[n, vocab, cols]``, top_ids int64 and top_logits (float32 or bfloat16) ``[n, tokens, top]``, as
+    ``torch.topk`` gives them, in any order (all without ``n`` for a single worker).  Entries whose id is ignore_index are none, and tokens without
+    entries take no part.  loss as in ``linear_cross_entropy_forward``; lse, float32 ``[n, tokens]``, is what the backward pass wants: the
+    logits' soft maximum, ``temperature * logsumexp(logits / temperature)``."""
+    device = _device_of(hidden=hidden, weight=weight, top_ids=top_ids, top_logits=top_logits)
+    plan = _distil_plan(hidden, weight, top_ids, top_logits, float(temperature), ignore_index, reduction)
+    top_ids, top_logits = top_ids.contiguous(), top_logits.contiguous()
+    where = hidden.device
+    loss, lse = _new(plan.loss, torch.float32, where), _new(plan.tokens, torch.float32, where)
+    ws = _new(plan.workspace[0], torch.uint8, where)
+    _call("rps_distil_forward", device, plan.desc, hidden.data_ptr(), weight.data_ptr(), top_ids.data_ptr(), top_logits.data_ptr(), loss.data_ptr(), lse.data_ptr(),
+          ws.data_ptr(), plan.sizes[0], _stream(device))
+    return loss, lse
+
+
+def linear_distillation_backward(dloss: torch.Tensor, hidden: torch.Tensor, weight: torch.Tensor, top_ids: torch.Tensor, top_logits: torch.Tensor,
+                                 lse: torch.Tensor, *, temperature: float = 1.0, ignore_index: int = -100, reduction: str = "mean",
+                                 dweight: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(dhidden, dweight) for the gradient ``dloss`` (float32, shaped as the loss) of the forward call with the same
+    arguments (``rps_distil_backward``).  ``dweight`` as in ``linear_cross_entropy_backward``.  The teacher gets no gradient."""
+    device = _device_of(hidden=hidden, weight=weight, top_ids=top_ids, top_logits=top_logits, dloss=dloss, lse=lse)
+    if dweight is not None:
+        _device_of(hidden=hidden, dweight=dweight)
+    plan = _distil_plan(hidden, weight, top_ids, top_logits, float(temperature), ignore_index, reduction, dweight)
+    top_ids, top_logits = top_ids.contiguous(), top_logits.contiguous()
+    for name, t, shape in (("dloss", dloss, plan.loss[0]), ("lse", lse, plan.tokens[0])):
+        if t.dtype != torch.float32 or t.shape != shape:
+            raise ValueError(f"{name} must be a float32 tensor of shape {shape}")
+        _dense(name, t)
+    where = hidden.device
+    if dweight is None:
+        dweight = _new(plan.weight, weight.dtype, where)
+    dhidden = _new(plan.hidden, hidden.dtype, where)
+    ws = _new(plan.workspace[1], torch.uint8, where)
+    _call("rps_distil_backward", device, plan.desc, hidden.data_ptr(), weight.data_ptr(), top_ids.data_ptr(), top_logits.data_ptr(), lse.data_ptr(), dloss.data_ptr(),
+          dhidden.data_ptr(), dweight.data_ptr(), ws.data_ptr(), plan.sizes[1], _stream(device))
+    return dhidden, dweight
+
+
+class _LinearDistillation(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, hidden, weight, top_ids, top_logits, temperature, ignore_index, reduction):
+        settings = {"temperature": temperature, "ignore_index": ignore_index, "reduction": reduction}
+        loss, lse = linear_distillation_forward(hidden, weight, top_ids, top_logits, **settings)
+        ctx.save_for_backward(hidden, weight, top_ids, top_logits, lse)
+        ctx.settings = settings
+        return loss
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dloss):
+        dhidden, dweight = linear_distillation_backward(dloss.float().contiguous(), *ctx.saved_tensors, **ctx.settings)
+        return dhidden, dweight, None, None, None, None, None
+
+
+def linear_distillation(hidden: torch.Tensor, weight: torch.Tensor, top_ids: torch.Tensor, top_logits: torch.Tensor, *, temperature: float = 1.0,
+                        ignore_index: int = -100, reduction: str = "mean") -> torch.Tensor:
+    """Differentiable ``linear_distillation_forward``: the loss alone."""
+    if isinstance(top_logits, torch.Tensor) and top_logits.requires_grad and torch.is_grad_enabled():
+        raise ValueError("top_logits gets no gradient: detach the teacher")
+    return _LinearDistillation.apply(hidden, weight, top_ids, top_logits, _finite("temperature", temperature), ignore_index, reduction)
 
 
 # ------------------------------------------------------------------------------------------------------ 8-bit activations
@@ -600,12 +742,6 @@ def gated_residual_norm(x: torch.Tensor, f: torch.Tensor, gate: torch.Tensor, po
 
 
 # ----------------------------------------------------------------------------------------------------------- embedding
-def _finite(name: str, value) -> float:
-    if isinstance(value, torch.Tensor) and value.requires_grad and torch.is_grad_enabled():
-        raise ValueError(f"{name} gets no gradient: it has to be a number")
-    return float(value)
-
-
 def _tokens_of(tokens: torch.Tensor) -> Tuple[Tuple[int, ...], int, int]:
     """(leading axes, workers, tokens) of int64 tokens."""
     if tokens.dim() not in (1, 2) or tokens.dtype != torch.int64:
@@ -690,3 +826,178 @@ class _Embedding(torch.autograd.Function):
 def embedding(tokens: torch.Tensor, weight: torch.Tensor, *, scale: float = 1.0, ignore_index: int = -100) -> torch.Tensor:
     """Differentiable ``embedding_forward``."""
     return _Embedding.apply(tokens, weight, _finite("scale", scale), ignore_index)
+
+
+# ---------------------------------------------------------------------------------------------------- linear attention
+def _head_strides(name: str, t: torch.Tensor, tokens: bool) -> rps_axis_strides:
+    """Strides of [n, sequences, tokens, heads, cols] (without `tokens` for single tokens); an axis of one element takes any."""
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"the last axis of {name} must be contiguous")
+    strides = [t.stride(i) if t.shape[i] > 1 else 0 for i in range(t.dim() - 1)]
+    if not tokens:
+        strides.insert(-1, 0)
+    if len(strides) == 3:
+        strides.insert(0, 0)
+    return rps_axis_strides(*strides)
+
+
+class _AttentionPlan(NamedTuple):
+    desc: object
+    out: object                        # layouts
+    keys: object
+    values: object
+    state: object
+    sizes: Tuple[int, int]             # bytes of workspace, forward and backward
+    workspace: Tuple[object, object]
+
+
+def _attention_plan(q, k, v, log_decay, state, lengths, scale, dout=None, tokens=True) -> _AttentionPlan:
+    key = ("attention", tokens, scale) + tuple(None if t is None else (t.dtype, t.shape, t.stride()) for t in (q, k, v, log_decay, state, lengths, dout))
+    plan = _plans.get(key)
+    if plan is not None:
+        return plan
+    axes = 4 if tokens else 3
+    if q.dim() not in (axes, axes + 1):
+        shape = "[n, sequences, tokens, heads, cols]" if tokens else "[n, sequences, heads, cols]"
+        raise ValueError(f"q must be a tensor {shape}, or without n")
+    lead = tuple(q.shape[:-1])         # all but the columns
+    workers = lead[:q.dim() - axes]
+    heads = q.shape[-2]
+    _check("q", q, None, tuple(q.shape))
+    _check("k", k, q, tuple(q.shape))
+    if v.dim() != q.dim():
+        raise ValueError("v must have the axes of q and k")
+    _check("v", v, q, lead + (v.shape[-1],))
+    key_cols, value_cols = q.shape[-1], v.shape[-1]
+    sequences = q.shape[len(workers)]
+    n = workers[0] if workers else 1
+    if log_decay.dtype != torch.float32 or tuple(log_decay.shape) != workers + (heads,):
+        raise ValueError(f"log_decay must be a float32 tensor of shape {workers + (heads,)}")
+    _dense("log_decay", log_decay)
+    layout = _dense_layout(workers + (sequences, heads, key_cols, value_cols))
+    if state is not None:
+        if state.dtype != torch.float32 or tuple(state.shape) != layout[0]:
+            raise ValueError(f"state must be a float32 tensor of shape {layout[0]}")
+        _dense("state", state)
+    if lengths is not None and (lengths.dtype != torch.int64 or tuple(lengths.shape) != workers + (sequences,)):
+        raise ValueError(f"lengths must be an int64 tensor of shape {workers + (sequences,)}")
+    d = rps_linear_attention_desc(dtype=_DTYPE[q.dtype], n=n, heads=heads, sequences=sequences, tokens=q.shape[-3] if tokens else 1, key_cols=key_cols,
+                                  value_cols=value_cols, scale=scale)
+    d.q, d.k, d.v = (_head_strides(name, t, tokens) for name, t in (("q", q), ("k", k), ("v", v)))
+    if dout is not None:
+        _check("dout", dout, q, tuple(v.shape))
+        d.dout = _head_strides("dout", dout, tokens)
+    sizes = []
+    for backward in (0, 1):
+        size = ctypes.c_size_t()
+        _call("rps_linear_attention_workspace", q.get_device(), ctypes.byref(d), backward, ctypes.byref(size))
+        sizes.append(size.value)
+    values = _dense_layout(v.shape)
+    return _keep(key, _AttentionPlan(ctypes.byref(d), values, _dense_layout(q.shape), values, layout, tuple(sizes), tuple(_dense_layout((size,)) for size in sizes)))
+
+
+def _pointer(t: Optional[torch.Tensor]):
+    return None if t is None else t.data_ptr()
+
+
+def _attention_device(state, lengths, **tensors) -> int:
+    if state is not None:
+        tensors["state"] = state
+    if lengths is not None:
+        tensors["lengths"] = lengths
+    return _device_of(**tensors)
+
+
+def linear_attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_decay: torch.Tensor, *, scale: Optional[float] = None,
+                             state: Optional[torch.Tensor] = None, lengths: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(out, state after the last token) of ``S = exp(log_decay) S + k^T v; out = scale q S``, token by token
+    (``rps_linear_attention_forward``).
+
+    q, k ``[n, sequences, tokens, heads, key_cols]``, v the same with value_cols, at any strides of the outer axes; log_decay float32 ``[n, heads]``,
+    at most 0; state (None: zeros) float32 ``[n, sequences, heads, key_cols, value_cols]``; lengths int64 ``[n, sequences]``: how many of a
+    sequence's tokens take part (None: all), the rows of the others are zeros; all without ``n`` for a single worker.  scale is
+    ``key_cols ** -0.5`` unless given."""
+    device = _attention_device(state, lengths, q=q, k=k, v=v, log_decay=log_decay)
+    plan = _attention_plan(q, k, v, log_decay, state, lengths, float(q.shape[-1] ** -0.5 if scale is None else scale))
+    if lengths is not None:
+        lengths = lengths.contiguous()
+    where = q.device
+    out, after = _new(plan.out, q.dtype, where), _new(plan.state, torch.float32, where)
+    ws = _new(plan.workspace[0], torch.uint8, where)
+    _call("rps_linear_attention_forward", device, plan.desc, q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(), _pointer(lengths), _pointer(state),
+          out.data_ptr(), after.data_ptr(), ws.data_ptr(), plan.sizes[0], _stream(device))
+    return out, after
+
+
+def linear_attention_backward(dout: torch.Tensor, dstate: Optional[torch.Tensor], q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_decay: torch.Tensor, *,
+                              scale: Optional[float] = None, state: Optional[torch.Tensor] = None, lengths: Optional[torch.Tensor] = None):
+    """(dq, dk, dv, gradient of the first state) for the gradients dout and dstate (None: none reaches the last state) of the forward
+    call's results with the same arguments (``rps_linear_attention_backward``).  log_decay and scale get no gradient."""
+    device = _attention_device(state, lengths, q=q, k=k, v=v, log_decay=log_decay, dout=dout)
+    plan = _attention_plan(q, k, v, log_decay, state, lengths, float(q.shape[-1] ** -0.5 if scale is None else scale), dout)
+    if dstate is not None:
+        _device_of(q=q, dstate=dstate)
+        if dstate.dtype != torch.float32 or dstate.shape != plan.state[0]:
+            raise ValueError(f"dstate must be a float32 tensor of shape {plan.state[0]}")
+        _dense("dstate", dstate)
+    if lengths is not None:
+        lengths = lengths.contiguous()
+    where = q.device
+    dq, dk, dv = _new(plan.keys, q.dtype, where), _new(plan.keys, q.dtype, where), _new(plan.values, q.dtype, where)
+    first = _new(plan.state, torch.float32, where)
+    ws = _new(plan.workspace[1], torch.uint8, where)
+    _call("rps_linear_attention_backward", device, plan.desc, dout.data_ptr(), _pointer(dstate), q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(),
+          _pointer(lengths), _pointer(state), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), first.data_ptr(), ws.data_ptr(), plan.sizes[1], _stream(device))
+    return dq, dk, dv, first
+
+
+def linear_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_decay: torch.Tensor, state: torch.Tensor, *, scale: Optional[float] = None,
+                          new_state: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """``linear_attention_forward`` of one more token of every sequence (``rps_linear_attention_step``): q, k ``[n, sequences, heads, key_cols]``, v
+    with value_cols.  The state is updated in place, or written to ``new_state``, which does not overlap it, if that is given."""
+    device = _device_of(q=q, k=k, v=v, log_decay=log_decay, state=state)
+    plan = _attention_plan(q, k, v, log_decay, state, None, float(q.shape[-1] ** -0.5 if scale is None else scale), tokens=False)
+    if new_state is None:
+        new_state = state
+    else:
+        _device_of(q=q, new_state=new_state)
+        if new_state.dtype != torch.float32 or new_state.shape != plan.state[0]:
+            raise ValueError(f"new_state must be a float32 tensor of shape {plan.state[0]}")
+        _dense("new_state", new_state)
+        apart = abs(new_state.data_ptr() - state.data_ptr())
+        if 0 < apart < 4 * state.numel():
+            raise ValueError("new_state overlaps state")
+    out = _new(plan.out, q.dtype, q.device)
+    _call("rps_linear_attention_step", device, plan.desc, q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(), state.data_ptr(), out.data_ptr(),
+          new_state.data_ptr(), _stream(device))
+    return out
+
+
+class _LinearAttention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, log_decay, scale, state, lengths):
+        out, after = linear_attention_forward(q, k, v, log_decay, scale=scale, state=state, lengths=lengths)
+        ctx.set_materialize_grads(False)
+        ctx.save_for_backward(q, k, v, log_decay, state, lengths)
+        ctx.scale = scale
+        return out, after
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dout, dstate):
+        q, k, v, log_decay, state, lengths = ctx.saved_tensors
+        if dout is None:  # out was not used
+            dout = torch.zeros_like(v)
+        elif dout.shape[-1] > 1 and dout.stride(-1) != 1:
+            dout = dout.contiguous()
+        dq, dk, dv, first = linear_attention_backward(dout, None if dstate is None else dstate.contiguous(), q, k, v, log_decay, scale=ctx.scale, state=state,
+                                                      lengths=lengths)
+        return dq, dk, dv, None, None, first if state is not None else None, None
+
+
+def linear_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_decay: torch.Tensor, *, scale: Optional[float] = None,
+                     state: Optional[torch.Tensor] = None, lengths: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Differentiable ``linear_attention_forward``: (out, state after the last token)."""
+    if isinstance(log_decay, torch.Tensor) and log_decay.requires_grad and torch.is_grad_enabled():
+        raise ValueError("log_decay gets no gradient: the heads' decays are constants of the model")
+    return _LinearAttention.apply(q, k, v, log_decay, _finite("scale", q.shape[-1] ** -0.5 if scale is None else scale), state, lengths)
