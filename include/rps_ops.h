@@ -288,6 +288,9 @@ typedef struct rps_linear_attention_desc {
     int32_t dtype;          /* of q, k, v, out, dout, dq, dk, dv                        */
     int32_t n;              /* workers, 1..RPS_MAX_WORKERS                              */
     int32_t heads;          /* 1..65535                                                 */
+    int32_t wait_limit_ms;  /* every wait of a kernel on data gives up after this many milliseconds (0 = 2000) */
+    int32_t withhold_copies; /* test aid for that: 1 = kernels that copy ahead issue no copies, so their waits run out, the results
+                                are not written and rps_ops_check reports it; 0 otherwise */
     int32_t reserved;       /* 0                                                        */
     int64_t sequences;      /* of a worker; n * sequences * heads < 2^28                */
     int64_t tokens;         /* of a sequence, 0 <= tokens < 2^31                        */
@@ -315,7 +318,7 @@ int rps_linear_attention_backward(const rps_linear_attention_desc* desc, const v
 int rps_linear_attention_step(const rps_linear_attention_desc* desc, const void* q, const void* k, const void* v, const float* log_decay,
                               const float* state_in, void* out, float* state_out, void* cuda_stream);
 
-/* Every wait inside a kernel is bounded (two seconds, unless a description says otherwise): those of the matrix products on data, and those of the
+/* Every wait inside a kernel is bounded (two seconds, unless a description says otherwise): those of the matrix products and of linear attention on data, and those of the
  * norms whose rows are shared by several CTAs on one another's sums.  One that gives up ends its kernel early; what the call had
  * not written by then is not written, and what it has written is not valid.  rps_ops_check synchronises the stream and returns
  * RPS_ECUDA if that happened on the current device since the last check. */

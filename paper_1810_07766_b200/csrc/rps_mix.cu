@@ -14,11 +14,11 @@
 //
 // Products go through the tensor cores (mma.sync: tiles are 64 x 64 with 16 rows to a warp, and every operand is scaled or masked in registers
 // on its way from one product to the next).  bf16 operands are used as they are; what is made here is rounded to bf16 where it is multiplied
-// once more on its way to a bf16 result (the masked products, W), and kept in two parts, 17 bits, where it is summed into a state (r^(C-1-j) y_j).
+// once more on its way to a bf16 result (the masked products, W), and kept in three parts where it is summed into a state (r^(C-1-j) y_j).
 // fp32 operands are three bf16 parts each, of whose products six are made (split_two).
 #include <algorithm>
 
-#include "rps_rows.cuh"
+#include "rps_mix.cuh"
 #include "rps_tma.cuh"
 
 namespace rps_ops {
@@ -61,11 +61,6 @@ __device__ __forceinline__ void split_pair(float a, float b, uint32_t (&word)[PA
 {
     if constexpr (PARTS == 1) {
         word[0] = two_bf16(a, b);
-    } else if constexpr (PARTS == 2) {
-        // the second part of an infinity or a NaN is itself, after a zero (split_two)
-        const bool finite_a = fabsf(a) <= 3.402823466e38f, finite_b = fabsf(b) <= 3.402823466e38f;
-        word[0] = nearest_two_bf16(finite_a ? a : 0.0f, finite_b ? b : 0.0f);
-        word[1] = two_bf16(a - __uint_as_float(word[0] << 16), b - __uint_as_float(word[0] & 0xFFFF0000u));
     } else {
         split_two(a, b, word);
     }
@@ -198,35 +193,6 @@ __device__ __forceinline__ void multiply_parts(float (&sum)[TILES][4], const Lef
 }
 
 // ------------------------------------------------------------------------------------------------------------ kernel
-// The decay's powers, as double: a log_decay of minus infinity is a decay of zero, whose power 0 is one; a positive one or NaN gives NaN.
-__device__ __forceinline__ double power(float log_decay, int64_t exponent)
-{
-    if (!(log_decay <= 0.0f)) return nan("");
-    return exp((double)fmaxf(log_decay, -1e4f) * (double)exponent);
-}
-
-struct Place {
-    int w, sequence, head;
-    int64_t length;  // tokens of the sequence that take part
-};
-
-__device__ __forceinline__ Place place_of(const MixParams& prm, int64_t unit)
-{
-    Place p;
-    p.head = (int)(unit % prm.heads);
-    const int64_t s = unit / prm.heads;
-    p.w = (int)(s / prm.sequences), p.sequence = (int)(s % prm.sequences);
-    p.length = prm.tokens;
-    if (prm.lengths != nullptr) p.length = max((int64_t)0, min(prm.tokens, __ldg(prm.lengths + s)));
-    return p;
-}
-
-template <typename T>
-__device__ __forceinline__ const T* first_token(const MixOperand& o, const Place& p)
-{
-    return static_cast<const T*>(o.base) + p.w * o.worker + p.sequence * o.sequence + p.head * o.head;
-}
-
 // MT: 64 columns of x and y each; WN: warps that share a chunk's 16 rows.  STATES: no output, only each segment's own sum.
 template <typename T, int MT, int WN>
 struct Shape {
@@ -241,7 +207,7 @@ __global__ void __launch_bounds__(Shape<T, MT, WN>::kThreads) rps_mix_kernel(con
 {
     after_the_kernel_before();
     using S = Shape<T, MT, WN>;
-    constexpr int W = Slice<T>::kWidth, kParts = Tile<T>::kParts, kStateParts = kParts == 1 ? 2 : 3, NT = S::kTiles;
+    constexpr int W = Slice<T>::kWidth, kParts = Tile<T>::kParts, kStateParts = 3, NT = S::kTiles;
     extern __shared__ __align__(128) unsigned char raw[];
     T* const stages = reinterpret_cast<T*>(raw);
     T* const state = stages + 2 * S::kStage;
@@ -477,6 +443,15 @@ __global__ void __launch_bounds__(Shape<T, MT, WN>::kThreads) rps_mix_kernel(con
 // The states that segments begin with, out of the segments' own sums: slot s + 1 holds that of segment s, slot 0 becomes the first state.
 constexpr int kJoinThreads = 256;
 
+// Tokens of segment s; `end_aligned`: it is the first chunk of a sequence that is not full, not the last.
+__device__ __forceinline__ int64_t segment_length(const MixParams& prm, int64_t length, int s, bool end_aligned)
+{
+    const int64_t first = s * prm.segment_tokens;
+    if (!end_aligned) return max((int64_t)0, min(prm.segment_tokens, length - first));
+    const int64_t whole = (length + kMixTensorChunk - 1) / kMixTensorChunk * kMixTensorChunk, missing = whole - length;
+    return max((int64_t)0, min(prm.segment_tokens, whole - first) - (s == 0 ? missing : 0));
+}
+
 __global__ void __launch_bounds__(kJoinThreads) rps_mix_join_kernel(const __grid_constant__ MixParams prm)
 {
     after_the_kernel_before();
@@ -487,7 +462,7 @@ __global__ void __launch_bounds__(kJoinThreads) rps_mix_join_kernel(const __grid
     const Place at = place_of(prm, unit);
     const float log_decay = __ldg(prm.log_decay + at.w * prm.heads + at.head);
     for (int s = threadIdx.x; s + 1 < prm.segments; s += kJoinThreads)
-        decay[s] = (float)power(log_decay, max((int64_t)0, min(prm.segment_tokens, at.length - s * prm.segment_tokens)));
+        decay[s] = (float)power(log_decay, segment_length(prm, at.length, s, prm.tensor && !term.reversed));
     __syncthreads();
     if (e >= term.a * term.b) return;
     float* slot = prm.segment_states + (blockIdx.y * prm.units + unit) * prm.segments * prm.state_room + e;
@@ -587,13 +562,17 @@ cudaError_t launch_kernel(const MixParams& prm, cudaStream_t stream)
                         stream, 1, prm);
 }
 
+cudaError_t launch_join(const MixParams& prm, cudaStream_t stream)
+{
+    return launch_after(rps_mix_join_kernel, dim3((unsigned)(prm.units * prm.join_blocks), (unsigned)prm.terms), kJoinThreads, 0, stream, 1, prm);
+}
+
 template <typename T, int MT, int WN, int ALIGN>
 cudaError_t run(const MixParams& prm, cudaStream_t stream)
 {
     if (prm.segments > 1) {
         cudaError_t err = launch_kernel<T, MT, WN, ALIGN, true>(prm, stream);
-        if (err != cudaSuccess) return err;
-        err = launch_after(rps_mix_join_kernel, dim3((unsigned)(prm.units * prm.join_blocks), (unsigned)prm.terms), kJoinThreads, 0, stream, 1, prm);
+        if (err == cudaSuccess) err = launch_join(prm, stream);
         if (err != cudaSuccess) return err;
     }
     return launch_kernel<T, MT, WN, ALIGN, false>(prm, stream);
@@ -620,25 +599,44 @@ cudaError_t mix(const MixParams& prm, cudaStream_t stream)
 
 }  // namespace
 
+// Sequences are cut into as many segments as take the least time by this count of chunks of 128 tokens: a round of CTAs (one to an SM) takes its
+// segment's chunks and one more to begin and end with; the segments' own sums, made first, 0.6 of a chunk each; joining them 3.
 void plan_mix(MixParams* prm)
 {
     MixParams& p = *prm;
     p.units = (int64_t)p.n * p.sequences * p.heads;
-    p.columns = 1, p.state_room = 0, p.join_blocks = 1;
+    p.columns = 1, p.state_room = 0;
     for (int i = 0; i < p.terms; ++i) {
         p.columns = std::max(p.columns, (int)ceil_div(p.term[i].b, kTile));
         p.state_room = std::max<int64_t>(p.state_room, round_up(p.term[i].a * p.term[i].b, 4));
     }
     p.join_blocks = (int)ceil_div(p.state_room, kJoinThreads);
-    const int64_t chunks = std::max<int64_t>(1, ceil_div(p.tokens, kC)), ctas = std::max<int64_t>(1, p.units * p.columns * p.terms);
-    int64_t segments = 1;
-    if (ctas < 2 * kSms) segments = std::min<int64_t>({ceil_div(3 * kSms, ctas), chunks / 4, kMixSegments});
-    segments = std::max<int64_t>(1, segments);
-    p.segment_tokens = ceil_div(chunks, segments) * kC;
-    p.segments = (int)std::max<int64_t>(1, ceil_div(p.tokens, p.segment_tokens));
+    const int64_t chunks = std::max<int64_t>(1, ceil_div(p.tokens, kMixTensorChunk)), ctas = p.units * p.terms * (p.f32 ? p.columns : 1);
+    int64_t best = 1;
+    double least = 0.0;
+    for (int64_t s = 1; s <= std::min<int64_t>(chunks, kMixSegments); ++s) {
+        const int64_t each = ceil_div(chunks, s);
+        if (s > 1 && (ceil_div(chunks, each) != s || ctas * s > 4 * kSms)) continue;
+        const double cost = (double)ceil_div(ctas * s, kSms) * (double)(each + 1) + (s > 1 ? (double)ceil_div(ctas * (s - 1), kSms) * (0.6 * (double)each + 1.0) + 3.0 : 0.0);
+        if (s == 1 || cost < least) best = s, least = cost;
+    }
+    p.segment_tokens = ceil_div(chunks, best) * kMixTensorChunk;
+    p.segments = (int)best;
 }
 
-cudaError_t launch_mix(const MixParams& prm, cudaStream_t stream) { return prm.f32 ? mix<float, 2>(prm, stream) : mix<bf16, 1>(prm, stream); }
+cudaError_t launch_mix(const MixParams& prm, cudaStream_t stream)
+{
+    if (prm.f32) return mix<float, 2>(prm, stream);
+    if (!mix_fits_tensor(prm)) return mix<bf16, 1>(prm, stream);
+    MixParams p = prm;
+    p.tensor = 1;
+    if (p.segments > 1) {
+        cudaError_t err = launch_mix_tensor(p, true, stream);
+        if (err == cudaSuccess) err = launch_join(p, stream);
+        if (err != cudaSuccess) return err;
+    }
+    return launch_mix_tensor(p, false, stream);
+}
 
 cudaError_t launch_mix_step(const MixParams& prm, cudaStream_t stream)
 {

@@ -1,0 +1,458 @@
+// Linear attention's form (rps_mix.cu) on the fifth-generation tensor cores, for bf16 operands that TMA can copy: 16-byte aligned, columns in eights.
+//
+// A CTA takes a segment of a sequence's head in chunks of 128 tokens, rows l in the order of memory whichever way time runs; with the masked decays D,
+//
+//   P = x y^T,  O = (P o D) z + r^e (x W),  U = (r^f y)^T z,  W' = r^c W + U
+//
+// are four tcgen05 products of 128 rows, whose sums lie in tensor memory side by side.  The chunks end with the sequence's last token, so it
+// is the first one that may begin ahead of the sequence; TMA fills zeros there, and never reads past the last token that takes part.
+//
+// Roles (groups of four warps): warp 0 copies x, y and z of the next chunk while this one is worked on, warp 1 issues the products; four warps (a lane to a row) turn P
+// into the masked product, which goes back to tensor memory as the left operand of the next one, and write O; eight warps make r^f y in parts, in place of
+// y and x when those have been read, and hold W as fp32 in registers (a lane to a row of W, 64 columns), which they bring up to date out of U and
+// lay down as bf16 for the next chunk.  Only the last of these depends on the chunk before.
+//
+// r^f y is three bf16 parts where a state is written (fp32 has 24 bits, and a state sums many terms); where W only goes on into bf16 results, as itself
+// rounded to bf16, it is one.
+#include "rps_mix.cuh"
+#include "rps_tensor.cuh"
+
+namespace rps_ops {
+namespace {
+
+using rps::mbar_arrive_expect_tx;
+using rps::mbar_init;
+using rps::smem_addr;
+
+constexpr int kC = kMixTensorChunk;
+constexpr int kBox = 64, kBoxBytes = kC * kBox * 2;  // columns of a copy: one swizzled line of 128 bytes a row
+constexpr int kOutWarps = 4, kStateWarps = 8, kFirstOut = 4, kFirstState = kFirstOut + kOutWarps;
+constexpr int kThreads = 32 * (kFirstState + kStateWarps);
+// Registers of a thread, shared out anew among the groups of four warps: those that hold W have more than the 128 that all alike could have.
+constexpr int kLaunchRegisters = 128, kIssueRegisters = 80, kOutRegisters = 104, kStateRegisters = 160;
+static_assert(4 * kIssueRegisters + kOutWarps * kOutRegisters + kStateWarps * kStateRegisters <= kThreads / 32 * kLaunchRegisters, "the block's own");
+// columns of tensor memory: P, and P o D as 16-bit pairs in its place; x W; (P o D) z; U
+constexpr int kAtP = 0, kAtState = 128, kAtOut = 256, kAtU = 384;
+
+struct Control {
+    uint64_t full[2], empty[2], scores, masked, of_state, state_read, out_done, out_free, parts, parts_used, last_part, update, state_ready;
+    uint32_t tensor_memory;
+    float powers[kC + 1];  // r^0 .. r^128
+};
+
+struct MixMaps {
+    CUtensorMap of[3][3];  // x, y, z of each term
+};
+
+__device__ int g_gave_up = 0;
+
+__device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, int col, int token, const Place& at, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(dst), "l"(map), "r"(col),
+                 "r"(token), "r"(at.head), "r"(at.sequence), "r"(at.w), "r"(bar)
+                 : "memory");
+}
+
+// The left operand in tensor memory.
+__device__ __forceinline__ void multiply_from_tensor(uint32_t sum, uint32_t a, uint32_t b, uint32_t descriptor, bool add)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 db;\n\tsetp.ne.u32 p, %5, 0;\n\tmov.b64 db, {%2, %3};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %4, p;\n\t}" ::"r"(sum),
+        "r"(a), "r"(b), "n"(kDescriptorHigh), "r"(descriptor), "r"((uint32_t)add)
+        : "memory");
+}
+
+// 16 words of this lane's row.
+__device__ __forceinline__ void store_words(uint32_t addr, const uint32_t (&v)[16])
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(addr), "r"(v[0]), "r"(v[1]),
+        "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
+        : "memory");
+}
+
+__device__ __forceinline__ void tensor_loads_done() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+// What this thread wrote to shared memory is there for the tensor cores and TMA.
+__device__ __forceinline__ void writes_done() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+__device__ __forceinline__ uint4 read_shared(uint32_t addr) { return read_slot(addr); }
+__device__ __forceinline__ void write_shared(uint32_t addr, const uint4& v)
+{
+    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+
+template <bool STATES>
+__global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __grid_constant__ MixParams prm, const __grid_constant__ MixMaps maps)
+{
+    after_the_kernel_before();
+    const MixTerm& term = prm.term[blockIdx.y];
+    const int segment = (int)(blockIdx.x % prm.segments);
+    const int64_t unit = blockIdx.x / prm.segments;
+    if (STATES && segment + 1 == prm.segments) return;
+    extern __shared__ unsigned char raw[];
+    const uint32_t base = (smem_addr(raw) + 1023) / 1024 * 1024;
+    const int a = term.a, b = term.b, a_boxes = (a + kBox - 1) / kBox, b_boxes = (b + kBox - 1) / kBox;
+    const uint32_t y_at = a_boxes * kBoxBytes, z_at = 2 * y_at, stage_bytes = z_at + b_boxes * kBoxBytes;
+    const uint32_t w_at = base + 2 * stage_bytes, w_box = a_boxes * kBox * kBox * 2;
+    Control& control = *reinterpret_cast<Control*>(raw + (w_at + b_boxes * w_box - smem_addr(raw)));
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const Place at = place_of(prm, unit);
+    const bool reversed = term.reversed != 0;
+
+    // the segment's chunks, counted in the order of time
+    const int length = (int)at.length, chunks = (length + kC - 1) / kC, missing = chunks * kC - length;  // of the first chunk's rows
+    const int per_segment = (int)(prm.segment_tokens / kC), begin = segment * per_segment, count = max(0, min(chunks - begin, per_segment));
+    const auto chunk_at = [&](int i) { return reversed ? chunks - 1 - (begin + i) : begin + i; };
+    const bool last = segment + 1 == prm.segments;
+    const int parts = STATES || term.state_out != nullptr ? 3 : 1;
+    // the last chunk's part of W counts only where W is written
+    const bool writes_state = STATES || (last && term.state_out != nullptr);
+    const auto updates = [&](int i) { return i + 1 < count || writes_state; };
+
+    if (warp == 0 && lane == 0) {
+        for (int s = 0; s < 2; ++s) mbar_init(smem_addr(&control.full[s]), 1), mbar_init(smem_addr(&control.empty[s]), 1);
+        mbar_init(smem_addr(&control.scores), 1), mbar_init(smem_addr(&control.of_state), 1), mbar_init(smem_addr(&control.out_done), 1);
+        mbar_init(smem_addr(&control.parts_used), 1), mbar_init(smem_addr(&control.update), 1);
+        mbar_init(smem_addr(&control.masked), kOutWarps), mbar_init(smem_addr(&control.out_free), kOutWarps);
+        mbar_init(smem_addr(&control.parts), kStateWarps), mbar_init(smem_addr(&control.last_part), kStateWarps);
+        mbar_init(smem_addr(&control.state_ready), kStateWarps);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) take_tensor_memory<1>(smem_addr(&control.tensor_memory));
+    const float log_decay = __ldg(prm.log_decay + at.w * prm.heads + at.head);
+    if (threadIdx.x <= kC) control.powers[threadIdx.x] = (float)power(log_decay, threadIdx.x);
+    before_sync();
+    __syncthreads();
+    after_sync();
+    const uint32_t tensor = control.tensor_memory;
+
+    bool fine = true;
+    const uint64_t limit_ns = prm.wait_limit_ms > 0 ? (uint64_t)prm.wait_limit_ms * 1000000u : rps::kDefaultWaitLimitNs;
+    const auto wait = [&](uint64_t& bar, int turn) { return wait_for(smem_addr(&bar), turn & 1, limit_ns); };  // for the turn-th completion
+    const auto warp_wait = [&](uint64_t& bar, int turn) {
+        fine = __all_sync(0xFFFFFFFFu, wait(bar, turn));
+        after_sync();
+        return fine;
+    };
+    const auto warp_arrive = [&](uint64_t& bar) {
+        before_sync();
+        __syncwarp();
+        if (lane == 0) rps::mbar_arrive(smem_addr(&bar));
+    };
+
+    if (warp < kFirstOut) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kIssueRegisters));
+        if (warp == 0 && lane == 0) {
+            const uint32_t bytes = ((STATES ? 1 : 2) * a_boxes + b_boxes) * kBoxBytes;
+            const CUtensorMap* map = maps.of[blockIdx.y];
+            int issued = 0;
+            for (int i = 0; i < count && prm.withhold_copies == 0; ++i) {
+                const int s = i & 1;
+                fine = wait(control.empty[s], (i >> 1) + 1);
+                if (!fine) break;
+                const uint32_t bar = smem_addr(&control.full[s]), to = base + s * stage_bytes;
+                const int token = length - kC * (chunks - chunk_at(i));
+                mbar_arrive_expect_tx(bar, bytes);
+                for (int c = 0; c < a_boxes; ++c) load_box(to + y_at + c * kBoxBytes, map + 1, c * kBox, token, at, bar);
+                if (!STATES)
+                    for (int c = 0; c < a_boxes; ++c) load_box(to + c * kBoxBytes, map, c * kBox, token, at, bar);
+                for (int c = 0; c < b_boxes; ++c) load_box(to + z_at + c * kBoxBytes, map + 2, c * kBox, token, at, bar);
+                ++issued;
+            }
+            for (int i = max(0, issued - 2); i < issued; ++i) fine = wait(control.full[i & 1], i >> 1) && fine;  // all copies have arrived before the CTA may end
+        }
+        if (warp == 1 && lane == 0) {
+            const int b16 = (b + 15) / 16 * 16, a_steps = (a + 15) / 16;
+            const uint32_t of_scores = instruction_descriptor(false, false, kC, kC), of_state = instruction_descriptor(false, true, kC, b16);
+            const uint32_t of_update = instruction_descriptor(true, true, kC, b16);
+            // along the rows of a tile 16 columns further: 32 bytes, after 64 the next box; along its columns 16 rows of 128 bytes
+            const auto along = [](int k) { return (uint32_t)(k / 4 * kBoxBytes + k % 4 * 32) / 16; };
+            const auto scores = [&](int s) {
+                const uint32_t x = descriptor_low(base + s * stage_bytes, false, kBoxBytes), y = descriptor_low(base + s * stage_bytes + y_at, false, kBoxBytes);
+                for (int k = 0; k < a_steps; ++k) multiply<1>(tensor + kAtP, x + along(k), y + along(k), of_scores, k > 0);
+                commit<1>(smem_addr(&control.scores));
+            };
+            const auto update = [&](uint32_t left, uint32_t right, bool add) {
+                for (int k = 0; k < kC / 16; ++k) multiply<1>(tensor + kAtU, left + k * (2048 / 16), right + k * (2048 / 16), of_update, add || k > 0);
+            };
+            for (int i = 0; i < count; ++i) {
+                const int s = i & 1;
+                const uint32_t x_at = base + s * stage_bytes, z = descriptor_low(x_at + z_at, true, kBoxBytes);
+                if (i == 0 || STATES) {
+                    if (!(fine = wait(control.full[s], i >> 1))) break;
+                    after_sync();
+                    if (!STATES) scores(s);
+                }
+                if (!STATES) {
+                    if (!(fine = wait(control.state_ready, i) && wait(control.out_free, i + 1))) break;
+                    after_sync();
+                    const uint32_t x = descriptor_low(x_at, false, kBoxBytes), w = descriptor_low(w_at, true, w_box);
+                    for (int k = 0; k < a_steps; ++k) multiply<1>(tensor + kAtState, x + along(k), w + k * (2048 / 16), of_state, k > 0);
+                    commit<1>(smem_addr(&control.of_state));
+                    if (!(fine = wait(control.masked, i))) break;
+                    after_sync();
+                    for (int k = 0; k < kC / 16; ++k)
+                        multiply_from_tensor(tensor + kAtOut, tensor + kAtP + k / 4 * 64 + k % 4 * 8, z + k * (2048 / 16), of_state, k > 0);
+                    commit<1>(smem_addr(&control.out_done));
+                }
+                if (updates(i)) {
+                    if (!(fine = wait(control.parts, i))) break;
+                    after_sync();
+                    update(descriptor_low(x_at + y_at, true, kBoxBytes), z, false);
+                    if (parts == 3) {
+                        update(descriptor_low(x_at, true, kBoxBytes), z, true);
+                        commit<1>(smem_addr(&control.parts_used));
+                        if (!(fine = wait(control.last_part, i))) break;
+                        after_sync();
+                        update(descriptor_low(x_at + y_at, true, kBoxBytes), z, true);
+                    }
+                    commit<1>(smem_addr(&control.update));
+                }
+                commit<1>(smem_addr(&control.empty[s]));
+                if (!STATES && i + 1 < count) {
+                    // P's place holds the left operand of the product for out
+                    if (!(fine = wait(control.out_done, i) && wait(control.full[s ^ 1], (i + 1) >> 1))) break;
+                    after_sync();
+                    scores(s ^ 1);
+                }
+            }
+        }
+    } else if (warp < kFirstState) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOutRegisters));
+        if constexpr (!STATES) {
+            const int quarter = warp % 4, row = quarter * 32 + lane;
+            const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+            bf16* const out = static_cast<bf16*>(term.out) + ((at.w * prm.sequences + at.sequence) * prm.tokens * prm.heads + at.head) * b;
+            for (int i = 0; i < count; ++i) {
+                const int chunk = chunk_at(i), token = length - kC * (chunks - chunk) + row;
+                if (!warp_wait(control.scores, i)) break;
+#pragma unroll 1
+                for (int c = 0; c < kC; c += 32) {
+                    float p[32];
+                    uint32_t word[16];
+                    __syncwarp();
+                    load_sums(p, tensor + lanes + kAtP + c), load_sums(p + 16, tensor + lanes + kAtP + c + 16);
+                    tensor_loads_done();
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) {
+                        const int apart = reversed ? c + j - row : row - c - j;
+                        p[j] = apart >= 0 ? p[j] * (term.score_scale * control.powers[max(apart, 0)]) : 0.0f;
+                    }
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) word[j] = two_bf16(p[2 * j], p[2 * j + 1]);
+                    // pairs of 64 columns in the first half of their places, which have been read by then
+                    store_words(tensor + lanes + kAtP + c / 64 * 64 + c % 64 / 2, word);
+                }
+                asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+                warp_arrive(control.masked);
+                if (!warp_wait(control.out_done, i)) break;
+                const int first = chunk == 0 ? missing : 0;
+                const float factor = term.state_scale * control.powers[reversed ? kC - 1 - row : max(row + 1 - first, 0)];
+#pragma unroll 1
+                for (int c = 0; c < b; c += 32) {
+                    float v[32], u[32];
+                    __syncwarp();
+                    load_sums(v, tensor + lanes + kAtOut + c), load_sums(v + 16, tensor + lanes + kAtOut + c + 16);
+                    load_sums(u, tensor + lanes + kAtState + c), load_sums(u + 16, tensor + lanes + kAtState + c + 16);
+                    tensor_loads_done();
+                    if (c + 32 >= b) warp_arrive(control.out_free);
+#pragma unroll
+                    for (int j = 0; j < 32; j += 8) {
+                        uint32_t word[4];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) word[k] = two_bf16(fmaf(factor, u[j + 2 * k], v[j + 2 * k]), fmaf(factor, u[j + 2 * k + 1], v[j + 2 * k + 1]));
+                        if (token >= 0 && c + j < b) *reinterpret_cast<uint4*>(out + (int64_t)token * prm.heads * b + c + j) = make_uint4(word[0], word[1], word[2], word[3]);
+                    }
+                }
+            }
+            // rows behind the sequence's last token
+            const int64_t t1 = min(prm.tokens, (segment + 1) * prm.segment_tokens);
+            for (int64_t t = max(at.length, segment * prm.segment_tokens) + warp - kFirstOut; t < t1 && fine; t += kOutWarps)
+                for (int c = lane * 8; c < b; c += 256) *reinterpret_cast<uint4*>(out + t * prm.heads * b + c) = make_uint4(0, 0, 0, 0);
+        }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kStateRegisters));
+        const int quarter = warp % 4, half = (warp - kFirstState) / 4, row = quarter * 32 + lane;
+        const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+        // W: row `row`, columns from col0 on: 64 of them, or 32 where there are no more than 64
+        const int width = b_boxes == 2 ? 64 : 32, col0 = half * width;
+        float w[64];
+        const float* init = nullptr;
+        int64_t init_a = b, init_b = 1;
+        if (!STATES && prm.segments > 1)
+            init = prm.segment_states + ((blockIdx.y * prm.units + unit) * prm.segments + segment) * prm.state_room;
+        else if (!STATES && term.state_in != nullptr)
+            init = term.state_in + unit * a * b, init_a = term.state_a, init_b = term.state_b;
+#pragma unroll
+        for (int j = 0; j < 64; ++j) w[j] = init != nullptr && row < a && j < width && col0 + j < b ? __ldg(init + row * init_a + (col0 + j) * init_b) : 0.0f;
+        const auto publish = [&] {  // W where the products read it
+            if (row < a_boxes * kBox) {
+#pragma unroll
+                for (int j = 0; j < 64; j += 8) {
+                    if (j >= width) break;
+                    const int col = col0 + j;
+                    write_shared(w_at + col / kBox * w_box + row * 128 + ((col % kBox / 8 ^ (row & 7)) << 4),
+                                 make_uint4(two_bf16(w[j], w[j + 1]), two_bf16(w[j + 2], w[j + 3]), two_bf16(w[j + 4], w[j + 5]), two_bf16(w[j + 6], w[j + 7])));
+                }
+            }
+            writes_done();
+            warp_arrive(control.state_ready);
+        };
+        if (!STATES && count > 0) publish();
+        // this thread's columns of a row of y: a box, or half of the only one
+        const int pieces = a_boxes == 2 ? 8 : 4, piece0 = a_boxes == 2 ? 0 : half * 4;
+        const uint32_t row_at = (a_boxes == 2 ? half * kBoxBytes : 0) + row * 128;
+        for (int i = 0; i < count && updates(i); ++i) {
+            const int s = i & 1, first = chunk_at(i) == 0 ? missing : 0;
+            const uint32_t x_row = base + s * stage_bytes + row_at, y_row = x_row + y_at;
+            if (!warp_wait(control.full[s], i >> 1)) break;
+            const float factor = term.update_scale * control.powers[reversed ? max(row + 1 - first, 0) : kC - 1 - row];
+            uint4 third[8];  // y, then its last parts
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+                if (q < pieces) third[q] = read_shared(y_row + (((piece0 + q) ^ (row & 7)) << 4));
+            if (!STATES && !warp_wait(control.scores, i)) break;
+            if (parts == 3) {
+                // the second part takes x's place, which the product with W has read by then
+                if (!STATES && !warp_wait(control.of_state, i)) break;
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    if (q >= pieces) break;
+                    float v[8];
+                    widen(third[q], v);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[j] *= factor;
+                    uint4 part[3];
+                    split_slice(v, part);
+                    const uint32_t to = ((piece0 + q) ^ (row & 7)) << 4;
+                    write_shared(y_row + to, part[0]), write_shared(x_row + to, part[1]);
+                    third[q] = part[2];
+                }
+            } else {
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    if (q >= pieces) break;
+                    float v[8];
+                    widen(third[q], v);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[j] *= factor;
+                    write_shared(y_row + (((piece0 + q) ^ (row & 7)) << 4), narrow(v));
+                }
+            }
+            writes_done();
+            warp_arrive(control.parts);
+            if (parts == 3) {
+                if (!warp_wait(control.parts_used, i)) break;
+#pragma unroll
+                for (int q = 0; q < 8; ++q)
+                    if (q < pieces) write_shared(y_row + (((piece0 + q) ^ (row & 7)) << 4), third[q]);
+                writes_done();
+                warp_arrive(control.last_part);
+            }
+            if (!warp_wait(control.update, i)) break;
+            const float whole = control.powers[kC - first];
+#pragma unroll
+            for (int c = 0; c < 64; c += 32) {
+                if (c >= width) break;
+                float u[32];
+                __syncwarp();
+                load_sums(u, tensor + lanes + kAtU + col0 + c), load_sums(u + 16, tensor + lanes + kAtU + col0 + c + 16);
+                tensor_loads_done();
+#pragma unroll
+                for (int j = 0; j < 32; ++j) w[c + j] = fmaf(whole, w[c + j], u[j]);
+            }
+            before_sync();
+            if (!STATES && i + 1 < count) {
+                if (parts == 1 && !warp_wait(control.of_state, i)) break;  // W's place has been read
+                publish();
+            }
+        }
+        float* to = nullptr;
+        int64_t to_a = b, to_b = 1;
+        if (STATES)
+            to = prm.segment_states + ((blockIdx.y * prm.units + unit) * prm.segments + segment + 1) * prm.state_room;
+        else if (writes_state)
+            to = term.state_out + unit * a * b, to_a = term.state_a, to_b = term.state_b;
+        if (to != nullptr && fine && row < a) {
+#pragma unroll
+            for (int j = 0; j < 64; ++j)
+                if (j < width && col0 + j < b) to[row * to_a + (col0 + j) * to_b] = w[j];
+        }
+    }
+    if (!fine && lane == 0) atomicExch(&g_gave_up, 1);
+    before_sync();
+    __syncthreads();
+    after_sync();
+    __syncwarp();
+    if (warp == 1) free_tensor_memory<1>(tensor);
+}
+
+// -------------------------------------------------------------------------------------------------------------- host
+// Whether TMA can copy an operand as it lies: axes of more than one element need strides that are multiples of 16 bytes (and not zero).
+bool fits(const MixParams& prm, const MixOperand& o, int cols)
+{
+    const auto stride = [](int64_t size, int64_t step) { return size <= 1 || (step > 0 && step % 8 == 0 && step < 1ll << 38); };
+    return cols % 8 == 0 && reinterpret_cast<uintptr_t>(o.base) % 16 == 0 && stride(prm.tokens, o.token) && stride(prm.heads, o.head) && stride(prm.sequences, o.sequence) &&
+           stride(prm.n, o.worker);
+}
+
+bool encode(CUtensorMap* map, const MixParams& prm, const MixOperand& o, int cols)
+{
+    rps::EncodeTiledFn encode = rps::encode_tiled_fn();
+    if (encode == nullptr) return false;
+    const auto bytes = [](int64_t size, int64_t step) { return (cuuint64_t)(size <= 1 ? 16 : step * 2); };  // an axis of one element takes any stride
+    const cuuint64_t dims[5] = {(cuuint64_t)cols, (cuuint64_t)prm.tokens, (cuuint64_t)prm.heads, (cuuint64_t)prm.sequences, (cuuint64_t)prm.n};
+    const cuuint64_t strides[4] = {bytes(prm.tokens, o.token), bytes(prm.heads, o.head), bytes(prm.sequences, o.sequence), bytes(prm.n, o.worker)};
+    const cuuint32_t box[5] = {kBox, kC, 1, 1, 1}, steps[5] = {1, 1, 1, 1, 1};
+    return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void*>(o.base), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Shared memory of a CTA: more than half of an SM's, as the tensor memory that a CTA takes is all there is.
+size_t shared_bytes(int a, int b)
+{
+    const int a_boxes = (int)ceil_div(a, kBox), b_boxes = (int)ceil_div(b, kBox);
+    return std::max<size_t>(120 << 10, 1024 + 2 * (2 * a_boxes + b_boxes) * kBoxBytes + a_boxes * b_boxes * kBox * kBox * 2 + sizeof(Control));
+}
+
+template <bool STATES>
+cudaError_t launch(const MixParams& prm, const MixMaps& maps, cudaStream_t stream)
+{
+    static rps::LaunchState granted;
+    size_t bytes = 0;
+    for (int i = 0; i < prm.terms; ++i) bytes = std::max(bytes, shared_bytes(prm.term[i].a, prm.term[i].b));
+    cudaError_t err = rps::grant_smem(granted, rps_mix_tensor_kernel<STATES>, (uint32_t)bytes);
+    if (err != cudaSuccess) return err;
+    static std::atomic<int> registers{0};
+    if ((err = check_registers(registers, rps_mix_tensor_kernel<STATES>, kLaunchRegisters)) != cudaSuccess) return err;
+    return launch_after(rps_mix_tensor_kernel<STATES>, dim3((unsigned)(prm.units * prm.segments), (unsigned)prm.terms), kThreads, bytes, stream, 1, prm, maps);
+}
+
+}  // namespace
+
+bool mix_fits_tensor(const MixParams& prm)
+{
+    if (prm.tokens < 1 || prm.tokens >= 1ll << 30) return false;
+    for (int i = 0; i < prm.terms; ++i) {
+        const MixTerm& t = prm.term[i];
+        if (!fits(prm, t.x, t.a) || !fits(prm, t.y, t.a) || !fits(prm, t.z, t.b) || reinterpret_cast<uintptr_t>(t.out) % 16 != 0) return false;
+    }
+    return true;
+}
+
+cudaError_t launch_mix_tensor(const MixParams& prm, bool states, cudaStream_t stream)
+{
+    MixMaps maps{};
+    for (int i = 0; i < prm.terms; ++i) {
+        const MixTerm& t = prm.term[i];
+        if (!encode(&maps.of[i][0], prm, t.x, t.a) || !encode(&maps.of[i][1], prm, t.y, t.a) || !encode(&maps.of[i][2], prm, t.z, t.b)) return cudaErrorInvalidValue;
+    }
+    return states ? launch<true>(prm, maps, stream) : launch<false>(prm, maps, stream);
+}
+
+cudaError_t read_mix_gave_up(int* value, cudaStream_t stream) { return read_and_clear(g_gave_up, value, stream); }
+
+}  // namespace rps_ops

@@ -189,10 +189,11 @@ extern "C" const char* rps_ops_last_error(void) { return g_error; }
 extern "C" int rps_ops_check(void* cuda_stream)
 {
     start();
-    int gave_up = 0, norm_gave_up = 0;
+    int gave_up = 0, norm_gave_up = 0, mix_gave_up = 0;
     RPS_TRY(read_gave_up(&gave_up, static_cast<cudaStream_t>(cuda_stream)));
     RPS_TRY(read_norm_gave_up(&norm_gave_up, static_cast<cudaStream_t>(cuda_stream)));
-    return gave_up == 0 && norm_gave_up == 0 ? RPS_OK : fail(RPS_ECUDA, "a wait inside a kernel gave up; the outputs of the calls since the last check are not valid");
+    RPS_TRY(read_mix_gave_up(&mix_gave_up, static_cast<cudaStream_t>(cuda_stream)));
+    return gave_up == 0 && norm_gave_up == 0 && mix_gave_up == 0 ? RPS_OK : fail(RPS_ECUDA, "a wait inside a kernel gave up; the outputs of the calls since the last check are not valid");
 }
 
 extern "C" int rps_lce_workspace(const rps_lce_desc* desc, const void* weight, int backward, size_t* bytes)

@@ -247,7 +247,7 @@ cudaError_t launch_embed_lookup(const EmbedParams& prm, cudaStream_t stream);
 cudaError_t launch_embed_gradient(const EmbedParams& prm, cudaStream_t stream);
 
 // ---------------------------------------------------------------------------------------------------- linear attention
-constexpr int kMixChunk = 64, kMixMaxCols = RPS_MAX_HEAD_COLS, kMixSegments = 64;
+constexpr int kMixChunk = 64, kMixTensorChunk = 128, kMixMaxCols = RPS_MAX_HEAD_COLS, kMixSegments = 64;
 
 // [worker][sequence][token][head][cols]; strides
 struct MixOperand {
@@ -272,13 +272,17 @@ struct MixParams {
     const int64_t* lengths;   // [n][sequences], or NULL
     const float* log_decay;   // [n][heads]
     MixTerm term[3];
+    int wait_limit_ms, withhold_copies;  // 0: the default; see rps_linear_attention_desc
     // plan_mix
-    int64_t units, segment_tokens, state_room;
-    int columns, segments, join_blocks;
+    int64_t units, segment_tokens, state_room;  // segment_tokens: a multiple of kMixTensorChunk
+    int columns, segments, join_blocks, tensor;
     float* segment_states;    // [term][unit][segment][state_room] (segments > 1)
 };
 void plan_mix(MixParams* prm);
 cudaError_t launch_mix(const MixParams& prm, cudaStream_t stream);
+bool mix_fits_tensor(const MixParams& prm);  // whether rps_mix_tensor.cu takes it
+cudaError_t launch_mix_tensor(const MixParams& prm, bool states, cudaStream_t stream);  // states: the segments' own sums
+cudaError_t read_mix_gave_up(int* value, cudaStream_t stream);
 cudaError_t launch_mix_step(const MixParams& prm, cudaStream_t stream);
 
 // ---------------------------------------------------------------------------------------------------- device helpers

@@ -17,12 +17,11 @@
 // fp32 operands are three bf16 parts each (24 significant bits); of the nine products of parts six are made, and the others are below 2^-24 of
 // the result (split_two).  The three parts of a block lie in three stages of the ring, so each is copied once for its three products.
 #include <algorithm>
-#include <atomic>
 #include <mutex>
 #include <type_traits>
 
-#include "rps_cluster.cuh"
 #include "rps_rows.cuh"
+#include "rps_tensor.cuh"
 
 namespace rps_ops {
 namespace {
@@ -138,83 +137,6 @@ __device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, i
             "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
             "l"(map), "r"(x), "r"(y), "r"(plane), "r"(worker), "r"(bar)
             : "memory");
-}
-
-// Descriptor of a shared-memory tile with the 128-byte swizzle: start address and two strides in units of 16 bytes, the constant 1 at
-// bit 46, layout 2 (128-byte swizzle) at bit 61.  Summed axis contiguous: the stride at bit 32 leads from 8 rows to the next 8.
-// Other axis contiguous: it leads from 8 steps of the summed axis to the next 8, and the one at bit 16 from one 64-wide box to the
-// next.  The upper word is the same for all, and in the lower one tiles and their parts lie a constant apart.
-constexpr uint32_t kDescriptorHigh = 1024 / 16 | 1u << 14 | 2u << 29;
-
-__device__ __forceinline__ uint32_t descriptor_low(uint32_t addr, bool other) { return addr >> 4 | (uint32_t)(other ? kBoxBytes / 16 : 1) << 16; }
-
-// fp32 sums of bf16 products, rows x tile_n.
-__device__ __forceinline__ uint32_t instruction_descriptor(bool a_other, bool b_other, int rows, int tile_n)
-{
-    return 1u << 4 | 1u << 7 | 1u << 10 | (a_other ? 1u : 0u) << 15 | (b_other ? 1u : 0u) << 16 | (uint32_t)(tile_n / 8) << 17 | (uint32_t)(rows / 16) << 24;
-}
-
-// `a`, `b`: lower words of the descriptors.
-template <int CTAS>
-__device__ __forceinline__ void multiply(uint32_t sum, uint32_t a, uint32_t b, uint32_t descriptor, bool add)
-{
-    if constexpr (CTAS == 2)
-        asm volatile(
-            "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\tsetp.ne.u32 p, %5, 0;\n\tmov.b64 da, {%1, %3};\n\tmov.b64 db, {%2, %3};\n\t"
-            "tcgen05.mma.cta_group::2.kind::f16 [%0], da, db, %4, p;\n\t}" ::"r"(sum),
-            "r"(a), "r"(b), "n"(kDescriptorHigh), "r"(descriptor), "r"((uint32_t)add)
-            : "memory");
-    else
-        asm volatile(
-            "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\tsetp.ne.u32 p, %5, 0;\n\tmov.b64 da, {%1, %3};\n\tmov.b64 db, {%2, %3};\n\t"
-            "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, p;\n\t}" ::"r"(sum),
-            "r"(a), "r"(b), "n"(kDescriptorHigh), "r"(descriptor), "r"((uint32_t)add)
-            : "memory");
-}
-
-// Arrives on the barrier at this offset (in both CTAs of a pair) once the products issued so far are done.
-template <int CTAS>
-__device__ __forceinline__ void commit(uint32_t bar)
-{
-    if constexpr (CTAS == 2)
-        asm volatile(
-            "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3)
-            : "memory");
-    else
-        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
-}
-
-// All 512 columns of tensor memory, for the whole kernel.
-template <int CTAS>
-__device__ __forceinline__ void take_tensor_memory(uint32_t address_to)
-{
-    if constexpr (CTAS == 2) {
-        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(address_to) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
-    } else {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(address_to) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
-    }
-}
-
-template <int CTAS>
-__device__ __forceinline__ void free_tensor_memory(uint32_t address)
-{
-    if constexpr (CTAS == 2)
-        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(address) : "memory");
-    else
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(address) : "memory");
-}
-
-// 16 columns of this lane's row.
-__device__ __forceinline__ void load_sums(float* v, uint32_t addr)
-{
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-        : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]), "=f"(v[10]),
-          "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
-        : "r"(addr)
-        : "memory");
 }
 
 // COLS columns of this lane's row: taken over, or added to those of the segments before.  (Of a narrower tile the last ones are whatever
@@ -751,7 +673,7 @@ __global__ void __launch_bounds__(Epilogue<PLANES>::kThreads, 1)
                 const uint32_t descriptor = instruction_descriptor(kAOther, kBOther, kRows, tile_n);
                 // one product covers 16 of the summed axis: 32 bytes further along swizzled rows, or 16 rows of 128 bytes further
                 constexpr uint32_t a_step = (kAOther ? 2048 : 32) / 16, b_step = (kBOther ? 2048 : 32) / 16;
-                const uint32_t a_first = descriptor_low(base, kAOther), b_first = descriptor_low(base + a_bytes, kBOther), stage_step = (a_bytes + b_bytes) / 16;
+                const uint32_t a_first = descriptor_low(base, kAOther, kBoxBytes), b_first = descriptor_low(base + a_bytes, kBOther, kBoxBytes), stage_step = (a_bytes + b_bytes) / 16;
                 int stage = 0, made = 0;
                 uint32_t phase = 0;
                 for (int tile = blockIdx.x / CTAS; tile < total && fine; tile += groups) {
@@ -882,21 +804,6 @@ bool encode_operand(CUtensorMap* map, const Operand& o, int planes, int workers,
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Whether the kernel was compiled to the registers that its epilogue shares out anew: it would wait for ever for those that a smaller launch does not have.
-// `known` keeps the number once it has been asked for; a question that fails is asked again.
-template <typename Kernel>
-cudaError_t check_registers(std::atomic<int>& known, Kernel kernel)
-{
-    int registers = known.load(std::memory_order_relaxed);
-    if (registers == 0) {
-        cudaFuncAttributes attributes{};
-        const cudaError_t err = cudaFuncGetAttributes(&attributes, kernel);
-        if (err != cudaSuccess) return err;
-        known.store(registers = attributes.numRegs, std::memory_order_relaxed);
-    }
-    return registers == kLaunchRegisters ? cudaSuccess : cudaErrorInvalidKernelImage;
-}
-
 template <Product WHICH, int PLANES, int CTAS, bool LONG>
 cudaError_t launch(const ProductParams& prm, cudaStream_t stream)
 {
@@ -905,7 +812,7 @@ cudaError_t launch(const ProductParams& prm, cudaStream_t stream)
     if (err != cudaSuccess) return err;
     if constexpr (PLANES == 3) {
         static std::atomic<int> registers{0};
-        if ((err = check_registers(registers, rps_product_kernel<WHICH, PLANES, CTAS, LONG>)) != cudaSuccess) return err;
+        if ((err = check_registers(registers, rps_product_kernel<WHICH, PLANES, CTAS, LONG>, kLaunchRegisters)) != cudaSuccess) return err;
     }
     int sms = 0;
     if ((err = sm_count(&sms)) != cudaSuccess) return err;

@@ -90,6 +90,8 @@ int check_attention(const rps_linear_attention_desc* d)
     if (d == nullptr) return fail(RPS_EINVAL, "desc is NULL");
     if (int rc = check_common(d->dtype, d->n)) return rc;
     if (d->reserved != 0) return fail(RPS_EINVAL, "reserved = %d", d->reserved);
+    if (d->wait_limit_ms < 0 || d->withhold_copies < 0 || d->withhold_copies > 1)
+        return fail(RPS_EINVAL, "wait_limit_ms = %d, withhold_copies = %d", d->wait_limit_ms, d->withhold_copies);
     if (d->heads < 1 || d->heads > 65535) return fail(RPS_EINVAL, "heads = %d", d->heads);
     if (d->sequences < 0 || d->sequences >= 1ll << 28 || d->n * d->sequences * d->heads >= 1ll << 28) return fail(RPS_EINVAL, "sequences = %lld", (long long)d->sequences);
     if (d->tokens < 0 || d->tokens >= 1ll << 31) return fail(RPS_EINVAL, "tokens = %lld", (long long)d->tokens);
@@ -109,7 +111,7 @@ MixParams mix_params(const rps_linear_attention_desc& d, const float* log_decay,
 {
     MixParams p{};
     p.f32 = d.dtype == RPS_F32, p.n = d.n, p.heads = d.heads, p.sequences = d.sequences, p.tokens = d.tokens;
-    p.log_decay = log_decay, p.lengths = lengths;
+    p.log_decay = log_decay, p.lengths = lengths, p.wait_limit_ms = d.wait_limit_ms, p.withhold_copies = d.withhold_copies;
     return p;
 }
 

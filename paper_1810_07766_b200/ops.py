@@ -77,7 +77,7 @@ class rps_axis_strides(ctypes.Structure):
 
 
 class rps_linear_attention_desc(ctypes.Structure):
-    _fields_ = [("dtype", _i32), ("n", _i32), ("heads", _i32), ("reserved", _i32), ("sequences", _i64), ("tokens", _i64), ("key_cols", _i64),
+    _fields_ = [("dtype", _i32), ("n", _i32), ("heads", _i32), ("wait_limit_ms", _i32), ("withhold_copies", _i32), ("reserved", _i32), ("sequences", _i64), ("tokens", _i64), ("key_cols", _i64),
                 ("value_cols", _i64), ("q", rps_axis_strides), ("k", rps_axis_strides), ("v", rps_axis_strides), ("dout", rps_axis_strides),
                 ("scale", _dbl)]
 

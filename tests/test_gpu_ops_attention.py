@@ -3,12 +3,12 @@
 Tolerances, from the number formats.  `size` is a result made of the sizes of all inputs, so the sum of the sizes of its terms.
   bf16 results  masked scores and states are rounded to bf16 where they are multiplied once more: each term once, by 2^-8 at most; one
                 rounding of the result; fp32 sums below that
-  states        terms are kept in 16 bits and more (2^-16); fp32 results: each term in the three parts that stand for fp32 values, which leave
-                out 6 * 2^-24, and a decay rounded to fp32 twice
+  fp32 results  and states: each term in the three parts that stand for fp32 values, which leave out 6 * 2^-24, and a decay rounded to
+                fp32 twice
   fp32 sums     may be cut off instead of rounded, 2^-23 a step: 6 products for every 16 of the summed axes (cols, 64 tokens, cols), one step for each
                 chunk, two for each segment
   fp32's end    a decay's power or a term below 2^-126 may count as zero: at most 2^26 (tokens * cols * sizes) of those to a result
-Whole results are nearer than their elements' bounds say, as the errors are of independent roundings: 5e-3 (bf16), 2e-5 (states of bf16), 5e-6 (fp32)."""
+Whole results are nearer than their elements' bounds say, as the errors are of independent roundings: 5e-3 (bf16), 5e-6 (fp32, states)."""
 import pytest
 import torch
 
@@ -82,11 +82,11 @@ def check(ops, x, scale=0.3, lengths=None):
     for name, t in got.items():
         assert t.shape == want[name].shape and t.dtype == (torch.float32 if "state" in name else dtype) and t.is_contiguous(), name
         half = dtype == torch.bfloat16
-        term = sums + (2.0 ** -16 if half and "state" in name else 2.0 ** -8 if half else 2.0 ** -21)
+        term = sums + (2.0 ** -8 if half and "state" not in name else 2.0 ** -21)
         rounding = torch.finfo(t.dtype).eps / 2
         off = (t - want[name]).abs() - (term * size[name] + rounding * want[name].abs() + 2.0 ** -100)
         assert (off <= 0).all(), (name, float(off.max()))
-        near = (2e-5 if "state" in name else 5e-3) if half else 5e-6
+        near = 5e-3 if half and "state" not in name else 5e-6
         assert (t - want[name]).norm() <= near * want[name].norm(), (name, float((t - want[name]).norm() / want[name].norm()))
     return got
 
@@ -156,8 +156,11 @@ def test_decays_at_the_ends_of_their_range(ops, dtype):
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("K,W,shift", [(64, 64, 0), (32, 48, 8), (64, 64, 2), (33, 31, 1)])
 def test_strides_and_addresses(ops, dtype, K, W, shift):
-    """Parts of one projection's output, axes in another order, addresses of every alignment; results are those of dense copies."""
+    """Parts of one projection's output, axes in another order, addresses of every alignment: all hold to the definition.  fp32 results are those
+    of dense copies; bf16 operands go through one kernel or another by how they lie, which round the same sums in other places (chunks of
+    64 or of 128 tokens), so there the definition's bounds are all that both share."""
     n, B, T, H = 2, 3, 150, 2
+    same = lambda a, b: dtype == "bf16" or all(torch.equal(a[name], b[name]) for name in b)  # noqa: E731
     x = inputs(dtype, n, B, T, H, K, W, seed=4)
     want = run(ops, x, 0.5)
     joint = torch.zeros(n, B, T, H, 2 * K + W + shift, dtype=TYPES[dtype], device="cuda")
@@ -165,13 +168,13 @@ def test_strides_and_addresses(ops, dtype, K, W, shift):
     for name in ("q", "k", "v"):
         y[name].copy_(x[name])
     y["dout"] = x["dout"].permute(3, 1, 0, 2, 4).contiguous().permute(2, 1, 3, 0, 4)
-    got = run(ops, y, 0.5)
-    assert all(torch.equal(got[name], want[name]) for name in want)
+    assert same(check(ops, y, 0.5), want)
     # broadcast inputs
     one = dict(x, k=x["k"][:, :, :, :1].expand(n, B, T, H, K), q=x["q"][:1].expand(n, B, T, H, K))
     dense = {name: None if t is None else t.contiguous() for name, t in one.items()}
-    a, b = run(ops, one, 0.5), run(ops, dense, 0.5)
-    assert all(torch.equal(a[name], b[name]) for name in a)
+    assert same(check(ops, one, 0.5), run(ops, dense, 0.5))
+    spread = dict(x, v=x["v"][:, :, :1].expand(n, B, T, H, W), dout=x["dout"][:, :1].expand(n, B, T, H, W))
+    check(ops, spread, 0.5)
     # a worker by itself
     single = {name: t[1] for name, t in x.items()}
     got = run(ops, single, 0.5)
@@ -216,7 +219,7 @@ def test_steps_and_parts_go_on_where_a_sequence_ends(ops, dtype):
     out = torch.cat(parts, 2)
     near = 5e-3 if dtype == "bf16" else 5e-6
     assert (out - want["out"]).norm() <= near * want["out"].norm()
-    assert (state - want["state"]).norm() <= 2e-5 * want["state"].norm()
+    assert (state - want["state"]).norm() <= 5e-6 * want["state"].norm()
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
@@ -309,7 +312,7 @@ def test_offsets_past_32_bits(ops):
     want = t.square().sum(-1, keepdim=True) * t
     assert not out[:, :-3].any() and (out[:, -3:] - want).norm() <= 5e-3 * want.norm()
     last = t[:, -1, :, :, None] * t[:, -1, :, None, :]
-    assert (state - last).norm() <= 2e-5 * last.norm()
+    assert (state - last).norm() <= 5e-6 * last.norm()
     del out
     dq, dk, dv, first = ops.linear_attention_backward(x, None, x, x, x, never, scale=1.0)
     for grad in (dq, dk, dv):
@@ -340,3 +343,38 @@ def test_arguments_are_refused(ops):
     room = torch.zeros(s.numel() + 4, device="cuda")
     with pytest.raises(ValueError, match="overlaps"):
         t(q1, k1, v1, ld.detach(), room[:-4].view_as(s), new_state=room[4:].view_as(s))
+
+
+@pytest.mark.parametrize("backward", [False, True])
+@pytest.mark.parametrize("T,K,W", [(100, 64, 64), (3000, 128, 128), (5000, 40, 72)])
+def test_a_wait_that_runs_out_is_reported(ops, backward, T, K, W):
+    """No copies are issued, so the kernel's waits for data give up after 200 ms; it ends by itself and the next check says so.  After that
+    the same call works."""
+    import ctypes
+
+    lib = ops._library()
+    x = inputs("bf16", 1, 2, T, 3, K, W, seed=13)
+    want = run(ops, x, 0.5)
+    ops.check()
+    d = ops.rps_linear_attention_desc(dtype=1, n=1, heads=3, wait_limit_ms=200, withhold_copies=1, sequences=2, tokens=T, key_cols=K, value_cols=W, scale=0.5)
+    d.q = d.k = ops.rps_axis_strides(0, T * 3 * K, 3 * K, K)
+    d.v = d.dout = ops.rps_axis_strides(0, T * 3 * W, 3 * W, W)
+    size = ctypes.c_size_t()
+    assert lib.rps_linear_attention_workspace(ctypes.byref(d), int(backward), ctypes.byref(size)) == 0
+    ws = torch.zeros(size.value + 256, dtype=torch.uint8, device="cuda")
+    p = {name: t.data_ptr() for name, t in x.items()}
+    out = [torch.empty_like(t) for t in want.values()]
+    o = dict(zip(want, (t.data_ptr() for t in out)))
+    stream = torch.cuda.current_stream().cuda_stream
+    if backward:
+        assert lib.rps_linear_attention_backward(ctypes.byref(d), p["dout"], p["dstate"], p["q"], p["k"], p["v"], p["log_decay"], None, p["state"], o["dq"], o["dk"],
+                                                 o["dv"], o["dstate"], ws.data_ptr(), size.value, stream) == 0
+    else:
+        assert lib.rps_linear_attention_forward(ctypes.byref(d), p["q"], p["k"], p["v"], p["log_decay"], None, p["state"], o["out"], o["state"], ws.data_ptr(),
+                                                size.value, stream) == 0
+    with pytest.raises(ops.RPSError, match="gave up"):
+        ops.check()
+    ops.check()      # reported once
+    got = run(ops, x, 0.5)
+    ops.check()
+    assert all(torch.equal(got[name], want[name]) for name in want)
