@@ -7,13 +7,14 @@
 // are four tcgen05 products of 128 rows, whose sums lie in tensor memory side by side.  The chunks end with the sequence's last token, so it
 // is the first one that may begin ahead of the sequence; TMA fills zeros there, and never reads past the last token that takes part.
 //
-// Roles (groups of four warps): warp 0 copies x, y and z of the next chunk while this one is worked on, warp 1 issues the products; four warps (a lane to a row) turn P
-// into the masked product, which goes back to tensor memory as the left operand of the next one, and write O; eight warps make r^f y in parts, in place of
-// y and x when those have been read, and hold W as fp32 in registers (a lane to a row of W, 64 columns), which they bring up to date out of U and
-// lay down as bf16 for the next chunk.  Only the last of these depends on the chunk before.
+// Roles (groups of four warps): warp 0 copies y and z of the next chunk (and x, once x W has been made) while this one is worked on, warp 1 issues the
+// products; four warps (a lane to a row) turn P into the masked product, which goes back to tensor memory as the left operand of the next one, and
+// write O; eight warps make r^f y in parts, the first in place of y, the others one after the other in a place of their own, and hold W as fp32 in
+// registers (a lane to a row of W, 64 columns), which they bring up to date out of U and lay down as bf16 for the next chunk.  Only the last of
+// these depends on the chunk before.
 //
-// r^f y is three bf16 parts where a state is written (fp32 has 24 bits, and a state sums many terms); where W only goes on into bf16 results, as itself
-// rounded to bf16, it is one.
+// r^f y is three bf16 parts where a state is written (fp32 has 24 bits, and a state sums many terms); where W only goes on into bf16 results, two.
+// (One, whose rounding is then as large as those of P o D and W, took dq and dk of heads of 128 from 2.3e-3 to 2.7e-3 of their norm off.)
 #include "rps_mix.cuh"
 #include "rps_tensor.cuh"
 
@@ -35,9 +36,10 @@ static_assert(4 * kIssueRegisters + kOutWarps * kOutRegisters + kStateWarps * kS
 constexpr int kAtP = 0, kAtState = 128, kAtOut = 256, kAtU = 384;
 
 struct Control {
-    uint64_t full[2], empty[2], scores, masked, of_state, state_read, out_done, out_free, parts, parts_used, last_part, update, state_ready;
+    uint64_t full[2], empty[2], x_full, scores, masked, of_state, out_done, out_free, parts, parts_used, last_part, update, state_ready;
     uint32_t tensor_memory;
     float powers[kC + 1];  // r^0 .. r^128
+    float near[64];        // score_scale r^(e - 32), zero where the exponent is negative
 };
 
 struct MixMaps {
@@ -95,8 +97,9 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
     extern __shared__ unsigned char raw[];
     const uint32_t base = (smem_addr(raw) + 1023) / 1024 * 1024;
     const int a = term.a, b = term.b, a_boxes = (a + kBox - 1) / kBox, b_boxes = (b + kBox - 1) / kBox;
-    const uint32_t y_at = a_boxes * kBoxBytes, z_at = 2 * y_at, stage_bytes = z_at + b_boxes * kBoxBytes;
-    const uint32_t w_at = base + 2 * stage_bytes, w_box = a_boxes * kBox * kBox * 2;
+    const uint32_t y_bytes = a_boxes * kBoxBytes, z_bytes = b_boxes * kBoxBytes;
+    const uint32_t x_at = base, y_at = x_at + y_bytes, z_at = y_at + 2 * y_bytes, part_at = z_at + 2 * z_bytes;  // two places for y and z
+    const uint32_t w_at = part_at + y_bytes, w_box = a_boxes * kBox * kBox * 2;
     Control& control = *reinterpret_cast<Control*>(raw + (w_at + b_boxes * w_box - smem_addr(raw)));
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const Place at = place_of(prm, unit);
@@ -107,14 +110,14 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
     const int per_segment = (int)(prm.segment_tokens / kC), begin = segment * per_segment, count = max(0, min(chunks - begin, per_segment));
     const auto chunk_at = [&](int i) { return reversed ? chunks - 1 - (begin + i) : begin + i; };
     const bool last = segment + 1 == prm.segments;
-    const int parts = STATES || term.state_out != nullptr ? 3 : 1;
+    const bool third_part = STATES || term.state_out != nullptr;
     // the last chunk's part of W counts only where W is written
     const bool writes_state = STATES || (last && term.state_out != nullptr);
     const auto updates = [&](int i) { return i + 1 < count || writes_state; };
 
     if (warp == 0 && lane == 0) {
         for (int s = 0; s < 2; ++s) mbar_init(smem_addr(&control.full[s]), 1), mbar_init(smem_addr(&control.empty[s]), 1);
-        mbar_init(smem_addr(&control.scores), 1), mbar_init(smem_addr(&control.of_state), 1), mbar_init(smem_addr(&control.out_done), 1);
+        mbar_init(smem_addr(&control.x_full), 1), mbar_init(smem_addr(&control.scores), 1), mbar_init(smem_addr(&control.of_state), 1), mbar_init(smem_addr(&control.out_done), 1);
         mbar_init(smem_addr(&control.parts_used), 1), mbar_init(smem_addr(&control.update), 1);
         mbar_init(smem_addr(&control.masked), kOutWarps), mbar_init(smem_addr(&control.out_free), kOutWarps);
         mbar_init(smem_addr(&control.parts), kStateWarps), mbar_init(smem_addr(&control.last_part), kStateWarps);
@@ -124,6 +127,7 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
     if (warp == 1) take_tensor_memory<1>(smem_addr(&control.tensor_memory));
     const float log_decay = __ldg(prm.log_decay + at.w * prm.heads + at.head);
     if (threadIdx.x <= kC) control.powers[threadIdx.x] = (float)power(log_decay, threadIdx.x);
+    else if (threadIdx.x >= 256 && threadIdx.x < 320) control.near[threadIdx.x - 256] = threadIdx.x < 288 ? 0.0f : term.score_scale * (float)power(log_decay, threadIdx.x - 288);
     before_sync();
     __syncthreads();
     after_sync();
@@ -146,23 +150,26 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
     if (warp < kFirstOut) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kIssueRegisters));
         if (warp == 0 && lane == 0) {
-            const uint32_t bytes = ((STATES ? 1 : 2) * a_boxes + b_boxes) * kBoxBytes;
             const CUtensorMap* map = maps.of[blockIdx.y];
             int issued = 0;
             for (int i = 0; i < count && prm.withhold_copies == 0; ++i) {
-                const int s = i & 1;
-                fine = wait(control.empty[s], (i >> 1) + 1);
-                if (!fine) break;
-                const uint32_t bar = smem_addr(&control.full[s]), to = base + s * stage_bytes;
-                const int token = length - kC * (chunks - chunk_at(i));
-                mbar_arrive_expect_tx(bar, bytes);
-                for (int c = 0; c < a_boxes; ++c) load_box(to + y_at + c * kBoxBytes, map + 1, c * kBox, token, at, bar);
-                if (!STATES)
-                    for (int c = 0; c < a_boxes; ++c) load_box(to + c * kBoxBytes, map, c * kBox, token, at, bar);
-                for (int c = 0; c < b_boxes; ++c) load_box(to + z_at + c * kBoxBytes, map + 2, c * kBox, token, at, bar);
+                const int s = i & 1, token = length - kC * (chunks - chunk_at(i));
+                if (!(fine = wait(control.empty[s], (i >> 1) + 1))) break;
+                uint32_t bar = smem_addr(&control.full[s]);
+                mbar_arrive_expect_tx(bar, y_bytes + z_bytes);
+                for (int c = 0; c < a_boxes; ++c) load_box(y_at + s * y_bytes + c * kBoxBytes, map + 1, c * kBox, token, at, bar);
+                for (int c = 0; c < b_boxes; ++c) load_box(z_at + s * z_bytes + c * kBoxBytes, map + 2, c * kBox, token, at, bar);
                 ++issued;
+                if (!STATES) {
+                    if (i > 0 && !(fine = wait(control.of_state, i - 1))) break;  // the chunk before has read x
+                    bar = smem_addr(&control.x_full);
+                    mbar_arrive_expect_tx(bar, y_bytes);
+                    for (int c = 0; c < a_boxes; ++c) load_box(x_at + c * kBoxBytes, map, c * kBox, token, at, bar);
+                }
             }
-            for (int i = max(0, issued - 2); i < issued; ++i) fine = wait(control.full[i & 1], i >> 1) && fine;  // all copies have arrived before the CTA may end
+            // all copies have arrived before the CTA may end
+            for (int i = max(0, issued - 2); i < issued; ++i) fine = wait(control.full[i & 1], i >> 1) && fine;
+            if (!STATES && issued > 0) fine = wait(control.x_full, issued - 1) && fine;
         }
         if (warp == 1 && lane == 0) {
             const int b16 = (b + 15) / 16 * 16, a_steps = (a + 15) / 16;
@@ -170,54 +177,47 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
             const uint32_t of_update = instruction_descriptor(true, true, kC, b16);
             // along the rows of a tile 16 columns further: 32 bytes, after 64 the next box; along its columns 16 rows of 128 bytes
             const auto along = [](int k) { return (uint32_t)(k / 4 * kBoxBytes + k % 4 * 32) / 16; };
-            const auto scores = [&](int s) {
-                const uint32_t x = descriptor_low(base + s * stage_bytes, false, kBoxBytes), y = descriptor_low(base + s * stage_bytes + y_at, false, kBoxBytes);
-                for (int k = 0; k < a_steps; ++k) multiply<1>(tensor + kAtP, x + along(k), y + along(k), of_scores, k > 0);
-                commit<1>(smem_addr(&control.scores));
-            };
+            const uint32_t x = descriptor_low(x_at, false, kBoxBytes), w = descriptor_low(w_at, true, w_box), rest = descriptor_low(part_at, true, kBoxBytes);
             const auto update = [&](uint32_t left, uint32_t right, bool add) {
                 for (int k = 0; k < kC / 16; ++k) multiply<1>(tensor + kAtU, left + k * (2048 / 16), right + k * (2048 / 16), of_update, add || k > 0);
             };
             for (int i = 0; i < count; ++i) {
                 const int s = i & 1;
-                const uint32_t x_at = base + s * stage_bytes, z = descriptor_low(x_at + z_at, true, kBoxBytes);
-                if (i == 0 || STATES) {
-                    if (!(fine = wait(control.full[s], i >> 1))) break;
-                    after_sync();
-                    if (!STATES) scores(s);
-                }
+                const uint32_t y = y_at + s * y_bytes, z = descriptor_low(z_at + s * z_bytes, true, kBoxBytes);
+                if (!(fine = wait(control.full[s], i >> 1))) break;
                 if (!STATES) {
+                    // P's place holds the left operand of the product for out of the chunk before
+                    if (!(fine = wait(control.x_full, i) && (i == 0 || wait(control.out_done, i - 1)))) break;
+                    after_sync();
+                    const uint32_t right = descriptor_low(y, false, kBoxBytes);
+                    for (int k = 0; k < a_steps; ++k) multiply<1>(tensor + kAtP, x + along(k), right + along(k), of_scores, k > 0);
+                    commit<1>(smem_addr(&control.scores));
                     if (!(fine = wait(control.state_ready, i) && wait(control.out_free, i + 1))) break;
                     after_sync();
-                    const uint32_t x = descriptor_low(x_at, false, kBoxBytes), w = descriptor_low(w_at, true, w_box);
                     for (int k = 0; k < a_steps; ++k) multiply<1>(tensor + kAtState, x + along(k), w + k * (2048 / 16), of_state, k > 0);
                     commit<1>(smem_addr(&control.of_state));
+                }
+                if (updates(i)) {
+                    if (!(fine = wait(control.parts, i))) break;
+                    after_sync();
+                    update(descriptor_low(y, true, kBoxBytes), z, false);
+                    update(rest, z, true);
+                    commit<1>(smem_addr(third_part ? &control.parts_used : &control.update));
+                }
+                if (!STATES) {
                     if (!(fine = wait(control.masked, i))) break;
                     after_sync();
                     for (int k = 0; k < kC / 16; ++k)
                         multiply_from_tensor(tensor + kAtOut, tensor + kAtP + k / 4 * 64 + k % 4 * 8, z + k * (2048 / 16), of_state, k > 0);
                     commit<1>(smem_addr(&control.out_done));
                 }
-                if (updates(i)) {
-                    if (!(fine = wait(control.parts, i))) break;
+                if (updates(i) && third_part) {
+                    if (!(fine = wait(control.last_part, i))) break;
                     after_sync();
-                    update(descriptor_low(x_at + y_at, true, kBoxBytes), z, false);
-                    if (parts == 3) {
-                        update(descriptor_low(x_at, true, kBoxBytes), z, true);
-                        commit<1>(smem_addr(&control.parts_used));
-                        if (!(fine = wait(control.last_part, i))) break;
-                        after_sync();
-                        update(descriptor_low(x_at + y_at, true, kBoxBytes), z, true);
-                    }
+                    update(rest, z, true);
                     commit<1>(smem_addr(&control.update));
                 }
                 commit<1>(smem_addr(&control.empty[s]));
-                if (!STATES && i + 1 < count) {
-                    // P's place holds the left operand of the product for out
-                    if (!(fine = wait(control.out_done, i) && wait(control.full[s ^ 1], (i + 1) >> 1))) break;
-                    after_sync();
-                    scores(s ^ 1);
-                }
             }
         }
     } else if (warp < kFirstState) {
@@ -226,23 +226,42 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
             const int quarter = warp % 4, row = quarter * 32 + lane;
             const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
             bf16* const out = static_cast<bf16*>(term.out) + ((at.w * prm.sequences + at.sequence) * prm.tokens * prm.heads + at.head) * b;
+            // Of 32 columns that lie wholly on the near side of these rows, a decay is one of the row's distance to them times one of the column's.
+            Pair within[16];
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+                within[j] = reversed ? Pair(control.powers[2 * j], control.powers[2 * j + 1]) : Pair(control.powers[31 - 2 * j], control.powers[30 - 2 * j]);
             for (int i = 0; i < count; ++i) {
                 const int chunk = chunk_at(i), token = length - kC * (chunks - chunk) + row;
                 if (!warp_wait(control.scores, i)) break;
 #pragma unroll 1
                 for (int c = 0; c < kC; c += 32) {
-                    float p[32];
                     uint32_t word[16];
-                    __syncwarp();
-                    load_sums(p, tensor + lanes + kAtP + c), load_sums(p + 16, tensor + lanes + kAtP + c + 16);
-                    tensor_loads_done();
+                    const int apart = reversed ? c - quarter * 32 : quarter * 32 - c;  // of the rows' 32 and the columns'
+                    if (apart < 0) {
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) {
-                        const int apart = reversed ? c + j - row : row - c - j;
-                        p[j] = apart >= 0 ? p[j] * (term.score_scale * control.powers[max(apart, 0)]) : 0.0f;
+                        for (int j = 0; j < 16; ++j) word[j] = 0;
+                    } else {
+                        float p[32];
+                        __syncwarp();
+                        load_sums(p, tensor + lanes + kAtP + c), load_sums(p + 16, tensor + lanes + kAtP + c + 16);
+                        tensor_loads_done();
+                        if (apart == 0) {
+                            const float* near = control.near + 32 + (reversed ? -lane : lane);
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) p[j] *= reversed ? near[j] : near[-j];
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) word[j] = two_bf16(p[2 * j], p[2 * j + 1]);
+                        } else {
+                            const Pair far(term.score_scale * control.powers[reversed ? c - row : row - c - 31]);
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) {
+                                float lo, hi;
+                                (Pair(p[2 * j], p[2 * j + 1]) * far * within[j]).get(lo, hi);
+                                word[j] = two_bf16(lo, hi);
+                            }
+                        }
                     }
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) word[j] = two_bf16(p[2 * j], p[2 * j + 1]);
                     // pairs of 64 columns in the first half of their places, which have been read by then
                     store_words(tensor + lanes + kAtP + c / 64 * 64 + c % 64 / 2, word);
                 }
@@ -307,48 +326,43 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
         const uint32_t row_at = (a_boxes == 2 ? half * kBoxBytes : 0) + row * 128;
         for (int i = 0; i < count && updates(i); ++i) {
             const int s = i & 1, first = chunk_at(i) == 0 ? missing : 0;
-            const uint32_t x_row = base + s * stage_bytes + row_at, y_row = x_row + y_at;
-            if (!warp_wait(control.full[s], i >> 1)) break;
-            const float factor = term.update_scale * control.powers[reversed ? max(row + 1 - first, 0) : kC - 1 - row];
-            uint4 third[8];  // y, then its last parts
+            const uint32_t y_row = y_at + s * y_bytes + row_at, part_row = part_at + row_at;
+            // y has been read by the product for P; the other place was left by the chunk before (`update`)
+            if (!warp_wait(control.full[s], i >> 1) || (!STATES && !warp_wait(control.scores, i))) break;
+            const Pair factor(term.update_scale * control.powers[reversed ? max(row + 1 - first, 0) : kC - 1 - row]);
+            uint4 third[8];
 #pragma unroll
-            for (int q = 0; q < 8; ++q)
-                if (q < pieces) third[q] = read_shared(y_row + (((piece0 + q) ^ (row & 7)) << 4));
-            if (!STATES && !warp_wait(control.scores, i)) break;
-            if (parts == 3) {
-                // the second part takes x's place, which the product with W has read by then
-                if (!STATES && !warp_wait(control.of_state, i)) break;
+            for (int q = 0; q < 8; ++q) {
+                if (q >= pieces) break;
+                const uint32_t to = ((piece0 + q) ^ (row & 7)) << 4;
+                Pair v[4];
+                widen(read_shared(y_row + to), v);
+                uint32_t part[3][4];
 #pragma unroll
-                for (int q = 0; q < 8; ++q) {
-                    if (q >= pieces) break;
-                    float v[8];
-                    widen(third[q], v);
+                for (int j = 0; j < 4; ++j) {
+                    // as split_two, but that an infinity's first parts are the largest number
+                    Pair rest = v[j] * factor;
+                    float lo, hi;
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) v[j] *= factor;
-                    uint4 part[3];
-                    split_slice(v, part);
-                    const uint32_t to = ((piece0 + q) ^ (row & 7)) << 4;
-                    write_shared(y_row + to, part[0]), write_shared(x_row + to, part[1]);
-                    third[q] = part[2];
+                    for (int k = 0; k < 2; ++k) {
+                        rest.get(lo, hi);
+                        part[k][j] = nearest_two_bf16(lo, hi);
+                        rest = rest + Pair(__uint_as_float(part[k][j] << 16 ^ 0x80000000u), __uint_as_float((part[k][j] & 0xFFFF0000u) ^ 0x80000000u));
+                    }
+                    rest.get(lo, hi);
+                    part[2][j] = two_bf16(lo, hi);
                 }
-            } else {
-#pragma unroll
-                for (int q = 0; q < 8; ++q) {
-                    if (q >= pieces) break;
-                    float v[8];
-                    widen(third[q], v);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) v[j] *= factor;
-                    write_shared(y_row + (((piece0 + q) ^ (row & 7)) << 4), narrow(v));
-                }
+                write_shared(y_row + to, make_uint4(part[0][0], part[0][1], part[0][2], part[0][3]));
+                write_shared(part_row + to, make_uint4(part[1][0], part[1][1], part[1][2], part[1][3]));
+                third[q] = make_uint4(part[2][0], part[2][1], part[2][2], part[2][3]);
             }
             writes_done();
             warp_arrive(control.parts);
-            if (parts == 3) {
+            if (third_part) {
                 if (!warp_wait(control.parts_used, i)) break;
 #pragma unroll
                 for (int q = 0; q < 8; ++q)
-                    if (q < pieces) write_shared(y_row + (((piece0 + q) ^ (row & 7)) << 4), third[q]);
+                    if (q < pieces) write_shared(part_row + (((piece0 + q) ^ (row & 7)) << 4), third[q]);
                 writes_done();
                 warp_arrive(control.last_part);
             }
@@ -366,7 +380,7 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
             }
             before_sync();
             if (!STATES && i + 1 < count) {
-                if (parts == 1 && !warp_wait(control.of_state, i)) break;  // W's place has been read
+                if (!warp_wait(control.of_state, i)) break;  // W's place has been read
                 publish();
             }
         }
@@ -415,7 +429,7 @@ bool encode(CUtensorMap* map, const MixParams& prm, const MixOperand& o, int col
 size_t shared_bytes(int a, int b)
 {
     const int a_boxes = (int)ceil_div(a, kBox), b_boxes = (int)ceil_div(b, kBox);
-    return std::max<size_t>(120 << 10, 1024 + 2 * (2 * a_boxes + b_boxes) * kBoxBytes + a_boxes * b_boxes * kBox * kBox * 2 + sizeof(Control));
+    return std::max<size_t>(120 << 10, 1024 + (4 * a_boxes + 2 * b_boxes) * kBoxBytes + a_boxes * b_boxes * kBox * kBox * 2 + sizeof(Control));
 }
 
 template <bool STATES>
