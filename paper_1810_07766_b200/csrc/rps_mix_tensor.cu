@@ -8,8 +8,8 @@
 // is the first one that may begin ahead of the sequence; TMA fills zeros there, and never reads past the last token that takes part.
 //
 // Roles (groups of four warps): warp 0 copies y and z of the next chunk (and x, once x W has been made) while this one is worked on, warp 1 issues the
-// products; four warps (a lane to a row) turn P into the masked product, which goes back to tensor memory as the left operand of the next one, and
-// write O; eight warps make r^f y in parts, the first in place of y, the others one after the other in a place of their own, and hold W as fp32 in
+// products, warp 2 sends out away; eight (a lane to a row, half of the columns) turn P into the masked product, which goes back to tensor memory as
+// the left operand of the next one, and lay O down in shared memory; eight warps make r^f y in parts, the first in place of y, the others one after the other in a place of their own, and hold W as fp32 in
 // registers (a lane to a row of W, 64 columns), which they bring up to date out of U and lay down as bf16 for the next chunk.  Only the last of
 // these depends on the chunk before.
 //
@@ -27,23 +27,24 @@ using rps::smem_addr;
 
 constexpr int kC = kMixTensorChunk;
 constexpr int kBox = 64, kBoxBytes = kC * kBox * 2;  // columns of a copy: one swizzled line of 128 bytes a row
-constexpr int kOutWarps = 4, kStateWarps = 8, kFirstOut = 4, kFirstState = kFirstOut + kOutWarps;
+constexpr int kOutWarps = 8, kStateWarps = 8, kFirstOut = 4, kFirstState = kFirstOut + kOutWarps;
 constexpr int kThreads = 32 * (kFirstState + kStateWarps);
-// Registers of a thread, shared out anew among the groups of four warps: those that hold W have more than the 128 that all alike could have.
-constexpr int kLaunchRegisters = 128, kIssueRegisters = 80, kOutRegisters = 104, kStateRegisters = 160;
+// Registers of a thread, shared out anew among the groups of four warps: those that hold W have more than the 96 that all alike could have.
+constexpr int kLaunchRegisters = 96, kIssueRegisters = 64, kOutRegisters = 72, kStateRegisters = 136;
 static_assert(4 * kIssueRegisters + kOutWarps * kOutRegisters + kStateWarps * kStateRegisters <= kThreads / 32 * kLaunchRegisters, "the block's own");
 // columns of tensor memory: P, and P o D as 16-bit pairs in its place; x W; (P o D) z; U
 constexpr int kAtP = 0, kAtState = 128, kAtOut = 256, kAtU = 384;
 
 struct Control {
-    uint64_t full[2], empty[2], x_full, scores, masked, of_state, out_done, out_free, parts, parts_used, last_part, update, state_ready;
+    uint64_t full[2], empty[2], x_full, scores, masked, of_state, out_done, out_free, parts, parts_used, last_part, update, state_ready, staged, left;
     uint32_t tensor_memory;
     float powers[kC + 1];  // r^0 .. r^128
     float near[64];        // score_scale r^(e - 32), zero where the exponent is negative
+    alignas(16) float within[32];  // a decay's share of each of 32 columns
 };
 
 struct MixMaps {
-    CUtensorMap of[3][3];  // x, y, z of each term
+    CUtensorMap of[3][4];  // x, y, z and out of each term
 };
 
 __device__ int g_gave_up = 0;
@@ -52,6 +53,13 @@ __device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, i
 {
     asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(dst), "l"(map), "r"(col),
                  "r"(token), "r"(at.head), "r"(at.sequence), "r"(at.w), "r"(bar)
+                 : "memory");
+}
+
+__device__ __forceinline__ void store_box(uint32_t src, const CUtensorMap* map, int col, int token, const Place& at)
+{
+    asm volatile("cp.async.bulk.tensor.5d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3, %4, %5}], [%6];" ::"l"(map), "r"(col), "r"(token), "r"(at.head),
+                 "r"(at.sequence), "r"(at.w), "r"(src)
                  : "memory");
 }
 
@@ -100,7 +108,10 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
     const uint32_t y_bytes = a_boxes * kBoxBytes, z_bytes = b_boxes * kBoxBytes;
     const uint32_t x_at = base, y_at = x_at + y_bytes, z_at = y_at + 2 * y_bytes, part_at = z_at + 2 * z_bytes;  // two places for y and z
     const uint32_t w_at = part_at + y_bytes, w_box = a_boxes * kBox * kBox * 2;
-    Control& control = *reinterpret_cast<Control*>(raw + (w_at + b_boxes * w_box - smem_addr(raw)));
+    // out on its way to memory: where there is no room for a place of its own, in y's, whose first part has been multiplied by then
+    const bool out_in_y = a_boxes == 2 && b_boxes == 2;
+    const uint32_t own_out_at = w_at + b_boxes * w_box;
+    Control& control = *reinterpret_cast<Control*>(raw + (own_out_at + (out_in_y ? 0 : z_bytes) - smem_addr(raw)));
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const Place at = place_of(prm, unit);
     const bool reversed = term.reversed != 0;
@@ -116,17 +127,19 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
     const auto updates = [&](int i) { return i + 1 < count || writes_state; };
 
     if (warp == 0 && lane == 0) {
-        for (int s = 0; s < 2; ++s) mbar_init(smem_addr(&control.full[s]), 1), mbar_init(smem_addr(&control.empty[s]), 1);
+        for (int s = 0; s < 2; ++s) mbar_init(smem_addr(&control.full[s]), 1), mbar_init(smem_addr(&control.empty[s]), out_in_y && !STATES ? 2 : 1);
         mbar_init(smem_addr(&control.x_full), 1), mbar_init(smem_addr(&control.scores), 1), mbar_init(smem_addr(&control.of_state), 1), mbar_init(smem_addr(&control.out_done), 1);
         mbar_init(smem_addr(&control.parts_used), 1), mbar_init(smem_addr(&control.update), 1);
         mbar_init(smem_addr(&control.masked), kOutWarps), mbar_init(smem_addr(&control.out_free), kOutWarps);
         mbar_init(smem_addr(&control.parts), kStateWarps), mbar_init(smem_addr(&control.last_part), kStateWarps);
-        mbar_init(smem_addr(&control.state_ready), kStateWarps);
+        mbar_init(smem_addr(&control.state_ready), kStateWarps), mbar_init(smem_addr(&control.staged), kOutWarps), mbar_init(smem_addr(&control.left), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) take_tensor_memory<1>(smem_addr(&control.tensor_memory));
     const float log_decay = __ldg(prm.log_decay + at.w * prm.heads + at.head);
     if (threadIdx.x <= kC) control.powers[threadIdx.x] = (float)power(log_decay, threadIdx.x);
+    else if (threadIdx.x >= 192 && threadIdx.x < 224)
+        control.within[threadIdx.x - 192] = (float)power(log_decay, reversed ? threadIdx.x - 192 : 223 - threadIdx.x);
     else if (threadIdx.x >= 256 && threadIdx.x < 320) control.near[threadIdx.x - 256] = threadIdx.x < 288 ? 0.0f : term.score_scale * (float)power(log_decay, threadIdx.x - 288);
     before_sync();
     __syncthreads();
@@ -149,7 +162,7 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
 
     if (warp < kFirstOut) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kIssueRegisters));
-        if (warp == 0 && lane == 0) {
+        if (warp == 0 && elect_one()) {
             const CUtensorMap* map = maps.of[blockIdx.y];
             int issued = 0;
             for (int i = 0; i < count && prm.withhold_copies == 0; ++i) {
@@ -171,7 +184,7 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
             for (int i = max(0, issued - 2); i < issued; ++i) fine = wait(control.full[i & 1], i >> 1) && fine;
             if (!STATES && issued > 0) fine = wait(control.x_full, issued - 1) && fine;
         }
-        if (warp == 1 && lane == 0) {
+        if (warp == 1 && elect_one()) {
             const int b16 = (b + 15) / 16 * 16, a_steps = (a + 15) / 16;
             const uint32_t of_scores = instruction_descriptor(false, false, kC, kC), of_state = instruction_descriptor(false, true, kC, b16);
             const uint32_t of_update = instruction_descriptor(true, true, kC, b16);
@@ -179,6 +192,7 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
             const auto along = [](int k) { return (uint32_t)(k / 4 * kBoxBytes + k % 4 * 32) / 16; };
             const uint32_t x = descriptor_low(x_at, false, kBoxBytes), w = descriptor_low(w_at, true, w_box), rest = descriptor_low(part_at, true, kBoxBytes);
             const auto update = [&](uint32_t left, uint32_t right, bool add) {
+#pragma unroll
                 for (int k = 0; k < kC / 16; ++k) multiply<1>(tensor + kAtU, left + k * (2048 / 16), right + k * (2048 / 16), of_update, add || k > 0);
             };
             for (int i = 0; i < count; ++i) {
@@ -190,11 +204,15 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
                     if (!(fine = wait(control.x_full, i) && (i == 0 || wait(control.out_done, i - 1)))) break;
                     after_sync();
                     const uint32_t right = descriptor_low(y, false, kBoxBytes);
-                    for (int k = 0; k < a_steps; ++k) multiply<1>(tensor + kAtP, x + along(k), right + along(k), of_scores, k > 0);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        if (k < a_steps) multiply<1>(tensor + kAtP, x + along(k), right + along(k), of_scores, k > 0);
                     commit<1>(smem_addr(&control.scores));
                     if (!(fine = wait(control.state_ready, i) && wait(control.out_free, i + 1))) break;
                     after_sync();
-                    for (int k = 0; k < a_steps; ++k) multiply<1>(tensor + kAtState, x + along(k), w + k * (2048 / 16), of_state, k > 0);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        if (k < a_steps) multiply<1>(tensor + kAtState, x + along(k), w + k * (2048 / 16), of_state, k > 0);
                     commit<1>(smem_addr(&control.of_state));
                 }
                 if (updates(i)) {
@@ -207,6 +225,7 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
                 if (!STATES) {
                     if (!(fine = wait(control.masked, i))) break;
                     after_sync();
+#pragma unroll
                     for (int k = 0; k < kC / 16; ++k)
                         multiply_from_tensor(tensor + kAtOut, tensor + kAtP + k / 4 * 64 + k % 4 * 8, z + k * (2048 / 16), of_state, k > 0);
                     commit<1>(smem_addr(&control.out_done));
@@ -220,22 +239,32 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
                 commit<1>(smem_addr(&control.empty[s]));
             }
         }
+        if (!STATES && warp == 2 && elect_one()) {
+            for (int i = 0; i < count; ++i) {
+                if (!(fine = wait(control.staged, i))) break;
+                const int chunk = chunk_at(i), token = length - kC * (chunks - chunk);
+                if (token >= 0) {
+                    for (int c = 0; c < b_boxes; ++c)
+                        store_box((out_in_y ? y_at + (i & 1) * y_bytes : own_out_at) + c * kBoxBytes, maps.of[blockIdx.y] + 3, c * kBox, token, at);
+                    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                    asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                }
+                rps::mbar_arrive(smem_addr(out_in_y ? &control.empty[i & 1] : &control.left));
+            }
+            asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+        }
     } else if (warp < kFirstState) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOutRegisters));
         if constexpr (!STATES) {
-            const int quarter = warp % 4, row = quarter * 32 + lane;
+            const int quarter = warp % 4, half = (warp - kFirstOut) / 4, row = quarter * 32 + lane;
             const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+            const int first_col = half * (b_boxes == 2 ? 64 : 32), last_col = min(b, first_col + (b_boxes == 2 ? 64 : 32));
             bf16* const out = static_cast<bf16*>(term.out) + ((at.w * prm.sequences + at.sequence) * prm.tokens * prm.heads + at.head) * b;
-            // Of 32 columns that lie wholly on the near side of these rows, a decay is one of the row's distance to them times one of the column's.
-            Pair within[16];
-#pragma unroll
-            for (int j = 0; j < 16; ++j)
-                within[j] = reversed ? Pair(control.powers[2 * j], control.powers[2 * j + 1]) : Pair(control.powers[31 - 2 * j], control.powers[30 - 2 * j]);
             for (int i = 0; i < count; ++i) {
                 const int chunk = chunk_at(i), token = length - kC * (chunks - chunk) + row;
                 if (!warp_wait(control.scores, i)) break;
 #pragma unroll 1
-                for (int c = 0; c < kC; c += 32) {
+                for (int c = half * 64; c < half * 64 + 64; c += 32) {
                     uint32_t word[16];
                     const int apart = reversed ? c - quarter * 32 : quarter * 32 - c;  // of the rows' 32 and the columns'
                     if (apart < 0) {
@@ -253,12 +282,16 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
 #pragma unroll
                             for (int j = 0; j < 16; ++j) word[j] = two_bf16(p[2 * j], p[2 * j + 1]);
                         } else {
+                            // columns that lie wholly on the near side of these rows: a decay is one of the row's distance to them times one of the column's
                             const Pair far(term.score_scale * control.powers[reversed ? c - row : row - c - 31]);
 #pragma unroll
-                            for (int j = 0; j < 16; ++j) {
+                            for (int j = 0; j < 16; j += 2) {
+                                const float4 f = *reinterpret_cast<const float4*>(control.within + 2 * j);
                                 float lo, hi;
-                                (Pair(p[2 * j], p[2 * j + 1]) * far * within[j]).get(lo, hi);
+                                (Pair(p[2 * j], p[2 * j + 1]) * far * Pair(f.x, f.y)).get(lo, hi);
                                 word[j] = two_bf16(lo, hi);
+                                (Pair(p[2 * j + 2], p[2 * j + 3]) * far * Pair(f.z, f.w)).get(lo, hi);
+                                word[j + 1] = two_bf16(lo, hi);
                             }
                         }
                     }
@@ -268,24 +301,35 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
                 asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
                 warp_arrive(control.masked);
                 if (!warp_wait(control.out_done, i)) break;
+                // (before out_free: the barrier may not get two phases ahead)
+                if (out_in_y && updates(i) && !warp_wait(third_part ? control.parts_used : control.update, i)) break;
                 const int first = chunk == 0 ? missing : 0;
-                const float factor = term.state_scale * control.powers[reversed ? kC - 1 - row : max(row + 1 - first, 0)];
+                const Pair factor(term.state_scale * control.powers[reversed ? kC - 1 - row : max(row + 1 - first, 0)]);
+                const uint32_t stage_at = out_in_y ? y_at + (i & 1) * y_bytes : own_out_at;
+                if (!out_in_y && i > 0 && !warp_wait(control.left, i - 1)) break;  // the chunk before has left its place
+                if (first_col >= b) warp_arrive(control.out_free);
 #pragma unroll 1
-                for (int c = 0; c < b; c += 32) {
-                    float v[32], u[32];
+                for (int c = first_col; c < last_col; c += 16) {
+                    float v[16], u[16];
                     __syncwarp();
-                    load_sums(v, tensor + lanes + kAtOut + c), load_sums(v + 16, tensor + lanes + kAtOut + c + 16);
-                    load_sums(u, tensor + lanes + kAtState + c), load_sums(u + 16, tensor + lanes + kAtState + c + 16);
+                    load_sums(v, tensor + lanes + kAtOut + c), load_sums(u, tensor + lanes + kAtState + c);
                     tensor_loads_done();
-                    if (c + 32 >= b) warp_arrive(control.out_free);
+                    if (c + 16 >= last_col) warp_arrive(control.out_free);
 #pragma unroll
-                    for (int j = 0; j < 32; j += 8) {
-                        uint32_t word[4];
+                    for (int j = 0; j < 16; j += 8) {
+                        Pair o[4];
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) word[k] = two_bf16(fmaf(factor, u[j + 2 * k], v[j + 2 * k]), fmaf(factor, u[j + 2 * k + 1], v[j + 2 * k + 1]));
-                        if (token >= 0 && c + j < b) *reinterpret_cast<uint4*>(out + (int64_t)token * prm.heads * b + c + j) = make_uint4(word[0], word[1], word[2], word[3]);
+                        for (int k = 0; k < 4; ++k) o[k] = fma(factor, Pair(u[j + 2 * k], u[j + 2 * k + 1]), Pair(v[j + 2 * k], v[j + 2 * k + 1]));
+                        const uint4 word = narrow(o);
+                        const int col = c + j;
+                        if (first == 0)
+                            write_shared(stage_at + col / kBox * kBoxBytes + row * 128 + ((col % kBox / 8 ^ (row & 7)) << 4), word);
+                        else if (token >= 0 && col < b)  // a copy may not begin ahead of the array
+                            *reinterpret_cast<uint4*>(out + (int64_t)token * prm.heads * b + col) = word;
                     }
                 }
+                writes_done();
+                warp_arrive(control.staged);
             }
             // rows behind the sequence's last token
             const int64_t t1 = min(prm.tokens, (segment + 1) * prm.segment_tokens);
@@ -340,17 +384,16 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
                 uint32_t part[3][4];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    // as split_two, but that an infinity's first parts are the largest number
+                    // 8 of the 24 bits at a time, cut off: the three parts are the value exactly
                     Pair rest = v[j] * factor;
                     float lo, hi;
 #pragma unroll
-                    for (int k = 0; k < 2; ++k) {
+                    for (int k = 0; k < 3; ++k) {
                         rest.get(lo, hi);
-                        part[k][j] = nearest_two_bf16(lo, hi);
-                        rest = rest + Pair(__uint_as_float(part[k][j] << 16 ^ 0x80000000u), __uint_as_float((part[k][j] & 0xFFFF0000u) ^ 0x80000000u));
+                        part[k][j] = __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x7632);
+                        if (k < 2)
+                            rest = rest + Pair(__uint_as_float((__float_as_uint(lo) & 0xFFFF0000u) ^ 0x80000000u), __uint_as_float((__float_as_uint(hi) & 0xFFFF0000u) ^ 0x80000000u));
                     }
-                    rest.get(lo, hi);
-                    part[2][j] = two_bf16(lo, hi);
                 }
                 write_shared(y_row + to, make_uint4(part[0][0], part[0][1], part[0][2], part[0][3]));
                 write_shared(part_row + to, make_uint4(part[1][0], part[1][1], part[1][2], part[1][3]));
@@ -367,7 +410,7 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
                 warp_arrive(control.last_part);
             }
             if (!warp_wait(control.update, i)) break;
-            const float whole = control.powers[kC - first];
+            const Pair whole(control.powers[kC - first]);
 #pragma unroll
             for (int c = 0; c < 64; c += 32) {
                 if (c >= width) break;
@@ -376,7 +419,7 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
                 load_sums(u, tensor + lanes + kAtU + col0 + c), load_sums(u + 16, tensor + lanes + kAtU + col0 + c + 16);
                 tensor_loads_done();
 #pragma unroll
-                for (int j = 0; j < 32; ++j) w[c + j] = fmaf(whole, w[c + j], u[j]);
+                for (int j = 0; j < 32; j += 2) fma(whole, Pair(w[c + j], w[c + j + 1]), Pair(u[j], u[j + 1])).get(w[c + j], w[c + j + 1]);
             }
             before_sync();
             if (!STATES && i + 1 < count) {
@@ -396,7 +439,7 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
                 if (j < width && col0 + j < b) to[row * to_a + (col0 + j) * to_b] = w[j];
         }
     }
-    if (!fine && lane == 0) atomicExch(&g_gave_up, 1);
+    if (!fine) atomicExch(&g_gave_up, 1);
     before_sync();
     __syncthreads();
     after_sync();
@@ -429,7 +472,7 @@ bool encode(CUtensorMap* map, const MixParams& prm, const MixOperand& o, int col
 size_t shared_bytes(int a, int b)
 {
     const int a_boxes = (int)ceil_div(a, kBox), b_boxes = (int)ceil_div(b, kBox);
-    return std::max<size_t>(120 << 10, 1024 + (4 * a_boxes + 2 * b_boxes) * kBoxBytes + a_boxes * b_boxes * kBox * kBox * 2 + sizeof(Control));
+    return std::max<size_t>(120 << 10, 1024 + (4 * a_boxes + (a_boxes == 2 && b_boxes == 2 ? 2 : 3) * b_boxes) * kBoxBytes + a_boxes * b_boxes * kBox * kBox * 2 + sizeof(Control));
 }
 
 template <bool STATES>
@@ -462,7 +505,9 @@ cudaError_t launch_mix_tensor(const MixParams& prm, bool states, cudaStream_t st
     MixMaps maps{};
     for (int i = 0; i < prm.terms; ++i) {
         const MixTerm& t = prm.term[i];
-        if (!encode(&maps.of[i][0], prm, t.x, t.a) || !encode(&maps.of[i][1], prm, t.y, t.a) || !encode(&maps.of[i][2], prm, t.z, t.b)) return cudaErrorInvalidValue;
+        if (!encode(&maps.of[i][0], prm, t.x, t.a) || !encode(&maps.of[i][1], prm, t.y, t.a) || !encode(&maps.of[i][2], prm, t.z, t.b) ||
+            !encode(&maps.of[i][3], prm, {t.out, prm.sequences * prm.tokens * prm.heads * t.b, prm.tokens * prm.heads * t.b, (int64_t)prm.heads * t.b, t.b}, t.b))
+            return cudaErrorInvalidValue;
     }
     return states ? launch<true>(prm, maps, stream) : launch<false>(prm, maps, stream);
 }
