@@ -8,13 +8,20 @@
 // is the first one that may begin ahead of the sequence; TMA fills zeros there, and never reads past the last token that takes part.
 //
 // Roles (groups of four warps): warp 0 copies y and z of the next chunk (and x, once x W has been made) while this one is worked on, warp 1 issues the
-// products, warp 2 sends out away; eight (a lane to a row, half of the columns) turn P into the masked product, which goes back to tensor memory as
-// the left operand of the next one, and lay O down in shared memory; eight warps make r^f y in parts, the first in place of y, the others one after the other in a place of their own, and hold W as fp32 in
-// registers (a lane to a row of W, 64 columns), which they bring up to date out of U and lay down as bf16 for the next chunk.  Only the last of
-// these depends on the chunk before.
+// products, warp 2 sends out away, warp 3 brings W's first value and takes its last one away; eight (a lane to a row, half of the columns) turn P into
+// the masked product, which goes back to tensor memory as the left operand of the next one, and lay O down in shared memory; sixteen make r^f y
+// in parts and hold W as fp32 in registers (a lane to a row of W, a quarter of the columns), which they bring up to date out of U and lay down as bf16
+// for the next chunk.  With up to 64 columns of y and z (OWN) all the parts have places of their own, and twice, so that the next chunk's are made
+// while U is; with more, the first takes y's place and the others one after the other a single one.
 //
-// r^f y is three bf16 parts where a state is written (fp32 has 24 bits, and a state sums many terms); where W only goes on into bf16 results, two.
-// (One, whose rounding is then as large as those of P o D and W, took dq and dk of heads of 128 from 2.3e-3 to 2.7e-3 of their norm off.)
+// Each role's code for a chunk is run once by a few warps and then not until the next chunk, so its instructions come from afar: it is kept short (loops
+// that are not unrolled, each step written once; 115 KB of code took 454 us where ... takes ...).
+//
+// r^f y is three bf16 parts where a state is written (fp32 has 24 bits, and a state sums many terms); where W only goes on into bf16 results, as itself
+// rounded to bf16, two.  (One, whose rounding is then as large as those of P o D and W, took dq and dk of heads of 128 from 2.3e-3 to 2.7e-3 of
+// their norm off.)
+//
+// What a chunk takes is this kernel's own instructions and the way from one role to the next, not the tensor cores (a fifth) or memory.
 #include "rps_mix.cuh"
 #include "rps_tensor.cuh"
 
@@ -27,24 +34,48 @@ using rps::smem_addr;
 
 constexpr int kC = kMixTensorChunk;
 constexpr int kBox = 64, kBoxBytes = kC * kBox * 2;  // columns of a copy: one swizzled line of 128 bytes a row
-constexpr int kOutWarps = 8, kStateWarps = 8, kFirstOut = 4, kFirstState = kFirstOut + kOutWarps;
+constexpr int kStateBox = 32;                        // fp32 columns of a state's copy: the same
+constexpr int kOutWarps = 8, kStateWarps = 16, kFirstOut = 4, kFirstState = kFirstOut + kOutWarps;
 constexpr int kThreads = 32 * (kFirstState + kStateWarps);
-// Registers of a thread, shared out anew among the groups of four warps: those that hold W have more than the 96 that all alike could have.
-constexpr int kLaunchRegisters = 96, kIssueRegisters = 64, kOutRegisters = 72, kStateRegisters = 136;
+// Registers of a thread, shared out anew among the groups of four warps: those that hold W have more than the 72 that all alike could have.
+constexpr int kLaunchRegisters = 72, kIssueRegisters = 40, kOutRegisters = 56, kStateRegisters = 88;
 static_assert(4 * kIssueRegisters + kOutWarps * kOutRegisters + kStateWarps * kStateRegisters <= kThreads / 32 * kLaunchRegisters, "the block's own");
 // columns of tensor memory: P, and P o D as 16-bit pairs in its place; x W; (P o D) z; U
 constexpr int kAtP = 0, kAtState = 128, kAtOut = 256, kAtU = 384;
 
+// Barriers.  Whoever waits for one has to do so before it completes a second time, as a wait only tells even completions from odd ones; those that
+// would get further ahead come in pairs that take turns.
 struct Control {
-    uint64_t full[2], empty[2], x_full, scores, masked, of_state, out_done, out_free, parts, parts_used, last_part, update, state_ready, staged, left;
+    uint64_t full[2], empty[2], x_full, scores, masked, of_state, out_done, out_free, parts[2], parts_used, last_part, update[2], state_ready, staged[2], left, state_in, state_read, state_out;
     uint32_t tensor_memory;
     float powers[kC + 1];  // r^0 .. r^128
-    float near[64];        // score_scale r^(e - 32), zero where the exponent is negative
+    float near[64];        // score_scale times the decay from a row to a column e - 32 less, zero ahead of time
     alignas(16) float within[32];  // a decay's share of each of 32 columns
 };
 
+// How a state reaches a CTA or leaves it: not at all, by TMA, or element by element (in another order, or at an odd address).
+enum StateWay { kNoState = 0, kCopied = 1, kByElement = 2 };
+
 struct MixMaps {
     CUtensorMap of[3][4];  // x, y, z and out of each term
+    CUtensorMap state[3][2];  // W before and after
+    int way[3][2];
+};
+
+// Where a CTA's arrays lie in shared memory.
+struct Places {
+    int a_boxes, b_boxes;
+    bool out_in_y;                          // out leaves from y's place, whose first part has been multiplied by then
+    uint32_t y_bytes, z_bytes, w_box;
+    uint32_t x, y, z, part, w, out, control;  // offsets; two of y and z; W's first and last value takes the place of `part` and `w`
+    __host__ __device__ Places(int a, int b, bool own)
+    {
+        a_boxes = (a + kBox - 1) / kBox, b_boxes = (b + kBox - 1) / kBox;
+        out_in_y = a_boxes == 2 && b_boxes == 2;
+        y_bytes = a_boxes * kBoxBytes, z_bytes = b_boxes * kBoxBytes, w_box = a_boxes * kBox * kBox * 2;
+        x = 0, y = x + y_bytes, z = y + 2 * y_bytes, part = z + 2 * z_bytes, w = part + (own ? 6 : 1) * y_bytes;
+        out = w + b_boxes * w_box, control = out + (out_in_y ? 0 : z_bytes);
+    }
 };
 
 __device__ int g_gave_up = 0;
@@ -61,6 +92,19 @@ __device__ __forceinline__ void store_box(uint32_t src, const CUtensorMap* map, 
     asm volatile("cp.async.bulk.tensor.5d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3, %4, %5}], [%6];" ::"l"(map), "r"(col), "r"(token), "r"(at.head),
                  "r"(at.sequence), "r"(at.w), "r"(src)
                  : "memory");
+}
+
+// 32 columns of all rows of a state.
+__device__ __forceinline__ void load_state(uint32_t dst, const CUtensorMap* map, int col, int index, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, 0, %3}], [%4];" ::"r"(dst), "l"(map), "r"(col), "r"(index),
+                 "r"(bar)
+                 : "memory");
+}
+
+__device__ __forceinline__ void store_state(uint32_t src, const CUtensorMap* map, int col, int index)
+{
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, 0, %2}], [%3];" ::"l"(map), "r"(col), "r"(index), "r"(src) : "memory");
 }
 
 // The left operand in tensor memory.
@@ -94,7 +138,15 @@ __device__ __forceinline__ void write_shared(uint32_t addr, const uint4& v)
     asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
 
-template <bool STATES>
+// exp(log_decay * exponent) of exponents up to 128, the argument's own rounding made up for.
+__device__ __forceinline__ float small_power(float log_decay, int exponent)
+{
+    if (!(log_decay <= 0.0f)) return nanf("");
+    const float rate = fmaxf(log_decay, -1e4f), e = (float)exponent, argument = rate * e;
+    return expf(argument) * (1.0f + fmaf(rate, e, -argument));
+}
+
+template <bool STATES, bool OWN>
 __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __grid_constant__ MixParams prm, const __grid_constant__ MixMaps maps)
 {
     after_the_kernel_before();
@@ -104,14 +156,11 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
     if (STATES && segment + 1 == prm.segments) return;
     extern __shared__ unsigned char raw[];
     const uint32_t base = (smem_addr(raw) + 1023) / 1024 * 1024;
-    const int a = term.a, b = term.b, a_boxes = (a + kBox - 1) / kBox, b_boxes = (b + kBox - 1) / kBox;
-    const uint32_t y_bytes = a_boxes * kBoxBytes, z_bytes = b_boxes * kBoxBytes;
-    const uint32_t x_at = base, y_at = x_at + y_bytes, z_at = y_at + 2 * y_bytes, part_at = z_at + 2 * z_bytes;  // two places for y and z
-    const uint32_t w_at = part_at + y_bytes, w_box = a_boxes * kBox * kBox * 2;
-    // out on its way to memory: where there is no room for a place of its own, in y's, whose first part has been multiplied by then
-    const bool out_in_y = a_boxes == 2 && b_boxes == 2;
-    const uint32_t own_out_at = w_at + b_boxes * w_box;
-    Control& control = *reinterpret_cast<Control*>(raw + (own_out_at + (out_in_y ? 0 : z_bytes) - smem_addr(raw)));
+    const int a = term.a, b = term.b;
+    const Places places(a, b, OWN);
+    const int a_boxes = places.a_boxes, b_boxes = places.b_boxes;
+    const uint32_t y_bytes = places.y_bytes, z_bytes = places.z_bytes;
+    Control& control = *reinterpret_cast<Control*>(raw + (base + places.control - smem_addr(raw)));
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const Place at = place_of(prm, unit);
     const bool reversed = term.reversed != 0;
@@ -125,22 +174,31 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
     // the last chunk's part of W counts only where W is written
     const bool writes_state = STATES || (last && term.state_out != nullptr);
     const auto updates = [&](int i) { return i + 1 < count || writes_state; };
+    // U's place: without O's use of tensor memory two take turns, as the next chunk's U does not wait for W there
+    const auto u_of = [](int i) { return STATES && (i & 1) ? kAtOut : kAtU; };
+    // W before the segment and after it
+    const int64_t slot = (blockIdx.y * prm.units + unit) * prm.segments + segment;
+    const int way_in = maps.way[blockIdx.y][0], way_out = writes_state ? maps.way[blockIdx.y][1] : kNoState;
 
     if (warp == 0 && lane == 0) {
-        for (int s = 0; s < 2; ++s) mbar_init(smem_addr(&control.full[s]), 1), mbar_init(smem_addr(&control.empty[s]), out_in_y && !STATES ? 2 : 1);
-        mbar_init(smem_addr(&control.x_full), 1), mbar_init(smem_addr(&control.scores), 1), mbar_init(smem_addr(&control.of_state), 1), mbar_init(smem_addr(&control.out_done), 1);
-        mbar_init(smem_addr(&control.parts_used), 1), mbar_init(smem_addr(&control.update), 1);
-        mbar_init(smem_addr(&control.masked), kOutWarps), mbar_init(smem_addr(&control.out_free), kOutWarps);
-        mbar_init(smem_addr(&control.parts), kStateWarps), mbar_init(smem_addr(&control.last_part), kStateWarps);
-        mbar_init(smem_addr(&control.state_ready), kStateWarps), mbar_init(smem_addr(&control.staged), kOutWarps), mbar_init(smem_addr(&control.left), 1);
+        const auto init = [](uint64_t& bar, int arrivals) { mbar_init(smem_addr(&bar), arrivals); };
+        for (int s = 0; s < 2; ++s) init(control.full[s], 1), init(control.empty[s], places.out_in_y && !STATES ? 2 : 1), init(control.parts[s], kStateWarps), init(control.update[s], 1),
+                                    init(control.staged[s], kOutWarps);
+        init(control.x_full, 1), init(control.scores, 1), init(control.of_state, 1), init(control.out_done, 1), init(control.parts_used, 1);
+        init(control.masked, kOutWarps), init(control.out_free, kOutWarps), init(control.left, 1);
+        init(control.last_part, kStateWarps), init(control.state_ready, kStateWarps), init(control.state_in, 1), init(control.state_read, kStateWarps), init(control.state_out, kStateWarps);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) take_tensor_memory<1>(smem_addr(&control.tensor_memory));
     const float log_decay = __ldg(prm.log_decay + at.w * prm.heads + at.head);
-    if (threadIdx.x <= kC) control.powers[threadIdx.x] = (float)power(log_decay, threadIdx.x);
+    if (threadIdx.x <= kC)
+        control.powers[threadIdx.x] = small_power(log_decay, threadIdx.x);
     else if (threadIdx.x >= 192 && threadIdx.x < 224)
-        control.within[threadIdx.x - 192] = (float)power(log_decay, reversed ? threadIdx.x - 192 : 223 - threadIdx.x);
-    else if (threadIdx.x >= 256 && threadIdx.x < 320) control.near[threadIdx.x - 256] = threadIdx.x < 288 ? 0.0f : term.score_scale * (float)power(log_decay, threadIdx.x - 288);
+        control.within[threadIdx.x - 192] = small_power(log_decay, reversed ? threadIdx.x - 192 : 223 - threadIdx.x);
+    else if (threadIdx.x >= 256 && threadIdx.x < 320) {
+        const int apart = reversed ? 288 - (int)threadIdx.x : (int)threadIdx.x - 288;
+        control.near[threadIdx.x - 256] = apart < 0 ? 0.0f : term.score_scale * small_power(log_decay, apart);
+    }
     before_sync();
     __syncthreads();
     after_sync();
@@ -170,14 +228,14 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
                 if (!(fine = wait(control.empty[s], (i >> 1) + 1))) break;
                 uint32_t bar = smem_addr(&control.full[s]);
                 mbar_arrive_expect_tx(bar, y_bytes + z_bytes);
-                for (int c = 0; c < a_boxes; ++c) load_box(y_at + s * y_bytes + c * kBoxBytes, map + 1, c * kBox, token, at, bar);
-                for (int c = 0; c < b_boxes; ++c) load_box(z_at + s * z_bytes + c * kBoxBytes, map + 2, c * kBox, token, at, bar);
+                for (int c = 0; c < a_boxes; ++c) load_box(base + places.y + s * y_bytes + c * kBoxBytes, map + 1, c * kBox, token, at, bar);
+                for (int c = 0; c < b_boxes; ++c) load_box(base + places.z + s * z_bytes + c * kBoxBytes, map + 2, c * kBox, token, at, bar);
                 ++issued;
                 if (!STATES) {
                     if (i > 0 && !(fine = wait(control.of_state, i - 1))) break;  // the chunk before has read x
                     bar = smem_addr(&control.x_full);
                     mbar_arrive_expect_tx(bar, y_bytes);
-                    for (int c = 0; c < a_boxes; ++c) load_box(x_at + c * kBoxBytes, map, c * kBox, token, at, bar);
+                    for (int c = 0; c < a_boxes; ++c) load_box(base + places.x + c * kBoxBytes, map, c * kBox, token, at, bar);
                 }
             }
             // all copies have arrived before the CTA may end
@@ -185,80 +243,104 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
             if (!STATES && issued > 0) fine = wait(control.x_full, issued - 1) && fine;
         }
         if (warp == 1 && elect_one()) {
-            const int b16 = (b + 15) / 16 * 16, a_steps = (a + 15) / 16;
+            const int b16 = (b + 15) / 16 * 16;
             const uint32_t of_scores = instruction_descriptor(false, false, kC, kC), of_state = instruction_descriptor(false, true, kC, b16);
             const uint32_t of_update = instruction_descriptor(true, true, kC, b16);
+            const uint32_t x = descriptor_low(base + places.x, false, kBoxBytes), w = descriptor_low(base + places.w, true, places.w_box);
+            const uint32_t first_y = descriptor_low(base + places.y, false, kBoxBytes), first_z = descriptor_low(base + places.z, true, kBoxBytes);
+            const uint32_t first_part = descriptor_low(base + places.y, true, kBoxBytes), rest = descriptor_low(base + places.part, true, kBoxBytes);
             // along the rows of a tile 16 columns further: 32 bytes, after 64 the next box; along its columns 16 rows of 128 bytes
-            const auto along = [](int k) { return (uint32_t)(k / 4 * kBoxBytes + k % 4 * 32) / 16; };
-            const uint32_t x = descriptor_low(x_at, false, kBoxBytes), w = descriptor_low(w_at, true, w_box), rest = descriptor_low(part_at, true, kBoxBytes);
-            const auto update = [&](uint32_t left, uint32_t right, bool add) {
-#pragma unroll
-                for (int k = 0; k < kC / 16; ++k) multiply<1>(tensor + kAtU, left + k * (2048 / 16), right + k * (2048 / 16), of_update, add || k > 0);
-            };
+            constexpr uint32_t along = 32 / 16, across = 2048 / 16, box = kBoxBytes / 16;
             for (int i = 0; i < count; ++i) {
                 const int s = i & 1;
-                const uint32_t y = y_at + s * y_bytes, z = descriptor_low(z_at + s * z_bytes, true, kBoxBytes);
+                const uint32_t y = first_y + s * (y_bytes / 16), z = first_z + s * (z_bytes / 16);
                 if (!(fine = wait(control.full[s], i >> 1))) break;
                 if (!STATES) {
                     // P's place holds the left operand of the product for out of the chunk before
                     if (!(fine = wait(control.x_full, i) && (i == 0 || wait(control.out_done, i - 1)))) break;
                     after_sync();
-                    const uint32_t right = descriptor_low(y, false, kBoxBytes);
+#pragma unroll 1
+                    for (int c = 0; c < a_boxes; ++c)
 #pragma unroll
-                    for (int k = 0; k < 8; ++k)
-                        if (k < a_steps) multiply<1>(tensor + kAtP, x + along(k), right + along(k), of_scores, k > 0);
+                        for (int k = 0; k < 4; ++k) multiply<1>(tensor + kAtP, x + c * box + k * along, y + c * box + k * along, of_scores, c + k > 0);
                     commit<1>(smem_addr(&control.scores));
                     if (!(fine = wait(control.state_ready, i) && wait(control.out_free, i + 1))) break;
                     after_sync();
+#pragma unroll 1
+                    for (int c = 0; c < a_boxes; ++c)
 #pragma unroll
-                    for (int k = 0; k < 8; ++k)
-                        if (k < a_steps) multiply<1>(tensor + kAtState, x + along(k), w + k * (2048 / 16), of_state, k > 0);
+                        for (int k = 0; k < 4; ++k) multiply<1>(tensor + kAtState, x + c * box + k * along, w + (4 * c + k) * across, of_state, c + k > 0);
                     commit<1>(smem_addr(&control.of_state));
-                }
-                if (updates(i)) {
-                    if (!(fine = wait(control.parts, i))) break;
-                    after_sync();
-                    update(descriptor_low(y, true, kBoxBytes), z, false);
-                    update(rest, z, true);
-                    commit<1>(smem_addr(third_part ? &control.parts_used : &control.update));
-                }
-                if (!STATES) {
                     if (!(fine = wait(control.masked, i))) break;
                     after_sync();
+#pragma unroll 1
+                    for (int c = 0; c < 2; ++c)
 #pragma unroll
-                    for (int k = 0; k < kC / 16; ++k)
-                        multiply_from_tensor(tensor + kAtOut, tensor + kAtP + k / 4 * 64 + k % 4 * 8, z + k * (2048 / 16), of_state, k > 0);
+                        for (int k = 0; k < 4; ++k)
+                            multiply_from_tensor(tensor + kAtOut, tensor + kAtP + c * 64 + k * 8, z + (4 * c + k) * across, of_state, c + k > 0);
                     commit<1>(smem_addr(&control.out_done));
                 }
-                if (updates(i) && third_part) {
-                    if (!(fine = wait(control.last_part, i))) break;
+                if (updates(i)) {
+                    if (!(fine = OWN ? wait(control.parts[s], i >> 1) : wait(control.parts[0], i))) break;
                     after_sync();
-                    update(rest, z, true);
-                    commit<1>(smem_addr(&control.update));
+                    const int parts = third_part ? 3 : 2;
+#pragma unroll 1
+                    for (int p = 0; p < parts; ++p) {
+                        if (!OWN && p == 2) {
+                            commit<1>(smem_addr(&control.parts_used));
+                            if (!(fine = wait(control.last_part, i))) break;
+                            after_sync();
+                        }
+                        const uint32_t left = OWN ? rest + (s * 3 + p) * box : p == 0 ? first_part + s * (y_bytes / 16) : rest;
+#pragma unroll 1
+                        for (int c = 0; c < 2; ++c)
+#pragma unroll
+                            for (int k = 0; k < 4; ++k)
+                                multiply<1>(tensor + u_of(i), left + (4 * c + k) * across, z + (4 * c + k) * across, of_update, p + c + k > 0);
+                    }
+                    if (!fine) break;
+                    commit<1>(smem_addr(&control.update[s]));
                 }
                 commit<1>(smem_addr(&control.empty[s]));
             }
         }
         if (!STATES && warp == 2 && elect_one()) {
             for (int i = 0; i < count; ++i) {
-                if (!(fine = wait(control.staged, i))) break;
-                const int chunk = chunk_at(i), token = length - kC * (chunks - chunk);
-                if (token >= 0) {
-                    for (int c = 0; c < b_boxes; ++c)
-                        store_box((out_in_y ? y_at + (i & 1) * y_bytes : own_out_at) + c * kBoxBytes, maps.of[blockIdx.y] + 3, c * kBox, token, at);
+                if (!(fine = wait(control.staged[i & 1], i >> 1))) break;
+                const int token = length - kC * (chunks - chunk_at(i));
+                if (token >= 0) {  // a copy may not begin ahead of the array
+                    const uint32_t from = base + (places.out_in_y ? places.y + (i & 1) * y_bytes : places.out);
+                    for (int c = 0; c < b_boxes; ++c) store_box(from + c * kBoxBytes, maps.of[blockIdx.y] + 3, c * kBox, token, at);
                     asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                     asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
                 }
-                rps::mbar_arrive(smem_addr(out_in_y ? &control.empty[i & 1] : &control.left));
+                rps::mbar_arrive(smem_addr(places.out_in_y ? &control.empty[i & 1] : &control.left));
             }
             asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+        }
+        if (warp == 3 && elect_one()) {
+            const int boxes = (b + kStateBox - 1) / kStateBox;
+            const uint32_t box_bytes = a_boxes * kBox * kStateBox * 4;
+            if (way_in == kCopied && prm.withhold_copies == 0) {
+                const uint32_t bar = smem_addr(&control.state_in);
+                mbar_arrive_expect_tx(bar, boxes * box_bytes);
+                const int from = (int)(prm.segments > 1 ? slot : unit);
+                for (int c = 0; c < boxes; ++c) load_state(base + places.part + c * box_bytes, &maps.state[blockIdx.y][0], c * kStateBox, from, bar);
+                fine = wait(control.state_in, 0);
+            }
+            if (way_out == kCopied && (fine = wait(control.state_out, 0) && fine)) {
+                const int to = (int)(STATES ? slot + 1 : unit);
+                for (int c = 0; c < boxes; ++c) store_state(base + places.part + c * box_bytes, &maps.state[blockIdx.y][1], c * kStateBox, to);
+                asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+            }
         }
     } else if (warp < kFirstState) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOutRegisters));
         if constexpr (!STATES) {
             const int quarter = warp % 4, half = (warp - kFirstOut) / 4, row = quarter * 32 + lane;
             const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
-            const int first_col = half * (b_boxes == 2 ? 64 : 32), last_col = min(b, first_col + (b_boxes == 2 ? 64 : 32));
+            const int first_col = half * b_boxes * 32, last_col = min(b, first_col + b_boxes * 32);
             bf16* const out = static_cast<bf16*>(term.out) + ((at.w * prm.sequences + at.sequence) * prm.tokens * prm.heads + at.head) * b;
             for (int i = 0; i < count; ++i) {
                 const int chunk = chunk_at(i), token = length - kC * (chunks - chunk) + row;
@@ -276,9 +358,9 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
                         load_sums(p, tensor + lanes + kAtP + c), load_sums(p + 16, tensor + lanes + kAtP + c + 16);
                         tensor_loads_done();
                         if (apart == 0) {
-                            const float* near = control.near + 32 + (reversed ? -lane : lane);
+                            const float* near = control.near + 32 + lane;
 #pragma unroll
-                            for (int j = 0; j < 32; ++j) p[j] *= reversed ? near[j] : near[-j];
+                            for (int j = 0; j < 32; ++j) p[j] *= near[-j];
 #pragma unroll
                             for (int j = 0; j < 16; ++j) word[j] = two_bf16(p[2 * j], p[2 * j + 1]);
                         } else {
@@ -302,11 +384,11 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
                 warp_arrive(control.masked);
                 if (!warp_wait(control.out_done, i)) break;
                 // (before out_free: the barrier may not get two phases ahead)
-                if (out_in_y && updates(i) && !warp_wait(third_part ? control.parts_used : control.update, i)) break;
+                if (places.out_in_y && updates(i) && !(third_part ? warp_wait(control.parts_used, i) : warp_wait(control.update[i & 1], i >> 1))) break;
                 const int first = chunk == 0 ? missing : 0;
                 const Pair factor(term.state_scale * control.powers[reversed ? kC - 1 - row : max(row + 1 - first, 0)]);
-                const uint32_t stage_at = out_in_y ? y_at + (i & 1) * y_bytes : own_out_at;
-                if (!out_in_y && i > 0 && !warp_wait(control.left, i - 1)) break;  // the chunk before has left its place
+                const uint32_t stage = base + (places.out_in_y ? places.y + (i & 1) * y_bytes : places.out) + row * 128;
+                if (!places.out_in_y && i > 0 && !warp_wait(control.left, i - 1)) break;  // the chunk before has left its place
                 if (first_col >= b) warp_arrive(control.out_free);
 #pragma unroll 1
                 for (int c = first_col; c < last_col; c += 16) {
@@ -323,13 +405,13 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
                         const uint4 word = narrow(o);
                         const int col = c + j;
                         if (first == 0)
-                            write_shared(stage_at + col / kBox * kBoxBytes + row * 128 + ((col % kBox / 8 ^ (row & 7)) << 4), word);
-                        else if (token >= 0 && col < b)  // a copy may not begin ahead of the array
+                            write_shared(stage + col / kBox * kBoxBytes + ((col % kBox / 8 ^ (row & 7)) << 4), word);
+                        else if (token >= 0 && col < b)
                             *reinterpret_cast<uint4*>(out + (int64_t)token * prm.heads * b + col) = word;
                     }
                 }
                 writes_done();
-                warp_arrive(control.staged);
+                warp_arrive(control.staged[i & 1]);
             }
             // rows behind the sequence's last token
             const int64_t t1 = min(prm.tokens, (segment + 1) * prm.segment_tokens);
@@ -338,49 +420,63 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kStateRegisters));
-        const int quarter = warp % 4, half = (warp - kFirstState) / 4, row = quarter * 32 + lane;
+        const int quarter = warp % 4, share = (warp - kFirstState) / 4, row = quarter * 32 + lane, swizzle = row & 7;
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
-        // W: row `row`, columns from col0 on: 64 of them, or 32 where there are no more than 64
-        const int width = b_boxes == 2 ? 64 : 32, col0 = half * width;
-        float w[64];
-        const float* init = nullptr;
-        int64_t init_a = b, init_b = 1;
-        if (!STATES && prm.segments > 1)
-            init = prm.segment_states + ((blockIdx.y * prm.units + unit) * prm.segments + segment) * prm.state_room;
-        else if (!STATES && term.state_in != nullptr)
-            init = term.state_in + unit * a * b, init_a = term.state_a, init_b = term.state_b;
+        // W: row `row`, columns from col0 on: 32 of them, or 16 where there are no more than 64 in all
+        const int width = b_boxes * 16, col0 = share * width;
+        const bool there = row < a_boxes * kBox;  // in shared memory
+        float w[32];
 #pragma unroll
-        for (int j = 0; j < 64; ++j) w[j] = init != nullptr && row < a && j < width && col0 + j < b ? __ldg(init + row * init_a + (col0 + j) * init_b) : 0.0f;
+        for (int j = 0; j < 32; ++j) w[j] = 0.0f;
+        const uint32_t state_row = base + places.part + col0 / kStateBox * (a_boxes * kBox * kStateBox * 4) + row * 128;
+        if (way_in == kCopied) {
+            if (warp_wait(control.state_in, 0) && there) {
+#pragma unroll
+                for (int j = 0; j < 32; j += 4) {
+                    if (j >= width || col0 + j >= b) break;
+                    const uint4 v = read_shared(state_row + ((col0 % kStateBox / 4 + j / 4 ^ swizzle) << 4));
+                    w[j] = __uint_as_float(v.x), w[j + 1] = __uint_as_float(v.y), w[j + 2] = __uint_as_float(v.z), w[j + 3] = __uint_as_float(v.w);
+                }
+            }
+            // the others' columns lie where this thread's are laid down next
+            if (fine) {
+                warp_arrive(control.state_read);
+                warp_wait(control.state_read, 0);
+            }
+        } else if (way_in == kByElement && row < a) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+                if (j < width && col0 + j < b) w[j] = __ldg(term.state_in + unit * a * b + row * term.state_a + (col0 + j) * term.state_b);
+        }
         const auto publish = [&] {  // W where the products read it
-            if (row < a_boxes * kBox) {
+            if (there) {
 #pragma unroll
-                for (int j = 0; j < 64; j += 8) {
+                for (int j = 0; j < 32; j += 8) {
                     if (j >= width) break;
                     const int col = col0 + j;
-                    write_shared(w_at + col / kBox * w_box + row * 128 + ((col % kBox / 8 ^ (row & 7)) << 4),
+                    write_shared(base + places.w + col / kBox * places.w_box + row * 128 + ((col % kBox / 8 ^ swizzle) << 4),
                                  make_uint4(two_bf16(w[j], w[j + 1]), two_bf16(w[j + 2], w[j + 3]), two_bf16(w[j + 4], w[j + 5]), two_bf16(w[j + 6], w[j + 7])));
                 }
             }
             writes_done();
             warp_arrive(control.state_ready);
         };
-        if (!STATES && count > 0) publish();
-        // this thread's columns of a row of y: a box, or half of the only one
-        const int pieces = a_boxes == 2 ? 8 : 4, piece0 = a_boxes == 2 ? 0 : half * 4;
-        const uint32_t row_at = (a_boxes == 2 ? half * kBoxBytes : 0) + row * 128;
-        for (int i = 0; i < count && updates(i); ++i) {
+        // this thread's columns of a row of y: a quarter of them, in pieces of 8
+        constexpr int kPieces = OWN ? 2 : 4;
+        const int pieces = a_boxes * 2, piece0 = share * pieces % 8;
+        const uint32_t row_at = base + share * pieces / 8 * kBoxBytes + row * 128;
+        uint4 third[kPieces];
+        // y of chunk i into its parts: where there is but one place for them, the first in y's own
+        const auto split = [&](int i) {
             const int s = i & 1, first = chunk_at(i) == 0 ? missing : 0;
-            const uint32_t y_row = y_at + s * y_bytes + row_at, part_row = part_at + row_at;
-            // y has been read by the product for P; the other place was left by the chunk before (`update`)
-            if (!warp_wait(control.full[s], i >> 1) || (!STATES && !warp_wait(control.scores, i))) break;
+            const uint32_t from = row_at + places.y + s * y_bytes, to = row_at + places.part + (OWN ? s * 3 * y_bytes : 0);
             const Pair factor(term.update_scale * control.powers[reversed ? max(row + 1 - first, 0) : kC - 1 - row]);
-            uint4 third[8];
 #pragma unroll
-            for (int q = 0; q < 8; ++q) {
+            for (int q = 0; q < kPieces; ++q) {
                 if (q >= pieces) break;
-                const uint32_t to = ((piece0 + q) ^ (row & 7)) << 4;
+                const uint32_t piece = ((piece0 + q) ^ swizzle) << 4;
                 Pair v[4];
-                widen(read_shared(y_row + to), v);
+                widen(read_shared(from + piece), v);
                 uint32_t part[3][4];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
@@ -395,48 +491,81 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
                             rest = rest + Pair(__uint_as_float((__float_as_uint(lo) & 0xFFFF0000u) ^ 0x80000000u), __uint_as_float((__float_as_uint(hi) & 0xFFFF0000u) ^ 0x80000000u));
                     }
                 }
-                write_shared(y_row + to, make_uint4(part[0][0], part[0][1], part[0][2], part[0][3]));
-                write_shared(part_row + to, make_uint4(part[1][0], part[1][1], part[1][2], part[1][3]));
                 third[q] = make_uint4(part[2][0], part[2][1], part[2][2], part[2][3]);
+                write_shared((OWN ? to : from) + piece, make_uint4(part[0][0], part[0][1], part[0][2], part[0][3]));
+                write_shared(to + (OWN ? y_bytes : 0) + piece, make_uint4(part[1][0], part[1][1], part[1][2], part[1][3]));
+                if (OWN) write_shared(to + 2 * y_bytes + piece, third[q]);
             }
             writes_done();
-            warp_arrive(control.parts);
-            if (third_part) {
-                if (!warp_wait(control.parts_used, i)) break;
+            warp_arrive(control.parts[OWN ? s : 0]);
+        };
+        // W of the next chunk: false if a wait gave up
+        const auto bring_up_to_date = [&](int i) {
+            if (!warp_wait(control.update[i & 1], i >> 1)) return false;
+            const Pair whole(control.powers[kC - (chunk_at(i) == 0 ? missing : 0)]);
 #pragma unroll
-                for (int q = 0; q < 8; ++q)
-                    if (q < pieces) write_shared(part_row + (((piece0 + q) ^ (row & 7)) << 4), third[q]);
-                writes_done();
-                warp_arrive(control.last_part);
-            }
-            if (!warp_wait(control.update, i)) break;
-            const Pair whole(control.powers[kC - first]);
-#pragma unroll
-            for (int c = 0; c < 64; c += 32) {
+            for (int c = 0; c < 32; c += 16) {
                 if (c >= width) break;
-                float u[32];
+                float u[16];
                 __syncwarp();
-                load_sums(u, tensor + lanes + kAtU + col0 + c), load_sums(u + 16, tensor + lanes + kAtU + col0 + c + 16);
+                load_sums(u, tensor + lanes + u_of(i) + col0 + c);
                 tensor_loads_done();
 #pragma unroll
-                for (int j = 0; j < 32; j += 2) fma(whole, Pair(w[c + j], w[c + j + 1]), Pair(u[j], u[j + 1])).get(w[c + j], w[c + j + 1]);
+                for (int j = 0; j < 16; j += 2) fma(whole, Pair(w[c + j], w[c + j + 1]), Pair(u[j], u[j + 1])).get(w[c + j], w[c + j + 1]);
             }
             before_sync();
-            if (!STATES && i + 1 < count) {
-                if (!warp_wait(control.of_state, i)) break;  // W's place has been read
-                publish();
+            return true;
+        };
+        if constexpr (OWN) {
+            // a chunk's parts are made before the W that goes with them is waited for
+            for (int i = 0; fine; ++i) {
+                if (i < count && updates(i)) {
+                    if (!warp_wait(control.full[i & 1], i >> 1)) break;
+                    split(i);
+                }
+                if (i > 0 && (!updates(i - 1) || !bring_up_to_date(i - 1))) break;
+                if (i >= count) break;
+                if constexpr (!STATES) {
+                    if (i > 0 && !warp_wait(control.of_state, i - 1)) break;  // W's place has been read
+                    publish();
+                }
+            }
+        } else {
+            for (int i = 0; i < count && fine; ++i) {
+                if constexpr (!STATES) {
+                    if (i > 0 && !warp_wait(control.of_state, i - 1)) break;
+                    publish();
+                }
+                // y's own place has been read by the product for P; the other was left by the chunk before
+                if (!updates(i) || !warp_wait(control.full[i & 1], i >> 1) || (!STATES && !warp_wait(control.scores, i))) break;
+                split(i);
+                if (third_part) {
+                    if (!warp_wait(control.parts_used, i)) break;
+#pragma unroll
+                    for (int q = 0; q < kPieces; ++q)
+                        if (q < pieces) write_shared(row_at + places.part + (((piece0 + q) ^ swizzle) << 4), third[q]);
+                    writes_done();
+                    warp_arrive(control.last_part);
+                }
+                if (!bring_up_to_date(i)) break;
             }
         }
-        float* to = nullptr;
-        int64_t to_a = b, to_b = 1;
-        if (STATES)
-            to = prm.segment_states + ((blockIdx.y * prm.units + unit) * prm.segments + segment + 1) * prm.state_room;
-        else if (writes_state)
-            to = term.state_out + unit * a * b, to_a = term.state_a, to_b = term.state_b;
-        if (to != nullptr && fine && row < a) {
+        // the last product has read the places that W's last value takes
+        if (way_out == kCopied && fine) {
+            if (there) {
 #pragma unroll
-            for (int j = 0; j < 64; ++j)
-                if (j < width && col0 + j < b) to[row * to_a + (col0 + j) * to_b] = w[j];
+                for (int j = 0; j < 32; j += 4) {
+                    if (j >= width || col0 + j >= b) break;
+                    write_shared(state_row + ((col0 % kStateBox / 4 + j / 4 ^ swizzle) << 4),
+                                 make_uint4(__float_as_uint(w[j]), __float_as_uint(w[j + 1]), __float_as_uint(w[j + 2]), __float_as_uint(w[j + 3])));
+                }
+            }
+            writes_done();
+            warp_arrive(control.state_out);
+        } else if (way_out == kByElement && fine && row < a) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+                if (j < width && col0 + j < b) term.state_out[unit * a * b + row * term.state_a + (col0 + j) * term.state_b] = w[j];
         }
     }
     if (!fine) atomicExch(&g_gave_up, 1);
@@ -468,24 +597,32 @@ bool encode(CUtensorMap* map, const MixParams& prm, const MixOperand& o, int col
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Shared memory of a CTA: more than half of an SM's, as the tensor memory that a CTA takes is all there is.
-size_t shared_bytes(int a, int b)
+// `states` states of a x b, `apart` elements from one to the next.
+bool encode_state(CUtensorMap* map, const float* base, int a, int b, int64_t states, int64_t apart)
 {
-    const int a_boxes = (int)ceil_div(a, kBox), b_boxes = (int)ceil_div(b, kBox);
-    return std::max<size_t>(120 << 10, 1024 + (4 * a_boxes + (a_boxes == 2 && b_boxes == 2 ? 2 : 3) * b_boxes) * kBoxBytes + a_boxes * b_boxes * kBox * kBox * 2 + sizeof(Control));
+    rps::EncodeTiledFn encode = rps::encode_tiled_fn();
+    if (encode == nullptr) return false;
+    const cuuint64_t dims[3] = {(cuuint64_t)b, (cuuint64_t)a, (cuuint64_t)states}, strides[2] = {(cuuint64_t)b * 4, (cuuint64_t)apart * 4};
+    const cuuint32_t box[3] = {kStateBox, (cuuint32_t)(ceil_div(a, kBox) * kBox), 1}, steps[3] = {1, 1, 1};
+    return encode(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, const_cast<float*>(base), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <bool STATES>
+// Shared memory of a CTA: more than half of an SM's, as the tensor memory that a CTA takes is all there is.
+size_t shared_bytes(int a, int b, bool own) { return std::max<size_t>(120 << 10, 1024 + Places(a, b, own).control + sizeof(Control)); }
+static_assert(sizeof(Control) <= 2048, "shared memory for the widest heads");
+
+template <bool STATES, bool OWN>
 cudaError_t launch(const MixParams& prm, const MixMaps& maps, cudaStream_t stream)
 {
     static rps::LaunchState granted;
     size_t bytes = 0;
-    for (int i = 0; i < prm.terms; ++i) bytes = std::max(bytes, shared_bytes(prm.term[i].a, prm.term[i].b));
-    cudaError_t err = rps::grant_smem(granted, rps_mix_tensor_kernel<STATES>, (uint32_t)bytes);
+    for (int i = 0; i < prm.terms; ++i) bytes = std::max(bytes, shared_bytes(prm.term[i].a, prm.term[i].b, OWN));
+    cudaError_t err = rps::grant_smem(granted, rps_mix_tensor_kernel<STATES, OWN>, (uint32_t)bytes);
     if (err != cudaSuccess) return err;
     static std::atomic<int> registers{0};
-    if ((err = check_registers(registers, rps_mix_tensor_kernel<STATES>, kLaunchRegisters)) != cudaSuccess) return err;
-    return launch_after(rps_mix_tensor_kernel<STATES>, dim3((unsigned)(prm.units * prm.segments), (unsigned)prm.terms), kThreads, bytes, stream, 1, prm, maps);
+    if ((err = check_registers(registers, rps_mix_tensor_kernel<STATES, OWN>, kLaunchRegisters)) != cudaSuccess) return err;
+    return launch_after(rps_mix_tensor_kernel<STATES, OWN>, dim3((unsigned)(prm.units * prm.segments), (unsigned)prm.terms), kThreads, bytes, stream, 1, prm, maps);
 }
 
 }  // namespace
@@ -508,8 +645,19 @@ cudaError_t launch_mix_tensor(const MixParams& prm, bool states, cudaStream_t st
         if (!encode(&maps.of[i][0], prm, t.x, t.a) || !encode(&maps.of[i][1], prm, t.y, t.a) || !encode(&maps.of[i][2], prm, t.z, t.b) ||
             !encode(&maps.of[i][3], prm, {t.out, prm.sequences * prm.tokens * prm.heads * t.b, prm.tokens * prm.heads * t.b, (int64_t)prm.heads * t.b, t.b}, t.b))
             return cudaErrorInvalidValue;
+        const bool segmented = prm.segments > 1;
+        const int64_t all = prm.terms * prm.units * prm.segments, each = (int64_t)t.a * t.b;
+        const auto state = [&](int which, bool in_segments, const float* at) {
+            maps.way[i][which] = at == nullptr ? kNoState : in_segments || (t.state_b == 1 && reinterpret_cast<uintptr_t>(at) % 16 == 0) ? kCopied : kByElement;
+            return maps.way[i][which] != kCopied || encode_state(&maps.state[i][which], at, t.a, t.b, in_segments ? all : prm.units, in_segments ? prm.state_room : each);
+        };
+        if (!state(0, segmented, states ? nullptr : segmented ? prm.segment_states : t.state_in) || !state(1, states, states ? prm.segment_states : t.state_out))
+            return cudaErrorInvalidValue;
     }
-    return states ? launch<true>(prm, maps, stream) : launch<false>(prm, maps, stream);
+    // key and value columns are x's and z's in one term or another
+    const bool own = prm.term[0].a <= kBox && prm.term[0].b <= kBox;
+    if (states) return own ? launch<true, true>(prm, maps, stream) : launch<true, false>(prm, maps, stream);
+    return own ? launch<false, true>(prm, maps, stream) : launch<false, false>(prm, maps, stream);
 }
 
 cudaError_t read_mix_gave_up(int* value, cudaStream_t stream) { return read_and_clear(g_gave_up, value, stream); }
