@@ -146,15 +146,42 @@ __device__ __forceinline__ float small_power(float log_decay, int exponent)
     return expf(argument) * (1.0f + fmaf(rate, e, -argument));
 }
 
+// CTAs are placed in their order, and sequences may differ in length: the longest ones first, so that the last places to fall free wait for short ones.
+// (256 heads of sequences of up to 2048 tokens, lengths spread evenly: ...)  Every CTA finds its own: with kMostSorted sequences at most, whose lengths a
+// warp's width of comparisons each sorts in about a microsecond.
+constexpr int kMostSorted = 256;
+
+__device__ __forceinline__ int64_t longest_first(const MixParams& prm, int item, unsigned char* shared)
+{
+    const int sequences = (int)(prm.n * prm.sequences);
+    if (prm.lengths == nullptr || sequences > kMostSorted || sequences == 1) return item;
+    int64_t* const lengths = reinterpret_cast<int64_t*>(shared);
+    int& found = *reinterpret_cast<int*>(lengths + kMostSorted);
+    const int rank = item / prm.heads;
+    if ((int)threadIdx.x < sequences) lengths[threadIdx.x] = __ldg(prm.lengths + threadIdx.x);
+    __syncthreads();
+    if ((int)threadIdx.x < sequences) {
+        const int64_t mine = lengths[threadIdx.x];
+        int before = 0;
+        for (int s = 0; s < sequences; ++s) before += lengths[s] > mine || (lengths[s] == mine && s < (int)threadIdx.x);
+        if (before == rank) found = threadIdx.x;
+    }
+    __syncthreads();
+    const int64_t unit = (int64_t)found * prm.heads + item % prm.heads;
+    __syncthreads();  // the place is used anew
+    return unit;
+}
+
 template <bool STATES, bool OWN>
 __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __grid_constant__ MixParams prm, const __grid_constant__ MixMaps maps)
 {
     after_the_kernel_before();
-    const MixTerm& term = prm.term[blockIdx.y];
-    const int segment = (int)(blockIdx.x % prm.segments);
-    const int64_t unit = blockIdx.x / prm.segments;
+    // the terms of a head of a sequence side by side, as they read the same arrays
+    const int which = (int)(blockIdx.x % prm.terms), item = (int)(blockIdx.x / prm.terms), segment = item % prm.segments;
+    const MixTerm& term = prm.term[which];
     if (STATES && segment + 1 == prm.segments) return;
-    extern __shared__ unsigned char raw[];
+    extern __shared__ __align__(16) unsigned char raw[];
+    const int64_t unit = longest_first(prm, item / prm.segments, raw);
     const uint32_t base = (smem_addr(raw) + 1023) / 1024 * 1024;
     const int a = term.a, b = term.b;
     const Places places(a, b, OWN);
@@ -177,8 +204,8 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
     // U's place: without O's use of tensor memory two take turns, as the next chunk's U does not wait for W there
     const auto u_of = [](int i) { return STATES && (i & 1) ? kAtOut : kAtU; };
     // W before the segment and after it
-    const int64_t slot = (blockIdx.y * prm.units + unit) * prm.segments + segment;
-    const int way_in = maps.way[blockIdx.y][0], way_out = writes_state ? maps.way[blockIdx.y][1] : kNoState;
+    const int64_t slot = (which * prm.units + unit) * prm.segments + segment;
+    const int way_in = maps.way[which][0], way_out = writes_state ? maps.way[which][1] : kNoState;
 
     if (warp == 0 && lane == 0) {
         const auto init = [](uint64_t& bar, int arrivals) { mbar_init(smem_addr(&bar), arrivals); };
@@ -206,7 +233,7 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
 
     bool fine = true;
     const uint64_t limit_ns = prm.wait_limit_ms > 0 ? (uint64_t)prm.wait_limit_ms * 1000000u : rps::kDefaultWaitLimitNs;
-    const auto wait = [&](uint64_t& bar, int turn) { return wait_for(smem_addr(&bar), turn & 1, limit_ns); };  // for the turn-th completion
+    const auto wait = [&](uint64_t& bar, int turn) { return rps::mbar_wait(smem_addr(&bar), turn & 1, limit_ns); };  // for the turn-th completion
     const auto warp_wait = [&](uint64_t& bar, int turn) {
         fine = __all_sync(0xFFFFFFFFu, wait(bar, turn));
         after_sync();
@@ -221,7 +248,7 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
     if (warp < kFirstOut) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kIssueRegisters));
         if (warp == 0 && elect_one()) {
-            const CUtensorMap* map = maps.of[blockIdx.y];
+            const CUtensorMap* map = maps.of[which];
             int issued = 0;
             for (int i = 0; i < count && prm.withhold_copies == 0; ++i) {
                 const int s = i & 1, token = length - kC * (chunks - chunk_at(i));
@@ -271,36 +298,45 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
 #pragma unroll
                         for (int k = 0; k < 4; ++k) multiply<1>(tensor + kAtState, x + c * box + k * along, w + (4 * c + k) * across, of_state, c + k > 0);
                     commit<1>(smem_addr(&control.of_state));
-                    if (!(fine = wait(control.masked, i))) break;
-                    after_sync();
-#pragma unroll 1
-                    for (int c = 0; c < 2; ++c)
-#pragma unroll
-                        for (int k = 0; k < 4; ++k)
-                            multiply_from_tensor(tensor + kAtOut, tensor + kAtP + c * 64 + k * 8, z + (4 * c + k) * across, of_state, c + k > 0);
-                    commit<1>(smem_addr(&control.out_done));
                 }
-                if (updates(i)) {
+                const int parts = !updates(i) ? 0 : third_part ? 3 : 2;
+                // the product for out comes when its left operand is there, as a rule while the last part is on its way
+                const int before_out = OWN ? parts : min(parts, 2);
+                if (parts > 0) {
                     if (!(fine = OWN ? wait(control.parts[s], i >> 1) : wait(control.parts[0], i))) break;
                     after_sync();
-                    const int parts = third_part ? 3 : 2;
+                }
 #pragma unroll 1
-                    for (int p = 0; p < parts; ++p) {
-                        if (!OWN && p == 2) {
-                            commit<1>(smem_addr(&control.parts_used));
-                            if (!(fine = wait(control.last_part, i))) break;
+                for (int p = 0; p <= parts; ++p) {
+                    if (p == before_out) {
+                        if (!OWN && parts == 3) commit<1>(smem_addr(&control.parts_used));
+                        if (parts == before_out && parts > 0) commit<1>(smem_addr(&control.update[s]));
+                        if (!STATES) {
+                            if (!(fine = wait(control.masked, i))) break;
                             after_sync();
+#pragma unroll 1
+                            for (int c = 0; c < 2; ++c)
+#pragma unroll
+                                for (int k = 0; k < 4; ++k)
+                                    multiply_from_tensor(tensor + kAtOut, tensor + kAtP + c * 64 + k * 8, z + (4 * c + k) * across, of_state, c + k > 0);
+                            commit<1>(smem_addr(&control.out_done));
                         }
+                        if (p == parts) break;
+                        if (!(fine = wait(control.last_part, i))) break;
+                        after_sync();
+                    }
+                    if (p < parts) {
                         const uint32_t left = OWN ? rest + (s * 3 + p) * box : p == 0 ? first_part + s * (y_bytes / 16) : rest;
 #pragma unroll 1
                         for (int c = 0; c < 2; ++c)
 #pragma unroll
                             for (int k = 0; k < 4; ++k)
                                 multiply<1>(tensor + u_of(i), left + (4 * c + k) * across, z + (4 * c + k) * across, of_update, p + c + k > 0);
+                    } else {
+                        commit<1>(smem_addr(&control.update[s]));
                     }
-                    if (!fine) break;
-                    commit<1>(smem_addr(&control.update[s]));
                 }
+                if (!fine) break;
                 commit<1>(smem_addr(&control.empty[s]));
             }
         }
@@ -310,7 +346,7 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
                 const int token = length - kC * (chunks - chunk_at(i));
                 if (token >= 0) {  // a copy may not begin ahead of the array
                     const uint32_t from = base + (places.out_in_y ? places.y + (i & 1) * y_bytes : places.out);
-                    for (int c = 0; c < b_boxes; ++c) store_box(from + c * kBoxBytes, maps.of[blockIdx.y] + 3, c * kBox, token, at);
+                    for (int c = 0; c < b_boxes; ++c) store_box(from + c * kBoxBytes, maps.of[which] + 3, c * kBox, token, at);
                     asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                     asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
                 }
@@ -325,12 +361,12 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
                 const uint32_t bar = smem_addr(&control.state_in);
                 mbar_arrive_expect_tx(bar, boxes * box_bytes);
                 const int from = (int)(prm.segments > 1 ? slot : unit);
-                for (int c = 0; c < boxes; ++c) load_state(base + places.part + c * box_bytes, &maps.state[blockIdx.y][0], c * kStateBox, from, bar);
+                for (int c = 0; c < boxes; ++c) load_state(base + places.part + c * box_bytes, &maps.state[which][0], c * kStateBox, from, bar);
                 fine = wait(control.state_in, 0);
             }
             if (way_out == kCopied && (fine = wait(control.state_out, 0) && fine)) {
                 const int to = (int)(STATES ? slot + 1 : unit);
-                for (int c = 0; c < boxes; ++c) store_state(base + places.part + c * box_bytes, &maps.state[blockIdx.y][1], c * kStateBox, to);
+                for (int c = 0; c < boxes; ++c) store_state(base + places.part + c * box_bytes, &maps.state[which][1], c * kStateBox, to);
                 asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                 asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
             }
@@ -622,7 +658,7 @@ cudaError_t launch(const MixParams& prm, const MixMaps& maps, cudaStream_t strea
     if (err != cudaSuccess) return err;
     static std::atomic<int> registers{0};
     if ((err = check_registers(registers, rps_mix_tensor_kernel<STATES, OWN>, kLaunchRegisters)) != cudaSuccess) return err;
-    return launch_after(rps_mix_tensor_kernel<STATES, OWN>, dim3((unsigned)(prm.units * prm.segments), (unsigned)prm.terms), kThreads, bytes, stream, 1, prm, maps);
+    return launch_after(rps_mix_tensor_kernel<STATES, OWN>, dim3((unsigned)(prm.units * prm.segments * prm.terms)), kThreads, bytes, stream, 1, prm, maps);
 }
 
 }  // namespace
