@@ -378,6 +378,12 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
             const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
             const int first_col = half * b_boxes * 32, last_col = min(b, first_col + b_boxes * 32);
             bf16* const out = static_cast<bf16*>(term.out) + ((at.w * prm.sequences + at.sequence) * prm.tokens * prm.heads + at.head) * b;
+            // rows behind the sequence's last token, while the first chunk is on its way
+            const int pieces = b / 8, rows = 32 / pieces;
+            const int64_t t1 = min(prm.tokens, (segment + 1) * prm.segment_tokens);
+            if (lane < rows * pieces)
+                for (int64_t t = max(at.length, segment * prm.segment_tokens) + (warp - kFirstOut) * rows + lane / pieces; t < t1; t += kOutWarps * rows)
+                    *reinterpret_cast<uint4*>(out + t * prm.heads * b + lane % pieces * 8) = make_uint4(0, 0, 0, 0);
             for (int i = 0; i < count; ++i) {
                 const int chunk = chunk_at(i), token = length - kC * (chunks - chunk) + row;
                 if (!warp_wait(control.scores, i)) break;
@@ -449,10 +455,6 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
                 writes_done();
                 warp_arrive(control.staged[i & 1]);
             }
-            // rows behind the sequence's last token
-            const int64_t t1 = min(prm.tokens, (segment + 1) * prm.segment_tokens);
-            for (int64_t t = max(at.length, segment * prm.segment_tokens) + warp - kFirstOut; t < t1 && fine; t += kOutWarps)
-                for (int c = lane * 8; c < b; c += 256) *reinterpret_cast<uint4*>(out + t * prm.heads * b + c) = make_uint4(0, 0, 0, 0);
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kStateRegisters));
