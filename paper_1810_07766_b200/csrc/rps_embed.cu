@@ -4,11 +4,13 @@
 // time and write fp32; here the tokens are sorted by row first (stably, so that a row's sum goes through its tokens in their order),
 // then every run of equal tokens is summed in fp32 registers and its row written once, rounded once.
 //
+//   few    up to kFew tokens of a worker: one launch, whose CTAs each sort all of them and then write their own rows of the gradient, zeros or sums
 //   sort   least significant digit first, 8 bits or fewer a pass; up to kSortHere tokens of a worker stay in one CTA's shared memory, more
-//          go through passes of counting, scanning and scattering
-//   sum    the sorted tokens are cut into tiles of equal length, a warp to a tile and 32 slices of 16 bytes of the columns, so that a
+//          go through passes of counting, scanning and scattering.  Few SMs have work in these; the others clear the gradient meanwhile.
+//   sum    the sorted tokens are cut into tiles of equal length, a warp to a tile and 512 bytes of the columns, so that a
 //          word that every other token is does not make one warp's work; runs that cross tiles leave fp32 parts, which are joined in order
 #include <algorithm>
+#include <type_traits>
 
 #include "rps_kernels.h"
 #include "rps_rows.cuh"
@@ -16,15 +18,51 @@
 namespace rps_ops {
 namespace {
 
+// 16 bytes of a row are a thread's, in pieces of ALIGN bytes: what all rows' addresses are multiples of.  `across` threads side by side take the first
+// pieces, then the second ones, so that any alignment is read and written in whole lines.
+template <typename T, int ALIGN>
+struct Piece {
+    static constexpr int kWidth = 16 / sizeof(T), kEach = ALIGN / sizeof(T), kPieces = 16 / ALIGN;
+    using Word = std::conditional_t<ALIGN == 16, uint4, std::conditional_t<ALIGN == 8, uint2, std::conditional_t<ALIGN == 4, uint32_t, unsigned short>>>;
+    // column of piece j of thread x where the threads' columns begin at `first`
+    static __device__ __forceinline__ int column(int first, int x, int across, int j) { return first + (j * across + x) * kEach; }
+    static __device__ __forceinline__ uint4 load(const T* row, int first, int x, int across, int cols)
+    {
+        union {
+            Word word[kPieces];
+            uint4 all;
+        } v;
+#pragma unroll
+        for (int j = 0; j < kPieces; ++j) {
+            const int c = column(first, x, across, j);
+            v.word[j] = c < cols ? __ldcs(reinterpret_cast<const Word*>(row + c)) : Word{};
+        }
+        return v.all;
+    }
+    static __device__ __forceinline__ void store(T* row, int first, int x, int across, int cols, const uint4& value)
+    {
+        union {
+            Word word[kPieces];
+            uint4 all;
+        } v;
+        v.all = value;
+#pragma unroll
+        for (int j = 0; j < kPieces; ++j) {
+            const int c = column(first, x, across, j);
+            if (c < cols) __stcs(reinterpret_cast<Word*>(row + c), v.word[j]);
+        }
+    }
+};
+
 constexpr int kRowThreads = 256, kRowsAtATime = 4;
 
-// Rows of the table: a thread takes its slices of four tokens at a time, 2^log_across threads to a row.
+// Rows of the table: a thread takes its pieces of four tokens at a time, 2^log_across threads to a row.
 template <typename T, int ALIGN>
 __global__ void __launch_bounds__(kRowThreads) rps_embed_lookup_kernel(const EmbedParams prm, int log_across)
 {
     after_the_kernel_before();
-    constexpr int W = Slice<T>::kWidth;
-    const int across = 1 << log_across, down = kRowThreads >> log_across, D = (int)prm.cols, w = blockIdx.y;
+    using P = Piece<T, ALIGN>;
+    const int across = 1 << log_across, down = kRowThreads >> log_across, D = (int)prm.cols, w = blockIdx.y, x = threadIdx.x & (across - 1);
     const int64_t* tokens = prm.tokens + w * prm.count;
     const T* table = static_cast<const T*>(prm.weight) + w * prm.weight_worker;
     T* out = static_cast<T*>(prm.out) + w * prm.count * prm.cols;
@@ -35,33 +73,49 @@ __global__ void __launch_bounds__(kRowThreads) rps_embed_lookup_kernel(const Emb
         const int64_t t = t0 + i * down;
         token[i] = t < prm.count ? __ldg(tokens + t) : prm.ignore_index;
     }
-    for (int c = (threadIdx.x & (across - 1)) * W; c < D; c += across * W) {
+    for (int c = 0; c < D; c += across * P::kWidth) {
         uint4 slice[kRowsAtATime];
         bool there[kRowsAtATime];
 #pragma unroll
         for (int i = 0; i < kRowsAtATime; ++i) {
             there[i] = token[i] != prm.ignore_index && token[i] >= 0 && token[i] < prm.vocab;
-            slice[i] = load_slice<T, ALIGN, false>(table + (there[i] ? token[i] : 0) * prm.weight_row, c, there[i] ? D : 0);
+            slice[i] = P::load(table + (there[i] ? token[i] : 0) * prm.weight_row, c, x, across, there[i] ? D : 0);
         }
 #pragma unroll
         for (int i = 0; i < kRowsAtATime; ++i) {
             const int64_t t = t0 + i * down;
             if (t >= prm.count) break;
-            float v[W];
+            float v[P::kWidth];
             widen(slice[i], v);
             // a token that names no row gives NaN
             const float factor = there[i] ? prm.scale : token[i] == prm.ignore_index ? 0.0f : __int_as_float(0x7FFFFFFF);
 #pragma unroll
-            for (int j = 0; j < W; ++j) v[j] *= factor;
-            store_slice<T, ALIGN>(out + t * prm.cols, c, D, narrow(v));
+            for (int j = 0; j < P::kWidth; ++j) v[j] *= factor;
+            P::store(out + t * prm.cols, c, x, across, D, narrow(v));
         }
+    }
+}
+
+// Zeros into rows v0 .. v1 - 1 of each worker's gradient, by `threads` of a launch's threads of which this is number `thread`.
+template <typename T, int ALIGN>
+__device__ __forceinline__ void clear_rows(const EmbedParams& prm, int64_t v0, int64_t v1, int64_t thread, int64_t threads)
+{
+    using P = Piece<T, ALIGN>;
+    const int D = (int)prm.cols, warps_across = (D + 32 * P::kWidth - 1) / (32 * P::kWidth), lane = threadIdx.x % 32;
+    const int64_t rows = v1 - v0, items = prm.n * rows * warps_across;
+    if (items <= 0) return;
+    // a warp for 512 bytes of a row
+    for (int64_t item = thread / 32; item < items; item += threads / 32) {
+        const int64_t row = item / warps_across, w = row / rows;
+        T* out = static_cast<T*>(prm.dweight) + w * prm.dweight_worker + (v0 + row - w * rows) * prm.dweight_row;
+        P::store(out, (int)(item - row * warps_across) * 32 * P::kWidth, lane, 32, D, make_uint4(0, 0, 0, 0));
     }
 }
 
 // ---------------------------------------------------------------------------------------------------------------- sort
 constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32, kBins = 256;
-constexpr int kBlockItems = 4;                               // of a thread where several CTAs sort
-constexpr int kSortBlock = kSortThreads * kBlockItems;
+// Items of a thread where several CTAs sort: one, so that many CTAs share them, but of very many tokens 8, as one CTA scans the CTAs' counts.
+constexpr int kManyItems = 8, kMany = 1 << 18;
 constexpr int kMostItems = 16, kSortHere = kSortThreads * kMostItems;
 
 struct SortShared {
@@ -137,16 +191,20 @@ __device__ __forceinline__ void rank_items(SortShared& sh, const uint32_t (&key)
         if (key[i] != kNone) place[i] += sh.of_warp[warp][key[i] >> shift & mask];
 }
 
-// A worker's tokens in one CTA.
-template <int ITEMS>
-__global__ void __launch_bounds__(kSortThreads) rps_embed_sort_kernel(const EmbedParams prm)
+// CTAs of a launch that have no sorting to do clear their share of the gradient: of `launches` launches this is number `launch`.
+template <typename T, int ALIGN>
+__device__ __forceinline__ void clear_meanwhile(const EmbedParams& prm, int sorting, int launch, int launches)
 {
-    after_the_kernel_before();
-    extern __shared__ uint32_t raw[];
-    SortShared& sh = *reinterpret_cast<SortShared*>(raw);
-    uint32_t* keys = raw + sizeof(SortShared) / 4;
-    uint32_t* from = keys + kSortThreads * ITEMS;
-    const int w = blockIdx.x, count = (int)prm.count, lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    if (prm.accumulate) return;
+    clear_rows<T, ALIGN>(prm, prm.vocab * launch / launches, prm.vocab * (launch + 1) / launches, (int64_t)(blockIdx.x - sorting) * kSortThreads + threadIdx.x,
+                         (int64_t)(gridDim.x - sorting) * kSortThreads);
+}
+
+// A worker's tokens sorted in one CTA's shared memory: their rows, and their numbers.
+template <int ITEMS>
+__device__ __forceinline__ void sort_in_shared(const EmbedParams& prm, int w, SortShared& sh, uint32_t* keys, uint32_t* from)
+{
+    const int count = (int)prm.count, lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     const int first = warp * 32 * ITEMS + lane;
     uint32_t key[ITEMS], token[ITEMS], place[ITEMS];
 #pragma unroll
@@ -171,38 +229,54 @@ __global__ void __launch_bounds__(kSortThreads) rps_embed_sort_kernel(const Embe
             if (at < count) key[i] = keys[at], token[i] = from[at];
         }
     }
-#pragma unroll
-    for (int i = 0; i < ITEMS; ++i) {
-        const int at = first + i * 32;
-        if (at < count) prm.keys[0][w * prm.count + at] = key[i], prm.from[0][w * prm.count + at] = token[i];
-    }
+}
+
+// A worker's tokens in one CTA.
+template <int ITEMS, typename T, int ALIGN>
+__global__ void __launch_bounds__(kSortThreads) rps_embed_sort_kernel(const EmbedParams prm)
+{
+    after_the_kernel_before();
+    if ((int)blockIdx.x >= prm.n) return clear_meanwhile<T, ALIGN>(prm, prm.n, 0, 1);
+    extern __shared__ uint32_t raw[];
+    SortShared& sh = *reinterpret_cast<SortShared*>(raw);
+    uint32_t* keys = raw + sizeof(SortShared) / 4;
+    uint32_t* from = keys + kSortThreads * ITEMS;
+    const int w = blockIdx.x;
+    sort_in_shared<ITEMS>(prm, w, sh, keys, from);
+    for (int at = threadIdx.x; at < (int)prm.count; at += kSortThreads) prm.keys[0][w * prm.count + at] = keys[at], prm.from[0][w * prm.count + at] = from[at];
 }
 
 // Several CTAs to a worker: how many items of each digit every block has ([digit][block] of a worker) ...
-__global__ void __launch_bounds__(kSortThreads) rps_embed_count_kernel(const EmbedParams prm, int pass)
+template <int ITEMS, typename T, int ALIGN>
+__global__ void __launch_bounds__(kSortThreads) rps_embed_count_kernel(const EmbedParams prm, int pass, int launches)
 {
     after_the_kernel_before();
     __shared__ uint32_t bins[kBins];
-    const int w = blockIdx.y, shift = pass * prm.digit_bits;
+    const int blocks = (int)prm.sort_blocks, w = blockIdx.x / blocks, block = blockIdx.x - w * blocks;
+    if (w >= prm.n) return clear_meanwhile<T, ALIGN>(prm, prm.n * blocks, 3 * pass, launches);
+    const int shift = pass * prm.digit_bits;
     const uint32_t mask = (1u << prm.digit_bits) - 1;
     if (threadIdx.x < kBins) bins[threadIdx.x] = 0;
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kBlockItems; ++i) {
-        const int64_t t = (int64_t)blockIdx.x * kSortBlock + i * kSortThreads + threadIdx.x;
+    for (int i = 0; i < ITEMS; ++i) {
+        const int64_t t = (int64_t)block * kSortThreads * ITEMS + i * kSortThreads + threadIdx.x;
         if (t >= prm.count) break;
         const uint32_t key = pass == 0 ? sort_key(prm, __ldg(prm.tokens + w * prm.count + t)) : prm.keys[(pass + 1) & 1][w * prm.count + t];
         atomicAdd(&bins[key >> shift & mask], 1u);
     }
     __syncthreads();
-    if (threadIdx.x < kBins) prm.counts[((int64_t)w * kBins + threadIdx.x) * gridDim.x + blockIdx.x] = bins[threadIdx.x];
+    if (threadIdx.x < kBins) prm.counts[((int64_t)w * kBins + threadIdx.x) * blocks + block] = bins[threadIdx.x];
 }
 
 // ... where each block's items of each digit begin (a CTA to a worker) ...
-__global__ void __launch_bounds__(kSortThreads) rps_embed_scan_kernel(const EmbedParams prm, int blocks)
+template <typename T, int ALIGN>
+__global__ void __launch_bounds__(kSortThreads) rps_embed_scan_kernel(const EmbedParams prm, int pass, int launches)
 {
     after_the_kernel_before();
+    if ((int)blockIdx.x >= prm.n) return clear_meanwhile<T, ALIGN>(prm, prm.n, 3 * pass + 1, launches);
     __shared__ uint32_t sums[kSortWarps];
+    const int blocks = (int)prm.sort_blocks;
     uint32_t* counts = prm.counts + (int64_t)blockIdx.x * kBins * blocks;
     const int total = kBins * blocks, lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     uint32_t before = 0;
@@ -237,29 +311,32 @@ __global__ void __launch_bounds__(kSortThreads) rps_embed_scan_kernel(const Embe
 }
 
 // ... and the items moved there.
-__global__ void __launch_bounds__(kSortThreads) rps_embed_scatter_kernel(const EmbedParams prm, int pass)
+template <int ITEMS, typename T, int ALIGN>
+__global__ void __launch_bounds__(kSortThreads) rps_embed_scatter_kernel(const EmbedParams prm, int pass, int launches)
 {
     after_the_kernel_before();
     __shared__ SortShared sh;
-    const int w = blockIdx.y, shift = pass * prm.digit_bits, lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    const int blocks = (int)prm.sort_blocks, w = blockIdx.x / blocks, block = blockIdx.x - w * blocks;
+    if (w >= prm.n) return clear_meanwhile<T, ALIGN>(prm, prm.n * blocks, 3 * pass + 2, launches);
+    const int shift = pass * prm.digit_bits, lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     const uint32_t mask = (1u << prm.digit_bits) - 1;
     const int64_t base = w * prm.count;
-    uint32_t key[kBlockItems], token[kBlockItems], place[kBlockItems];
+    uint32_t key[ITEMS], token[ITEMS], place[ITEMS];
 #pragma unroll
-    for (int i = 0; i < kBlockItems; ++i) {
-        const int64_t t = (int64_t)blockIdx.x * kSortBlock + warp * 32 * kBlockItems + i * 32 + lane;
+    for (int i = 0; i < ITEMS; ++i) {
+        const int64_t t = (int64_t)block * kSortThreads * ITEMS + warp * 32 * ITEMS + i * 32 + lane;
         const bool there = t < prm.count;
         if (pass == 0)
             token[i] = (uint32_t)t, key[i] = there ? sort_key(prm, __ldg(prm.tokens + base + t)) : kNone;
         else
             token[i] = there ? prm.from[(pass + 1) & 1][base + t] : 0, key[i] = there ? prm.keys[(pass + 1) & 1][base + t] : kNone;
     }
-    rank_items<kBlockItems>(sh, key, place, shift, prm.digit_bits);
+    rank_items<ITEMS>(sh, key, place, shift, prm.digit_bits);
 #pragma unroll
-    for (int i = 0; i < kBlockItems; ++i) {
+    for (int i = 0; i < ITEMS; ++i) {
         if (key[i] == kNone) continue;
         const uint32_t digit = key[i] >> shift & mask;
-        const int64_t to = base + prm.counts[((int64_t)w * kBins + digit) * gridDim.x + blockIdx.x] + place[i];
+        const int64_t to = base + prm.counts[((int64_t)w * kBins + digit) * blocks + block] + place[i];
         prm.keys[pass & 1][to] = key[i], prm.from[pass & 1][to] = token[i];
     }
 }
@@ -267,36 +344,39 @@ __global__ void __launch_bounds__(kSortThreads) rps_embed_scatter_kernel(const E
 // ----------------------------------------------------------------------------------------------------------------- sum
 constexpr int kSumWarps = 8;
 
+// 512 bytes of a row of the gradient from column `first` on, a warp's.
 template <typename T, int ALIGN>
-__device__ __forceinline__ void write_row(const EmbedParams& prm, int w, uint32_t row, int c, const float (&sum)[Slice<T>::kWidth])
+__device__ __forceinline__ void write_row(const EmbedParams& prm, int w, uint32_t row, int first, const float (&sum)[Slice<T>::kWidth])
 {
-    constexpr int W = Slice<T>::kWidth;
+    using P = Piece<T, ALIGN>;
     T* out = static_cast<T*>(prm.dweight) + w * prm.dweight_worker + (int64_t)row * prm.dweight_row;
-    float v[W];
+    const int lane = threadIdx.x % 32;
+    float v[P::kWidth];
 #pragma unroll
-    for (int j = 0; j < W; ++j) v[j] = 0.0f;
-    if (prm.accumulate) widen(load_slice<T, ALIGN, false>(out, c, (int)prm.cols), v);
+    for (int j = 0; j < P::kWidth; ++j) v[j] = 0.0f;
+    if (prm.accumulate) widen(P::load(out, first, lane, 32, (int)prm.cols), v);
 #pragma unroll
-    for (int j = 0; j < W; ++j) v[j] = prm.accumulate ? fmaf(prm.scale, sum[j], v[j]) : prm.scale * sum[j];
-    store_slice<T, ALIGN>(out, c, (int)prm.cols, narrow(v));
+    for (int j = 0; j < P::kWidth; ++j) v[j] = prm.accumulate ? fmaf(prm.scale, sum[j], v[j]) : prm.scale * sum[j];
+    P::store(out, first, lane, 32, (int)prm.cols, narrow(v));
 }
 
-// A warp for 32 slices of the columns of a tile of sorted tokens.
+// A warp for 512 bytes of the columns of a tile of sorted tokens.
 template <typename T, int ALIGN>
 __global__ void __launch_bounds__(32 * kSumWarps) rps_embed_sum_kernel(const EmbedParams prm, int slabs)
 {
     after_the_kernel_before();
-    constexpr int W = Slice<T>::kWidth, kAtATime = 8;
+    using P = Piece<T, ALIGN>;
+    constexpr int W = P::kWidth, kAtATime = 8;
     const int lane = threadIdx.x % 32, w = blockIdx.y, D = (int)prm.cols;
     const int64_t item = (int64_t)blockIdx.x * kSumWarps + threadIdx.x / 32;
     const int64_t tile = item / slabs;
     if (tile >= prm.tiles) return;
-    const int c = ((int)(item - tile * slabs) * 32 + lane) * W;
+    const int first = (int)(item - tile * slabs) * 32 * W;
     const uint32_t* keys = prm.keys[prm.sorted] + w * prm.count;
     const uint32_t* from = prm.from[prm.sorted] + w * prm.count;
     const T* dout = static_cast<const T*>(prm.dout) + w * prm.count * prm.cols;
     const int64_t p0 = tile * prm.tile, p1 = min(p0 + prm.tile, prm.count);
-    float* parts = prm.parts + (w * prm.tiles + tile) * 2 * prm.part_row + c;
+    float* parts = prm.parts + (w * prm.tiles + tile) * 2 * prm.part_row + first + lane * W;  // (whatever columns they are)
     uint32_t current = __ldg(keys + p0);
     if (current >= prm.vocab) return;
     bool head = p0 > 0 && __ldg(keys + p0 - 1) == current;  // the run goes on from the tile before
@@ -305,7 +385,6 @@ __global__ void __launch_bounds__(32 * kSumWarps) rps_embed_sum_kernel(const Emb
     for (int j = 0; j < W; ++j) sum[j] = 0.0f;
     const auto store_part = [&](int slot) {
         float* to = parts + slot * prm.part_row;
-        if (c >= D) return;
 #pragma unroll
         for (int j = 0; j < W; j += 4) *reinterpret_cast<float4*>(to + j) = make_float4(sum[j], sum[j + 1], sum[j + 2], sum[j + 3]);
     };
@@ -320,7 +399,7 @@ __global__ void __launch_bounds__(32 * kSumWarps) rps_embed_sum_kernel(const Emb
             for (int i = 0; i < kAtATime; ++i) {
                 key[i] = __shfl_sync(0xFFFFFFFFu, my_key, q + i);
                 const int64_t row = __shfl_sync(0xFFFFFFFFu, my_from, q + i);
-                slice[i] = load_slice<T, ALIGN, true>(dout + row * prm.cols, c, key[i] < prm.vocab ? D : 0);
+                slice[i] = P::load(dout + row * prm.cols, first, lane, 32, key[i] < prm.vocab ? D : 0);
             }
 #pragma unroll
             for (int i = 0; i < kAtATime; ++i) {
@@ -329,7 +408,7 @@ __global__ void __launch_bounds__(32 * kSumWarps) rps_embed_sum_kernel(const Emb
                         if (head)
                             store_part(0);
                         else
-                            write_row<T, ALIGN>(prm, w, current, c, sum);
+                            write_row<T, ALIGN>(prm, w, current, first, sum);
                     }
                     head = false, current = key[i];
 #pragma unroll
@@ -347,7 +426,7 @@ __global__ void __launch_bounds__(32 * kSumWarps) rps_embed_sum_kernel(const Emb
     if (head || on)
         store_part(head ? 0 : 1);
     else
-        write_row<T, ALIGN>(prm, w, current, c, sum);
+        write_row<T, ALIGN>(prm, w, current, first, sum);
 }
 
 // Runs that cross tiles: the warp of the tile that a run begins in adds its parts up.
@@ -356,7 +435,7 @@ __global__ void __launch_bounds__(32 * kSumWarps) rps_embed_join_kernel(const Em
 {
     after_the_kernel_before();
     constexpr int W = Slice<T>::kWidth;
-    const int lane = threadIdx.x % 32, w = blockIdx.y, D = (int)prm.cols;
+    const int lane = threadIdx.x % 32, w = blockIdx.y;
     const int64_t item = (int64_t)blockIdx.x * kSumWarps + threadIdx.x / 32;
     const int64_t tile = item / slabs;
     if (tile + 1 >= prm.tiles) return;
@@ -365,7 +444,7 @@ __global__ void __launch_bounds__(32 * kSumWarps) rps_embed_join_kernel(const Em
     const uint32_t key = __ldg(keys + p1);
     if (key >= prm.vocab || __ldg(keys + p1 - 1) != key) return;                                   // none crosses
     if (__ldg(keys + p0) == key && p0 > 0 && __ldg(keys + p0 - 1) == key) return;                  // it began before
-    const int c = ((int)(item - tile * slabs) * 32 + lane) * W;
+    const int first = (int)(item - tile * slabs) * 32 * W;
     // the run's last tile
     int64_t last = tile + 1;
     while (last + 1 < prm.tiles) {
@@ -376,34 +455,99 @@ __global__ void __launch_bounds__(32 * kSumWarps) rps_embed_join_kernel(const Em
         last += n;
         if (n < 32) break;
     }
-    if (c >= D) return;
     float sum[W];
-    const float* parts = prm.parts + w * prm.tiles * 2 * prm.part_row + c;
-    const auto add = [&](int64_t t, int slot, bool first) {
+    const float* parts = prm.parts + w * prm.tiles * 2 * prm.part_row + first + lane * W;
+    const auto add = [&](int64_t t, int slot, bool start) {
         const float* at = parts + (t * 2 + slot) * prm.part_row;
 #pragma unroll
         for (int j = 0; j < W; j += 4) {
             const float4 v = __ldcg(reinterpret_cast<const float4*>(at + j));
-            sum[j] = first ? v.x : sum[j] + v.x, sum[j + 1] = first ? v.y : sum[j + 1] + v.y;
-            sum[j + 2] = first ? v.z : sum[j + 2] + v.z, sum[j + 3] = first ? v.w : sum[j + 3] + v.w;
+            sum[j] = start ? v.x : sum[j] + v.x, sum[j + 1] = start ? v.y : sum[j + 1] + v.y;
+            sum[j + 2] = start ? v.z : sum[j + 2] + v.z, sum[j + 3] = start ? v.w : sum[j + 3] + v.w;
         }
     };
     add(tile, 1, true);
 #pragma unroll 8
     for (int64_t t = tile + 1; t <= last; ++t) add(t, 0, false);
-    write_row<T, ALIGN>(prm, w, key, c, sum);
+    write_row<T, ALIGN>(prm, w, key, first, sum);
 }
 
-// Zeros into the rows of the gradient.
+// ----------------------------------------------------------------------------------------------------------------- few
+// All in one launch: every CTA sorts its worker's tokens and takes rows v0 .. v1 - 1 of the gradient (or, where it is added to, a share of the
+// runs), a warp to 512 bytes of a row.
+constexpr int kFew = 512, kFewRows = 4096;
+
 template <typename T, int ALIGN>
-__global__ void __launch_bounds__(kRowThreads) rps_embed_clear_kernel(const EmbedParams prm, int log_across)
+__global__ void __launch_bounds__(kSortThreads) rps_embed_few_kernel(const EmbedParams prm, int slabs)
 {
     after_the_kernel_before();
-    constexpr int W = Slice<T>::kWidth;
-    const int across = 1 << log_across, down = kRowThreads >> log_across, D = (int)prm.cols;
-    T* out = static_cast<T*>(prm.dweight) + blockIdx.y * prm.dweight_worker;
-    for (int64_t v = (int64_t)blockIdx.x * down + (threadIdx.x >> log_across); v < prm.vocab; v += (int64_t)gridDim.x * down)
-        for (int c = (threadIdx.x & (across - 1)) * W; c < D; c += across * W) store_slice<T, ALIGN>(out + v * prm.dweight_row, c, D, make_uint4(0, 0, 0, 0));
+    using P = Piece<T, ALIGN>;
+    constexpr int W = P::kWidth, kAtATime = 8;
+    __shared__ union {
+        SortShared sort;
+        unsigned short start[kFewRows];  // of a row's run, kFew: none
+    } sh;
+    __shared__ uint32_t keys[kSortThreads], from[kSortThreads];
+    const int w = blockIdx.y, count = (int)prm.count, lane = threadIdx.x % 32, warp = threadIdx.x / 32, D = (int)prm.cols;
+    sort_in_shared<1>(prm, w, sh.sort, keys, from);
+    const T* dout = static_cast<const T*>(prm.dout) + w * prm.count * prm.cols;
+    const auto sum_run = [&](int p, int first) {
+        const uint32_t row = keys[p];
+        float sum[W];
+#pragma unroll
+        for (int j = 0; j < W; ++j) sum[j] = 0.0f;
+        for (bool on = true; on;) {
+            uint4 slice[kAtATime];
+#pragma unroll
+            for (int i = 0; i < kAtATime; ++i, ++p) {
+                on = on && p < count && keys[p] == row;
+                slice[i] = P::load(dout + (on ? (int64_t)from[p] : 0) * prm.cols, first, lane, 32, on ? D : 0);
+            }
+#pragma unroll
+            for (int i = 0; i < kAtATime; ++i) {
+                float v[W];
+                widen(slice[i], v);
+#pragma unroll
+                for (int j = 0; j < W; ++j) sum[j] += v[j];
+            }
+        }
+        write_row<T, ALIGN>(prm, w, row, first, sum);
+    };
+    if (prm.accumulate) {
+        __syncthreads();
+        for (int item = blockIdx.x * kSortWarps + warp; item < count * slabs; item += gridDim.x * kSortWarps) {
+            const int p = item / slabs;
+            if (keys[p] < prm.vocab && (p == 0 || keys[p - 1] != keys[p])) sum_run(p, (item - p * slabs) * 32 * W);
+        }
+        return;
+    }
+    const int64_t v0 = prm.vocab * blockIdx.x / gridDim.x, v1 = prm.vocab * (blockIdx.x + 1) / gridDim.x;
+    for (int64_t v = v0; v < v1; v += kFewRows) {
+        const int rows = (int)min((int64_t)kFewRows, v1 - v);
+        __syncthreads();
+        for (int i = threadIdx.x; i < rows; i += kSortThreads) sh.start[i] = kFew;
+        __syncthreads();
+        if ((int)threadIdx.x < count) {
+            const int p = threadIdx.x;
+            const int64_t row = (int64_t)keys[p] - v;
+            if (row >= 0 && row < rows && (p == 0 || keys[p - 1] != keys[p])) sh.start[row] = (unsigned short)p;
+        }
+        __syncthreads();
+        for (int64_t item = warp; item < (int64_t)rows * slabs; item += kSortWarps) {
+            const int row = (int)(item / slabs), first = (int)(item - (int64_t)row * slabs) * 32 * W, p = sh.start[row];
+            if (p < kFew)
+                sum_run(p, first);
+            else
+                P::store(static_cast<T*>(prm.dweight) + w * prm.dweight_worker + (v + row) * prm.dweight_row, first, lane, 32, D, make_uint4(0, 0, 0, 0));
+        }
+    }
+}
+
+template <typename T, int ALIGN>
+__global__ void __launch_bounds__(kSortThreads) rps_embed_clear_kernel(const EmbedParams prm)
+{
+    after_the_kernel_before();
+    clear_meanwhile<T, ALIGN>(prm, 0, 0, 1);
 }
 
 // ---------------------------------------------------------------------------------------------------------------- host
@@ -414,62 +558,92 @@ int log_threads_across(int64_t cols, int width)
     return log;
 }
 
+// Bytes that every row's address is a multiple of, and its length.
 template <typename T>
+int row_alignment(const void* p, int64_t cols, int64_t row, int64_t worker)
+{
+    const uint64_t bits = reinterpret_cast<uintptr_t>(p) | (uint64_t)(cols | row | worker) * sizeof(T);
+    return bits % 16 == 0 ? 16 : bits % 8 == 0 ? 8 : bits % 4 == 0 ? 4 : 2;
+}
+
+template <typename T, int ALIGN>
 cudaError_t lookup(const EmbedParams& prm, cudaStream_t stream)
 {
     const int log = log_threads_across(prm.cols, Slice<T>::kWidth);
-    const int align = std::min({alignment<T>(prm.weight, prm.cols, prm.weight_row), alignment<T>(prm.weight, prm.cols, prm.weight_worker),
-                                alignment<T>(prm.out, prm.cols, prm.cols)});
     const dim3 grid((unsigned)ceil_div(prm.count, (kRowThreads >> log) * kRowsAtATime), (unsigned)prm.n);
-    const auto kernel = align == 16 ? rps_embed_lookup_kernel<T, 16> : align == 4 ? rps_embed_lookup_kernel<T, 4> : rps_embed_lookup_kernel<T, sizeof(T)>;
-    return launch_after(kernel, grid, kRowThreads, 0, stream, 1, prm, log);
+    return launch_after(rps_embed_lookup_kernel<T, ALIGN>, grid, kRowThreads, 0, stream, 1, prm, log);
 }
 
-template <int ITEMS>
+// CTAs that clear beside those that sort.
+unsigned with_clearing(const EmbedParams& prm, int64_t sorting) { return (unsigned)(sorting + (prm.accumulate ? 0 : std::max<int64_t>(kSms - sorting, kSms / 2))); }
+
+template <int ITEMS, typename T, int ALIGN>
 cudaError_t sort_here(const EmbedParams& prm, cudaStream_t stream)
 {
     static rps::LaunchState state;
     const uint32_t bytes = sizeof(SortShared) + kSortThreads * ITEMS * 8;
-    const cudaError_t err = rps::grant_smem(state, rps_embed_sort_kernel<ITEMS>, bytes);
+    const cudaError_t err = rps::grant_smem(state, rps_embed_sort_kernel<ITEMS, T, ALIGN>, bytes);
     if (err != cudaSuccess) return err;
-    return launch_after(rps_embed_sort_kernel<ITEMS>, dim3((unsigned)prm.n), kSortThreads, bytes, stream, 1, prm);
+    return launch_after(rps_embed_sort_kernel<ITEMS, T, ALIGN>, dim3(with_clearing(prm, prm.n)), kSortThreads, bytes, stream, 1, prm);
 }
 
-cudaError_t sort(const EmbedParams& prm, cudaStream_t stream)
+template <int ITEMS, typename T, int ALIGN>
+cudaError_t sort_in_passes(const EmbedParams& prm, cudaStream_t stream)
 {
-    if (prm.count <= kSortThreads) return sort_here<1>(prm, stream);
-    if (prm.count <= kSortThreads * 4) return sort_here<4>(prm, stream);
-    if (prm.count <= kSortHere) return sort_here<kMostItems>(prm, stream);
-    const dim3 grid((unsigned)ceil_div(prm.count, kSortBlock), (unsigned)prm.n);
+    const int passes = (int)ceil_div(prm.key_bits, prm.digit_bits);
+    const dim3 grid(with_clearing(prm, prm.n * prm.sort_blocks)), scan(with_clearing(prm, prm.n));
     cudaError_t err = cudaSuccess;
-    for (int pass = 0; pass * prm.digit_bits < prm.key_bits && err == cudaSuccess; ++pass) {
-        err = launch_after(rps_embed_count_kernel, grid, kSortThreads, 0, stream, 1, prm, pass);
-        if (err == cudaSuccess) err = launch_after(rps_embed_scan_kernel, dim3((unsigned)prm.n), kSortThreads, 0, stream, 1, prm, (int)grid.x);
-        if (err == cudaSuccess) err = launch_after(rps_embed_scatter_kernel, grid, kSortThreads, 0, stream, 1, prm, pass);
+    for (int pass = 0; pass < passes && err == cudaSuccess; ++pass) {
+        err = launch_after(rps_embed_count_kernel<ITEMS, T, ALIGN>, grid, kSortThreads, 0, stream, 1, prm, pass, 3 * passes);
+        if (err == cudaSuccess) err = launch_after(rps_embed_scan_kernel<T, ALIGN>, scan, kSortThreads, 0, stream, 1, prm, pass, 3 * passes);
+        if (err == cudaSuccess) err = launch_after(rps_embed_scatter_kernel<ITEMS, T, ALIGN>, grid, kSortThreads, 0, stream, 1, prm, pass, 3 * passes);
     }
     return err;
 }
 
-template <typename T>
+template <typename T, int ALIGN>
+cudaError_t sort(const EmbedParams& prm, cudaStream_t stream)
+{
+    if (prm.count <= kSortThreads) return sort_here<1, T, ALIGN>(prm, stream);
+    if (prm.count <= kSortThreads * 4) return sort_here<4, T, ALIGN>(prm, stream);
+    if (prm.count <= kSortHere) return sort_here<kMostItems, T, ALIGN>(prm, stream);
+    return prm.count <= kMany ? sort_in_passes<1, T, ALIGN>(prm, stream) : sort_in_passes<kManyItems, T, ALIGN>(prm, stream);
+}
+
+template <typename T, int ALIGN>
 cudaError_t gradient(const EmbedParams& prm, cudaStream_t stream)
 {
-    cudaError_t err = cudaSuccess;
-    const int out_align = std::min(alignment<T>(prm.dweight, prm.cols, prm.dweight_row), alignment<T>(prm.dweight, prm.cols, prm.dweight_worker));
-    if (!prm.accumulate) {
-        const int log = log_threads_across(prm.cols, Slice<T>::kWidth);
-        const dim3 grid((unsigned)std::min<int64_t>(ceil_div(prm.vocab, kRowThreads >> log), ceil_div((int64_t)kSms * 8, prm.n)), (unsigned)prm.n);
-        const auto kernel = out_align == 16 ? rps_embed_clear_kernel<T, 16> : out_align == 4 ? rps_embed_clear_kernel<T, 4> : rps_embed_clear_kernel<T, sizeof(T)>;
-        if ((err = launch_after(kernel, grid, kRowThreads, 0, stream, 1, prm, log)) != cudaSuccess) return err;
-    }
-    if (prm.count == 0) return cudaSuccess;
-    if ((err = sort(prm, stream)) != cudaSuccess) return err;
-    const int align = std::min(out_align, alignment<T>(prm.dout, prm.cols, prm.cols));
     const int slabs = (int)ceil_div(prm.cols, 32 * Slice<T>::kWidth);
+    if (prm.count == 0) {
+        if (prm.accumulate) return cudaSuccess;
+        return launch_after(rps_embed_clear_kernel<T, ALIGN>, dim3(2 * kSms), kSortThreads, 0, stream, 1, prm);
+    }
+    if (prm.count <= kFew) {
+        const int64_t items = prm.accumulate ? prm.count * slabs : prm.vocab * slabs;
+        const int64_t ctas = std::max<int64_t>(1, std::min(ceil_div(items, kSortWarps), ceil_div((int64_t)2 * kSms, prm.n)));
+        return launch_after(rps_embed_few_kernel<T, ALIGN>, dim3((unsigned)ctas, (unsigned)prm.n), kSortThreads, 0, stream, 1, prm, slabs);
+    }
+    cudaError_t err = sort<T, ALIGN>(prm, stream);
+    if (err != cudaSuccess) return err;
     const dim3 grid((unsigned)ceil_div(prm.tiles * slabs, kSumWarps), (unsigned)prm.n);
-    const auto kernel = align == 16 ? rps_embed_sum_kernel<T, 16> : align == 4 ? rps_embed_sum_kernel<T, 4> : rps_embed_sum_kernel<T, sizeof(T)>;
-    if ((err = launch_after(kernel, grid, 32 * kSumWarps, 0, stream, 1, prm, slabs)) != cudaSuccess || prm.tiles == 1) return err;
-    const auto join = align == 16 ? rps_embed_join_kernel<T, 16> : align == 4 ? rps_embed_join_kernel<T, 4> : rps_embed_join_kernel<T, sizeof(T)>;
-    return launch_after(join, grid, 32 * kSumWarps, 0, stream, 1, prm, slabs);
+    if ((err = launch_after(rps_embed_sum_kernel<T, ALIGN>, grid, 32 * kSumWarps, 0, stream, 1, prm, slabs)) != cudaSuccess || prm.tiles == 1) return err;
+    return launch_after(rps_embed_join_kernel<T, ALIGN>, grid, 32 * kSumWarps, 0, stream, 1, prm, slabs);
+}
+
+// The kernels for rows of this alignment.
+#define RPS_BY_ALIGNMENT(function, align)                                                                        \
+    (prm.f32 ? ((align) == 16  ? function<float, 16>(prm, stream)                                                \
+                : (align) == 8 ? function<float, 8>(prm, stream)                                                 \
+                               : function<float, 4>(prm, stream))                                                \
+             : ((align) == 16  ? function<bf16, 16>(prm, stream)                                                 \
+                : (align) == 8 ? function<bf16, 8>(prm, stream)                                                  \
+                : (align) == 4 ? function<bf16, 4>(prm, stream)                                                  \
+                               : function<bf16, 2>(prm, stream)))
+
+int alignment_of(const EmbedParams& prm, const void* dense, const void* rows, int64_t row, int64_t worker)
+{
+    return prm.f32 ? std::min(row_alignment<float>(dense, prm.cols, 0, 0), row_alignment<float>(rows, prm.cols, row, worker))
+                   : std::min(row_alignment<bf16>(dense, prm.cols, 0, 0), row_alignment<bf16>(rows, prm.cols, row, worker));
 }
 
 }  // namespace
@@ -482,18 +656,26 @@ void plan_embed(EmbedParams* prm)
     const int passes = (int)ceil_div(p.key_bits, 8);
     p.digit_bits = (int)ceil_div(p.key_bits, passes);
     p.sorted = p.count <= kSortHere ? 0 : (passes - 1) & 1;
-    p.sort_blocks = p.count <= kSortHere ? 0 : ceil_div(p.count, kSortBlock);
+    p.sort_blocks = p.count <= kSortHere ? 0 : ceil_div(p.count, kSortThreads * (p.count <= kMany ? 1 : kManyItems));
     const int width = p.f32 ? Slice<float>::kWidth : Slice<bf16>::kWidth;
     const int64_t slabs = ceil_div(p.cols, 32 * width);
     // long tiles leave fewer parts, short ones more warps
     p.tile = 256;
     while (p.tile > 16 && p.n * ceil_div(p.count, p.tile) * slabs < kSms * 24) p.tile /= 2;
-    p.tiles = ceil_div(p.count, p.tile);
+    p.tiles = p.count <= kFew ? 1 : ceil_div(p.count, p.tile);
     p.part_row = slabs * 32 * width;
 }
 
-cudaError_t launch_embed_lookup(const EmbedParams& prm, cudaStream_t stream) { return prm.f32 ? lookup<float>(prm, stream) : lookup<bf16>(prm, stream); }
+cudaError_t launch_embed_lookup(const EmbedParams& prm, cudaStream_t stream)
+{
+    const int align = alignment_of(prm, prm.out, prm.weight, prm.weight_row, prm.weight_worker);
+    return RPS_BY_ALIGNMENT(lookup, align);
+}
 
-cudaError_t launch_embed_gradient(const EmbedParams& prm, cudaStream_t stream) { return prm.f32 ? gradient<float>(prm, stream) : gradient<bf16>(prm, stream); }
+cudaError_t launch_embed_gradient(const EmbedParams& prm, cudaStream_t stream)
+{
+    const int align = alignment_of(prm, prm.dout, prm.dweight, prm.dweight_row, prm.dweight_worker);
+    return RPS_BY_ALIGNMENT(gradient, align);
+}
 
 }  // namespace rps_ops
