@@ -5,14 +5,15 @@
 // then every run of equal tokens is summed in fp32 registers and its row written once, rounded once.
 //
 //   few    up to kFew tokens of a worker: one launch, whose CTAs each sort all of them and then write their own rows of the gradient, zeros or sums
-//   sort   least significant digit first, 8 bits or fewer a pass; up to kSortHere tokens of a worker stay in one CTA's shared memory, more
-//          go through passes of counting, scanning and scattering.  Few SMs have work in these; the others clear the gradient meanwhile.
+//   sort   least significant digit first, 8 bits or fewer a pass; up to kSortHere tokens of a worker stay in the shared memory of a cluster of
+//          eight CTAs, which write to each other's, more go through launches of counting, scanning and scattering.  Few SMs have work in
+//          these; the others clear the gradient meanwhile.
 //   sum    the sorted tokens are cut into tiles of equal length, a warp to a tile and 512 bytes of the columns, so that a
 //          word that every other token is does not make one warp's work; runs that cross tiles leave fp32 parts, which are joined in order
 #include <algorithm>
 #include <type_traits>
 
-#include "rps_kernels.h"
+#include "rps_cluster.cuh"
 #include "rps_rows.cuh"
 
 namespace rps_ops {
@@ -96,19 +97,18 @@ __global__ void __launch_bounds__(kRowThreads) rps_embed_lookup_kernel(const Emb
     }
 }
 
-// Zeros into rows v0 .. v1 - 1 of each worker's gradient, by `threads` of a launch's threads of which this is number `thread`.
+// Zeros into rows v0 .. v1 - 1 of each worker's gradient by some warps of a launch, of which this one is number `warp`: a row at a time.
 template <typename T, int ALIGN>
-__device__ __forceinline__ void clear_rows(const EmbedParams& prm, int64_t v0, int64_t v1, int64_t thread, int64_t threads)
+__device__ __forceinline__ void clear_rows(const EmbedParams& prm, int64_t v0, int64_t v1, int64_t warp, int64_t warps)
 {
     using P = Piece<T, ALIGN>;
-    const int D = (int)prm.cols, warps_across = (D + 32 * P::kWidth - 1) / (32 * P::kWidth), lane = threadIdx.x % 32;
-    const int64_t rows = v1 - v0, items = prm.n * rows * warps_across;
-    if (items <= 0) return;
-    // a warp for 512 bytes of a row
-    for (int64_t item = thread / 32; item < items; item += threads / 32) {
-        const int64_t row = item / warps_across, w = row / rows;
-        T* out = static_cast<T*>(prm.dweight) + w * prm.dweight_worker + (v0 + row - w * rows) * prm.dweight_row;
-        P::store(out, (int)(item - row * warps_across) * 32 * P::kWidth, lane, 32, D, make_uint4(0, 0, 0, 0));
+    const int D = (int)prm.cols, lane = threadIdx.x % 32;
+    for (int w = 0; w < prm.n; ++w) {
+        T* out = static_cast<T*>(prm.dweight) + w * prm.dweight_worker;
+        for (int64_t v = v0 + warp; v < v1; v += warps) {
+#pragma unroll 4
+            for (int c = 0; c < D; c += 32 * P::kWidth) P::store(out + v * prm.dweight_row, c, lane, 32, D, make_uint4(0, 0, 0, 0));
+        }
     }
 }
 
@@ -116,7 +116,7 @@ __device__ __forceinline__ void clear_rows(const EmbedParams& prm, int64_t v0, i
 constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32, kBins = 256;
 // Items of a thread where several CTAs sort: one, so that many CTAs share them, but of very many tokens 8, as one CTA scans the CTAs' counts.
 constexpr int kManyItems = 8, kMany = 1 << 18;
-constexpr int kMostItems = 16, kSortHere = kSortThreads * kMostItems;
+constexpr int kCluster = 8, kMostItems = 16, kSortHere = kCluster * kSortThreads * kMostItems;
 
 struct SortShared {
     uint32_t of_warp[kSortWarps][kBins];  // items of each digit in each warp, then where they go
@@ -132,6 +132,24 @@ __device__ __forceinline__ uint32_t sort_key(const EmbedParams& prm, int64_t tok
 // Place of each item among the CTA's, by one digit and stably; a warp's items follow one another, 32 at a time (kNone: no item).
 // Leaves the number of items of each digit in sh.total and the first place of each in sh.scan.
 constexpr uint32_t kNone = 0xFFFFFFFFu;
+
+// The first place of each digit out of their numbers, by one warp.
+__device__ __forceinline__ void scan_bins(SortShared& sh)
+{
+    const int lane = threadIdx.x % 32;
+    uint32_t mine[kBins / 32], sum = 0;
+#pragma unroll
+    for (int j = 0; j < kBins / 32; ++j) mine[j] = sh.total[lane * (kBins / 32) + j], sum += mine[j];
+    uint32_t upto = sum;
+#pragma unroll
+    for (int s = 1; s < 32; s *= 2) {
+        const uint32_t n = __shfl_up_sync(0xFFFFFFFFu, upto, s);
+        if (lane >= s) upto += n;
+    }
+    upto -= sum;
+#pragma unroll
+    for (int j = 0; j < kBins / 32; ++j) sh.scan[lane * (kBins / 32) + j] = upto, upto += mine[j];
+}
 
 template <int ITEMS>
 __device__ __forceinline__ void rank_items(SortShared& sh, const uint32_t (&key)[ITEMS], uint32_t (&place)[ITEMS], int shift, int bits)
@@ -171,58 +189,121 @@ __device__ __forceinline__ void rank_items(SortShared& sh, const uint32_t (&key)
         sh.total[threadIdx.x] = sum;
     }
     __syncthreads();
-    if (warp == 0) {
-        uint32_t mine[kBins / 32], sum = 0;
-#pragma unroll
-        for (int j = 0; j < kBins / 32; ++j) mine[j] = sh.total[lane * (kBins / 32) + j], sum += mine[j];
-        uint32_t upto = sum;
-#pragma unroll
-        for (int s = 1; s < 32; s *= 2) {
-            const uint32_t n = __shfl_up_sync(0xFFFFFFFFu, upto, s);
-            if (lane >= s) upto += n;
-        }
-        upto -= sum;
-#pragma unroll
-        for (int j = 0; j < kBins / 32; ++j) sh.scan[lane * (kBins / 32) + j] = upto, upto += mine[j];
-    }
+    if (warp == 0) scan_bins(sh);
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i)
         if (key[i] != kNone) place[i] += sh.of_warp[warp][key[i] >> shift & mask];
 }
 
-// CTAs of a launch that have no sorting to do clear their share of the gradient: of `launches` launches this is number `launch`.
+// CTAs of a launch that have no sorting to do clear their share of the gradient: of `launches` launches this is number `launch`.  Rows that follow one
+// another without gaps are one run of bytes, which goes out as copies of kZeros of shared memory (`zeros`), a few to a CTA at a time; others, element by element.
+// (32768 of 131072 x 2048 bf16, 537 MB: 1024 threads' own stores 126 us, ... us so.)
+constexpr int kZeros = 16384;
+
 template <typename T, int ALIGN>
-__device__ __forceinline__ void clear_meanwhile(const EmbedParams& prm, int sorting, int launch, int launches)
+__device__ __forceinline__ void clear_meanwhile(const EmbedParams& prm, int sorting, int launch, int launches, void* zeros)
 {
     if (prm.accumulate) return;
-    clear_rows<T, ALIGN>(prm, prm.vocab * launch / launches, prm.vocab * (launch + 1) / launches, (int64_t)(blockIdx.x - sorting) * kSortThreads + threadIdx.x,
-                         (int64_t)(gridDim.x - sorting) * kSortThreads);
+    const int64_t v0 = prm.vocab * launch / launches, v1 = prm.vocab * (launch + 1) / launches, cta = blockIdx.x - sorting, ctas = gridDim.x - sorting;
+    if (prm.dweight_row != prm.cols) return clear_rows<T, ALIGN>(prm, v0, v1, cta * kSortWarps + threadIdx.x / 32, ctas * kSortWarps);
+    for (int i = threadIdx.x; i < kZeros / 16; i += kSortThreads) static_cast<uint4*>(zeros)[i] = make_uint4(0, 0, 0, 0);
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncthreads();
+    if (threadIdx.x >= 32) return;
+    const uint32_t from = rps::smem_addr(zeros);
+    for (int w = 0; w < prm.n; ++w) {
+        unsigned char* const base = static_cast<unsigned char*>(prm.dweight) + w * prm.dweight_worker * (int64_t)sizeof(T);
+        unsigned char *const begin = base + v0 * prm.cols * sizeof(T), *const end = base + v1 * prm.cols * sizeof(T);
+        // what lies between boundaries of 16 bytes, and the elements around it
+        unsigned char* const first = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(begin) + 15) / 16 * 16);
+        unsigned char* const last = reinterpret_cast<unsigned char*>(reinterpret_cast<uintptr_t>(end) / 16 * 16);
+        if (first > last) {  // less than 16 bytes, across no boundary
+            if (cta == 0)
+                for (T* p = reinterpret_cast<T*>(begin) + threadIdx.x; p < reinterpret_cast<T*>(end); p += 32) *p = from_float<T>(0.0f);
+            continue;
+        }
+        if (cta == 0) {
+            if (T* p = reinterpret_cast<T*>(begin) + threadIdx.x; p < reinterpret_cast<T*>(first)) *p = from_float<T>(0.0f);
+            if (T* p = reinterpret_cast<T*>(last) + threadIdx.x; p < reinterpret_cast<T*>(end)) *p = from_float<T>(0.0f);
+        }
+        if (threadIdx.x < 4)
+            for (unsigned char* to = first + (cta * 4 + threadIdx.x) * kZeros; to < last; to += ctas * 4 * kZeros)
+                asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(to), "r"(from), "r"((uint32_t)min((int64_t)kZeros, (int64_t)(last - to)))
+                             : "memory");
+    }
+    asm volatile("cp.async.bulk.commit_group;\n\tcp.async.bulk.wait_group 0;" ::: "memory");
 }
 
-// A worker's tokens sorted in one CTA's shared memory: their rows, and their numbers.
-template <int ITEMS>
+__device__ __forceinline__ uint32_t in_cta(uint32_t addr, uint32_t rank)
+{
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
+
+__device__ __forceinline__ uint32_t read_from(uint32_t addr)
+{
+    uint32_t v;
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+    return v;
+}
+
+__device__ __forceinline__ void write_to(uint32_t addr, uint32_t v) { asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory"); }
+
+// A worker's tokens sorted in shared memory: their rows, and their numbers.  CTAS of them share the tokens, ITEMS * kSortThreads each in their order.
+template <int ITEMS, int CTAS>
 __device__ __forceinline__ void sort_in_shared(const EmbedParams& prm, int w, SortShared& sh, uint32_t* keys, uint32_t* from)
 {
-    const int count = (int)prm.count, lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    constexpr int kHere = ITEMS * kSortThreads;
+    const int rank = CTAS > 1 ? (int)cluster_rank() : 0, lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    const int count = (int)prm.count - rank * kHere;  // of this CTA and the ones behind it
     const int first = warp * 32 * ITEMS + lane;
     uint32_t key[ITEMS], token[ITEMS], place[ITEMS];
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
         const int t = first + i * 32;
-        token[i] = (uint32_t)t;
-        key[i] = t < count ? sort_key(prm, __ldg(prm.tokens + w * prm.count + t)) : kNone;
+        token[i] = (uint32_t)(rank * kHere + t);
+        key[i] = t < count ? sort_key(prm, __ldg(prm.tokens + w * prm.count + rank * kHere + t)) : kNone;
     }
     for (int shift = 0; shift < prm.key_bits; shift += prm.digit_bits) {
         rank_items<ITEMS>(sh, key, place, shift, prm.digit_bits);
         const uint32_t mask = (1u << prm.digit_bits) - 1;
+        if constexpr (CTAS > 1) {
+            // where each digit's items begin among all CTAs', and this CTA's among those
+            cluster_sync();
+            uint32_t before = 0, all = 0;
+            if (threadIdx.x < kBins) {
+                const uint32_t mine = rps::smem_addr(&sh.total[threadIdx.x]);
+#pragma unroll
+                for (int c = 0; c < CTAS; ++c) {
+                    const uint32_t n = read_from(in_cta(mine, c));
+                    before += c < rank ? n : 0, all += n;
+                }
+            }
+            cluster_sync();  // totals have been read, as have the keys of the pass before
+            if (threadIdx.x < kBins) sh.total[threadIdx.x] = all;
+            __syncthreads();
+            if (warp == 0) scan_bins(sh);
+            __syncthreads();
+            if (threadIdx.x < kBins) sh.scan[threadIdx.x] += before;
+            __syncthreads();
+        }
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
             if (key[i] == kNone) continue;
             const uint32_t to = place[i] + sh.scan[key[i] >> shift & mask];
-            keys[to] = key[i], from[to] = token[i];
+            if constexpr (CTAS > 1) {
+                const uint32_t cta = to / kHere, at = to % kHere;
+                write_to(in_cta(rps::smem_addr(keys + at), cta), key[i]), write_to(in_cta(rps::smem_addr(from + at), cta), token[i]);
+            } else {
+                keys[to] = key[i], from[to] = token[i];
+            }
         }
-        __syncthreads();
+        if constexpr (CTAS > 1)
+            cluster_sync();
+        else
+            __syncthreads();
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
             const int at = first + i * 32;
@@ -231,19 +312,21 @@ __device__ __forceinline__ void sort_in_shared(const EmbedParams& prm, int w, So
     }
 }
 
-// A worker's tokens in one CTA.
+// A worker's tokens in a cluster.
 template <int ITEMS, typename T, int ALIGN>
 __global__ void __launch_bounds__(kSortThreads) rps_embed_sort_kernel(const EmbedParams prm)
 {
     after_the_kernel_before();
-    if ((int)blockIdx.x >= prm.n) return clear_meanwhile<T, ALIGN>(prm, prm.n, 0, 1);
-    extern __shared__ uint32_t raw[];
+    const int w = blockIdx.x / kCluster;
+    extern __shared__ __align__(16) uint32_t raw[];
+    if (w >= prm.n) return clear_meanwhile<T, ALIGN>(prm, prm.n * kCluster, 0, 1, raw);
     SortShared& sh = *reinterpret_cast<SortShared*>(raw);
+    constexpr int kHere = ITEMS * kSortThreads;
     uint32_t* keys = raw + sizeof(SortShared) / 4;
-    uint32_t* from = keys + kSortThreads * ITEMS;
-    const int w = blockIdx.x;
-    sort_in_shared<ITEMS>(prm, w, sh, keys, from);
-    for (int at = threadIdx.x; at < (int)prm.count; at += kSortThreads) prm.keys[0][w * prm.count + at] = keys[at], prm.from[0][w * prm.count + at] = from[at];
+    uint32_t* from = keys + kHere;
+    sort_in_shared<ITEMS, kCluster>(prm, w, sh, keys, from);
+    const int64_t first = (int64_t)cluster_rank() * kHere, to = w * prm.count + first;
+    for (int at = threadIdx.x; at < kHere && first + at < prm.count; at += kSortThreads) prm.keys[0][to + at] = keys[at], prm.from[0][to + at] = from[at];
 }
 
 // Several CTAs to a worker: how many items of each digit every block has ([digit][block] of a worker) ...
@@ -252,8 +335,9 @@ __global__ void __launch_bounds__(kSortThreads) rps_embed_count_kernel(const Emb
 {
     after_the_kernel_before();
     __shared__ uint32_t bins[kBins];
+    __shared__ uint4 zeros[kZeros / 16];
     const int blocks = (int)prm.sort_blocks, w = blockIdx.x / blocks, block = blockIdx.x - w * blocks;
-    if (w >= prm.n) return clear_meanwhile<T, ALIGN>(prm, prm.n * blocks, 3 * pass, launches);
+    if (w >= prm.n) return clear_meanwhile<T, ALIGN>(prm, prm.n * blocks, 3 * pass, launches, zeros);
     const int shift = pass * prm.digit_bits;
     const uint32_t mask = (1u << prm.digit_bits) - 1;
     if (threadIdx.x < kBins) bins[threadIdx.x] = 0;
@@ -274,7 +358,8 @@ template <typename T, int ALIGN>
 __global__ void __launch_bounds__(kSortThreads) rps_embed_scan_kernel(const EmbedParams prm, int pass, int launches)
 {
     after_the_kernel_before();
-    if ((int)blockIdx.x >= prm.n) return clear_meanwhile<T, ALIGN>(prm, prm.n, 3 * pass + 1, launches);
+    __shared__ uint4 zeros[kZeros / 16];
+    if ((int)blockIdx.x >= prm.n) return clear_meanwhile<T, ALIGN>(prm, prm.n, 3 * pass + 1, launches, zeros);
     __shared__ uint32_t sums[kSortWarps];
     const int blocks = (int)prm.sort_blocks;
     uint32_t* counts = prm.counts + (int64_t)blockIdx.x * kBins * blocks;
@@ -315,9 +400,9 @@ template <int ITEMS, typename T, int ALIGN>
 __global__ void __launch_bounds__(kSortThreads) rps_embed_scatter_kernel(const EmbedParams prm, int pass, int launches)
 {
     after_the_kernel_before();
-    __shared__ SortShared sh;
+    __shared__ __align__(16) SortShared sh;
     const int blocks = (int)prm.sort_blocks, w = blockIdx.x / blocks, block = blockIdx.x - w * blocks;
-    if (w >= prm.n) return clear_meanwhile<T, ALIGN>(prm, prm.n * blocks, 3 * pass + 2, launches);
+    if (w >= prm.n) return clear_meanwhile<T, ALIGN>(prm, prm.n * blocks, 3 * pass + 2, launches, &sh);
     const int shift = pass * prm.digit_bits, lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     const uint32_t mask = (1u << prm.digit_bits) - 1;
     const int64_t base = w * prm.count;
@@ -346,22 +431,34 @@ constexpr int kSumWarps = 8;
 
 // 512 bytes of a row of the gradient from column `first` on, a warp's.
 template <typename T, int ALIGN>
-__device__ __forceinline__ void write_row(const EmbedParams& prm, int w, uint32_t row, int first, const float (&sum)[Slice<T>::kWidth])
+__device__ __forceinline__ T* row_of(const EmbedParams& prm, int w, uint32_t row)
+{
+    return static_cast<T*>(prm.dweight) + w * prm.dweight_worker + (int64_t)row * prm.dweight_row;
+}
+
+// `old`: what is there, where it is added to.
+template <typename T, int ALIGN>
+__device__ __forceinline__ void write_row(const EmbedParams& prm, int w, uint32_t row, int first, const float (&sum)[Slice<T>::kWidth], const uint4& old)
 {
     using P = Piece<T, ALIGN>;
-    T* out = static_cast<T*>(prm.dweight) + w * prm.dweight_worker + (int64_t)row * prm.dweight_row;
+    T* out = row_of<T, ALIGN>(prm, w, row);
     const int lane = threadIdx.x % 32;
     float v[P::kWidth];
-#pragma unroll
-    for (int j = 0; j < P::kWidth; ++j) v[j] = 0.0f;
-    if (prm.accumulate) widen(P::load(out, first, lane, 32, (int)prm.cols), v);
+    widen(old, v);
 #pragma unroll
     for (int j = 0; j < P::kWidth; ++j) v[j] = prm.accumulate ? fmaf(prm.scale, sum[j], v[j]) : prm.scale * sum[j];
     P::store(out, first, lane, 32, (int)prm.cols, narrow(v));
 }
 
-// A warp for 512 bytes of the columns of a tile of sorted tokens.
 template <typename T, int ALIGN>
+__device__ __forceinline__ void write_row(const EmbedParams& prm, int w, uint32_t row, int first, const float (&sum)[Slice<T>::kWidth])
+{
+    using P = Piece<T, ALIGN>;
+    write_row<T, ALIGN>(prm, w, row, first, sum, prm.accumulate ? P::load(row_of<T, ALIGN>(prm, w, row), first, threadIdx.x % 32, 32, (int)prm.cols) : make_uint4(0, 0, 0, 0));
+}
+
+// A warp for 512 bytes of the columns of a tile of sorted tokens.  ADD: to what is there, which is read with the tokens of a run's end.
+template <typename T, int ALIGN, bool ADD>
 __global__ void __launch_bounds__(32 * kSumWarps) rps_embed_sum_kernel(const EmbedParams prm, int slabs)
 {
     after_the_kernel_before();
@@ -393,13 +490,17 @@ __global__ void __launch_bounds__(32 * kSumWarps) rps_embed_sum_kernel(const Emb
         const uint32_t my_key = mine ? __ldg(keys + p + lane) : (uint32_t)prm.vocab, my_from = mine ? __ldg(from + p + lane) : 0;
         const int here = (int)min((int64_t)32, p1 - p);
         for (int q = 0; q < here; q += kAtATime) {
-            uint4 slice[kAtATime];
+            uint4 slice[kAtATime], old[ADD ? kAtATime : 1];
             uint32_t key[kAtATime];
 #pragma unroll
             for (int i = 0; i < kAtATime; ++i) {
                 key[i] = __shfl_sync(0xFFFFFFFFu, my_key, q + i);
                 const int64_t row = __shfl_sync(0xFFFFFFFFu, my_from, q + i);
                 slice[i] = P::load(dout + row * prm.cols, first, lane, 32, key[i] < prm.vocab ? D : 0);
+                if constexpr (ADD) {
+                    const uint32_t ending = i > 0 ? key[i - 1] : current;
+                    old[i] = P::load(row_of<T, ALIGN>(prm, w, ending < prm.vocab ? ending : 0), first, lane, 32, ending != key[i] && ending < prm.vocab ? D : 0);
+                }
             }
 #pragma unroll
             for (int i = 0; i < kAtATime; ++i) {
@@ -408,7 +509,7 @@ __global__ void __launch_bounds__(32 * kSumWarps) rps_embed_sum_kernel(const Emb
                         if (head)
                             store_part(0);
                         else
-                            write_row<T, ALIGN>(prm, w, current, first, sum);
+                            write_row<T, ALIGN>(prm, w, current, first, sum, ADD ? old[i] : make_uint4(0, 0, 0, 0));
                     }
                     head = false, current = key[i];
 #pragma unroll
@@ -467,7 +568,7 @@ __global__ void __launch_bounds__(32 * kSumWarps) rps_embed_join_kernel(const Em
         }
     };
     add(tile, 1, true);
-#pragma unroll 8
+#pragma unroll 16
     for (int64_t t = tile + 1; t <= last; ++t) add(t, 0, false);
     write_row<T, ALIGN>(prm, w, key, first, sum);
 }
@@ -489,7 +590,7 @@ __global__ void __launch_bounds__(kSortThreads) rps_embed_few_kernel(const Embed
     } sh;
     __shared__ uint32_t keys[kSortThreads], from[kSortThreads];
     const int w = blockIdx.y, count = (int)prm.count, lane = threadIdx.x % 32, warp = threadIdx.x / 32, D = (int)prm.cols;
-    sort_in_shared<1>(prm, w, sh.sort, keys, from);
+    sort_in_shared<1, 1>(prm, w, sh.sort, keys, from);
     const T* dout = static_cast<const T*>(prm.dout) + w * prm.count * prm.cols;
     const auto sum_run = [&](int p, int first) {
         const uint32_t row = keys[p];
@@ -547,7 +648,8 @@ template <typename T, int ALIGN>
 __global__ void __launch_bounds__(kSortThreads) rps_embed_clear_kernel(const EmbedParams prm)
 {
     after_the_kernel_before();
-    clear_meanwhile<T, ALIGN>(prm, 0, 0, 1);
+    __shared__ uint4 zeros[kZeros / 16];
+    clear_meanwhile<T, ALIGN>(prm, 0, 0, 1, zeros);
 }
 
 // ---------------------------------------------------------------------------------------------------------------- host
@@ -574,7 +676,9 @@ cudaError_t lookup(const EmbedParams& prm, cudaStream_t stream)
     return launch_after(rps_embed_lookup_kernel<T, ALIGN>, grid, kRowThreads, 0, stream, 1, prm, log);
 }
 
-// CTAs that clear beside those that sort.
+// CTAs that clear beside those that sort.  Clusters of eight are placed whole, two to a group of SMs that has room for them: 16 at a time; with three
+// more the clearing took two rounds (126 us instead of 90).
+unsigned clusters_with_clearing(const EmbedParams& prm) { return (unsigned)(kCluster * (prm.n + (prm.accumulate ? 0 : std::max(16 - prm.n, 4)))); }
 unsigned with_clearing(const EmbedParams& prm, int64_t sorting) { return (unsigned)(sorting + (prm.accumulate ? 0 : std::max<int64_t>(kSms - sorting, kSms / 2))); }
 
 template <int ITEMS, typename T, int ALIGN>
@@ -584,7 +688,7 @@ cudaError_t sort_here(const EmbedParams& prm, cudaStream_t stream)
     const uint32_t bytes = sizeof(SortShared) + kSortThreads * ITEMS * 8;
     const cudaError_t err = rps::grant_smem(state, rps_embed_sort_kernel<ITEMS, T, ALIGN>, bytes);
     if (err != cudaSuccess) return err;
-    return launch_after(rps_embed_sort_kernel<ITEMS, T, ALIGN>, dim3(with_clearing(prm, prm.n)), kSortThreads, bytes, stream, 1, prm);
+    return launch_after(rps_embed_sort_kernel<ITEMS, T, ALIGN>, dim3(clusters_with_clearing(prm)), kSortThreads, bytes, stream, kCluster, prm);
 }
 
 template <int ITEMS, typename T, int ALIGN>
@@ -604,8 +708,9 @@ cudaError_t sort_in_passes(const EmbedParams& prm, cudaStream_t stream)
 template <typename T, int ALIGN>
 cudaError_t sort(const EmbedParams& prm, cudaStream_t stream)
 {
-    if (prm.count <= kSortThreads) return sort_here<1, T, ALIGN>(prm, stream);
-    if (prm.count <= kSortThreads * 4) return sort_here<4, T, ALIGN>(prm, stream);
+    constexpr int kOnce = kCluster * kSortThreads;
+    if (prm.count <= kOnce) return sort_here<1, T, ALIGN>(prm, stream);
+    if (prm.count <= kOnce * 4) return sort_here<4, T, ALIGN>(prm, stream);
     if (prm.count <= kSortHere) return sort_here<kMostItems, T, ALIGN>(prm, stream);
     return prm.count <= kMany ? sort_in_passes<1, T, ALIGN>(prm, stream) : sort_in_passes<kManyItems, T, ALIGN>(prm, stream);
 }
@@ -626,7 +731,8 @@ cudaError_t gradient(const EmbedParams& prm, cudaStream_t stream)
     cudaError_t err = sort<T, ALIGN>(prm, stream);
     if (err != cudaSuccess) return err;
     const dim3 grid((unsigned)ceil_div(prm.tiles * slabs, kSumWarps), (unsigned)prm.n);
-    if ((err = launch_after(rps_embed_sum_kernel<T, ALIGN>, grid, 32 * kSumWarps, 0, stream, 1, prm, slabs)) != cudaSuccess || prm.tiles == 1) return err;
+    const auto sum = prm.accumulate ? rps_embed_sum_kernel<T, ALIGN, true> : rps_embed_sum_kernel<T, ALIGN, false>;
+    if ((err = launch_after(sum, grid, 32 * kSumWarps, 0, stream, 1, prm, slabs)) != cudaSuccess || prm.tiles == 1) return err;
     return launch_after(rps_embed_join_kernel<T, ALIGN>, grid, 32 * kSumWarps, 0, stream, 1, prm, slabs);
 }
 

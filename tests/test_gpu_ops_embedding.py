@@ -74,7 +74,8 @@ def check_gradient(ops, tokens, weight, dout, scale, accumulate, dweight=None):
 
 SIZES = [(1, 1, 1, 1), (1, 1, 7, 3), (2, 3, 5, 7), (3, 31, 40, 64), (1, 33, 1000, 65), (4, 100, 30, 129), (2, 1024, 257, 72), (1, 1025, 300, 256), (64, 17, 90, 20),
          (2, 4096, 3, 40), (1, 4097, 70000, 33), (3, 5000, 513, 100), (1, 16384, 2000, 24), (2, 16385, 1000, 33), (1, 70001, 131072, 16), (1, 300, 50, 2051),
-         (1, 512, 400, 36), (2, 513, 400, 36), (1, 300_001, 5000, 8)]
+         (1, 512, 400, 36), (2, 513, 400, 36), (1, 300_001, 5000, 8),
+         (2, 8192, 700, 20), (1, 8193, 700, 20), (1, 32769, 70000, 12), (1, 131072, 3000, 8), (2, 131073, 3000, 8)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
