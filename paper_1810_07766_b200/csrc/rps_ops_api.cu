@@ -138,6 +138,8 @@ LcePlan plan_lce(const rps_lce_desc& d, const void* weight, bool backward, void*
     if (top > 0) {
         TeacherParams& t = plan.teacher;
         t.n = p.n, t.top = top, t.tokens = p.tokens, t.vocab = p.vocab, t.sharpness = p.sharpness;
+        t.bucket_rows = (int)ceil_div(p.vocab, kTopBuckets);
+        t.entry_bucket = c.take<unsigned short>(p.n * p.tokens * kTopBuckets);
         t.entry_id = c.take<int>(p.n * p.tokens * top);
         t.entry_weight = c.take<float>(p.n * p.tokens * top);
         t.targets = c.take<int64_t>(p.n * p.tokens);
@@ -145,7 +147,7 @@ LcePlan plan_lce(const rps_lce_desc& d, const void* weight, bool backward, void*
             t.entropy = c.take<float>(p.n * p.tokens);
             g.entry_logit = c.take<float>(p.n * p.tokens * top);
         }
-        g.top = top, g.sharpness = p.sharpness, g.entry_id = t.entry_id, g.entry_weight = t.entry_weight;
+        g.top = top, g.bucket_rows = t.bucket_rows, g.entry_bucket = t.entry_bucket, g.sharpness = p.sharpness, g.entry_id = t.entry_id, g.entry_weight = t.entry_weight;
         p.targets = t.targets, p.entropy = t.entropy, p.entry_id = t.entry_id, p.entry_weight = t.entry_weight, p.entry_logit = g.entry_logit;
     }
     plan.bytes = c.used;

@@ -57,6 +57,8 @@ enum class Product {
     kDweight   // A = dl or dy [k][m], B = hidden or x [k][n]
 };
 
+constexpr int kTopBuckets = 64;
+
 // How a product is cut: columns of its tiles, runs of its summed axis, and CTAs that make a tile (1 or 2).
 struct ProductShape {
     int tile_cols, splits, ctas;
@@ -76,8 +78,9 @@ struct ProductParams {
     const float2* info;     // [worker][tokens_padded]: lse, g
     bf16* dl;               // [worker][plane][tokens_padded][piece]
     // kTopLse, kTopDlogits: up to `top` entries of each token, by rising row of the weight (behind the last: the largest int)
-    int top;
+    int top, bucket_rows;      // kTopBuckets buckets of this many rows of the weight each
     float sharpness;
+    const unsigned short* entry_bucket;  // [worker][tokens][kTopBuckets]: first entry in the bucket or behind it
     const int* entry_id;       // [worker][tokens][top]
     const float* entry_weight; // their probabilities
     float* entry_logit;        // written by kTopLse
@@ -159,7 +162,9 @@ struct TeacherParams {
     float sharpness;
     const int64_t* ids;     // [n][tokens][top]
     const void* logits;
-    int* entry_id;          // as ProductParams
+    int bucket_rows;
+    unsigned short* entry_bucket;  // as ProductParams
+    int* entry_id;
     float* entry_weight;
     float* entropy;         // [n][tokens], or NULL
     int64_t* targets;       // [n][tokens]: 0, kNoTeacher for a token without entries, -1 for one whose entries are no distribution

@@ -347,14 +347,25 @@ struct RowInfo {
     float2 info;  // kDlogits, kTopDlogits: lse and g
     int index;    // of the row where it is stored, -1 if it is not
     float scale;
-    // kTopLse, kTopDlogits: the row's entries, the next of them from this warp's columns on, and its column (the largest int: none)
+    // kTopLse, kTopDlogits: the row's entries, the next of them from this warp's columns on, and the columns (the largest int: none) and weights of that
+    // one and the one after it, so that a column that has one entry does not wait for another's
     int64_t entries;
-    int next, next_col;
+    int next, next_col, after_col;
+    float next_weight, after_weight;
 };
 
-__device__ __forceinline__ int entry_column(const ProductParams& prm, const RowInfo& r, int first)
+template <Product WHICH>
+__device__ __forceinline__ void load_entry(const ProductParams& prm, const RowInfo& r, int i, int first, int& col, float& weight)
 {
-    return r.next < prm.top ? __ldg(prm.entry_id + r.entries + r.next) - first : 0x7FFFFFFF;
+    col = i < prm.top ? __ldg(prm.entry_id + r.entries + i) - first : 0x7FFFFFFF;
+    if (kGradient<WHICH>) weight = i < prm.top ? __ldg(prm.entry_weight + r.entries + i) : 0.0f;
+}
+
+template <Product WHICH>
+__device__ __forceinline__ void next_entry(const ProductParams& prm, RowInfo& r, int first)
+{
+    ++r.next, r.next_col = r.after_col, r.next_weight = r.after_weight;
+    load_entry<WHICH>(prm, r, r.next + 1, first, r.after_col, r.after_weight);
 }
 
 template <Product WHICH>
@@ -364,11 +375,15 @@ __device__ __forceinline__ RowInfo row_info(const ProductParams& prm, int w, int
     const bool in = row < (WHICH == Product::kDweight ? prm.m : count);
     if constexpr (kStatistics<WHICH> || kGradient<WHICH>) {
         if constexpr (kTop<WHICH>) {
-            r.next = prm.top, r.next_col = 0x7FFFFFFF;
+            r.next = prm.top, r.next_col = r.after_col = 0x7FFFFFFF;
             if (in) {
-                r.entries = (w * prm.tokens + __ldg(prm.rows + w * prm.tokens + row)) * prm.top;
-                const int first = prm.v0 + n0;
-                int low = 0, high = prm.top;
+                const int64_t token = w * prm.tokens + __ldg(prm.rows + w * prm.tokens + row);
+                r.entries = token * prm.top;
+                // among those of the first column's bucket: every step of the search is a way to memory (2048 tokens of 50001 words x 1024 with 50 entries:
+                // all of them searched 165 us, ...)
+                const int first = prm.v0 + n0, bucket = min(first / prm.bucket_rows, kTopBuckets - 1);
+                const unsigned short* at = prm.entry_bucket + token * kTopBuckets + bucket;
+                int low = __ldg(at), high = bucket + 1 < kTopBuckets ? __ldg(at + 1) : prm.top;
                 while (low < high) {
                     const int middle = (low + high) / 2;
                     if (__ldg(prm.entry_id + r.entries + middle) < first)
@@ -377,7 +392,7 @@ __device__ __forceinline__ RowInfo row_info(const ProductParams& prm, int w, int
                         high = middle;
                 }
                 r.next = low;
-                r.next_col = entry_column(prm, r, first);
+                load_entry<WHICH>(prm, r, low, first, r.next_col, r.next_weight), load_entry<WHICH>(prm, r, low + 1, first, r.after_col, r.after_weight);
             }
         } else {
             r.target = in ? __ldg(prm.target + w * prm.tokens_padded + row) - prm.v0 - n0 : -1;
@@ -436,8 +451,7 @@ __device__ __forceinline__ bool statistics(const ProductParams& prm, int w, int 
             for (int j = 0; j < COLS; ++j)
                 if (j == info.next_col) logit = v[j];
             prm.entry_logit[info.entries + info.next] = logit;
-            ++info.next;
-            info.next_col = entry_column(prm, info, prm.v0 + n0);
+            next_entry<WHICH>(prm, info, prm.v0 + n0);
         }
     }
     sum = total.sum();
@@ -477,12 +491,10 @@ __device__ __forceinline__ void store_columns(const ProductParams& prm, int w, i
 #pragma unroll
             for (int j = 0; j < COLS; ++j) v[j] = exp_of_difference(v[j], info.info.x, factor);
             while (info.next_col - c0 < cols) {
-                const float q = __ldg(prm.entry_weight + info.entries + info.next);
 #pragma unroll
                 for (int j = 0; j < COLS; ++j)
-                    if (j == info.next_col - c0) v[j] -= q;
-                ++info.next;
-                info.next_col = entry_column(prm, info, prm.v0 + n0 - c0);
+                    if (j == info.next_col - c0) v[j] -= info.next_weight;
+                next_entry<WHICH>(prm, info, prm.v0 + n0 - c0);
             }
         }
 #pragma unroll
@@ -618,7 +630,7 @@ __global__ void __launch_bounds__(Epilogue<PLANES>::kThreads, 1)
     if (warp < Epilogue<PLANES>::kFirst) {
         if constexpr (PLANES == 3) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kIssueRegisters));
         if (warp == 0) {
-            if (lane == 0) {
+            if (elect_one()) {
                 int stage = 0, issued = 0;
                 uint32_t phase = 0;
                 for (int tile = blockIdx.x / CTAS; tile < total && fine; tile += groups) {
@@ -669,7 +681,7 @@ __global__ void __launch_bounds__(Epilogue<PLANES>::kThreads, 1)
                 }
             }
         } else if (warp == 1) {
-            if (rank == 0 && lane == 0) {
+            if (rank == 0 && elect_one()) {
                 const uint32_t descriptor = instruction_descriptor(kAOther, kBOther, kRows, tile_n);
                 // one product covers 16 of the summed axis: 32 bytes further along swizzled rows, or 16 rows of 128 bytes further
                 constexpr uint32_t a_step = (kAOther ? 2048 : 32) / 16, b_step = (kBOther ? 2048 : 32) / 16;
@@ -779,7 +791,7 @@ __global__ void __launch_bounds__(Epilogue<PLANES>::kThreads, 1)
             }
         }
     }
-    if (!fine && lane == 0) atomicExch(&g_gave_up, 1);
+    if (!fine) atomicExch(&g_gave_up, 1);
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
     if constexpr (CTAS == 2) cluster_sync();

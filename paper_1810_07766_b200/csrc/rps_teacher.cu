@@ -96,11 +96,19 @@ __global__ void __launch_bounds__(kThreads) rps_teacher_kernel(const TeacherPara
                 }
             }
         }
+    // the buckets that begin with each entry: those behind its predecessor's up to its own
+    unsigned short* bucket = prm.entry_bucket + t * kTopBuckets;
+    int before = -1;  // of the last entry of the 32 before
 #pragma unroll
     for (int r = 0; r < PER; ++r) {
-        const int at = r * 32 + lane;
+        const int at = r * 32 + lane, own = min(id[r] / prm.bucket_rows, kTopBuckets - 1);
+        const int left = __shfl_up_sync(0xFFFFFFFFu, own, 1), previous = lane > 0 ? left : before;
+        for (int b = previous + 1; b <= own; ++b) bucket[b] = (unsigned short)min(at, prm.top);
+        before = __shfl_sync(0xFFFFFFFFu, own, 31);
         if (at < prm.top) prm.entry_id[first + at] = id[r], prm.entry_weight[first + at] = e[r];
     }
+    // (what is no entry sorts behind all buckets but the last; where there is no such place all are entries)
+    for (int b = before + 1 + lane; b < kTopBuckets; b += 32) bucket[b] = (unsigned short)prm.top;
 }
 
 }  // namespace
