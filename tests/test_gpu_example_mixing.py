@@ -1,0 +1,84 @@
+"""The language-model example with attention, a teacher and texts that go on: it runs, its gradients are those of the same model in plain operations."""
+import math
+import os
+import sys
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+
+
+@pytest.fixture(scope="module")
+def example():
+    if not torch.cuda.is_available():
+        pytest.fail("these tests need a CUDA device")
+    import train_language_model
+
+    train_language_model.build.build()
+    return train_language_model
+
+
+@pytest.mark.parametrize("dtype,drop,heads,teacher", [("f32", 0.0, 2, 4), ("bf16", 0.1, 4, 0), ("bf16", 0.1, 2, 8)])
+def test_it_runs(example, dtype, drop, heads, teacher):
+    losses, further = example.train(steps=10, workers=3, drop=drop, vocab=150, width=64, blocks=2, tokens=96, dtype=dtype, heads=heads, sequences=3, teacher=teacher,
+                                    further_words=5)
+    assert len(losses) == 10 and torch.isfinite(losses).all()
+    assert further.shape == (4, 5) and (further >= 0).all() and (further < 150).all()
+
+
+def plain(p, tokens, targets, blocks, heads, sequences, teacher, decay):
+    """The example's model of one worker in elementary operations."""
+    def norm(z):
+        return z / torch.sqrt((z * z).mean(-1, keepdim=True) + 1e-6)
+
+    def rejoin(x, f, name):
+        x = x + (1.0 / math.sqrt(blocks)) * p[f"{name}.gate"] * norm(f) * p[f"{name}.post"]
+        return x, norm(x) * p[f"{name}.pre"]
+
+    x = y = p["embedding"][tokens]
+    for i in range(blocks):
+        q, k, v = (y @ p[f"{i}.qkv"].T).view(sequences, -1, heads, 3 * y.shape[-1] // heads).chunk(3, -1)
+        T = q.shape[1]
+        apart = torch.arange(T, device="cuda")[:, None] - torch.arange(T, device="cuda")
+        weight = torch.where(apart >= 0, torch.exp(decay[:, None, None].double() * apart.clamp(min=0)), 0.0)
+        scores = torch.einsum("sihd,sjhd->shij", q, k) * weight / math.sqrt(q.shape[-1])
+        f = torch.einsum("shij,sjhd->sihd", scores, v).reshape(len(tokens), -1) @ p[f"{i}.out"].T
+        x, y = rejoin(x, f, f"{i}.mix")
+        f = torch.relu(y @ p[f"{i}.up"].T) @ p[f"{i}.down"].T
+        x, y = rejoin(x, f, str(i))
+    z = torch.log_softmax(y @ p["head"].T, -1)
+    loss = -z.gather(1, targets[:, None]).mean()
+    ids, logits = teacher
+    q = torch.softmax(logits.double().masked_fill(ids < 0, -math.inf), -1)
+    near = (torch.special.xlogy(q, q) - q * z.gather(1, ids.clamp(min=0))).sum(-1).mean()
+    return 0.5 * (loss + near)
+
+
+def test_gradients_of_the_whole_model(example):
+    """fp32 through four norms, three products and a softmax each way: errors of a few 2^-22 of the terms, kept below 2^-12 of a gradient's norm
+    with "values"; kept in 8 bits, a half step of 1/254 of the largest of 128 (about 2^-7 of a value) in each weight gradient's input."""
+    n, vocab, width, blocks, heads, sequences, tokens = 2, 90, 32, 2, 2, 3, 60
+    g = torch.Generator(device="cuda").manual_seed(0)
+    shapes = {"embedding": (vocab, width), "head": (vocab, width)}
+    for i in range(blocks):
+        shapes.update({f"{i}.up": (4 * width, width), f"{i}.down": (width, 4 * width), f"{i}.qkv": (3 * width, width), f"{i}.out": (width, width)})
+        for name in (f"{i}", f"{i}.mix"):
+            shapes.update({f"{name}.gate": (1, width), f"{name}.post": (width,), f"{name}.pre": (width,)})
+    p = {name: (torch.randn(n, *shape, generator=g, device="cuda") / math.sqrt(shape[-1]) + (1.0 if len(shape) == 1 else 0.0)).requires_grad_() for name, shape in shapes.items()}
+    text, targets = (torch.randint(0, vocab, (n, tokens), generator=g, device="cuda") for _ in range(2))
+    successor = torch.randperm(vocab, generator=g, device="cuda")
+    teacher = example.largest_logits(text, successor, vocab, 5, g)
+    loss = example.model(p, text, targets, blocks, "values", heads, sequences, teacher)
+    loss.sum().backward()
+    for w in range(n):
+        q = {name: leaf.detach()[w].double().requires_grad_() for name, leaf in p.items()}
+        want = plain(q, text[w], targets[w], blocks, heads, sequences, (teacher[0][w], teacher[1][w]), example.decays(n, heads)[w])
+        want.backward()
+        assert abs(float(loss.detach()[w]) - float(want.detach())) <= 1e-5 * float(want.detach())
+        for name, leaf in p.items():
+            # the weight gradients of linear_8bit come out of inputs in 8 bits
+            near = 2.0 ** -5 if name.split(".")[-1] in ("up", "down", "qkv", "out") else 2.0 ** -12
+            assert (leaf.grad[w] - q[name].grad).norm() <= near * q[name].grad.norm(), name
