@@ -12,7 +12,7 @@ LIB = os.path.join(CSRC, "librps.so")
 SOURCES = ["rps_api.cu", "rps_kernels.cu", "rps_direct_track.cu", "rps_blocked.cu", "rps_staged.cu",
            "rps_staged_grad.cu", "rps_staged_track.cu", "rps_ring.cu", "rps_stream.cu", "rps_static.cu",
            "rps_ops_api.cu", "rps_product.cu", "rps_lce.cu", "rps_lce_dot.cu", "rps_teacher.cu", "rps_norm.cu", "rps_pack.cu",
-           "rps_sequence_api.cu", "rps_embed.cu", "rps_mix.cu", "rps_mix_tensor.cu"]
+           "rps_sequence_api.cu", "rps_embed.cu", "rps_mix.cu", "rps_mix_tensor.cu", "rps_mix_mma.cu"]
 HEADERS = ["rps_device.cuh", "rps_kernels.h", "rps_direct.cuh", "rps_staged.cuh", "rps_tma.cuh", "rps_ops_kernels.h", "rps_ops_host.h", "rps_rows.cuh", "rps_lce.cuh", "rps_cluster.cuh", "rps_tensor.cuh",
            "rps_mix.cuh"]
 PUBLIC = ["rps.h", "rps_ops.h"]

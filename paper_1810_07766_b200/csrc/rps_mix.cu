@@ -8,14 +8,13 @@
 // the gradient and a token's own factor comes one step later (`late`), dk (v, dout, q) and dv (k, q, dout).  The three gradients go
 // through one launch, so that the third reads what the others have brought into L2.
 //
-// A CTA takes a sequence's head and 64 columns of z, chunk by chunk; W stays in its registers as fp32.  Where there are too few of those to fill
-// the SMs, sequences are cut into segments: one launch makes each segment's own sum of y^T z, one adds them up in order into the states that
-// segments begin with, and the main one then runs all segments at once (y and z are read twice).
+// Where there are too few heads of sequences to fill the SMs, sequences are cut into segments: one launch makes each segment's own sum of y^T z,
+// one adds them up in order into the states that segments begin with, and the main one then runs all segments at once (y and z are read twice).
 //
-// Products go through the tensor cores (mma.sync: tiles are 64 x 64 with 16 rows to a warp, and every operand is scaled or masked in registers
-// on its way from one product to the next).  bf16 operands are used as they are; what is made here is rounded to bf16 where it is multiplied
-// once more on its way to a bf16 result (the masked products, W), and kept in three parts where it is summed into a state (r^(C-1-j) y_j).
-// fp32 operands are three bf16 parts each, of whose products six are made (split_two).
+// The kernel here takes fp32 operands (bf16 ones: rps_mix_tensor.cu, or rps_mix_mma.cu where TMA cannot copy them).  A CTA has a sequence's head and 64 columns of z,
+// chunk by chunk of 64 tokens; all products are of fp32 in registers, 4 x 4 results to a thread with two 16-byte reads of shared memory for every 16
+// to 32 multiplications.  Bound by those: 128 a cycle and SM.  (As six products of bf16 parts on the tensor cores, mma.sync, whose operands every
+// warp had to cut into parts for itself, 4 x 3 sequences of 333 x 5 x 48 x 40 took 193 us forward and backward, 155 so.)
 #include <algorithm>
 
 #include "rps_mix.cuh"
@@ -27,194 +26,45 @@ namespace {
 using rps::LaunchState;
 
 constexpr int kC = kMixChunk, kTile = 64;  // tokens of a chunk; columns of z of a CTA
+constexpr int kThreads = 256;              // 16 x 16, with 4 x 4 results each
 
-// ------------------------------------------------------------------------------------------------------ instructions
-__device__ __forceinline__ void multiply(float (&sum)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
-{
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-                 : "+f"(sum[0]), "+f"(sum[1]), "+f"(sum[2]), "+f"(sum[3])
-                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-
-template <bool TRANSPOSED>
-__device__ __forceinline__ void load_matrices(uint32_t (&r)[4], uint32_t addr)
-{
-    if constexpr (TRANSPOSED)
-        asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
-    else
-        asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
-}
-
-// A 16 x 16 operand (rows x summed axis) and two 16 x 8 ones (summed axis x columns), as parts whose sum they are.
-template <int PARTS>
-struct Left {
-    uint32_t part[PARTS][4];
-};
-template <int PARTS>
-struct Right {
-    uint32_t part[PARTS][2][2];
-};
-
-// Two values as PARTS words.
-template <int PARTS>
-__device__ __forceinline__ void split_pair(float a, float b, uint32_t (&word)[PARTS])
-{
-    if constexpr (PARTS == 1) {
-        word[0] = two_bf16(a, b);
-    } else {
-        split_two(a, b, word);
-    }
-}
-
-// How tiles lie in shared memory, and how operands come out of them.  ROW: elements from a row to the next, chosen so that a warp's
-// reads meet no bank twice.
-template <typename T>
-struct Tile;
-
-template <>
-struct Tile<bf16> {
-    static constexpr int kPad = 8, kParts = 1;
-    // [row][summed axis]
-    template <int ROW>
-    static __device__ __forceinline__ void left(Left<1>& a, const bf16* tile, int row, int k)
-    {
-        const int lane = threadIdx.x % 32;
-        load_matrices<false>(a.part[0], rps::smem_addr(tile + (row + lane % 16) * ROW + k + lane / 16 * 8));
-    }
-    // [column][summed axis]
-    template <int ROW>
-    static __device__ __forceinline__ void right_across(Right<1>& b, const bf16* tile, int k, int col)
-    {
-        const int lane = threadIdx.x % 32;
-        uint32_t r[4];
-        load_matrices<false>(r, rps::smem_addr(tile + (col + lane % 8 + lane / 16 * 8) * ROW + k + lane / 8 % 2 * 8));
-        b.part[0][0][0] = r[0], b.part[0][0][1] = r[1], b.part[0][1][0] = r[2], b.part[0][1][1] = r[3];
-    }
-    // [summed axis][column]
-    template <int ROW>
-    static __device__ __forceinline__ void right(Right<1>& b, const bf16* tile, int k, int col)
-    {
-        const int lane = threadIdx.x % 32;
-        uint32_t r[4];
-        load_matrices<true>(r, rps::smem_addr(tile + (k + lane % 16) * ROW + col + lane / 16 * 8));
-        b.part[0][0][0] = r[0], b.part[0][0][1] = r[1], b.part[0][1][0] = r[2], b.part[0][1][1] = r[3];
-    }
-    // [summed axis][row], times a factor for each step of the summed axis: the lane's are at k + 2 (lane % 4) + {0, 1, 8, 9}
-    template <int ROW, int PARTS>
-    static __device__ __forceinline__ void left_across(Left<PARTS>& a, const bf16* tile, int k, int row, const float (&factor)[4])
-    {
-        const int lane = threadIdx.x % 32;
-        uint32_t r[4];
-        load_matrices<true>(r, rps::smem_addr(tile + (k + lane % 8 + lane / 16 * 8) * ROW + row + lane / 8 % 2 * 8));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            uint32_t word[PARTS];
-            split_pair<PARTS>(__uint_as_float(r[i] << 16) * factor[i / 2 * 2], __uint_as_float(r[i] & 0xFFFF0000u) * factor[i / 2 * 2 + 1], word);
-#pragma unroll
-            for (int q = 0; q < PARTS; ++q) a.part[q][i] = word[q];
-        }
-    }
-    static __device__ __forceinline__ void store_two(bf16* at, float a, float b) { *reinterpret_cast<uint32_t*>(at) = two_bf16(a, b); }
-};
-
-template <>
-struct Tile<float> {
-    static constexpr int kPad = 4, kParts = 3;
-    static __device__ __forceinline__ void split(float a, float b, uint32_t& first, uint32_t& second, uint32_t& third)
-    {
-        uint32_t word[3];
-        split_two(a, b, word);
-        first = word[0], second = word[1], third = word[2];
-    }
-    template <int ROW>
-    static __device__ __forceinline__ void left(Left<3>& a, const float* tile, int row, int k)
-    {
-        const int lane = threadIdx.x % 32;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float2 v = *reinterpret_cast<const float2*>(tile + (row + lane / 4 + i % 2 * 8) * ROW + k + lane % 4 * 2 + i / 2 * 8);
-            split(v.x, v.y, a.part[0][i], a.part[1][i], a.part[2][i]);
-        }
-    }
-    template <int ROW>
-    static __device__ __forceinline__ void right_across(Right<3>& b, const float* tile, int k, int col)
-    {
-        const int lane = threadIdx.x % 32;
-#pragma unroll
-        for (int n = 0; n < 2; ++n)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const float2 v = *reinterpret_cast<const float2*>(tile + (col + n * 8 + lane / 4) * ROW + k + lane % 4 * 2 + i * 8);
-                split(v.x, v.y, b.part[0][n][i], b.part[1][n][i], b.part[2][n][i]);
-            }
-    }
-    template <int ROW>
-    static __device__ __forceinline__ void right(Right<3>& b, const float* tile, int k, int col)
-    {
-        const int lane = threadIdx.x % 32;
-#pragma unroll
-        for (int n = 0; n < 2; ++n)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const float* at = tile + (k + lane % 4 * 2 + i * 8) * ROW + col + n * 8 + lane / 4;
-                split(at[0], at[ROW], b.part[0][n][i], b.part[1][n][i], b.part[2][n][i]);
-            }
-    }
-    template <int ROW, int PARTS>
-    static __device__ __forceinline__ void left_across(Left<PARTS>& a, const float* tile, int k, int row, const float (&factor)[4])
-    {
-        static_assert(PARTS == 3, "fp32 values are three parts");
-        const int lane = threadIdx.x % 32;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float* at = tile + (k + lane % 4 * 2 + i / 2 * 8) * ROW + row + lane / 4 + i % 2 * 8;
-            split(at[0] * factor[i / 2 * 2], at[ROW] * factor[i / 2 * 2 + 1], a.part[0][i], a.part[1][i], a.part[2][i]);
-        }
-    }
-    static __device__ __forceinline__ void store_two(float* at, float a, float b) { *reinterpret_cast<float2*>(at) = make_float2(a, b); }
-};
-
-// Products of parts, the smallest first; TILES tiles of 8 columns side by side, of which the first `tiles` are wanted.
-template <int LEFT, int RIGHT, int TILES>
-__device__ __forceinline__ void multiply_parts(float (&sum)[TILES][4], const Left<LEFT>& a, const Right<RIGHT> (&b)[TILES / 2], int tiles)
-{
-#pragma unroll
-    for (int order = LEFT + RIGHT - 2; order >= 0; --order) {
-        if (order > 2) continue;  // what these would add is below 2^-24 of the result
-#pragma unroll
-        for (int p = 0; p < LEFT; ++p) {
-            const int q = order - p;
-            if (q < 0 || q >= RIGHT) continue;
-#pragma unroll
-            for (int n = 0; n < TILES; ++n)
-                if (n < tiles) multiply(sum[n], a.part[p], b[n / 2].part[q][n % 2][0], b[n / 2].part[q][n % 2][1]);
-        }
-    }
-}
-
-// ------------------------------------------------------------------------------------------------------------ kernel
-// MT: 64 columns of x and y each; WN: warps that share a chunk's 16 rows.  STATES: no output, only each segment's own sum.
-template <typename T, int MT, int WN>
+// Shared memory, in floats: rows of x and y, of z and of what is made, none of which meet a bank twice in a read.  MT: 64 columns of x and y each.
+template <int MT>
 struct Shape {
-    static constexpr int kThreads = 128 * WN, kTiles = 8 / WN;              // tiles of 8 columns of a warp
-    static constexpr int kRowA = MT * 64 + Tile<T>::kPad, kRowB = kTile + Tile<T>::kPad;
-    static constexpr int kStage = kC * (2 * kRowA + kRowB);                  // elements: x, y, z
-    static constexpr int kBytes = (2 * kStage + MT * 64 * kRowB) * (int)sizeof(T) + (kC + 4) * 4;
+    static constexpr int kRowA = MT * 64 + 4, kRow = kTile + 4, kStages = MT;  // two CTAs share an SM where one stage is all there is
+    static constexpr int kStage = kC * (2 * kRowA + kRow);
+    static constexpr int kBytes = (kStages * kStage + kC * kRow + MT * 64 * kRow + kC + 4) * 4;
 };
 
-template <typename T, int MT, int WN, int ALIGN, bool STATES>
-__global__ void __launch_bounds__(Shape<T, MT, WN>::kThreads) rps_mix_kernel(const __grid_constant__ MixParams prm)
+__device__ __forceinline__ float4 four(const float* p) { return *reinterpret_cast<const float4*>(p); }
+
+// Four values into columns c.. of a row of `cols`.
+template <int ALIGN>
+__device__ __forceinline__ void store_four(float* row, int c, int cols, const float (&v)[4])
+{
+    if constexpr (ALIGN == 16) {
+        if (c < cols) *reinterpret_cast<float4*>(row + c) = make_float4(v[0], v[1], v[2], v[3]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (c + j < cols) row[c + j] = v[j];
+    }
+}
+
+// STATES: no output, only each segment's own sum.
+template <int MT, int ALIGN, bool STATES>
+__global__ void __launch_bounds__(kThreads, MT == 1 ? 2 : 1) rps_mix_kernel(const __grid_constant__ MixParams prm)
 {
     after_the_kernel_before();
-    using S = Shape<T, MT, WN>;
-    constexpr int W = Slice<T>::kWidth, kParts = Tile<T>::kParts, kStateParts = 3, NT = S::kTiles;
-    extern __shared__ __align__(128) unsigned char raw[];
-    T* const stages = reinterpret_cast<T*>(raw);
-    T* const state = stages + 2 * S::kStage;
-    float* const powers = reinterpret_cast<float*>(state + MT * 64 * S::kRowB);  // r^0 .. r^64
+    using S = Shape<MT>;
+    constexpr int W = 4;
+    extern __shared__ __align__(16) float shared[];
+    float* const scores = shared + S::kStages * S::kStage;
+    float* const state = scores + kC * S::kRow;
+    float* const powers = state + MT * 64 * S::kRow;  // r^0 .. r^64
 
     const MixTerm& term = prm.term[blockIdx.y];
-    const int a = term.a, b = term.b, a16 = (a + 15) / 16 * 16;
+    const int a = term.a, b = term.b, a4 = (a + 3) / 4 * 4;
     const int64_t item = blockIdx.x / prm.columns;
     const int col0 = (int)(blockIdx.x - item * prm.columns) * kTile;
     if (col0 >= b) return;
@@ -222,195 +72,167 @@ __global__ void __launch_bounds__(Shape<T, MT, WN>::kThreads) rps_mix_kernel(con
     const int64_t unit = item / prm.segments;
     if (STATES && segment + 1 == prm.segments) return;
     const Place at = place_of(prm, unit);
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, wr = warp % 4, wn = warp / 4, g = lane / 4, t2 = lane % 4 * 2;
-    const int cols = min(kTile, b - col0), tiles = max(0, min(NT, (cols + 7) / 8 - wn * NT));  // of this warp
+    const int warp = threadIdx.x / 32, tx = threadIdx.x % 16, ty = threadIdx.x / 16;
+    const int cols = min(kTile, b - col0);
     const int64_t i0 = segment * prm.segment_tokens, i1 = min(at.length, i0 + prm.segment_tokens);
     const int late = term.reversed;
     const float log_decay = __ldg(prm.log_decay + at.w * prm.heads + at.head);
     if (threadIdx.x <= kC) powers[threadIdx.x] = (float)power(log_decay, threadIdx.x);
 
-    const T* const x = first_token<T>(term.x, at);
-    const T* const y = first_token<T>(term.y, at);
-    const T* const z = first_token<T>(term.z, at);
+    const float* const x = first_token<float>(term.x, at);
+    const float* const y = first_token<float>(term.y, at);
+    const float* const z = first_token<float>(term.z, at);
+    float* const out = static_cast<float*>(term.out) + ((at.w * prm.sequences + at.sequence) * prm.tokens * prm.heads + at.head) * b + col0;
     // a chunk's rows; behind the last token zeros
     const auto load = [&](int64_t i, int stage) {
-        T* const to = stages + stage * S::kStage;
-        const auto rows = [&](T* tile, int row_length, const T* from, int64_t stride, int c0, int limit, int width) {
+        float* const to = shared + stage * S::kStage;
+        const auto rows = [&](float* tile, int row_length, const float* from, int64_t stride, int c0, int limit, int width) {
             const int across = (width + W - 1) / W;
-            for (int u = threadIdx.x; u < kC * across; u += S::kThreads) {
+            for (int u = threadIdx.x; u < kC * across; u += kThreads) {
                 const int r = u / across, c = (u - r * across) * W;
                 const int64_t at_row = i + r, token = late ? at.length - 1 - at_row : at_row;
                 const bool there = at_row < i1;
-                copy_slice<T, ALIGN>(rps::smem_addr(tile + r * row_length + c), from + (there ? token : 0) * stride, c0 + c, there ? limit : 0);
+                copy_slice<float, ALIGN>(rps::smem_addr(tile + r * row_length + c), from + (there ? token : 0) * stride, c0 + c, there ? limit : 0);
             }
         };
-        if (!STATES) rows(to, S::kRowA, x, term.x.token, 0, a, a16);
-        rows(to + kC * S::kRowA, S::kRowA, y, term.y.token, 0, a, a16);
-        rows(to + 2 * kC * S::kRowA, S::kRowB, z, term.z.token, col0, b, kTile);
+        if (!STATES) rows(to, S::kRowA, x, term.x.token, 0, a, a);
+        rows(to + kC * S::kRowA, S::kRowA, y, term.y.token, 0, a, a);
+        rows(to + 2 * kC * S::kRowA, S::kRow, z, term.z.token, col0, b, kTile);
         copies_sent();
     };
 
-    // W: rows 16 (wr + 4 m) + g and + 8, columns (wn NT + n) 8 + t2 and + 1
-    float w[MT][NT][4];
-    bool zero = true;  // so far
-    const float* init = prm.segments > 1 && !STATES ? prm.segment_states + ((blockIdx.y * prm.units + unit) * prm.segments + segment) * prm.state_room : nullptr;
+    // W: rows 64 m + 4 ty + i, columns 4 tx + j
+    float w[MT][4][4];
+    const float* init = nullptr;
     int64_t init_a = b, init_b = 1;
-    if (!STATES && prm.segments == 1 && term.state_in != nullptr) init = term.state_in + unit * a * b, init_a = term.state_a, init_b = term.state_b;
+    if (!STATES && prm.segments > 1)
+        init = prm.segment_states + ((blockIdx.y * prm.units + unit) * prm.segments + segment) * prm.state_room;
+    else if (!STATES && term.state_in != nullptr)
+        init = term.state_in + unit * a * b, init_a = term.state_a, init_b = term.state_b;
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int row = (wr + 4 * m) * 16 + g + e / 2 * 8, col = col0 + (wn * NT + n) * 8 + t2 + e % 2;
-                w[m][n][e] = init != nullptr && row < a && col < b ? __ldg(init + row * init_a + col * init_b) : 0.0f;
+            for (int j = 0; j < 4; ++j) {
+                const int row = m * 64 + ty * 4 + i, col = col0 + tx * 4 + j;
+                w[m][i][j] = init != nullptr && row < a && col < b ? __ldg(init + row * init_a + col * init_b) : 0.0f;
             }
-    if (init != nullptr) zero = false;
+    bool zero = init == nullptr;  // so far
     const auto publish = [&] {  // W where the products read it
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int e = 0; e < 4; e += 2)
-                    Tile<T>::store_two(state + ((wr + 4 * m) * 16 + g + e / 2 * 8) * S::kRowB + (wn * NT + n) * 8 + t2, w[m][n][e], w[m][n][e + 1]);
+            for (int i = 0; i < 4; ++i) *reinterpret_cast<float4*>(state + (m * 64 + ty * 4 + i) * S::kRow + tx * 4) = make_float4(w[m][i][0], w[m][i][1], w[m][i][2], w[m][i][3]);
     };
-    if (i0 < i1) load(i0, 0);
     if (!STATES && !zero) publish();
+    if (S::kStages == 2 && i0 < i1) load(i0, 0);
 
     int stage = 0;
-    for (int64_t i = i0; i < i1; i += kC, stage ^= 1) {
-        if (i + kC < i1) {
+    for (int64_t i = i0; i < i1; i += kC) {
+        if constexpr (S::kStages == 1) {
+            load(i, 0);
+            copies_arrived<0>();
+        } else if (i + kC < i1) {
             load(i + kC, stage ^ 1);
             copies_arrived<1>();
         } else {
             copies_arrived<0>();
         }
         __syncthreads();
-        T* const tx = stages + stage * S::kStage;
-        const T* const ty = tx + kC * S::kRowA;
-        const T* const tz = ty + kC * S::kRowA;
+        const float* const tx_rows = shared + stage * S::kStage;
+        const float* const ty_rows = tx_rows + kC * S::kRowA;
+        const float* const tz_rows = ty_rows + kC * S::kRowA;
         const int inside = (int)min((int64_t)kC, i1 - i);
         if constexpr (!STATES) {
-            const int row0 = wr * 16;
-            // x . y of these rows with the tokens up to them
-            float p[8][4];
+            const float* const own = tx_rows + ty * 4 * S::kRowA;
+            // x . y of these rows with tokens tx + 16 j, the blocks of 16 up to this warp's rows
+            {
+                float s[4][4] = {};
+                for (int k = 0; k < a4; k += 4) {
+                    float4 l[4];
 #pragma unroll
-            for (int n = 0; n < 8; ++n)
+                    for (int q = 0; q < 4; ++q) l[q] = four(own + q * S::kRowA + k);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) p[n][e] = 0.0f;
-            const int keys = 2 * wr + 2;
-            for (int k = 0; k < a16; k += 16) {
-                Left<kParts> left;
-                Tile<T>::template left<S::kRowA>(left, tx, row0, k);
-                Right<kParts> right[4];
+                    for (int j = 0; j < 4; ++j) {
+                        if (j > warp / 2) break;
+                        const float4 r = four(ty_rows + (tx + 16 * j) * S::kRowA + k);
 #pragma unroll
-                for (int n = 0; n < 4; ++n)
-                    if (2 * n < keys) Tile<T>::template right_across<S::kRowA>(right[n], ty, k, n * 16);
-                multiply_parts<kParts, kParts, 8>(p, left, right, keys);
+                        for (int q = 0; q < 4; ++q) s[q][j] = fmaf(l[q].x, r.x, fmaf(l[q].y, r.y, fmaf(l[q].z, r.z, fmaf(l[q].w, r.w, s[q][j]))));
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (j > warp / 2) break;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const int apart = ty * 4 + q - (tx + 16 * j);
+                        scores[(ty * 4 + q) * S::kRow + tx + 16 * j] = apart >= 0 ? s[q][j] * (term.score_scale * powers[max(apart, 0)]) : 0.0f;
+                    }
+                }
             }
-            float out[NT][4];
+            float o[4][4] = {};
+            const auto add = [&](const float4& l, const float4 (&r)[4], float (&sum)[4]) {
+                const float f[4] = {l.x, l.y, l.z, l.w};
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) out[n][e] = 0.0f;
+                for (int k = 0; k < 4; ++k)
+                    sum[0] = fmaf(f[k], r[k].x, sum[0]), sum[1] = fmaf(f[k], r[k].y, sum[1]), sum[2] = fmaf(f[k], r[k].z, sum[2]), sum[3] = fmaf(f[k], r[k].w, sum[3]);
+            };
             if (!zero) {
-                for (int k = 0; k < a16; k += 16) {
-                    Left<kParts> left;
-                    Tile<T>::template left<S::kRowA>(left, tx, row0, k);
-                    Right<kParts> right[NT / 2];
+                for (int k = 0; k < a4; k += 4) {
+                    float4 r[4];
 #pragma unroll
-                    for (int n = 0; n < NT / 2; ++n)
-                        if (2 * n < tiles) Tile<T>::template right<S::kRowB>(right[n], state, k, (wn * NT + 2 * n) * 8);
-                    multiply_parts<kParts, kParts, NT>(out, left, right, tiles);
+                    for (int q = 0; q < 4; ++q) r[q] = four(state + (k + q) * S::kRow + tx * 4);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) add(four(own + q * S::kRowA + k), r, o[q]);
                 }
 #pragma unroll
-                for (int e = 0; e < 4; e += 2) {
-                    const float factor = term.state_scale * powers[row0 + g + e / 2 * 8 + 1 - late];
+                for (int q = 0; q < 4; ++q) {
+                    const float factor = term.state_scale * powers[ty * 4 + q + 1 - late];
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) out[n][e] *= factor, out[n][e + 1] *= factor;
+                    for (int j = 0; j < 4; ++j) o[q][j] *= factor;
                 }
             }
+            __syncwarp();  // a warp's rows of scores are its own
+            for (int k = 0; k < warp * 8 + 8; k += 4) {
+                float4 r[4];
 #pragma unroll
-            for (int n = 0; n < 8; ++n)
+                for (int q = 0; q < 4; ++q) r[q] = four(tz_rows + (k + q) * S::kRow + tx * 4);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int apart = row0 + g + e / 2 * 8 - (n * 8 + t2 + e % 2);
-                    p[n][e] = apart >= 0 ? p[n][e] * (term.score_scale * powers[max(apart, 0)]) : 0.0f;
-                }
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                if (k > wr) break;
-                Left<kParts> left;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    uint32_t word[kParts];
-                    split_pair<kParts>(p[2 * k + i / 2][i % 2 * 2], p[2 * k + i / 2][i % 2 * 2 + 1], word);
-#pragma unroll
-                    for (int q = 0; q < kParts; ++q) left.part[q][i] = word[q];
-                }
-                Right<kParts> right[NT / 2];
-#pragma unroll
-                for (int n = 0; n < NT / 2; ++n)
-                    if (2 * n < tiles) Tile<T>::template right<S::kRowB>(right[n], tz, k * 16, (wn * NT + 2 * n) * 8);
-                multiply_parts<kParts, kParts, NT>(out, left, right, tiles);
+                for (int q = 0; q < 4; ++q) add(four(scores + (ty * 4 + q) * S::kRow + k), r, o[q]);
             }
-            // out through this warp's rows of x, which have been read (by all warps that share them)
-            if constexpr (WN > 1)
-                asm volatile("bar.sync %0, %1;" ::"r"(1 + wr), "n"(32 * WN) : "memory");
-            else
-                __syncwarp();
-            T* const own = tx + row0 * S::kRowA;
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int e = 0; e < 4; e += 2) Tile<T>::store_two(own + (g + e / 2 * 8) * S::kRowA + (wn * NT + n) * 8 + t2, out[n][e], out[n][e + 1]);
-            __syncwarp();
-            constexpr int kAcross = NT * 8 / W, kDown = 32 / kAcross;
-            const int c = wn * NT * 8 + lane % kAcross * W;
-#pragma unroll
-            for (int r = lane / kAcross; r < 16; r += kDown) {
-                const int64_t row = i + row0 + r, token = late ? at.length - 1 - row : row;
-                if (row < i1)
-                    store_slice<T, ALIGN>(static_cast<T*>(term.out) + (((at.w * prm.sequences + at.sequence) * prm.tokens + token) * prm.heads + at.head) * b + col0, c,
-                                          cols, *reinterpret_cast<const uint4*>(own + r * S::kRowA + c));
+            for (int q = 0; q < 4; ++q) {
+                const int64_t row = i + ty * 4 + q, token = late ? at.length - 1 - row : row;
+                if (row < i1) store_four<ALIGN>(out + token * prm.heads * b, tx * 4, cols, o[q]);
             }
         }
         // W
         const float whole = powers[inside];
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
-            if ((wr + 4 * m) * 16 >= a16) break;
-            float u[NT][4];
+            if (m * 64 + warp * 8 >= a) break;
+            float u[4][4] = {};
+#pragma unroll 4
+            for (int k = 0; k < inside; ++k) {
+                const float factor = term.update_scale * powers[inside - 1 - k + late];
+                const float4 l = four(ty_rows + k * S::kRowA + m * 64 + ty * 4);
+                float4 r = four(tz_rows + k * S::kRow + tx * 4);
+                r = make_float4(r.x * factor, r.y * factor, r.z * factor, r.w * factor);
+                const float f[4] = {l.x, l.y, l.z, l.w};
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) u[n][e] = 0.0f;
-#pragma unroll
-            for (int k = 0; k < kC; k += 16) {
-                if (k >= inside) break;
-                float factor[4];
-#pragma unroll
-                for (int f = 0; f < 4; ++f) {
-                    const int left = inside - 1 - (k + t2 + f % 2 + f / 2 * 8);
-                    factor[f] = left >= 0 ? term.update_scale * powers[left + late] : 0.0f;
-                }
-                Left<kStateParts> left;
-                Tile<T>::template left_across<S::kRowA, kStateParts>(left, ty, k, (wr + 4 * m) * 16, factor);
-                Right<kParts> right[NT / 2];
-#pragma unroll
-                for (int n = 0; n < NT / 2; ++n)
-                    if (2 * n < tiles) Tile<T>::template right<S::kRowB>(right[n], tz, k, (wn * NT + 2 * n) * 8);
-                multiply_parts<kStateParts, kParts, NT>(u, left, right, tiles);
+                for (int q = 0; q < 4; ++q)
+                    u[q][0] = fmaf(f[q], r.x, u[q][0]), u[q][1] = fmaf(f[q], r.y, u[q][1]), u[q][2] = fmaf(f[q], r.z, u[q][2]), u[q][3] = fmaf(f[q], r.w, u[q][3]);
             }
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
+            for (int q = 0; q < 4; ++q)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) w[m][n][e] = fmaf(whole, w[m][n][e], u[n][e]);
+                for (int j = 0; j < 4; ++j) w[m][q][j] = m * 64 + ty * 4 + q < a ? fmaf(whole, w[m][q][j], u[q][j]) : 0.0f;
         }
         zero = false;
         __syncthreads();
         if (!STATES && i + kC < i1) publish();
+        if (S::kStages == 2) stage ^= 1;
     }
 
     float* to = nullptr;
@@ -423,20 +245,18 @@ __global__ void __launch_bounds__(Shape<T, MT, WN>::kThreads) rps_mix_kernel(con
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
+            for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int row = (wr + 4 * m) * 16 + g + e / 2 * 8, col = col0 + (wn * NT + n) * 8 + t2 + e % 2;
-                    if (row < a && col < b) to[row * to_a + col * to_b] = w[m][n][e];
+                for (int j = 0; j < 4; ++j) {
+                    const int row = m * 64 + ty * 4 + i, col = col0 + tx * 4 + j;
+                    if (row < a && col < b) to[row * to_a + col * to_b] = w[m][i][j];
                 }
     }
     if constexpr (!STATES) {
         // rows behind the sequence's last token
         const int64_t t1 = min(prm.tokens, i0 + prm.segment_tokens);
-        for (int64_t t = max(at.length, i0) + warp; t < t1; t += 4 * WN)
-            for (int c = lane * W; c < cols; c += 32 * W)
-                store_slice<T, ALIGN>(static_cast<T*>(term.out) + (((at.w * prm.sequences + at.sequence) * prm.tokens + t) * prm.heads + at.head) * b + col0, c, cols,
-                                      make_uint4(0, 0, 0, 0));
+        const float none[4] = {};
+        for (int64_t t = max(at.length, i0) + ty; t < t1; t += 16) store_four<ALIGN>(out + t * prm.heads * b, tx * 4, cols, none);
     }
 }
 
@@ -551,56 +371,41 @@ __global__ void __launch_bounds__(kStepThreads) rps_mix_step_kernel(const __grid
 }
 
 // -------------------------------------------------------------------------------------------------------------- host
-template <typename T, int MT, int WN, int ALIGN, bool STATES>
-cudaError_t launch_kernel(const MixParams& prm, cudaStream_t stream)
-{
-    static LaunchState granted;
-    using S = Shape<T, MT, WN>;
-    const cudaError_t err = rps::grant_smem(granted, rps_mix_kernel<T, MT, WN, ALIGN, STATES>, S::kBytes);
-    if (err != cudaSuccess) return err;
-    return launch_after(rps_mix_kernel<T, MT, WN, ALIGN, STATES>, dim3((unsigned)(prm.units * prm.segments * prm.columns), (unsigned)prm.terms), S::kThreads, S::kBytes,
-                        stream, 1, prm);
-}
-
 cudaError_t launch_join(const MixParams& prm, cudaStream_t stream)
 {
     return launch_after(rps_mix_join_kernel, dim3((unsigned)(prm.units * prm.join_blocks), (unsigned)prm.terms), kJoinThreads, 0, stream, 1, prm);
 }
 
-template <typename T, int MT, int WN, int ALIGN>
-cudaError_t run(const MixParams& prm, cudaStream_t stream)
+template <int MT, int ALIGN, bool STATES>
+cudaError_t launch_kernel(const MixParams& prm, cudaStream_t stream)
 {
-    if (prm.segments > 1) {
-        cudaError_t err = launch_kernel<T, MT, WN, ALIGN, true>(prm, stream);
-        if (err == cudaSuccess) err = launch_join(prm, stream);
-        if (err != cudaSuccess) return err;
-    }
-    return launch_kernel<T, MT, WN, ALIGN, false>(prm, stream);
+    static LaunchState granted;
+    const cudaError_t err = rps::grant_smem(granted, rps_mix_kernel<MT, ALIGN, STATES>, Shape<MT>::kBytes);
+    if (err != cudaSuccess) return err;
+    return launch_after(rps_mix_kernel<MT, ALIGN, STATES>, dim3((unsigned)(prm.units * prm.segments * prm.columns), (unsigned)prm.terms), kThreads, Shape<MT>::kBytes, stream, 1,
+                        prm);
 }
 
-template <typename T>
-int operand_alignment(const MixOperand& o, int64_t cols)
+template <int MT, int ALIGN>
+cudaError_t launch_either(const MixParams& prm, bool states, cudaStream_t stream)
 {
-    return std::min({alignment<T>(o.base, cols, o.token), alignment<T>(o.base, cols, o.head), alignment<T>(o.base, cols, o.sequence), alignment<T>(o.base, cols, o.worker)});
+    return states ? launch_kernel<MT, ALIGN, true>(prm, stream) : launch_kernel<MT, ALIGN, false>(prm, stream);
 }
 
-template <typename T, int WN>
-cudaError_t mix(const MixParams& prm, cudaStream_t stream)
+cudaError_t launch_f32(const MixParams& prm, bool states, cudaStream_t stream)
 {
-    int align = 16, widest = 0;
-    for (int i = 0; i < prm.terms; ++i) {
-        const MixTerm& t = prm.term[i];
-        align = std::min({align, operand_alignment<T>(t.x, t.a), operand_alignment<T>(t.y, t.a), operand_alignment<T>(t.z, t.b), alignment<T>(t.out, t.b, t.b)});
-        widest = std::max(widest, t.a);
-    }
-    if (widest <= 64) return align == 16 ? run<T, 1, WN, 16>(prm, stream) : align == 4 ? run<T, 1, WN, 4>(prm, stream) : run<T, 1, WN, sizeof(T)>(prm, stream);
-    return align == 16 ? run<T, 2, WN, 16>(prm, stream) : align == 4 ? run<T, 2, WN, 4>(prm, stream) : run<T, 2, WN, sizeof(T)>(prm, stream);
+    int widest = 0;
+    for (int i = 0; i < prm.terms; ++i) widest = std::max(widest, prm.term[i].a);
+    const bool wide = mix_alignment<float>(prm) == 16;
+    if (widest <= 64) return wide ? launch_either<1, 16>(prm, states, stream) : launch_either<1, 4>(prm, states, stream);
+    return wide ? launch_either<2, 16>(prm, states, stream) : launch_either<2, 4>(prm, states, stream);
 }
 
 }  // namespace
 
-// Sequences are cut into as many segments as take the least time by this count of chunks of 128 tokens: a round of CTAs (one to an SM) takes its
-// segment's chunks and one more to begin and end with; the segments' own sums, made first, 0.6 of a chunk each; joining them 3.
+// Sequences are cut into as many segments as take the least time by this count, in microseconds: a round of CTAs takes 6 to begin and end with and
+// for each 128 tokens, as measured, on the tensor cores 4 (2.8 to 4.7); in fp32 37, or with up to 64 columns, where two CTAs share an SM, 21 for one
+// and 35 for both; the segments' own sums, made first, 0.6 of that; joining them 6.
 void plan_mix(MixParams* prm)
 {
     MixParams& p = *prm;
@@ -612,12 +417,18 @@ void plan_mix(MixParams* prm)
     }
     p.join_blocks = (int)ceil_div(p.state_room, kJoinThreads);
     const int64_t chunks = std::max<int64_t>(1, ceil_div(p.tokens, kMixTensorChunk)), ctas = p.units * p.terms * (p.f32 ? p.columns : 1);
+    const bool narrow = std::max(p.term[0].a, p.term[0].b) <= kTile;
+    const auto rounds = [&](int64_t count, double chunks_each) {
+        if (!p.f32 || !narrow) return (double)ceil_div(count, kSms) * ((p.f32 ? 37.0 : 4.0) * chunks_each + 6.0);
+        const int64_t both = count / (2 * kSms), rest = count - both * 2 * kSms;
+        return (double)both * (35.0 * chunks_each + 6.0) + (rest == 0 ? 0.0 : (rest <= kSms ? 21.0 : 35.0) * chunks_each + 6.0);
+    };
     int64_t best = 1;
     double least = 0.0;
     for (int64_t s = 1; s <= std::min<int64_t>(chunks, kMixSegments); ++s) {
         const int64_t each = ceil_div(chunks, s);
         if (s > 1 && (ceil_div(chunks, each) != s || ctas * s > 4 * kSms)) continue;
-        const double cost = (double)ceil_div(ctas * s, kSms) * (double)(each + 1) + (s > 1 ? (double)ceil_div(ctas * (s - 1), kSms) * (0.6 * (double)each + 1.0) + 3.0 : 0.0);
+        const double cost = rounds(ctas * s, (double)each) + (s > 1 ? rounds(ctas * (s - 1), 0.6 * (double)each) + 6.0 : 0.0);
         if (s == 1 || cost < least) best = s, least = cost;
     }
     p.segment_tokens = ceil_div(chunks, best) * kMixTensorChunk;
@@ -626,16 +437,15 @@ void plan_mix(MixParams* prm)
 
 cudaError_t launch_mix(const MixParams& prm, cudaStream_t stream)
 {
-    if (prm.f32) return mix<float, 2>(prm, stream);
-    if (!mix_fits_tensor(prm)) return mix<bf16, 1>(prm, stream);
     MixParams p = prm;
-    p.tensor = 1;
+    p.tensor = !p.f32 && mix_fits_tensor(p);
+    const auto launch = p.f32 ? launch_f32 : p.tensor ? launch_mix_tensor : launch_mix_mma;
     if (p.segments > 1) {
-        cudaError_t err = launch_mix_tensor(p, true, stream);
+        cudaError_t err = launch(p, true, stream);
         if (err == cudaSuccess) err = launch_join(p, stream);
         if (err != cudaSuccess) return err;
     }
-    return launch_mix_tensor(p, false, stream);
+    return launch(p, false, stream);
 }
 
 cudaError_t launch_mix_step(const MixParams& prm, cudaStream_t stream)

@@ -1,6 +1,8 @@
 // What both kernels of linear attention share.
 #pragma once
 
+#include <algorithm>
+
 #include "rps_rows.cuh"
 
 namespace rps_ops {
@@ -33,6 +35,21 @@ template <typename T>
 __device__ __forceinline__ const T* first_token(const MixOperand& o, const Place& p)
 {
     return static_cast<const T*>(o.base) + p.w * o.worker + p.sequence * o.sequence + p.head * o.head;
+}
+
+// What all operands' rows of a call can be moved in.
+template <typename T>
+int mix_alignment(const MixParams& prm)
+{
+    const auto of = [](const MixOperand& o, int64_t cols) {
+        return std::min({alignment<T>(o.base, cols, o.token), alignment<T>(o.base, cols, o.head), alignment<T>(o.base, cols, o.sequence), alignment<T>(o.base, cols, o.worker)});
+    };
+    int align = 16;
+    for (int i = 0; i < prm.terms; ++i) {
+        const MixTerm& t = prm.term[i];
+        align = std::min({align, of(t.x, t.a), of(t.y, t.a), of(t.z, t.b), alignment<T>(t.out, t.b, t.b)});
+    }
+    return align;
 }
 
 }  // namespace

@@ -287,6 +287,7 @@ void plan_mix(MixParams* prm);
 cudaError_t launch_mix(const MixParams& prm, cudaStream_t stream);
 bool mix_fits_tensor(const MixParams& prm);  // whether rps_mix_tensor.cu takes it
 cudaError_t launch_mix_tensor(const MixParams& prm, bool states, cudaStream_t stream);  // states: the segments' own sums
+cudaError_t launch_mix_mma(const MixParams& prm, bool states, cudaStream_t stream);     // bf16 that it does not
 cudaError_t read_mix_gave_up(int* value, cudaStream_t stream);
 cudaError_t launch_mix_step(const MixParams& prm, cudaStream_t stream);
 
