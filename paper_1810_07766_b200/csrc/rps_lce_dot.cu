@@ -1,10 +1,10 @@
-// The loss of a few tokens.  Logits of a few tokens a worker are dot products of the weight's rows with their hidden states, and
+// The loss and the distillation of a few tokens.  Logits of a few tokens a worker are dot products of the weight's rows with their hidden states, and
 // their gradients are multiples of rows: each pass reads (or writes) the weight as it is, once, and memory bounds it.  The tensor
 // cores would make 128 rows for them, and would have fp32 weights and rows that no 16 bytes divide laid out anew first.
 //
 // Up to 4 tokens of bf16 and 8 of fp32 (forward and backward, tensor cores / here, us): 1 token x 131072 x 2048 bf16 467 / 409, 4 tokens
 // 467 / 451; 8 workers of 3 x 5000 x 4096 bf16 303 / 307, of 3 x 1000 x 256 39 / 25; 4 of 1 x 31046 x 1313 bf16 764 / 347; 4 of 8 x 17081 x
-// 1000 fp32 800 / 322; 1 x 1000 x 256 fp32 60 / 20.  More tokens would hold more sums than registers allow, for less gain.
+// 1000 fp32 800 / 322; 1 x 1000 x 256 fp32 60 / 20; distillation of 2 x 99794 x 652 fp32 with 38 entries 730 / 266.  More tokens would hold more sums than registers allow, for less gain.
 // Logits run at 5.0 TB/s (1 token) to 4.7 (4), the gradients' pass over weight and gradient at 5.6.
 #include "rps_kernels.h"
 #include "rps_lce.cuh"
@@ -111,8 +111,9 @@ template <int ROWS>
 constexpr int kResident = ROWS <= 2 ? 3 : 2;  // CTAs on an SM
 
 // A warp takes rows of the weight, all tokens' products with each at once; the hidden states lie in shared memory as fp32.  Forward: the
-// CTA's maximum and sum of exponentials of each token for rps_lce_merge_kernel; backward: dl.
-template <typename T, bool WIDE, int ROWS, bool BACKWARD>
+// CTA's maximum and sum of exponentials of each token for rps_lce_merge_kernel; backward: dl.  TOP: distillation, where a lane follows its token's entries
+// by rising row of the weight, as its rows rise.
+template <typename T, bool WIDE, int ROWS, bool BACKWARD, bool TOP>
 __global__ void __launch_bounds__(kThreads, kResident<ROWS>) rps_lce_dot_kernel(const LceParams prm)
 {
     constexpr int kR = kRowsAtATime, kValues = kR * ROWS, kPairs = kCols<T> / 2;
@@ -140,15 +141,30 @@ __global__ void __launch_bounds__(kThreads, kResident<ROWS>) rps_lce_dot_kernel(
     const bool first = lane % (32 / kValues) == 0, in = t < count;
     const int64_t token = in ? w * prm.tokens + row_of[t] : 0;
     const int64_t y = in ? prm.targets[token] : 0;
-    const int target = in && y >= 0 && y < V ? (int)y : -1;
+    const bool names_a_row = in && y >= 0 && y < V;
+    const int target = !TOP && names_a_row ? (int)y : -1;
+    const float sharpness = TOP ? prm.sharpness : 1.0f;
     float lse = 0.0f, g = 0.0f, top = -INFINITY, sum = 0.0f;
     if (BACKWARD && in) {
         lse = prm.lse_in[token];
-        g = target < 0 ? nanf("") : prm.reduction == RPS_REDUCE_NONE ? prm.dloss[token] : 1.0f;
+        g = !names_a_row ? nanf("") : prm.reduction == RPS_REDUCE_NONE ? prm.dloss[token] : 1.0f;
     }
     __syncthreads();
     const T* weight = static_cast<const T*>(prm.weight) + w * prm.weight_worker;
     const int each = (V + gridDim.x * kWarps - 1) / (gridDim.x * kWarps), start = min(V, (blockIdx.x * kWarps + warp) * each), end = min(V, start + each);
+    const int64_t entries = TOP ? token * prm.top : 0;
+    int next = TOP && in ? 0 : prm.top, next_id = 0x7FFFFFFF;
+    const auto entry = [&] { return next < prm.top ? __ldg(prm.entry_id + entries + next) : 0x7FFFFFFF; };
+    if constexpr (TOP) {
+        for (int high = prm.top; next < high;) {  // the first one of this warp's rows
+            const int middle = (next + high) / 2;
+            if (__ldg(prm.entry_id + entries + middle) < start)
+                next = middle + 1;
+            else
+                high = middle;
+        }
+        next_id = entry();
+    }
     for (int v0 = start; v0 < end; v0 += kR) {
         Pair acc[kValues];
 #pragma unroll
@@ -183,13 +199,23 @@ __global__ void __launch_bounds__(kThreads, kResident<ROWS>) rps_lce_dot_kernel(
         const int at = v0 + r;
         const float l = logit[0];
         if (at >= end) continue;
+        if constexpr (TOP) {
+            while (next_id < at) ++next, next_id = entry();  // other rows of the warp's
+        }
         if constexpr (BACKWARD) {
-            const float p = exp_of_difference(l, lse) - (at == target ? 1.0f : 0.0f);
+            float p = exp_of_difference(l, lse, kLog2e * sharpness) - (at == target ? 1.0f : 0.0f);
+            if constexpr (TOP) {
+                for (; next_id == at; ++next, next_id = entry()) p -= __ldg(prm.entry_weight + entries + next);
+            }
             if (first) prm.dot_dl[((int64_t)w * V + at) * ROWS + t] = in ? g * p : 0.0f;
         } else if (in) {
             if (at == target && first) const_cast<float*>(prm.hit)[w * prm.tokens_padded + t] = l;
+            if constexpr (TOP) {
+                for (; next_id == at; ++next, next_id = entry())
+                    if (first) const_cast<float*>(prm.entry_logit)[entries + next] = l;
+            }
             const float m = fmaxf(top, l), from = m == -INFINITY ? 0.0f : m;
-            sum = fmaf(sum, __expf(top - from), __expf(l - from));
+            sum = fmaf(sum, __expf((top - from) * sharpness), __expf((l - from) * sharpness));
             top = m;
         }
     }
@@ -201,7 +227,7 @@ __global__ void __launch_bounds__(kThreads, kResident<ROWS>) rps_lce_dot_kernel(
             for (int i = 0; i < kWarps * kR; ++i) {
                 const float2 p = statistics[i / kR][i % kR * ROWS + threadIdx.x];
                 const float m = fmaxf(top, p.x), from = m == -INFINITY ? 0.0f : m;
-                sum = sum * __expf(top - from) + p.y * __expf(p.x - from);
+                sum = sum * __expf((top - from) * sharpness) + p.y * __expf((p.x - from) * sharpness);
                 top = m;
             }
             const_cast<float2*>(prm.part)[((int64_t)w * prm.stat_tiles + blockIdx.x) * prm.tokens_padded + threadIdx.x] = make_float2(top, sum);
@@ -312,14 +338,20 @@ int chunks_of(int64_t cols)
     return (int)ceil_div(cols, kChunk<T>);
 }
 
-template <typename T, bool WIDE, int ROWS, bool BACKWARD>
+template <typename T, bool WIDE, int ROWS, bool BACKWARD, bool TOP>
 cudaError_t logits(const LceParams& prm, cudaStream_t stream)
 {
     static rps::LaunchState state;
     const size_t bytes = (size_t)ROWS * chunks_of<T>(prm.cols) * kChunk<T> * sizeof(float);
-    const cudaError_t err = rps::grant_smem(state, rps_lce_dot_kernel<T, WIDE, ROWS, BACKWARD>, (uint32_t)bytes);
+    const cudaError_t err = rps::grant_smem(state, rps_lce_dot_kernel<T, WIDE, ROWS, BACKWARD, TOP>, (uint32_t)bytes);
     if (err != cudaSuccess) return err;
-    return launch_after(rps_lce_dot_kernel<T, WIDE, ROWS, BACKWARD>, dim3((unsigned)prm.dot_blocks, (unsigned)prm.n), kThreads, bytes, stream, 1, prm);
+    return launch_after(rps_lce_dot_kernel<T, WIDE, ROWS, BACKWARD, TOP>, dim3((unsigned)prm.dot_blocks, (unsigned)prm.n), kThreads, bytes, stream, 1, prm);
+}
+
+template <typename T, bool WIDE, int ROWS, bool BACKWARD>
+cudaError_t logits(const LceParams& prm, cudaStream_t stream)
+{
+    return prm.top > 0 ? logits<T, WIDE, ROWS, BACKWARD, true>(prm, stream) : logits<T, WIDE, ROWS, BACKWARD, false>(prm, stream);
 }
 
 template <typename T, int ROWS>

@@ -76,7 +76,24 @@ LcePlan plan_lce(const rps_lce_desc& d, const void* weight, bool backward, void*
     p.hidden_row = d.hidden_row, p.hidden_worker = d.hidden_worker;
     plan.lay_out_weight = p.f32 || !aligned_matrix(weight, d.weight_row, d.weight_worker);
     p.top = top, p.factor = (float)temperature, p.sharpness = (float)(1.0 / temperature);
-    if (top == 0) plan_lce_dot(&p);
+    const auto take_teacher = [&](Carver& c) {
+        if (top == 0) return;
+        TeacherParams& t = plan.teacher;
+        ProductParams& g = plan.product;
+        t.n = p.n, t.top = top, t.tokens = p.tokens, t.vocab = p.vocab, t.sharpness = p.sharpness;
+        t.bucket_rows = (int)ceil_div(p.vocab, kTopBuckets);
+        t.entry_bucket = c.take<unsigned short>(p.n * p.tokens * kTopBuckets);
+        t.entry_id = c.take<int>(p.n * p.tokens * top);
+        t.entry_weight = c.take<float>(p.n * p.tokens * top);
+        t.targets = c.take<int64_t>(p.n * p.tokens);
+        if (!backward) {
+            t.entropy = c.take<float>(p.n * p.tokens);
+            g.entry_logit = c.take<float>(p.n * p.tokens * top);
+        }
+        g.top = top, g.bucket_rows = t.bucket_rows, g.entry_bucket = t.entry_bucket, g.sharpness = p.sharpness, g.entry_id = t.entry_id, g.entry_weight = t.entry_weight;
+        p.targets = t.targets, p.entropy = t.entropy, p.entry_id = t.entry_id, p.entry_weight = t.entry_weight, p.entry_logit = g.entry_logit;
+    };
+    plan_lce_dot(&p);
     if (p.dot_rows > 0) {
         Carver c{static_cast<unsigned char*>(workspace)};
         p.count = c.take<int>(p.n);
@@ -94,6 +111,7 @@ LcePlan plan_lce(const rps_lce_desc& d, const void* weight, bool backward, void*
             p.part = c.take<float2>(p.n * p.stat_tiles * p.tokens_padded);
             p.hit = c.take<float>(p.n * p.tokens_padded);
         }
+        take_teacher(c);
         plan.bytes = c.used;
         return plan;
     }
@@ -135,21 +153,7 @@ LcePlan plan_lce(const rps_lce_desc& d, const void* weight, bool backward, void*
         p.part = c.take<float2>(p.n * p.stat_tiles * p.tokens_padded);
         p.hit = c.take<float>(p.n * p.tokens_padded);
     }
-    if (top > 0) {
-        TeacherParams& t = plan.teacher;
-        t.n = p.n, t.top = top, t.tokens = p.tokens, t.vocab = p.vocab, t.sharpness = p.sharpness;
-        t.bucket_rows = (int)ceil_div(p.vocab, kTopBuckets);
-        t.entry_bucket = c.take<unsigned short>(p.n * p.tokens * kTopBuckets);
-        t.entry_id = c.take<int>(p.n * p.tokens * top);
-        t.entry_weight = c.take<float>(p.n * p.tokens * top);
-        t.targets = c.take<int64_t>(p.n * p.tokens);
-        if (!backward) {
-            t.entropy = c.take<float>(p.n * p.tokens);
-            g.entry_logit = c.take<float>(p.n * p.tokens * top);
-        }
-        g.top = top, g.bucket_rows = t.bucket_rows, g.entry_bucket = t.entry_bucket, g.sharpness = p.sharpness, g.entry_id = t.entry_id, g.entry_weight = t.entry_weight;
-        p.targets = t.targets, p.entropy = t.entropy, p.entry_id = t.entry_id, p.entry_weight = t.entry_weight, p.entry_logit = g.entry_logit;
-    }
+    take_teacher(c);
     plan.bytes = c.used;
 
     g.workers = p.n, g.planes = p.planes, g.count = p.count;
@@ -208,6 +212,32 @@ extern "C" int rps_lce_workspace(const rps_lce_desc* desc, const void* weight, i
 }
 
 namespace {
+
+// A few tokens, in dot products.
+int lce_dot_statistics(const rps_lce_desc& d, const LcePlan& plan, const void* weight, cudaStream_t stream)
+{
+    LceParams p = plan.p;
+    p.weight = weight, p.weight_row = d.weight_row, p.weight_worker = d.weight_worker;
+    RPS_TRY(launch_lce_dot(p, stream));
+    RPS_TRY(launch_lce_merge(p, stream));
+    return RPS_OK;
+}
+
+int lce_dot_gradients(const rps_lce_desc& d, const LcePlan& plan, const void* weight, void* dhidden, void* dweight, cudaStream_t stream)
+{
+    LceParams p = plan.p;
+    p.weight = weight, p.weight_row = d.weight_row, p.weight_worker = d.weight_worker;
+    p.dweight = dweight, p.dweight_row = d.dweight_row, p.dweight_worker = d.dweight_worker;
+    RPS_TRY(launch_lce_dot(p, stream));
+    RPS_TRY(launch_lce_dot_grads(p, stream));
+    ProductParams g{};
+    g.workers = p.n, g.planes = p.planes, g.count = p.count, g.rows = p.rows, g.tokens = p.tokens, g.scale = p.scale;
+    g.m = (int)d.tokens, g.n = (int)d.cols, g.splits = p.dot_ranges;
+    g.parts = p.dot_parts, g.part_rows = p.dot_rows, g.part_row = round_up(d.cols, 4);
+    g.out = dhidden, g.out_row = d.cols, g.out_worker = d.tokens * d.cols;
+    RPS_TRY(launch_join(Product::kDhidden, g, stream));
+    return RPS_OK;
+}
 
 // The products of a forward pass, once the plan knows its arrays and the tokens that take part have been sorted out.
 int lce_statistics(const rps_lce_desc& d, const LcePlan& plan, const void* weight, cudaStream_t stream)
@@ -274,12 +304,7 @@ extern "C" int rps_lce_forward(const rps_lce_desc* desc, const void* hidden, con
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     LceParams& p = plan.p;
     p.targets = targets, p.hidden = hidden, p.loss = loss, p.lse = lse;
-    if (p.dot_rows > 0) {
-        p.weight = weight, p.weight_row = d.weight_row, p.weight_worker = d.weight_worker;
-        RPS_TRY(launch_lce_dot(p, stream));
-        RPS_TRY(launch_lce_merge(p, stream));
-        return RPS_OK;
-    }
+    if (p.dot_rows > 0) return lce_dot_statistics(d, plan, weight, stream);
     RPS_TRY(launch_lce_rows(p, stream));
     return d.tokens == 0 ? RPS_OK : lce_statistics(d, plan, weight, stream);
 }
@@ -300,19 +325,7 @@ extern "C" int rps_lce_backward(const rps_lce_desc* desc, const void* hidden, co
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     LceParams& p = plan.p;
     p.targets = targets, p.hidden = hidden, p.lse_in = lse, p.dloss = dloss, p.dhidden = dhidden;
-    if (p.dot_rows > 0) {
-        p.weight = weight, p.weight_row = d.weight_row, p.weight_worker = d.weight_worker;
-        p.dweight = dweight, p.dweight_row = d.dweight_row, p.dweight_worker = d.dweight_worker;
-        RPS_TRY(launch_lce_dot(p, stream));
-        RPS_TRY(launch_lce_dot_grads(p, stream));
-        ProductParams g{};
-        g.workers = p.n, g.planes = p.planes, g.count = p.count, g.rows = p.rows, g.tokens = p.tokens, g.scale = p.scale;
-        g.m = (int)d.tokens, g.n = (int)d.cols, g.splits = p.dot_ranges;
-        g.parts = p.dot_parts, g.part_rows = p.dot_rows, g.part_row = round_up(d.cols, 4);
-        g.out = dhidden, g.out_row = d.cols, g.out_worker = d.tokens * d.cols;
-        RPS_TRY(launch_join(Product::kDhidden, g, stream));
-        return RPS_OK;
-    }
+    if (p.dot_rows > 0) return lce_dot_gradients(d, plan, weight, dhidden, dweight, stream);
     RPS_TRY(launch_lce_rows(p, stream));
     return lce_gradients(d, plan, weight, dhidden, dweight, stream);
 }
@@ -344,7 +357,7 @@ int sort_out(const rps_distil_desc& d, const LcePlan& plan, const int64_t* top_i
         t.ids = top_ids, t.logits = top_logits, t.top_f32 = d.top_dtype == RPS_F32, t.ignore_index = d.ignore_index;
         RPS_TRY(launch_teacher(t, stream));
     }
-    RPS_TRY(launch_lce_rows(plan.p, stream));
+    if (plan.p.dot_rows == 0) RPS_TRY(launch_lce_rows(plan.p, stream));
     return RPS_OK;
 }
 
@@ -374,6 +387,7 @@ extern "C" int rps_distil_forward(const rps_distil_desc* desc, const void* hidde
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     plan.p.hidden = hidden, plan.p.loss = loss, plan.p.lse = lse;
     if (int rc = sort_out(*desc, plan, top_ids, top_logits, stream)) return rc;
+    if (plan.p.dot_rows > 0) return lce_dot_statistics(d, plan, weight, stream);
     return d.tokens == 0 ? RPS_OK : lce_statistics(d, plan, weight, stream);
 }
 
@@ -394,6 +408,7 @@ extern "C" int rps_distil_backward(const rps_distil_desc* desc, const void* hidd
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     plan.p.hidden = hidden, plan.p.lse_in = lse, plan.p.dloss = dloss, plan.p.dhidden = dhidden;
     if (int rc = sort_out(*desc, plan, top_ids, top_logits, stream)) return rc;
+    if (plan.p.dot_rows > 0) return lce_dot_gradients(d, plan, weight, dhidden, dweight, stream);
     return lce_gradients(d, plan, weight, dhidden, dweight, stream);
 }
 

@@ -116,6 +116,30 @@ def test_sizes(ops, dtype, n, T, V, D, top):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,T,V,D,top", [(1, 1, 20000, 300, 40), (2, 2, 1000, 2049, 5), (8, 3, 5000, 64, 256), (3, 4, 777, 130, 100), (1, 5, 9000, 96, 64), (2, 8, 3000, 200, 33),
+                                         (1, 9, 3000, 200, 33)])
+def test_a_few_tokens(ops, dtype, n, T, V, D, top):
+    """Up to four of bf16 and eight of fp32 go through dot products; some without entries, words in the same entries, the vocabulary's first and last."""
+    h, w, ids, x = inputs(dtype, n, T, V, D, top, seed=T)
+    ids[:, :, 0], ids[:, :, 1], ids[:, :, 2] = V - 1, 0, V - 1
+    check(ops, dtype, h, w, ids, x, tau=1.5)
+    ids[-1, T // 2] = IGNORE
+    h[-1, T // 2] = float("nan")
+    for reduction in ("none", "sum"):
+        check(ops, dtype, h, w, ids, x, tau=0.7, reduction=reduction)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_few_tokens_with_mistakes(ops, dtype):
+    h, w, ids, x = inputs(dtype, 2, 3, 50, 16, 4, seed=1)
+    ids[1, 2, 1] = 50
+    loss, lse = ops.linear_distillation_forward(h, w, ids, x)
+    dh, dw = ops.linear_distillation_backward(torch.ones(2, device="cuda"), h, w, ids, x, lse)
+    assert torch.isfinite(loss[0]) and torch.isnan(loss[1]) and torch.isfinite(dh[0]).all() and torch.isfinite(dw[0]).all()
+    assert torch.isnan(dh[1, 2]).all() and torch.isnan(dw[1]).all() and torch.isfinite(dh[1, :2]).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("reduction", ["none", "sum", "mean"])
 @pytest.mark.parametrize("tau", [0.5, 3.0])
 def test_reductions_temperatures_and_tokens_without_entries(ops, dtype, reduction, tau):
