@@ -6,12 +6,18 @@ without one (a single worker), in float32 or bfloat16, one type for all tensors 
 into the rows of an ``[n][pitch]`` array such as ``RPS.x_dev``: only the innermost axis has to be contiguous.
 
 * ``linear_cross_entropy``: softmax cross entropy of ``hidden @ weight.T`` over a large vocabulary without keeping the logits;
+* ``linear_distillation``: the same layer's divergence from a teacher of whom each token's largest logits are kept;
+* ``embedding``: rows of a table by token, and the table's gradient by itself or added to that of an output layer that shares the table;
+* ``linear_attention``: attention whose state decays, over whole sequences; ``linear_attention_step``: one token more of each;
 * ``gated_residual_norm``: norm after a block, gate, residual scale, residual sum, norm before the next block;
 * ``pack_activation`` / ``unpack_activation`` / ``packed_weight_grad``: activations kept in 8 bits, and their use in the
   backward pass (``gated_residual_norm(..., keep="int8")``, ``linear_8bit``).
 
 The functions named ``*_forward`` and ``*_backward`` are single calls of the library; the names without a suffix are
 differentiable.  There is no CPU fallback: a missing library, a CPU tensor or a failing call raises.
+
+Calls can be captured into CUDA graphs.  A backward pass is captured best by ``torch.autograd.grad``: ``backward()`` ends in
+nodes of the leaves that belong to the stream of an earlier graph of them, if one is still alive, and PyTorch cannot capture that.
 """
 from __future__ import annotations
 
@@ -954,8 +960,11 @@ def linear_attention_backward(dout: torch.Tensor, dstate: Optional[torch.Tensor]
 def linear_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_decay: torch.Tensor, state: torch.Tensor, *, scale: Optional[float] = None,
                           new_state: Optional[torch.Tensor] = None) -> torch.Tensor:
     """``linear_attention_forward`` of one more token of every sequence (``rps_linear_attention_step``): q, k ``[n, sequences, heads, key_cols]``, v
-    with value_cols.  The state is updated in place, or written to ``new_state``, which does not overlap it, if that is given."""
+    with value_cols.  The state is updated in place, or written to ``new_state``, which does not overlap it, if that is given.  There is no gradient
+    of a step: where one is recorded, tensors that want one are refused."""
     device = _device_of(q=q, k=k, v=v, log_decay=log_decay, state=state)
+    if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad or log_decay.requires_grad or state.requires_grad):
+        raise ValueError("a step has no gradient: call it under torch.no_grad(), or linear_attention with sequences of one token")
     plan = _attention_plan(q, k, v, log_decay, state, None, float(q.shape[-1] ** -0.5 if scale is None else scale), tokens=False)
     if new_state is None:
         new_state = state
@@ -967,6 +976,7 @@ def linear_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log
         apart = abs(new_state.data_ptr() - state.data_ptr())
         if 0 < apart < 4 * state.numel():
             raise ValueError("new_state overlaps state")
+    torch.autograd.graph.increment_version(new_state)  # a gradient that still needs its old values will say so
     out = _new(plan.out, q.dtype, q.device)
     _call("rps_linear_attention_step", device, plan.desc, q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(), state.data_ptr(), out.data_ptr(),
           new_state.data_ptr(), _stream(device))

@@ -345,6 +345,30 @@ def test_arguments_are_refused(ops):
         t(q1, k1, v1, ld.detach(), room[:-4].view_as(s), new_state=room[4:].view_as(s))
 
 
+def test_a_step_records_no_gradient(ops):
+    """It is refused where one is wanted, and a gradient that needs the state from before it says so."""
+    n, B, H, K = 1, 2, 2, 8
+    q, k, v = (torch.randn(n, B, 3, H, K, device="cuda") for _ in "qkv")
+    ld, state = torch.full((n, H), -0.1, device="cuda"), torch.randn(n, B, H, K, K, device="cuda")
+    one = [t[:, :, 0] for t in (q, k, v)]
+    for i in range(3):
+        with pytest.raises(ValueError, match="no gradient"):
+            ops.linear_attention_step(*[t.clone().requires_grad_() if i == j else t for j, t in enumerate(one)], ld, state)
+    with pytest.raises(ValueError, match="no gradient"):
+        ops.linear_attention_step(*one, ld, state.clone().requires_grad_())
+    leaf = q.clone().requires_grad_()
+    out, _ = ops.linear_attention(leaf, k, v, ld, state=state)
+    other = torch.empty_like(state)
+    ops.linear_attention_step(*one, ld, state, new_state=other)
+    torch.autograd.grad(out.sum(), leaf, retain_graph=True)
+    with torch.no_grad():
+        ops.linear_attention_step(leaf[:, :, 0], *one[1:], ld, state)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        torch.autograd.grad(out.sum(), leaf)
+    with torch.inference_mode():
+        ops.linear_attention_step(*one, ld, state.clone())
+
+
 @pytest.mark.parametrize("backward", [False, True])
 @pytest.mark.parametrize("T,K,W", [(100, 64, 64), (3000, 128, 128), (5000, 40, 72)])
 def test_a_wait_that_runs_out_is_reported(ops, backward, T, K, W):
