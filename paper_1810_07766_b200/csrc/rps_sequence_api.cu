@@ -17,7 +17,7 @@ int check_embed(const rps_embed_desc* d)
     if (d->tokens < 0 || d->tokens > kMaxSize || d->n * d->tokens >= 1ll << 31) return fail(RPS_EINVAL, "tokens = %lld", (long long)d->tokens);
     if (d->vocab < 1 || d->vocab >= 1ll << 30) return fail(RPS_EINVAL, "vocab = %lld", (long long)d->vocab);
     if (d->cols < 1 || d->cols > kMaxSize) return fail(RPS_EINVAL, "cols = %lld", (long long)d->cols);
-    if (!std::isfinite(d->scale)) return fail(RPS_EINVAL, "scale = %g", d->scale);
+    if (!std::isfinite((float)d->scale)) return fail(RPS_EINVAL, "scale = %g", d->scale);
     return RPS_OK;
 }
 
@@ -101,7 +101,7 @@ int check_attention(const rps_linear_attention_desc* d)
                     (int)RPS_MAX_HEAD_COLS);
     for (const rps_axis_strides* s : {&d->q, &d->k, &d->v, &d->dout})
         if (s->worker < 0 || s->sequence < 0 || s->token < 0 || s->head < 0) return fail(RPS_EINVAL, "a negative stride");
-    if (!std::isfinite(d->scale)) return fail(RPS_EINVAL, "scale = %g", d->scale);
+    if (!std::isfinite((float)d->scale)) return fail(RPS_EINVAL, "scale = %g", d->scale);
     return RPS_OK;
 }
 

@@ -192,3 +192,10 @@ def test_distillation_refuses_cpu_tensors():
     h, w, ids = torch.zeros(4, 8), torch.zeros(6, 8), torch.zeros(4, 2, dtype=torch.int64)
     with pytest.raises(ValueError, match="CUDA"):
         ops.linear_distillation(h, w, ids, torch.zeros(4, 2))
+
+
+def test_scales_beyond_fp32_are_refused(lib):
+    size = ctypes.c_size_t()
+    for scale, status in ((3.4e38, 0), (1e39, -1), (-1e300, -1)):
+        assert lib.rps_embed_workspace(ctypes.byref(embed_desc(scale=scale)), ctypes.byref(size)) == status
+        assert lib.rps_linear_attention_workspace(ctypes.byref(attention_desc(scale=scale)), 0, ctypes.byref(size)) == status
