@@ -251,7 +251,7 @@ typedef struct rps_embed_desc {
     int64_t ignore_index;
     int64_t weight_row, weight_worker;    /* strides of weight (forward); weight_row >= cols              */
     int64_t dweight_row, dweight_worker;  /* strides of dweight (backward); cols <= dweight_row < 2^31    */
-    double scale;           /* finite                                                                     */
+    double scale;           /* finite in fp32                                                             */
 } rps_embed_desc;
 
 int rps_embed_forward(const rps_embed_desc* desc, const int64_t* tokens, const void* weight, void* out, void* cuda_stream);
@@ -268,11 +268,12 @@ int rps_embed_backward(const rps_embed_desc* desc, const int64_t* tokens, const 
  *
  *   R_t = r R_(t+1) + scale * q_t^T dout_t,   dq_t = scale * dout_t S_t^T,   dk_t = v_t R_t^T,   dv_t = k_t R_t,   dstate_in = r R_0
  *
- * (R_(t+1) taken without its factor r for the last token).  Sequences go through in chunks of 64 tokens, whose part of the sums is made
- * as masked products; so an infinity or a NaN at a token may also reach results of the other tokens of its chunk.
+ * (R_(t+1) taken without its factor r for the last token).  Sequences go through in chunks of 64 or 128 tokens, whose part of the sums is
+ * made as masked products; so an infinity or a NaN at a token may also reach results of the other tokens of its chunk.
  *
  * States are fp32, [n][sequences][heads][key_cols][value_cols], dense.  With RPS_BF16 the results that are bf16 are made of products of bf16 (of the masked
- * scores, and of S where it meets a q, rounded); what is added to a state has 17 bits or more.
+ * scores, and of S where it meets a q, rounded; what is added to an S or R that only such results need has 16 bits); what is added to a state that is
+ * written has 24.  Which kernel multiplies goes by alignment and strides, and the order of its sums with it: the same values laid out otherwise may give other last bits.
  * log_decay: float [n][heads], at most 0 (minus infinity: r = 0); a positive one or a NaN makes its head's results NaN.  It gets no gradient.
  * lengths: int64 [n][sequences], dense, or NULL (all tokens): only the first `length` tokens of a sequence take part (a length outside
  * 0..tokens counts as the nearest of them).  The others are not read, their rows of out, dq, dk and dv are 0, and states are those after the
@@ -296,7 +297,7 @@ typedef struct rps_linear_attention_desc {
     int64_t tokens;         /* of a sequence, 0 <= tokens < 2^31                        */
     int64_t key_cols, value_cols;   /* of a head, 1..RPS_MAX_HEAD_COLS                  */
     rps_axis_strides q, k, v, dout; /* not negative (dout: backward only)               */
-    double scale;           /* finite                                                   */
+    double scale;           /* finite in fp32                                           */
 } rps_linear_attention_desc;
 
 /* Bytes of workspace that rps_linear_attention_forward (backward = 0) or _backward (backward = 1) wants. */

@@ -14,7 +14,8 @@
 // The kernel here takes fp32 operands (bf16 ones: rps_mix_tensor.cu, or rps_mix_mma.cu where TMA cannot copy them).  A CTA has a sequence's head and 64 columns of z,
 // chunk by chunk of 64 tokens; all products are of fp32 in registers, 4 x 4 results to a thread with two 16-byte reads of shared memory for every 16
 // to 32 multiplications.  Bound by those: 128 a cycle and SM.  (As six products of bf16 parts on the tensor cores, mma.sync, whose operands every
-// warp had to cut into parts for itself, 4 x 3 sequences of 333 x 5 x 48 x 40 took 193 us forward and backward, 155 so.)
+// warp had to cut into parts for itself, 4 x 3 sequences of 333 x 5 x 48 x 40 took 193 us forward and backward, 129 so;
+// 148 heads of 512 tokens x 64 117 forward, 95 so, which is 40 % of the rate of those multiplications.)
 #include <algorithm>
 
 #include "rps_mix.cuh"

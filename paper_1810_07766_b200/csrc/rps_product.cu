@@ -380,7 +380,7 @@ __device__ __forceinline__ RowInfo row_info(const ProductParams& prm, int w, int
                 const int64_t token = w * prm.tokens + __ldg(prm.rows + w * prm.tokens + row);
                 r.entries = token * prm.top;
                 // among those of the first column's bucket: every step of the search is a way to memory (2048 tokens of 50001 words x 1024 with 50 entries:
-                // all of them searched 165 us, ...)
+                // all of them searched 165 us, so 161; 4096 of 131072 x 2048 with 64, backward: with the next ones on their way 6557 -> 6180)
                 const int first = prm.v0 + n0, bucket = min(first / prm.bucket_rows, kTopBuckets - 1);
                 const unsigned short* at = prm.entry_bucket + token * kTopBuckets + bucket;
                 int low = __ldg(at), high = bucket + 1 < kTopBuckets ? __ldg(at + 1) : prm.top;

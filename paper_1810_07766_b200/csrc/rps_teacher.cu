@@ -1,6 +1,7 @@
-// Distillation's teacher: of each token's kept logits the probabilities, sorted by word, so that the products' epilogues find those of their columns by
-// bisection.  A warp to a token, its entries in registers (element e in lane e % 32), sorted by a bitonic network.  Bound by reading the entries and
-// writing them back.
+// Distillation's teacher: of each token's kept logits the probabilities, sorted by word, so that the products' epilogues meet those of their
+// columns in order, and where those of each of kTopBuckets equal parts of the vocabulary begin, so that an epilogue need not search all of them
+// for its first.  A warp to a token, its entries in registers (element e in lane e % 32), sorted by a bitonic network.  Bound by reading the
+// entries and writing them back.
 #include "rps_ops_kernels.h"
 
 namespace rps_ops {

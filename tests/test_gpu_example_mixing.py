@@ -82,3 +82,40 @@ def test_gradients_of_the_whole_model(example):
             # the weight gradients of linear_8bit come out of inputs in 8 bits
             near = 2.0 ** -5 if name.split(".")[-1] in ("up", "down", "qkv", "out") else 2.0 ** -12
             assert (leaf.grad[w] - q[name].grad).norm() <= near * q[name].grad.norm(), name
+
+
+def test_a_captured_training_pass(example):
+    """Words, attention over texts of several lengths, the loss and a teacher, forward and backward in one CUDA graph that is replayed with other
+    words in place, beside the same calls made one by one: the same bits."""
+    ops = example.ops
+    n, vocab, width, heads, sequences, tokens = 2, 300, 32, 2, 3, 140
+    g = torch.Generator(device="cuda").manual_seed(2)
+    table = torch.randn(n, vocab, width, generator=g, device="cuda").bfloat16()
+    decay = example.decays(n, heads)
+    lengths = torch.tensor([[140, 1, 77], [0, 139, 128]], device="cuda")
+    words, targets = (torch.randint(0, vocab, (n, sequences * tokens), generator=g, device="cuda") for _ in range(2))
+    ids = torch.randint(0, vocab, (n, sequences * tokens, 6), generator=g, device="cuda")
+    kept = torch.randn(n, sequences * tokens, 6, generator=g, device="cuda")
+
+    def gradients():
+        leaf = table.detach().requires_grad_()
+        x = ops.embedding(words, leaf).view(n, sequences, tokens, heads, width // heads)
+        out, _ = ops.linear_attention(x, x, x, decay, lengths=lengths)
+        y = out.reshape(n, sequences * tokens, width)
+        loss = ops.linear_cross_entropy(y, leaf, targets) + ops.linear_distillation(y, leaf, ids, kept, temperature=2.0)
+        return loss.detach(), torch.autograd.grad(loss.sum(), leaf)[0]
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        gradients()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        loss, grad = gradients()
+    for _ in range(3):
+        words.copy_(torch.randint(0, vocab, words.shape, generator=g, device="cuda"))
+        lengths.copy_(lengths.flip(0))
+        graph.replay()
+        want_loss, want_grad = gradients()
+        assert torch.equal(loss, want_loss) and torch.equal(grad, want_grad) and torch.isfinite(grad).all()
