@@ -279,7 +279,8 @@ int rps_embed_backward(const rps_embed_desc* desc, const int64_t* tokens, const 
  * 0..tokens counts as the nearest of them).  The others are not read, their rows of out, dq, dk and dv are 0, and states are those after the
  * last token that takes part.
  * q, k, v and dout are [n][sequences][tokens][heads][cols] at any strides of the outer axes (parts of one projection's output, say); out, dq,
- * dk and dv are dense in this order.  sequences and tokens may be 0.
+ * dk and dv are dense in this order.  sequences and tokens may be 0.  (With RPS_BF16, columns and strides in eights and 16-byte aligned addresses
+ * are read as they lie; of other arrays of longer sequences copies are made in the workspace first.)
  * ------------------------------------------------------------------------------------------------------------------ */
 typedef struct rps_axis_strides {
     int64_t worker, sequence, token, head;

@@ -11,7 +11,7 @@
 // Where there are too few heads of sequences to fill the SMs, sequences are cut into segments: one launch makes each segment's own sum of y^T z,
 // one adds them up in order into the states that segments begin with, and the main one then runs all segments at once (y and z are read twice).
 //
-// The kernel here takes fp32 operands (bf16 ones: rps_mix_tensor.cu, or rps_mix_mma.cu where TMA cannot copy them).  A CTA has a sequence's head and 64 columns of z,
+// The kernel here takes fp32 operands (bf16 ones: rps_mix_tensor.cu; where TMA cannot copy them, copies of theirs, or in short sequences rps_mix_mma.cu).  A CTA has a sequence's head and 64 columns of z,
 // chunk by chunk of 64 tokens; all products are of fp32 in registers, 4 x 4 results to a thread with two 16-byte reads of shared memory for every 16
 // to 32 multiplications.  Bound by those: 128 a cycle and SM.  (As six products of bf16 parts on the tensor cores, mma.sync, whose operands every
 // warp had to cut into parts for itself, 4 x 3 sequences of 333 x 5 x 48 x 40 took 193 us forward and backward, 129 so;
@@ -287,7 +287,8 @@ __global__ void __launch_bounds__(kJoinThreads) rps_mix_join_kernel(const __grid
     __syncthreads();
     if (e >= term.a * term.b) return;
     float* slot = prm.segment_states + (blockIdx.y * prm.units + unit) * prm.segments * prm.state_room + e;
-    float w = term.state_in != nullptr ? __ldg(term.state_in + unit * term.a * term.b + row * term.state_a + col * term.state_b) : 0.0f;
+    const bool there = term.state_in != nullptr && row < term.rows && col < term.cols;
+    float w = there ? __ldg(term.state_in + unit * term.rows * term.cols + row * term.state_a + col * term.state_b) : 0.0f;
     slot[0] = w;
     for (int s0 = 0; s0 + 1 < prm.segments; s0 += 8) {
         float own[8];
@@ -371,7 +372,131 @@ __global__ void __launch_bounds__(kStepThreads) rps_mix_step_kernel(const __grid
     }
 }
 
+// ------------------------------------------------------------------------------------------------------------ copies
+// Rows of bf16 into another layout: columns past `from_cols` become zeros, those past `to_cols` are left out.
+struct MixMove {
+    MixOperand from, to;
+    int from_cols, to_cols, from_pairs, to_pairs;  // pairs: two columns lie within 4 aligned bytes
+};
+
+struct MixMoves {
+    MixMove move[4];
+    int count, log_across;  // 2^log_across threads to a row, two columns to a thread
+    int64_t blocks;         // CTAs of a sequence's tokens
+    int head_blocks;
+    bool all;               // tokens that take no part as well
+};
+
+constexpr int kMoveThreads = 256, kMoveTokens = 4, kMoveHeads = 4;  // of a thread, all under way at once
+
+__global__ void __launch_bounds__(kMoveThreads) rps_mix_move_kernel(const __grid_constant__ MixParams prm, const __grid_constant__ MixMoves moves)
+{
+    after_the_kernel_before();
+    const MixMove& m = moves.move[blockIdx.y];
+    const int64_t part = blockIdx.x / moves.head_blocks, s = part / moves.blocks;
+    const int h0 = (int)(blockIdx.x - part * moves.head_blocks) * kMoveHeads, heads = min(kMoveHeads, prm.heads - h0);
+    const int c = (threadIdx.x & ((1 << moves.log_across) - 1)) * 2, down = kMoveThreads >> moves.log_across;
+    const Place at = place_of(prm, s * prm.heads + h0);
+    const int64_t t0 = (part - s * moves.blocks) * down * kMoveTokens + (threadIdx.x >> moves.log_across), limit = moves.all ? prm.tokens : at.length;
+    if (c >= m.to_cols) return;
+    const bf16* const from = first_token<bf16>(m.from, at) + t0 * m.from.token + c;
+    bf16* const to = const_cast<bf16*>(first_token<bf16>(m.to, at)) + t0 * m.to.token + c;
+    uint32_t v[kMoveTokens][kMoveHeads], next[kMoveTokens][kMoveHeads];
+    const auto load = [&](uint32_t(&to)[kMoveTokens][kMoveHeads], const auto* first, bool there) {
+#pragma unroll
+        for (int i = 0; i < kMoveTokens; ++i)
+#pragma unroll
+            for (int h = 0; h < kMoveHeads; ++h) {
+                const auto* p = first + ((int64_t)i * down * m.from.token + h * m.from.head) * (int64_t)sizeof(bf16) / (int64_t)sizeof(*first);
+                to[i][h] = there && t0 + i * down < limit && h < heads ? __ldg(p) : 0;
+            }
+    };
+    if (m.from_pairs) {
+        load(v, reinterpret_cast<const uint32_t*>(from), c < m.from_cols);
+    } else {
+        load(v, reinterpret_cast<const unsigned short*>(from), c < m.from_cols), load(next, reinterpret_cast<const unsigned short*>(from) + 1, c + 1 < m.from_cols);
+#pragma unroll
+        for (int i = 0; i < kMoveTokens; ++i)
+#pragma unroll
+            for (int h = 0; h < kMoveHeads; ++h) v[i][h] |= next[i][h] << 16;
+    }
+#pragma unroll
+    for (int i = 0; i < kMoveTokens; ++i)
+#pragma unroll
+        for (int h = 0; h < kMoveHeads; ++h) {
+            bf16* p = to + (int64_t)i * down * m.to.token + h * m.to.head;
+            if (t0 + i * down >= limit || h >= heads) continue;
+            if (m.to_pairs) {
+                *reinterpret_cast<uint32_t*>(p) = v[i][h];
+            } else {
+                *reinterpret_cast<unsigned short*>(p) = (unsigned short)v[i][h];
+                if (c + 1 < m.to_cols) reinterpret_cast<unsigned short*>(p)[1] = (unsigned short)(v[i][h] >> 16);
+            }
+        }
+}
+
 // -------------------------------------------------------------------------------------------------------------- host
+cudaError_t launch_moves(const MixParams& prm, MixMoves& moves, cudaStream_t stream)
+{
+    if (moves.count == 0) return cudaSuccess;
+    int widest = 0;
+    for (int i = 0; i < moves.count; ++i) {
+        MixMove& m = moves.move[i];
+        const auto pairs = [&](const MixOperand& o, int cols) { return alignment<bf16>(o.base, cols, o.token | o.head | o.sequence | o.worker) >= 4; };
+        m.from_pairs = pairs(m.from, m.from_cols), m.to_pairs = pairs(m.to, m.to_cols);
+        widest = std::max(widest, m.to_cols);
+    }
+    moves.log_across = 0;
+    while (2 << moves.log_across < widest) ++moves.log_across;
+    moves.blocks = ceil_div(prm.tokens, (kMoveThreads >> moves.log_across) * kMoveTokens);
+    moves.head_blocks = (int)ceil_div(prm.heads, kMoveHeads);
+    return launch_after(rps_mix_move_kernel, dim3((unsigned)(prm.n * prm.sequences * moves.blocks * moves.head_blocks), (unsigned)moves.count), kMoveThreads, 0, stream, 1,
+                        prm, moves);
+}
+
+// Of the terms of a call the arrays that are distinct: a forward call's x, y, z, and a backward one's (dout, v, k), (v, dout, q), (k, q, dout).
+constexpr int kOperands[3][3] = {{0, 1, 2}, {1, 0, 3}, {2, 3, 0}};
+
+// `p` with copies that TMA can copy in place of what it cannot, and how they are made; the bytes that they take.
+size_t with_copies(MixParams* prm, MixMoves* in, MixMoves* out)
+{
+    MixParams& p = *prm;
+    const int64_t rows = p.n * p.sequences * p.tokens * p.heads;
+    unsigned char* at = p.copies;
+    size_t bytes = 0;
+    const auto dense = [&](const void* base, int64_t cols) -> MixOperand {
+        return {base, p.sequences * p.tokens * p.heads * cols, p.tokens * p.heads * cols, p.heads * cols, cols};
+    };
+    const auto room = [&](int cols) {
+        const MixOperand o = dense(at == nullptr ? nullptr : at + bytes, round_up(cols, 8));
+        bytes += round_up(rows * round_up(cols, 8) * 2, 256);
+        return o;
+    };
+    MixOperand copy[4];
+    bool copied[4] = {}, known[4] = {};
+    in->count = out->count = 0, in->all = false, out->all = true;
+    for (int i = 0; i < p.terms; ++i) {
+        MixTerm& t = p.term[i];
+        MixOperand* const operands[3] = {&t.x, &t.y, &t.z};
+        for (int j = 0; j < 3; ++j) {
+            const int which = kOperands[i][j], cols = j < 2 ? t.a : t.b;
+            MixOperand& o = *operands[j];
+            if (!known[which]) {
+                known[which] = true, copied[which] = !mix_fits_tensor(p, o, cols);
+                if (copied[which]) copy[which] = room(cols), in->move[in->count++] = {o, copy[which], cols, (int)round_up(cols, 8)};
+            }
+            if (copied[which]) o = copy[which];
+        }
+        if (t.b % 8 != 0) {
+            const MixOperand o = room(t.b);
+            out->move[out->count++] = {o, dense(t.out, t.b), (int)round_up(t.b, 8), t.b};
+            t.out = const_cast<void*>(o.base);
+        }
+        t.a = (int)round_up(t.a, 8), t.b = (int)round_up(t.b, 8);
+    }
+    return bytes;
+}
+
 cudaError_t launch_join(const MixParams& prm, cudaStream_t stream)
 {
     return launch_after(rps_mix_join_kernel, dim3((unsigned)(prm.units * prm.join_blocks), (unsigned)prm.terms), kJoinThreads, 0, stream, 1, prm);
@@ -404,6 +529,11 @@ cudaError_t launch_f32(const MixParams& prm, bool states, cudaStream_t stream)
 
 }  // namespace
 
+// From so many tokens of a sequence on, bf16 arrays that TMA cannot copy as they lie go by way of copies that it can, for the tensor cores' fifth
+// generation.  By way of copies / as they lie (us): 64 sequences of 16 x 61, 64 tokens 99 / 57 forward, 321 / 205 with backward; 128 tokens 121 / 107,
+// 375 / 431; 256 tokens 177 / 230, 545 / 863; 27 of 212 tokens x 18 x (14, 117) 115 / 113, 318 / 446; 2 of 3841 x 14 x (85, 98) 125 / 347, 345 / 1361.
+int64_t copied_tokens(const MixParams& prm) { return prm.terms == 1 ? 193 : 128; }
+
 // Sequences are cut into as many segments as take the least time by this count, in microseconds: a round of CTAs takes 6 to begin and end with and
 // for each 128 tokens, as measured, on the tensor cores 4 (2.8 to 4.7); in fp32 37, or with up to 64 columns, where two CTAs share an SM, 21 for one
 // and 35 for both; the segments' own sums, made first, 0.6 of that; joining them 6.
@@ -415,6 +545,13 @@ void plan_mix(MixParams* prm)
     for (int i = 0; i < p.terms; ++i) {
         p.columns = std::max(p.columns, (int)ceil_div(p.term[i].b, kTile));
         p.state_room = std::max<int64_t>(p.state_room, round_up(p.term[i].a * p.term[i].b, 4));
+    }
+    if (!p.f32 && p.tokens < 1ll << 30 && p.tokens >= copied_tokens(p)) {
+        MixParams q = p;
+        MixMoves in, out;
+        q.copies = nullptr;
+        p.copies_bytes = with_copies(&q, &in, &out);
+        for (int i = 0; i < q.terms; ++i) p.state_room = std::max<int64_t>(p.state_room, q.term[i].a * q.term[i].b);
     }
     p.join_blocks = (int)ceil_div(p.state_room, kJoinThreads);
     const int64_t chunks = std::max<int64_t>(1, ceil_div(p.tokens, kMixTensorChunk)), ctas = p.units * p.terms * (p.f32 ? p.columns : 1);
@@ -439,14 +576,21 @@ void plan_mix(MixParams* prm)
 cudaError_t launch_mix(const MixParams& prm, cudaStream_t stream)
 {
     MixParams p = prm;
+    MixMoves in, out;
+    in.count = out.count = 0;
+    if (p.copies_bytes > 0) {
+        with_copies(&p, &in, &out);
+        if (!mix_fits_tensor(p)) p = prm, in.count = out.count = 0;  // what needs no copy lies at an odd address
+    }
     p.tensor = !p.f32 && mix_fits_tensor(p);
     const auto launch = p.f32 ? launch_f32 : p.tensor ? launch_mix_tensor : launch_mix_mma;
-    if (p.segments > 1) {
-        cudaError_t err = launch(p, true, stream);
+    cudaError_t err = launch_moves(p, in, stream);
+    if (err == cudaSuccess && p.segments > 1) {
+        err = launch(p, true, stream);
         if (err == cudaSuccess) err = launch_join(p, stream);
-        if (err != cudaSuccess) return err;
     }
-    return launch(p, false, stream);
+    if (err == cudaSuccess) err = launch(p, false, stream);
+    return err == cudaSuccess ? launch_moves(p, out, stream) : err;
 }
 
 cudaError_t launch_mix_step(const MixParams& prm, cudaStream_t stream)

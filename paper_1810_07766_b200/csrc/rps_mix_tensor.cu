@@ -483,10 +483,10 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
                 warp_arrive(control.state_read);
                 warp_wait(control.state_read, 0);
             }
-        } else if (way_in == kByElement && row < a) {
+        } else if (way_in == kByElement && row < term.rows) {
 #pragma unroll
             for (int j = 0; j < 32; ++j)
-                if (j < width && col0 + j < b) w[j] = __ldg(term.state_in + unit * a * b + row * term.state_a + (col0 + j) * term.state_b);
+                if (j < width && col0 + j < term.cols) w[j] = __ldg(term.state_in + unit * term.rows * term.cols + row * term.state_a + (col0 + j) * term.state_b);
         }
         const auto publish = [&] {  // W where the products read it
             if (there) {
@@ -602,10 +602,10 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
             }
             writes_done();
             warp_arrive(control.state_out);
-        } else if (way_out == kByElement && fine && row < a) {
+        } else if (way_out == kByElement && fine && row < term.rows) {
 #pragma unroll
             for (int j = 0; j < 32; ++j)
-                if (j < width && col0 + j < b) term.state_out[unit * a * b + row * term.state_a + (col0 + j) * term.state_b] = w[j];
+                if (j < width && col0 + j < term.cols) term.state_out[unit * term.rows * term.cols + row * term.state_a + (col0 + j) * term.state_b] = w[j];
         }
     }
     if (!fine) atomicExch(&g_gave_up, 1);
@@ -617,13 +617,7 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
 }
 
 // -------------------------------------------------------------------------------------------------------------- host
-// Whether TMA can copy an operand as it lies: axes of more than one element need strides that are multiples of 16 bytes (and not zero).
-bool fits(const MixParams& prm, const MixOperand& o, int cols)
-{
-    const auto stride = [](int64_t size, int64_t step) { return size <= 1 || (step > 0 && step % 8 == 0 && step < 1ll << 38); };
-    return cols % 8 == 0 && reinterpret_cast<uintptr_t>(o.base) % 16 == 0 && stride(prm.tokens, o.token) && stride(prm.heads, o.head) && stride(prm.sequences, o.sequence) &&
-           stride(prm.n, o.worker);
-}
+bool fits(const MixParams& prm, const MixOperand& o, int cols) { return reinterpret_cast<uintptr_t>(o.base) % 16 == 0 && mix_fits_tensor(prm, o, cols); }
 
 bool encode(CUtensorMap* map, const MixParams& prm, const MixOperand& o, int cols)
 {
@@ -667,6 +661,13 @@ cudaError_t launch(const MixParams& prm, const MixMaps& maps, cudaStream_t strea
 
 }  // namespace
 
+// Whether TMA can copy an operand as it lies: axes of more than one element need strides that are multiples of 16 bytes (and not zero).
+bool mix_fits_tensor(const MixParams& prm, const MixOperand& o, int cols)
+{
+    const auto stride = [](int64_t size, int64_t step) { return size <= 1 || (step > 0 && step % 8 == 0 && step < 1ll << 38); };
+    return cols % 8 == 0 && stride(prm.tokens, o.token) && stride(prm.heads, o.head) && stride(prm.sequences, o.sequence) && stride(prm.n, o.worker);
+}
+
 bool mix_fits_tensor(const MixParams& prm)
 {
     if (prm.tokens < 1 || prm.tokens >= 1ll << 30) return false;
@@ -688,7 +689,8 @@ cudaError_t launch_mix_tensor(const MixParams& prm, bool states, cudaStream_t st
         const bool segmented = prm.segments > 1;
         const int64_t all = prm.terms * prm.units * prm.segments, each = (int64_t)t.a * t.b;
         const auto state = [&](int which, bool in_segments, const float* at) {
-            maps.way[i][which] = at == nullptr ? kNoState : in_segments || (t.state_b == 1 && reinterpret_cast<uintptr_t>(at) % 16 == 0) ? kCopied : kByElement;
+            const bool dense = t.state_b == 1 && t.rows == t.a && t.cols == t.b;
+            maps.way[i][which] = at == nullptr ? kNoState : in_segments || (dense && reinterpret_cast<uintptr_t>(at) % 16 == 0) ? kCopied : kByElement;
             return maps.way[i][which] != kCopied || encode_state(&maps.state[i][which], at, t.a, t.b, in_segments ? all : prm.units, in_segments ? prm.state_room : each);
         };
         if (!state(0, segmented, states ? nullptr : segmented ? prm.segment_states : t.state_in) || !state(1, states, states ? prm.segment_states : t.state_out))

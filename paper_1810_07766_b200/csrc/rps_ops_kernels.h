@@ -269,6 +269,7 @@ struct MixTerm {
     float* state_out;       // or NULL
     int64_t state_a, state_b;  // strides of the states' elements
     float score_scale, state_scale, update_scale;  // of x . y, of x W, and of what is added to W
+    int rows, cols;         // of the states: a and b, but where a and b are columns of copies (plan_mix)
 };
 
 struct MixParams {
@@ -282,10 +283,13 @@ struct MixParams {
     int64_t units, segment_tokens, state_room;  // segment_tokens: a multiple of kMixTensorChunk
     int columns, segments, join_blocks, tensor;
     float* segment_states;    // [term][unit][segment][state_room] (segments > 1)
+    size_t copies_bytes;      // of copies of the operands and results that TMA cannot copy as they lie, with columns in eights (0: none are made)
+    unsigned char* copies;
 };
 void plan_mix(MixParams* prm);
 cudaError_t launch_mix(const MixParams& prm, cudaStream_t stream);
 bool mix_fits_tensor(const MixParams& prm);  // whether rps_mix_tensor.cu takes it
+bool mix_fits_tensor(const MixParams& prm, const MixOperand& o, int cols);  // an operand, at a 16-byte aligned address
 cudaError_t launch_mix_tensor(const MixParams& prm, bool states, cudaStream_t stream);  // states: the segments' own sums
 cudaError_t launch_mix_mma(const MixParams& prm, bool states, cudaStream_t stream);     // bf16 that it does not
 cudaError_t read_mix_gave_up(int* value, cudaStream_t stream);

@@ -122,7 +122,7 @@ MixParams forward_params(const rps_linear_attention_desc& d, const void* q, cons
     MixParams p = mix_params(d, log_decay, lengths);
     const float scale = (float)d.scale;
     p.terms = 1;
-    p.term[0] = {operand(q, d.q), operand(k, d.k), operand(v, d.v), out, (int)d.key_cols, (int)d.value_cols, 0, state_in, state_out, d.value_cols, 1, scale, scale, 1.0f};
+    p.term[0] = {operand(q, d.q), operand(k, d.k), operand(v, d.v), out, (int)d.key_cols, (int)d.value_cols, 0, state_in, state_out, d.value_cols, 1, scale, scale, 1.0f, (int)d.key_cols, (int)d.value_cols};
     plan_mix(&p);
     return p;
 }
@@ -134,9 +134,9 @@ MixParams backward_params(const rps_linear_attention_desc& d, const void* dout, 
     const float scale = (float)d.scale;
     const int kc = (int)d.key_cols, vc = (int)d.value_cols;
     p.terms = 3;
-    p.term[0] = {operand(dout, d.dout), operand(v, d.v), operand(k, d.k), dq, vc, kc, 0, state_in, nullptr, 1, vc, scale, scale, 1.0f};
-    p.term[1] = {operand(v, d.v), operand(dout, d.dout), operand(q, d.q), dk, vc, kc, 1, dstate_out, nullptr, 1, vc, scale, 1.0f, scale};
-    p.term[2] = {operand(k, d.k), operand(q, d.q), operand(dout, d.dout), dv, kc, vc, 1, dstate_out, dstate_in, vc, 1, scale, 1.0f, scale};
+    p.term[0] = {operand(dout, d.dout), operand(v, d.v), operand(k, d.k), dq, vc, kc, 0, state_in, nullptr, 1, vc, scale, scale, 1.0f, vc, kc};
+    p.term[1] = {operand(v, d.v), operand(dout, d.dout), operand(q, d.q), dk, vc, kc, 1, dstate_out, nullptr, 1, vc, scale, 1.0f, scale, vc, kc};
+    p.term[2] = {operand(k, d.k), operand(q, d.q), operand(dout, d.dout), dv, kc, vc, 1, dstate_out, dstate_in, vc, 1, scale, 1.0f, scale, kc, vc};
     plan_mix(&p);
     return p;
 }
@@ -145,6 +145,7 @@ size_t mix_workspace(MixParams* p, void* workspace)
 {
     Carver c{static_cast<unsigned char*>(workspace)};
     if (p->segments > 1) p->segment_states = c.take<float>(p->terms * p->units * p->segments * p->state_room);
+    if (p->copies_bytes > 0) p->copies = c.take<unsigned char>(p->copies_bytes);
     return c.used;
 }
 

@@ -127,6 +127,29 @@ def test_lengths(ops, dtype, T):
     assert (got["state"][0, 1] == 0).all() and (got["dstate"][1, 3] == 0).all()
 
 
+@pytest.mark.parametrize("K,W", [(33, 40), (40, 33), (85, 98), (1, 127), (120, 2)])
+@pytest.mark.parametrize("T", [129, 192, 193, 700])
+def test_columns_that_are_not_in_eights(ops, K, W, T):
+    """bf16 heads of odd sizes in sequences of several lengths, as dense arrays, as parts of a projection's output, and at an odd address: whether
+    copies are made of some, of all or of none of them, the rows behind a sequence are not read and those of results are zeros."""
+    n, B, H = 2, 3, 5
+    x = inputs("bf16", n, B, T, H, K, W, seed=T)
+    lengths = torch.tensor([[T, 0, 1], [128, T - 1, 130]], device="cuda")
+    for name in ("q", "k", "v", "dout"):
+        x[name][(torch.arange(T, device="cuda") >= lengths[:, :, None])] = float("nan")
+    check(ops, x, lengths=lengths)
+    room = torch.full((n * B * T * H * (2 * K + W + 3) + 1,), float("nan"), dtype=torch.bfloat16, device="cuda")
+    for shift in (0, 1):
+        joint = room[shift:room.numel() - 1 + shift].view(n, B, T, H, 2 * K + W + 3)
+        y = dict(x, q=joint[..., :K], k=joint[..., K:2 * K], v=joint[..., 2 * K:2 * K + W])
+        for name in ("q", "k", "v"):
+            y[name].copy_(x[name])
+        check(ops, y, lengths=lengths)
+    one = room[1:1 + x["v"].numel()].view_as(x["v"])
+    one.copy_(x["v"])
+    check(ops, dict(x, v=one, state=None, dstate=None), lengths=lengths)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_no_tokens_and_no_sequences(ops, dtype):
     x = inputs(dtype, 2, 3, 0, 2, 16, 8)
