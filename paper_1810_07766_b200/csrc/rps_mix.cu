@@ -11,11 +11,12 @@
 // Where there are too few heads of sequences to fill the SMs, sequences are cut into segments: one launch makes each segment's own sum of y^T z,
 // one adds them up in order into the states that segments begin with, and the main one then runs all segments at once (y and z are read twice).
 //
-// The kernel here takes fp32 operands (bf16 ones: rps_mix_tensor.cu; where TMA cannot copy them, copies of theirs, or in short sequences rps_mix_mma.cu).  A CTA has a sequence's head and 64 columns of z,
-// chunk by chunk of 64 tokens; all products are of fp32 in registers, 4 x 4 results to a thread with two 16-byte reads of shared memory for every 16
-// to 32 multiplications.  Bound by those: 128 a cycle and SM.  (As six products of bf16 parts on the tensor cores, mma.sync, whose operands every
-// warp had to cut into parts for itself, 4 x 3 sequences of 333 x 5 x 48 x 40 took 193 us forward and backward, 129 so;
-// 148 heads of 512 tokens x 64 117 forward, 95 so, which is 40 % of the rate of those multiplications.)
+// The kernel here takes fp32 operands (bf16 ones: rps_mix_tensor.cu; where TMA cannot copy them, copies of theirs, or in short sequences
+// rps_mix_mma.cu).  A CTA has a sequence's head and 64 columns of z, chunk by chunk of 64 tokens; all products are of fp32 in registers, 4 x 4 results to a
+// thread with two 16-byte reads of shared memory for every 16 to 32 multiplications.  148 heads of 512 tokens x 64 take 95 us forward, 444 take 234: 40 % of
+// the multiplications' rate; what else a chunk needs of issue slots and its barriers bound it.  (8 x 8 results in 64 threads: 163 and 261, 8 x 4
+// in 128 104 and 194, but 4 x 3 sequences of 333 x 5 x 48 x 40, forward and backward, 164 us instead of 129.  Six products of bf16 parts on the
+// tensor cores, mma.sync, whose operands every warp had to cut for itself: 117 for the 148 heads, 193 for the latter.)
 #include <algorithm>
 
 #include "rps_mix.cuh"
