@@ -48,7 +48,8 @@ constexpr int kAtP = 0, kAtState = 128, kAtOut = 256, kAtU = 384;
 // Barriers.  Whoever waits for one has to do so before it completes a second time, as a wait only tells even completions from odd ones; those that
 // would get further ahead come in pairs that take turns.
 struct Control {
-    uint64_t full[2], empty[2], x_full, scores, masked, of_state, out_done, out_free, parts[2], parts_used, last_part, update[2], state_ready, staged[2], left, state_in, state_read, state_out;
+    uint64_t full[2], empty[2], x_full, scores, masked, of_state, out_done, out_free, parts[2], parts_used, last_part, update[2];
+    uint64_t state_ready, staged[2], left, state_in, state_read, state_out;
     uint32_t tensor_memory;
     float powers[kC + 1];  // r^0 .. r^128
     float near[64];        // score_scale times the decay from a row to a column e - 32 less, zero ahead of time
@@ -149,8 +150,8 @@ __device__ __forceinline__ float small_power(float log_decay, int exponent)
 }
 
 // CTAs are placed in their order, and sequences may differ in length: the longest ones first, so that the last places to fall free wait for short ones.
-// (256 heads of sequences of up to 2048 tokens, lengths spread evenly, forward and backward: 421 us in the order given, 406 so.)  Every CTA finds its own: with kMostSorted sequences at most, whose lengths a
-// warp's width of comparisons each sorts in about a microsecond.
+// (256 heads of sequences of up to 2048 tokens, lengths spread evenly, forward and backward: 421 us in the order given, 406 so.)  Every CTA finds its
+// own: with kMostSorted sequences at most, whose lengths a warp's width of comparisons each sorts in about a microsecond.
 constexpr int kMostSorted = 256;
 
 __device__ __forceinline__ int64_t longest_first(const MixParams& prm, int item, unsigned char* shared)
@@ -211,11 +212,14 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
 
     if (warp == 0 && lane == 0) {
         const auto init = [](uint64_t& bar, int arrivals) { mbar_init(smem_addr(&bar), arrivals); };
-        for (int s = 0; s < 2; ++s) init(control.full[s], 1), init(control.empty[s], places.out_in_y && !STATES ? 2 : 1), init(control.parts[s], kStateWarps), init(control.update[s], 1),
-                                    init(control.staged[s], kOutWarps);
+        for (int s = 0; s < 2; ++s) {
+            init(control.full[s], 1), init(control.empty[s], places.out_in_y && !STATES ? 2 : 1);
+            init(control.parts[s], kStateWarps), init(control.update[s], 1), init(control.staged[s], kOutWarps);
+        }
         init(control.x_full, 1), init(control.scores, 1), init(control.of_state, 1), init(control.out_done, 1), init(control.parts_used, 1);
         init(control.masked, kOutWarps), init(control.out_free, kOutWarps), init(control.left, 1);
-        init(control.last_part, kStateWarps), init(control.state_ready, kStateWarps), init(control.state_in, 1), init(control.state_read, kStateWarps), init(control.state_out, kStateWarps);
+        init(control.last_part, kStateWarps), init(control.state_ready, kStateWarps);
+        init(control.state_in, 1), init(control.state_read, kStateWarps), init(control.state_out, kStateWarps);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) take_tensor_memory<1>(smem_addr(&control.tensor_memory));

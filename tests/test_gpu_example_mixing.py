@@ -119,3 +119,49 @@ def test_a_captured_training_pass(example):
         graph.replay()
         want_loss, want_grad = gradients()
         assert torch.equal(loss, want_loss) and torch.equal(grad, want_grad) and torch.isfinite(grad).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_two_streams_at_once(example, dtype):
+    """Two users of the operators on streams of their own, with nothing between them: each gets the bits that it gets alone."""
+    ops = example.ops
+    kind = {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
+
+    def user(seed, n, vocab, width, heads, sequences, tokens, top):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        table = torch.randn(n, vocab, width, generator=g, device="cuda").to(kind)
+        words = torch.randint(0, vocab, (n, sequences * tokens), generator=g, device="cuda")
+        ids = torch.randint(0, vocab, (n, sequences * tokens, top), generator=g, device="cuda")
+        kept = torch.randn(n, sequences * tokens, top, generator=g, device="cuda")
+        dloss = torch.ones(n, device="cuda")
+        decay = example.decays(n, heads)
+
+        def call():
+            x = ops.embedding_forward(words, table).view(n, sequences, tokens, heads, -1)
+            out, state = ops.linear_attention_forward(x, x, x, decay)
+            y = out.view(n, sequences * tokens, width)
+            loss, lse = ops.linear_distillation_forward(y, table, ids, kept)
+            dy, dtable = ops.linear_distillation_backward(dloss, y, table, ids, kept, lse)
+            dq, dk, dv, _ = ops.linear_attention_backward(dy.view_as(out), None, x, x, x, decay)
+            ops.embedding_backward((dq + dk + dv).view_as(y), words, vocab, dweight=dtable, accumulate=True)
+            step = ops.linear_attention_step(x[:, :, 0], x[:, :, 0], x[:, :, 0], decay, state)
+            return loss, dtable, state, step
+
+        return call
+
+    users = [user(1, 2, 3000, 128, 2, 4, 300, 7), user(2, 1, 5000, 240, 4, 3, 700, 33)]
+    want = [call() for call in users]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in users]
+    got = [[], []]
+    for _ in range(10):
+        for i, call in enumerate(users):
+            with torch.cuda.stream(streams[i]):
+                got[i].append(call())
+    for stream in streams:
+        with torch.cuda.stream(stream):
+            ops.check()
+    torch.cuda.synchronize()
+    for i in range(2):
+        for results in got[i]:
+            assert all(torch.equal(a, b) for a, b in zip(results, want[i]))
