@@ -269,7 +269,9 @@ int rps_embed_backward(const rps_embed_desc* desc, const int64_t* tokens, const 
  *   R_t = r R_(t+1) + scale * q_t^T dout_t,   dq_t = scale * dout_t S_t^T,   dk_t = v_t R_t^T,   dv_t = k_t R_t,   dstate_in = r R_0
  *
  * (R_(t+1) taken without its factor r for the last token).  Sequences go through in chunks of 64 or 128 tokens, whose part of the sums is
- * made as masked products; so an infinity or a NaN at a token may also reach results of the other tokens of its chunk.
+ * made as masked products.  So an infinity or a NaN at a token makes those results of its chunk that it reaches infinite or NaN, and may make NaN of
+ * the chunk's other results.  States and the results of other chunks become infinite or NaN as the recurrence's do, as long as no factor on the way (a power
+ * of r, times the other operand) is below 2^-80: that may count as zero, and zero times infinity is NaN.
  *
  * States are fp32, [n][sequences][heads][key_cols][value_cols], dense.  With RPS_BF16 the results that are bf16 are made of products of bf16 (of the masked
  * scores, and of S where it meets a q, rounded; what is added to an S or R that only such results need has 16 bits); what is added to a state that is

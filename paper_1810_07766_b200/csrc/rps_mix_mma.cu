@@ -80,7 +80,9 @@ struct Tile {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             uint32_t word[3];
-            split_two(__uint_as_float(r[i] << 16) * factor[i / 2 * 2], __uint_as_float(r[i] & 0xFFFF0000u) * factor[i / 2 * 2 + 1], word);
+            const Pair scaled = Pair(__uint_as_float(r[i] << 16), __uint_as_float(r[i] & 0xFFFF0000u)) * Pair(factor[i / 2 * 2], factor[i / 2 * 2 + 1]);
+            cut_in_parts(scaled, word[0], word[1], word[2]);
+            keep_infinities(word[0], word[1], word[2]);
 #pragma unroll
             for (int q = 0; q < 3; ++q) a.part[q][i] = word[q];
         }
@@ -314,7 +316,8 @@ __global__ void __launch_bounds__(kThreads) rps_mix_mma_kernel(const __grid_cons
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) w[m][n][e] = fmaf(whole, w[m][n][e], u[n][e]);
+                for (int e = 0; e < 4; ++e)  // rows behind the heads' columns stay zeros: an infinite z makes NaN of their part of u
+                    w[m][n][e] = (wr + 4 * m) * 16 + g + e / 2 * 8 < a ? fmaf(whole, w[m][n][e], u[n][e]) : 0.0f;
         }
         zero = false;
         __syncthreads();

@@ -523,17 +523,11 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
                 widen(read_shared(from + piece), v);
                 uint32_t part[3][4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    // 8 of the 24 bits at a time, cut off: the three parts are the value exactly
-                    Pair rest = v[j] * factor;
-                    float lo, hi;
+                for (int j = 0; j < 4; ++j) cut_in_parts(v[j] * factor, part[0][j], part[1][j], part[2][j]);
+                // NaN among the third parts; next to values beyond 2^15, which this may take for some, nothing is changed either
+                if (has_infinite_exponent(part[2][0] | part[2][1] | part[2][2] | part[2][3])) {
 #pragma unroll
-                    for (int k = 0; k < 3; ++k) {
-                        rest.get(lo, hi);
-                        part[k][j] = __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x7632);
-                        if (k < 2)
-                            rest = rest + Pair(__uint_as_float((__float_as_uint(lo) & 0xFFFF0000u) ^ 0x80000000u), __uint_as_float((__float_as_uint(hi) & 0xFFFF0000u) ^ 0x80000000u));
-                    }
+                    for (int j = 0; j < 4; ++j) keep_infinities(part[0][j], part[1][j], part[2][j]);
                 }
                 third[q] = make_uint4(part[2][0], part[2][1], part[2][2], part[2][3]);
                 write_shared((OWN ? to : from) + piece, make_uint4(part[0][0], part[0][1], part[0][2], part[0][3]));
@@ -543,7 +537,8 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
             writes_done();
             warp_arrive(control.parts[OWN ? s : 0]);
         };
-        // W of the next chunk: false if a wait gave up
+        // W of the next chunk: false if a wait gave up.  Rows behind the heads' columns stay zeros: an infinite z makes NaN of their part of U.
+        const bool row_of_w = row < term.rows;
         const auto bring_up_to_date = [&](int i) {
             if (!warp_wait(control.update[i & 1], i >> 1)) return false;
             const Pair whole(control.powers[kC - (chunk_at(i) == 0 ? missing : 0)]);
@@ -554,6 +549,7 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
                 __syncwarp();
                 load_sums(u, tensor + lanes + u_of(i) + col0 + c);
                 tensor_loads_done();
+                if (!row_of_w) continue;
 #pragma unroll
                 for (int j = 0; j < 16; j += 2) fma(whole, Pair(w[c + j], w[c + j + 1]), Pair(u[j], u[j + 1])).get(w[c + j], w[c + j + 1]);
             }
