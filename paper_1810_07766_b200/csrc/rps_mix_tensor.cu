@@ -8,10 +8,10 @@
 // is the first one that may begin ahead of the sequence; TMA fills zeros there, and never reads past the last token that takes part.
 //
 // Roles (groups of four warps): warp 0 copies y and z of the next chunk (and x, once x W has been made) while this one is worked on, warp 1 issues the
-// products, warp 2 sends out away, warp 3 brings W's first value and takes its last one away; eight (a lane to a row, half of the columns) turn P into
+// products, warp 2 sends out away, warp 3 brings W's first value; eight (a lane to a row, half of the columns) turn P into
 // the masked product, which goes back to tensor memory as the left operand of the next one, and lay O down in shared memory; sixteen make r^f y
 // in parts and hold W as fp32 in registers (a lane to a row of W, a quarter of the columns), which they bring up to date out of U and lay down as bf16
-// for the next chunk.  With up to 64 columns of y and z (OWN) all the parts have places of their own, and twice, so that the next chunk's are made
+// for the next chunk; the first of them sends its last value away.  With up to 64 columns of y and z (OWN) all the parts have places of their own, and twice, so that the next chunk's are made
 // while U is; with more, the first takes y's place and the others one after the other a single one.
 //
 // Each role's code for a chunk is run once by a few warps and then not until the next chunk, so its instructions come from afar: it is kept short (loops
@@ -209,6 +209,8 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
     // W before the segment and after it
     const int64_t slot = (which * prm.units + unit) * prm.segments + segment;
     const int way_in = maps.way[which][0], way_out = writes_state ? maps.way[which][1] : kNoState;
+    const int state_boxes = (b + kStateBox - 1) / kStateBox;
+    const uint32_t state_box_bytes = a_boxes * kBox * kStateBox * 4;
 
     if (warp == 0 && lane == 0) {
         const auto init = [](uint64_t& bar, int arrivals) { mbar_init(smem_addr(&bar), arrivals); };
@@ -361,20 +363,12 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
             asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
         }
         if (warp == 3 && elect_one()) {
-            const int boxes = (b + kStateBox - 1) / kStateBox;
-            const uint32_t box_bytes = a_boxes * kBox * kStateBox * 4;
             if (way_in == kCopied && prm.withhold_copies == 0) {
                 const uint32_t bar = smem_addr(&control.state_in);
-                mbar_arrive_expect_tx(bar, boxes * box_bytes);
+                mbar_arrive_expect_tx(bar, state_boxes * state_box_bytes);
                 const int from = (int)(prm.segments > 1 ? slot : unit);
-                for (int c = 0; c < boxes; ++c) load_state(base + places.part + c * box_bytes, &maps.state[which][0], c * kStateBox, from, bar);
+                for (int c = 0; c < state_boxes; ++c) load_state(base + places.part + c * state_box_bytes, &maps.state[which][0], c * kStateBox, from, bar);
                 fine = wait(control.state_in, 0);
-            }
-            if (way_out == kCopied && (fine = wait(control.state_out, 0) && fine)) {
-                const int to = (int)(STATES ? slot + 1 : unit);
-                for (int c = 0; c < boxes; ++c) store_state(base + places.part + c * box_bytes, &maps.state[which][1], c * kStateBox, to);
-                asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-                asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
             }
         }
     } else if (warp < kFirstState) {
@@ -472,7 +466,7 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
         float w[32];
 #pragma unroll
         for (int j = 0; j < 32; ++j) w[j] = 0.0f;
-        const uint32_t state_row = base + places.part + col0 / kStateBox * (a_boxes * kBox * kStateBox * 4) + row * 128;
+        const uint32_t state_row = base + places.part + col0 / kStateBox * state_box_bytes + row * 128;
         if (way_in == kCopied) {
             if (warp_wait(control.state_in, 0) && there) {
 #pragma unroll
@@ -602,6 +596,13 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
             }
             writes_done();
             warp_arrive(control.state_out);
+            // (a warp that has come this far: from the segment's start on a wait for all of it would be longer than for any data)
+            if (warp == kFirstState && warp_wait(control.state_out, 0) && elect_one()) {
+                const int to = (int)(STATES ? slot + 1 : unit);
+                for (int c = 0; c < state_boxes; ++c) store_state(base + places.part + c * state_box_bytes, &maps.state[which][1], c * kStateBox, to);
+                asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+            }
         } else if (way_out == kByElement && fine && row < term.rows) {
 #pragma unroll
             for (int j = 0; j < 32; ++j)

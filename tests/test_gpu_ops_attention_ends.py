@@ -1,4 +1,4 @@
-"""Linear attention at the ends of what it takes: infinities among bf16 operands."""
+"""Linear attention at the ends of what it takes: infinities among bf16 operands, long sequences under a short limit on waits."""
 import pytest
 import torch
 
@@ -52,3 +52,32 @@ def test_an_infinity_goes_through_states(ops, T, H, K, W, mixed):  # noqa: F811
     # one of q is in its own token's result alone
     rows = torch.arange(T, device="cuda") != t
     assert torch.equal(got["out"][0, 2, rows, 0], clean["out"][0, 2, rows, 0]) and torch.equal(got["state"][0, 2, 0], clean["state"][0, 2, 0])
+
+
+@pytest.mark.parametrize("backward", [False, True])
+def test_a_limit_on_waits_is_none_on_sequences(ops, backward):  # noqa: F811
+    """Sequences that a CTA takes several times longer for than its waits for data may last: 1875 chunks of 2.8 us against 2 ms.  Nothing gives up, and
+    results are those of the default limit."""
+    import ctypes
+
+    T, H, K = 240_000, 300, 8
+    g = torch.Generator(device="cuda").manual_seed(1)
+    q, k, v = (torch.randn(1, T, H, K, generator=g, device="cuda", dtype=torch.bfloat16) for _ in "qkv")
+    ld = torch.full((H,), -0.05, device="cuda")
+    rest = {"scale": 0.5}
+    want = ops.linear_attention_backward(v, None, q, k, v, ld, **rest) if backward else ops.linear_attention_forward(q, k, v, ld, **rest)
+    ops.check()
+    s = ops.rps_axis_strides(0, T * H * K, H * K, K)
+    d = ops.rps_linear_attention_desc(dtype=1, n=1, heads=H, wait_limit_ms=2, sequences=1, tokens=T, key_cols=K, value_cols=K, q=s, k=s, v=s, dout=s, scale=0.5)
+    size, lib = ctypes.c_size_t(), ops._library()
+    assert lib.rps_linear_attention_workspace(ctypes.byref(d), int(backward), ctypes.byref(size)) == 0 and size.value == 0   # no segments
+    got = [torch.full_like(t, float("nan")) for t in want]
+    p = [t.data_ptr() for t in got]
+    stream = torch.cuda.current_stream().cuda_stream
+    if backward:
+        status = lib.rps_linear_attention_backward(ctypes.byref(d), v.data_ptr(), None, q.data_ptr(), k.data_ptr(), v.data_ptr(), ld.data_ptr(), None, None, *p, None, 0, stream)
+    else:
+        status = lib.rps_linear_attention_forward(ctypes.byref(d), q.data_ptr(), k.data_ptr(), v.data_ptr(), ld.data_ptr(), None, None, *p, None, 0, stream)
+    assert status == 0
+    ops.check()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
