@@ -111,6 +111,8 @@ int rps_lce_backward(const rps_lce_desc* desc, const void* hidden, const void* w
  * ignore_index nor in 0..vocab-1, or a logit that is NaN or infinity, is a mistake of the caller that the host cannot see: it gives that
  * token's loss, and every gradient it takes part in, the value NaN.  A word may be in several entries, which count one by one.
  * dl is rounded as in the cross entropy above.
+ * Next to what the logits' own roundings make of them, p is off by up to 2^-23 |lse| / tau and 2^-19 of itself, as lse is one fp32 number, and the loss by
+ * up to tau^2 (2^-19 + 2^-22 times its terms): temperatures beyond 0.01..100, where little of either would be left, are refused.
  * ------------------------------------------------------------------------------------------------------------------ */
 typedef struct rps_distil_desc {
     int32_t dtype;         /* of hidden, weight, dhidden, dweight                                        */
@@ -125,7 +127,7 @@ typedef struct rps_distil_desc {
     int64_t hidden_row, hidden_worker;   /* strides as in rps_lce_desc                                   */
     int64_t weight_row, weight_worker;
     int64_t dweight_row, dweight_worker;
-    double temperature;    /* 1e-6..1e6                                                                  */
+    double temperature;    /* 0.01..100                                                                  */
 } rps_distil_desc;
 
 /* As rps_lce_workspace. */

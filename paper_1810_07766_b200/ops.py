@@ -397,7 +397,7 @@ def linear_distillation_forward(hidden: torch.Tensor, weight: torch.Tensor, top_
     hidden ``[n, tokens, cols]``, weight ``[n, vocab, cols]``, top_ids int64 and top_logits (float32 or bfloat16) ``[n, tokens, top]``, as
     ``torch.topk`` gives them, in any order (all without ``n`` for a single worker).  Entries whose id is ignore_index are none, and tokens without
     entries take no part.  loss as in ``linear_cross_entropy_forward``; lse, float32 ``[n, tokens]``, is what the backward pass wants: the
-    logits' soft maximum, ``temperature * logsumexp(logits / temperature)``."""
+    logits' soft maximum, ``temperature * logsumexp(logits / temperature)``.  temperature is 0.01 to 100."""
     device = _device_of(hidden=hidden, weight=weight, top_ids=top_ids, top_logits=top_logits)
     plan = _distil_plan(hidden, weight, top_ids, top_logits, float(temperature), ignore_index, reduction)
     top_ids, top_logits = top_ids.contiguous(), top_logits.contiguous()
