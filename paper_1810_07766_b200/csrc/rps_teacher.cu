@@ -39,7 +39,7 @@ __global__ void __launch_bounds__(kThreads) rps_teacher_kernel(const TeacherPara
             wrong = true;
             continue;
         }
-        x[r] = load_logit(prm.logits, prm.top_f32, first + e) * prm.sharpness;
+        x[r] = load_logit(prm.logits, prm.top_f32, first + e);
         wrong = wrong || !(x[r] < INFINITY);
         if (x[r] != -INFINITY) id[r] = (int)word;
         top = fmaxf(top, x[r]);
@@ -49,15 +49,16 @@ __global__ void __launch_bounds__(kThreads) rps_teacher_kernel(const TeacherPara
     for (int s = 16; s > 0; s /= 2) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, s));
     const bool none = top == -INFINITY;
     float e[PER], sum = 0.0f;
+    // differences before the temperature: they may be exact where logits divided by it are not, or are infinite
 #pragma unroll
-    for (int r = 0; r < PER; ++r) e[r] = id[r] != kNoWord ? expf(x[r] - top) : 0.0f, sum += e[r];
+    for (int r = 0; r < PER; ++r) x[r] = (x[r] - top) * prm.sharpness, e[r] = id[r] != kNoWord ? expf(x[r]) : 0.0f, sum += e[r];
 #pragma unroll
     for (int s = 16; s > 0; s /= 2) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, s);
     const float log_sum = logf(sum);
     float entropy = 0.0f;
 #pragma unroll
     for (int r = 0; r < PER; ++r) {
-        const float log_q = x[r] - top - log_sum;
+        const float log_q = x[r] - log_sum;
         e[r] = none || wrong ? 0.0f : e[r] / sum;
         if (e[r] == 0.0f)
             id[r] = kNoWord;  // takes no part

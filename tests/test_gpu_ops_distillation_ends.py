@@ -54,3 +54,17 @@ def test_the_coldest_and_the_hottest(ops, dtype, T, tau):  # noqa: F811
     loss, lse, dh, dw = check(ops, dtype, h, w, ids, x * tau, tau)
     if dtype == "f32":
         assert (dw[..., 0].sum(1).abs() <= T * tau * (2.0 ** -23 * 32 / tau + 2.0 ** -19)).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [3, 70])
+def test_teachers_whose_logits_are_large_next_to_their_differences(ops, dtype, T):  # noqa: F811
+    """Differences that fp32 holds exactly are what probabilities are made of, and infinite ones of finite logits are certainty."""
+    h, w, ids, x = exact(dtype, 2, T, 300, 20, seed=T)
+    x = 32768.0 + torch.arange(20, device="cuda") / 256 + torch.zeros_like(x)
+    check(ops, dtype, h, w, ids, x, 0.01)
+    x[..., 7], x[..., 9] = 3e38, -3e38
+    loss, lse, dh, dw = check(ops, dtype, h, w, ids, x, 0.01)
+    assert torch.isfinite(loss).all() and torch.isfinite(dw).all()
+    x[:] = -3e38
+    check(ops, dtype, h, w, ids, x, 0.01)
