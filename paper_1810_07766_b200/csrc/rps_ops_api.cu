@@ -86,12 +86,9 @@ LcePlan plan_lce(const rps_lce_desc& d, const void* weight, bool backward, void*
         t.entry_id = c.take<int>(p.n * p.tokens * top);
         t.entry_weight = c.take<float>(p.n * p.tokens * top);
         t.targets = c.take<int64_t>(p.n * p.tokens);
-        if (!backward) {
-            t.entropy = c.take<float>(p.n * p.tokens);
-            g.entry_logit = c.take<float>(p.n * p.tokens * top);
-        }
+        if (!backward) g.entry_logit = c.take<float>(p.n * p.tokens * top);
         g.top = top, g.bucket_rows = t.bucket_rows, g.entry_bucket = t.entry_bucket, g.sharpness = p.sharpness, g.entry_id = t.entry_id, g.entry_weight = t.entry_weight;
-        p.targets = t.targets, p.entropy = t.entropy, p.entry_id = t.entry_id, p.entry_weight = t.entry_weight, p.entry_logit = g.entry_logit;
+        p.targets = t.targets, p.entry_id = t.entry_id, p.entry_weight = t.entry_weight, p.entry_logit = g.entry_logit;
     };
     plan_lce_dot(&p);
     if (p.dot_rows > 0) {

@@ -133,7 +133,6 @@ struct LceParams {
     float factor, sharpness;  // of the loss's gradient, and of the logits: 1 but for distillation
     // distillation (top > 0): see ProductParams
     int top;
-    const float* entropy;     // [n][tokens]: sum of p log p over the entries
     const int* entry_id;
     const float *entry_weight, *entry_logit;
     float* loss;
@@ -166,7 +165,6 @@ struct TeacherParams {
     unsigned short* entry_bucket;  // as ProductParams
     int* entry_id;
     float* entry_weight;
-    float* entropy;         // [n][tokens], or NULL
     int64_t* targets;       // [n][tokens]: 0, kNoTeacher for a token without entries, -1 for one whose entries are no distribution
 };
 constexpr int64_t kNoTeacher = -100;

@@ -54,23 +54,12 @@ __global__ void __launch_bounds__(kThreads) rps_teacher_kernel(const TeacherPara
     for (int r = 0; r < PER; ++r) x[r] = (x[r] - top) * prm.sharpness, e[r] = id[r] != kNoWord ? expf(x[r]) : 0.0f, sum += e[r];
 #pragma unroll
     for (int s = 16; s > 0; s /= 2) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, s);
-    const float log_sum = logf(sum);
-    float entropy = 0.0f;
 #pragma unroll
     for (int r = 0; r < PER; ++r) {
-        const float log_q = x[r] - log_sum;
         e[r] = none || wrong ? 0.0f : e[r] / sum;
-        if (e[r] == 0.0f)
-            id[r] = kNoWord;  // takes no part
-        else
-            entropy = fmaf(e[r], log_q, entropy);
+        if (e[r] == 0.0f) id[r] = kNoWord;  // takes no part
     }
-#pragma unroll
-    for (int s = 16; s > 0; s /= 2) entropy += __shfl_xor_sync(0xFFFFFFFFu, entropy, s);
-    if (lane == 0) {
-        prm.targets[t] = wrong ? -1 : none ? kNoTeacher : 0;
-        if (prm.entropy != nullptr) prm.entropy[t] = wrong ? nanf("") : none ? 0.0f : entropy;
-    }
+    if (lane == 0) prm.targets[t] = wrong ? -1 : none ? kNoTeacher : 0;
 #pragma unroll
     for (int size = 2; size <= 32 * PER; size *= 2)
 #pragma unroll

@@ -57,6 +57,19 @@ def test_the_coldest_and_the_hottest(ops, dtype, T, tau):  # noqa: F811
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [3, 300])
+def test_logits_all_larger_by_a_number(ops, dtype, T):  # noqa: F811
+    """It changes neither probabilities nor losses, and so not what the losses are off by: no term of them is as large as the logits are."""
+    tau = 1.0
+    h, w, ids, x = exact(dtype, 2, T, 300, 40, shift=1024.0, seed=T)
+    loss, lse = ops.linear_distillation_forward(h, w, ids, x, temperature=tau, reduction="none")
+    want = definition(h, w, ids, x, tau, torch.ones(2, T, device="cuda"), "none")
+    terms = want["sl"] - tau * (want["lse"].abs() + tau)     # without lse's
+    off = (loss - want["loss"]).abs() - (tau ** 2 * 2.0 ** -19 + 2.0 ** -22 * terms)
+    assert (off <= 0).all(), float(off.max())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("T", [3, 70])
 def test_teachers_whose_logits_are_large_next_to_their_differences(ops, dtype, T):  # noqa: F811
     """Differences that fp32 holds exactly are what probabilities are made of, and infinite ones of finite logits are certainty."""
