@@ -228,6 +228,11 @@ def _parameter_stride(name: str, t: torch.Tensor) -> int:
     return t.stride(0) if t.shape[0] > 1 else 0
 
 
+def _changed(t: torch.Tensor) -> None:
+    """Says to autograd that a call has written to a tensor of the caller's: a gradient that still needs its old values will raise."""
+    torch.autograd.graph.increment_version(t)
+
+
 def _finite(name: str, value) -> float:
     if isinstance(value, torch.Tensor) and value.requires_grad and torch.is_grad_enabled():
         raise ValueError(f"{name} gets no gradient: it has to be a number")
@@ -424,12 +429,13 @@ def linear_distillation_backward(dloss: torch.Tensor, hidden: torch.Tensor, weig
             raise ValueError(f"{name} must be a float32 tensor of shape {shape}")
         _dense(name, t)
     where = hidden.device
-    if dweight is None:
-        dweight = _new(plan.weight, weight.dtype, where)
+    given, dweight = dweight, _new(plan.weight, weight.dtype, where) if dweight is None else dweight
     dhidden = _new(plan.hidden, hidden.dtype, where)
     ws = _new(plan.workspace[1], torch.uint8, where)
     _call("rps_distil_backward", device, plan.desc, hidden.data_ptr(), weight.data_ptr(), top_ids.data_ptr(), top_logits.data_ptr(), lse.data_ptr(), dloss.data_ptr(),
           dhidden.data_ptr(), dweight.data_ptr(), ws.data_ptr(), plan.sizes[1], _stream(device))
+    if given is not None:
+        _changed(given)
     return dhidden, dweight
 
 
@@ -809,10 +815,11 @@ def embedding_backward(dout: torch.Tensor, tokens: torch.Tensor, vocab: int, *, 
         plan = _keep(key, (ctypes.byref(d), _dense_layout(lead + (vocab, cols)), size.value, _dense_layout((size.value,))))
     desc, layout, size, ws_layout = plan
     tokens = tokens.contiguous()
-    if dweight is None:
-        dweight = _new(layout, dout.dtype, dout.device)
+    given, dweight = dweight, _new(layout, dout.dtype, dout.device) if dweight is None else dweight
     ws = _new(ws_layout, torch.uint8, dout.device)
     _call("rps_embed_backward", device, desc, tokens.data_ptr(), dout.data_ptr(), dweight.data_ptr(), ws.data_ptr(), size, _stream(device))
+    if given is not None:
+        _changed(given)
     return dweight
 
 
