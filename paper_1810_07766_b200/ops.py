@@ -983,10 +983,12 @@ def linear_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log
         apart = abs(new_state.data_ptr() - state.data_ptr())
         if 0 < apart < 4 * state.numel():
             raise ValueError("new_state overlaps state")
-    torch.autograd.graph.increment_version(new_state)  # a gradient that still needs its old values will say so
+    if torch.is_grad_enabled() and new_state.requires_grad:
+        raise ValueError("new_state would be overwritten where its gradient is recorded: call a step under torch.no_grad()")
     out = _new(plan.out, q.dtype, q.device)
     _call("rps_linear_attention_step", device, plan.desc, q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(), state.data_ptr(), out.data_ptr(),
           new_state.data_ptr(), _stream(device))
+    _changed(new_state)
     return out
 
 
