@@ -909,6 +909,14 @@ def _attention_plan(q, k, v, log_decay, state, lengths, scale, dout=None, tokens
     return _keep(key, _AttentionPlan(ctypes.byref(d), values, _dense_layout(q.shape), values, layout, tuple(sizes), tuple(_dense_layout((size,)) for size in sizes)))
 
 
+def _attention_scale(q, scale) -> float:
+    """``key_cols ** -0.5`` unless given (a q without columns is refused by the library)."""
+    if scale is not None:
+        return float(scale)
+    cols = q.shape[-1] if isinstance(q, torch.Tensor) and q.dim() else 0
+    return float(cols ** -0.5) if cols else 1.0
+
+
 def _pointer(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
 
@@ -931,7 +939,7 @@ def linear_attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, 
     sequence's tokens take part (None: all), the rows of the others are zeros; all without ``n`` for a single worker.  scale is
     ``key_cols ** -0.5`` unless given."""
     device = _attention_device(state, lengths, q=q, k=k, v=v, log_decay=log_decay)
-    plan = _attention_plan(q, k, v, log_decay, state, lengths, float(q.shape[-1] ** -0.5 if scale is None else scale))
+    plan = _attention_plan(q, k, v, log_decay, state, lengths, _attention_scale(q, scale))
     if lengths is not None:
         lengths = lengths.contiguous()
     where = q.device
@@ -947,7 +955,7 @@ def linear_attention_backward(dout: torch.Tensor, dstate: Optional[torch.Tensor]
     """(dq, dk, dv, gradient of the first state) for the gradients dout and dstate (None: none reaches the last state) of the forward
     call's results with the same arguments (``rps_linear_attention_backward``).  log_decay and scale get no gradient."""
     device = _attention_device(state, lengths, q=q, k=k, v=v, log_decay=log_decay, dout=dout)
-    plan = _attention_plan(q, k, v, log_decay, state, lengths, float(q.shape[-1] ** -0.5 if scale is None else scale), dout)
+    plan = _attention_plan(q, k, v, log_decay, state, lengths, _attention_scale(q, scale), dout)
     if dstate is not None:
         _device_of(q=q, dstate=dstate)
         if dstate.dtype != torch.float32 or dstate.shape != plan.state[0]:
@@ -972,7 +980,7 @@ def linear_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log
     device = _device_of(q=q, k=k, v=v, log_decay=log_decay, state=state)
     if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad or log_decay.requires_grad or state.requires_grad):
         raise ValueError("a step has no gradient: call it under torch.no_grad(), or linear_attention with sequences of one token")
-    plan = _attention_plan(q, k, v, log_decay, state, None, float(q.shape[-1] ** -0.5 if scale is None else scale), tokens=False)
+    plan = _attention_plan(q, k, v, log_decay, state, None, _attention_scale(q, scale), tokens=False)
     if new_state is None:
         new_state = state
     else:
@@ -1019,4 +1027,4 @@ def linear_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_deca
     """Differentiable ``linear_attention_forward``: (out, state after the last token)."""
     if isinstance(log_decay, torch.Tensor) and log_decay.requires_grad and torch.is_grad_enabled():
         raise ValueError("log_decay gets no gradient: the heads' decays are constants of the model")
-    return _LinearAttention.apply(q, k, v, log_decay, _finite("scale", q.shape[-1] ** -0.5 if scale is None else scale), state, lengths)
+    return _LinearAttention.apply(q, k, v, log_decay, _attention_scale(q, None) if scale is None else _finite("scale", scale), state, lengths)

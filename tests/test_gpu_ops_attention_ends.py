@@ -81,3 +81,14 @@ def test_a_limit_on_waits_is_none_on_sequences(ops, backward):  # noqa: F811
     assert status == 0
     ops.check()
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_heads_without_columns_are_refused(ops):  # noqa: F811
+    x = inputs("f32", 1, 2, 5, 3, 4, 8)
+    q, v, ld, s = x["q"][..., :0], x["v"], x["log_decay"], x["state"][..., :0, :].contiguous()
+    for call in (lambda: ops.linear_attention(q, q, v, ld), lambda: ops.linear_attention_forward(q, q, v, ld), lambda: ops.linear_attention_backward(v, None, q, q, v, ld),
+                 lambda: ops.linear_attention_step(q[:, :, 0], q[:, :, 0], v[:, :, 0], ld, s)):
+        with pytest.raises(ops.RPSError, match="key_cols"):
+            call()
+    with pytest.raises(ValueError, match="q must be"):
+        ops.linear_attention(q.sum(), q, v, ld)
