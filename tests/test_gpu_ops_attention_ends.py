@@ -1,8 +1,9 @@
-"""Linear attention at the ends of what it takes: infinities among bf16 operands, long sequences under a short limit on waits."""
+"""Linear attention at the ends of what it takes: infinities among bf16 operands, long sequences under a short limit on waits,
+hundreds of lengths."""
 import pytest
 import torch
 
-from test_gpu_ops_attention import inputs, ops, definition, run  # noqa: F401
+from test_gpu_ops_attention import check, definition, inputs, ops, run  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -92,3 +93,12 @@ def test_heads_without_columns_are_refused(ops):  # noqa: F811
             call()
     with pytest.raises(ValueError, match="q must be"):
         ops.linear_attention(q.sum(), q, v, ld)
+
+
+@pytest.mark.parametrize("n,B", [(4, 64), (1, 257), (2, 129)])
+def test_sequences_of_many_lengths(ops, n, B):  # noqa: F811
+    """Up to 256 sequences are taken the longest first, more as they come; several have the same length."""
+    x = inputs("bf16", n, B, 140, 2, 32, 24, seed=B)
+    lengths = torch.randint(-1, 142, (n, B), generator=torch.Generator(device="cuda").manual_seed(B), device="cuda")
+    lengths[:, ::5] = 130
+    check(ops, x, lengths=lengths)
