@@ -277,7 +277,7 @@ int rps_embed_backward(const rps_embed_desc* desc, const int64_t* tokens, const 
  *
  * States are fp32, [n][sequences][heads][key_cols][value_cols], dense.  With RPS_BF16 the results that are bf16 are made of products of bf16 (of the masked
  * scores, and of S where it meets a q, rounded; what is added to an S or R that only such results need has 16 bits); what is added to a state that is
- * written has 24.  Which kernel multiplies goes by alignment and strides, and the order of its sums with it: the same values laid out otherwise may give other last bits.
+ * written has 24.  Which kernel multiplies goes by sizes, alignment and strides, and the order of its sums with it: the same values laid out otherwise may give other last bits.
  * log_decay: float [n][heads], at most 0 (minus infinity: r = 0); a positive one or a NaN makes its head's results NaN.  It gets no gradient.
  * lengths: int64 [n][sequences], dense, or NULL (all tokens): only the first `length` tokens of a sequence take part (a length outside
  * 0..tokens counts as the nearest of them).  The others are not read, their rows of out, dq, dk and dv are 0, and states are those after the

@@ -11,8 +11,8 @@
 // Where there are too few heads of sequences to fill the SMs, sequences are cut into segments: one launch makes each segment's own sum of y^T z,
 // one adds them up in order into the states that segments begin with, and the main one then runs all segments at once (y and z are read twice).
 //
-// The kernel here takes fp32 operands (bf16 ones: rps_mix_tensor.cu; where TMA cannot copy them, copies of theirs, or in short sequences
-// rps_mix_mma.cu).  A CTA has a sequence's head and 64 columns of z, chunk by chunk of 64 tokens; all products are of fp32 in registers, 4 x 4 results to a
+// The kernel here takes fp32 operands (bf16 ones: rps_mix_tensor.cu; where TMA cannot copy them, copies of theirs; rps_mix_mma.cu in short sequences of narrow
+// heads or of what TMA cannot copy).  A CTA has a sequence's head and 64 columns of z, chunk by chunk of 64 tokens; all products are of fp32 in registers, 4 x 4 results to a
 // thread with two 16-byte reads of shared memory for every 16 to 32 multiplications.  148 heads of 512 tokens x 64 take 95 us forward, 444 take 234: 40 % of
 // the multiplications' rate; what else a chunk needs of issue slots and its barriers bound it.  (8 x 8 results in 64 threads: 163 and 261, 8 x 4
 // in 128 104 and 194, but 4 x 3 sequences of 333 x 5 x 48 x 40, forward and backward, 164 us instead of 129.  Six products of bf16 parts on the
@@ -535,6 +535,16 @@ cudaError_t launch_f32(const MixParams& prm, bool states, cudaStream_t stream)
 // 375 / 431; 256 tokens 177 / 230, 545 / 863; 27 of 212 tokens x 18 x (14, 117) 115 / 113, 318 / 446; 2 of 3841 x 14 x (85, 98) 125 / 347, 345 / 1361.
 int64_t copied_tokens(const MixParams& prm) { return prm.terms == 1 ? 193 : 128; }
 
+// Short sequences of narrow heads, which TMA could copy, go through the fourth generation's tensor cores all the same: a chunk of 64 tokens is less padded
+// than one of 128, and several CTAs share an SM, where the other kernel's takes all of its tensor memory.  That one / this (us), 2048 heads of 64
+// columns: 8 tokens 103 / 54 forward, 420 / 191 with backward; 64 tokens 117 / 72, 437 / 245; 128 tokens 114 / 103, 441 / 386; 192 tokens 148 / 142,
+// 588 / 534; 256 tokens 148 / 180, 590 / 682.  256 heads of 64 tokens 65 / 38 with backward, 16 heads of 128 40 / 38.  Wider heads: 2048 of
+// 128 columns 152 / 187 with 8 tokens, 159 / 228 with 64.  (A call that is to withhold copies goes to the kernel that makes them.)
+bool short_and_narrow(const MixParams& p)
+{
+    return p.tokens <= 3 * kMixChunk && std::max(p.term[0].a, p.term[0].b) <= kTile && p.copies_bytes == 0 && p.withhold_copies == 0;
+}
+
 // Sequences are cut into as many segments as take the least time by this count, in microseconds: a round of CTAs takes 6 to begin and end with and
 // for each 128 tokens, as measured, on the tensor cores 4 (2.8 to 4.7); in fp32 37, or with up to 64 columns, where two CTAs share an SM, 21 for one
 // and 35 for both; the segments' own sums, made first, 0.6 of that; joining them 6.
@@ -583,7 +593,7 @@ cudaError_t launch_mix(const MixParams& prm, cudaStream_t stream)
         with_copies(&p, &in, &out);
         if (!mix_fits_tensor(p)) p = prm, in.count = out.count = 0;  // what needs no copy lies at an odd address
     }
-    p.tensor = !p.f32 && mix_fits_tensor(p);
+    p.tensor = !p.f32 && mix_fits_tensor(p) && !short_and_narrow(p);
     const auto launch = p.f32 ? launch_f32 : p.tensor ? launch_mix_tensor : launch_mix_mma;
     cudaError_t err = launch_moves(p, in, stream);
     if (err == cudaSuccess && p.segments > 1) {

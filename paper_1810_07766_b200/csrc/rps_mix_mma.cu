@@ -1,5 +1,5 @@
-// Linear attention's form (rps_mix.cu) for bf16 operands that TMA cannot copy: odd numbers of columns or strides in short sequences (of long ones copies
-// are made, plan_mix), and odd addresses.
+// Linear attention's form (rps_mix.cu) for bf16 operands in short sequences of narrow heads, and for those that TMA cannot copy: odd numbers of columns or
+// strides in short sequences (of long ones copies are made, plan_mix), and odd addresses.
 //
 // A CTA has a sequence's head and 64 columns of z, chunk by chunk of 64 tokens; W stays in its registers as fp32.  Products go through the tensor cores by
 // mma.sync: tiles are 64 x 64 with 16 rows to a warp, and every operand is scaled or masked in registers on its way from one product to the next.

@@ -102,3 +102,15 @@ def test_sequences_of_many_lengths(ops, n, B):  # noqa: F811
     lengths = torch.randint(-1, 142, (n, B), generator=torch.Generator(device="cuda").manual_seed(B), device="cuda")
     lengths[:, ::5] = 130
     check(ops, x, lengths=lengths)
+
+
+@pytest.mark.parametrize("n,B,T,H,K,W", [(1, 40, 8, 8, 64, 64), (2, 3, 64, 5, 16, 48), (1, 2, 150, 3, 64, 8), (3, 7, 192, 2, 40, 64), (1, 5, 1, 4, 8, 8)])
+def test_short_sequences_of_narrow_heads_at_any_address(ops, n, B, T, H, K, W):  # noqa: F811
+    """They go through the kernel of short chunks however they lie, so that their results do not depend on it."""
+    x = inputs("bf16", n, B, T, H, K, W, seed=T)
+    want, y = check(ops, x), dict(x)
+    for name in ("q", "k", "v", "dout"):
+        room = torch.zeros(x[name].numel() + 1, dtype=torch.bfloat16, device="cuda")[1:].view_as(x[name])
+        y[name] = room.copy_(x[name])
+    got = run(ops, y, 0.3)
+    assert all(torch.equal(got[name], want[name]) for name in want)
