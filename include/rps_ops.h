@@ -284,7 +284,8 @@ int rps_embed_backward(const rps_embed_desc* desc, const int64_t* tokens, const 
  * last token that takes part.
  * q, k, v and dout are [n][sequences][tokens][heads][cols] at any strides of the outer axes (parts of one projection's output, say); out, dq,
  * dk and dv are dense in this order.  sequences and tokens may be 0.  (With RPS_BF16, columns and strides in eights and 16-byte aligned addresses
- * are read as they lie; of other arrays of longer sequences copies are made in the workspace first.)
+ * are read as they lie; of arrays of longer sequences with other columns or strides copies are made in the workspace first.  Where an array whose columns
+ * and strides are in eights begins at another address, all of the call's arrays are read as they lie, by a kernel that takes up to four times as long.)
  * ------------------------------------------------------------------------------------------------------------------ */
 typedef struct rps_axis_strides {
     int64_t worker, sequence, token, head;

@@ -937,7 +937,7 @@ def linear_attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, 
     q, k ``[n, sequences, tokens, heads, key_cols]``, v the same with value_cols, at any strides of the outer axes; log_decay float32 ``[n, heads]``,
     at most 0; state (None: zeros) float32 ``[n, sequences, heads, key_cols, value_cols]``; lengths int64 ``[n, sequences]``: how many of a
     sequence's tokens take part (None: all), the rows of the others are zeros; all without ``n`` for a single worker.  scale is
-    ``key_cols ** -0.5`` unless given."""
+    ``key_cols ** -0.5`` unless given.  (A view of bfloat16 whose strides are multiples of 8 should begin at one, too: see ``rps_ops.h``.)"""
     device = _attention_device(state, lengths, q=q, k=k, v=v, log_decay=log_decay)
     plan = _attention_plan(q, k, v, log_decay, state, lengths, _attention_scale(q, scale))
     if lengths is not None:
