@@ -33,14 +33,13 @@ __device__ __forceinline__ void load_matrices(uint32_t (&r)[4], uint32_t addr)
         asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
 
-// A 16 x 16 operand (rows x summed axis) and two 16 x 8 ones (summed axis x columns), as parts whose sum they are.
+// A 16 x 16 operand (rows x summed axis), as parts whose sum it is, and two 16 x 8 ones (summed axis x columns).
 template <int PARTS>
 struct Left {
     uint32_t part[PARTS][4];
 };
-template <int PARTS>
 struct Right {
-    uint32_t part[PARTS][2][2];
+    uint32_t word[2][2];
 };
 
 // How operands come out of tiles in shared memory.  ROW: elements from a row to the next, chosen so that a warp's reads meet no bank twice.
@@ -54,21 +53,21 @@ struct Tile {
     }
     // [column][summed axis]
     template <int ROW>
-    static __device__ __forceinline__ void right_across(Right<1>& b, const bf16* tile, int k, int col)
+    static __device__ __forceinline__ void right_across(Right& b, const bf16* tile, int k, int col)
     {
         const int lane = threadIdx.x % 32;
         uint32_t r[4];
         load_matrices<false>(r, rps::smem_addr(tile + (col + lane % 8 + lane / 16 * 8) * ROW + k + lane / 8 % 2 * 8));
-        b.part[0][0][0] = r[0], b.part[0][0][1] = r[1], b.part[0][1][0] = r[2], b.part[0][1][1] = r[3];
+        b.word[0][0] = r[0], b.word[0][1] = r[1], b.word[1][0] = r[2], b.word[1][1] = r[3];
     }
     // [summed axis][column]
     template <int ROW>
-    static __device__ __forceinline__ void right(Right<1>& b, const bf16* tile, int k, int col)
+    static __device__ __forceinline__ void right(Right& b, const bf16* tile, int k, int col)
     {
         const int lane = threadIdx.x % 32;
         uint32_t r[4];
         load_matrices<true>(r, rps::smem_addr(tile + (k + lane % 16) * ROW + col + lane / 16 * 8));
-        b.part[0][0][0] = r[0], b.part[0][0][1] = r[1], b.part[0][1][0] = r[2], b.part[0][1][1] = r[3];
+        b.word[0][0] = r[0], b.word[0][1] = r[1], b.word[1][0] = r[2], b.word[1][1] = r[3];
     }
     // [summed axis][row], times a factor for each step of the summed axis: the lane's are at k + 2 (lane % 4) + {0, 1, 8, 9}
     template <int ROW>
@@ -91,21 +90,14 @@ struct Tile {
 };
 
 // Products of parts, the smallest first; TILES tiles of 8 columns side by side, of which the first `tiles` are wanted.
-template <int LEFT, int RIGHT, int TILES>
-__device__ __forceinline__ void multiply_parts(float (&sum)[TILES][4], const Left<LEFT>& a, const Right<RIGHT> (&b)[TILES / 2], int tiles)
+template <int PARTS, int TILES>
+__device__ __forceinline__ void multiply_parts(float (&sum)[TILES][4], const Left<PARTS>& a, const Right (&b)[TILES / 2], int tiles)
 {
 #pragma unroll
-    for (int order = LEFT + RIGHT - 2; order >= 0; --order) {
-        if (order > 2) continue;  // what these would add is below 2^-24 of the result
+    for (int p = PARTS - 1; p >= 0; --p)
 #pragma unroll
-        for (int p = 0; p < LEFT; ++p) {
-            const int q = order - p;
-            if (q < 0 || q >= RIGHT) continue;
-#pragma unroll
-            for (int n = 0; n < TILES; ++n)
-                if (n < tiles) multiply(sum[n], a.part[p], b[n / 2].part[q][n % 2][0], b[n / 2].part[q][n % 2][1]);
-        }
-    }
+        for (int n = 0; n < TILES; ++n)
+            if (n < tiles) multiply(sum[n], a.part[p], b[n / 2].word[n % 2][0], b[n / 2].word[n % 2][1]);
 }
 
 // ------------------------------------------------------------------------------------------------------------ kernel
@@ -219,11 +211,11 @@ __global__ void __launch_bounds__(kThreads) rps_mix_mma_kernel(const __grid_cons
             for (int k = 0; k < a16; k += 16) {
                 Left<1> left;
                 Tile::left<S::kRowA>(left, tx, row0, k);
-                Right<1> right[4];
+                Right right[4];
 #pragma unroll
                 for (int n = 0; n < 4; ++n)
                     if (2 * n < keys) Tile::right_across<S::kRowA>(right[n], ty, k, n * 16);
-                multiply_parts<1, 1, 8>(p, left, right, keys);
+                multiply_parts<1, 8>(p, left, right, keys);
             }
             float out[NT][4];
 #pragma unroll
@@ -234,11 +226,11 @@ __global__ void __launch_bounds__(kThreads) rps_mix_mma_kernel(const __grid_cons
                 for (int k = 0; k < a16; k += 16) {
                     Left<1> left;
                     Tile::left<S::kRowA>(left, tx, row0, k);
-                    Right<1> right[NT / 2];
+                    Right right[NT / 2];
 #pragma unroll
                     for (int n = 0; n < NT / 2; ++n)
                         if (2 * n < tiles) Tile::right<S::kRowB>(right[n], state, k, 2 * n * 8);
-                    multiply_parts<1, 1, NT>(out, left, right, tiles);
+                    multiply_parts<1, NT>(out, left, right, tiles);
                 }
 #pragma unroll
                 for (int e = 0; e < 4; e += 2) {
@@ -262,11 +254,11 @@ __global__ void __launch_bounds__(kThreads) rps_mix_mma_kernel(const __grid_cons
                 for (int i = 0; i < 4; ++i) {
                     left.part[0][i] = two_bf16(p[2 * k + i / 2][i % 2 * 2], p[2 * k + i / 2][i % 2 * 2 + 1]);
                 }
-                Right<1> right[NT / 2];
+                Right right[NT / 2];
 #pragma unroll
                 for (int n = 0; n < NT / 2; ++n)
                     if (2 * n < tiles) Tile::right<S::kRowB>(right[n], tz, k * 16, 2 * n * 8);
-                multiply_parts<1, 1, NT>(out, left, right, tiles);
+                multiply_parts<1, NT>(out, left, right, tiles);
             }
             // out through this warp's rows of x, which have been read
             __syncwarp();
@@ -307,11 +299,11 @@ __global__ void __launch_bounds__(kThreads) rps_mix_mma_kernel(const __grid_cons
                 }
                 Left<3> left;
                 Tile::left_across<S::kRowA>(left, ty, k, (wr + 4 * m) * 16, factor);
-                Right<1> right[NT / 2];
+                Right right[NT / 2];
 #pragma unroll
                 for (int n = 0; n < NT / 2; ++n)
                     if (2 * n < tiles) Tile::right<S::kRowB>(right[n], tz, k, 2 * n * 8);
-                multiply_parts<3, 1, NT>(u, left, right, tiles);
+                multiply_parts<3, NT>(u, left, right, tiles);
             }
 #pragma unroll
             for (int n = 0; n < NT; ++n)

@@ -239,7 +239,7 @@ struct EmbedParams {
     int64_t dweight_row, dweight_worker;
     // backward (plan_embed): the tokens sorted by row, in one of two places each
     int key_bits, digit_bits, sorted;  // sorted: which place
-    int64_t sort_blocks;               // CTAs that sort a worker's tokens; 0: one, in shared memory
+    int64_t sort_blocks;               // CTAs that sort a worker's tokens; 0: a cluster of eight, in shared memory (few: each of those that sum)
     uint32_t *keys[2], *from[2];       // [n][count]
     uint32_t* counts;                  // [n][256][sort_blocks]
     int64_t tile, tiles, part_row;     // sorted tokens of a tile; of a worker
