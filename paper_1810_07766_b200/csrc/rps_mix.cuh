@@ -15,31 +15,34 @@ __device__ __forceinline__ double power(float log_decay, int64_t exponent)
     return exp((double)fmaxf(log_decay, -1e4f) * (double)exponent);
 }
 
-// Two fp32 values as three bf16 parts each, as words: 8 of the 24 bits at a time, cut off, so the parts add up to the value exactly and have its sign.
+// The upper halves of two fp32 values as a word of bf16, and what they leave (taken from infinity or NaN: NaN).
+__device__ __forceinline__ Pair cut(const Pair& v, uint32_t& word)
+{
+    float lo, hi;
+    v.get(lo, hi);
+    word = __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x7632);
+    return v + Pair(__uint_as_float((__float_as_uint(lo) & 0xFFFF0000u) ^ 0x80000000u), __uint_as_float((__float_as_uint(hi) & 0xFFFF0000u) ^ 0x80000000u));
+}
+
+// Two fp32 values as bf16 parts, as words: 8 of the 24 bits at a time, cut off, so three parts add up to the value exactly and have its sign.
 // Parts that would be zero are 2^-50 of the value, which changes no sum (it is below half of a last place of any part that is not zero, and 2^-26 of one
 // of the value's), so that an infinity of the other operand meets none that is zero where the value is not: infinity times a number is infinity.
-// What is itself infinite or NaN gives NaN here (keep_infinities).
-__device__ __forceinline__ void cut_in_parts(const Pair& value, uint32_t& first, uint32_t& second, uint32_t& third)
-{
-    const Pair least(0x1p-50f);
-    const auto cut = [](const Pair& v, uint32_t& word) {
-        float lo, hi;
-        v.get(lo, hi);
-        word = __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x7632);
-        return Pair(__uint_as_float((__float_as_uint(lo) & 0xFFFF0000u) ^ 0x80000000u), __uint_as_float((__float_as_uint(hi) & 0xFFFF0000u) ^ 0x80000000u));
-    };
-    const Pair rest = fma(value, least, value + cut(value, first)), last = fma(value, least, rest + cut(rest, second));
-    cut(last, third);
-}
+// What is itself infinite or NaN leaves NaN behind the first part (keep_infinities).
+__device__ __forceinline__ Pair next_part(const Pair& value, const Pair& rest, uint32_t& word) { return cut(fma(value, Pair(0x1p-50f), rest), word); }
 
 // Of the exponents of two bf16 values those that are all ones, as the sign bit of each half.
 __device__ __forceinline__ uint32_t has_infinite_exponent(uint32_t word) { return ((word & 0x7F807F80u) + 0x00800080u) & 0x80008000u; }
 
-// Parts of infinity or NaN: all of them are the value itself.
-__device__ __forceinline__ void keep_infinities(uint32_t first, uint32_t& second, uint32_t& third)
+// A further part of infinity or NaN: the value itself, as the first one is.
+__device__ __forceinline__ uint32_t keep_infinities(uint32_t first, uint32_t further)
 {
     const uint32_t mask = (has_infinite_exponent(first) >> 15) * 0xFFFFu;
-    second = (second & ~mask) | (first & mask), third = (third & ~mask) | (first & mask);
+    return (further & ~mask) | (first & mask);
+}
+
+__device__ __forceinline__ uint4 keep_infinities(const uint4& first, const uint4& further)
+{
+    return make_uint4(keep_infinities(first.x, further.x), keep_infinities(first.y, further.y), keep_infinities(first.z, further.z), keep_infinities(first.w, further.w));
 }
 
 struct Place {

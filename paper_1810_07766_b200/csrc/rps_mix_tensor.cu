@@ -508,7 +508,9 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
         const auto split = [&](int i) {
             const int s = i & 1, first = chunk_at(i) == 0 ? missing : 0;
             const uint32_t from = row_at + places.y + s * y_bytes, to = row_at + places.part + (OWN ? s * 3 * y_bytes : 0);
+            const uint32_t first_to = OWN ? to : from, second_to = to + (OWN ? y_bytes : 0);
             const Pair factor(term.update_scale * control.powers[reversed ? max(row + 1 - first, 0) : kC - 1 - row]);
+            uint32_t odd = 0;
 #pragma unroll
             for (int q = 0; q < kPieces; ++q) {
                 if (q >= pieces) break;
@@ -517,16 +519,27 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
                 widen(read_shared(from + piece), v);
                 uint32_t part[3][4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) cut_in_parts(v[j] * factor, part[0][j], part[1][j], part[2][j]);
-                // NaN among the third parts; next to values beyond 2^15, which this may take for some, nothing is changed either
-                if (has_infinite_exponent(part[2][0] | part[2][1] | part[2][2] | part[2][3])) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) keep_infinities(part[0][j], part[1][j], part[2][j]);
+                for (int j = 0; j < 4; ++j) {
+                    const Pair scaled = v[j] * factor;
+                    next_part(scaled, next_part(scaled, cut(scaled, part[0][j]), part[1][j]), part[2][j]);
+                    odd |= part[2][j];
                 }
                 third[q] = make_uint4(part[2][0], part[2][1], part[2][2], part[2][3]);
-                write_shared((OWN ? to : from) + piece, make_uint4(part[0][0], part[0][1], part[0][2], part[0][3]));
-                write_shared(to + (OWN ? y_bytes : 0) + piece, make_uint4(part[1][0], part[1][1], part[1][2], part[1][3]));
+                write_shared(first_to + piece, make_uint4(part[0][0], part[0][1], part[0][2], part[0][3]));
+                write_shared(second_to + piece, make_uint4(part[1][0], part[1][1], part[1][2], part[1][3]));
                 if (OWN) write_shared(to + 2 * y_bytes + piece, third[q]);
+            }
+            // NaN among the third parts; next to values beyond 2^15, which this may take for some, nothing is changed either
+            if (has_infinite_exponent(odd)) {
+#pragma unroll
+                for (int q = 0; q < kPieces; ++q) {
+                    if (q >= pieces) break;
+                    const uint32_t piece = ((piece0 + q) ^ swizzle) << 4;
+                    const uint4 is = read_shared(first_to + piece);
+                    write_shared(second_to + piece, keep_infinities(is, read_shared(second_to + piece)));
+                    third[q] = keep_infinities(is, third[q]);
+                    if (OWN) write_shared(to + 2 * y_bytes + piece, third[q]);
+                }
             }
             writes_done();
             warp_arrive(control.parts[OWN ? s : 0]);
