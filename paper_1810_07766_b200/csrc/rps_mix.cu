@@ -536,7 +536,7 @@ cudaError_t launch_f32(const MixParams& prm, bool states, cudaStream_t stream)
 int64_t copied_tokens(const MixParams& prm) { return prm.terms == 1 ? 193 : 128; }
 
 // Short sequences of narrow heads, which TMA could copy, go through the fourth generation's tensor cores all the same: a chunk of 64 tokens is less padded
-// than one of 128, and several CTAs share an SM, where the other kernel's takes all of its tensor memory.  That one / this (us), 2048 heads of 64
+// than one of 128, and two CTAs share an SM, where the other kernel's takes all of its tensor memory.  That one / this (us), 2048 heads of 64
 // columns: 8 tokens 103 / 54 forward, 420 / 191 with backward; 64 tokens 117 / 72, 437 / 245; 128 tokens 114 / 103, 441 / 386; 192 tokens 148 / 142,
 // 588 / 534; 256 tokens 148 / 180, 590 / 682.  256 heads of 64 tokens 65 / 38 with backward, 16 heads of 128 40 / 38.  Wider heads: 2048 of
 // 128 columns 152 / 187 with 8 tokens, 159 / 228 with 64.  (A call that is to withhold copies goes to the kernel that makes them.)
@@ -546,7 +546,7 @@ bool short_and_narrow(const MixParams& p)
 }
 
 // Sequences are cut into as many segments as take the least time by this count, in microseconds: a round of CTAs takes 6 to begin and end with and
-// for each 128 tokens, as measured, on the tensor cores 4 (2.8 to 4.7); in fp32 37, or with up to 64 columns, where two CTAs share an SM, 21 for one
+// for each 128 tokens, as measured, on the tensor cores 4 (2.5 for heads of 64, 4.3 of 128); in fp32 37, or with up to 64 columns, where two CTAs share an SM, 21 for one
 // and 35 for both; the segments' own sums, made first, 0.6 of that; joining them 6.
 void plan_mix(MixParams* prm)
 {

@@ -22,7 +22,8 @@
 // rounded to bf16, two.  (One, whose rounding is then as large as those of P o D and W, took dq and dk of heads of 128 from 2.3e-3 to 2.7e-3 of
 // their norm off.)
 //
-// 2 x 8 sequences of 2048 tokens x 16 x 128: 138 us forward, 387 backward (a CTA: 6.8 us and 4.7 for every chunk; with heads of 64, 5.3 and 2.8).
+// 2 x 8 sequences of 2048 tokens x 16 x 128: 145 us forward, 395 backward (a CTA: some 7 us and 4.3 for every chunk; with heads of 64, 2.5).  Parts that go with
+// infinities, too (rps_mix.cuh), are 4 % of the latter; with parts that were zero where the rest was, and made NaN of one, 139 and 379.
 // What a chunk takes is this kernel's own instructions and the way from one role to the next, not the tensor cores (a fifth) or memory.
 #include "rps_mix.cuh"
 #include "rps_tensor.cuh"
