@@ -342,7 +342,8 @@ int check_distil(const rps_distil_desc* d, rps_lce_desc* lce)
     if (d->top > RPS_MAX_TOP) return fail(RPS_ELIMIT, "top = %lld; up to %d logits of a token are possible", (long long)d->top, (int)RPS_MAX_TOP);
     if (d->n * d->tokens >= 1ll << 31) return fail(RPS_EINVAL, "n * tokens = %lld", (long long)(d->n * d->tokens));
     // lse is one fp32 number, whose rounding 1 / temperature magnifies, and temperature^2 that of the loss's logarithms
-    if (!(d->temperature >= 0.01 && d->temperature <= 100.0)) return fail(RPS_EINVAL, "temperature = %g; 0.01..100 are possible", d->temperature);
+    // (compared as fp32, where 0.01 is a little less)
+    if (!((float)d->temperature >= 0.01f && (float)d->temperature <= 100.0f)) return fail(RPS_EINVAL, "temperature = %g; 0.01..100 are possible", d->temperature);
     return RPS_OK;
 }
 
