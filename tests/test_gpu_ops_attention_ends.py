@@ -17,15 +17,15 @@ def kind(t):
 
 @pytest.mark.parametrize("mixed", [False, True])
 @pytest.mark.parametrize("T,H,K,W", [(400, 3, 64, 64), (400, 3, 128, 128), (3000, 2, 40, 72), (180, 3, 33, 31), (120, 3, 100, 127), (400, 3, 20, 77)])
-def test_an_infinity_goes_through_states(ops, T, H, K, W, mixed):  # noqa: F811
+def test_an_infinity_goes_through_states(ops, T, H, K, W, mixed, dtype="bf16"):  # noqa: F811
     """One infinity in each of several heads of sequences, of operands of one sign or of both.  States, and results that lie in other chunks, are finite,
     infinite or NaN as the definition's; in its own chunk what the definition makes infinite or NaN is one of these; all other heads keep their bits.
     Sequences for the tensor cores' both kernels, in segments, and by way of copies."""
     n, B, t = 1, 6, T // 2 if T < 1000 else 2100
-    x = inputs("bf16", n, B, T, H, K, W, seed=T + K)
+    x = inputs(dtype, n, B, T, H, K, W, seed=T + K)
     x["log_decay"].fill_(-0.02)
     for name in ("q", "k", "v", "dout"):
-        x[name] = torch.where(x[name] == 0, 1.0, x[name]).to(torch.bfloat16)
+        x[name] = torch.where(x[name] == 0, torch.ones_like(x[name]), x[name])
     if not mixed:
         x = {name: a if name == "log_decay" else a.abs() for name, a in x.items()}
     clean = run(ops, x, 0.5)
@@ -53,6 +53,12 @@ def test_an_infinity_goes_through_states(ops, T, H, K, W, mixed):  # noqa: F811
     # one of q is in its own token's result alone
     rows = torch.arange(T, device="cuda") != t
     assert torch.equal(got["out"][0, 2, rows, 0], clean["out"][0, 2, rows, 0]) and torch.equal(got["state"][0, 2, 0], clean["state"][0, 2, 0])
+
+
+@pytest.mark.parametrize("T,H,K,W", [(400, 3, 64, 64), (3000, 2, 40, 72), (180, 3, 33, 31)])
+def test_an_infinity_goes_through_states_in_fp32(ops, T, H, K, W):  # noqa: F811
+    for mixed in (False, True):
+        test_an_infinity_goes_through_states(ops, T, H, K, W, mixed, "f32")
 
 
 @pytest.mark.parametrize("backward", [False, True])
@@ -114,3 +120,23 @@ def test_short_sequences_of_narrow_heads_at_any_address(ops, n, B, T, H, K, W): 
         y[name] = room.copy_(x[name])
     got = run(ops, y, 0.3)
     assert all(torch.equal(got[name], want[name]) for name in want)
+
+
+def test_offsets_past_32_bits_in_short_sequences(ops):  # noqa: F811
+    """2^31 elements and more in every tensor, states among them.  Heads that forget at once: each result is its own token's."""
+    B, T, H, D = 262_400, 64, 2, 64
+    x = torch.zeros(B, T, H, D, dtype=torch.bfloat16, device="cuda")
+    tail = torch.randn(T, H, D, device="cuda").bfloat16()
+    x[-1] = tail
+    never = torch.full((H,), float("-inf"), device="cuda")
+    t = tail.double()
+    want = t.square().sum(-1, keepdim=True) * t
+    last = t[-1, :, :, None] * t[-1, :, None, :]
+    out, state = ops.linear_attention_forward(x, x, x, never, scale=1.0)
+    assert state.numel() > 2 ** 31 and not out[:-1].any() and (out[-1] - want).norm() <= 5e-3 * want.norm()
+    assert not state[:-1].any() and (state[-1] - last).norm() <= 5e-6 * last.norm()
+    del out, state
+    dq, dk, dv, first = ops.linear_attention_backward(x, None, x, x, x, never, scale=1.0)
+    for grad in (dq, dk, dv):
+        assert not grad[:-1].any() and (grad[-1] - want).norm() <= 5e-3 * want.norm()
+    assert not first.any()
