@@ -15,20 +15,29 @@ __device__ __forceinline__ double power(float log_decay, int64_t exponent)
     return exp((double)fmaxf(log_decay, -1e4f) * (double)exponent);
 }
 
-// The upper halves of two fp32 values as a word of bf16, and what they leave (taken from infinity or NaN: NaN).
-__device__ __forceinline__ Pair cut(const Pair& v, uint32_t& word)
+// The upper halves of two fp32 values as a word of bf16, and these less zero.
+__device__ __forceinline__ Pair upper_halves(const Pair& v, uint32_t& word)
 {
     float lo, hi;
     v.get(lo, hi);
     word = __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x7632);
-    return v + Pair(__uint_as_float((__float_as_uint(lo) & 0xFFFF0000u) ^ 0x80000000u), __uint_as_float((__float_as_uint(hi) & 0xFFFF0000u) ^ 0x80000000u));
+    return Pair(__uint_as_float((__float_as_uint(lo) & 0xFFFF0000u) ^ 0x80000000u), __uint_as_float((__float_as_uint(hi) & 0xFFFF0000u) ^ 0x80000000u));
 }
 
-// Two fp32 values as bf16 parts, as words: 8 of the 24 bits at a time, cut off, so three parts add up to the value exactly and have its sign.
-// Parts that would be zero are 2^-50 of the value, which changes no sum (it is below half of a last place of any part that is not zero, and 2^-26 of one
-// of the value's), so that an infinity of the other operand meets none that is zero where the value is not: infinity times a number is infinity.
-// What is itself infinite or NaN leaves NaN behind the first part (keep_infinities).
-__device__ __forceinline__ Pair next_part(const Pair& value, const Pair& rest, uint32_t& word) { return cut(fma(value, Pair(0x1p-50f), rest), word); }
+// The largest fp32 value below a positive one (0 of 0), as a factor makes it.
+constexpr float kBelow = 0x1.fffffep-1f;
+
+// Two products v * factor as three bf16 parts each, as words: 8 bits at a time, which add up to the product but for 2^-24 of it.  `below`: factor * kBelow.
+// All parts have the product's sign, and none is zero unless it is: the first is cut off from a little less than the product, so that something is left,
+// and of what the second leaves 2^-24 of it are left in any case (2^-31 of the product).  So an infinity of the other operand meets no zero: infinity times a
+// number is infinity.  What is itself infinite or NaN has NaN as its second and third part (keep_infinities).
+__device__ __forceinline__ void cut_in_parts(const Pair& v, const Pair& factor, const Pair& below, uint32_t& first, uint32_t& second, uint32_t& third)
+{
+    const Pair rest = fma(v, factor, upper_halves(v * below, first));
+    float lo, hi;
+    fma(upper_halves(rest, second), Pair(kBelow), rest).get(lo, hi);
+    third = two_bf16(lo, hi);
+}
 
 // Of the exponents of two bf16 values those that are all ones, as the sign bit of each half.
 __device__ __forceinline__ uint32_t has_infinite_exponent(uint32_t word) { return ((word & 0x7F807F80u) + 0x00800080u) & 0x80008000u; }

@@ -79,8 +79,8 @@ struct Tile {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             uint32_t word[3];
-            const Pair scaled = Pair(__uint_as_float(r[i] << 16), __uint_as_float(r[i] & 0xFFFF0000u)) * Pair(factor[i / 2 * 2], factor[i / 2 * 2 + 1]);
-            next_part(scaled, next_part(scaled, cut(scaled, word[0]), word[1]), word[2]);
+            const Pair scale(factor[i / 2 * 2], factor[i / 2 * 2 + 1]);
+            cut_in_parts(Pair(__uint_as_float(r[i] << 16), __uint_as_float(r[i] & 0xFFFF0000u)), scale, scale * Pair(kBelow), word[0], word[1], word[2]);
             word[1] = keep_infinities(word[0], word[1]), word[2] = keep_infinities(word[0], word[2]);
 #pragma unroll
             for (int q = 0; q < 3; ++q) a.part[q][i] = word[q];

@@ -22,8 +22,8 @@
 // rounded to bf16, two.  (One, whose rounding is then as large as those of P o D and W, took dq and dk of heads of 128 from 2.3e-3 to 2.7e-3 of
 // their norm off.)
 //
-// 2 x 8 sequences of 2048 tokens x 16 x 128: 145 us forward, 395 backward (a CTA: some 7 us and 4.3 for every chunk; with heads of 64, 2.5).  Parts that go with
-// infinities, too (rps_mix.cuh), are 4 % of the latter; with parts that were zero where the rest was, and made NaN of one, 139 and 379.
+// 2 x 8 sequences of 2048 tokens x 16 x 128: 143 us forward, 388 backward (a CTA: some 7 us and 4.3 for every chunk; with heads of 64, 2.5).  That parts go with
+// infinities, too (rps_mix.cuh), is 2 % of both.
 // What a chunk takes is this kernel's own instructions and the way from one role to the next, not the tensor cores (a fifth) or memory.
 #include "rps_mix.cuh"
 #include "rps_tensor.cuh"
@@ -511,6 +511,7 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
             const uint32_t from = row_at + places.y + s * y_bytes, to = row_at + places.part + (OWN ? s * 3 * y_bytes : 0);
             const uint32_t first_to = OWN ? to : from, second_to = to + (OWN ? y_bytes : 0);
             const Pair factor(term.update_scale * control.powers[reversed ? max(row + 1 - first, 0) : kC - 1 - row]);
+            const Pair below = factor * Pair(kBelow);
             uint32_t odd = 0;
 #pragma unroll
             for (int q = 0; q < kPieces; ++q) {
@@ -521,8 +522,7 @@ __global__ void __launch_bounds__(kThreads, 1) rps_mix_tensor_kernel(const __gri
                 uint32_t part[3][4];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const Pair scaled = v[j] * factor;
-                    next_part(scaled, next_part(scaled, cut(scaled, part[0][j]), part[1][j]), part[2][j]);
+                    cut_in_parts(v[j], factor, below, part[0][j], part[1][j], part[2][j]);
                     odd |= part[2][j];
                 }
                 third[q] = make_uint4(part[2][0], part[2][1], part[2][2], part[2][3]);
